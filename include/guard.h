@@ -20,6 +20,10 @@
  * Section 5), and the ledger calls (persistence kept per indicator, ranking by the
  * score averaged over the window, recurrence of flag episodes as in Section 7).
  *
+ * What a sweep has its GPUs run stands at the end: the operators on both sides of a
+ * language model's vocabulary (gd_embed, gd_vocab_loss, gd_adamw and the gradients),
+ * which make one training step of the job's own kind and repeat bit for bit.
+ *
  * The paper states the decision in words only.  The estimators and constants
  * used here (median / MAD x 1.4826 / threshold 3.5 / k-of-W / scaled node sum)
  * are the defaults written into gd_config below.
@@ -374,6 +378,157 @@ gd_status gd_ledger_flags(gd_handle h, uint8_t* d_rank_pmask, uint8_t* d_rank_pf
  * k == 0 selects the configured default; k > N is GD_ERR_INVALID_ARG.
  */
 gd_status gd_topk_nodes_mean(gd_handle h, uint32_t k, int32_t* d_idx, uint64_t* d_key, void* stream);
+
+/*
+ * The operators of a sweep's own training step (Section 5, "Single-Node Sweep": sustained
+ * throughput under work like the job's).  They load three parts of a GPU -- scattered rows
+ * of a large table, the matrix cores, the memory's streams -- and give the same bits for
+ * the same inputs on every pass and every GPU, so that a pass that differs is a fault.
+ * All of them are independent of the handle's configuration and state (the handle keeps
+ * the text of the last error), take caller-owned device memory, enqueue on `stream` and
+ * can be captured into a graph.  Sums are held in fp32; a result in a 16-bit type is rounded
+ * once, to nearest even.
+ */
+typedef enum {
+    GD_F32 = 0,
+    GD_BF16 = 1,
+    GD_F16 = 2,
+    GD_I32 = 3,
+    GD_I64 = 4,
+    GD_E4M3 = 5 /* the 8-bit states of gd_adamw */
+} gd_dtype;
+
+/* A matrix in device memory: row r begins at element r * stride, its cols elements are next to
+ * each other.  stride >= cols; the pointer is aligned to its element.  A list (tokens, targets)
+ * has cols = 1, with any stride.  A matrix without elements may have a null pointer. */
+typedef struct gd_matrix {
+    void* d_data;
+    uint64_t rows, cols, stride;
+    uint32_t dtype;    /* gd_dtype */
+    uint32_t reserved; /* 0 */
+} gd_matrix;
+
+#define GD_MAX_TOKENS 16777216u /* rows of a call: 2^24 */
+#define GD_MAX_VOCAB 16777216u
+#define GD_MAX_WIDTH 65536u
+
+/*
+ * Embedding lookup: out[i] = round(scale * weight[tokens[i]]).
+ *   weight [vocab][width] in   f32, bf16 or f16
+ *   tokens [n][1]         in   i32 or i64; a negative token is padding and gives a row of zeros;
+ *                              one that is no row of weight gives a row of NaN
+ *   out    [n][width]     out  of the type of weight
+ */
+gd_status gd_embed(gd_handle h, const gd_matrix* weight, const gd_matrix* tokens, float scale,
+                   const gd_matrix* out, void* stream);
+
+/*
+ * Its gradient: weight_grad[v] = round(scale * sum of out_grad[i] over the i with tokens[i] == v),
+ * summed in an order that depends on the tokens alone (they are sorted, equal ones in order of
+ * their positions).  Negative tokens and those that are no row have no part in it; the rows of
+ * out_grad that they stand at are not read.
+ *   accumulate != 0: weight_grad[v] = round(weight_grad[v] + scale * sum) instead, for tied weights and
+ *   gradients gathered over several calls; rows without a token are then not touched
+ *   (without it they become zeros).
+ *   out_grad [n][width] in, f32, bf16 or f16; weight_grad [vocab][width] of the same type
+ *   d_work: gd_embed_grad_work_bytes(n, vocab, width) bytes, 256-byte aligned
+ */
+size_t gd_embed_grad_work_bytes(uint64_t n, uint64_t vocab, uint64_t width);
+gd_status gd_embed_grad(gd_handle h, const gd_matrix* out_grad, const gd_matrix* tokens, float scale,
+                        int32_t accumulate, const gd_matrix* weight_grad, void* d_work, size_t work_bytes,
+                        void* stream);
+
+/*
+ * Softmax cross entropy of hidden states projected onto a vocabulary, in pieces of the
+ * vocabulary: the logits l[i][v] = logit_scale * <hidden[i], weight[v]> are never kept.
+ *   hidden  [n][width]     in   bf16 or f16
+ *   weight  [vocab][width] in   of the same type
+ *   targets [n][1]         in   i32 or i64; a negative target leaves its row out (loss 0); a target
+ *                               that is no row of weight makes the row's loss NaN
+ *   d_loss  [n] f32 out  lse[i] - l[i][targets[i]]
+ *   d_lse   [n] f32 out  log(sum over v of exp(l[i][v])), for rows left out too
+ *   d_mean  [2] f32 out  the sum of the losses over the larger of 1 and the number of rows not left
+ *                        out; that number
+ *   d_work: gd_vocab_loss_work_bytes(n, vocab, width, 0) bytes, 256-byte aligned
+ * n == 0 gives a mean of 0 over 0 rows.
+ */
+size_t gd_vocab_loss_work_bytes(uint64_t n, uint64_t vocab, uint64_t width, int32_t with_grad);
+gd_status gd_vocab_loss(gd_handle h, const gd_matrix* hidden, const gd_matrix* weight,
+                        const gd_matrix* targets, float logit_scale, float* d_loss, float* d_lse,
+                        float* d_mean, void* d_work, size_t work_bytes, void* stream);
+
+/*
+ * Its gradients, from the d_lse and d_mean that gd_vocab_loss left for the same inputs.  With
+ *   c[i] = d_grad_rows[i] + d_grad_mean[0] / max(1, d_mean[1])   (a null pointer counts as zeros,
+ *          at least one of the two is there; 0 for a row left out or whose target is no row)
+ *   G[i][v] = c[i] * (exp(l[i][v] - lse[i]) - (v == targets[i]))
+ *   hidden_grad = logit_scale * G weight          [n][width]
+ *   weight_grad = logit_scale * transposed G hidden  [vocab][width]
+ * both of the type of hidden; either may be null.  G is rounded to that type for the matrix
+ * cores (relative to the largest c in f16, so that no gradient underflows for being a mean's).
+ * Rows with c[i] == 0 have no part in weight_grad, whatever their hidden state holds.
+ *   d_work: gd_vocab_loss_work_bytes(n, vocab, width, 1) bytes, 256-byte aligned
+ */
+gd_status gd_vocab_loss_grad(gd_handle h, const gd_matrix* hidden, const gd_matrix* weight,
+                             const gd_matrix* targets, float logit_scale, const float* d_lse,
+                             const float* d_mean, const float* d_grad_mean, const float* d_grad_rows,
+                             const gd_matrix* hidden_grad, const gd_matrix* weight_grad, void* d_work,
+                             size_t work_bytes, void* stream);
+
+/*
+ * AdamW over many tensors in one launch.  For each element, every operation rounded to fp32 in
+ * this order (the factors in brackets worked out in double and rounded once):
+ *   g = grad * grad_scale                       (no multiplication where d_grad_scale is null)
+ *   m = m * [beta1] + g * [1 - beta1]
+ *   v = v * [beta2] + (g * [1 - beta2]) * g;    r = sqrt(v)
+ *   p = param * [1 - lr * lr_scale * weight_decay]
+ *       - (m * [lr * lr_scale / (1 - beta1^step)]) / (r * [1 / sqrt(1 - beta2^step)] + [eps])
+ * param = round(p) and, where d_copy is given, copy = round(p).
+ *
+ * State types: GD_F32 keeps m and v.  GD_E4M3 keeps m and r as e4m3 codes (1 byte) in blocks of
+ * GD_STATE_BLOCK elements with a power of two each: 2^(e - 127) for a byte e of 1..254 such that
+ * the block's largest magnitude is at most 448 of it and, for e > 1, more than 224; e = 0 for a block
+ * of zeros; e = 255 for a block that an infinity or a NaN came into, which reads as NaN from then
+ * on.  Codes are rounded with a dither that a hash of (seed, element's index) gives, so that a mean
+ * that moves by less than half a code's step at a time still moves on average; a root above 0 keeps
+ * a code above 0, since a mean over a root of zero would be a step without bound.
+ */
+#define GD_STATE_BLOCK 256u
+
+typedef struct gd_adamw_tensor {
+    void* d_param;
+    const void* d_grad;
+    void* d_m;          /* f32, or e4m3 codes */
+    void* d_v;          /* f32 v, or e4m3 codes of r */
+    uint8_t* d_m_exp;   /* one byte per GD_STATE_BLOCK elements, for GD_E4M3 alone */
+    uint8_t* d_v_exp;
+    void* d_copy;       /* or null */
+    uint64_t n;         /* elements, next to each other in every array */
+    uint64_t first_index; /* the element index that the dither counts from (a shard's offset) */
+    double lr_scale, weight_decay;
+    uint32_t param_type, grad_type; /* f32, bf16 or f16 */
+    uint32_t copy_type;             /* bf16 or f16; read where d_copy is given */
+    uint32_t state_type;            /* GD_F32 or GD_E4M3 */
+} gd_adamw_tensor;
+
+typedef struct gd_adamw_config {
+    uint32_t struct_size;  /* = sizeof(gd_adamw_config) */
+    uint32_t seed;         /* of the dither; another one for each step, for instance the step */
+    double lr, beta1, beta2, eps;
+    uint64_t step;         /* 1 for the first update */
+} gd_adamw_config;
+
+/* What the launch reads about its tensors, as bytes that the caller copies to the device once
+ * (256-byte aligned there) and keeps as long as the tensors stay where they are: gd_adamw_table_bytes
+ * of them (0 where the list is refused), written to host memory by gd_adamw_fill_table. */
+size_t gd_adamw_table_bytes(gd_handle h, const gd_adamw_tensor* tensors, uint32_t n_tensors);
+gd_status gd_adamw_fill_table(gd_handle h, const gd_adamw_tensor* tensors, uint32_t n_tensors,
+                              void* host_table, size_t bytes);
+
+/* One update of all tensors of a table.  d_grad_scale: one f32 in device memory that every gradient is
+ * multiplied by (clipping, loss scaling), or null; where it is infinite or NaN nothing is written. */
+gd_status gd_adamw(gd_handle h, const void* d_table, size_t table_bytes, const gd_adamw_config* cfg,
+                   const float* d_grad_scale, void* stream);
 
 /*
  * NOT part of the detector's contract -- a diagnostic for benchmarks, exported so that

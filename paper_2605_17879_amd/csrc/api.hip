@@ -10,6 +10,7 @@
 
 #include "../../include/guard.h"
 #include "gd_internal.h"
+#include "gd_operators.h"
 
 struct gd_handle_s {
     gd_config cfg;
@@ -77,6 +78,89 @@ gd_status fail(gd_handle h, gd_status st, const std::string& msg) {
 
 gd_status hip_fail(gd_handle h, hipError_t e, const char* what) {
     return fail(h, GD_ERR_HIP, std::string(what) + ": " + hipGetErrorString(e));
+}
+
+// ---- arguments of the operators of a training step ----
+
+// Rows are addressed by 32-bit byte offsets from a tile's first one.
+constexpr uint64_t MAX_STRIDE = 1u << 22;
+
+uint32_t bytes_of(uint32_t type) { return type == GD_F32 || type == GD_I32 ? 4 : type == GD_I64 ? 8 : type == GD_E4M3 ? 1 : 2; }
+bool is_float(uint32_t type) { return type == GD_F32 || type == GD_BF16 || type == GD_F16; }
+
+// What is wrong with a matrix of rows x cols elements, or null.
+const char* bad_matrix(const gd_matrix* m, uint64_t rows, uint64_t cols) {
+    if (!m) return "null matrix";
+    if (m->reserved != 0) return "reserved field of a matrix is not 0";
+    if (m->rows != rows || m->cols != cols) return "sizes of the matrices do not fit each other";
+    if (rows == 0 || cols == 0) return nullptr;
+    if (!m->d_data) return "null pointer of a matrix";
+    if (m->stride < cols) return "stride below the row's length";
+    if (m->stride > MAX_STRIDE && cols > 1) return "stride above 2^22 elements";
+    if (m->stride > (1ull << 40)) return "stride above 2^40 elements";
+    if ((uintptr_t)m->d_data % bytes_of(m->dtype)) return "pointer of a matrix not aligned to its element";
+    return nullptr;
+}
+
+// The same for a list of tokens or targets.
+const char* bad_tokens(const gd_matrix* m) {
+    if (!m) return "null matrix";
+    if (m->dtype != GD_I32 && m->dtype != GD_I64) return "tokens must be i32 or i64";
+    if (m->cols != 1) return "tokens must have one column";
+    if (m->rows > GD_MAX_TOKENS) return "more than 2^24 tokens";
+    return bad_matrix(m, m->rows, 1);
+}
+
+gd_token_list tokens_of(const gd_matrix* m) {
+    return gd_token_list{m->d_data, m->stride, (uint32_t)m->rows, m->dtype == GD_I64 ? 1u : 0u};
+}
+
+gd_status invalid(gd_handle h, const char* call, const char* what) {
+    return fail(h, GD_ERR_INVALID_ARG, std::string(call) + ": " + what);
+}
+
+// The work area of a call that needs one.
+gd_status bad_work(gd_handle h, const char* call, const void* d_work, size_t have, size_t need) {
+    if (need && !d_work) return invalid(h, call, "null work area");
+    if ((uintptr_t)d_work & 255) return invalid(h, call, "work area not 256-byte aligned");
+    if (have < need) return fail(h, GD_ERR_BUFFER_TOO_SMALL, std::string(call) + ": work area too small");
+    return GD_OK;
+}
+
+// Sizes and types of a projection onto a vocabulary, or what is wrong with them.
+const char* bad_projection(const gd_matrix* hidden, const gd_matrix* weight, const gd_matrix* targets) {
+    if (const char* e = bad_tokens(targets)) return e;
+    if (!hidden || !weight) return "null matrix";
+    if (hidden->dtype != weight->dtype) return "hidden and weight differ in type";
+    if (weight->rows == 0 || weight->cols == 0) return "weight has no elements";
+    if (weight->rows > GD_MAX_VOCAB) return "vocabulary above 2^24 rows";
+    if (weight->cols > GD_MAX_WIDTH) return "width above 65536";
+    if (const char* e = bad_matrix(weight, weight->rows, weight->cols)) return e;
+    return bad_matrix(hidden, targets->rows, weight->cols);
+}
+
+// What is wrong with one tensor of an update, or null.
+const char* bad_tensor(const gd_adamw_tensor& t) {
+    if (!is_float(t.param_type) || !is_float(t.grad_type)) return "param and grad must be f32, bf16 or f16";
+    if (t.state_type != GD_F32 && t.state_type != GD_E4M3) return "states must be f32 or e4m3";
+    if (t.d_copy && t.copy_type != GD_BF16 && t.copy_type != GD_F16) return "a copy must be bf16 or f16";
+    if (!(isfinite(t.lr_scale) && isfinite(t.weight_decay))) return "lr_scale and weight_decay must be finite";
+    if (t.n > (1ull << 42)) return "tensor of more than 2^42 elements";
+    if (t.n == 0) return nullptr;
+    if (!t.d_param || !t.d_grad || !t.d_m || !t.d_v) return "null pointer of a tensor";
+    if (t.state_type == GD_E4M3 && (!t.d_m_exp || !t.d_v_exp)) return "8-bit states need their exponents";
+    const uint32_t state = bytes_of(t.state_type);
+    if ((uintptr_t)t.d_param % bytes_of(t.param_type) || (uintptr_t)t.d_grad % bytes_of(t.grad_type) ||
+        (uintptr_t)t.d_m % state || (uintptr_t)t.d_v % state || (uintptr_t)t.d_copy % 2)
+        return "pointer of a tensor not aligned to its element";
+    return nullptr;
+}
+
+const char* bad_tensors(const gd_adamw_tensor* t, uint32_t n) {
+    if (n && !t) return "null list of tensors";
+    for (uint32_t i = 0; i < n; ++i)
+        if (const char* e = bad_tensor(t[i])) return e;
+    return nullptr;
 }
 
 }  // namespace
@@ -492,6 +576,163 @@ gd_status gd_probe_read(gd_handle h, const float* d_x, uint64_t n_bytes, uint32_
         return fail(h, GD_ERR_INVALID_ARG, "gd_probe_read: misaligned pointer");
     hipError_t e = gd_launch_read_probe(d_x, n_bytes, d_sink, static_cast<hipStream_t>(stream));
     if (e != hipSuccess) return hip_fail(h, e, "gd_probe_read");
+    return GD_OK;
+}
+
+gd_status gd_embed(gd_handle h, const gd_matrix* weight, const gd_matrix* tokens, float scale, const gd_matrix* out, void* stream) {
+    if (!h) return GD_ERR_INVALID_ARG;
+    if (const char* e = bad_tokens(tokens)) return invalid(h, "gd_embed", e);
+    if (!weight || !out) return invalid(h, "gd_embed", "null matrix");
+    if (!is_float(weight->dtype)) return fail(h, GD_ERR_UNSUPPORTED, "gd_embed: weight must be f32, bf16 or f16");
+    if (out->dtype != weight->dtype) return invalid(h, "gd_embed", "out and weight differ in type");
+    if (weight->rows > GD_MAX_VOCAB) return invalid(h, "gd_embed", "vocabulary above 2^24 rows");
+    if (weight->cols > GD_MAX_WIDTH) return invalid(h, "gd_embed", "width above 65536");
+    if (const char* e = bad_matrix(weight, weight->rows, weight->cols)) return invalid(h, "gd_embed", e);
+    if (const char* e = bad_matrix(out, tokens->rows, weight->cols)) return invalid(h, "gd_embed", e);
+    gd_embed_args a;
+    a.weight = weight->d_data; a.weight_stride = weight->stride;
+    a.out = out->d_data; a.out_stride = out->stride;
+    a.tokens = tokens_of(tokens);
+    a.vocab = (uint32_t)weight->rows; a.width = (uint32_t)weight->cols; a.dtype = weight->dtype; a.scale = scale;
+    hipError_t e = gd_launch_embed(a, static_cast<hipStream_t>(stream));
+    if (e != hipSuccess) return hip_fail(h, e, "gd_embed");
+    return GD_OK;
+}
+
+size_t gd_embed_grad_work_bytes(uint64_t n, uint64_t vocab, uint64_t width) {
+    if (n > GD_MAX_TOKENS || vocab > GD_MAX_VOCAB || width > GD_MAX_WIDTH) return 0;
+    return gd_embed_grad_work(n, width);
+}
+
+gd_status gd_embed_grad(gd_handle h, const gd_matrix* out_grad, const gd_matrix* tokens, float scale, int32_t accumulate,
+                        const gd_matrix* weight_grad, void* d_work, size_t work_bytes, void* stream) {
+    if (!h) return GD_ERR_INVALID_ARG;
+    if (const char* e = bad_tokens(tokens)) return invalid(h, "gd_embed_grad", e);
+    if (!out_grad || !weight_grad) return invalid(h, "gd_embed_grad", "null matrix");
+    if (!is_float(out_grad->dtype)) return fail(h, GD_ERR_UNSUPPORTED, "gd_embed_grad: gradients must be f32, bf16 or f16");
+    if (out_grad->dtype != weight_grad->dtype) return invalid(h, "gd_embed_grad", "the gradients differ in type");
+    if (weight_grad->rows > GD_MAX_VOCAB) return invalid(h, "gd_embed_grad", "vocabulary above 2^24 rows");
+    if (weight_grad->cols > GD_MAX_WIDTH) return invalid(h, "gd_embed_grad", "width above 65536");
+    if (const char* e = bad_matrix(weight_grad, weight_grad->rows, weight_grad->cols)) return invalid(h, "gd_embed_grad", e);
+    if (const char* e = bad_matrix(out_grad, tokens->rows, weight_grad->cols)) return invalid(h, "gd_embed_grad", e);
+    if (gd_status st = bad_work(h, "gd_embed_grad", d_work, work_bytes, gd_embed_grad_work(tokens->rows, weight_grad->cols))) return st;
+    gd_embed_grad_args a;
+    a.out_grad = out_grad->d_data; a.out_grad_stride = out_grad->stride;
+    a.weight_grad = weight_grad->d_data; a.weight_grad_stride = weight_grad->stride;
+    a.tokens = tokens_of(tokens);
+    a.vocab = (uint32_t)weight_grad->rows; a.width = (uint32_t)weight_grad->cols; a.dtype = out_grad->dtype;
+    a.accumulate = accumulate != 0; a.scale = scale;
+    a.work = static_cast<uint8_t*>(d_work);
+    hipError_t e = gd_launch_embed_grad(a, static_cast<hipStream_t>(stream));
+    if (e != hipSuccess) return hip_fail(h, e, "gd_embed_grad");
+    return GD_OK;
+}
+
+size_t gd_vocab_loss_work_bytes(uint64_t n, uint64_t vocab, uint64_t width, int32_t with_grad) {
+    if (n > GD_MAX_TOKENS || vocab < 1 || vocab > GD_MAX_VOCAB || width < 1 || width > GD_MAX_WIDTH) return 0;
+    return gd_vocab_loss_work(n, vocab, width, with_grad != 0);
+}
+
+gd_status gd_vocab_loss(gd_handle h, const gd_matrix* hidden, const gd_matrix* weight, const gd_matrix* targets, float logit_scale,
+                        float* d_loss, float* d_lse, float* d_mean, void* d_work, size_t work_bytes, void* stream) {
+    if (!h) return GD_ERR_INVALID_ARG;
+    if (const char* e = bad_projection(hidden, weight, targets)) return invalid(h, "gd_vocab_loss", e);
+    if (hidden->dtype != GD_BF16 && hidden->dtype != GD_F16)
+        return fail(h, GD_ERR_UNSUPPORTED, "gd_vocab_loss: hidden and weight must be bf16 or f16");
+    const uint64_t n = targets->rows;
+    if (!d_mean || (n && (!d_loss || !d_lse))) return invalid(h, "gd_vocab_loss", "null output");
+    if (((uintptr_t)d_loss & 3) || ((uintptr_t)d_lse & 3) || ((uintptr_t)d_mean & 3)) return invalid(h, "gd_vocab_loss", "misaligned output");
+    if (gd_status st = bad_work(h, "gd_vocab_loss", d_work, work_bytes, gd_vocab_loss_work(n, weight->rows, weight->cols, false))) return st;
+    gd_vocab_loss_args a;
+    a.hidden = hidden->d_data; a.hidden_stride = hidden->stride;
+    a.weight = weight->d_data; a.weight_stride = weight->stride;
+    a.targets = tokens_of(targets);
+    a.vocab = (uint32_t)weight->rows; a.width = (uint32_t)weight->cols; a.dtype = hidden->dtype; a.scale = logit_scale;
+    a.loss = d_loss; a.lse = d_lse; a.mean = d_mean;
+    a.work = static_cast<uint8_t*>(d_work);
+    hipError_t e = gd_launch_vocab_loss(a, static_cast<hipStream_t>(stream));
+    if (e != hipSuccess) return hip_fail(h, e, "gd_vocab_loss");
+    return GD_OK;
+}
+
+gd_status gd_vocab_loss_grad(gd_handle h, const gd_matrix* hidden, const gd_matrix* weight, const gd_matrix* targets,
+                             float logit_scale, const float* d_lse, const float* d_mean, const float* d_grad_mean,
+                             const float* d_grad_rows, const gd_matrix* hidden_grad, const gd_matrix* weight_grad, void* d_work,
+                             size_t work_bytes, void* stream) {
+    if (!h) return GD_ERR_INVALID_ARG;
+    const char* call = "gd_vocab_loss_grad";
+    if (const char* e = bad_projection(hidden, weight, targets)) return invalid(h, call, e);
+    if (hidden->dtype != GD_BF16 && hidden->dtype != GD_F16)
+        return fail(h, GD_ERR_UNSUPPORTED, "gd_vocab_loss_grad: hidden and weight must be bf16 or f16");
+    const uint64_t n = targets->rows;
+    if (!d_grad_mean && !d_grad_rows) return invalid(h, call, "no gradient of the loss");
+    if ((n && !d_lse) || (d_grad_mean && !d_mean)) return invalid(h, call, "null result of the loss");
+    if (((uintptr_t)d_lse & 3) || ((uintptr_t)d_mean & 3) || ((uintptr_t)d_grad_mean & 3) || ((uintptr_t)d_grad_rows & 3))
+        return invalid(h, call, "misaligned pointer");
+    if (hidden_grad) {
+        if (const char* e = bad_matrix(hidden_grad, n, weight->cols)) return invalid(h, call, e);
+        if (hidden_grad->dtype != hidden->dtype) return invalid(h, call, "the gradients must have the type of hidden");
+    }
+    if (weight_grad) {
+        if (const char* e = bad_matrix(weight_grad, weight->rows, weight->cols)) return invalid(h, call, e);
+        if (weight_grad->dtype != hidden->dtype) return invalid(h, call, "the gradients must have the type of hidden");
+    }
+    if (!hidden_grad && !weight_grad) return GD_OK;
+    if (gd_status st = bad_work(h, call, d_work, work_bytes, gd_vocab_loss_work(n, weight->rows, weight->cols, true))) return st;
+    gd_vocab_grad_args a;
+    a.hidden = hidden->d_data; a.hidden_stride = hidden->stride;
+    a.weight = weight->d_data; a.weight_stride = weight->stride;
+    a.targets = tokens_of(targets);
+    a.vocab = (uint32_t)weight->rows; a.width = (uint32_t)weight->cols; a.dtype = hidden->dtype; a.scale = logit_scale;
+    a.lse = d_lse; a.mean = d_mean; a.grad_mean = d_grad_mean; a.grad_rows = d_grad_rows;
+    a.hidden_grad = hidden_grad ? hidden_grad->d_data : nullptr; a.hidden_grad_stride = hidden_grad ? hidden_grad->stride : 0;
+    a.weight_grad = weight_grad ? weight_grad->d_data : nullptr; a.weight_grad_stride = weight_grad ? weight_grad->stride : 0;
+    a.work = static_cast<uint8_t*>(d_work);
+    hipError_t e = gd_launch_vocab_grad(a, static_cast<hipStream_t>(stream));
+    if (e != hipSuccess) return hip_fail(h, e, call);
+    return GD_OK;
+}
+
+size_t gd_adamw_table_bytes(gd_handle h, const gd_adamw_tensor* tensors, uint32_t n_tensors) {
+    if (!h) return 0;
+    if (const char* e = bad_tensors(tensors, n_tensors)) { invalid(h, "gd_adamw_table_bytes", e); return 0; }
+    const size_t bytes = gd_adamw_table(tensors, n_tensors, nullptr);
+    if (!bytes) invalid(h, "gd_adamw_table_bytes", "too many elements");
+    return bytes;
+}
+
+gd_status gd_adamw_fill_table(gd_handle h, const gd_adamw_tensor* tensors, uint32_t n_tensors, void* host_table, size_t bytes) {
+    if (!h) return GD_ERR_INVALID_ARG;
+    if (const char* e = bad_tensors(tensors, n_tensors)) return invalid(h, "gd_adamw_fill_table", e);
+    const size_t need = gd_adamw_table(tensors, n_tensors, nullptr);
+    if (!need) return invalid(h, "gd_adamw_fill_table", "too many elements");
+    if (!host_table || ((uintptr_t)host_table & 7)) return invalid(h, "gd_adamw_fill_table", "null or misaligned table");
+    if (bytes != need) return fail(h, GD_ERR_BUFFER_TOO_SMALL, "gd_adamw_fill_table: not gd_adamw_table_bytes bytes");
+    gd_adamw_table(tensors, n_tensors, host_table);
+    return GD_OK;
+}
+
+gd_status gd_adamw(gd_handle h, const void* d_table, size_t table_bytes, const gd_adamw_config* c, const float* d_grad_scale, void* stream) {
+    if (!h) return GD_ERR_INVALID_ARG;
+    if (!d_table || !c) return invalid(h, "gd_adamw", "null argument");
+    if (c->struct_size != sizeof(gd_adamw_config))
+        return fail(h, GD_ERR_BAD_CONFIG, "gd_adamw: struct_size does not match this library's gd_adamw_config");
+    if (((uintptr_t)d_table & 255) || ((uintptr_t)d_grad_scale & 3)) return invalid(h, "gd_adamw", "misaligned pointer");
+    if (table_bytes < 256 || (table_bytes & 255)) return invalid(h, "gd_adamw", "table_bytes is no table's size");
+    if (!(c->beta1 >= 0.0 && c->beta1 < 1.0 && c->beta2 >= 0.0 && c->beta2 < 1.0))
+        return fail(h, GD_ERR_BAD_CONFIG, "gd_adamw: beta1 and beta2 must be in [0, 1)");
+    if (!(isfinite(c->lr) && c->eps >= 0.0 && isfinite(c->eps))) return fail(h, GD_ERR_BAD_CONFIG, "gd_adamw: lr must be finite, eps finite and not negative");
+    if (c->step < 1) return fail(h, GD_ERR_BAD_CONFIG, "gd_adamw: step counts from 1");
+    gd_adamw_args a;
+    a.table = static_cast<const uint8_t*>(d_table); a.table_bytes = table_bytes; a.grad_scale = d_grad_scale;
+    a.lr = c->lr;
+    a.fbeta1 = (float)c->beta1; a.fbeta2 = (float)c->beta2;
+    a.one_beta1 = (float)(1.0 - c->beta1); a.one_beta2 = (float)(1.0 - c->beta2);
+    a.c1 = 1.0 - pow(c->beta1, (double)c->step);
+    a.inv_root_c2 = (float)(1.0 / sqrt(1.0 - pow(c->beta2, (double)c->step)));
+    a.eps = (float)c->eps; a.seed = c->seed;
+    hipError_t e = gd_launch_adamw(a, static_cast<hipStream_t>(stream));
+    if (e != hipSuccess) return hip_fail(h, e, "gd_adamw");
     return GD_OK;
 }
 

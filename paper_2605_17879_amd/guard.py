@@ -26,7 +26,12 @@ EXPORTS = ("gd_default_config", "gd_create", "gd_destroy", "gd_state_bytes", "gd
            "gd_topk_nodes", "gd_severity", "gd_sweep_score", "gd_probe_read", "gd_last_error",
            "gd_default_ledger_config", "gd_ledger_bytes", "gd_bind_ledger", "gd_update_ledger",
            "gd_ledger_flags", "gd_topk_nodes_mean", "gd_set_streaming_hints", "gd_apply_membership",
-           "gd_update_ledger_static", "gd_ledger_static_scratch_bytes")
+           "gd_update_ledger_static", "gd_ledger_static_scratch_bytes",
+           "gd_embed", "gd_embed_grad", "gd_embed_grad_work_bytes", "gd_vocab_loss", "gd_vocab_loss_grad",
+           "gd_vocab_loss_work_bytes", "gd_adamw", "gd_adamw_table_bytes", "gd_adamw_fill_table")
+
+F32, BF16, F16, I32, I64, E4M3 = range(6)      # gd_dtype
+STATE_BLOCK = 256                              # GD_STATE_BLOCK
 
 
 class GuardError(RuntimeError):
@@ -50,6 +55,26 @@ class _CLedgerConfig(ctypes.Structure):
     _fields_ = [("struct_size", ctypes.c_uint32), ("score_quant", ctypes.c_float),
                 ("recur_limit", ctypes.c_uint32), ("reserved", ctypes.c_uint32),
                 ("recur_horizon", ctypes.c_uint64)]
+
+
+class _CMatrix(ctypes.Structure):
+    _fields_ = [("d_data", ctypes.c_void_p), ("rows", ctypes.c_uint64), ("cols", ctypes.c_uint64),
+                ("stride", ctypes.c_uint64), ("dtype", ctypes.c_uint32), ("reserved", ctypes.c_uint32)]
+
+
+class _CAdamwTensor(ctypes.Structure):
+    _fields_ = [("d_param", ctypes.c_void_p), ("d_grad", ctypes.c_void_p), ("d_m", ctypes.c_void_p),
+                ("d_v", ctypes.c_void_p), ("d_m_exp", ctypes.c_void_p), ("d_v_exp", ctypes.c_void_p),
+                ("d_copy", ctypes.c_void_p), ("n", ctypes.c_uint64), ("first_index", ctypes.c_uint64),
+                ("lr_scale", ctypes.c_double), ("weight_decay", ctypes.c_double),
+                ("param_type", ctypes.c_uint32), ("grad_type", ctypes.c_uint32),
+                ("copy_type", ctypes.c_uint32), ("state_type", ctypes.c_uint32)]
+
+
+class _CAdamwConfig(ctypes.Structure):
+    _fields_ = [("struct_size", ctypes.c_uint32), ("seed", ctypes.c_uint32), ("lr", ctypes.c_double),
+                ("beta1", ctypes.c_double), ("beta2", ctypes.c_double), ("eps", ctypes.c_double),
+                ("step", ctypes.c_uint64)]
 
 
 def library_path() -> str:
@@ -114,6 +139,25 @@ def load_library() -> ctypes.CDLL:
     lib.gd_topk_nodes_mean.restype = ctypes.c_int
     lib.gd_apply_membership.argtypes = [vp, vp, u32, vp, vp]
     lib.gd_apply_membership.restype = ctypes.c_int
+    mat, sz, i32 = ctypes.POINTER(_CMatrix), ctypes.c_size_t, ctypes.c_int32
+    lib.gd_embed.argtypes = [vp, mat, mat, f32, mat, vp]
+    lib.gd_embed.restype = ctypes.c_int
+    lib.gd_embed_grad_work_bytes.argtypes = [u64, u64, u64]
+    lib.gd_embed_grad_work_bytes.restype = sz
+    lib.gd_embed_grad.argtypes = [vp, mat, mat, f32, i32, mat, vp, sz, vp]
+    lib.gd_embed_grad.restype = ctypes.c_int
+    lib.gd_vocab_loss_work_bytes.argtypes = [u64, u64, u64, i32]
+    lib.gd_vocab_loss_work_bytes.restype = sz
+    lib.gd_vocab_loss.argtypes = [vp, mat, mat, mat, f32, vp, vp, vp, vp, sz, vp]
+    lib.gd_vocab_loss.restype = ctypes.c_int
+    lib.gd_vocab_loss_grad.argtypes = [vp, mat, mat, mat, f32, vp, vp, vp, vp, mat, mat, vp, sz, vp]
+    lib.gd_vocab_loss_grad.restype = ctypes.c_int
+    lib.gd_adamw_table_bytes.argtypes = [vp, ctypes.POINTER(_CAdamwTensor), u32]
+    lib.gd_adamw_table_bytes.restype = sz
+    lib.gd_adamw_fill_table.argtypes = [vp, ctypes.POINTER(_CAdamwTensor), u32, vp, sz]
+    lib.gd_adamw_fill_table.restype = ctypes.c_int
+    lib.gd_adamw.argtypes = [vp, vp, sz, ctypes.POINTER(_CAdamwConfig), vp, vp]
+    lib.gd_adamw.restype = ctypes.c_int
     lib.gd_last_error.argtypes = [vp]
     lib.gd_last_error.restype = ctypes.c_char_p
     _lib = lib
@@ -378,3 +422,146 @@ class Detector:
     def topk_nodes_mean(self, k: int, tk: dict, stream=None):
         self._check(self.lib.gd_topk_nodes_mean(self.h, k, _p(tk["idx"]), _p(tk.get("key")),
                                                 self._stream(stream)))
+
+    # ---- the operators of a sweep's own training step ---------------------------------
+    def _type(self, t) -> int:
+        torch = self._torch
+        code = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16, torch.int32: I32,
+                torch.int64: I64}.get(t.dtype)
+        if code is None:
+            raise GuardError(4, f"tensors of {t.dtype} are not built")
+        return code
+
+    def _on_device(self, *tensors):
+        for t in tensors:
+            assert t is None or (t.is_cuda and (self.device.index is None or t.device == self.device)), \
+                f"a tensor is on {t.device}, the detector on {self.device}"
+
+    def _matrix(self, t) -> _CMatrix:
+        """t[rows][cols], rows any distance apart; a list t[n] is a matrix of one column."""
+        self._on_device(t)
+        assert t.dim() in (1, 2)
+        rows, cols = (t.shape[0], 1) if t.dim() == 1 else t.shape
+        assert t.dim() == 1 or cols <= 1 or t.stride(1) == 1, "the elements of a row must be next to each other"
+        # the distance to a row that is not there says nothing
+        stride = t.stride(0) if rows > 1 else max(cols, 1)
+        return _CMatrix(t.data_ptr(), rows, cols, stride, self._type(t), 0)
+
+    def _vector(self, t, n: int):
+        """The address of n f32 values next to each other, or None."""
+        if t is None:
+            return None
+        self._on_device(t)
+        assert t.dtype == self._torch.float32 and t.is_contiguous() and t.numel() == n
+        return t.data_ptr()
+
+    def _bytes(self, n: int):
+        return self._torch.empty(n, dtype=self._torch.uint8, device=self.device)
+
+    def embed(self, weight, tokens, out, scale: float = 1.0, stream=None):
+        """out[i] = scale * weight[tokens[i]]; zeros for a negative token."""
+        w, t, o = self._matrix(weight), self._matrix(tokens), self._matrix(out)
+        self._check(self.lib.gd_embed(self.h, w, t, scale, o, self._stream(stream)))
+
+    def embed_grad_work_bytes(self, n: int, vocab: int, width: int) -> int:
+        return int(self.lib.gd_embed_grad_work_bytes(n, vocab, width))
+
+    def alloc_embed_grad_work(self, n: int, vocab: int, width: int):
+        return self._bytes(self.embed_grad_work_bytes(n, vocab, width))
+
+    def embed_grad(self, out_grad, tokens, weight_grad, work, scale: float = 1.0, accumulate: bool = False,
+                   stream=None):
+        """weight_grad[v] = (its old value, with accumulate) + scale * sum of out_grad[i] over tokens[i] == v."""
+        g, t, w = self._matrix(out_grad), self._matrix(tokens), self._matrix(weight_grad)
+        self._on_device(work)
+        self._check(self.lib.gd_embed_grad(self.h, g, t, scale, int(accumulate), w, work.data_ptr(),
+                                           work.numel() * work.element_size(), self._stream(stream)))
+
+    def alloc_vocab_loss(self, n: int) -> dict:
+        """Outputs of vocab_loss: loss[n], lse[n] and mean[2] (the mean and the rows in it)."""
+        e = lambda k: self._torch.empty(k, dtype=self._torch.float32, device=self.device)
+        return dict(loss=e(n), lse=e(n), mean=e(2))
+
+    def vocab_loss_work_bytes(self, n: int, vocab: int, width: int, grad: bool = False) -> int:
+        return int(self.lib.gd_vocab_loss_work_bytes(n, vocab, width, int(grad)))
+
+    def alloc_vocab_loss_work(self, n: int, vocab: int, width: int, grad: bool = False):
+        """A work area for vocab_loss and, with grad, for vocab_loss_grad too."""
+        return self._bytes(self.vocab_loss_work_bytes(n, vocab, width, grad))
+
+    def vocab_loss(self, hidden, weight, targets, out: dict, work, logit_scale: float = 1.0, stream=None):
+        """Cross entropy of softmax(logit_scale * hidden weight^T) against targets (negative: left out)."""
+        h, w, t = self._matrix(hidden), self._matrix(weight), self._matrix(targets)
+        n = targets.shape[0]
+        self._on_device(work)
+        self._check(self.lib.gd_vocab_loss(
+            self.h, h, w, t, logit_scale, self._vector(out["loss"], n), self._vector(out["lse"], n),
+            self._vector(out["mean"], 2), work.data_ptr(), work.numel() * work.element_size(), self._stream(stream)))
+
+    def vocab_loss_grad(self, hidden, weight, targets, out: dict, grad: dict, work, grad_mean=None, grad_rows=None,
+                        logit_scale: float = 1.0, stream=None):
+        """Gradients grad["hidden"] and grad["weight"] (either may be missing) of
+        sum(grad_rows * loss) + grad_mean * mean, behind vocab_loss on the same inputs."""
+        h, w, t = self._matrix(hidden), self._matrix(weight), self._matrix(targets)
+        n = targets.shape[0]
+        gh, gw = grad.get("hidden"), grad.get("weight")
+        self._on_device(work)
+        self._check(self.lib.gd_vocab_loss_grad(
+            self.h, h, w, t, logit_scale, self._vector(out["lse"], n), self._vector(out["mean"], 2),
+            self._vector(grad_mean, 1), self._vector(grad_rows, n), None if gh is None else self._matrix(gh),
+            None if gw is None else self._matrix(gw), work.data_ptr(), work.numel() * work.element_size(),
+            self._stream(stream)))
+
+    def alloc_adamw_state(self, params, bits: int = 32) -> dict:
+        """Fresh moments for a list of tensors: fp32, or 8-bit codes m, v with their m_exp, v_exp."""
+        assert bits in (32, 8)
+        z = lambda n, t: self._torch.zeros(n, dtype=t, device=self.device)
+        kind = self._torch.float32 if bits == 32 else self._torch.uint8
+        state = {k: [z(p.numel(), kind) for p in params] for k in ("m", "v")}
+        if bits == 8:
+            for k in ("m_exp", "v_exp"):
+                state[k] = [z(-(-p.numel() // STATE_BLOCK), self._torch.uint8) for p in params]
+        return state
+
+    def adamw_table(self, params, grads, state: dict, copies=None, weight_decay=0.0, lr_scale=1.0, first_index=0):
+        """What adamw needs to know about its tensors (lists of the same length; weight_decay,
+        lr_scale and first_index are lists too, or one value for all).  The tensors are kept
+        alive by it and must stay where they are."""
+        torch, n = self._torch, len(params)
+        each = lambda v: list(v) if isinstance(v, (list, tuple)) else [v] * n
+        eight = "m_exp" in state
+        lists = [params, grads, state["m"], state["v"], copies if copies is not None else [None] * n,
+                 each(weight_decay), each(lr_scale), each(first_index),
+                 state["m_exp"] if eight else [None] * n, state["v_exp"] if eight else [None] * n]
+        assert all(len(l) == n for l in lists)
+        rows = (_CAdamwTensor * max(n, 1))()
+        for row, p, g, m, v, c, decay, rate, first, me, ve in zip(rows, *lists):
+            k = p.numel()
+            self._on_device(p, g, m, v, c, me, ve)
+            assert all(t is None or (t.is_contiguous() and t.numel() == k) for t in (p, g, m, v, c))
+            assert all(t is None or (t.is_contiguous() and t.dtype == torch.uint8 and
+                                     t.numel() == -(-k // STATE_BLOCK)) for t in (me, ve))
+            assert all(t.dtype == (torch.uint8 if eight else torch.float32) for t in (m, v))
+            row.d_param, row.d_grad, row.d_m, row.d_v = _p(p), _p(g), _p(m), _p(v)
+            row.d_m_exp, row.d_v_exp, row.d_copy = _p(me), _p(ve), _p(c)
+            row.n, row.first_index, row.lr_scale, row.weight_decay = k, first, rate, decay
+            row.param_type, row.grad_type = self._type(p), self._type(g)
+            row.copy_type = BF16 if c is None else self._type(c)
+            row.state_type = E4M3 if eight else F32
+        size = int(self.lib.gd_adamw_table_bytes(self.h, rows, n))
+        if size == 0:
+            raise GuardError(1, (self.lib.gd_last_error(self.h) or b"").decode())
+        host = torch.empty(size, dtype=torch.uint8)
+        self._check(self.lib.gd_adamw_fill_table(self.h, rows, n, host.data_ptr(), size))
+        return dict(bytes=host.to(self.device), tensors=lists)
+
+    def adamw(self, table: dict, lr: float, step: int, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8,
+              grad_scale=None, seed: Optional[int] = None, stream=None):
+        """One update (step counts from 1) of every tensor of the table, in place.  grad_scale: a
+        device scalar that multiplies the gradients; where it is not finite nothing is written.
+        seed: of the 8-bit states' rounding, the step unless it is given."""
+        c = _CAdamwConfig(ctypes.sizeof(_CAdamwConfig), (step if seed is None else seed) & 0xFFFFFFFF, lr, beta1,
+                          beta2, eps, step)
+        b = table["bytes"]
+        self._check(self.lib.gd_adamw(self.h, b.data_ptr(), b.numel(), c, self._vector(grad_scale, 1),
+                                      self._stream(stream)))
