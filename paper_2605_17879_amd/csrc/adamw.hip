@@ -7,17 +7,19 @@
 // decoding and scaling are exact and the only rounding is the one to four significant bits.
 //
 // The tensors are cut into pieces of CHUNK elements that a table on the device lists; a workgroup
-// takes piece after piece.  A wave takes 256 elements at a time, four a lane: 16-byte accesses
-// in fp32, and exactly one block of an 8-bit state, whose largest magnitude then takes six exchanges
-// between lanes and no LDS.
+// takes piece after piece.  A lane holds eight elements at a time, so that 32 lanes hold one block of an
+// 8-bit state, whose largest magnitude then takes five exchanges between lanes and no LDS.
 #include "gd_lanes.h"
 #include "gd_operators.h"
 
 namespace {
 
 constexpr uint32_t NT = 256;
-constexpr uint32_t CHUNK = 4096;          // elements of a piece: four rounds of a workgroup
-constexpr uint32_t ROUNDS = CHUNK / (NT * 4);
+constexpr uint32_t V = 8;                 // elements of a lane at a time
+constexpr uint32_t ROUND = NT * V;
+constexpr uint32_t CHUNK = 8192;          // elements of a piece: four rounds of a workgroup
+constexpr uint32_t ROUNDS = CHUNK / ROUND;
+constexpr uint32_t BLOCK_LANES = GD_STATE_BLOCK / V;
 
 struct table_head {
     uint64_t bytes;         // of the whole table
@@ -29,7 +31,7 @@ struct table_tensor {
     uint64_t n, first_index;
     double lr_scale, weight_decay;
     uint8_t param_type, grad_type, copy_type, eight;
-    uint8_t aligned;        // every array aligned to four of its elements
+    uint8_t aligned;        // every array aligned to what a lane reads of it at once
     uint8_t pad[3];
 };
 struct table_chunk {
@@ -39,67 +41,81 @@ constexpr size_t HEAD = 64;
 
 __host__ __device__ inline size_t chunks_at(uint32_t n_tensors) { return HEAD + (size_t)n_tensors * sizeof(table_tensor); }
 
-// Four numbers of an array of type T, those below `n` alone.
+// V numbers of an array as they lie in memory.
+template <typename T> struct raw { gd_vec<T, 16 / sizeof(T)> q[V * sizeof(T) / 16]; };
+template <> struct raw<uint8_t> { uint2 q; };
+
 template <typename T>
-__device__ __forceinline__ void load4(const void* p, uint64_t at, uint32_t n, bool whole, float x[4]) {
-    if (whole) {
-        const gd_vec<T, 4> q = *reinterpret_cast<const gd_vec<T, 4>*>(static_cast<const T*>(p) + at);
+__device__ __forceinline__ raw<T> load_raw(const void* p, uint64_t at) { return *reinterpret_cast<const raw<T>*>(static_cast<const T*>(p) + at); }
+template <typename T>
+__device__ __forceinline__ void to_floats(const raw<T>& r, float x[V]) {
+    constexpr int E = 16 / sizeof(T);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) x[j] = gd_to_f32(q.v[j]);
+    for (int j = 0; j < (int)V; ++j) x[j] = gd_to_f32(r.q[j / E].v[j % E]);
+}
+// The first n of them: all at once (`vec`) or one by one, zeros behind.
+template <typename T>
+__device__ __forceinline__ void load_some(const void* p, uint64_t at, uint32_t n, bool vec, float x[V]) {
+    if (vec) {
+        to_floats<T>(load_raw<T>(p, at), x);
     } else {
 #pragma unroll
-        for (uint32_t j = 0; j < 4; ++j) x[j] = j < n ? gd_to_f32(static_cast<const T*>(p)[at + j]) : 0.0f;
+        for (uint32_t j = 0; j < V; ++j) x[j] = j < n ? gd_to_f32(static_cast<const T*>(p)[at + j]) : 0.0f;
     }
 }
 template <typename T>
-__device__ __forceinline__ void store4(void* p, uint64_t at, uint32_t n, bool whole, const float x[4]) {
-    if (whole) {
-        gd_vec<T, 4> q;
+__device__ __forceinline__ void store(void* p, uint64_t at, uint32_t n, bool vec, const float x[V]) {
+    if (vec) {
+        constexpr int E = 16 / sizeof(T);
+        raw<T> r;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) q.v[j] = gd_from_f32<T>(x[j]);
-        *reinterpret_cast<gd_vec<T, 4>*>(static_cast<T*>(p) + at) = q;
+        for (int j = 0; j < (int)V; ++j) r.q[j / E].v[j % E] = gd_from_f32<T>(x[j]);
+        *reinterpret_cast<raw<T>*>(static_cast<T*>(p) + at) = r;
     } else {
 #pragma unroll
-        for (uint32_t j = 0; j < 4; ++j)
+        for (uint32_t j = 0; j < V; ++j)
             if (j < n) static_cast<T*>(p)[at + j] = gd_from_f32<T>(x[j]);
     }
 }
-
-__device__ __forceinline__ uint32_t load_codes(const void* p, uint64_t at, uint32_t n, bool whole) {
+__device__ __forceinline__ uint2 load_some_codes(const void* p, uint64_t at, uint32_t n, bool vec) {
     const uint8_t* b = static_cast<const uint8_t*>(p) + at;
-    if (whole) return *reinterpret_cast<const uint32_t*>(b);
-    uint32_t c = 0;
+    if (vec) return *reinterpret_cast<const uint2*>(b);
+    uint32_t c[2] = {0, 0};
 #pragma unroll
-    for (uint32_t j = 0; j < 4; ++j)
-        if (j < n) c |= (uint32_t)b[j] << (8 * j);
-    return c;
+    for (uint32_t j = 0; j < V; ++j)
+        if (j < n) c[j / 4] |= (uint32_t)b[j] << (8 * (j & 3));
+    return make_uint2(c[0], c[1]);
 }
-__device__ __forceinline__ void store_codes(void* p, uint64_t at, uint32_t n, bool whole, uint32_t c) {
+__device__ __forceinline__ void store_codes(void* p, uint64_t at, uint32_t n, bool vec, uint32_t c0, uint32_t c1) {
     uint8_t* b = static_cast<uint8_t*>(p) + at;
-    if (whole) {
-        *reinterpret_cast<uint32_t*>(b) = c;
+    if (vec) {
+        *reinterpret_cast<uint2*>(b) = make_uint2(c0, c1);
     } else {
 #pragma unroll
-        for (uint32_t j = 0; j < 4; ++j)
-            if (j < n) b[j] = (uint8_t)(c >> (8 * j));
+        for (uint32_t j = 0; j < V; ++j)
+            if (j < n) b[j] = (uint8_t)((j < 4 ? c0 : c1) >> (8 * (j & 3)));
     }
 }
 
-// Four e4m3 codes times their block's power of two (byte e): exact.
-__device__ __forceinline__ void decode4(uint32_t c, uint32_t e, float x[4]) {
+// e4m3 codes times their block's power of two (byte e): exact.
+__device__ __forceinline__ void decode(uint2 c, uint32_t e, float x[V]) {
     const float two = e == 255 ? __uint_as_float(0x7FC00000u) : __uint_as_float(e << 23);
-    x[0] = __builtin_amdgcn_cvt_f32_fp8((int)c, 0) * two;
-    x[1] = __builtin_amdgcn_cvt_f32_fp8((int)c, 1) * two;
-    x[2] = __builtin_amdgcn_cvt_f32_fp8((int)c, 2) * two;
-    x[3] = __builtin_amdgcn_cvt_f32_fp8((int)c, 3) * two;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const int w = (int)(h ? c.y : c.x);
+        x[4 * h] = __builtin_amdgcn_cvt_f32_fp8(w, 0) * two;
+        x[4 * h + 1] = __builtin_amdgcn_cvt_f32_fp8(w, 1) * two;
+        x[4 * h + 2] = __builtin_amdgcn_cvt_f32_fp8(w, 2) * two;
+        x[4 * h + 3] = __builtin_amdgcn_cvt_f32_fp8(w, 3) * two;
+    }
 }
 
-// The largest of a value over the wave.
-__device__ __forceinline__ uint32_t wave_max(uint32_t v, uint32_t lane) {
+// The largest of a value over the lanes of a block (half a wave).
+static_assert(BLOCK_LANES == 32, "block_max");
+__device__ __forceinline__ uint32_t block_max(uint32_t v, uint32_t lane) {
     v = max(v, gd_lane_xor<1>(v, lane));  v = max(v, gd_lane_xor<2>(v, lane));
     v = max(v, gd_lane_xor<4>(v, lane));  v = max(v, gd_lane_xor<8>(v, lane));
-    v = max(v, gd_lane_xor<16>(v, lane)); v = max(v, gd_lane_xor<32>(v, lane));
-    return v;
+    return max(v, gd_lane_xor<16>(v, lane));
 }
 
 // The byte of the power of two that brings a magnitude (as bits) into (224, 448], at least 1.
@@ -110,122 +126,184 @@ __device__ __forceinline__ uint32_t block_exponent(uint32_t bits) {
     return e < 1 ? 1u : (uint32_t)e;
 }
 
-// One magnitude q <= 448 to a multiple of its e4m3 step, dithered: the digits below the step are dropped
-// after a number of 0 to 2^20 - 1 units of 2^-20 of a step was added.  Below 2^-6 the step stays
-// 2^-9; adding 2^-6 moves these to numbers of the same step whose bits can be handled alike.
-__device__ __forceinline__ float dither_e4m3(float q, uint32_t d) {
-    const bool small = q < 0.015625f;
-    const float t = small ? q + 0.015625f : q;
-    const float y = __uint_as_float((__float_as_uint(t) + d) & 0xFFF00000u);
-    return small ? y - 0.015625f : y;
-}
-
-// Four numbers to codes under the block's power of two.  d: two 16-bit numbers a word, `high` picks.
+// Four numbers to codes under the block's power of two.  The conversion with a dither adds the upper 20
+// bits of its second operand, in units of 2^-20 of a step, to the magnitude and drops what is below the step
+// (2^-9 for numbers below 2^-6), subnormal codes included: a lower neighbour becomes the upper one
+// as often as the number is near to that.  `hash`: two 16-bit numbers a word, one for each state.
 template <bool ROOT>
 __device__ __forceinline__ uint32_t encode4(const float x[4], uint32_t e, const uint32_t hash[4]) {
     if (e == 255) return 0x7F7F7F7Fu;                        // NaN
     const float up = __uint_as_float(e == 0 ? 0u : (254u - e) << 23);
-    float y[4];
+    uint32_t d[4];
+    float q[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-        const float q = fabsf(x[j]) * up;
-        const uint32_t d = ((ROOT ? hash[j] >> 16 : hash[j] & 0xFFFFu) << 4) + 8u;
-        y[j] = dither_e4m3(q, d);
-        if (ROOT) y[j] = y[j] == 0.0f && q > 0.0f ? 0.001953125f : y[j];
-        y[j] = copysignf(y[j], x[j]);
+        q[j] = x[j] * up;
+        d[j] = (ROOT ? hash[j] & 0xFFFF0000u : hash[j] << 16) | 0x8000u;
     }
-    int c = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false);
-    return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], c, true);
+    int c = __builtin_amdgcn_cvt_sr_fp8_f32(q[0], d[0], 0, 0);
+    c = __builtin_amdgcn_cvt_sr_fp8_f32(q[1], d[1], c, 1);
+    c = __builtin_amdgcn_cvt_sr_fp8_f32(q[2], d[2], c, 2);
+    c = __builtin_amdgcn_cvt_sr_fp8_f32(q[3], d[3], c, 3);
+    if (ROOT) {                                              // no root above 0 becomes 0
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (((uint32_t)c >> (8 * j) & 255u) == 0 && q[j] > 0.0f) c |= 1 << (8 * j);
+    }
+    return (uint32_t)c;
 }
 
-// A well-mixed word from an element's index and the seed: a multiplicative start, then two rounds of
-// shift, exclusive or and multiplication by odd numbers.
-__device__ __forceinline__ uint32_t index_hash(uint64_t i, uint32_t seed) {
-    uint32_t x = (uint32_t)i * 0x9E3779B1u + (uint32_t)(i >> 32) * 0x7F4A7C15u + seed * 0x85157AF5u;
-    x = (x ^ (x >> 16)) * 0x58F38DEDu;
-    x = (x ^ (x >> 15)) * 0x1AC2F6EBu;
-    return x ^ (x >> 16);
+// Well-mixed words from the indexes of V elements next to each other and the seed: a multiplicative
+// start, then two rounds of shift, exclusive or and multiplication by odd numbers.
+__device__ __forceinline__ void index_hash(uint64_t i, uint32_t seed, uint32_t h[V]) {
+    const uint32_t lo = (uint32_t)i, start = lo * 0x9E3779B1u + (uint32_t)(i >> 32) * 0x7F4A7C15u + seed * 0x85157AF5u;
+#pragma unroll
+    for (uint32_t j = 0; j < V; ++j) {
+        uint32_t x = start + j * 0x9E3779B1u;
+        if (lo + j < lo) x += 0x7F4A7C15u;                   // (the index's upper word counts on)
+        x = (x ^ (x >> 16)) * 0x58F38DEDu;
+        x = (x ^ (x >> 15)) * 0x1AC2F6EBu;
+        h[j] = x ^ (x >> 16);
+    }
 }
 
-template <typename P, typename G, bool EIGHT>
-__device__ __forceinline__ void update_chunk(const table_tensor& t, uint32_t chunk, const gd_adamw_args& a, float gs,
-                                             bool scaled) {
+// What one lane holds of a round.
+template <typename P, typename G, typename S>
+struct round_data {
+    raw<P> p;
+    raw<G> g;
+    raw<S> m, v;
+    uint32_t me, ve;
+};
+
+template <typename P, typename G, typename S>
+__device__ __forceinline__ void load_round(const table_tensor& t, uint64_t at, round_data<P, G, S>& d) {
+    d.p = load_raw<P>(t.param, at);
+    d.g = load_raw<G>(t.grad, at);
+    d.m = load_raw<S>(t.m, at);
+    d.v = load_raw<S>(t.v, at);
+    if (sizeof(S) == 1) {
+        d.me = t.m_exp[at / GD_STATE_BLOCK];
+        d.ve = t.v_exp[at / GD_STATE_BLOCK];
+    }
+}
+
+struct factors {
+    float keep, size, gs;
+    bool scaled;
+};
+
+// One lane's elements: updated and written back.  WHOLE: all V of them are there, aligned and loaded (d);
+// else the first n, `vec` where that are all V of them and they are aligned.
+template <typename P, typename G, typename S, bool WHOLE>
+__device__ __forceinline__ void update(const table_tensor& t, const gd_adamw_args& a, const factors& f, uint64_t at, uint32_t n,
+                                       bool vec, const round_data<P, G, S>* d) {
+    constexpr bool EIGHT = sizeof(S) == 1;
     const uint32_t lane = threadIdx.x & 63;
-    const float keep = (float)(1.0 - a.lr * t.lr_scale * t.weight_decay);
-    const float size = (float)(a.lr * t.lr_scale / a.c1);
-    const uint64_t base = (uint64_t)chunk * CHUNK;
-    for (uint32_t r = 0; r < ROUNDS; ++r) {
-        const uint64_t at = base + (uint64_t)r * (NT * 4) + threadIdx.x * 4;
-        // a wave is in or out as a whole for the exchanges of an 8-bit block
-        if (base + (uint64_t)r * (NT * 4) + (threadIdx.x & ~63u) * 4 >= t.n) break;
-        const uint32_t n = at >= t.n ? 0u : (uint32_t)(t.n - at < 4 ? t.n - at : 4);
-        const bool whole = n == 4 && t.aligned;
-        float p[4], g[4], m[4], v[4];
-        load4<P>(t.param, at, n, whole, p);
-        load4<G>(t.grad, at, n, whole, g);
-        if (EIGHT) {
-            const uint64_t block = at / GD_STATE_BLOCK;
-            float q[4];
-            decode4(load_codes(t.m, at, n, whole), t.m_exp[block], m);
-            decode4(load_codes(t.v, at, n, whole), t.v_exp[block], q);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) v[j] = q[j] * q[j];
+    float p[V], g[V], m[V], v[V], root[V];
+    if constexpr (WHOLE) {
+        to_floats<P>(d->p, p);
+        to_floats<G>(d->g, g);
+        if constexpr (EIGHT) {
+            decode(d->m.q, d->me, m);
+            decode(d->v.q, d->ve, v);
         } else {
-            load4<float>(t.m, at, n, whole, m);
-            load4<float>(t.v, at, n, whole, v);
+            to_floats<S>(d->m, m);
+            to_floats<S>(d->v, v);
         }
-        float root[4];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const float gj = scaled ? g[j] * gs : g[j];
-            m[j] = m[j] * a.fbeta1 + gj * a.one_beta1;
-            v[j] = v[j] * a.fbeta2 + (gj * a.one_beta2) * gj;
-            root[j] = sqrtf(v[j]);
-            p[j] = p[j] * keep - (m[j] * size) / (root[j] * a.inv_root_c2 + a.eps);
-        }
-        store4<P>(t.param, at, n, whole, p);
-        if (t.copy) {
-            if (t.copy_type == GD_BF16) store4<gd_bf16>(t.copy, at, n, whole, p);
-            else store4<gd_f16>(t.copy, at, n, whole, p);
-        }
-        if (EIGHT) {
-            // elements behind the end count as zeros
-            uint32_t mm = 0, mv = 0, hash[4];
-#pragma unroll
-            for (uint32_t j = 0; j < 4; ++j) {
-                if (j >= n) m[j] = root[j] = 0.0f;
-                mm = max(mm, __float_as_uint(m[j]) & 0x7FFFFFFFu);
-                mv = max(mv, __float_as_uint(root[j]) & 0x7FFFFFFFu);
-                hash[j] = index_hash(t.first_index + at + j, a.seed);
-            }
-            const uint32_t em = block_exponent(wave_max(mm, lane)), ev = block_exponent(wave_max(mv, lane));
-            store_codes(t.m, at, n, whole, encode4<false>(m, em, hash));
-            store_codes(t.v, at, n, whole, encode4<true>(root, ev, hash));
-            if (lane == 0) {
-                t.m_exp[at / GD_STATE_BLOCK] = (uint8_t)em;
-                t.v_exp[at / GD_STATE_BLOCK] = (uint8_t)ev;
-            }
+    } else {
+        load_some<P>(t.param, at, n, vec, p);
+        load_some<G>(t.grad, at, n, vec, g);
+        if constexpr (EIGHT) {
+            decode(load_some_codes(t.m, at, n, vec), t.m_exp[at / GD_STATE_BLOCK], m);
+            decode(load_some_codes(t.v, at, n, vec), t.v_exp[at / GD_STATE_BLOCK], v);
         } else {
-            store4<float>(t.m, at, n, whole, m);
-            store4<float>(t.v, at, n, whole, v);
+            load_some<S>(t.m, at, n, vec, m);
+            load_some<S>(t.v, at, n, vec, v);
         }
+    }
+#pragma unroll
+    for (int j = 0; j < (int)V; ++j) {
+        const float gj = f.scaled ? g[j] * f.gs : g[j];
+        if (EIGHT) v[j] = v[j] * v[j];
+        m[j] = m[j] * a.fbeta1 + gj * a.one_beta1;
+        v[j] = v[j] * a.fbeta2 + (gj * a.one_beta2) * gj;
+        root[j] = sqrtf(v[j]);
+        p[j] = p[j] * f.keep - (m[j] * f.size) / (root[j] * a.inv_root_c2 + a.eps);
+    }
+    store<P>(t.param, at, n, vec, p);
+    if (t.copy) {
+        if (t.copy_type == GD_BF16) store<gd_bf16>(t.copy, at, n, vec, p);
+        else store<gd_f16>(t.copy, at, n, vec, p);
+    }
+    if constexpr (EIGHT) {
+        // elements behind the end count as zeros
+        uint32_t mm = 0, mv = 0, hash[V];
+#pragma unroll
+        for (uint32_t j = 0; j < V; ++j) {
+            if (!WHOLE && j >= n) m[j] = root[j] = 0.0f;
+            mm = max(mm, __float_as_uint(m[j]) & 0x7FFFFFFFu);
+            mv = max(mv, __float_as_uint(root[j]) & 0x7FFFFFFFu);
+        }
+        index_hash(t.first_index + at, a.seed, hash);
+        const uint32_t em = block_exponent(block_max(mm, lane)), ev = block_exponent(block_max(mv, lane));
+        store_codes(t.m, at, n, vec, encode4<false>(m, em, hash), encode4<false>(m + 4, em, hash + 4));
+        store_codes(t.v, at, n, vec, encode4<true>(root, ev, hash), encode4<true>(root + 4, ev, hash + 4));
+        if ((lane & (BLOCK_LANES - 1)) == 0 && (WHOLE || n > 0)) {
+            t.m_exp[at / GD_STATE_BLOCK] = (uint8_t)em;
+            t.v_exp[at / GD_STATE_BLOCK] = (uint8_t)ev;
+        }
+    } else {
+        store<float>(t.m, at, n, vec, m);
+        store<float>(t.v, at, n, vec, v);
     }
 }
 
-template <typename P, bool EIGHT>
+template <typename P, typename G, typename S>
+__device__ __forceinline__ void update_chunk(const table_tensor& t, uint32_t chunk, const gd_adamw_args& a, float gs, bool scaled) {
+    factors f;
+    f.keep = (float)(1.0 - a.lr * t.lr_scale * t.weight_decay);
+    f.size = (float)(a.lr * t.lr_scale / a.c1);
+    f.gs = gs;
+    f.scaled = scaled;
+    const uint64_t base = (uint64_t)chunk * CHUNK;
+    if (base + CHUNK <= t.n && t.aligned) {
+        // the next round's loads are on their way while this one is worked out
+        round_data<P, G, S> d[2];
+        uint64_t at = base + threadIdx.x * V;
+        load_round(t, at, d[0]);
+#pragma unroll
+        for (uint32_t r = 0; r < ROUNDS; ++r, at += ROUND) {
+            if (r + 1 < ROUNDS) load_round(t, at + ROUND, d[(r + 1) & 1]);
+            update<P, G, S, true>(t, a, f, at, V, true, &d[r & 1]);
+        }
+        return;
+    }
+    for (uint32_t r = 0; r < ROUNDS; ++r) {
+        const uint64_t at = base + r * ROUND + threadIdx.x * V;
+        // a wave is in or out as a whole, for the exchanges of an 8-bit block; lanes of a block that is not
+        // there read the exponents of the last one and write nothing
+        if (base + r * ROUND + (threadIdx.x & ~63u) * V >= t.n) break;
+        const uint32_t n = at >= t.n ? 0u : (uint32_t)(t.n - at < V ? t.n - at : V);
+        const uint64_t block = at & ~(uint64_t)(GD_STATE_BLOCK - 1);
+        update<P, G, S, false>(t, a, f, block < t.n ? at : t.n - 1, n, n == V && t.aligned, nullptr);
+    }
+}
+
+template <typename P, typename S>
 __device__ __forceinline__ void by_grad(const table_tensor& t, uint32_t chunk, const gd_adamw_args& a, float gs, bool scaled) {
     switch (t.grad_type) {
-        case GD_F32: update_chunk<P, float, EIGHT>(t, chunk, a, gs, scaled); break;
-        case GD_BF16: update_chunk<P, gd_bf16, EIGHT>(t, chunk, a, gs, scaled); break;
-        default: update_chunk<P, gd_f16, EIGHT>(t, chunk, a, gs, scaled); break;
+        case GD_F32: update_chunk<P, float, S>(t, chunk, a, gs, scaled); break;
+        case GD_BF16: update_chunk<P, gd_bf16, S>(t, chunk, a, gs, scaled); break;
+        default: update_chunk<P, gd_f16, S>(t, chunk, a, gs, scaled); break;
     }
 }
-template <bool EIGHT>
+template <typename S>
 __device__ __forceinline__ void by_param(const table_tensor& t, uint32_t chunk, const gd_adamw_args& a, float gs, bool scaled) {
     switch (t.param_type) {
-        case GD_F32: by_grad<float, EIGHT>(t, chunk, a, gs, scaled); break;
-        case GD_BF16: by_grad<gd_bf16, EIGHT>(t, chunk, a, gs, scaled); break;
-        default: by_grad<gd_f16, EIGHT>(t, chunk, a, gs, scaled); break;
+        case GD_F32: by_grad<float, S>(t, chunk, a, gs, scaled); break;
+        case GD_BF16: by_grad<gd_bf16, S>(t, chunk, a, gs, scaled); break;
+        default: by_grad<gd_f16, S>(t, chunk, a, gs, scaled); break;
     }
 }
 
@@ -241,12 +319,10 @@ __global__ __launch_bounds__(NT) void adamw_kernel(const gd_adamw_args a) {
     const table_tensor* tensors = reinterpret_cast<const table_tensor*>(a.table + HEAD);
     for (uint32_t c = blockIdx.x; c < head->n_chunks; c += gridDim.x) {
         const table_tensor& t = tensors[chunks[c].tensor];
-        if (t.eight) by_param<true>(t, chunks[c].chunk, a, gs, a.grad_scale != nullptr);
-        else by_param<false>(t, chunks[c].chunk, a, gs, a.grad_scale != nullptr);
+        if (t.eight) by_param<uint8_t>(t, chunks[c].chunk, a, gs, a.grad_scale != nullptr);
+        else by_param<float>(t, chunks[c].chunk, a, gs, a.grad_scale != nullptr);
     }
 }
-
-size_t size_of(uint32_t type) { return type == GD_F32 ? 4 : 2; }
 
 }  // namespace
 
@@ -270,10 +346,9 @@ size_t gd_adamw_table(const gd_adamw_tensor* t, uint32_t n, void* out) {
         d[i].lr_scale = s.lr_scale; d[i].weight_decay = s.weight_decay;
         d[i].param_type = (uint8_t)s.param_type; d[i].grad_type = (uint8_t)s.grad_type;
         d[i].copy_type = (uint8_t)s.copy_type; d[i].eight = s.state_type == GD_E4M3;
-        const size_t state = d[i].eight ? 1 : 4;
-        const bool off = ((uintptr_t)s.d_param % (4 * size_of(s.param_type))) || ((uintptr_t)s.d_grad % (4 * size_of(s.grad_type))) ||
-                         ((uintptr_t)s.d_m % (4 * state)) || ((uintptr_t)s.d_v % (4 * state)) ||
-                         (s.d_copy && (uintptr_t)s.d_copy % 8);
+        const size_t state = d[i].eight ? 8 : 16;
+        const bool off = (uintptr_t)s.d_param % 16 || (uintptr_t)s.d_grad % 16 || (uintptr_t)s.d_m % state || (uintptr_t)s.d_v % state ||
+                         (s.d_copy && (uintptr_t)s.d_copy % 16);
         d[i].aligned = off ? 0 : 1;
         for (uint64_t k = 0; k * CHUNK < s.n; ++k) { c->tensor = i; c->chunk = (uint32_t)k; ++c; }
     }
