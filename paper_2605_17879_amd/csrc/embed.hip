@@ -5,18 +5,23 @@
 //
 // The gradient must not depend on the order in which workgroups run, so there are no float
 // atomics: the (token, position) pairs are sorted by token, stably, and the sorted list is cut into
-// stretches of SPAN.  A workgroup sums the rows of one stretch, one column vector per lane, and writes a
+// stretches.  A workgroup sums the rows of one stretch, one column vector per lane, and writes a
 // token's sum when the next token begins.  A token that goes on over a stretch's end leaves fp32
 // partial sums (one at the front and one at the back of each stretch), which a second kernel adds up in
 // order: however often a token occurs, the work stays even.
+//
+// The gradient's zeros are written by workgroups of the sorting launches that have no keys: sorting is
+// a chain of short launches that leaves the memory idle.
 #include "gd_operators.h"
 
 namespace {
 
 constexpr uint32_t NT = 256;
-constexpr uint32_t SPAN = 32;             // sorted entries of a workgroup
-constexpr uint32_t DIGITS = 256;          // of a sorting pass
-constexpr uint32_t SORT_KEYS = 4096;      // keys of a workgroup in a sorting pass
+constexpr uint32_t BITS = 9, DIGITS = 1u << BITS;   // of a sorting pass: two passes up to 262 143 rows
+constexpr uint32_t SORT_KEYS = 1024;      // keys of a workgroup in a sorting pass
+constexpr uint32_t ONE_SORT = 4096;       // most keys that one workgroup sorts by itself
+constexpr uint32_t SELF_SCAN = 64;        // most workgroups of a pass that add up the counts before them themselves
+constexpr uint32_t BATCH = 8;             // rows on their way at once in the sums
 constexpr uint32_t NO_ROW = 0xFFFFFFFFu;
 
 // ---- lookup ------------------------------------------------------------------------------------
@@ -60,123 +65,259 @@ uint32_t vector_of(const void* p, uint64_t ps, const void* q, uint64_t qs, uint6
 
 // ---- the stable sort by token ---------------------------------------------------------------
 
-struct sort_buffers {
+struct sort_args {
+    gd_token_list tokens;
     uint32_t* key[2];
     uint32_t* pos[2];
-    uint32_t* hist;      // [DIGITS][blocks], then its exclusive prefix sums
-    uint32_t blocks;
+    uint32_t* hist;      // [blocks + 1][DIGITS] counts; where they were scanned, those before a block, and totals
+    uint32_t n, vocab, blocks, from, shift, scanned;
 };
 
-// Tokens to keys: NO_ROW for those without a row, which sort behind all others.
+// Zeros that a launch writes beside its own work: rows from..to of the gradient.
+struct fill_args {
+    void* p;  uint64_t stride;
+    uint32_t width, from, to;
+};
+
+// Tokens to keys: those without a row get the largest one and sort behind all others.
 __device__ __forceinline__ uint32_t key_of(const gd_token_list& l, uint32_t i, uint32_t vocab) {
     const int64_t t = gd_token(l, i);
     return t >= 0 && t < (int64_t)vocab ? (uint32_t)t : vocab;
 }
 
-// Keys of a wave stand in order of (wave, round, lane): each wave owns a stretch of the block's keys.
-constexpr uint32_t SORT_ROUNDS = SORT_KEYS / NT;
-
 // For each lane: which lanes of the wave hold the same digit (among those with a key).
 __device__ __forceinline__ uint64_t same_digit(uint32_t d, bool there) {
     uint64_t same = __ballot(there);
 #pragma unroll
-    for (int b = 0; b < 8; ++b) {
+    for (uint32_t b = 0; b < BITS; ++b) {
         const uint64_t with = __ballot((d >> b) & 1);
         same &= ((d >> b) & 1) ? with : ~with;
     }
     return same;
 }
 
-template <bool FIRST>
-__global__ __launch_bounds__(NT) void sort_count(sort_buffers b, gd_token_list tokens, uint32_t n, uint32_t vocab, uint32_t from,
-                                                 uint32_t shift) {
-    __shared__ uint32_t h[DIGITS];
-    h[threadIdx.x] = 0;
-    __syncthreads();
-    const uint32_t base = blockIdx.x * SORT_KEYS;
-    for (uint32_t r = 0; r < SORT_ROUNDS; ++r) {
-        const uint32_t i = base + r * NT + threadIdx.x;
-        if (i < n) atomicAdd(&h[((FIRST ? key_of(tokens, i, vocab) : b.key[from][i]) >> shift) & (DIGITS - 1)], 1u);
+// Workgroup `block` of `blocks` fills its share.
+template <typename T, int V, int THREADS>
+__device__ __forceinline__ void fill_rows(const fill_args& f, uint32_t block, uint32_t blocks) {
+    gd_vec<T, V> zero;
+#pragma unroll
+    for (int j = 0; j < V; ++j) zero.v[j] = gd_from_f32<T>(0.0f);
+    if (f.stride == f.width) {                                // one stretch of memory
+        T* p = static_cast<T*>(f.p);
+        const uint64_t end = (uint64_t)f.to * f.width;
+        for (uint64_t i = (uint64_t)f.from * f.width + ((uint64_t)block * THREADS + threadIdx.x) * V; i < end;
+             i += (uint64_t)blocks * THREADS * V)
+            *reinterpret_cast<gd_vec<T, V>*>(p + i) = zero;
+    } else {
+        for (uint32_t r = f.from + block; r < f.to; r += blocks)
+            for (uint32_t c = threadIdx.x * V; c < f.width; c += THREADS * V)
+                *reinterpret_cast<gd_vec<T, V>*>(static_cast<T*>(f.p) + (uint64_t)r * f.stride + c) = zero;
     }
-    __syncthreads();
-    b.hist[threadIdx.x * b.blocks + blockIdx.x] = h[threadIdx.x];
 }
 
-// Exclusive prefix sums of `count` words, one workgroup.
-__global__ __launch_bounds__(1024) void sort_scan(uint32_t* h, uint32_t count) {
-    __shared__ uint32_t part[1024];
-    const uint32_t per = (count + 1023) / 1024, from = threadIdx.x * per;
-    uint32_t sum = 0;
-    for (uint32_t i = from; i < from + per && i < count; ++i) sum += h[i];
-    part[threadIdx.x] = sum;
-    __syncthreads();
-    for (uint32_t d = 1; d < 1024; d <<= 1) {
-        const uint32_t v = threadIdx.x >= d ? part[threadIdx.x - d] : 0;
+// All passes by one workgroup of sixteen waves, the keys in its registers and, between passes, in the LDS.
+// A wave owns ONE_SORT / 16 keys next to each other, 64 a round.
+template <typename T, int V>
+__global__ __launch_bounds__(1024) void sort_alone(sort_args a, fill_args f) {
+    if (blockIdx.x > 0) return fill_rows<T, V, 1024>(f, blockIdx.x - 1, gridDim.x - 1);
+    constexpr uint32_t WAVES = 16, ROUNDS = ONE_SORT / 1024;
+    __shared__ uint32_t skey[ONE_SORT];
+    __shared__ uint16_t spos[ONE_SORT];
+    __shared__ uint16_t next[WAVES][DIGITS];
+    __shared__ uint32_t part[DIGITS / 64];
+    const uint32_t wave = threadIdx.x / 64, lane = threadIdx.x & 63, base = wave * (ONE_SORT / WAVES);
+    uint32_t key[ROUNDS], pos[ROUNDS];
+#pragma unroll
+    for (uint32_t r = 0; r < ROUNDS; ++r) {
+        pos[r] = base + r * 64 + lane;
+        key[r] = pos[r] < a.n ? key_of(a.tokens, pos[r], a.vocab) : 0;
+    }
+    for (uint32_t shift = 0; shift == 0 || (a.vocab >> shift) > 0; shift += BITS) {
+        for (uint32_t i = threadIdx.x; i < WAVES * DIGITS; i += 1024) (&next[0][0])[i] = 0;
         __syncthreads();
-        part[threadIdx.x] += v;
+        uint32_t before[ROUNDS];
+#pragma unroll
+        for (uint32_t r = 0; r < ROUNDS; ++r) {
+            // (the wave's own counter: its lanes read it before the first of them adds)
+            const uint32_t d = (key[r] >> shift) & (DIGITS - 1);
+            const bool there = base + r * 64 + lane < a.n;
+            const uint64_t same = same_digit(d, there);
+            const uint32_t mine = (uint32_t)__popcll(same & ((1ull << lane) - 1));
+            before[r] = next[wave][d] + mine;
+            __builtin_amdgcn_wave_barrier();
+            if (there && mine == 0) next[wave][d] = (uint16_t)(next[wave][d] + (uint32_t)__popcll(same));
+            __builtin_amdgcn_wave_barrier();
+        }
         __syncthreads();
-    }
-    uint32_t at = part[threadIdx.x] - sum;
-    for (uint32_t i = from; i < from + per && i < count; ++i) { const uint32_t v = h[i]; h[i] = at; at += v; }
-}
-
-template <bool FIRST>
-__global__ __launch_bounds__(NT) void sort_scatter(sort_buffers b, gd_token_list tokens, uint32_t n, uint32_t vocab, uint32_t from,
-                                                   uint32_t shift) {
-    constexpr uint32_t WAVES = NT / 64;
-    __shared__ uint32_t next[WAVES][DIGITS];
-    const uint32_t wave = threadIdx.x / 64, lane = threadIdx.x & 63;
-    const uint32_t base = blockIdx.x * SORT_KEYS + wave * (SORT_KEYS / WAVES);
+        // counts to places: of the waves before, then of the digits before
+        uint32_t total = 0, sum = 0;
+        if (threadIdx.x < DIGITS) {
 #pragma unroll
-    for (uint32_t w = 0; w < WAVES; ++w) next[w][threadIdx.x] = 0;
-    __syncthreads();
-    uint32_t key[SORT_ROUNDS];
+            for (uint32_t w = 0; w < WAVES; ++w) {
+                const uint32_t c = next[w][threadIdx.x];
+                next[w][threadIdx.x] = (uint16_t)total;
+                total += c;
+            }
+            sum = total;
 #pragma unroll
-    for (uint32_t r = 0; r < SORT_ROUNDS; ++r) {
-        const uint32_t i = base + r * 64 + lane;
-        key[r] = i < n ? (FIRST ? key_of(tokens, i, vocab) : b.key[from][i]) : 0;
-        if (i < n) atomicAdd(&next[wave][(key[r] >> shift) & (DIGITS - 1)], 1u);
-    }
-    __syncthreads();
-    {   // where each wave's keys of a digit begin
-        uint32_t at = b.hist[threadIdx.x * b.blocks + blockIdx.x];
+            for (uint32_t d = 1; d < 64; d <<= 1) {
+                const uint32_t v = __shfl_up(sum, d);
+                if (lane >= d) sum += v;
+            }
+            if (lane == 63) part[wave] = sum;
+        }
+        __syncthreads();
+        if (threadIdx.x < DIGITS) {
+            uint32_t at = sum - total;
+            for (uint32_t w = 0; w < wave; ++w) at += part[w];
 #pragma unroll
-        for (uint32_t w = 0; w < WAVES; ++w) { const uint32_t c = next[w][threadIdx.x]; next[w][threadIdx.x] = at; at += c; }
-    }
-    __syncthreads();
+            for (uint32_t w = 0; w < WAVES; ++w) next[w][threadIdx.x] = (uint16_t)(next[w][threadIdx.x] + at);
+        }
+        __syncthreads();
 #pragma unroll
-    for (uint32_t r = 0; r < SORT_ROUNDS; ++r) {
-        const uint32_t i = base + r * 64 + lane;
-        const bool there = i < n;
-        const uint32_t d = (key[r] >> shift) & (DIGITS - 1);
-        const uint64_t same = same_digit(d, there);
-        const uint32_t before = (uint32_t)__popcll(same & ((1ull << lane) - 1));
-        uint32_t at = 0;
-        if (there) at = next[wave][d] + before;
-        __builtin_amdgcn_wave_barrier();
-        if (there && before == 0) next[wave][d] += (uint32_t)__popcll(same);
-        __builtin_amdgcn_wave_barrier();
-        if (there) {
-            b.key[from ^ 1][at] = key[r];
-            b.pos[from ^ 1][at] = FIRST ? i : b.pos[from][i];
+        for (uint32_t r = 0; r < ROUNDS; ++r)
+            if (base + r * 64 + lane < a.n) {
+                const uint32_t at = next[wave][(key[r] >> shift) & (DIGITS - 1)] + before[r];
+                skey[at] = key[r];
+                spos[at] = (uint16_t)pos[r];
+            }
+        __syncthreads();
+#pragma unroll
+        for (uint32_t r = 0; r < ROUNDS; ++r) {
+            const uint32_t i = base + r * 64 + lane;
+            if (i < a.n) { key[r] = skey[i]; pos[r] = spos[i]; }
         }
     }
-}
-
-// ---- sums over stretches of the sorted list -----------------------------------------------
-
-template <typename T, int V>
-__global__ __launch_bounds__(NT) void grad_zero(gd_embed_grad_args a) {
-    const uint32_t vecs = a.width / V;
-    const uint64_t total = (uint64_t)a.vocab * vecs;
-    for (uint64_t i = (uint64_t)blockIdx.x * NT + threadIdx.x; i < total; i += (uint64_t)gridDim.x * NT) {
-        gd_vec<T, V> q;
 #pragma unroll
-        for (int j = 0; j < V; ++j) q.v[j] = gd_from_f32<T>(0.0f);
-        const uint64_t row = i / vecs;
-        *reinterpret_cast<gd_vec<T, V>*>(static_cast<T*>(a.weight_grad) + row * a.weight_grad_stride + (i - row * vecs) * V) = q;
+    for (uint32_t r = 0; r < ROUNDS; ++r) {
+        const uint32_t i = base + r * 64 + lane;
+        if (i < a.n) { a.key[0][i] = key[r]; a.pos[0][i] = pos[r]; }
     }
 }
+
+template <typename T, int V>
+__global__ __launch_bounds__(NT) void sort_count(sort_args a, fill_args f) {
+    if (blockIdx.x >= a.blocks) return fill_rows<T, V, NT>(f, blockIdx.x - a.blocks, gridDim.x - a.blocks);
+    __shared__ uint32_t h[DIGITS];
+    for (uint32_t d = threadIdx.x; d < DIGITS; d += NT) h[d] = 0;
+    __syncthreads();
+#pragma unroll
+    for (uint32_t r = 0; r < SORT_KEYS / NT; ++r) {
+        const uint32_t i = blockIdx.x * SORT_KEYS + r * NT + threadIdx.x;
+        if (i < a.n) {
+            const uint32_t key = a.shift ? a.key[a.from][i] : key_of(a.tokens, i, a.vocab);
+            atomicAdd(&h[(key >> a.shift) & (DIGITS - 1)], 1u);
+        }
+    }
+    __syncthreads();
+    for (uint32_t d = threadIdx.x; d < DIGITS; d += NT) a.hist[(uint64_t)blockIdx.x * DIGITS + d] = h[d];
+}
+
+// A digit's counts to the counts of the blocks before each, workgroup d for digit d; its total goes into the
+// row behind the last block's.
+__global__ __launch_bounds__(NT) void sort_scan(uint32_t* h, uint32_t blocks) {
+    __shared__ uint32_t s[NT];
+    uint32_t sum = 0;
+    for (uint32_t base = 0; base < blocks; base += NT) {
+        const uint32_t b = base + threadIdx.x;
+        const uint32_t c = b < blocks ? h[(uint64_t)b * DIGITS + blockIdx.x] : 0;
+        s[threadIdx.x] = c;
+        __syncthreads();
+        for (uint32_t d = 1; d < NT; d <<= 1) {
+            const uint32_t v = threadIdx.x >= d ? s[threadIdx.x - d] : 0;
+            __syncthreads();
+            s[threadIdx.x] += v;
+            __syncthreads();
+        }
+        if (b < blocks) h[(uint64_t)b * DIGITS + blockIdx.x] = sum + s[threadIdx.x] - c;
+        sum += s[NT - 1];
+        __syncthreads();
+    }
+    if (threadIdx.x == 0) h[(uint64_t)blocks * DIGITS + blockIdx.x] = sum;
+}
+
+template <typename T, int V>
+__global__ __launch_bounds__(NT) void sort_scatter(sort_args a, fill_args f) {
+    if (blockIdx.x >= a.blocks) return fill_rows<T, V, NT>(f, blockIdx.x - a.blocks, gridDim.x - a.blocks);
+    constexpr uint32_t WAVES = NT / 64, ROUNDS = SORT_KEYS / NT, PER = DIGITS / NT;
+    __shared__ uint32_t next[WAVES][DIGITS];
+    __shared__ uint32_t part[WAVES];
+    const uint32_t wave = threadIdx.x / 64, lane = threadIdx.x & 63;
+    const uint32_t base = blockIdx.x * SORT_KEYS + wave * (SORT_KEYS / WAVES);
+    for (uint32_t i = threadIdx.x; i < WAVES * DIGITS; i += NT) (&next[0][0])[i] = 0;
+    __syncthreads();
+    uint32_t key[ROUNDS], pos[ROUNDS], before[ROUNDS];
+#pragma unroll
+    for (uint32_t r = 0; r < ROUNDS; ++r) {
+        const uint32_t i = base + r * 64 + lane;
+        key[r] = i < a.n ? (a.shift ? a.key[a.from][i] : key_of(a.tokens, i, a.vocab)) : 0;
+        pos[r] = i < a.n && a.shift ? a.pos[a.from][i] : i;
+    }
+#pragma unroll
+    for (uint32_t r = 0; r < ROUNDS; ++r) {
+        const uint32_t d = (key[r] >> a.shift) & (DIGITS - 1);
+        const bool there = base + r * 64 + lane < a.n;
+        const uint64_t same = same_digit(d, there);
+        const uint32_t mine = (uint32_t)__popcll(same & ((1ull << lane) - 1));
+        before[r] = next[wave][d] + mine;
+        __builtin_amdgcn_wave_barrier();
+        if (there && mine == 0) next[wave][d] += (uint32_t)__popcll(same);
+        __builtin_amdgcn_wave_barrier();
+    }
+    __syncthreads();
+    // lane t has the digits PER * t and on: places of the block's keys, then of each wave's
+    uint32_t total = 0, at[PER], all[PER];
+#pragma unroll
+    for (uint32_t e = 0; e < PER; ++e) {
+        const uint32_t* h = a.hist + threadIdx.x * PER + e;
+        at[e] = a.scanned ? h[(uint64_t)blockIdx.x * DIGITS] : 0;
+        all[e] = a.scanned ? h[(uint64_t)a.blocks * DIGITS] : 0;
+    }
+    if (!a.scanned)
+        for (uint32_t b = 0; b < a.blocks; ++b)
+#pragma unroll
+            for (uint32_t e = 0; e < PER; ++e) {
+                const uint32_t c = a.hist[(uint64_t)b * DIGITS + threadIdx.x * PER + e];
+                all[e] += c;
+                if (b < blockIdx.x) at[e] += c;
+            }
+#pragma unroll
+    for (uint32_t e = 0; e < PER; ++e) total += all[e];
+    uint32_t sum = total;
+#pragma unroll
+    for (uint32_t d = 1; d < 64; d <<= 1) {
+        const uint32_t v = __shfl_up(sum, d);
+        if (lane >= d) sum += v;
+    }
+    if (lane == 63) part[wave] = sum;
+    __syncthreads();
+    sum -= total;
+    for (uint32_t w = 0; w < wave; ++w) sum += part[w];
+#pragma unroll
+    for (uint32_t e = 0; e < PER; ++e) { at[e] += sum; sum += all[e]; }
+#pragma unroll
+    for (uint32_t e = 0; e < PER; ++e)
+#pragma unroll
+        for (uint32_t w = 0; w < WAVES; ++w) {
+            uint32_t& slot = next[w][threadIdx.x * PER + e];
+            const uint32_t c = slot;
+            slot = at[e];
+            at[e] += c;
+        }
+    __syncthreads();
+#pragma unroll
+    for (uint32_t r = 0; r < ROUNDS; ++r)
+        if (base + r * 64 + lane < a.n) {
+            const uint32_t to = next[wave][(key[r] >> a.shift) & (DIGITS - 1)] + before[r];
+            a.key[a.from ^ 1][to] = key[r];
+            a.pos[a.from ^ 1][to] = pos[r];
+        }
+}
+
+template <typename T, int V>
+__global__ __launch_bounds__(NT) void fill_kernel(fill_args f) { fill_rows<T, V, NT>(f, blockIdx.x, gridDim.x); }
+
+// ---- sums over stretches of the sorted list -----------------------------------------------
 
 template <typename T, int V>
 __device__ __forceinline__ void write_sum(const gd_embed_grad_args& a, uint32_t token, uint32_t c, const float sum[V]) {
@@ -193,43 +334,57 @@ __device__ __forceinline__ void write_sum(const gd_embed_grad_args& a, uint32_t 
     *p = q;
 }
 
-// Stretch blockIdx.x, columns by blockIdx.y.  partial: [stretch][2][width], the sums of a token that
-// began before the stretch and of one that goes on behind it.
+// Stretch blockIdx.x of `span` entries, columns by blockIdx.y.  partial: [stretch][2][width], the sums of
+// a token that began before the stretch and of one that goes on behind it.  Rows are asked for BATCH at a
+// time, whatever their tokens.
 template <typename T, int V>
-__global__ __launch_bounds__(NT) void grad_sum(gd_embed_grad_args a, const uint32_t* key, const uint32_t* pos, float* partial,
-                                               uint32_t n) {
+__global__ __launch_bounds__(NT) void grad_sum(gd_embed_grad_args a, const uint32_t* __restrict__ key, const uint32_t* __restrict__ pos,
+                                               float* partial, uint32_t n, uint32_t span) {
     const uint32_t c = (blockIdx.y * NT + threadIdx.x) * V;
-    const uint32_t from = blockIdx.x * SPAN, to = min(from + SPAN, n);
-    if (c >= a.width) return;
-    const uint32_t before = from ? key[from - 1] : NO_ROW, behind = to < n ? key[to] : NO_ROW;
+    const uint32_t from = blockIdx.x * span, to = min(from + span, n);
     const uint32_t begin = key[from];
+    if (begin == a.vocab || c >= a.width) return;             // tokens without a row stand at the end
+    const uint32_t before = from ? key[from - 1] : NO_ROW, behind = to < n ? key[to] : NO_ROW;
+    const T* rows = static_cast<const T*>(a.out_grad) + c;
     float sum[V];
 #pragma unroll
     for (int j = 0; j < V; ++j) sum[j] = 0.0f;
     uint32_t token = begin;
-    for (uint32_t i = from; i < to; ++i) {
-        const uint32_t k = key[i];
-        if (k != token) {
-            if (token == before) {                           // (only the stretch's first token can be)
-                float* p = partial + ((uint64_t)blockIdx.x * 2) * a.width + c;
+    for (uint32_t i0 = from; i0 < to; i0 += BATCH) {
+        uint32_t k[BATCH];
+        gd_vec<T, V> q[BATCH];
 #pragma unroll
-                for (int j = 0; j < V; ++j) p[j] = sum[j];
-            } else {
-                write_sum<T, V>(a, token, c, sum);
-            }
-#pragma unroll
-            for (int j = 0; j < V; ++j) sum[j] = 0.0f;
-            token = k;
+        for (uint32_t b = 0; b < BATCH; ++b) {
+            const uint32_t i = i0 + b;
+            k[b] = i < to ? key[i] : a.vocab;
+            // (one without a row: the stretch's first row once more)
+            q[b] = *reinterpret_cast<const gd_vec<T, V>*>(rows + (uint64_t)pos[k[b] != a.vocab ? i : from] * a.out_grad_stride);
         }
-        if (k == a.vocab) break;                             // tokens without a row stand at the end
-        const gd_vec<T, V> q =
-            *reinterpret_cast<const gd_vec<T, V>*>(static_cast<const T*>(a.out_grad) + (uint64_t)pos[i] * a.out_grad_stride + c);
 #pragma unroll
-        for (int j = 0; j < V; ++j) sum[j] += gd_to_f32(q.v[j]);
+        for (uint32_t b = 0; b < BATCH; ++b) {
+            if (k[b] != token && token != a.vocab) {
+                if (token == before) {                       // (only the stretch's first token can be)
+                    float* p = partial + ((uint64_t)blockIdx.x * 2) * a.width + c;
+#pragma unroll
+                    for (int j = 0; j < V; ++j) p[j] = sum[j];
+                } else if (token == behind) {                // (the stretch's last, at its end)
+                    float* p = partial + ((uint64_t)blockIdx.x * 2 + 1) * a.width + c;
+#pragma unroll
+                    for (int j = 0; j < V; ++j) p[j] = sum[j];
+                } else {
+                    write_sum<T, V>(a, token, c, sum);
+                }
+#pragma unroll
+                for (int j = 0; j < V; ++j) sum[j] = 0.0f;
+            }
+            token = k[b];
+            if (token != a.vocab)
+#pragma unroll
+                for (int j = 0; j < V; ++j) sum[j] += gd_to_f32(q[b].v[j]);
+        }
     }
     if (token == a.vocab) return;
     if (token == behind || token == before) {
-        // goes on behind the stretch (its back) or ends with it (its front)
         float* p = partial + ((uint64_t)blockIdx.x * 2 + (token == before ? 0 : 1)) * a.width + c;
 #pragma unroll
         for (int j = 0; j < V; ++j) p[j] = sum[j];
@@ -240,9 +395,10 @@ __global__ __launch_bounds__(NT) void grad_sum(gd_embed_grad_args a, const uint3
 
 // The token that begins in stretch blockIdx.x and goes on behind it: its parts in order.
 template <typename T, int V>
-__global__ __launch_bounds__(NT) void grad_join(gd_embed_grad_args a, const uint32_t* key, const float* partial, uint32_t n) {
+__global__ __launch_bounds__(NT) void grad_join(gd_embed_grad_args a, const uint32_t* __restrict__ key, const float* __restrict__ partial,
+                                                uint32_t n, uint32_t span) {
     const uint32_t c = (blockIdx.y * NT + threadIdx.x) * V;
-    const uint32_t from = blockIdx.x * SPAN, to = min(from + SPAN, n);
+    const uint32_t from = blockIdx.x * span, to = min(from + span, n);
     if (to >= n || c >= a.width) return;
     const uint32_t token = key[to - 1];
     if (token != key[to] || token == a.vocab) return;
@@ -251,29 +407,46 @@ __global__ __launch_bounds__(NT) void grad_join(gd_embed_grad_args a, const uint
     float sum[V];
 #pragma unroll
     for (int j = 0; j < V; ++j) sum[j] = p[j];
-    for (uint32_t s = blockIdx.x + 1; (uint64_t)s * SPAN < n && key[s * SPAN] == token; ++s) {
-        p = partial + ((uint64_t)s * 2) * a.width + c;
+    // stretches that the token reaches into: a search by doubling, then by halves
+    const uint32_t stretches = (n + span - 1) / span;
+    uint32_t lo = blockIdx.x + 1, hi = lo + 1, step = 1;
+    while (hi < stretches && key[(uint64_t)hi * span] == token) { lo = hi; step *= 2; hi = lo + step; }
+    hi = min(hi, stretches);
+    while (hi - lo > 1) {
+        const uint32_t mid = lo + (hi - lo) / 2;
+        if (key[(uint64_t)mid * span] == token) lo = mid; else hi = mid;
+    }
+    for (uint32_t s0 = blockIdx.x + 1; s0 < hi; s0 += BATCH) {
+        gd_vec<float, V> q[BATCH];
 #pragma unroll
-        for (int j = 0; j < V; ++j) sum[j] += p[j];
+        for (uint32_t b = 0; b < BATCH; ++b)
+            q[b] = *reinterpret_cast<const gd_vec<float, V>*>(partial + (uint64_t)min(s0 + b, hi - 1) * 2 * a.width + c);
+#pragma unroll
+        for (uint32_t b = 0; b < BATCH; ++b)
+            if (s0 + b < hi)
+#pragma unroll
+                for (int j = 0; j < V; ++j) sum[j] += q[b].v[j];
     }
     write_sum<T, V>(a, token, c, sum);
 }
 
 struct grad_layout {
     size_t key[2], pos[2], hist, partial, total;
-    uint32_t blocks;
+    uint32_t blocks, span;
 };
 
 grad_layout layout_of(uint64_t n, uint64_t width) {
     grad_layout l;
     l.blocks = (uint32_t)((n + SORT_KEYS - 1) / SORT_KEYS);
+    // stretches: 1 024 of them, that all CUs have some, between one batch and four
+    l.span = n <= 1024 * BATCH ? BATCH : n <= 2048 * BATCH ? 2 * BATCH : 4 * BATCH;
     size_t o = 0;
     for (int i = 0; i < 2; ++i) {
         l.key[i] = o; o = gd_align256(o + n * 4);
         l.pos[i] = o; o = gd_align256(o + n * 4);
     }
-    l.hist = o;    o = gd_align256(o + (size_t)l.blocks * DIGITS * 4);
-    l.partial = o; o = gd_align256(o + (n + SPAN - 1) / SPAN * 2 * width * 4);
+    l.hist = o;    o = gd_align256(o + (size_t)(l.blocks + 1) * DIGITS * 4);
+    l.partial = o; o = gd_align256(o + (n + l.span - 1) / l.span * 2 * width * 4);
     l.total = o;
     return l;
 }
@@ -282,33 +455,53 @@ template <typename T, int V>
 hipError_t launch_grad(const gd_embed_grad_args& a, hipStream_t s) {
     const uint32_t n = a.tokens.n;
     const grad_layout l = layout_of(n, a.width);
-    if (!a.accumulate) {
-        const uint64_t vecs = (uint64_t)a.vocab * (a.width / V), blocks = (vecs + NT - 1) / NT;
-        hipLaunchKernelGGL((grad_zero<T, V>), dim3((uint32_t)(blocks < 8192 ? blocks : 8192)), dim3(NT), 0, s, a);
+    fill_args f;
+    f.p = a.weight_grad; f.stride = a.weight_grad_stride; f.width = a.width; f.from = 0; f.to = 0;
+    // workgroups that fill: enough for the memory, no more than have 4 KB each to write
+    const auto fillers = [&](const fill_args& g, uint32_t threads) {
+        const uint64_t w = ((uint64_t)(g.to - g.from) * g.width * sizeof(T) + 4095) / 4096, most = 2048 * 256 / threads;
+        return (uint32_t)(w < most ? w : most);
+    };
+    if (n == 0) {
+        if (a.accumulate) return hipSuccess;
+        f.to = a.vocab;
+        hipLaunchKernelGGL((fill_kernel<T, V>), dim3(fillers(f, NT)), dim3(NT), 0, s, f);
+        return hipGetLastError();
     }
-    if (n == 0) return hipGetLastError();
-    sort_buffers b;
+    sort_args b;
     for (int i = 0; i < 2; ++i) {
         b.key[i] = reinterpret_cast<uint32_t*>(a.work + l.key[i]);
         b.pos[i] = reinterpret_cast<uint32_t*>(a.work + l.pos[i]);
     }
     b.hist = reinterpret_cast<uint32_t*>(a.work + l.hist);
-    b.blocks = l.blocks;
-    uint32_t from = 1;
-    bool first = true;
-    for (uint32_t shift = 0; shift == 0 || ((uint64_t)a.vocab >> shift) > 0; shift += 8) {
-        if (first) hipLaunchKernelGGL((sort_count<true>), dim3(l.blocks), dim3(NT), 0, s, b, a.tokens, n, a.vocab, from, shift);
-        else hipLaunchKernelGGL((sort_count<false>), dim3(l.blocks), dim3(NT), 0, s, b, a.tokens, n, a.vocab, from, shift);
-        hipLaunchKernelGGL(sort_scan, dim3(1), dim3(1024), 0, s, b.hist, l.blocks * DIGITS);
-        if (first) hipLaunchKernelGGL((sort_scatter<true>), dim3(l.blocks), dim3(NT), 0, s, b, a.tokens, n, a.vocab, from, shift);
-        else hipLaunchKernelGGL((sort_scatter<false>), dim3(l.blocks), dim3(NT), 0, s, b, a.tokens, n, a.vocab, from, shift);
-        first = false;
-        from ^= 1;
+    b.tokens = a.tokens; b.n = n; b.vocab = a.vocab; b.blocks = l.blocks; b.from = 1; b.shift = 0;
+    uint32_t sorted = 0;
+    if (n <= ONE_SORT) {
+        if (!a.accumulate) f.to = a.vocab;
+        hipLaunchKernelGGL((sort_alone<T, V>), dim3(1 + fillers(f, 1024)), dim3(1024), 0, s, b, f);
+    } else {
+        uint32_t passes = 1;
+        while (((uint64_t)a.vocab >> (passes * BITS)) > 0) ++passes;
+        b.scanned = l.blocks > SELF_SCAN;
+        for (uint32_t i = 0; i < passes; ++i) {
+            b.shift = i * BITS;
+            for (uint32_t half = 0; half < 2; ++half) {       // (each launch fills its share)
+                f.from = f.to;
+                if (!a.accumulate) f.to = (uint32_t)((uint64_t)a.vocab * (2 * i + half + 1) / (2 * passes));
+                const dim3 grid(l.blocks + fillers(f, NT));
+                if (half == 0) hipLaunchKernelGGL((sort_count<T, V>), grid, dim3(NT), 0, s, b, f);
+                else hipLaunchKernelGGL((sort_scatter<T, V>), grid, dim3(NT), 0, s, b, f);
+                if (half == 0 && b.scanned) hipLaunchKernelGGL(sort_scan, dim3(DIGITS), dim3(NT), 0, s, b.hist, l.blocks);
+            }
+            b.from ^= 1;
+        }
+        sorted = b.from;
     }
     float* partial = reinterpret_cast<float*>(a.work + l.partial);
-    const dim3 grid((n + SPAN - 1) / SPAN, (a.width + NT * V - 1) / (NT * V));
-    hipLaunchKernelGGL((grad_sum<T, V>), grid, dim3(NT), 0, s, a, b.key[from], b.pos[from], partial, n);
-    hipLaunchKernelGGL((grad_join<T, V>), grid, dim3(NT), 0, s, a, b.key[from], partial, n);
+    const dim3 grid((n + l.span - 1) / l.span, (a.width + NT * V - 1) / (NT * V));
+    hipLaunchKernelGGL((grad_sum<T, V>), grid, dim3(NT), 0, s, a, b.key[sorted], b.pos[sorted], partial, n, l.span);
+    if (n > l.span)
+        hipLaunchKernelGGL((grad_join<T, V>), grid, dim3(NT), 0, s, a, b.key[sorted], partial, n, l.span);
     return hipGetLastError();
 }
 
