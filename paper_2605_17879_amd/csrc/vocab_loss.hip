@@ -18,6 +18,8 @@
 // Tiles are staged with loads that go from memory straight to the LDS, into one of two buffers while
 // the other is multiplied.  Places in the LDS are exchanged by exclusive or within a row, so that reads
 // of eight or sixteen rows at one k fall on different banks.
+#include <type_traits>
+
 #include "gd_lanes.h"
 #include "gd_operators.h"
 
@@ -58,7 +60,7 @@ struct operand {
 // Written by prepare_rows for the launches of the gradients.
 struct grad_head {
     uint32_t count;      // rows with a gradient
-    float back;          // what the products with G have to be multiplied by
+    float back, more;    // what the products with G have to be multiplied by
 };
 
 struct product_args {
@@ -82,6 +84,7 @@ struct product_args {
     uint64_t slab;                  // elements between two slabs of dH
     uint32_t add;                   // dH: add to what is there
     uint32_t splits;                // dH: parts of k, a slab each
+    uint32_t large;                 // tiles of 256 x 256 instead of 128 x 128 (the host's choice)
 };
 
 enum { EPI_LSE, EPI_G, EPI_SLAB, EPI_OUT };
@@ -102,8 +105,9 @@ struct stager {
     uint32_t pitch;                               // bytes between rows
     uint32_t last;                                // chunks (ALONG_K) or rows that are there from k0 on, less one
 
-    // first: the tile's first row (ALONG_K) or column.  k0 < cols where rows lie along k.
-    __device__ __forceinline__ void init(const operand& o, uint32_t first, uint32_t k0) {
+    // first: the tile's first row (ALONG_K) or column, a row that is there; ROWS rows from first + more on are
+    // staged.  k0 < cols where rows lie along k.
+    __device__ __forceinline__ void init(const operand& o, uint32_t first, uint32_t more, uint32_t k0) {
         pitch = (uint32_t)o.stride * 2;
         base = static_cast<const uint8_t*>(o.p) + (ALONG_K ? (uint64_t)first * pitch + (uint64_t)k0 * 2 : 0);
         last = ALONG_K ? (o.cols - k0) / 8 - 1 : o.rows - 1;
@@ -113,10 +117,10 @@ struct stager {
             if (ALONG_K) {
                 const uint32_t r = i / 8;
                 place[j] = (i & 7) ^ (r & 7);
-                at[j] = min(r, o.rows - 1 - first) * pitch;
+                at[j] = min(more + r, o.rows - 1 - first) * pitch;
             } else {
                 place[j] = i / (ROWS / 8);
-                at[j] = min(first / 8 + ((i % (ROWS / 8)) ^ (turn(place[j]) % (ROWS / 8))), o.cols / 8 - 1) * 16;
+                at[j] = min((first + more) / 8 + ((i % (ROWS / 8)) ^ (turn(place[j]) % (ROWS / 8))), o.cols / 8 - 1) * 16;
             }
         }
     }
@@ -170,14 +174,230 @@ __device__ __forceinline__ void tile_of(uint32_t b, uint32_t tiles_m, uint32_t t
     tm = in / width;
 }
 
-template <typename T, int BM, int BN, int WM, int WN, bool A_ALONG, bool B_ALONG, int EPI>
-__global__ __launch_bounds__(WM* WN * 64) void product_kernel(const product_args p) {
-    constexpr int NT = WM * WN * 64, FM = BM / WM / 16, FN = BN / WN / 16;
+// The sum over k for tiles of 128 x 128 by four waves, two workgroups a CU.  Sixteen rows of A at a
+// time (a step) are multiplied by all of the wave's columns, over the first half of the block's k, then the
+// second.  A's fragments are read AHEAD steps before they are multiplied, B's half a block before; the
+// last steps of a block already read from the next one, so that the matrix cores do not wait for the LDS
+// behind the barrier.
+template <typename T, bool A_ALONG, bool B_ALONG>
+struct small_tile {
+    static constexpr int BM = 128, BN = 128, WM = 2, WN = 2, NT = 256, FM = 4, FN = 4;
     typedef typename of_type<T>::x8 X8;
-    // (one array a buffer, so that the compiler knows which loads a read has to wait for)
-    __shared__ __attribute__((aligned(16))) uint8_t sa0[BM * BK * 2], sb0[BN * BK * 2];
-    __shared__ __attribute__((aligned(16))) uint8_t sa1[BM * BK * 2], sb1[BN * BK * 2];
 
+    // Rows (columns) of the tile that fragment i of wave wm (j of wn) begins at.
+    static __device__ __forceinline__ uint32_t row_of(uint32_t wm, int i) { return wm * 64 + i * 16; }
+    static __device__ __forceinline__ uint32_t col_of(uint32_t wn, int j) { return wn * 64 + j * 16; }
+
+    static __device__ __forceinline__ void run(const operand& oa, const operand& ob, uint32_t m0, uint32_t n0, uint32_t kfirst,
+                                               uint32_t blocks, uint32_t ends, f32x4 (&acc)[FM][FN]) {
+        // (one array a buffer, so that the compiler knows which loads a read has to wait for)
+        __shared__ __attribute__((aligned(16))) uint8_t sa0[BM * BK * 2], sb0[BN * BK * 2];
+        __shared__ __attribute__((aligned(16))) uint8_t sa1[BM * BK * 2], sb1[BN * BK * 2];
+        const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+        const uint32_t wm = wave / WN, wn = wave % WN;
+        stager<BM, A_ALONG, NT> la;
+        stager<BN, B_ALONG, NT> lb;
+        la.init(oa, m0, 0, kfirst * BK);
+        lb.init(ob, n0, 0, kfirst * BK);
+        auto stage = [&](uint8_t* a, uint8_t* b, uint32_t kt) {
+            la.stage(a, kfirst * BK, kt);
+            lb.stage(b, kfirst * BK, kt);
+        };
+        auto end_rows = [&](uint8_t* a, uint8_t* b) {
+            for (uint32_t i = threadIdx.x; i < BM * 8; i += NT)
+                if (((i & 7) ^ ((i >> 3) & 7)) * 8 >= ends) *reinterpret_cast<X8*>(a + i * 16) = X8(0);
+            for (uint32_t i = threadIdx.x; i < BN * 8; i += NT)
+                if (((i & 7) ^ ((i >> 3) & 7)) * 8 >= ends) *reinterpret_cast<X8*>(b + i * 16) = X8(0);
+            __syncthreads();
+        };
+        constexpr int STEPS = 2 * FM, AHEAD = 3, RING = AHEAD + 1;
+        static_assert(STEPS % RING == 0, "fragments keep their registers from block to block");
+        X8 fa[RING], fb[2][FN];
+        auto read_a = [&](const uint8_t* a, int s) { fa[s % RING] = fragment<BM, A_ALONG, X8>(a, row_of(wm, s % FM), s / FM, lane); };
+        auto read_b = [&](const uint8_t* b, int half) {
+#pragma unroll
+            for (int j = 0; j < FN; ++j) fb[half][j] = fragment<BN, B_ALONG, X8>(b, col_of(wn, j), half, lane);
+        };
+        // Block kt from (a, b), then the first fragments of the one behind it from (na, nb): where there is none
+        // they are read for nothing.
+        auto block = [&](uint8_t* a, uint8_t* b, uint8_t* na, uint8_t* nb, uint32_t kt) {
+#pragma unroll
+            for (int s = 0; s < STEPS; ++s) {
+                if (s == 1) read_b(b, 1);
+                if (s + AHEAD == STEPS) {
+                    __syncthreads();                         // (the next block is there, this one read by all)
+                    if (ends != 0 && kt + 2 == blocks) end_rows(na, nb);
+                    if (kt + 2 < blocks) stage(a, b, kt + 2);
+                    read_b(nb, 0);
+                }
+                if (s + AHEAD < STEPS) read_a(a, s + AHEAD);
+                else read_a(na, s + AHEAD - STEPS);
+#pragma unroll
+                for (int j = 0; j < FN; ++j) acc[s % FM][j] = multiply(fa[s % RING], fb[s / FM][j], acc[s % FM][j]);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        };
+        // blocks go through the buffers in turn and end with the second one
+        uint32_t kt = blocks & 1;
+        auto start = [&](uint8_t* a, uint8_t* b, uint8_t* na, uint8_t* nb) {
+            stage(a, b, 0);
+            __syncthreads();
+            if (ends != 0 && blocks == 1) end_rows(a, b);
+            if (blocks > 1) stage(na, nb, 1);
+            read_b(b, 0);
+#pragma unroll
+            for (int s = 0; s < AHEAD; ++s) read_a(a, s);
+        };
+        if (kt) {
+            start(sa1, sb1, sa0, sb0);
+            block(sa1, sb1, sa0, sb0, 0);
+        } else {
+            start(sa0, sb0, sa1, sb1);
+        }
+        for (; kt < blocks; kt += 2) {
+            block(sa0, sb0, sa1, sb1, kt);
+            block(sa1, sb1, sa0, sb0, kt + 1);
+        }
+    }
+};
+
+// The sum over k for tiles of 256 x 256 by eight waves, one workgroup a CU, two waves a SIMD that take
+// turns: while the waves of one group multiply, those of the other read their operands from the LDS, and
+// a barrier changes the roles.  A block of 64 k takes two turns of a wave: B and the upper half of A's rows,
+// then the lower half.  The buffers of B and of A's upper half are free again behind the first turn and are
+// filled for the block after the next at once, those of the lower half behind the second: every load has
+// three turns of both groups, one and a half blocks, to arrive.
+//
+//   turn          g0 reads    g1 reads     loads issued (each group in its reading turn)
+//   4 kt          B, upper    (lower kt-1) g0: lower kt+1
+//   4 kt + 1                  B, upper     g1: lower kt+1
+//   4 kt + 2      lower                    g0: B, upper kt+2
+//   4 kt + 3                  lower        g1: B, upper kt+2
+//
+// A wave has eight loads a block.  What is read in turns 4 kt and on was issued before the latest eight; the wait
+// stands before the barrier in front of the even turns, which g0 reaches multiplying and g1 reading.
+template <typename T, bool A_ALONG, bool B_ALONG>
+struct large_tile {
+    static constexpr int BM = 256, BN = 256, WM = 2, WN = 4, NT = 512, FM = 8, FN = 4;
+    typedef typename of_type<T>::x8 X8;
+
+    static __device__ __forceinline__ uint32_t row_of(uint32_t wm, int i) { return (i / 4) * 128 + wm * 64 + (i % 4) * 16; }
+    static __device__ __forceinline__ uint32_t col_of(uint32_t wn, int j) { return wn * 64 + j * 16; }
+
+    // s_waitcnt operands: all but `n` loads (n below 16); all LDS reads
+    static constexpr int loads_but(int n) { return 0x0F70 | n; }
+    static constexpr int LDS_READ = 0xC07F;
+
+    static __device__ __forceinline__ void run(const operand& oa, const operand& ob, uint32_t m0, uint32_t n0, uint32_t kfirst,
+                                               uint32_t blocks, uint32_t ends, f32x4 (&acc)[FM][FN]) {
+        __shared__ __attribute__((aligned(16))) uint8_t up0[128 * BK * 2], low0[128 * BK * 2], sb0[BN * BK * 2];
+        __shared__ __attribute__((aligned(16))) uint8_t up1[128 * BK * 2], low1[128 * BK * 2], sb1[BN * BK * 2];
+        const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+        const uint32_t wm = wave / WN, wn = wave % WN, group = wm;   // (waves w and w + 4 share a SIMD)
+        stager<128, A_ALONG, NT> lu, ll;
+        stager<BN, B_ALONG, NT> lb;
+        lu.init(oa, m0, 0, kfirst * BK);
+        ll.init(oa, m0, 128, kfirst * BK);
+        lb.init(ob, n0, 0, kfirst * BK);
+        X8 fa[4][2], fb[FN][2];
+        auto read_a = [&](const uint8_t* a) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) fa[i][h] = fragment<128, A_ALONG, X8>(a, wm * 64 + i * 16, h, lane);
+        };
+        auto read_b = [&](const uint8_t* b) {
+#pragma unroll
+            for (int j = 0; j < FN; ++j)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) fb[j][h] = fragment<BN, B_ALONG, X8>(b, col_of(wn, j), h, lane);
+        };
+        // what lies behind the end of k: zeros
+        auto cut = [&](X8 (&f)[4][2]) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (uint32_t h = 0; h < 2; ++h)
+                    if (h * 32 + (lane >> 4) * 8 >= ends) f[i][h] = X8(0);
+        };
+        // `newer`: how many of the wave's loads were issued behind those that the next turn reads
+        auto turn_over = [&](bool wait, uint32_t newer) {
+            asm volatile("" ::: "memory");
+            if (wait) {
+                if (newer == 8) __builtin_amdgcn_s_waitcnt(loads_but(8));
+                else if (newer == 2) __builtin_amdgcn_s_waitcnt(loads_but(2));
+                else __builtin_amdgcn_s_waitcnt(loads_but(0));
+            }
+            __builtin_amdgcn_s_barrier();
+            asm volatile("" ::: "memory");
+            __builtin_amdgcn_sched_barrier(0);
+        };
+        auto multiply_half = [&](int first) {
+            __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int j = 0; j < FN; ++j) acc[first + i][j] = multiply(fa[i][h], fb[j][h], acc[first + i][j]);
+            __builtin_amdgcn_s_setprio(0);
+            __builtin_amdgcn_sched_barrier(0);
+        };
+        auto block = [&](uint8_t* up, uint8_t* low, uint8_t* b, uint8_t* nlow, uint32_t kt) {
+            const bool tail = ends != 0 && kt + 1 == blocks;
+            const uint32_t newer_up = kt + 1 < blocks ? 8 : 0, newer_low = kt + 2 < blocks ? 8 : kt + 1 < blocks ? 2 : 0;
+            read_b(b);
+            read_a(up);
+            if (kt > 0 && kt + 1 < blocks) ll.stage(nlow, kfirst * BK, kt + 1);
+            if (tail) { cut(fa); cut(fb); }
+            __builtin_amdgcn_s_waitcnt(LDS_READ);
+            turn_over(group == 1, newer_up);
+            multiply_half(0);
+            turn_over(group == 0, newer_up);
+            read_a(low);
+            if (kt + 2 < blocks) {
+                lb.stage(b, kfirst * BK, kt + 2);
+                lu.stage(up, kfirst * BK, kt + 2);
+            }
+            if (tail) cut(fa);
+            __builtin_amdgcn_s_waitcnt(LDS_READ);
+            turn_over(group == 1, newer_low);
+            multiply_half(4);
+            turn_over(group == 0, newer_low);
+        };
+        auto start = [&](uint8_t* up, uint8_t* low, uint8_t* b, uint8_t* nup, uint8_t* nlow, uint8_t* nb) {
+            lb.stage(b, kfirst * BK, 0);
+            lu.stage(up, kfirst * BK, 0);
+            ll.stage(low, kfirst * BK, 0);
+            if (blocks > 1) {
+                lb.stage(nb, kfirst * BK, 1);
+                lu.stage(nup, kfirst * BK, 1);
+                ll.stage(nlow, kfirst * BK, 1);
+                __builtin_amdgcn_s_waitcnt(loads_but(8));
+            } else {
+                __builtin_amdgcn_s_waitcnt(loads_but(0));
+            }
+            turn_over(false, 0);
+            if (group == 1) turn_over(false, 0);             // one turn behind
+        };
+        uint32_t kt = blocks & 1;
+        if (kt) {
+            start(up1, low1, sb1, up0, low0, sb0);
+            block(up1, low1, sb1, low0, 0);
+        } else {
+            start(up0, low0, sb0, up1, low1, sb1);
+        }
+        for (; kt < blocks; kt += 2) {
+            block(up0, low0, sb0, low1, kt);
+            block(up1, low1, sb1, low0, kt + 1);
+        }
+        if (group == 0) turn_over(false, 0);
+    }
+};
+
+template <typename T, typename TILE, int EPI>
+__global__ __launch_bounds__(TILE::NT, 512 / TILE::NT) void product_kernel(const product_args p) {
+    constexpr int BM = TILE::BM, BN = TILE::BN, WM = TILE::WM, WN = TILE::WN, FM = TILE::FM, FN = TILE::FN;
     uint32_t tm, tn;
     tile_of(blockIdx.x, p.tiles_m, p.tiles_n, tm, tn);
     uint32_t n = p.n, k = p.k;
@@ -191,7 +411,6 @@ __global__ __launch_bounds__(WM* WN * 64) void product_kernel(const product_args
         kfirst = min(blocks, blockIdx.y * per);
         blocks = min(per, blocks - kfirst);
     }
-
     const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const uint32_t wm = wave / WN, wn = wave % WN;
     f32x4 acc[FM][FN];
@@ -199,69 +418,28 @@ __global__ __launch_bounds__(WM* WN * 64) void product_kernel(const product_args
     for (int i = 0; i < FM; ++i)
 #pragma unroll
         for (int j = 0; j < FN; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-
-    if (blocks > 0) {
-        stager<BM, A_ALONG, NT> la;
-        stager<BN, B_ALONG, NT> lb;
-        la.init(p.a, m0, kfirst * BK);
-        lb.init(p.b, n0, kfirst * BK);
-        // operands that lie along k end where their rows do
-        const uint32_t ends = (A_ALONG && B_ALONG && EPI != EPI_SLAB) ? k % BK : 0;
-        auto stage = [&](uint8_t* a, uint8_t* b, uint32_t kt) {
-            la.stage(a, kfirst * BK, kt);
-            lb.stage(b, kfirst * BK, kt);
-        };
-        auto compute = [&](const uint8_t* a, const uint8_t* b, uint32_t kt) {
-            const bool tail = ends != 0 && kt == blocks - 1;
-#pragma unroll
-            for (uint32_t half = 0; half < 2; ++half) {
-                X8 fa[FM], fb[FN];
-#pragma unroll
-                for (int j = 0; j < FN; ++j) fb[j] = fragment<BN, B_ALONG, X8>(b, wn * (BN / WN) + j * 16, half, lane);
-#pragma unroll
-                for (int i = 0; i < FM; ++i) fa[i] = fragment<BM, A_ALONG, X8>(a, wm * (BM / WM) + i * 16, half, lane);
-                if (tail && half * 32 + (lane >> 4) * 8 >= ends) {
-#pragma unroll
-                    for (int j = 0; j < FN; ++j) fb[j] = X8(0);
-#pragma unroll
-                    for (int i = 0; i < FM; ++i) fa[i] = X8(0);
-                }
-#pragma unroll
-                for (int i = 0; i < FM; ++i)
-#pragma unroll
-                    for (int j = 0; j < FN; ++j) acc[i][j] = multiply(fa[i], fb[j], acc[i][j]);
-            }
-        };
-        stage(sa0, sb0, 0);
-        for (uint32_t kt = 0; kt < blocks; kt += 2) {
-            __syncthreads();
-            if (kt + 1 < blocks) stage(sa1, sb1, kt + 1);
-            __builtin_amdgcn_sched_barrier(0);
-            compute(sa0, sb0, kt);
-            if (kt + 1 < blocks) {
-                __syncthreads();
-                if (kt + 2 < blocks) stage(sa0, sb0, kt + 2);
-                __builtin_amdgcn_sched_barrier(0);
-                compute(sa1, sb1, kt + 1);
-            }
-        }
-    }
+    // operands that lie along k end where their rows do
+    if (blocks > 0)
+        TILE::run(p.a, p.b, m0, n0, kfirst, blocks, EPI == EPI_LSE || EPI == EPI_G ? k % BK : 0, acc);
 
     // lane l holds rows 4 (l / 16) + 0..3 and column l % 16 of each 16 x 16 block
-    const uint32_t mw = m0 + wm * (BM / WM) + (lane >> 4) * 4, nw = n0 + wn * (BN / WN) + (lane & 15);
+    uint32_t row[FM], col[FN];
+#pragma unroll
+    for (int i = 0; i < FM; ++i) row[i] = m0 + TILE::row_of(wm, i) + (lane >> 4) * 4;
+#pragma unroll
+    for (int j = 0; j < FN; ++j) col[j] = n0 + TILE::col_of(wn, j) + (lane & 15);
     if (EPI == EPI_LSE) {
-        __syncthreads();
-        float2* join = reinterpret_cast<float2*>(sa0);               // [WM][BN]
+        __shared__ float2 join[WM * BN];
 #pragma unroll
         for (int j = 0; j < FN; ++j) {
-            const uint32_t i = nw + j * 16;
+            const uint32_t i = col[j];
             const int64_t t = i < n ? gd_token(p.targets, i) : -1;
             float top = -__builtin_inff();
 #pragma unroll
             for (int f = 0; f < FM; ++f)
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
-                    const uint32_t v = p.v0 + mw + f * 16 + r;
+                    const uint32_t v = p.v0 + row[f] + r;
                     if (v < p.vocab) {
                         if (t == (int64_t)v) p.target_logit[i] = acc[f][j][r] * p.scale;
                         acc[f][j][r] *= p.scale2;
@@ -280,7 +458,7 @@ __global__ __launch_bounds__(WM* WN * 64) void product_kernel(const product_args
                 for (int r = 0; r < 4; ++r) sum += __builtin_amdgcn_exp2f(acc[f][j][r] - from);
             sum += __uint_as_float(gd_lane_xor<16>(__float_as_uint(sum), lane));
             sum += __uint_as_float(gd_lane_xor<32>(__float_as_uint(sum), lane));
-            if (lane < 16) join[wm * BN + wn * (BN / WN) + j * 16 + lane] = make_float2(top, sum);
+            if (lane < 16) join[wm * BN + TILE::col_of(wn, j) + lane] = make_float2(top, sum);
         }
         __syncthreads();
         if (threadIdx.x < BN && n0 + threadIdx.x < n) {
@@ -298,32 +476,32 @@ __global__ __launch_bounds__(WM* WN * 64) void product_kernel(const product_args
         T* g = static_cast<T*>(p.c);
 #pragma unroll
         for (int j = 0; j < FN; ++j) {
-            const uint32_t i = nw + j * 16;                          // (there is room for whole tiles of rows)
-            const bool row = i < n;
-            const float lse2 = row ? p.row_lse2[i] : 0.0f, coef = row ? p.row_coef[i] : 0.0f;
-            const int32_t t = row ? p.row_target[i] : -1;
+            const uint32_t i = col[j];                          // (there is room for whole tiles of rows)
+            const bool there = i < n;
+            const float lse2 = there ? p.row_lse2[i] : 0.0f, coef = there ? p.row_coef[i] : 0.0f;
+            const int32_t t = there ? p.row_target[i] : -1;
 #pragma unroll
             for (int f = 0; f < FM; ++f) {
                 gd_vec<T, 4> q;
-                const uint32_t v = p.v0 + mw + f * 16;
+                const uint32_t v = p.v0 + row[f];
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
                     float e = exp2f(acc[f][j][r] * p.scale2 - lse2);    // (the instruction alone drops subnormal results)
                     if ((int32_t)(v + r) == t) e -= 1.0f;
-                    q.v[r] = gd_from_f32<T>(row && v + r < p.vocab ? coef * e : 0.0f);
+                    q.v[r] = gd_from_f32<T>(there && v + r < p.vocab ? coef * e : 0.0f);
                 }
-                *reinterpret_cast<gd_vec<T, 4>*>(g + (uint64_t)i * p.ldc + mw + f * 16) = q;
+                *reinterpret_cast<gd_vec<T, 4>*>(g + (uint64_t)i * p.ldc + row[f]) = q;
             }
         }
     } else if (EPI == EPI_SLAB) {
         float* c = static_cast<float*>(p.c) + blockIdx.y * p.slab;
 #pragma unroll
         for (int j = 0; j < FN; ++j) {
-            const uint32_t i = nw + j * 16;
+            const uint32_t i = col[j];
             if (i >= n) continue;
 #pragma unroll
             for (int f = 0; f < FM; ++f) {
-                const uint32_t e = mw + f * 16;                      // slabs are padded to four columns
+                const uint32_t e = row[f];                      // slabs are padded to four columns
                 if (e >= p.m) continue;
                 f32x4* to = reinterpret_cast<f32x4*>(c + (uint64_t)i * p.ldc + e);
                 *to = p.add ? *to + acc[f][j] : acc[f][j];
@@ -331,24 +509,24 @@ __global__ __launch_bounds__(WM* WN * 64) void product_kernel(const product_args
         }
     } else {
         T* c = static_cast<T*>(p.c);
-        const float back = p.head->back * p.scale;
+        const float back = p.head->back, more = p.head->more * p.scale;
 #pragma unroll
         for (int j = 0; j < FN; ++j) {
-            const uint32_t i = nw + j * 16;
+            const uint32_t i = col[j];
             if (i >= p.n) continue;
 #pragma unroll
             for (int f = 0; f < FM; ++f) {
-                const uint32_t e = mw + f * 16;
+                const uint32_t e = row[f];
                 T* to = c + (uint64_t)i * p.ldc + e;
                 if (e + 4 <= p.m && (p.ldc & 3) == 0 && ((uintptr_t)c & 7) == 0) {
                     gd_vec<T, 4> q;
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) q.v[r] = gd_from_f32<T>(acc[f][j][r] * back);
+                    for (int r = 0; r < 4; ++r) q.v[r] = gd_from_f32<T>(acc[f][j][r] * back * more);
                     *reinterpret_cast<gd_vec<T, 4>*>(to) = q;
                 } else {
 #pragma unroll
                     for (uint32_t r = 0; r < 4; ++r)
-                        if (e + r < p.m) to[r] = gd_from_f32<T>(acc[f][j][r] * back);
+                        if (e + r < p.m) to[r] = gd_from_f32<T>(acc[f][j][r] * back * more);
                 }
             }
         }
@@ -383,11 +561,11 @@ __global__ __launch_bounds__(256) void pack_kernel(const void* in, uint64_t stri
 }
 
 // The tiles' sums of a row joined, one wave a row.
-__global__ __launch_bounds__(256) void join_kernel(const float2* part, uint32_t parts, gd_token_list targets, uint32_t vocab,
+__global__ __launch_bounds__(256) void join_kernel(const float2* part, uint32_t stride, uint32_t parts, gd_token_list targets, uint32_t vocab,
                                                    const float* target_logit, float* loss, float* lse) {
     const uint32_t i = blockIdx.x * 4 + threadIdx.x / 64, lane = threadIdx.x & 63;
     if (i >= targets.n) return;
-    const float2* q = part + (uint64_t)i * parts;
+    const float2* q = part + (uint64_t)i * stride;
     float top = -__builtin_inff();
     bool nan = false;
     for (uint32_t c = lane; c < parts; c += 64) { top = fmaxf(top, q[c].x); nan |= q[c].x != q[c].x; }
@@ -458,9 +636,9 @@ __device__ __forceinline__ float coef_of(const rows_args& a, uint32_t i) {
 
 // Lists the rows with a gradient and works out what their tiles need.  One workgroup: the list is in
 // order of the rows.  Gradients of a mean over many rows, and of improbable words, would underflow as G
-// is rounded to 16 bits: coefficients are divided by the power of two of the largest one and multiplied by
-// 2^14 in f16 (G is below 2^15 then) and by 2^40 in bf16 (where every probability that fp32 holds stays
-// a normal number), which `back` undoes behind the products; both are exact.
+// is rounded to 16 bits, and the -1 at the target would be rounded as well: coefficients are divided by the
+// largest one and multiplied by 2^15 in f16 (G is at most that then) and by 2^40 in bf16 (where every
+// probability that fp32 holds stays a normal number), which is undone behind the products.
 __global__ __launch_bounds__(1024) void prepare_rows(const rows_args a) {
     __shared__ uint32_t s[16];
     const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x / 64, n = a.targets.n;
@@ -473,13 +651,8 @@ __global__ __launch_bounds__(1024) void prepare_rows(const rows_args a) {
     __syncthreads();
     for (int w = 0; w < 16; ++w) top = max(top, s[w]);
     __syncthreads();
-    // the largest power of two not above the largest coefficient (bounded so that all factors are normal)
-    float up = 1.0f, back = 1.0f;
-    if (top < 0x7F800000u && top != 0) {
-        const uint32_t e = min(max(top >> 23, 80u), 222u), more = a.half ? 14 : 40;
-        up = __uint_as_float((254u - e) << 23) * __uint_as_float((127u + more) << 23);
-        back = __uint_as_float(e << 23) * __uint_as_float((127u - more) << 23);
-    }
+    const float most = __uint_as_float(top), power = a.half ? 32768.0f : 1099511627776.0f;
+    const bool fine = top < 0x7F800000u && top != 0;
     uint32_t count = 0;
     for (uint32_t base = 0; base < n; base += 1024) {
         const uint32_t i = base + threadIdx.x;
@@ -494,13 +667,18 @@ __global__ __launch_bounds__(1024) void prepare_rows(const rows_args a) {
         if (in) {
             a.rows[at] = i;
             a.row_lse2[at] = a.lse[i] * LOG2E;
-            a.row_coef[at] = c * up;
+            a.row_coef[at] = fine ? c / most * power : c;
             a.row_target[at] = (int32_t)gd_token(a.targets, i);
         }
         if (i < n) a.slot[i] = in ? (int32_t)at : -1;
         __syncthreads();
     }
-    if (threadIdx.x == 0) { a.head->count = count; a.head->back = back; }
+    if (threadIdx.x == 0) {
+        // (two factors, so that neither is subnormal)
+        a.head->count = count;
+        a.head->back = fine ? (most >= 1.0f ? most / power : 1.0f / power) : 1.0f;
+        a.head->more = fine && most < 1.0f ? most : 1.0f;
+    }
 }
 
 // dH from its slabs, added up in order; zeros where a row has no gradient.
@@ -508,14 +686,14 @@ template <typename T>
 __global__ __launch_bounds__(256) void finish_hidden(const float* slabs, uint32_t lds, uint64_t slab, uint32_t splits,
                                                      const grad_head* head, const int32_t* slot, float scale, uint32_t n,
                                                      uint32_t width, T* out, uint64_t ldo) {
-    const float back = head->back * scale;
+    const float back = head->back, more = head->more * scale;
     for (uint32_t i = blockIdx.x; i < n; i += gridDim.x) {
         const int32_t at = slot[i];
         for (uint32_t c = threadIdx.x; c < width; c += 256) {
             float sum = 0.0f;
             if (at >= 0)
                 for (uint32_t s = 0; s < splits; ++s) sum += slabs[s * slab + (uint64_t)at * lds + c];
-            out[(uint64_t)i * ldo + c] = gd_from_f32<T>(sum * back);
+            out[(uint64_t)i * ldo + c] = gd_from_f32<T>(sum * back * more);
         }
     }
 }
@@ -584,15 +762,22 @@ loss_layout layout_of(uint64_t n, uint64_t vocab, uint64_t width, bool with_grad
 
 bool direct(const void* p, uint64_t stride, uint64_t width) { return (uintptr_t)p % 16 == 0 && stride % 8 == 0 && width % 8 == 0; }
 
+template <typename T, typename TILE, int EPI>
+void launch_tiles(product_args& p, hipStream_t s) {
+    p.tiles_m = (p.m + TILE::BM - 1) / TILE::BM;
+    p.tiles_n = (p.n + TILE::BN - 1) / TILE::BN;
+    if (EPI != EPI_SLAB) p.splits = 1;
+    hipLaunchKernelGGL((product_kernel<T, TILE, EPI>), dim3(p.tiles_m * p.tiles_n, p.splits), dim3(TILE::NT), 0, s, p);
+}
+
 template <typename T, bool A_ALONG, bool B_ALONG, int EPI>
 void launch_product(product_args& p, hipStream_t s) {
-    constexpr int B = 128;
-    p.tiles_m = (p.m + B - 1) / B;
-    p.tiles_n = (p.n + B - 1) / B;
-    if (EPI != EPI_SLAB) p.splits = 1;
-    hipLaunchKernelGGL((product_kernel<T, B, B, 2, 2, A_ALONG, B_ALONG, EPI>), dim3(p.tiles_m * p.tiles_n, p.splits), dim3(256), 0,
-                       s, p);
+    if (p.large) launch_tiles<T, large_tile<T, A_ALONG, B_ALONG>, EPI>(p, s);
+    else launch_tiles<T, small_tile<T, A_ALONG, B_ALONG>, EPI>(p, s);
 }
+
+// Tiles of 256 x 256 (half the reads of an operand, one workgroup a CU) where there are some for all CUs.
+bool large_tiles(uint64_t m, uint64_t n) { return up_to(m, 256) / 256 * (up_to(n, 256) / 256) >= 256; }
 
 template <typename T>
 hipError_t forward(const gd_vocab_loss_args& a, hipStream_t s) {
@@ -625,10 +810,13 @@ hipError_t forward(const gd_vocab_loss_args& a, hipStream_t s) {
             p.a = operand{weight, ldh, here, ldh};
         }
         p.k = p.a.cols < p.b.cols ? p.b.cols : p.a.cols;
-        p.m = here; p.v0 = v0; p.part0 = v0 / 128;
+        p.m = here; p.v0 = v0;
+        p.large = large_tiles(piece, n);
+        p.part0 = v0 / (p.large ? 256 : 128);
         launch_product<T, true, true, EPI_LSE>(p, s);
     }
-    hipLaunchKernelGGL(join_kernel, dim3((n + 3) / 4), dim3(256), 0, s, p.part, p.parts, a.targets, a.vocab, p.target_logit, a.loss, a.lse);
+    const uint32_t tiles = (a.vocab + (p.large ? 255 : 127)) / (p.large ? 256 : 128);
+    hipLaunchKernelGGL(join_kernel, dim3((n + 3) / 4), dim3(256), 0, s, p.part, p.parts, tiles, a.targets, a.vocab, p.target_logit, a.loss, a.lse);
     hipLaunchKernelGGL(mean_kernel, dim3(1), dim3(1024), 0, s, a.loss, a.targets, a.mean);
     return hipGetLastError();
 }
@@ -677,8 +865,9 @@ hipError_t backward(const gd_vocab_grad_args& a, hipStream_t s) {
         p.scale2 = a.scale * LOG2E; p.v0 = v0; p.vocab = a.vocab;
         p.row_lse2 = r.row_lse2; p.row_coef = r.row_coef; p.row_target = r.row_target;
         p.c = g; p.ldc = piece;
+        p.large = large_tiles(piece, n);
         launch_product<T, true, true, EPI_G>(p, s);
-        const uint32_t padded_here = (uint32_t)up_to(here, 128);     // what the tiles of G have written
+        const uint32_t padded_here = (uint32_t)up_to(here, p.large ? 256 : 128);     // what the tiles of G have written
         if (a.hidden_grad) {
             product_args q = {};
             q.head = head;
@@ -686,6 +875,7 @@ hipError_t backward(const gd_vocab_grad_args& a, hipStream_t s) {
             q.b = go;
             q.m = a.width; q.n = n; q.k = padded_here;
             q.c = slabs; q.ldc = lds; q.slab = l.slab; q.add = v0 > 0; q.splits = (uint32_t)l.splits;
+            q.large = large_tiles(q.m, q.n);
             launch_product<T, false, true, EPI_SLAB>(q, s);
         }
         if (a.weight_grad) {
@@ -696,6 +886,7 @@ hipError_t backward(const gd_vocab_grad_args& a, hipStream_t s) {
             q.m = a.width; q.n = here; q.k = n;
             q.scale = a.scale;
             q.c = static_cast<T*>(a.weight_grad) + (uint64_t)v0 * a.weight_grad_stride; q.ldc = a.weight_grad_stride;
+            q.large = large_tiles(q.m, piece);
             launch_product<T, false, false, EPI_OUT>(q, s);
         }
     }

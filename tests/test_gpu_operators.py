@@ -203,6 +203,18 @@ def test_loss_and_gradients(det, dtype, n, vocab, width, gap, padding):
     assert all(torch.equal(out[k], again[k]) for k in out), "a second pass differs"
 
 
+@pytest.mark.parametrize("n,vocab,width,gap,padding", [
+    # enough tiles of 256 x 256 for every CU: of the logits, of the hidden states' gradient, of the weights'
+    (2100, 9001, 72, 0, 0.1), (22000, 130, 520, 0, 0.3), (40, 33001, 264, 0, 0.0), (2305, 8000, 200, 8, 0.0), (2049, 8191, 33, 0, 0.5),
+])
+def test_loss_and_gradients_in_large_tiles(det, n, vocab, width, gap, padding):
+    say(f"large tiles n={n} vocab={vocab} width={width} gap={gap} padding={padding}")
+    h, w = randn((n, width), n + width, BF16), randn((vocab, width), n + vocab, BF16, 2 / width ** 0.5)
+    t = refs.tokens(n, vocab, n, padding)
+    ref = refs.Loss(h, w, t, grad_mean=1.0)
+    check_loss(run_loss(det, h, w, t, gap, grad_mean=1.0), ref)
+
+
 @pytest.mark.parametrize("dtype", [BF16, F16])
 def test_mean_over_many_rows_does_not_underflow(det, dtype):
     """c = 1 / rows and small probabilities: G is far below the least f16 number if it is not scaled."""
