@@ -84,7 +84,6 @@ struct product_args {
     uint64_t slab;                  // elements between two slabs of dH
     uint32_t add;                   // dH: add to what is there
     uint32_t splits;                // dH: parts of k, a slab each
-    uint32_t large;                 // tiles of 256 x 256 instead of 128 x 128 (the host's choice)
 };
 
 enum { EPI_LSE, EPI_G, EPI_SLAB, EPI_OUT };
@@ -174,6 +173,8 @@ __device__ __forceinline__ void tile_of(uint32_t b, uint32_t tiles_m, uint32_t t
     tm = in / width;
 }
 
+constexpr uint32_t SPARE = 4096;   // bytes of the LDS that a wave has to itself behind the sum
+
 // The sum over k for tiles of 128 x 128 by four waves, two workgroups a CU.  Sixteen rows of A at a
 // time (a step) are multiplied by all of the wave's columns, over the first half of the block's k, then the
 // second.  A's fragments are read AHEAD steps before they are multiplied, B's half a block before; the
@@ -189,12 +190,14 @@ struct small_tile {
     static __device__ __forceinline__ uint32_t col_of(uint32_t wn, int j) { return wn * 64 + j * 16; }
 
     static __device__ __forceinline__ void run(const operand& oa, const operand& ob, uint32_t m0, uint32_t n0, uint32_t kfirst,
-                                               uint32_t blocks, uint32_t ends, f32x4 (&acc)[FM][FN]) {
+                                               uint32_t blocks, uint32_t ends, f32x4 (&acc)[FM][FN], uint8_t*& spare) {
         // (one array a buffer, so that the compiler knows which loads a read has to wait for)
         __shared__ __attribute__((aligned(16))) uint8_t sa0[BM * BK * 2], sb0[BN * BK * 2];
         __shared__ __attribute__((aligned(16))) uint8_t sa1[BM * BK * 2], sb1[BN * BK * 2];
         const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
         const uint32_t wm = wave / WN, wn = wave % WN;
+        spare = sb0 + wave * SPARE;
+        if (blocks == 0) return;
         stager<BM, A_ALONG, NT> la;
         stager<BN, B_ALONG, NT> lb;
         la.init(oa, m0, 0, kfirst * BK);
@@ -258,6 +261,7 @@ struct small_tile {
             block(sa0, sb0, sa1, sb1, kt);
             block(sa1, sb1, sa0, sb0, kt + 1);
         }
+        __syncthreads();                                     // (the last block read for the next by all)
     }
 };
 
@@ -289,11 +293,13 @@ struct large_tile {
     static constexpr int LDS_READ = 0xC07F;
 
     static __device__ __forceinline__ void run(const operand& oa, const operand& ob, uint32_t m0, uint32_t n0, uint32_t kfirst,
-                                               uint32_t blocks, uint32_t ends, f32x4 (&acc)[FM][FN]) {
+                                               uint32_t blocks, uint32_t ends, f32x4 (&acc)[FM][FN], uint8_t*& spare) {
         __shared__ __attribute__((aligned(16))) uint8_t up0[128 * BK * 2], low0[128 * BK * 2], sb0[BN * BK * 2];
         __shared__ __attribute__((aligned(16))) uint8_t up1[128 * BK * 2], low1[128 * BK * 2], sb1[BN * BK * 2];
         const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
         const uint32_t wm = wave / WN, wn = wave % WN, group = wm;   // (waves w and w + 4 share a SIMD)
+        spare = sb0 + wave * SPARE;
+        if (blocks == 0) return;
         stager<128, A_ALONG, NT> lu, ll;
         stager<BN, B_ALONG, NT> lb;
         lu.init(oa, m0, 0, kfirst * BK);
@@ -395,6 +401,62 @@ struct large_tile {
     }
 };
 
+// ---- what becomes of a tile ------------------------------------------------------------------
+
+// Sums over parts of the vocabulary: x the largest logit (in units of log 2), y the sum of the exponentials
+// relative to it.  Nothing at all is (-inf, 0).
+__device__ __forceinline__ float2 join_sums(float2 a, float2 b) {
+    const float top = fmaxf(a.x, b.x), from = top == -__builtin_inff() ? 0.0f : top;
+    return make_float2(top, a.y * __builtin_amdgcn_exp2f(a.x - from) + b.y * __builtin_amdgcn_exp2f(b.x - from));
+}
+
+// Column j of a wave's tile over all of its rows (words rows[f] + 0..3), the same in the four lanes that share a
+// column i.  The target's logit is written where it is met; the tile is scaled to units of log 2.
+template <int FM, int FN>
+__device__ __forceinline__ float2 tile_sums(const product_args& p, f32x4 (&acc)[FM][FN], int j, const uint32_t (&rows)[FM], uint32_t i,
+                                            uint32_t n, uint32_t lane) {
+    const int64_t t = i < n ? gd_token(p.targets, i) : -1;
+    float top = -__builtin_inff();
+#pragma unroll
+    for (int f = 0; f < FM; ++f)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const uint32_t v = p.v0 + rows[f] + r;
+            if (v < p.vocab) {
+                if (t == (int64_t)v) p.target_logit[i] = acc[f][j][r] * p.scale;
+                acc[f][j][r] *= p.scale2;
+            } else {
+                acc[f][j][r] = -__builtin_inff();
+            }
+            top = fmaxf(top, acc[f][j][r]);
+        }
+    top = fmaxf(top, __uint_as_float(gd_lane_xor<16>(__float_as_uint(top), lane)));
+    top = fmaxf(top, __uint_as_float(gd_lane_xor<32>(__float_as_uint(top), lane)));
+    const float from = top == -__builtin_inff() ? 0.0f : top;
+    float sum = 0.0f;
+#pragma unroll
+    for (int f = 0; f < FM; ++f)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) sum += __builtin_amdgcn_exp2f(acc[f][j][r] - from);
+    sum += __uint_as_float(gd_lane_xor<16>(__float_as_uint(sum), lane));
+    sum += __uint_as_float(gd_lane_xor<32>(__float_as_uint(sum), lane));
+    return make_float2(top, sum);
+}
+
+// G of a row for the words v + 0..3.
+template <typename T>
+__device__ __forceinline__ gd_vec<T, 4> four_of_g(const product_args& p, const f32x4& logits, uint32_t v, int32_t t, float lse2, float coef,
+                                                  bool there) {
+    gd_vec<T, 4> q;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+        float e = exp2f(logits[r] * p.scale2 - lse2);            // (the instruction alone drops subnormal results)
+        if ((int32_t)(v + r) == t) e -= 1.0f;
+        q.v[r] = gd_from_f32<T>(there && v + r < p.vocab ? coef * e : 0.0f);
+    }
+    return q;
+}
+
 template <typename T, typename TILE, int EPI>
 __global__ __launch_bounds__(TILE::NT, 512 / TILE::NT) void product_kernel(const product_args p) {
     constexpr int BM = TILE::BM, BN = TILE::BN, WM = TILE::WM, WN = TILE::WN, FM = TILE::FM, FN = TILE::FN;
@@ -419,8 +481,8 @@ __global__ __launch_bounds__(TILE::NT, 512 / TILE::NT) void product_kernel(const
 #pragma unroll
         for (int j = 0; j < FN; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
     // operands that lie along k end where their rows do
-    if (blocks > 0)
-        TILE::run(p.a, p.b, m0, n0, kfirst, blocks, EPI == EPI_LSE || EPI == EPI_G ? k % BK : 0, acc);
+    uint8_t* spare;
+    TILE::run(p.a, p.b, m0, n0, kfirst, blocks, EPI == EPI_LSE || EPI == EPI_G ? k % BK : 0, acc, spare);
 
     // lane l holds rows 4 (l / 16) + 0..3 and column l % 16 of each 16 x 16 block
     uint32_t row[FM], col[FN];
@@ -428,48 +490,33 @@ __global__ __launch_bounds__(TILE::NT, 512 / TILE::NT) void product_kernel(const
     for (int i = 0; i < FM; ++i) row[i] = m0 + TILE::row_of(wm, i) + (lane >> 4) * 4;
 #pragma unroll
     for (int j = 0; j < FN; ++j) col[j] = n0 + TILE::col_of(wn, j) + (lane & 15);
+    // Rows are what lies next to each other in memory: through the wave's part of the LDS, 16 columns at a time, lanes
+    // that have four rows of a column each become lanes with eight, and whole lines are written.
+    constexpr uint32_t CH = FM * 2;                              // 16-byte chunks of a column
+    auto put = [&](uint32_t f, const gd_vec<T, 4>& q) {
+        const uint32_t c = lane & 15, ch = f * 2 + (lane >> 5);
+        *reinterpret_cast<gd_vec<T, 4>*>(spare + c * (CH * 16) + ((ch ^ (c & (CH - 1))) * 16) + ((lane >> 4) & 1) * 8) = q;
+    };
+    auto take = [&](auto write) {
+#pragma unroll
+        for (uint32_t it = 0; it < CH / 4; ++it) {
+            const uint32_t c = it * (64 / CH) + lane / CH, ch = lane % CH;
+            const gd_vec<T, 8> q = *reinterpret_cast<const gd_vec<T, 8>*>(spare + c * (CH * 16) + ((ch ^ (c & (CH - 1))) * 16));
+            write(c, m0 + TILE::row_of(wm, ch / 2) + (ch & 1) * 8, q);
+        }
+    };
     if (EPI == EPI_LSE) {
         __shared__ float2 join[WM * BN];
 #pragma unroll
         for (int j = 0; j < FN; ++j) {
-            const uint32_t i = col[j];
-            const int64_t t = i < n ? gd_token(p.targets, i) : -1;
-            float top = -__builtin_inff();
-#pragma unroll
-            for (int f = 0; f < FM; ++f)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const uint32_t v = p.v0 + row[f] + r;
-                    if (v < p.vocab) {
-                        if (t == (int64_t)v) p.target_logit[i] = acc[f][j][r] * p.scale;
-                        acc[f][j][r] *= p.scale2;
-                    } else {
-                        acc[f][j][r] = -__builtin_inff();
-                    }
-                    top = fmaxf(top, acc[f][j][r]);
-                }
-            top = fmaxf(top, __uint_as_float(gd_lane_xor<16>(__float_as_uint(top), lane)));
-            top = fmaxf(top, __uint_as_float(gd_lane_xor<32>(__float_as_uint(top), lane)));
-            const float from = top == -__builtin_inff() ? 0.0f : top;
-            float sum = 0.0f;
-#pragma unroll
-            for (int f = 0; f < FM; ++f)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) sum += __builtin_amdgcn_exp2f(acc[f][j][r] - from);
-            sum += __uint_as_float(gd_lane_xor<16>(__float_as_uint(sum), lane));
-            sum += __uint_as_float(gd_lane_xor<32>(__float_as_uint(sum), lane));
-            if (lane < 16) join[wm * BN + TILE::col_of(wn, j) + lane] = make_float2(top, sum);
+            const float2 q = tile_sums<FM, FN>(p, acc, j, row, col[j], n, lane);
+            if (lane < 16) join[wm * BN + TILE::col_of(wn, j) + lane] = q;
         }
         __syncthreads();
         if (threadIdx.x < BN && n0 + threadIdx.x < n) {
             float2 q = join[threadIdx.x];
 #pragma unroll
-            for (int w = 1; w < WM; ++w) {
-                const float2 o = join[w * BN + threadIdx.x];
-                const float top = fmaxf(q.x, o.x), from = top == -__builtin_inff() ? 0.0f : top;
-                q.y = q.y * __builtin_amdgcn_exp2f(q.x - from) + o.y * __builtin_amdgcn_exp2f(o.x - from);
-                q.x = top;
-            }
+            for (int w = 1; w < WM; ++w) q = join_sums(q, join[w * BN + threadIdx.x]);
             p.part[(uint64_t)(n0 + threadIdx.x) * p.parts + p.part0 + tm] = q;
         }
     } else if (EPI == EPI_G) {
@@ -481,115 +528,280 @@ __global__ __launch_bounds__(TILE::NT, 512 / TILE::NT) void product_kernel(const
             const float lse2 = there ? p.row_lse2[i] : 0.0f, coef = there ? p.row_coef[i] : 0.0f;
             const int32_t t = there ? p.row_target[i] : -1;
 #pragma unroll
-            for (int f = 0; f < FM; ++f) {
-                gd_vec<T, 4> q;
-                const uint32_t v = p.v0 + row[f];
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    float e = exp2f(acc[f][j][r] * p.scale2 - lse2);    // (the instruction alone drops subnormal results)
-                    if ((int32_t)(v + r) == t) e -= 1.0f;
-                    q.v[r] = gd_from_f32<T>(there && v + r < p.vocab ? coef * e : 0.0f);
-                }
-                *reinterpret_cast<gd_vec<T, 4>*>(g + (uint64_t)i * p.ldc + row[f]) = q;
-            }
+            for (int f = 0; f < FM; ++f) put(f, four_of_g<T>(p, acc[f][j], p.v0 + row[f], t, lse2, coef, there));
+            take([&](uint32_t c, uint32_t m, const gd_vec<T, 8>& q) {
+                *reinterpret_cast<gd_vec<T, 8>*>(g + (uint64_t)(n0 + TILE::col_of(wn, j) + c) * p.ldc + m) = q;
+            });
         }
     } else if (EPI == EPI_SLAB) {
-        float* c = static_cast<float*>(p.c) + blockIdx.y * p.slab;
+        float* slab = static_cast<float*>(p.c) + blockIdx.y * p.slab;
 #pragma unroll
         for (int j = 0; j < FN; ++j) {
             const uint32_t i = col[j];
             if (i >= n) continue;
 #pragma unroll
             for (int f = 0; f < FM; ++f) {
-                const uint32_t e = row[f];                      // slabs are padded to four columns
+                const uint32_t e = row[f];                       // slabs are padded to four columns
                 if (e >= p.m) continue;
-                f32x4* to = reinterpret_cast<f32x4*>(c + (uint64_t)i * p.ldc + e);
+                f32x4* to = reinterpret_cast<f32x4*>(slab + (uint64_t)i * p.ldc + e);
                 *to = p.add ? *to + acc[f][j] : acc[f][j];
             }
         }
     } else {
-        T* c = static_cast<T*>(p.c);
+        T* out = static_cast<T*>(p.c);
         const float back = p.head->back, more = p.head->more * p.scale;
+        const bool whole = (p.ldc & 7) == 0 && ((uintptr_t)out & 15) == 0;
 #pragma unroll
         for (int j = 0; j < FN; ++j) {
-            const uint32_t i = col[j];
-            if (i >= p.n) continue;
 #pragma unroll
             for (int f = 0; f < FM; ++f) {
-                const uint32_t e = row[f];
-                T* to = c + (uint64_t)i * p.ldc + e;
-                if (e + 4 <= p.m && (p.ldc & 3) == 0 && ((uintptr_t)c & 7) == 0) {
-                    gd_vec<T, 4> q;
+                gd_vec<T, 4> q;
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) q.v[r] = gd_from_f32<T>(acc[f][j][r] * back * more);
-                    *reinterpret_cast<gd_vec<T, 4>*>(to) = q;
+                for (int r = 0; r < 4; ++r) q.v[r] = gd_from_f32<T>(acc[f][j][r] * back * more);
+                put(f, q);
+            }
+            take([&](uint32_t c, uint32_t m, const gd_vec<T, 8>& q) {
+                const uint32_t i = n0 + TILE::col_of(wn, j) + c;
+                if (i >= p.n) return;
+                T* to = out + (uint64_t)i * p.ldc + m;
+                if (whole && m + 8 <= p.m) {
+                    *reinterpret_cast<gd_vec<T, 8>*>(to) = q;
                 } else {
 #pragma unroll
-                    for (uint32_t r = 0; r < 4; ++r)
-                        if (e + r < p.m) to[r] = gd_from_f32<T>(acc[f][j][r] * back * more);
+                    for (uint32_t r = 0; r < 8; ++r)
+                        if (m + r < p.m) to[r] = q.v[r];
                 }
-            }
+            });
         }
+    }
+}
+
+// ---- few rows ----------------------------------------------------------------------------------
+
+// Logits where rows and words make too few tiles for the chip: a workgroup takes 32 words and up to 64 rows, its
+// four waves a block of 64 k each in turn, straight into registers and DEPTH blocks ahead, with no LDS and no
+// barrier between the loads; their sums are added up through the LDS.
+template <typename T, int FN, int EPI>
+__global__ __launch_bounds__(256) void few_rows_kernel(const product_args p) {
+    typedef typename of_type<T>::x8 X8;
+    constexpr int FM = 2, DEPTH = FN == 4 ? 2 : 4;
+    constexpr uint32_t WAVES = 4, WORDS = 32;
+    const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    const uint32_t n = EPI == EPI_G ? p.head->count : p.n, n0 = blockIdx.y * (FN * 16);
+    if (n0 >= n) return;
+    const uint32_t m0 = blockIdx.x * WORDS, k = p.k;
+    const T* a[FM];
+    const T* b[FN];
+#pragma unroll
+    for (int i = 0; i < FM; ++i)
+        a[i] = static_cast<const T*>(p.a.p) + (uint64_t)min(m0 + i * 16 + (lane & 15), p.a.rows - 1) * p.a.stride + (lane >> 4) * 8;
+#pragma unroll
+    for (int j = 0; j < FN; ++j)
+        b[j] = static_cast<const T*>(p.b.p) + (uint64_t)min(n0 + j * 16 + (lane & 15), n - 1) * p.b.stride + (lane >> 4) * 8;
+    f32x4 acc[FM][FN];
+#pragma unroll
+    for (int i = 0; i < FM; ++i)
+#pragma unroll
+        for (int j = 0; j < FN; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    X8 fa[DEPTH][FM][2], fb[DEPTH][FN][2];
+    const uint32_t whole = k / BK, mine = whole > wave ? (whole - wave + WAVES - 1) / WAVES : 0;   // whole blocks
+    auto load = [&](int d, uint32_t q) {
+        const uint32_t at = (wave + q * WAVES) * BK;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+#pragma unroll
+            for (int i = 0; i < FM; ++i) fa[d][i][h] = *reinterpret_cast<const X8*>(a[i] + at + h * 32);
+#pragma unroll
+            for (int j = 0; j < FN; ++j) fb[d][j][h] = *reinterpret_cast<const X8*>(b[j] + at + h * 32);
+        }
+    };
+    auto use = [&](int d) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int i = 0; i < FM; ++i)
+#pragma unroll
+                for (int j = 0; j < FN; ++j) acc[i][j] = multiply(fa[d][i][h], fb[d][j][h], acc[i][j]);
+    };
+#pragma unroll
+    for (int d = 0; d < DEPTH; ++d)
+        if ((uint32_t)d < mine) load(d, d);
+    for (uint32_t q0 = 0; q0 < mine; q0 += DEPTH) {
+#pragma unroll
+        for (int d = 0; d < DEPTH; ++d)
+            if (q0 + d < mine) {
+                use(d);
+                if (q0 + d + DEPTH < mine) load(d, q0 + d + DEPTH);
+            }
+    }
+    if (k % BK && whole % WAVES == wave) {                       // the last block ends inside: zeros behind the end
+        const uint32_t at = whole * BK;
+#pragma unroll
+        for (uint32_t h = 0; h < 2; ++h) {
+            const bool in = at + h * 32 + (lane >> 4) * 8 < k;
+#pragma unroll
+            for (int i = 0; i < FM; ++i) fa[0][i][h] = in ? *reinterpret_cast<const X8*>(a[i] + at + h * 32) : X8(0);
+#pragma unroll
+            for (int j = 0; j < FN; ++j) fb[0][j][h] = in ? *reinterpret_cast<const X8*>(b[j] + at + h * 32) : X8(0);
+        }
+        use(0);
+    }
+    __shared__ f32x4 sums[WAVES][FM * FN][64];
+#pragma unroll
+    for (int i = 0; i < FM; ++i)
+#pragma unroll
+        for (int j = 0; j < FN; ++j) sums[wave][i * FN + j][lane] = acc[i][j];
+    __syncthreads();
+    if (wave > 0) return;
+#pragma unroll
+    for (int i = 0; i < FM; ++i)
+#pragma unroll
+        for (int j = 0; j < FN; ++j)
+#pragma unroll
+            for (uint32_t w = 1; w < WAVES; ++w) acc[i][j] += sums[w][i * FN + j][lane];
+    const uint32_t rows[FM] = {m0 + (lane >> 4) * 4, m0 + 16 + (lane >> 4) * 4};
+    if (EPI == EPI_LSE) {
+#pragma unroll
+        for (int j = 0; j < FN; ++j) {
+            const uint32_t i = n0 + j * 16 + (lane & 15);
+            const float2 q = tile_sums<FM, FN>(p, acc, j, rows, i, n, lane);
+            if (lane < 16 && i < n) p.part[(uint64_t)i * p.parts + p.part0 + blockIdx.x] = q;
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < FN; ++j) {
+            const uint32_t i = n0 + j * 16 + (lane & 15);        // (there is room for whole tiles)
+            const bool there = i < n;
+            const float lse2 = there ? p.row_lse2[i] : 0.0f, coef = there ? p.row_coef[i] : 0.0f;
+            const int32_t t = there ? p.row_target[i] : -1;
+#pragma unroll
+            for (int f = 0; f < FM; ++f)
+                *reinterpret_cast<gd_vec<T, 4>*>(static_cast<T*>(p.c) + (uint64_t)i * p.ldc + rows[f]) =
+                    four_of_g<T>(p, acc[f][j], p.v0 + rows[f], t, lse2, coef, there);
+        }
+        // (the weights' gradient takes the rows in blocks of 64)
+#pragma unroll
+        for (int j = FN; j < (int)BK / 16; ++j)
+#pragma unroll
+            for (int f = 0; f < FM; ++f)
+                *reinterpret_cast<gd_vec<T, 4>*>(static_cast<T*>(p.c) + (uint64_t)(j * 16 + (lane & 15)) * p.ldc + rows[f]) = gd_vec<T, 4>{};
     }
 }
 
 // ---- around the products -------------------------------------------------------------------
 
-// Rows of `in` (all, or those listed) into rows of a padded copy: zeros behind the row's end and,
-// up to `padded` rows, behind the last row.
+// Row r of `in` (or zeros) into a padded row, by a workgroup of 256.
 template <typename T>
-__global__ __launch_bounds__(256) void pack_kernel(const void* in, uint64_t stride, uint32_t width, const grad_head* head,
-                                                   const uint32_t* rows, uint32_t n, uint32_t padded, T* out, uint32_t ldo) {
-    if (head) n = head->count;
-    const uint32_t last = head ? min(padded, (n + 255) / 256 * 256) : padded;
-    for (uint64_t r = blockIdx.x; r < last; r += gridDim.x) {
-        const T* from = static_cast<const T*>(in) + (r < n ? (rows ? (uint64_t)rows[r] : r) : 0) * stride;
-        T* to = out + r * ldo;
-        if (((uintptr_t)in & 15) == 0 && stride % 8 == 0 && width % 8 == 0) {
-            for (uint32_t c = threadIdx.x * 8; c < ldo; c += 256 * 8) {
-                gd_vec<T, 8> q;
-                if (r < n && c < width) q = *reinterpret_cast<const gd_vec<T, 8>*>(from + c);
-                else
+__device__ __forceinline__ void pack_row(const void* in, uint64_t stride, uint32_t width, bool there, uint64_t r, T* to, uint32_t ldo) {
+    const T* from = static_cast<const T*>(in) + r * stride;
+    if (((uintptr_t)in & 15) == 0 && stride % 8 == 0 && width % 8 == 0) {
+        for (uint32_t c = threadIdx.x * 8; c < ldo; c += 256 * 8) {
+            gd_vec<T, 8> q{};
+            if (there && c < width) q = *reinterpret_cast<const gd_vec<T, 8>*>(from + c);
+            *reinterpret_cast<gd_vec<T, 8>*>(to + c) = q;
+        }
+    } else {
+        // elements one by one, eight of a lane at once
+        for (uint32_t c = threadIdx.x * 8; c < ldo; c += 256 * 8) {
+            gd_vec<T, 8> q{};
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) q.v[j] = gd_from_f32<T>(0.0f);
-                *reinterpret_cast<gd_vec<T, 8>*>(to + c) = q;
-            }
-        } else {
-            for (uint32_t c = threadIdx.x; c < ldo; c += 256) to[c] = r < n && c < width ? from[c] : gd_from_f32<T>(0.0f);
+            for (uint32_t j = 0; j < 8; ++j)
+                if (there && c + j < width) q.v[j] = from[c + j];
+            *reinterpret_cast<gd_vec<T, 8>*>(to + c) = q;
         }
     }
 }
 
-// The tiles' sums of a row joined, one wave a row.
-__global__ __launch_bounds__(256) void join_kernel(const float2* part, uint32_t stride, uint32_t parts, gd_token_list targets, uint32_t vocab,
-                                                   const float* target_logit, float* loss, float* lse) {
+// Rows of `in` (all, or those listed) into rows of a padded copy: zeros behind the row's end and, behind a list, up
+// to the next 256 rows.
+template <typename T>
+__global__ __launch_bounds__(256) void pack_kernel(const void* in, uint64_t stride, uint32_t width, const grad_head* head,
+                                                   const uint32_t* rows, uint32_t n, T* out, uint32_t ldo) {
+    if (head) n = head->count;
+    const uint32_t last = head ? (n + 255) / 256 * 256 : n;
+    for (uint64_t r = blockIdx.x; r < last; r += gridDim.x)
+        pack_row<T>(in, stride, width, r < n, r < n ? (rows ? (uint64_t)rows[r] : r) : 0, out + r * ldo, ldo);
+}
+
+// Sums joined over the lanes of a wave.
+__device__ __forceinline__ float2 wave_sums(float2 q, uint32_t lane) {
+    const auto with = [&](uint32_t x, uint32_t y) { q = join_sums(q, make_float2(__uint_as_float(x), __uint_as_float(y))); };
+    with(gd_lane_xor<1>(__float_as_uint(q.x), lane), gd_lane_xor<1>(__float_as_uint(q.y), lane));
+    with(gd_lane_xor<2>(__float_as_uint(q.x), lane), gd_lane_xor<2>(__float_as_uint(q.y), lane));
+    with(gd_lane_xor<4>(__float_as_uint(q.x), lane), gd_lane_xor<4>(__float_as_uint(q.y), lane));
+    with(gd_lane_xor<8>(__float_as_uint(q.x), lane), gd_lane_xor<8>(__float_as_uint(q.y), lane));
+    with(gd_lane_xor<16>(__float_as_uint(q.x), lane), gd_lane_xor<16>(__float_as_uint(q.y), lane));
+    with(gd_lane_xor<32>(__float_as_uint(q.x), lane), gd_lane_xor<32>(__float_as_uint(q.y), lane));
+    return q;
+}
+
+struct join_args {
+    const float2* part;
+    uint32_t stride, parts;          // elements between rows; parts of a row
+    gd_token_list targets;
+    uint32_t vocab;
+    const float* target_logit;
+    float* loss;  float* lse;  float* mean;
+};
+
+// Every `step`-th part of row i from `from` on, four at a time.
+__device__ __forceinline__ float2 parts_of(const join_args& a, uint32_t i, uint32_t from, uint32_t step) {
+    const float2* q = a.part + (uint64_t)i * a.stride;
+    float2 sum = make_float2(-__builtin_inff(), 0.0f);
+    for (uint32_t c = from; c < a.parts; c += 4 * step) {
+        float2 x[4];
+#pragma unroll
+        for (uint32_t b = 0; b < 4; ++b) x[b] = c + b * step < a.parts ? q[c + b * step] : make_float2(-__builtin_inff(), 0.0f);
+#pragma unroll
+        for (uint32_t b = 0; b < 4; ++b) sum = join_sums(sum, x[b]);
+    }
+    return sum;
+}
+
+// A row's results; returns its loss.
+__device__ __forceinline__ float finish_row(const join_args& a, uint32_t i, float2 q) {
+    const float l = (q.x + __builtin_amdgcn_logf(q.y)) * LN2;
+    const int64_t t = gd_token(a.targets, i);
+    const float loss = t < 0 ? 0.0f : t >= (int64_t)a.vocab ? __uint_as_float(0x7FC00000u) : l - a.target_logit[i];
+    a.lse[i] = l;
+    a.loss[i] = loss;
+    return loss;
+}
+
+// The tiles' sums joined, one wave a row.
+__global__ __launch_bounds__(256) void join_kernel(const join_args a) {
     const uint32_t i = blockIdx.x * 4 + threadIdx.x / 64, lane = threadIdx.x & 63;
-    if (i >= targets.n) return;
-    const float2* q = part + (uint64_t)i * stride;
-    float top = -__builtin_inff();
-    bool nan = false;
-    for (uint32_t c = lane; c < parts; c += 64) { top = fmaxf(top, q[c].x); nan |= q[c].x != q[c].x; }
-    top = fmaxf(top, __uint_as_float(gd_lane_xor<1>(__float_as_uint(top), lane)));
-    top = fmaxf(top, __uint_as_float(gd_lane_xor<2>(__float_as_uint(top), lane)));
-    top = fmaxf(top, __uint_as_float(gd_lane_xor<4>(__float_as_uint(top), lane)));
-    top = fmaxf(top, __uint_as_float(gd_lane_xor<8>(__float_as_uint(top), lane)));
-    top = fmaxf(top, __uint_as_float(gd_lane_xor<16>(__float_as_uint(top), lane)));
-    top = fmaxf(top, __uint_as_float(gd_lane_xor<32>(__float_as_uint(top), lane)));
-    const float from = top == -__builtin_inff() ? 0.0f : top;
-    float sum = 0.0f;
-    for (uint32_t c = lane; c < parts; c += 64) sum += q[c].y * __builtin_amdgcn_exp2f(q[c].x - from);
-    sum += __uint_as_float(gd_lane_xor<1>(__float_as_uint(sum), lane));
-    sum += __uint_as_float(gd_lane_xor<2>(__float_as_uint(sum), lane));
-    sum += __uint_as_float(gd_lane_xor<4>(__float_as_uint(sum), lane));
-    sum += __uint_as_float(gd_lane_xor<8>(__float_as_uint(sum), lane));
-    sum += __uint_as_float(gd_lane_xor<16>(__float_as_uint(sum), lane));
-    sum += __uint_as_float(gd_lane_xor<32>(__float_as_uint(sum), lane));
+    if (i >= a.targets.n) return;
+    const float2 q = wave_sums(parts_of(a, i, lane, 64), lane);
+    if (lane == 0) finish_row(a, i, q);
+}
+
+// The same and the mean for few rows and parts, by one workgroup of sixteen waves: `share` (a power of two) of
+// them work on a row.
+__global__ __launch_bounds__(1024) void join_alone(const join_args a, uint32_t share) {
+    __shared__ float2 sums[16];
+    __shared__ float losses[64];
+    const uint32_t wave = threadIdx.x / 64, lane = threadIdx.x & 63, n = a.targets.n, at_once = 16 / share;
+    for (uint32_t i0 = 0; i0 < n; i0 += at_once) {
+        const uint32_t i = i0 + wave / share;
+        float2 q = make_float2(-__builtin_inff(), 0.0f);
+        if (i < n) q = wave_sums(parts_of(a, i, (wave % share) * 64 + lane, share * 64), lane);
+        if (lane == 0) sums[wave] = q;
+        __syncthreads();
+        if (lane == 0 && wave % share == 0 && i < n) {
+            for (uint32_t w = 1; w < share; ++w) q = join_sums(q, sums[wave + w]);
+            losses[i] = finish_row(a, i, q);
+        }
+        __syncthreads();
+    }
+    if (wave > 0) return;
+    float sum = lane < n ? losses[lane] : 0.0f;
+    const float count = (float)__popcll(__ballot(lane < n && gd_token(a.targets, min(lane, n - 1)) >= 0));
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) sum += __shfl_xor(sum, d);
     if (lane == 0) {
-        float l = (top + __builtin_amdgcn_logf(sum)) * LN2;
-        if (nan) l = __uint_as_float(0x7FC00000u);
-        lse[i] = l;
-        const int64_t t = gd_token(targets, i);
-        loss[i] = t < 0 ? 0.0f : t >= (int64_t)vocab ? __uint_as_float(0x7FC00000u) : l - target_logit[i];
+        a.mean[0] = sum / fmaxf(count, 1.0f);
+        a.mean[1] = count;
     }
 }
 
@@ -634,25 +846,50 @@ __device__ __forceinline__ float coef_of(const rows_args& a, uint32_t i) {
     return c;
 }
 
-// Lists the rows with a gradient and works out what their tiles need.  One workgroup: the list is in
-// order of the rows.  Gradients of a mean over many rows, and of improbable words, would underflow as G
-// is rounded to 16 bits, and the -1 at the target would be rounded as well: coefficients are divided by the
+// What the coefficients are scaled by.  Gradients of a mean over many rows, and of improbable words, would underflow
+// as G is rounded to 16 bits, and the -1 at the target would be rounded as well: coefficients are divided by the
 // largest one and multiplied by 2^15 in f16 (G is at most that then) and by 2^40 in bf16 (where every
 // probability that fp32 holds stays a normal number), which is undone behind the products.
+struct coef_scale {
+    float most, power;
+    bool fine;                       // the largest one is a number, and not 0
+    __device__ __forceinline__ coef_scale(uint32_t top, uint32_t half)
+        : most(__uint_as_float(top)), power(half ? 32768.0f : 1099511627776.0f), fine(top < 0x7F800000u && top != 0) {}
+    __device__ __forceinline__ float of(float c) const { return fine ? c / most * power : c; }
+    __device__ __forceinline__ void write(grad_head* head, uint32_t count) const {
+        // (two factors, so that neither is subnormal)
+        head->count = count;
+        head->back = fine ? (most >= 1.0f ? most / power : 1.0f / power) : 1.0f;
+        head->more = fine && most < 1.0f ? most : 1.0f;
+    }
+};
+
+__device__ __forceinline__ uint32_t wave_max(uint32_t v, uint32_t lane) {
+    v = max(v, gd_lane_xor<1>(v, lane));  v = max(v, gd_lane_xor<2>(v, lane));
+    v = max(v, gd_lane_xor<4>(v, lane));  v = max(v, gd_lane_xor<8>(v, lane));
+    v = max(v, gd_lane_xor<16>(v, lane)); return max(v, gd_lane_xor<32>(v, lane));
+}
+
+// Row i, the at-th with a gradient.
+__device__ __forceinline__ void write_row(const rows_args& a, uint32_t i, uint32_t at, float coef) {
+    a.row_lse2[at] = a.lse[i] * LOG2E;
+    a.row_coef[at] = coef;
+    a.row_target[at] = (int32_t)gd_token(a.targets, i);
+}
+
+// Lists the rows with a gradient and works out what their tiles need.  One workgroup: the list is in order of the
+// rows.
 __global__ __launch_bounds__(1024) void prepare_rows(const rows_args a) {
     __shared__ uint32_t s[16];
     const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x / 64, n = a.targets.n;
     uint32_t top = 0;
     for (uint32_t i = threadIdx.x; i < n; i += 1024) top = max(top, __float_as_uint(coef_of(a, i)) & 0x7FFFFFFFu);
-    top = max(top, gd_lane_xor<1>(top, lane));  top = max(top, gd_lane_xor<2>(top, lane));
-    top = max(top, gd_lane_xor<4>(top, lane));  top = max(top, gd_lane_xor<8>(top, lane));
-    top = max(top, gd_lane_xor<16>(top, lane)); top = max(top, gd_lane_xor<32>(top, lane));
+    top = wave_max(top, lane);
     if (lane == 0) s[wave] = top;
     __syncthreads();
     for (int w = 0; w < 16; ++w) top = max(top, s[w]);
     __syncthreads();
-    const float most = __uint_as_float(top), power = a.half ? 32768.0f : 1099511627776.0f;
-    const bool fine = top < 0x7F800000u && top != 0;
+    const coef_scale scale(top, a.half);
     uint32_t count = 0;
     for (uint32_t base = 0; base < n; base += 1024) {
         const uint32_t i = base + threadIdx.x;
@@ -666,34 +903,94 @@ __global__ __launch_bounds__(1024) void prepare_rows(const rows_args a) {
         at += (uint32_t)__popcll(who & ((1ull << lane) - 1));
         if (in) {
             a.rows[at] = i;
-            a.row_lse2[at] = a.lse[i] * LOG2E;
-            a.row_coef[at] = fine ? c / most * power : c;
-            a.row_target[at] = (int32_t)gd_token(a.targets, i);
+            write_row(a, i, at, scale.of(c));
         }
         if (i < n) a.slot[i] = in ? (int32_t)at : -1;
         __syncthreads();
     }
-    if (threadIdx.x == 0) {
-        // (two factors, so that neither is subnormal)
-        a.head->count = count;
-        a.head->back = fine ? (most >= 1.0f ? most / power : 1.0f / power) : 1.0f;
-        a.head->more = fine && most < 1.0f ? most : 1.0f;
-    }
+    if (threadIdx.x == 0) scale.write(a.head, count);
 }
 
-// dH from its slabs, added up in order; zeros where a row has no gradient.
+// The list and the gathered rows in one launch, for up to GATHER rows: every workgroup makes the list for itself, the
+// first one writes it down.
+constexpr uint32_t GATHER = 2048;
+template <typename T>
+__global__ __launch_bounds__(256) void gather_rows(const rows_args a, const void* in, uint64_t stride, uint32_t width, T* out, uint32_t ldo) {
+    constexpr uint32_t PER = GATHER / 256;
+    __shared__ uint32_t s[4], counts[PER][4];
+    __shared__ uint16_t list[GATHER];
+    const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x / 64, n = a.targets.n;
+    float c[PER];
+    uint32_t top = 0, at[PER];
+#pragma unroll
+    for (uint32_t j = 0; j < PER; ++j) {
+        const uint32_t i = j * 256 + threadIdx.x;
+        c[j] = i < n ? coef_of(a, i) : 0.0f;
+        top = max(top, __float_as_uint(c[j]) & 0x7FFFFFFFu);
+        const uint64_t who = __ballot(c[j] != 0.0f);
+        at[j] = (uint32_t)__popcll(who & ((1ull << lane) - 1));
+        if (lane == 0) counts[j][wave] = (uint32_t)__popcll(who);
+    }
+    top = wave_max(top, lane);
+    if (lane == 0) s[wave] = top;
+    __syncthreads();
+    const coef_scale scale(max(max(s[0], s[1]), max(s[2], s[3])), a.half);
+    uint32_t count = 0;
+#pragma unroll
+    for (uint32_t j = 0; j < PER; ++j) {
+        uint32_t before = count;
+#pragma unroll
+        for (uint32_t w = 0; w < 4; ++w) { if (w < wave) before += counts[j][w]; count += counts[j][w]; }
+        at[j] += before;
+        const uint32_t i = j * 256 + threadIdx.x;
+        const bool in = c[j] != 0.0f;
+        if (in) list[at[j]] = (uint16_t)i;
+        if (blockIdx.x == 0) {
+            if (in) write_row(a, i, at[j], scale.of(c[j]));
+            if (i < n) a.slot[i] = in ? (int32_t)at[j] : -1;
+        }
+    }
+    if (blockIdx.x == 0 && threadIdx.x == 0) scale.write(a.head, count);
+    __syncthreads();
+    for (uint32_t r = blockIdx.x; r < (count + 255) / 256 * 256; r += gridDim.x)
+        pack_row<T>(in, stride, width, r < count, r < count ? list[r] : 0, out + (uint64_t)r * ldo, ldo);
+}
+
+// dH from its slabs, added up in order; zeros where a row has no gradient.  Four columns a lane.
 template <typename T>
 __global__ __launch_bounds__(256) void finish_hidden(const float* slabs, uint32_t lds, uint64_t slab, uint32_t splits,
                                                      const grad_head* head, const int32_t* slot, float scale, uint32_t n,
                                                      uint32_t width, T* out, uint64_t ldo) {
+    const uint32_t quads = lds / 4;
     const float back = head->back, more = head->more * scale;
-    for (uint32_t i = blockIdx.x; i < n; i += gridDim.x) {
+    const bool whole = (ldo & 3) == 0 && ((uintptr_t)out & 7) == 0;
+    const uint64_t total = (uint64_t)n * quads;
+    for (uint64_t x = (uint64_t)blockIdx.x * 256 + threadIdx.x; x < total; x += (uint64_t)gridDim.x * 256) {
+        const uint32_t i = (uint32_t)(x / quads), c = (uint32_t)(x - (uint64_t)i * quads) * 4;
         const int32_t at = slot[i];
-        for (uint32_t c = threadIdx.x; c < width; c += 256) {
-            float sum = 0.0f;
-            if (at >= 0)
-                for (uint32_t s = 0; s < splits; ++s) sum += slabs[s * slab + (uint64_t)at * lds + c];
-            out[(uint64_t)i * ldo + c] = gd_from_f32<T>(sum * back * more);
+        f32x4 sum = f32x4(0.0f);
+        if (at >= 0) {
+            const float* from = slabs + (uint64_t)at * lds + c;
+            uint32_t s = 0;
+            for (; s + 4 <= splits; s += 4) {
+                f32x4 q[4];
+#pragma unroll
+                for (uint32_t b = 0; b < 4; ++b) q[b] = *reinterpret_cast<const f32x4*>(from + (s + b) * slab);
+#pragma unroll
+                for (uint32_t b = 0; b < 4; ++b) sum += q[b];
+            }
+            for (; s < splits; ++s) sum += *reinterpret_cast<const f32x4*>(from + s * slab);
+        }
+        gd_vec<T, 4> q;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) q.v[r] = gd_from_f32<T>(sum[r] * back * more);
+        T* to = out + (uint64_t)i * ldo + c;
+        if (whole && c + 4 <= width) {
+            *reinterpret_cast<gd_vec<T, 4>*>(to) = q;
+        } else {
+#pragma unroll
+            for (uint32_t r = 0; r < 4; ++r)
+                if (c + r < width) to[r] = q.v[r];
         }
     }
 }
@@ -708,13 +1005,66 @@ __global__ __launch_bounds__(256) void zero_rows(T* out, uint64_t ldo, uint32_t 
 
 uint64_t up_to(uint64_t v, uint64_t unit) { return (v + unit - 1) / unit * unit; }
 
+// Which tiles.  Large ones move half as much per product but come one to a CU, small ones two, and a launch ends with
+// its last round: what a choice costs is rounds x (blocks of k + what a tile takes before and behind them) x the
+// time of a block of all CUs at once (measured with long k: 1.5 us for 256 large tiles, 1.1 for 512 small ones).
+constexpr uint64_t CUS = 256;
+constexpr double LARGE_BLOCK = 1.5, SMALL_BLOCK = 1.1, AROUND = 7.0;
+double large_cost(uint64_t tiles, double blocks) { return (double)((tiles + CUS - 1) / CUS) * (blocks + AROUND) * LARGE_BLOCK; }
+double small_cost(uint64_t tiles, double blocks) { return (double)((tiles + 2 * CUS - 1) / (2 * CUS)) * (blocks + AROUND) * SMALL_BLOCK; }
+
+// How many of `cols` go to large tiles where `rows` stand against them (a multiple of 256, or all of them): full rounds of
+// large tiles, the rest in small ones, or one kind alone.
+uint64_t large_part(uint64_t cols, uint64_t rows, uint64_t k) {
+    const double blocks = (double)up_to(k, BK) / BK;
+    const uint64_t across = up_to(rows, 256) / 256, all = up_to(cols, 256) / 256, small = up_to(rows, 128) / 128;
+    uint64_t best = 0;
+    double least = small_cost(small * (up_to(cols, 128) / 128), blocks);
+    const double whole = large_cost(across * all, blocks);
+    if (whole < least) { least = whole; best = cols; }
+    const uint64_t full = across * all / CUS * CUS / across;     // tiles across `cols` in full rounds
+    if (full > 0 && full < all) {
+        const double both = large_cost(across * full, blocks) + small_cost(small * (up_to(cols - full * 256, 128) / 128), blocks) + 3.0;
+        if (both < least) best = full * 256;
+    }
+    return best;
+}
+
+// The product with a long k and few tiles: parts of k, a slab of sums each, that the CUs have work alike.
+struct split_plan {
+    bool large;
+    uint32_t splits;
+};
+split_plan split_for(uint64_t m, uint64_t n, uint64_t k) {
+    const uint64_t blocks = up_to(k, BK) / BK;
+    const uint64_t large = up_to(m, 256) / 256 * (up_to(n, 256) / 256), small = up_to(m, 128) / 128 * (up_to(n, 128) / 128);
+    split_plan best{false, 1};
+    double least = 1e30;
+    for (uint32_t s = 1; s <= 64; ++s) {
+        const double per = (double)((blocks + s - 1) / s);
+        if (s > 1 && per < 8) break;
+        const double sums = s * (double)m * (double)n * 8 / 4.9e6;       // a slab written and read
+        const double l = large_cost(large * s, per) + sums, t = small_cost(small * s, per) + sums;
+        if (l < least) { least = l; best = split_plan{true, s}; }
+        if (t < least) { least = t; best = split_plan{false, s}; }
+    }
+    return best;
+}
+
+// Where rows and words make too few tiles for the chip, the waves' blocks of k in turn win: while tiles of 64 rows and
+// 128 words are at most half as many as CUs (us, tiles of 128 x 128 / in turn, width 2 048: 128 rows x 8 000 words
+// 37.9 / 33.4, x 16 000 43.1 / 58.2, 256 x 4 000 31.8 / 32.8, 512 x 2 000 32.1 / 32.6; width 4 096: 64 x 16 384
+// 70.4 / 58.6, 4 x 32 768 77.1 / 76.1).
+bool few_tiles(uint64_t n, uint64_t vocab) { return up_to(n, 64) / 64 * (up_to(vocab, 128) / 128) <= CUS / 2; }
+
 struct loss_layout {
     // forward and both
     size_t target_logit, part, hidden, weight;
     // gradients
     size_t head, rows, slot, lse2, coef, target, g, slabs;
     size_t total;
-    uint64_t padded_rows, ldh, piece, pack_piece, splits, slab;
+    uint64_t padded_rows, ldh, piece, pack_piece, slab;
+    split_plan split;
     uint32_t parts;
 };
 
@@ -727,7 +1077,7 @@ loss_layout layout_of(uint64_t n, uint64_t vocab, uint64_t width, bool with_grad
     l.pack_piece = PACK / l.ldh / 256 * 256;
     if (l.pack_piece < 256) l.pack_piece = 256;
     if (l.pack_piece > all) l.pack_piece = all;
-    l.parts = (uint32_t)(up_to(vocab, 128) / 128);
+    l.parts = (uint32_t)(few_tiles(n, vocab) ? up_to(vocab, 32) / 32 : up_to(vocab, 128) / 128);
     size_t o = 0;
     l.target_logit = o; o = gd_align256(o + n * 4);
     l.part = o;         o = gd_align256(o + n * l.parts * 8);
@@ -737,16 +1087,14 @@ loss_layout layout_of(uint64_t n, uint64_t vocab, uint64_t width, bool with_grad
     l.weight = f;  f = gd_align256(f + l.pack_piece * l.ldh * 2);
     l.total = f;
     l.head = l.rows = l.slot = l.lse2 = l.coef = l.target = l.g = l.slabs = 0;
-    l.piece = l.splits = l.slab = 0;
+    l.piece = l.slab = 0;
     if (!with_grad) return l;
-    l.piece = PIECE / (l.padded_rows ? l.padded_rows : 256) / 256 * 256;
-    if (l.piece < 256) l.piece = 256;
-    if (l.piece > all) l.piece = all;
-    // as many parts of the vocabulary for dH as make some 512 tiles of 128 x 128
-    const uint64_t tiles = up_to(n, 128) / 128 * (up_to(width, 128) / 128);
-    l.splits = tiles ? 512 / tiles : 1;
-    if (l.splits > l.piece / 512) l.splits = l.piece / 512;
-    if (l.splits < 1) l.splits = 1;
+    // pieces of G alike in size
+    uint64_t most = PIECE / (l.padded_rows ? l.padded_rows : 256) / 256 * 256;
+    if (most < 256) most = 256;
+    const uint64_t pieces = (all + most - 1) / most;
+    l.piece = up_to((all + pieces - 1) / pieces, 256);
+    l.split = split_for(width, n, l.piece);
     l.slab = n * up_to(width, 4);
     l.head = f;   f = gd_align256(f + sizeof(grad_head));
     l.rows = f;   f = gd_align256(f + n * 4);
@@ -755,29 +1103,81 @@ loss_layout layout_of(uint64_t n, uint64_t vocab, uint64_t width, bool with_grad
     l.coef = f;   f = gd_align256(f + n * 4);
     l.target = f; f = gd_align256(f + n * 4);
     l.g = f;      f = gd_align256(f + l.padded_rows * l.piece * 2);
-    l.slabs = f;  f = gd_align256(f + l.splits * l.slab * 4);
+    l.slabs = f;  f = gd_align256(f + l.split.splits * l.slab * 4);
     l.total = f;
     return l;
+}
+
+// Workgroups of 256 for so many items, in rounds where there are more than fill the chip.
+uint32_t blocks_for(uint64_t items) {
+    const uint64_t b = (items + 255) / 256;
+    return (uint32_t)(b < 8192 ? b : 8192);
 }
 
 bool direct(const void* p, uint64_t stride, uint64_t width) { return (uintptr_t)p % 16 == 0 && stride % 8 == 0 && width % 8 == 0; }
 
 template <typename T, typename TILE, int EPI>
-void launch_tiles(product_args& p, hipStream_t s) {
+void launch_tiles(product_args p, hipStream_t s) {
     p.tiles_m = (p.m + TILE::BM - 1) / TILE::BM;
     p.tiles_n = (p.n + TILE::BN - 1) / TILE::BN;
     if (EPI != EPI_SLAB) p.splits = 1;
     hipLaunchKernelGGL((product_kernel<T, TILE, EPI>), dim3(p.tiles_m * p.tiles_n, p.splits), dim3(TILE::NT), 0, s, p);
 }
 
-template <typename T, bool A_ALONG, bool B_ALONG, int EPI>
-void launch_product(product_args& p, hipStream_t s) {
-    if (p.large) launch_tiles<T, large_tile<T, A_ALONG, B_ALONG>, EPI>(p, s);
-    else launch_tiles<T, small_tile<T, A_ALONG, B_ALONG>, EPI>(p, s);
+template <typename T, int FN, int EPI>
+void launch_few(const product_args& p, hipStream_t s) {
+    // (G is read in blocks of 64 words)
+    const dim3 grid((uint32_t)up_to(p.m, EPI == EPI_G ? BK : 32) / 32, (p.n + FN * 16 - 1) / (FN * 16));
+    hipLaunchKernelGGL((few_rows_kernel<T, FN, EPI>), grid, dim3(256), 0, s, p);
 }
 
-// Tiles of 256 x 256 (half the reads of an operand, one workgroup a CU) where there are some for all CUs.
-bool large_tiles(uint64_t m, uint64_t n) { return up_to(m, 256) / 256 * (up_to(n, 256) / 256) >= 256; }
+// The logits of a piece; returns how many parts of the vocabulary each row's sums come in.
+template <typename T, int EPI>
+uint32_t launch_logits(const product_args& p, bool few, hipStream_t s) {
+    if (few) {
+        if (p.n <= 16) launch_few<T, 1, EPI>(p, s);
+        else if (p.n <= 32) launch_few<T, 2, EPI>(p, s);
+        else launch_few<T, 4, EPI>(p, s);
+        return (p.m + 31) / 32;
+    }
+    const uint32_t large = (uint32_t)large_part(p.m, p.n, p.k);
+    uint32_t parts = 0;
+    if (large > 0) {
+        product_args q = p;
+        q.m = large;
+        launch_tiles<T, large_tile<T, true, true>, EPI>(q, s);
+        parts = (large + 255) / 256;
+    }
+    if (large < p.m) {
+        product_args q = p;
+        q.m -= large; q.v0 += large; q.part0 += parts;
+        q.a.p = static_cast<const T*>(p.a.p) + (uint64_t)large * p.a.stride;
+        q.a.rows -= large;
+        q.c = static_cast<T*>(p.c) + large;
+        launch_tiles<T, small_tile<T, true, true>, EPI>(q, s);
+        parts += (q.m + 127) / 128;
+    }
+    return parts;
+}
+
+// The rows of the weights' gradient for a piece.
+template <typename T>
+void launch_weight_grad(const product_args& p, hipStream_t s) {
+    const uint32_t large = (uint32_t)large_part(p.n, p.m, p.k);
+    if (large > 0) {
+        product_args q = p;
+        q.n = large;
+        launch_tiles<T, large_tile<T, false, false>, EPI_OUT>(q, s);
+    }
+    if (large < p.n) {
+        product_args q = p;
+        q.n -= large;
+        q.b.p = static_cast<const T*>(p.b.p) + large;
+        q.b.cols -= large;
+        q.c = static_cast<T*>(p.c) + (uint64_t)large * p.ldc;
+        launch_tiles<T, small_tile<T, false, false>, EPI_OUT>(q, s);
+    }
+}
 
 template <typename T>
 hipError_t forward(const gd_vocab_loss_args& a, hipStream_t s) {
@@ -790,7 +1190,7 @@ hipError_t forward(const gd_vocab_loss_args& a, hipStream_t s) {
     p.b = operand{a.hidden, a.hidden_stride, n, a.width};
     if (!direct(a.hidden, a.hidden_stride, a.width)) {
         hipLaunchKernelGGL((pack_kernel<T>), dim3(n < 65536 ? n : 65536), dim3(256), 0, s, a.hidden, a.hidden_stride, a.width,
-                           (const grad_head*)nullptr, (const uint32_t*)nullptr, n, n, hidden, ldh);
+                           (const grad_head*)nullptr, (const uint32_t*)nullptr, n, hidden, ldh);
         p.b = operand{hidden, ldh, n, ldh};
     }
     const bool plain = direct(a.weight, a.weight_stride, a.width);
@@ -799,6 +1199,8 @@ hipError_t forward(const gd_vocab_loss_args& a, hipStream_t s) {
     p.part = reinterpret_cast<float2*>(a.work + l.part);
     p.parts = l.parts;
     const uint32_t piece = plain ? a.vocab : (uint32_t)l.pack_piece;
+    const bool few = few_tiles(n, a.vocab);
+    uint32_t parts = 0;
     for (uint32_t v0 = 0; v0 < a.vocab; v0 += piece) {
         const uint32_t here = a.vocab - v0 < piece ? a.vocab - v0 : piece;
         const T* w = static_cast<const T*>(a.weight) + (uint64_t)v0 * a.weight_stride;
@@ -806,17 +1208,21 @@ hipError_t forward(const gd_vocab_loss_args& a, hipStream_t s) {
             p.a = operand{w, a.weight_stride, here, a.width};
         } else {
             hipLaunchKernelGGL((pack_kernel<T>), dim3(here < 65536 ? here : 65536), dim3(256), 0, s, w, a.weight_stride, a.width,
-                               (const grad_head*)nullptr, (const uint32_t*)nullptr, here, here, weight, ldh);
+                               (const grad_head*)nullptr, (const uint32_t*)nullptr, here, weight, ldh);
             p.a = operand{weight, ldh, here, ldh};
         }
         p.k = p.a.cols < p.b.cols ? p.b.cols : p.a.cols;
-        p.m = here; p.v0 = v0;
-        p.large = large_tiles(piece, n);
-        p.part0 = v0 / (p.large ? 256 : 128);
-        launch_product<T, true, true, EPI_LSE>(p, s);
+        p.m = here; p.v0 = v0; p.part0 = parts;
+        parts += launch_logits<T, EPI_LSE>(p, few, s);
     }
-    const uint32_t tiles = (a.vocab + (p.large ? 255 : 127)) / (p.large ? 256 : 128);
-    hipLaunchKernelGGL(join_kernel, dim3((n + 3) / 4), dim3(256), 0, s, p.part, p.parts, tiles, a.targets, a.vocab, p.target_logit, a.loss, a.lse);
+    const join_args j{p.part, p.parts, parts, a.targets, a.vocab, p.target_logit, a.loss, a.lse, a.mean};
+    if (n <= 64 && n * j.parts <= 16384) {
+        uint32_t share = 1;
+        while (share < 16 && share * 2 * n <= 16 && share * 64 < j.parts) share *= 2;
+        hipLaunchKernelGGL(join_alone, dim3(1), dim3(1024), 0, s, j, share);
+        return hipGetLastError();
+    }
+    hipLaunchKernelGGL(join_kernel, dim3((n + 3) / 4), dim3(256), 0, s, j);
     hipLaunchKernelGGL(mean_kernel, dim3(1), dim3(1024), 0, s, a.loss, a.targets, a.mean);
     return hipGetLastError();
 }
@@ -840,20 +1246,25 @@ hipError_t backward(const gd_vocab_grad_args& a, hipStream_t s) {
     r.row_lse2 = reinterpret_cast<float*>(a.work + l.lse2);
     r.row_coef = reinterpret_cast<float*>(a.work + l.coef);
     r.row_target = reinterpret_cast<int32_t*>(a.work + l.target);
-    hipLaunchKernelGGL(prepare_rows, dim3(1), dim3(1024), 0, s, r);
     const uint32_t padded = (uint32_t)l.padded_rows;
-    hipLaunchKernelGGL((pack_kernel<T>), dim3(padded < 16384 ? padded : 16384), dim3(256), 0, s, a.hidden, a.hidden_stride, a.width,
-                       head, r.rows, n, padded, hidden, ldh);
+    if (n <= GATHER) {
+        hipLaunchKernelGGL((gather_rows<T>), dim3(padded), dim3(256), 0, s, r, a.hidden, a.hidden_stride, a.width, hidden, ldh);
+    } else {
+        hipLaunchKernelGGL(prepare_rows, dim3(1), dim3(1024), 0, s, r);
+        hipLaunchKernelGGL((pack_kernel<T>), dim3(padded < 16384 ? padded : 16384), dim3(256), 0, s, a.hidden, a.hidden_stride, a.width,
+                           head, r.rows, n, hidden, ldh);
+    }
     const bool plain = direct(a.weight, a.weight_stride, a.width);
     uint32_t piece = (uint32_t)l.piece;
     if (!plain && piece > l.pack_piece) piece = (uint32_t)l.pack_piece;
+    const bool few = few_tiles(n, a.vocab);
     for (uint32_t v0 = 0; v0 < a.vocab; v0 += piece) {
         const uint32_t here = a.vocab - v0 < piece ? a.vocab - v0 : piece;
         const T* w = static_cast<const T*>(a.weight) + (uint64_t)v0 * a.weight_stride;
         operand wo{w, a.weight_stride, here, a.width};
         if (!plain) {
             hipLaunchKernelGGL((pack_kernel<T>), dim3(here < 65536 ? here : 65536), dim3(256), 0, s, w, a.weight_stride, a.width,
-                               (const grad_head*)nullptr, (const uint32_t*)nullptr, here, here, weight, ldh);
+                               (const grad_head*)nullptr, (const uint32_t*)nullptr, here, weight, ldh);
             wo = operand{weight, ldh, here, ldh};
         }
         const operand go{g, piece, padded, piece};
@@ -865,18 +1276,17 @@ hipError_t backward(const gd_vocab_grad_args& a, hipStream_t s) {
         p.scale2 = a.scale * LOG2E; p.v0 = v0; p.vocab = a.vocab;
         p.row_lse2 = r.row_lse2; p.row_coef = r.row_coef; p.row_target = r.row_target;
         p.c = g; p.ldc = piece;
-        p.large = large_tiles(piece, n);
-        launch_product<T, true, true, EPI_G>(p, s);
-        const uint32_t padded_here = (uint32_t)up_to(here, p.large ? 256 : 128);     // what the tiles of G have written
+        launch_logits<T, EPI_G>(p, few, s);
+        const uint32_t padded_here = (uint32_t)up_to(here, BK);      // (the tiles of G have written so far at least)
         if (a.hidden_grad) {
             product_args q = {};
             q.head = head;
             q.a = wo;
             q.b = go;
             q.m = a.width; q.n = n; q.k = padded_here;
-            q.c = slabs; q.ldc = lds; q.slab = l.slab; q.add = v0 > 0; q.splits = (uint32_t)l.splits;
-            q.large = large_tiles(q.m, q.n);
-            launch_product<T, false, true, EPI_SLAB>(q, s);
+            q.c = slabs; q.ldc = lds; q.slab = l.slab; q.add = v0 > 0; q.splits = l.split.splits;
+            if (l.split.large) launch_tiles<T, large_tile<T, false, true>, EPI_SLAB>(q, s);
+            else launch_tiles<T, small_tile<T, false, true>, EPI_SLAB>(q, s);
         }
         if (a.weight_grad) {
             product_args q = {};
@@ -886,12 +1296,11 @@ hipError_t backward(const gd_vocab_grad_args& a, hipStream_t s) {
             q.m = a.width; q.n = here; q.k = n;
             q.scale = a.scale;
             q.c = static_cast<T*>(a.weight_grad) + (uint64_t)v0 * a.weight_grad_stride; q.ldc = a.weight_grad_stride;
-            q.large = large_tiles(q.m, piece);
-            launch_product<T, false, false, EPI_OUT>(q, s);
+            launch_weight_grad<T>(q, s);
         }
     }
     if (a.hidden_grad)
-        hipLaunchKernelGGL((finish_hidden<T>), dim3(n < 65536 ? n : 65536), dim3(256), 0, s, slabs, lds, l.slab, (uint32_t)l.splits,
+        hipLaunchKernelGGL((finish_hidden<T>), dim3(blocks_for((uint64_t)n * lds / 4)), dim3(256), 0, s, slabs, lds, l.slab, l.split.splits,
                            head, r.slot, a.scale, n, a.width, static_cast<T*>(a.hidden_grad), a.hidden_grad_stride);
     return hipGetLastError();
 }

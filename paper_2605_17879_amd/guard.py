@@ -219,6 +219,8 @@ class Detector:
         self.h = h
         self.device = torch.device(device)
         self._raw_stream = torch._C._cuda_getCurrentRawStream
+        self._index = self.device.index
+        self._types = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16, torch.int32: I32, torch.int64: I64}
         self.R, self.M = cfg.n_ranks, cfg.n_metrics
         self.N = self.R // cfg.gpus_per_node
         self.RW, self.NW = (self.R + 63) // 64, (self.N + 63) // 64
@@ -425,27 +427,34 @@ class Detector:
 
     # ---- the operators of a sweep's own training step ---------------------------------
     def _type(self, t) -> int:
-        torch = self._torch
-        code = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16, torch.int32: I32,
-                torch.int64: I64}.get(t.dtype)
+        code = self._types.get(t.dtype)
         if code is None:
             raise GuardError(4, f"tensors of {t.dtype} are not built")
         return code
 
     def _on_device(self, *tensors):
         for t in tensors:
-            assert t is None or (t.is_cuda and (self.device.index is None or t.device == self.device)), \
+            assert t is None or (t.is_cuda and (self._index is None or t.get_device() == self._index)), \
                 f"a tensor is on {t.device}, the detector on {self.device}"
 
     def _matrix(self, t) -> _CMatrix:
         """t[rows][cols], rows any distance apart; a list t[n] is a matrix of one column."""
-        self._on_device(t)
-        assert t.dim() in (1, 2)
-        rows, cols = (t.shape[0], 1) if t.dim() == 1 else t.shape
-        assert t.dim() == 1 or cols <= 1 or t.stride(1) == 1, "the elements of a row must be next to each other"
+        shape, strides = t.shape, t.stride()
+        rows = shape[0]
+        if len(shape) == 2:
+            cols = shape[1]
+            assert cols <= 1 or strides[1] == 1, "the elements of a row must be next to each other"
+        else:
+            assert len(shape) == 1, "a matrix or a list"
+            cols = 1
+        # (a short call's time is its marshalling: no helper is called for what is looked at here)
+        assert t.is_cuda and (self._index is None or t.get_device() == self._index), \
+            f"a tensor is on {t.device}, the detector on {self.device}"
+        code = self._types.get(t.dtype)
+        if code is None:
+            raise GuardError(4, f"tensors of {t.dtype} are not built")
         # the distance to a row that is not there says nothing
-        stride = t.stride(0) if rows > 1 else max(cols, 1)
-        return _CMatrix(t.data_ptr(), rows, cols, stride, self._type(t), 0)
+        return _CMatrix(t.data_ptr(), rows, cols, strides[0] if rows > 1 else cols or 1, code, 0)
 
     def _vector(self, t, n: int):
         """The address of n f32 values next to each other, or None."""

@@ -215,6 +215,19 @@ def test_loss_and_gradients_in_large_tiles(det, n, vocab, width, gap, padding):
     check_loss(run_loss(det, h, w, t, gap, grad_mean=1.0), ref)
 
 
+@pytest.mark.parametrize("n,vocab,width,padding", [
+    (1, 66001, 40, 0.0), (16, 65600, 72, 0.0), (17, 70003, 136, 0.3), (33, 66001, 64, 0.1), (64, 65537, 200, 0.0), (65, 66001, 72, 0.0),
+    (16, 1057, 200, 0.0), (17, 1025, 584, 0.0), (64, 1090, 1000, 0.2), (9, 95, 2056, 0.0), (40, 65536, 72, 0.9),
+])
+def test_loss_and_gradients_of_few_rows(det, n, vocab, width, padding):
+    """Up to 64 rows, with vocabularies on both sides of the line between 32 and 128 words a workgroup."""
+    say(f"few rows n={n} vocab={vocab} width={width} padding={padding}")
+    h, w = randn((n, width), n + width, BF16), randn((vocab, width), n + vocab, BF16, 2 / width ** 0.5)
+    t = refs.tokens(n, vocab, n, padding)
+    ref = refs.Loss(h, w, t, grad_mean=1.0)
+    check_loss(run_loss(det, h, w, t, grad_mean=1.0), ref)
+
+
 @pytest.mark.parametrize("dtype", [BF16, F16])
 def test_mean_over_many_rows_does_not_underflow(det, dtype):
     """c = 1 / rows and small probabilities: G is far below the least f16 number if it is not scaled."""
