@@ -96,6 +96,17 @@ __device__ __forceinline__ uint64_t same_digit(uint32_t d, bool there) {
     return same;
 }
 
+// A store of data that is not read again soon.
+template <typename T, int V>
+__device__ __forceinline__ void write_through(T* p, const gd_vec<T, V>& q) {
+    if constexpr (sizeof(q) == 16) {
+        typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+        __builtin_nontemporal_store(*reinterpret_cast<const u32x4*>(&q), reinterpret_cast<u32x4*>(p));
+    } else {
+        *reinterpret_cast<gd_vec<T, V>*>(p) = q;
+    }
+}
+
 // Workgroup `block` of `blocks` fills its share.
 template <typename T, int V, int THREADS>
 __device__ __forceinline__ void fill_rows(const fill_args& f, uint32_t block, uint32_t blocks) {
@@ -107,16 +118,16 @@ __device__ __forceinline__ void fill_rows(const fill_args& f, uint32_t block, ui
         const uint64_t end = (uint64_t)f.to * f.width;
         for (uint64_t i = (uint64_t)f.from * f.width + ((uint64_t)block * THREADS + threadIdx.x) * V; i < end;
              i += (uint64_t)blocks * THREADS * V)
-            *reinterpret_cast<gd_vec<T, V>*>(p + i) = zero;
+            write_through(p + i, zero);
     } else {
         for (uint32_t r = f.from + block; r < f.to; r += blocks)
             for (uint32_t c = threadIdx.x * V; c < f.width; c += THREADS * V)
-                *reinterpret_cast<gd_vec<T, V>*>(static_cast<T*>(f.p) + (uint64_t)r * f.stride + c) = zero;
+                write_through(static_cast<T*>(f.p) + (uint64_t)r * f.stride + c, zero);
     }
 }
 
 // All passes by one workgroup of sixteen waves, the keys in its registers and, between passes, in the LDS.
-// A wave owns ONE_SORT / 16 keys next to each other, 64 a round.
+// A wave owns a stretch of keys, 64 a round.
 template <typename T, int V>
 __global__ __launch_bounds__(1024) void sort_alone(sort_args a, fill_args f) {
     if (blockIdx.x > 0) return fill_rows<T, V, 1024>(f, blockIdx.x - 1, gridDim.x - 1);
@@ -125,27 +136,30 @@ __global__ __launch_bounds__(1024) void sort_alone(sort_args a, fill_args f) {
     __shared__ uint16_t spos[ONE_SORT];
     __shared__ uint16_t next[WAVES][DIGITS];
     __shared__ uint32_t part[DIGITS / 64];
-    const uint32_t wave = threadIdx.x / 64, lane = threadIdx.x & 63, base = wave * (ONE_SORT / WAVES);
+    const uint32_t rounds = (a.n + 1023) / 1024;
+    const uint32_t wave = threadIdx.x / 64, lane = threadIdx.x & 63, base = wave * rounds * 64;
     uint32_t key[ROUNDS], pos[ROUNDS];
+    // (rounds that there are not have no keys: every lane is behind the end)
+    const auto there = [&](uint32_t r) { return r < rounds && base + r * 64 + lane < a.n; };
 #pragma unroll
     for (uint32_t r = 0; r < ROUNDS; ++r) {
         pos[r] = base + r * 64 + lane;
-        key[r] = pos[r] < a.n ? key_of(a.tokens, pos[r], a.vocab) : 0;
+        key[r] = there(r) ? key_of(a.tokens, pos[r], a.vocab) : 0;
     }
     for (uint32_t shift = 0; shift == 0 || (a.vocab >> shift) > 0; shift += BITS) {
         for (uint32_t i = threadIdx.x; i < WAVES * DIGITS; i += 1024) (&next[0][0])[i] = 0;
         __syncthreads();
-        uint32_t before[ROUNDS];
+        uint32_t before[ROUNDS] = {};
 #pragma unroll
         for (uint32_t r = 0; r < ROUNDS; ++r) {
             // (the wave's own counter: its lanes read it before the first of them adds)
             const uint32_t d = (key[r] >> shift) & (DIGITS - 1);
-            const bool there = base + r * 64 + lane < a.n;
-            const uint64_t same = same_digit(d, there);
+            if (r >= rounds) continue;
+            const uint64_t same = same_digit(d, there(r));
             const uint32_t mine = (uint32_t)__popcll(same & ((1ull << lane) - 1));
             before[r] = next[wave][d] + mine;
             __builtin_amdgcn_wave_barrier();
-            if (there && mine == 0) next[wave][d] = (uint16_t)(next[wave][d] + (uint32_t)__popcll(same));
+            if (there(r) && mine == 0) next[wave][d] = (uint16_t)(next[wave][d] + (uint32_t)__popcll(same));
             __builtin_amdgcn_wave_barrier();
         }
         __syncthreads();
@@ -176,7 +190,7 @@ __global__ __launch_bounds__(1024) void sort_alone(sort_args a, fill_args f) {
         __syncthreads();
 #pragma unroll
         for (uint32_t r = 0; r < ROUNDS; ++r)
-            if (base + r * 64 + lane < a.n) {
+            if (there(r)) {
                 const uint32_t at = next[wave][(key[r] >> shift) & (DIGITS - 1)] + before[r];
                 skey[at] = key[r];
                 spos[at] = (uint16_t)pos[r];
@@ -185,13 +199,13 @@ __global__ __launch_bounds__(1024) void sort_alone(sort_args a, fill_args f) {
 #pragma unroll
         for (uint32_t r = 0; r < ROUNDS; ++r) {
             const uint32_t i = base + r * 64 + lane;
-            if (i < a.n) { key[r] = skey[i]; pos[r] = spos[i]; }
+            if (there(r)) { key[r] = skey[i]; pos[r] = spos[i]; }
         }
     }
 #pragma unroll
     for (uint32_t r = 0; r < ROUNDS; ++r) {
         const uint32_t i = base + r * 64 + lane;
-        if (i < a.n) { a.key[0][i] = key[r]; a.pos[0][i] = pos[r]; }
+        if (there(r)) { a.key[0][i] = key[r]; a.pos[0][i] = pos[r]; }
     }
 }
 
@@ -273,14 +287,19 @@ __global__ __launch_bounds__(NT) void sort_scatter(sort_args a, fill_args f) {
         at[e] = a.scanned ? h[(uint64_t)blockIdx.x * DIGITS] : 0;
         all[e] = a.scanned ? h[(uint64_t)a.blocks * DIGITS] : 0;
     }
+    static_assert(PER == 2, "two digits a lane");
     if (!a.scanned)
-        for (uint32_t b = 0; b < a.blocks; ++b)
+        for (uint32_t b0 = 0; b0 < a.blocks; b0 += 16) {         // (sixteen loads on their way at once)
+            uint2 c[16];
 #pragma unroll
-            for (uint32_t e = 0; e < PER; ++e) {
-                const uint32_t c = a.hist[(uint64_t)b * DIGITS + threadIdx.x * PER + e];
-                all[e] += c;
-                if (b < blockIdx.x) at[e] += c;
+            for (uint32_t b = 0; b < 16; ++b)
+                c[b] = b0 + b < a.blocks ? reinterpret_cast<const uint2*>(a.hist + (uint64_t)(b0 + b) * DIGITS)[threadIdx.x] : make_uint2(0, 0);
+#pragma unroll
+            for (uint32_t b = 0; b < 16; ++b) {
+                all[0] += c[b].x; all[1] += c[b].y;
+                if (b0 + b < blockIdx.x) { at[0] += c[b].x; at[1] += c[b].y; }
             }
+        }
 #pragma unroll
     for (uint32_t e = 0; e < PER; ++e) total += all[e];
     uint32_t sum = total;
@@ -350,16 +369,24 @@ __global__ __launch_bounds__(NT) void grad_sum(gd_embed_grad_args a, const uint3
 #pragma unroll
     for (int j = 0; j < V; ++j) sum[j] = 0.0f;
     uint32_t token = begin;
+    uint32_t next_k[BATCH];
+    gd_vec<T, V> next_q[BATCH];
+    auto ask = [&](uint32_t i0) {
+#pragma unroll
+        for (uint32_t b = 0; b < BATCH; ++b) {
+            const uint32_t i = i0 + b;
+            next_k[b] = i < to ? key[i] : a.vocab;
+            // (one without a row: the stretch's first row once more)
+            next_q[b] = *reinterpret_cast<const gd_vec<T, V>*>(rows + (uint64_t)pos[next_k[b] != a.vocab ? i : from] * a.out_grad_stride);
+        }
+    };
+    ask(from);
     for (uint32_t i0 = from; i0 < to; i0 += BATCH) {
         uint32_t k[BATCH];
         gd_vec<T, V> q[BATCH];
 #pragma unroll
-        for (uint32_t b = 0; b < BATCH; ++b) {
-            const uint32_t i = i0 + b;
-            k[b] = i < to ? key[i] : a.vocab;
-            // (one without a row: the stretch's first row once more)
-            q[b] = *reinterpret_cast<const gd_vec<T, V>*>(rows + (uint64_t)pos[k[b] != a.vocab ? i : from] * a.out_grad_stride);
-        }
+        for (uint32_t b = 0; b < BATCH; ++b) { k[b] = next_k[b]; q[b] = next_q[b]; }
+        if (i0 + BATCH < to) ask(i0 + BATCH);
 #pragma unroll
         for (uint32_t b = 0; b < BATCH; ++b) {
             if (k[b] != token && token != a.vocab) {
@@ -399,23 +426,24 @@ __global__ __launch_bounds__(NT) void grad_join(gd_embed_grad_args a, const uint
                                                 uint32_t n, uint32_t span) {
     const uint32_t c = (blockIdx.y * NT + threadIdx.x) * V;
     const uint32_t from = blockIdx.x * span, to = min(from + span, n);
-    if (to >= n || c >= a.width) return;
+    if (to >= n) return;
     const uint32_t token = key[to - 1];
     if (token != key[to] || token == a.vocab) return;
     if (from && key[from - 1] == token) return;              // began earlier
+    // stretches that the token reaches into, 64 looked at at once
+    const uint32_t stretches = (n + span - 1) / span, lane = threadIdx.x & 63;
+    uint32_t hi = blockIdx.x + 1;
+    while (true) {
+        const uint32_t at = hi + lane;
+        const uint64_t other = __ballot(at >= stretches || key[(uint64_t)min(at, stretches - 1) * span] != token);
+        if (other) { hi += (uint32_t)__builtin_ctzll(other); break; }
+        hi += 64;
+    }
+    if (c >= a.width) return;
     const float* p = partial + ((uint64_t)blockIdx.x * 2 + 1) * a.width + c;
     float sum[V];
 #pragma unroll
     for (int j = 0; j < V; ++j) sum[j] = p[j];
-    // stretches that the token reaches into: a search by doubling, then by halves
-    const uint32_t stretches = (n + span - 1) / span;
-    uint32_t lo = blockIdx.x + 1, hi = lo + 1, step = 1;
-    while (hi < stretches && key[(uint64_t)hi * span] == token) { lo = hi; step *= 2; hi = lo + step; }
-    hi = min(hi, stretches);
-    while (hi - lo > 1) {
-        const uint32_t mid = lo + (hi - lo) / 2;
-        if (key[(uint64_t)mid * span] == token) lo = mid; else hi = mid;
-    }
     for (uint32_t s0 = blockIdx.x + 1; s0 < hi; s0 += BATCH) {
         gd_vec<float, V> q[BATCH];
 #pragma unroll

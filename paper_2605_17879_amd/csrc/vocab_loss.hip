@@ -411,49 +411,86 @@ __device__ __forceinline__ float2 join_sums(float2 a, float2 b) {
 }
 
 // Column j of a wave's tile over all of its rows (words rows[f] + 0..3), the same in the four lanes that share a
-// column i.  The target's logit is written where it is met; the tile is scaled to units of log 2.
+// column i.  What few tiles need stands behind branches that all lanes take alike: words behind the vocabulary's
+// end, and the target's logit, which is written where it is met.
 template <int FM, int FN>
 __device__ __forceinline__ float2 tile_sums(const product_args& p, f32x4 (&acc)[FM][FN], int j, const uint32_t (&rows)[FM], uint32_t i,
                                             uint32_t n, uint32_t lane) {
-    const int64_t t = i < n ? gd_token(p.targets, i) : -1;
+    const uint32_t here = p.vocab - p.v0;                        // rows of this launch's words below the vocabulary's end
+    const int64_t t = (i < n ? gd_token(p.targets, i) : -1) - (int64_t)p.v0;
+    const bool met = t >= (int64_t)rows[0] && t < (int64_t)rows[FM - 1] + 4;
+    if (__ballot(met)) {
+#pragma unroll
+        for (int f = 0; f < FM; ++f)
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+                if (t == (int64_t)(rows[f] + r) && rows[f] + r < here) p.target_logit[i] = acc[f][j][r] * p.scale;
+    }
+    const float scale2 = p.scale2;
+    if (scale2 < 0.0f) {
+#pragma unroll
+        for (int f = 0; f < FM; ++f) acc[f][j] = -acc[f][j];
+    }
+    const float up = fabsf(scale2);
     float top = -__builtin_inff();
+    const bool ends = __ballot(rows[FM - 1] + 3 >= here) != 0;
+    if (ends) {
+#pragma unroll
+        for (int f = 0; f < FM; ++f)
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+                if (rows[f] + r >= here) acc[f][j][r] = -__builtin_inff();
+    }
 #pragma unroll
     for (int f = 0; f < FM; ++f)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            const uint32_t v = p.v0 + rows[f] + r;
-            if (v < p.vocab) {
-                if (t == (int64_t)v) p.target_logit[i] = acc[f][j][r] * p.scale;
-                acc[f][j][r] *= p.scale2;
-            } else {
-                acc[f][j][r] = -__builtin_inff();
-            }
-            top = fmaxf(top, acc[f][j][r]);
-        }
+        for (int r = 0; r < 4; ++r) top = fmaxf(top, acc[f][j][r]);
     top = fmaxf(top, __uint_as_float(gd_lane_xor<16>(__float_as_uint(top), lane)));
     top = fmaxf(top, __uint_as_float(gd_lane_xor<32>(__float_as_uint(top), lane)));
-    const float from = top == -__builtin_inff() ? 0.0f : top;
+    // (a scale of 0, or nothing below the end: -inf times 0 is no number)
+    const float from = top == -__builtin_inff() ? 0.0f : top * up;
     float sum = 0.0f;
 #pragma unroll
     for (int f = 0; f < FM; ++f)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) sum += __builtin_amdgcn_exp2f(acc[f][j][r] - from);
+        for (int r = 0; r < 4; ++r) {
+            float e = __builtin_amdgcn_exp2f(fmaf(acc[f][j][r], up, -from));
+            if (ends && rows[f] + r >= here) e = 0.0f;
+            sum += e;
+        }
     sum += __uint_as_float(gd_lane_xor<16>(__float_as_uint(sum), lane));
     sum += __uint_as_float(gd_lane_xor<32>(__float_as_uint(sum), lane));
-    return make_float2(top, sum);
+    return make_float2(top == -__builtin_inff() ? top : from, sum);
 }
 
-// G of a row for the words v + 0..3.
+// A row of G: what all its words share.
+struct g_row {
+    float lse2, coef, low;           // lse and 64 less than it in units of log 2; the coefficient; 2^-64 of it
+    int32_t target;                  // from the launch's first word on
+    bool met;                        // among the wave's words
+    // Rows without a gradient have a coefficient of 0.
+    __device__ __forceinline__ g_row(const product_args& p, uint32_t i, bool there, uint32_t first, uint32_t last)
+        : lse2(there ? p.row_lse2[i] - 64.0f : 0.0f), coef(there ? p.row_coef[i] : 0.0f), low(coef * 5.421010862427522e-20f),
+          target(there ? p.row_target[i] - (int32_t)p.v0 : -1), met(target >= (int32_t)first && target <= (int32_t)last) {}
+};
+
+// G of a row for the words v + 0..3.  The exponential's instruction drops subnormal results: it is taken 2^64 times
+// as large, and the coefficient as much smaller.
 template <typename T>
-__device__ __forceinline__ gd_vec<T, 4> four_of_g(const product_args& p, const f32x4& logits, uint32_t v, int32_t t, float lse2, float coef,
-                                                  bool there) {
+__device__ __forceinline__ gd_vec<T, 4> four_of_g(const product_args& p, const f32x4& logits, uint32_t v, const g_row& row, bool rare) {
+    float x[4];
+#pragma unroll
+    for (int r = 0; r < 4; ++r) x[r] = __builtin_amdgcn_exp2f(fmaf(logits[r], p.scale2, -row.lse2)) * row.low;
+    if (rare) {                                                  // (the same for all lanes)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            if ((int32_t)(v + r) == row.target) x[r] -= row.coef;
+            if (v + r >= p.vocab - p.v0) x[r] = 0.0f;
+        }
+    }
     gd_vec<T, 4> q;
 #pragma unroll
-    for (int r = 0; r < 4; ++r) {
-        float e = exp2f(logits[r] * p.scale2 - lse2);            // (the instruction alone drops subnormal results)
-        if ((int32_t)(v + r) == t) e -= 1.0f;
-        q.v[r] = gd_from_f32<T>(there && v + r < p.vocab ? coef * e : 0.0f);
-    }
+    for (int r = 0; r < 4; ++r) q.v[r] = gd_from_f32<T>(x[r]);
     return q;
 }
 
@@ -524,11 +561,10 @@ __global__ __launch_bounds__(TILE::NT, 512 / TILE::NT) void product_kernel(const
 #pragma unroll
         for (int j = 0; j < FN; ++j) {
             const uint32_t i = col[j];                          // (there is room for whole tiles of rows)
-            const bool there = i < n;
-            const float lse2 = there ? p.row_lse2[i] : 0.0f, coef = there ? p.row_coef[i] : 0.0f;
-            const int32_t t = there ? p.row_target[i] : -1;
+            const g_row gr(p, i, i < n, row[0], row[FM - 1] + 3);
+            const bool rare = __ballot(gr.met || row[FM - 1] + 3 >= p.vocab - p.v0) != 0;
 #pragma unroll
-            for (int f = 0; f < FM; ++f) put(f, four_of_g<T>(p, acc[f][j], p.v0 + row[f], t, lse2, coef, there));
+            for (int f = 0; f < FM; ++f) put(f, four_of_g<T>(p, acc[f][j], row[f], gr, rare));
             take([&](uint32_t c, uint32_t m, const gd_vec<T, 8>& q) {
                 *reinterpret_cast<gd_vec<T, 8>*>(g + (uint64_t)(n0 + TILE::col_of(wn, j) + c) * p.ldc + m) = q;
             });
@@ -671,13 +707,12 @@ __global__ __launch_bounds__(256) void few_rows_kernel(const product_args p) {
 #pragma unroll
         for (int j = 0; j < FN; ++j) {
             const uint32_t i = n0 + j * 16 + (lane & 15);        // (there is room for whole tiles)
-            const bool there = i < n;
-            const float lse2 = there ? p.row_lse2[i] : 0.0f, coef = there ? p.row_coef[i] : 0.0f;
-            const int32_t t = there ? p.row_target[i] : -1;
+            const g_row gr(p, i, i < n, rows[0], rows[FM - 1] + 3);
+            const bool rare = __ballot(gr.met || rows[FM - 1] + 3 >= p.vocab - p.v0) != 0;
 #pragma unroll
             for (int f = 0; f < FM; ++f)
                 *reinterpret_cast<gd_vec<T, 4>*>(static_cast<T*>(p.c) + (uint64_t)i * p.ldc + rows[f]) =
-                    four_of_g<T>(p, acc[f][j], p.v0 + rows[f], t, lse2, coef, there);
+                    four_of_g<T>(p, acc[f][j], rows[f], gr, rare);
         }
         // (the weights' gradient takes the rows in blocks of 64)
 #pragma unroll
@@ -911,9 +946,9 @@ __global__ __launch_bounds__(1024) void prepare_rows(const rows_args a) {
     if (threadIdx.x == 0) scale.write(a.head, count);
 }
 
-// The list and the gathered rows in one launch, for up to GATHER rows: every workgroup makes the list for itself, the
-// first one writes it down.
-constexpr uint32_t GATHER = 2048;
+// The list and the gathered rows in one launch, for up to GATHER rows, one a lane: every workgroup makes the list for
+// itself, the first one writes it down.  (With eight rows a lane and 2 000 rows this took 24 us, two launches 12.)
+constexpr uint32_t GATHER = 256;
 template <typename T>
 __global__ __launch_bounds__(256) void gather_rows(const rows_args a, const void* in, uint64_t stride, uint32_t width, T* out, uint32_t ldo) {
     constexpr uint32_t PER = GATHER / 256;
