@@ -338,25 +338,25 @@ __global__ __launch_bounds__(NT) void fill_kernel(fill_args f) { fill_rows<T, V,
 
 // ---- sums over stretches of the sorted list -----------------------------------------------
 
+// A token's row of the gradient from its sum and, where that is added to, its old values.
 template <typename T, int V>
-__device__ __forceinline__ void write_sum(const gd_embed_grad_args& a, uint32_t token, uint32_t c, const float sum[V]) {
-    gd_vec<T, V>* p = reinterpret_cast<gd_vec<T, V>*>(static_cast<T*>(a.weight_grad) + (uint64_t)token * a.weight_grad_stride + c);
+__device__ __forceinline__ void write_sum(const gd_embed_grad_args& a, uint32_t token, uint32_t c, const float sum[V], bool add,
+                                          const gd_vec<T, V>& old) {
     gd_vec<T, V> q;
-    if (a.accumulate) {
-        q = *p;
 #pragma unroll
-        for (int j = 0; j < V; ++j) q.v[j] = gd_from_f32<T>(gd_to_f32(q.v[j]) + a.scale * sum[j]);
-    } else {
-#pragma unroll
-        for (int j = 0; j < V; ++j) q.v[j] = gd_from_f32<T>(a.scale * sum[j]);
-    }
-    *p = q;
+    for (int j = 0; j < V; ++j) q.v[j] = gd_from_f32<T>(add ? gd_to_f32(old.v[j]) + a.scale * sum[j] : a.scale * sum[j]);
+    *reinterpret_cast<gd_vec<T, V>*>(static_cast<T*>(a.weight_grad) + (uint64_t)token * a.weight_grad_stride + c) = q;
+}
+template <typename T, int V>
+__device__ __forceinline__ gd_vec<T, V> old_row(const gd_embed_grad_args& a, uint32_t token, uint32_t c) {
+    return *reinterpret_cast<const gd_vec<T, V>*>(static_cast<const T*>(a.weight_grad) + (uint64_t)token * a.weight_grad_stride + c);
 }
 
 // Stretch blockIdx.x of `span` entries, columns by blockIdx.y.  partial: [stretch][2][width], the sums of
 // a token that began before the stretch and of one that goes on behind it.  Rows are asked for BATCH at a
-// time, whatever their tokens.
-template <typename T, int V>
+// time, whatever their tokens: with ADD together with the tokens' old rows (one after another, each was waited for),
+// without it a batch ahead.
+template <typename T, int V, bool ADD>
 __global__ __launch_bounds__(NT) void grad_sum(gd_embed_grad_args a, const uint32_t* __restrict__ key, const uint32_t* __restrict__ pos,
                                                float* partial, uint32_t n, uint32_t span) {
     const uint32_t c = (blockIdx.y * NT + threadIdx.x) * V;
@@ -368,56 +368,53 @@ __global__ __launch_bounds__(NT) void grad_sum(gd_embed_grad_args a, const uint3
     float sum[V];
 #pragma unroll
     for (int j = 0; j < V; ++j) sum[j] = 0.0f;
-    uint32_t token = begin;
-    uint32_t next_k[BATCH];
-    gd_vec<T, V> next_q[BATCH];
+    uint32_t token = begin, k[BATCH];
+    gd_vec<T, V> q[BATCH], old[ADD ? BATCH : 1], held{};
     auto ask = [&](uint32_t i0) {
 #pragma unroll
         for (uint32_t b = 0; b < BATCH; ++b) {
             const uint32_t i = i0 + b;
-            next_k[b] = i < to ? key[i] : a.vocab;
+            k[b] = i < to ? key[i] : a.vocab;
             // (one without a row: the stretch's first row once more)
-            next_q[b] = *reinterpret_cast<const gd_vec<T, V>*>(rows + (uint64_t)pos[next_k[b] != a.vocab ? i : from] * a.out_grad_stride);
+            const bool row = k[b] != a.vocab;
+            q[b] = *reinterpret_cast<const gd_vec<T, V>*>(rows + (uint64_t)pos[row ? i : from] * a.out_grad_stride);
+            if constexpr (ADD)
+                if (row && k[b] != before && k[b] != behind) old[b] = old_row<T, V>(a, k[b], c);
         }
     };
-    ask(from);
-    for (uint32_t i0 = from; i0 < to; i0 += BATCH) {
-        uint32_t k[BATCH];
-        gd_vec<T, V> q[BATCH];
+    // The token's rows here are summed up.
+    auto finish = [&]() {
+        if (token == before || token == behind) {            // (the stretch's first one, or its last)
+            float* p = partial + ((uint64_t)blockIdx.x * 2 + (token == before ? 0 : 1)) * a.width + c;
 #pragma unroll
-        for (uint32_t b = 0; b < BATCH; ++b) { k[b] = next_k[b]; q[b] = next_q[b]; }
-        if (i0 + BATCH < to) ask(i0 + BATCH);
+            for (int j = 0; j < V; ++j) p[j] = sum[j];
+        } else {
+            write_sum<T, V>(a, token, c, sum, ADD, held);
+        }
+    };
+    if (!ADD) ask(from);
+    for (uint32_t i0 = from; i0 < to; i0 += BATCH) {
+        if (ADD) ask(i0);
+        uint32_t now_k[BATCH];
+        gd_vec<T, V> now_q[BATCH];
+#pragma unroll
+        for (uint32_t b = 0; b < BATCH; ++b) { now_k[b] = k[b]; now_q[b] = q[b]; }
+        if (!ADD && i0 + BATCH < to) ask(i0 + BATCH);
 #pragma unroll
         for (uint32_t b = 0; b < BATCH; ++b) {
-            if (k[b] != token && token != a.vocab) {
-                if (token == before) {                       // (only the stretch's first token can be)
-                    float* p = partial + ((uint64_t)blockIdx.x * 2) * a.width + c;
-#pragma unroll
-                    for (int j = 0; j < V; ++j) p[j] = sum[j];
-                } else if (token == behind) {                // (the stretch's last, at its end)
-                    float* p = partial + ((uint64_t)blockIdx.x * 2 + 1) * a.width + c;
-#pragma unroll
-                    for (int j = 0; j < V; ++j) p[j] = sum[j];
-                } else {
-                    write_sum<T, V>(a, token, c, sum);
-                }
+            if (now_k[b] != token && token != a.vocab) {
+                finish();
 #pragma unroll
                 for (int j = 0; j < V; ++j) sum[j] = 0.0f;
             }
-            token = k[b];
+            token = now_k[b];
+            if constexpr (ADD) held = old[b];
             if (token != a.vocab)
 #pragma unroll
-                for (int j = 0; j < V; ++j) sum[j] += gd_to_f32(q[b].v[j]);
+                for (int j = 0; j < V; ++j) sum[j] += gd_to_f32(now_q[b].v[j]);
         }
     }
-    if (token == a.vocab) return;
-    if (token == behind || token == before) {
-        float* p = partial + ((uint64_t)blockIdx.x * 2 + (token == before ? 0 : 1)) * a.width + c;
-#pragma unroll
-        for (int j = 0; j < V; ++j) p[j] = sum[j];
-    } else {
-        write_sum<T, V>(a, token, c, sum);
-    }
+    if (token != a.vocab) finish();
 }
 
 // The token that begins in stretch blockIdx.x and goes on behind it: its parts in order.
@@ -441,21 +438,22 @@ __global__ __launch_bounds__(NT) void grad_join(gd_embed_grad_args a, const uint
     }
     if (c >= a.width) return;
     const float* p = partial + ((uint64_t)blockIdx.x * 2 + 1) * a.width + c;
+    constexpr uint32_t PARTS = 16;                            // on their way at once
     float sum[V];
 #pragma unroll
     for (int j = 0; j < V; ++j) sum[j] = p[j];
-    for (uint32_t s0 = blockIdx.x + 1; s0 < hi; s0 += BATCH) {
-        gd_vec<float, V> q[BATCH];
+    for (uint32_t s0 = blockIdx.x + 1; s0 < hi; s0 += PARTS) {
+        gd_vec<float, V> q[PARTS];
 #pragma unroll
-        for (uint32_t b = 0; b < BATCH; ++b)
+        for (uint32_t b = 0; b < PARTS; ++b)
             q[b] = *reinterpret_cast<const gd_vec<float, V>*>(partial + (uint64_t)min(s0 + b, hi - 1) * 2 * a.width + c);
 #pragma unroll
-        for (uint32_t b = 0; b < BATCH; ++b)
+        for (uint32_t b = 0; b < PARTS; ++b)
             if (s0 + b < hi)
 #pragma unroll
                 for (int j = 0; j < V; ++j) sum[j] += q[b].v[j];
     }
-    write_sum<T, V>(a, token, c, sum);
+    write_sum<T, V>(a, token, c, sum, a.accumulate, a.accumulate ? old_row<T, V>(a, token, c) : gd_vec<T, V>{});
 }
 
 struct grad_layout {
@@ -527,9 +525,15 @@ hipError_t launch_grad(const gd_embed_grad_args& a, hipStream_t s) {
     }
     float* partial = reinterpret_cast<float*>(a.work + l.partial);
     const dim3 grid((n + l.span - 1) / l.span, (a.width + NT * V - 1) / (NT * V));
-    hipLaunchKernelGGL((grad_sum<T, V>), grid, dim3(NT), 0, s, a, b.key[sorted], b.pos[sorted], partial, n, l.span);
-    if (n > l.span)
-        hipLaunchKernelGGL((grad_join<T, V>), grid, dim3(NT), 0, s, a, b.key[sorted], partial, n, l.span);
+    if (a.accumulate)
+        hipLaunchKernelGGL((grad_sum<T, V, true>), grid, dim3(NT), 0, s, a, b.key[sorted], b.pos[sorted], partial, n, l.span);
+    else
+        hipLaunchKernelGGL((grad_sum<T, V, false>), grid, dim3(NT), 0, s, a, b.key[sorted], b.pos[sorted], partial, n, l.span);
+    if (n > l.span) {
+        constexpr int W = V < 4 ? V : 4;                      // (16 bytes of fp32)
+        const dim3 join(grid.x, (a.width + NT * W - 1) / (NT * W));
+        hipLaunchKernelGGL((grad_join<T, W>), join, dim3(NT), 0, s, a, b.key[sorted], partial, n, l.span);
+    }
     return hipGetLastError();
 }
 
