@@ -725,37 +725,30 @@ __global__ __launch_bounds__(256) void few_rows_kernel(const product_args p) {
 
 // ---- around the products -------------------------------------------------------------------
 
-// Row r of `in` (or zeros) into a padded row, by a workgroup of 256.
-template <typename T>
-__device__ __forceinline__ void pack_row(const void* in, uint64_t stride, uint32_t width, bool there, uint64_t r, T* to, uint32_t ldo) {
-    const T* from = static_cast<const T*>(in) + r * stride;
-    if (((uintptr_t)in & 15) == 0 && stride % 8 == 0 && width % 8 == 0) {
-        for (uint32_t c = threadIdx.x * 8; c < ldo; c += 256 * 8) {
-            gd_vec<T, 8> q{};
-            if (there && c < width) q = *reinterpret_cast<const gd_vec<T, 8>*>(from + c);
-            *reinterpret_cast<gd_vec<T, 8>*>(to + c) = q;
-        }
-    } else {
-        // elements one by one, eight of a lane at once
-        for (uint32_t c = threadIdx.x * 8; c < ldo; c += 256 * 8) {
-            gd_vec<T, 8> q{};
-#pragma unroll
-            for (uint32_t j = 0; j < 8; ++j)
-                if (there && c + j < width) q.v[j] = from[c + j];
-            *reinterpret_cast<gd_vec<T, 8>*>(to + c) = q;
-        }
-    }
-}
-
-// Rows of `in` (all, or those listed) into rows of a padded copy: zeros behind the row's end and, behind a list, up
-// to the next 256 rows.
+// Rows of `in` (all, or those listed) into rows of a padded copy, eight elements a lane: zeros behind the row's end
+// and, behind a list, up to the next 256 rows.
 template <typename T>
 __global__ __launch_bounds__(256) void pack_kernel(const void* in, uint64_t stride, uint32_t width, const grad_head* head,
                                                    const uint32_t* rows, uint32_t n, T* out, uint32_t ldo) {
     if (head) n = head->count;
-    const uint32_t last = head ? (n + 255) / 256 * 256 : n;
-    for (uint64_t r = blockIdx.x; r < last; r += gridDim.x)
-        pack_row<T>(in, stride, width, r < n, r < n ? (rows ? (uint64_t)rows[r] : r) : 0, out + r * ldo, ldo);
+    const uint32_t last = head ? (n + 255) / 256 * 256 : n, chunks = ldo / 8;
+    const bool whole = ((uintptr_t)in & 15) == 0 && stride % 8 == 0 && width % 8 == 0;
+    const uint64_t total = (uint64_t)last * chunks;
+    for (uint64_t x = (uint64_t)blockIdx.x * 256 + threadIdx.x; x < total; x += (uint64_t)gridDim.x * 256) {
+        const uint32_t r = (uint32_t)(x / chunks), c = (uint32_t)(x - (uint64_t)r * chunks) * 8;
+        gd_vec<T, 8> q{};
+        if (r < n) {
+            const T* from = static_cast<const T*>(in) + (rows ? (uint64_t)rows[r] : (uint64_t)r) * stride + c;
+            if (whole) {
+                q = *reinterpret_cast<const gd_vec<T, 8>*>(from);
+            } else {
+#pragma unroll
+                for (uint32_t j = 0; j < 8; ++j)
+                    if (c + j < width) q.v[j] = from[j];
+            }
+        }
+        *reinterpret_cast<gd_vec<T, 8>*>(out + (uint64_t)r * ldo + c) = q;
+    }
 }
 
 // Sums joined over the lanes of a wave.
@@ -946,51 +939,6 @@ __global__ __launch_bounds__(1024) void prepare_rows(const rows_args a) {
     if (threadIdx.x == 0) scale.write(a.head, count);
 }
 
-// The list and the gathered rows in one launch, for up to GATHER rows, one a lane: every workgroup makes the list for
-// itself, the first one writes it down.  (With eight rows a lane and 2 000 rows this took 24 us, two launches 12.)
-constexpr uint32_t GATHER = 256;
-template <typename T>
-__global__ __launch_bounds__(256) void gather_rows(const rows_args a, const void* in, uint64_t stride, uint32_t width, T* out, uint32_t ldo) {
-    constexpr uint32_t PER = GATHER / 256;
-    __shared__ uint32_t s[4], counts[PER][4];
-    __shared__ uint16_t list[GATHER];
-    const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x / 64, n = a.targets.n;
-    float c[PER];
-    uint32_t top = 0, at[PER];
-#pragma unroll
-    for (uint32_t j = 0; j < PER; ++j) {
-        const uint32_t i = j * 256 + threadIdx.x;
-        c[j] = i < n ? coef_of(a, i) : 0.0f;
-        top = max(top, __float_as_uint(c[j]) & 0x7FFFFFFFu);
-        const uint64_t who = __ballot(c[j] != 0.0f);
-        at[j] = (uint32_t)__popcll(who & ((1ull << lane) - 1));
-        if (lane == 0) counts[j][wave] = (uint32_t)__popcll(who);
-    }
-    top = wave_max(top, lane);
-    if (lane == 0) s[wave] = top;
-    __syncthreads();
-    const coef_scale scale(max(max(s[0], s[1]), max(s[2], s[3])), a.half);
-    uint32_t count = 0;
-#pragma unroll
-    for (uint32_t j = 0; j < PER; ++j) {
-        uint32_t before = count;
-#pragma unroll
-        for (uint32_t w = 0; w < 4; ++w) { if (w < wave) before += counts[j][w]; count += counts[j][w]; }
-        at[j] += before;
-        const uint32_t i = j * 256 + threadIdx.x;
-        const bool in = c[j] != 0.0f;
-        if (in) list[at[j]] = (uint16_t)i;
-        if (blockIdx.x == 0) {
-            if (in) write_row(a, i, at[j], scale.of(c[j]));
-            if (i < n) a.slot[i] = in ? (int32_t)at[j] : -1;
-        }
-    }
-    if (blockIdx.x == 0 && threadIdx.x == 0) scale.write(a.head, count);
-    __syncthreads();
-    for (uint32_t r = blockIdx.x; r < (count + 255) / 256 * 256; r += gridDim.x)
-        pack_row<T>(in, stride, width, r < count, r < count ? list[r] : 0, out + (uint64_t)r * ldo, ldo);
-}
-
 // dH from its slabs, added up in order; zeros where a row has no gradient.  Four columns a lane.
 template <typename T>
 __global__ __launch_bounds__(256) void finish_hidden(const float* slabs, uint32_t lds, uint64_t slab, uint32_t splits,
@@ -1007,14 +955,21 @@ __global__ __launch_bounds__(256) void finish_hidden(const float* slabs, uint32_
         if (at >= 0) {
             const float* from = slabs + (uint64_t)at * lds + c;
             uint32_t s = 0;
-            for (; s + 4 <= splits; s += 4) {
-                f32x4 q[4];
+            for (; s + 8 <= splits; s += 8) {
+                f32x4 q[8];
 #pragma unroll
-                for (uint32_t b = 0; b < 4; ++b) q[b] = *reinterpret_cast<const f32x4*>(from + (s + b) * slab);
+                for (uint32_t b = 0; b < 8; ++b) q[b] = *reinterpret_cast<const f32x4*>(from + (s + b) * slab);
 #pragma unroll
-                for (uint32_t b = 0; b < 4; ++b) sum += q[b];
+                for (uint32_t b = 0; b < 8; ++b) sum += q[b];
             }
-            for (; s < splits; ++s) sum += *reinterpret_cast<const f32x4*>(from + s * slab);
+            if (s < splits) {
+                f32x4 q[7];
+#pragma unroll
+                for (uint32_t b = 0; b < 7; ++b) q[b] = *reinterpret_cast<const f32x4*>(from + min(s + b, splits - 1) * slab);
+#pragma unroll
+                for (uint32_t b = 0; b < 7; ++b)
+                    if (s + b < splits) sum += q[b];
+            }
         }
         gd_vec<T, 4> q;
 #pragma unroll
@@ -1224,7 +1179,7 @@ hipError_t forward(const gd_vocab_loss_args& a, hipStream_t s) {
     product_args p = {};
     p.b = operand{a.hidden, a.hidden_stride, n, a.width};
     if (!direct(a.hidden, a.hidden_stride, a.width)) {
-        hipLaunchKernelGGL((pack_kernel<T>), dim3(n < 65536 ? n : 65536), dim3(256), 0, s, a.hidden, a.hidden_stride, a.width,
+        hipLaunchKernelGGL((pack_kernel<T>), dim3(blocks_for((uint64_t)n * ldh / 8)), dim3(256), 0, s, a.hidden, a.hidden_stride, a.width,
                            (const grad_head*)nullptr, (const uint32_t*)nullptr, n, hidden, ldh);
         p.b = operand{hidden, ldh, n, ldh};
     }
@@ -1242,7 +1197,7 @@ hipError_t forward(const gd_vocab_loss_args& a, hipStream_t s) {
         if (plain) {
             p.a = operand{w, a.weight_stride, here, a.width};
         } else {
-            hipLaunchKernelGGL((pack_kernel<T>), dim3(here < 65536 ? here : 65536), dim3(256), 0, s, w, a.weight_stride, a.width,
+            hipLaunchKernelGGL((pack_kernel<T>), dim3(blocks_for((uint64_t)here * ldh / 8)), dim3(256), 0, s, w, a.weight_stride, a.width,
                                (const grad_head*)nullptr, (const uint32_t*)nullptr, here, weight, ldh);
             p.a = operand{weight, ldh, here, ldh};
         }
@@ -1282,13 +1237,9 @@ hipError_t backward(const gd_vocab_grad_args& a, hipStream_t s) {
     r.row_coef = reinterpret_cast<float*>(a.work + l.coef);
     r.row_target = reinterpret_cast<int32_t*>(a.work + l.target);
     const uint32_t padded = (uint32_t)l.padded_rows;
-    if (n <= GATHER) {
-        hipLaunchKernelGGL((gather_rows<T>), dim3(padded), dim3(256), 0, s, r, a.hidden, a.hidden_stride, a.width, hidden, ldh);
-    } else {
-        hipLaunchKernelGGL(prepare_rows, dim3(1), dim3(1024), 0, s, r);
-        hipLaunchKernelGGL((pack_kernel<T>), dim3(padded < 16384 ? padded : 16384), dim3(256), 0, s, a.hidden, a.hidden_stride, a.width,
-                           head, r.rows, n, hidden, ldh);
-    }
+    hipLaunchKernelGGL(prepare_rows, dim3(1), dim3(1024), 0, s, r);
+    hipLaunchKernelGGL((pack_kernel<T>), dim3(blocks_for((uint64_t)padded * ldh / 8)), dim3(256), 0, s, a.hidden, a.hidden_stride, a.width,
+                       head, r.rows, n, hidden, ldh);
     const bool plain = direct(a.weight, a.weight_stride, a.width);
     uint32_t piece = (uint32_t)l.piece;
     if (!plain && piece > l.pack_piece) piece = (uint32_t)l.pack_piece;
@@ -1298,7 +1249,7 @@ hipError_t backward(const gd_vocab_grad_args& a, hipStream_t s) {
         const T* w = static_cast<const T*>(a.weight) + (uint64_t)v0 * a.weight_stride;
         operand wo{w, a.weight_stride, here, a.width};
         if (!plain) {
-            hipLaunchKernelGGL((pack_kernel<T>), dim3(here < 65536 ? here : 65536), dim3(256), 0, s, w, a.weight_stride, a.width,
+            hipLaunchKernelGGL((pack_kernel<T>), dim3(blocks_for((uint64_t)here * ldh / 8)), dim3(256), 0, s, w, a.weight_stride, a.width,
                                (const grad_head*)nullptr, (const uint32_t*)nullptr, here, weight, ldh);
             wo = operand{weight, ldh, here, ldh};
         }
