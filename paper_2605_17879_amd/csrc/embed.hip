@@ -24,6 +24,17 @@ constexpr uint32_t SELF_SCAN = 64;        // most workgroups of a pass that add 
 constexpr uint32_t BATCH = 8;             // rows on their way at once in the sums
 constexpr uint32_t NO_ROW = 0xFFFFFFFFu;
 
+// A store of data that is not read again soon.
+template <typename T, int V>
+__device__ __forceinline__ void write_through(T* p, const gd_vec<T, V>& q) {
+    if constexpr (sizeof(q) == 16) {
+        typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+        __builtin_nontemporal_store(*reinterpret_cast<const u32x4*>(&q), reinterpret_cast<u32x4*>(p));
+    } else {
+        *reinterpret_cast<gd_vec<T, V>*>(p) = q;
+    }
+}
+
 // ---- lookup ------------------------------------------------------------------------------------
 
 // tx lanes side by side on a row, NT / tx rows a workgroup; V elements a lane at a time.
@@ -42,7 +53,7 @@ __global__ __launch_bounds__(NT) void embed_kernel(const gd_embed_args a, uint32
         if (row) q = *reinterpret_cast<const gd_vec<T, V>*>(w + c);
 #pragma unroll
         for (int j = 0; j < V; ++j) q.v[j] = gd_from_f32<T>(row ? gd_to_f32(q.v[j]) * a.scale : other);
-        *reinterpret_cast<gd_vec<T, V>*>(out + c) = q;
+        write_through(out + c, q);
     }
 }
 
@@ -94,17 +105,6 @@ __device__ __forceinline__ uint64_t same_digit(uint32_t d, bool there) {
         same &= ((d >> b) & 1) ? with : ~with;
     }
     return same;
-}
-
-// A store of data that is not read again soon.
-template <typename T, int V>
-__device__ __forceinline__ void write_through(T* p, const gd_vec<T, V>& q) {
-    if constexpr (sizeof(q) == 16) {
-        typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-        __builtin_nontemporal_store(*reinterpret_cast<const u32x4*>(&q), reinterpret_cast<u32x4*>(p));
-    } else {
-        *reinterpret_cast<gd_vec<T, V>*>(p) = q;
-    }
 }
 
 // Workgroup `block` of `blocks` fills its share.

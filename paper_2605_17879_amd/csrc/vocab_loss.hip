@@ -835,24 +835,34 @@ __global__ __launch_bounds__(1024) void join_alone(const join_args a, uint32_t s
 
 // Mean over the rows not left out, one workgroup, in a fixed order.
 __global__ __launch_bounds__(1024) void mean_kernel(const float* loss, gd_token_list targets, float* mean) {
-    __shared__ float s[1024];
-    __shared__ uint32_t c[1024];
+    __shared__ float s[16];
+    __shared__ uint32_t c[16];
+    const uint32_t wave = threadIdx.x / 64, lane = threadIdx.x & 63;
     float sum = 0.0f;
     uint32_t count = 0;
+#pragma unroll 4
     for (uint32_t i = threadIdx.x; i < targets.n; i += 1024) {
         sum += loss[i];
         count += gd_token(targets, i) >= 0;
     }
-    s[threadIdx.x] = sum;
-    c[threadIdx.x] = count;
-    __syncthreads();
-    for (uint32_t d = 512; d > 0; d >>= 1) {
-        if (threadIdx.x < d) { s[threadIdx.x] += s[threadIdx.x + d]; c[threadIdx.x] += c[threadIdx.x + d]; }
-        __syncthreads();
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) {
+        sum += __shfl_xor(sum, d);
+        count += __shfl_xor(count, d);
     }
-    if (threadIdx.x == 0) {
-        mean[0] = s[0] / fmaxf((float)c[0], 1.0f);
-        mean[1] = (float)c[0];
+    if (lane == 0) { s[wave] = sum; c[wave] = count; }
+    __syncthreads();
+    if (wave > 0) return;
+    sum = lane < 16 ? s[lane] : 0.0f;
+    count = lane < 16 ? c[lane] : 0;
+#pragma unroll
+    for (int d = 8; d > 0; d >>= 1) {
+        sum += __shfl_xor(sum, d);
+        count += __shfl_xor(count, d);
+    }
+    if (lane == 0) {
+        mean[0] = sum / fmaxf((float)count, 1.0f);
+        mean[1] = (float)count;
     }
 }
 
