@@ -24,17 +24,6 @@ constexpr uint32_t SELF_SCAN = 64;        // most workgroups of a pass that add 
 constexpr uint32_t BATCH = 8;             // rows on their way at once in the sums
 constexpr uint32_t NO_ROW = 0xFFFFFFFFu;
 
-// A store of data that is not read again soon.
-template <typename T, int V>
-__device__ __forceinline__ void write_through(T* p, const gd_vec<T, V>& q) {
-    if constexpr (sizeof(q) == 16) {
-        typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-        __builtin_nontemporal_store(*reinterpret_cast<const u32x4*>(&q), reinterpret_cast<u32x4*>(p));
-    } else {
-        *reinterpret_cast<gd_vec<T, V>*>(p) = q;
-    }
-}
-
 // ---- lookup ------------------------------------------------------------------------------------
 
 // tx lanes side by side on a row, NT / tx rows a workgroup; V elements a lane at a time.
@@ -53,7 +42,7 @@ __global__ __launch_bounds__(NT) void embed_kernel(const gd_embed_args a, uint32
         if (row) q = *reinterpret_cast<const gd_vec<T, V>*>(w + c);
 #pragma unroll
         for (int j = 0; j < V; ++j) q.v[j] = gd_from_f32<T>(row ? gd_to_f32(q.v[j]) * a.scale : other);
-        write_through(out + c, q);
+        gd_write_through(out + c, q);
     }
 }
 
@@ -118,11 +107,11 @@ __device__ __forceinline__ void fill_rows(const fill_args& f, uint32_t block, ui
         const uint64_t end = (uint64_t)f.to * f.width;
         for (uint64_t i = (uint64_t)f.from * f.width + ((uint64_t)block * THREADS + threadIdx.x) * V; i < end;
              i += (uint64_t)blocks * THREADS * V)
-            write_through(p + i, zero);
+            gd_write_through(p + i, zero);
     } else {
         for (uint32_t r = f.from + block; r < f.to; r += blocks)
             for (uint32_t c = threadIdx.x * V; c < f.width; c += THREADS * V)
-                write_through(static_cast<T*>(f.p) + (uint64_t)r * f.stride + c, zero);
+                gd_write_through(static_cast<T*>(f.p) + (uint64_t)r * f.stride + c, zero);
     }
 }
 
@@ -345,7 +334,7 @@ __device__ __forceinline__ void write_sum(const gd_embed_grad_args& a, uint32_t 
     gd_vec<T, V> q;
 #pragma unroll
     for (int j = 0; j < V; ++j) q.v[j] = gd_from_f32<T>(add ? gd_to_f32(old.v[j]) + a.scale * sum[j] : a.scale * sum[j]);
-    *reinterpret_cast<gd_vec<T, V>*>(static_cast<T*>(a.weight_grad) + (uint64_t)token * a.weight_grad_stride + c) = q;
+    gd_write_through(static_cast<T*>(a.weight_grad) + (uint64_t)token * a.weight_grad_stride + c, q);
 }
 template <typename T, int V>
 __device__ __forceinline__ gd_vec<T, V> old_row(const gd_embed_grad_args& a, uint32_t token, uint32_t c) {

@@ -96,6 +96,17 @@ template <typename T> __device__ __forceinline__ T gd_from_f32(float v) { return
 
 // V elements at once (V * sizeof(T) = 4, 8 or 16 bytes, aligned to that).
 template <typename T, int V> struct alignas(sizeof(T) * V) gd_vec { T v[V]; };
+
+// A store of data that is not read again soon.
+template <typename T, int V>
+__device__ __forceinline__ void gd_write_through(T* p, const gd_vec<T, V>& q) {
+    if constexpr (sizeof(q) == 16) {
+        typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+        __builtin_nontemporal_store(*reinterpret_cast<const u32x4*>(&q), reinterpret_cast<u32x4*>(p));
+    } else {
+        *reinterpret_cast<gd_vec<T, V>*>(p) = q;
+    }
+}
 #endif
 
 #endif  // GD_OPERATORS_H_

@@ -601,7 +601,7 @@ __global__ __launch_bounds__(TILE::NT, 512 / TILE::NT) void product_kernel(const
                 if (i >= p.n) return;
                 T* to = out + (uint64_t)i * p.ldc + m;
                 if (whole && m + 8 <= p.m) {
-                    *reinterpret_cast<gd_vec<T, 8>*>(to) = q;
+                    gd_write_through(to, q);
                 } else {
 #pragma unroll
                     for (uint32_t r = 0; r < 8; ++r)
