@@ -121,6 +121,19 @@ def test_lookup_grad(det, accumulate, dtype, n, vocab, width, gap):
     check_grad(det, randn((n, width), n, dtype), t, vocab, 1.7, accumulate, randn((vocab, width), n + 2, dtype), gap)
 
 
+@pytest.mark.parametrize("n", [5, 5000])
+@pytest.mark.parametrize("gap", [8, 3])
+def test_lookup_grad_into_rows_apart(det, n, gap):
+    """Zeros and sums stay inside the rows."""
+    vocab, width = 333, 48
+    t, g = refs.tokens(n, vocab, 4, 0.1), randn((n, width), 5, BF16)
+    store = torch.full((vocab, width + gap), 9.0, dtype=BF16, device="cuda")
+    det.embed_grad(g.cuda(), t.cuda(), store[:, :width], det.alloc_embed_grad_work(n, vocab, width), scale=0.5)
+    ref, bound = refs.lookup_grad(g, t, 0.5, vocab)
+    within(store[:, :width], ref, bound, "gradient")
+    assert bool((store[:, width:] == 9).all())
+
+
 @pytest.mark.parametrize("n", [32, 64, 95, 1000, 40000])
 def test_lookup_grad_of_one_token(det, n):
     """Every row is the same token's: one sum over all stretches."""
@@ -283,6 +296,30 @@ def test_confident_rows_and_far_logits(det):
     check_loss(run_loss(det, h, w, t, grad_mean=1.0), ref)
 
 
+@pytest.mark.parametrize("scale", [-0.75, 0.0])
+@pytest.mark.parametrize("n,vocab,width", [(9, 300, 64), (300, 5001, 72), (2100, 9001, 72)])
+def test_logit_scales_below_one(det, scale, n, vocab, width):
+    """A negative scale turns the order of the logits round; a scale of 0 leaves them all alike."""
+    h, w, t = randn((n, width), 1, BF16), randn((vocab, width), 2, BF16, 0.5), refs.tokens(n, vocab, 3, 0.1)
+    ref = refs.Loss(h, w, t, scale, grad_mean=1.0)
+    check_loss(run_loss(det, h, w, t, 0, scale, grad_mean=1.0), ref)
+
+
+def test_strided_targets_and_gradients(det):
+    n, V, d = 150, 700, 72
+    h, w = randn((n, d), 1, BF16), randn((V, d), 2, BF16, 0.3)
+    t = refs.tokens(2 * n, V, 3, 0.1)
+    ref = refs.Loss(h, w, t[::2], grad_mean=1.0)
+    out, work = det.alloc_vocab_loss(n), det.alloc_vocab_loss_work(n, V, d, grad=True)
+    det.vocab_loss(h.cuda(), w.cuda(), t.cuda()[::2], out, work)
+    for gap, at in ((0, 0), (8, 0), (3, 0), (8, 1)):
+        store = [torch.full((r * (d + gap) + at,), 9.0, dtype=BF16, device="cuda") for r in (n, V)]
+        g = dict(zip(("hidden", "weight"), (s[at:].view(r, d + gap)[:, :d] for s, r in zip(store, (n, V)))))
+        det.vocab_loss_grad(h.cuda(), w.cuda(), t.cuda()[::2], out, g, work, grad_mean=torch.ones(1, device="cuda"))
+        check_loss({**out, "hidden_grad": g["hidden"], "weight_grad": g["weight"]}, ref)
+        assert all(bool((s[at:].view(r, d + gap)[:, d:] == 9).all()) and bool((s[:at] == 9).all()) for s, r in zip(store, (n, V)))
+
+
 def test_one_gradient_alone(det):
     n, V, d = 100, 400, 72
     h, w, t = randn((n, d), 1, BF16).cuda(), randn((V, d), 2, BF16, 0.3).cuda(), refs.tokens(n, V, 3).cuda()
@@ -385,6 +422,13 @@ def test_adamw(det, sizes, param, grad, copy, bits, at):
             assert torch.equal(copies[i].cpu(), p.to(copy)), f"tensor {i}: copy"
         for name, r in zip(("m", "v", "m_exp", "v_exp"), ref[1:]):
             assert np.array_equal(x[name][i].cpu().numpy(), r), f"tensor {i}: {name}"
+
+
+def test_adamw_of_nothing(det):
+    det.adamw(det.adamw_table([], [], {"m": [], "v": []}), lr=1e-2, step=1)
+    e = torch.empty(0, device="cuda")
+    det.adamw(det.adamw_table([e], [e], {"m": [e], "v": [e]}), lr=1e-2, step=1)
+    torch.cuda.synchronize()
 
 
 def test_adamw_against_64_bits(det):
