@@ -162,11 +162,11 @@ __device__ __forceinline__ X8 fragment(const uint8_t* s, uint32_t row, uint32_t 
 // ---- the tiled product ---------------------------------------------------------------------
 
 // Tiles in an order in which those that run at the same time share operands: workgroups go to the
-// eight chiplets in turn, each takes a stretch of the tiles, walked in strips of eight tiles of n.
+// eight chiplets in turn, each takes a stretch of the tiles, walked in strips of STRIP tiles of n.
+template <uint32_t STRIP>
 __device__ __forceinline__ void tile_of(uint32_t b, uint32_t tiles_m, uint32_t tiles_n, uint32_t& tm, uint32_t& tn) {
     const uint32_t tiles = tiles_m * tiles_n, chip = b & 7, each = tiles / 8, more = tiles % 8;
     const uint32_t t = chip * each + min(chip, more) + b / 8;
-    constexpr uint32_t STRIP = 8;
     const uint32_t strip = t / (STRIP * tiles_m), in = t - strip * STRIP * tiles_m;
     const uint32_t width = min(STRIP, tiles_n - strip * STRIP);
     tn = strip * STRIP + in % width;
@@ -498,7 +498,8 @@ template <typename T, typename TILE, int EPI>
 __global__ __launch_bounds__(TILE::NT, 512 / TILE::NT) void product_kernel(const product_args p) {
     constexpr int BM = TILE::BM, BN = TILE::BN, WM = TILE::WM, WN = TILE::WN, FM = TILE::FM, FN = TILE::FN;
     uint32_t tm, tn;
-    tile_of(blockIdx.x, p.tiles_m, p.tiles_n, tm, tn);
+    // (strips of four for the weights' gradient: 6 970 against 7 150 us, 8 192 rows x 131 072 x 4 096; of eight otherwise)
+    tile_of<EPI == EPI_OUT ? 4 : 8>(blockIdx.x, p.tiles_m, p.tiles_n, tm, tn);
     uint32_t n = p.n, k = p.k;
     if (EPI == EPI_G || EPI == EPI_SLAB) n = p.head->count;
     if (EPI == EPI_OUT) k = p.head->count;
