@@ -189,8 +189,10 @@ struct small_tile {
     static __device__ __forceinline__ uint32_t row_of(uint32_t wm, int i) { return wm * 64 + i * 16; }
     static __device__ __forceinline__ uint32_t col_of(uint32_t wn, int j) { return wn * 64 + j * 16; }
 
+    template <typename Meanwhile>
     static __device__ __forceinline__ void run(const operand& oa, const operand& ob, uint32_t m0, uint32_t n0, uint32_t kfirst,
-                                               uint32_t blocks, uint32_t ends, f32x4 (&acc)[FM][FN], uint8_t*& spare) {
+                                               uint32_t blocks, uint32_t ends, f32x4 (&acc)[FM][FN], uint8_t*& spare,
+                                               Meanwhile meanwhile) {
         // (one array a buffer, so that the compiler knows which loads a read has to wait for)
         __shared__ __attribute__((aligned(16))) uint8_t sa0[BM * BK * 2], sb0[BN * BK * 2];
         __shared__ __attribute__((aligned(16))) uint8_t sa1[BM * BK * 2], sb1[BN * BK * 2];
@@ -244,6 +246,7 @@ struct small_tile {
         uint32_t kt = blocks & 1;
         auto start = [&](uint8_t* a, uint8_t* b, uint8_t* na, uint8_t* nb) {
             stage(a, b, 0);
+            meanwhile();
             __syncthreads();
             if (ends != 0 && blocks == 1) end_rows(a, b);
             if (blocks > 1) stage(na, nb, 1);
@@ -292,8 +295,10 @@ struct large_tile {
     static constexpr int loads_but(int n) { return 0x0F70 | n; }
     static constexpr int LDS_READ = 0xC07F;
 
+    template <typename Meanwhile>
     static __device__ __forceinline__ void run(const operand& oa, const operand& ob, uint32_t m0, uint32_t n0, uint32_t kfirst,
-                                               uint32_t blocks, uint32_t ends, f32x4 (&acc)[FM][FN], uint8_t*& spare) {
+                                               uint32_t blocks, uint32_t ends, f32x4 (&acc)[FM][FN], uint8_t*& spare,
+                                               Meanwhile meanwhile) {
         __shared__ __attribute__((aligned(16))) uint8_t up0[128 * BK * 2], low0[128 * BK * 2], sb0[BN * BK * 2];
         __shared__ __attribute__((aligned(16))) uint8_t up1[128 * BK * 2], low1[128 * BK * 2], sb1[BN * BK * 2];
         const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
@@ -379,8 +384,10 @@ struct large_tile {
                 lb.stage(nb, kfirst * BK, 1);
                 lu.stage(nup, kfirst * BK, 1);
                 ll.stage(nlow, kfirst * BK, 1);
+                meanwhile();
                 __builtin_amdgcn_s_waitcnt(loads_but(8));
             } else {
+                meanwhile();
                 __builtin_amdgcn_s_waitcnt(loads_but(0));
             }
             turn_over(false, 0);
@@ -410,36 +417,51 @@ __device__ __forceinline__ float2 join_sums(float2 a, float2 b) {
     return make_float2(top, a.y * __builtin_amdgcn_exp2f(a.x - from) + b.y * __builtin_amdgcn_exp2f(b.x - from));
 }
 
-// Column j of a wave's tile over all of its rows (words rows[f] + 0..3), the same in the four lanes that share a
-// column i.  What few tiles need stands behind branches that all lanes take alike: words behind the vocabulary's
-// end, and the target's logit, which is written where it is met.
+// Target i as it is seen from the launch's first word on; -1 where it has none there.
+__device__ __forceinline__ int32_t target_from(const product_args& p, uint32_t i, uint32_t n) {
+    const int64_t t = i < n ? gd_token(p.targets, i) : -1;
+    return t >= (int64_t)p.v0 && t < (int64_t)p.vocab ? (int32_t)(t - p.v0) : -1;
+}
+
+// How many of the launch's words lie below the vocabulary's end from `first` on, the same number each time.  (Comparisons
+// with it stay in the branches that need them.  Worked out once for all columns they fill the scalar registers: a tile of
+// 256 x 256 spent 6.7 us behind its sum, with a wait for each column's targets, where it spends 3.5 now.)
+__device__ __forceinline__ int32_t words_left(const product_args& p, uint32_t first) {
+    int32_t left = (int32_t)(p.vocab - p.v0) - (int32_t)first;
+    asm volatile("" : "+v"(left));
+    return left;
+}
+
+// Column j of a wave's tile, row i, over all of its words (words[f] + 0..3), the same in the four lanes that share the
+// column.  `target` as from target_from.  What few tiles need stands behind branches that all lanes take alike:
+// words behind the vocabulary's end, and the target's logit, which is written where it is met.
 template <int FM, int FN>
-__device__ __forceinline__ float2 tile_sums(const product_args& p, f32x4 (&acc)[FM][FN], int j, const uint32_t (&rows)[FM], uint32_t i,
-                                            uint32_t n, uint32_t lane) {
-    const uint32_t here = p.vocab - p.v0;                        // rows of this launch's words below the vocabulary's end
-    const int64_t t = (i < n ? gd_token(p.targets, i) : -1) - (int64_t)p.v0;
-    const bool met = t >= (int64_t)rows[0] && t < (int64_t)rows[FM - 1] + 4;
-    if (__ballot(met)) {
+__device__ __forceinline__ float2 tile_sums(const product_args& p, f32x4 (&acc)[FM][FN], int j, const uint32_t (&words)[FM], uint32_t i,
+                                            int32_t target, uint32_t lane) {
+    if (__ballot(target >= (int32_t)words[0] && target < (int32_t)words[FM - 1] + 4)) {
+        float logit = 0.0f;
+        bool met = false;
 #pragma unroll
         for (int f = 0; f < FM; ++f)
 #pragma unroll
             for (int r = 0; r < 4; ++r)
-                if (t == (int64_t)(rows[f] + r) && rows[f] + r < here) p.target_logit[i] = acc[f][j][r] * p.scale;
+                if (target - (int32_t)words[0] == (int32_t)(words[f] - words[0]) + r) { logit = acc[f][j][r]; met = true; }
+        if (met) p.target_logit[i] = logit * p.scale;
     }
-    const float scale2 = p.scale2;
-    if (scale2 < 0.0f) {
+    if (p.scale2 < 0.0f) {
 #pragma unroll
         for (int f = 0; f < FM; ++f) acc[f][j] = -acc[f][j];
     }
-    const float up = fabsf(scale2);
+    // (never 0: words that are not there are -inf, and their exponentials 0)
+    const float up = fmaxf(fabsf(p.scale2), 1.1754943508222875e-38f);
     float top = -__builtin_inff();
-    const bool ends = __ballot(rows[FM - 1] + 3 >= here) != 0;
-    if (ends) {
+    if (__ballot((int32_t)(words[FM - 1] - words[0]) + 3 >= words_left(p, words[0]))) {
+        const int32_t left = words_left(p, words[0]);
 #pragma unroll
         for (int f = 0; f < FM; ++f)
 #pragma unroll
             for (int r = 0; r < 4; ++r)
-                if (rows[f] + r >= here) acc[f][j][r] = -__builtin_inff();
+                if ((int32_t)(words[f] - words[0]) + r >= left) acc[f][j][r] = -__builtin_inff();
     }
 #pragma unroll
     for (int f = 0; f < FM; ++f)
@@ -447,51 +469,55 @@ __device__ __forceinline__ float2 tile_sums(const product_args& p, f32x4 (&acc)[
         for (int r = 0; r < 4; ++r) top = fmaxf(top, acc[f][j][r]);
     top = fmaxf(top, __uint_as_float(gd_lane_xor<16>(__float_as_uint(top), lane)));
     top = fmaxf(top, __uint_as_float(gd_lane_xor<32>(__float_as_uint(top), lane)));
-    // (a scale of 0, or nothing below the end: -inf times 0 is no number)
     const float from = top == -__builtin_inff() ? 0.0f : top * up;
     float sum = 0.0f;
 #pragma unroll
     for (int f = 0; f < FM; ++f)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            float e = __builtin_amdgcn_exp2f(fmaf(acc[f][j][r], up, -from));
-            if (ends && rows[f] + r >= here) e = 0.0f;
-            sum += e;
-        }
+        for (int r = 0; r < 4; ++r) sum += __builtin_amdgcn_exp2f(fmaf(acc[f][j][r], up, -from));
     sum += __uint_as_float(gd_lane_xor<16>(__float_as_uint(sum), lane));
     sum += __uint_as_float(gd_lane_xor<32>(__float_as_uint(sum), lane));
     return make_float2(top == -__builtin_inff() ? top : from, sum);
 }
 
 // A row of G: what all its words share.
-struct g_row {
-    float lse2, coef, low;           // lse and 64 less than it in units of log 2; the coefficient; 2^-64 of it
+struct alignas(16) g_row {
+    float lse2, coef, low;           // 64 less than lse in units of log 2; the coefficient; 2^-64 of it
     int32_t target;                  // from the launch's first word on
-    bool met;                        // among the wave's words
-    // Rows without a gradient have a coefficient of 0.
-    __device__ __forceinline__ g_row(const product_args& p, uint32_t i, bool there, uint32_t first, uint32_t last)
-        : lse2(there ? p.row_lse2[i] - 64.0f : 0.0f), coef(there ? p.row_coef[i] : 0.0f), low(coef * 5.421010862427522e-20f),
-          target(there ? p.row_target[i] - (int32_t)p.v0 : -1), met(target >= (int32_t)first && target <= (int32_t)last) {}
 };
+// Rows without a gradient have a coefficient of 0.
+__device__ __forceinline__ g_row g_row_of(const product_args& p, uint32_t i, bool there) {
+    if (!there) return g_row{0.0f, 0.0f, 0.0f, -1};
+    const float coef = p.row_coef[i];
+    return g_row{p.row_lse2[i] - 64.0f, coef, coef * 5.421010862427522e-20f, p.row_target[i] - (int32_t)p.v0};
+}
 
-// G of a row for the words v + 0..3.  The exponential's instruction drops subnormal results: it is taken 2^64 times
-// as large, and the coefficient as much smaller.
-template <typename T>
-__device__ __forceinline__ gd_vec<T, 4> four_of_g(const product_args& p, const f32x4& logits, uint32_t v, const g_row& row, bool rare) {
-    float x[4];
+// Column j of a wave's tile of logits to G.  The exponential's instruction drops subnormal results: it is taken 2^64
+// times as large, and the coefficient as much smaller.
+template <int FM, int FN>
+__device__ __forceinline__ void tile_g(const product_args& p, f32x4 (&acc)[FM][FN], int j, const uint32_t (&words)[FM], const g_row row) {
 #pragma unroll
-    for (int r = 0; r < 4; ++r) x[r] = __builtin_amdgcn_exp2f(fmaf(logits[r], p.scale2, -row.lse2)) * row.low;
-    if (rare) {                                                  // (the same for all lanes)
+    for (int f = 0; f < FM; ++f)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            if ((int32_t)(v + r) == row.target) x[r] -= row.coef;
-            if (v + r >= p.vocab - p.v0) x[r] = 0.0f;
-        }
+        for (int r = 0; r < 4; ++r) acc[f][j][r] = __builtin_amdgcn_exp2f(fmaf(acc[f][j][r], p.scale2, -row.lse2)) * row.low;
+    const int32_t span = (int32_t)(words[FM - 1] - words[0]) + 3, left = words_left(p, words[0]), met = row.target - (int32_t)words[0];
+    if (__ballot((met >= 0 && met <= span) || span >= left)) {       // (all lanes alike)
+#pragma unroll
+        for (int f = 0; f < FM; ++f)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int32_t w = (int32_t)(words[f] - words[0]) + r;
+                acc[f][j][r] -= w == met ? row.coef : 0.0f;
+                if (w >= left) acc[f][j][r] = 0.0f;
+            }
     }
-    gd_vec<T, 4> q;
-#pragma unroll
-    for (int r = 0; r < 4; ++r) q.v[r] = gd_from_f32<T>(x[r]);
-    return q;
+}
+
+// Four numbers to the nearest ones of a type.
+template <typename T>
+__device__ __forceinline__ gd_vec<T, 4> four_of(const f32x4& x) {
+    typedef T x4 __attribute__((ext_vector_type(4)));
+    return __builtin_bit_cast(gd_vec<T, 4>, __builtin_convertvector(x, x4));
 }
 
 template <typename T, typename TILE, int EPI>
@@ -518,9 +544,20 @@ __global__ __launch_bounds__(TILE::NT, 512 / TILE::NT) void product_kernel(const
     for (int i = 0; i < FM; ++i)
 #pragma unroll
         for (int j = 0; j < FN; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    // What the rows of a tile of logits need is loaded before everything else, and lies in the LDS while the sum is taken.
+    typedef typename std::conditional<EPI == EPI_G, g_row, int32_t>::type row_data;
+    __shared__ row_data row_of[EPI == EPI_LSE || EPI == EPI_G ? BN : 1];
+    row_data mine{};
+    if ((EPI == EPI_LSE || EPI == EPI_G) && threadIdx.x < BN) {
+        const uint32_t i = n0 + threadIdx.x;
+        if constexpr (EPI == EPI_G) mine = g_row_of(p, i, i < n);
+        else mine = target_from(p, i, n);
+    }
     // operands that lie along k end where their rows do
     uint8_t* spare;
-    TILE::run(p.a, p.b, m0, n0, kfirst, blocks, EPI == EPI_LSE || EPI == EPI_G ? k % BK : 0, acc, spare);
+    TILE::run(p.a, p.b, m0, n0, kfirst, blocks, EPI == EPI_LSE || EPI == EPI_G ? k % BK : 0, acc, spare, [&] {
+        if ((EPI == EPI_LSE || EPI == EPI_G) && threadIdx.x < BN) row_of[threadIdx.x] = mine;
+    });
 
     // lane l holds rows 4 (l / 16) + 0..3 and column l % 16 of each 16 x 16 block
     uint32_t row[FM], col[FN];
@@ -543,11 +580,11 @@ __global__ __launch_bounds__(TILE::NT, 512 / TILE::NT) void product_kernel(const
             write(c, m0 + TILE::row_of(wm, ch / 2) + (ch & 1) * 8, q);
         }
     };
-    if (EPI == EPI_LSE) {
+    if constexpr (EPI == EPI_LSE) {
         __shared__ float2 join[WM * BN];
 #pragma unroll
         for (int j = 0; j < FN; ++j) {
-            const float2 q = tile_sums<FM, FN>(p, acc, j, row, col[j], n, lane);
+            const float2 q = tile_sums<FM, FN>(p, acc, j, row, col[j], row_of[col[j] - n0], lane);
             if (lane < 16) join[wm * BN + TILE::col_of(wn, j) + lane] = q;
         }
         __syncthreads();
@@ -557,20 +594,19 @@ __global__ __launch_bounds__(TILE::NT, 512 / TILE::NT) void product_kernel(const
             for (int w = 1; w < WM; ++w) q = join_sums(q, join[w * BN + threadIdx.x]);
             p.part[(uint64_t)(n0 + threadIdx.x) * p.parts + p.part0 + tm] = q;
         }
-    } else if (EPI == EPI_G) {
+    } else if constexpr (EPI == EPI_G) {
         T* g = static_cast<T*>(p.c);
 #pragma unroll
         for (int j = 0; j < FN; ++j) {
-            const uint32_t i = col[j];                          // (there is room for whole tiles of rows)
-            const g_row gr(p, i, i < n, row[0], row[FM - 1] + 3);
-            const bool rare = __ballot(gr.met || row[FM - 1] + 3 >= p.vocab - p.v0) != 0;
+            tile_g<FM, FN>(p, acc, j, row, row_of[col[j] - n0]);
 #pragma unroll
-            for (int f = 0; f < FM; ++f) put(f, four_of_g<T>(p, acc[f][j], row[f], gr, rare));
+            for (int f = 0; f < FM; ++f) put(f, four_of<T>(acc[f][j]));
+            // (there is room for whole tiles of rows)
             take([&](uint32_t c, uint32_t m, const gd_vec<T, 8>& q) {
                 *reinterpret_cast<gd_vec<T, 8>*>(g + (uint64_t)(n0 + TILE::col_of(wn, j) + c) * p.ldc + m) = q;
             });
         }
-    } else if (EPI == EPI_SLAB) {
+    } else if constexpr (EPI == EPI_SLAB) {
         float* slab = static_cast<float*>(p.c) + blockIdx.y * p.slab;
 #pragma unroll
         for (int j = 0; j < FN; ++j) {
@@ -591,12 +627,7 @@ __global__ __launch_bounds__(TILE::NT, 512 / TILE::NT) void product_kernel(const
 #pragma unroll
         for (int j = 0; j < FN; ++j) {
 #pragma unroll
-            for (int f = 0; f < FM; ++f) {
-                gd_vec<T, 4> q;
-#pragma unroll
-                for (int r = 0; r < 4; ++r) q.v[r] = gd_from_f32<T>(acc[f][j][r] * back * more);
-                put(f, q);
-            }
+            for (int f = 0; f < FM; ++f) put(f, four_of<T>(acc[f][j] * back * more));
             take([&](uint32_t c, uint32_t m, const gd_vec<T, 8>& q) {
                 const uint32_t i = n0 + TILE::col_of(wn, j) + c;
                 if (i >= p.n) return;
@@ -701,19 +732,17 @@ __global__ __launch_bounds__(256) void few_rows_kernel(const product_args p) {
 #pragma unroll
         for (int j = 0; j < FN; ++j) {
             const uint32_t i = n0 + j * 16 + (lane & 15);
-            const float2 q = tile_sums<FM, FN>(p, acc, j, rows, i, n, lane);
+            const float2 q = tile_sums<FM, FN>(p, acc, j, rows, i, target_from(p, i, n), lane);
             if (lane < 16 && i < n) p.part[(uint64_t)i * p.parts + p.part0 + blockIdx.x] = q;
         }
     } else {
 #pragma unroll
         for (int j = 0; j < FN; ++j) {
             const uint32_t i = n0 + j * 16 + (lane & 15);        // (there is room for whole tiles)
-            const g_row gr(p, i, i < n, rows[0], rows[FM - 1] + 3);
-            const bool rare = __ballot(gr.met || rows[FM - 1] + 3 >= p.vocab - p.v0) != 0;
+            tile_g<FM, FN>(p, acc, j, rows, g_row_of(p, i, i < n));
 #pragma unroll
             for (int f = 0; f < FM; ++f)
-                *reinterpret_cast<gd_vec<T, 4>*>(static_cast<T*>(p.c) + (uint64_t)i * p.ldc + rows[f]) =
-                    four_of_g<T>(p, acc[f][j], rows[f], gr, rare);
+                *reinterpret_cast<gd_vec<T, 4>*>(static_cast<T*>(p.c) + (uint64_t)i * p.ldc + rows[f]) = four_of<T>(acc[f][j]);
         }
         // (the weights' gradient takes the rows in blocks of 64)
 #pragma unroll
