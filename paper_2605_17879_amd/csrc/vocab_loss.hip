@@ -572,14 +572,16 @@ __global__ __launch_bounds__(TILE::NT, 512 / TILE::NT) void product_kernel(const
         const uint32_t c = lane & 15, ch = f * 2 + (lane >> 5);
         *reinterpret_cast<gd_vec<T, 4>*>(spare + c * (CH * 16) + ((ch ^ (c & (CH - 1))) * 16) + ((lane >> 4) & 1) * 8) = q;
     };
-    auto take = [&](auto write) {
+    auto take = [&](auto wide, auto write) {                     // `wide`: elements a lane, 8 or fewer
+        constexpr uint32_t V = decltype(wide)::value, LANES = FM * 16 / V;
 #pragma unroll
-        for (uint32_t it = 0; it < CH / 4; ++it) {
-            const uint32_t c = it * (64 / CH) + lane / CH, ch = lane % CH;
-            const gd_vec<T, 8> q = *reinterpret_cast<const gd_vec<T, 8>*>(spare + c * (CH * 16) + ((ch ^ (c & (CH - 1))) * 16));
-            write(c, m0 + TILE::row_of(wm, ch / 2) + (ch & 1) * 8, q);
+        for (uint32_t it = 0; it < 16 * LANES / 64; ++it) {
+            const uint32_t at = it * 64 + lane, c = at / LANES, e = at % LANES * V, ch = e / 8;
+            const uint8_t* from = spare + c * (CH * 16) + ((ch ^ (c & (CH - 1))) * 16) + e % 8 * 2;
+            write(c, m0 + TILE::row_of(wm, e / 16) + e % 16, *reinterpret_cast<const gd_vec<T, V>*>(from));
         }
     };
+    typedef std::integral_constant<uint32_t, 8> eight;
     if constexpr (EPI == EPI_LSE) {
         __shared__ float2 join[WM * BN];
 #pragma unroll
@@ -602,7 +604,7 @@ __global__ __launch_bounds__(TILE::NT, 512 / TILE::NT) void product_kernel(const
 #pragma unroll
             for (int f = 0; f < FM; ++f) put(f, four_of<T>(acc[f][j]));
             // (there is room for whole tiles of rows)
-            take([&](uint32_t c, uint32_t m, const gd_vec<T, 8>& q) {
+            take(eight(), [&](uint32_t c, uint32_t m, const gd_vec<T, 8>& q) {
                 *reinterpret_cast<gd_vec<T, 8>*>(g + (uint64_t)(n0 + TILE::col_of(wn, j) + c) * p.ldc + m) = q;
             });
         }
@@ -623,24 +625,30 @@ __global__ __launch_bounds__(TILE::NT, 512 / TILE::NT) void product_kernel(const
     } else {
         T* out = static_cast<T*>(p.c);
         const float back = p.head->back, more = p.head->more * p.scale;
-        const bool whole = (p.ldc & 7) == 0 && ((uintptr_t)out & 15) == 0;
+        auto rows_of = [&](auto wide) {
+            constexpr uint32_t V = decltype(wide)::value;
 #pragma unroll
-        for (int j = 0; j < FN; ++j) {
+            for (int j = 0; j < FN; ++j) {
 #pragma unroll
-            for (int f = 0; f < FM; ++f) put(f, four_of<T>(acc[f][j] * back * more));
-            take([&](uint32_t c, uint32_t m, const gd_vec<T, 8>& q) {
-                const uint32_t i = n0 + TILE::col_of(wn, j) + c;
-                if (i >= p.n) return;
-                T* to = out + (uint64_t)i * p.ldc + m;
-                if (whole && m + 8 <= p.m) {
-                    gd_write_through(to, q);
-                } else {
+                for (int f = 0; f < FM; ++f) put(f, four_of<T>(acc[f][j] * back * more));
+                take(wide, [&](uint32_t c, uint32_t m, const gd_vec<T, V>& q) {
+                    const uint32_t i = n0 + TILE::col_of(wn, j) + c;
+                    if (i >= p.n) return;
+                    T* to = out + (uint64_t)i * p.ldc + m;
+                    if (m + V <= p.m) {
+                        gd_write_through(to, q);
+                    } else {
 #pragma unroll
-                    for (uint32_t r = 0; r < 8; ++r)
-                        if (m + r < p.m) to[r] = q.v[r];
-                }
-            });
-        }
+                        for (uint32_t r = 0; r < V; ++r)
+                            if (m + r < p.m) to[r] = q.v[r];
+                    }
+                });
+            }
+        };
+        // (what every row is aligned to; lanes side by side write what lies side by side)
+        if ((p.ldc & 7) == 0 && ((uintptr_t)out & 15) == 0) rows_of(eight());
+        else if ((p.ldc & 1) == 0 && ((uintptr_t)out & 3) == 0) rows_of(std::integral_constant<uint32_t, 2>());
+        else rows_of(std::integral_constant<uint32_t, 1>());
     }
 }
 
@@ -1102,7 +1110,7 @@ struct loss_layout {
 loss_layout layout_of(uint64_t n, uint64_t vocab, uint64_t width, bool with_grad) {
     loss_layout l;
     l.padded_rows = up_to(n, 256);
-    l.ldh = up_to(width, 8);
+    l.ldh = up_to(width, 64);                                   // (copies have rows of whole lines)
     const uint64_t all = up_to(vocab, 256);
     l.pack_piece = PACK / l.ldh / 256 * 256;
     if (l.pack_piece < 256) l.pack_piece = 256;
@@ -1300,7 +1308,7 @@ hipError_t backward(const gd_vocab_grad_args& a, hipStream_t s) {
         p.head = head;
         p.a = wo;
         p.b = operand{hidden, ldh, padded, ldh};
-        p.m = here; p.n = n; p.k = ldh;
+        p.m = here; p.n = n; p.k = (uint32_t)up_to(a.width, 8);
         p.scale2 = a.scale * LOG2E; p.v0 = v0; p.vocab = a.vocab;
         p.row_lse2 = r.row_lse2; p.row_coef = r.row_coef; p.row_target = r.row_target;
         p.c = g; p.ldc = piece;
