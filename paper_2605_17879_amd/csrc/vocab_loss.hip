@@ -1239,6 +1239,7 @@ hipError_t forward(const gd_vocab_loss_args& a, hipStream_t s) {
         p.b = operand{hidden, ldh, n, ldh};
     }
     const bool plain = direct(a.weight, a.weight_stride, a.width);
+    p.k = (uint32_t)up_to(a.width, 8);                           // (rows of a copy go on with zeros)
     p.n = n; p.scale = a.scale; p.scale2 = a.scale * LOG2E; p.vocab = a.vocab; p.targets = a.targets;
     p.target_logit = reinterpret_cast<float*>(a.work + l.target_logit);
     p.part = reinterpret_cast<float2*>(a.work + l.part);
@@ -1258,7 +1259,6 @@ hipError_t forward(const gd_vocab_loss_args& a, hipStream_t s) {
                                (const grad_head*)nullptr, (const uint32_t*)nullptr, here, weight, ldh);
             p.a = operand{weight, ldh, here, ldh};
         }
-        p.k = p.a.cols < p.b.cols ? p.b.cols : p.a.cols;
         p.m = here; p.v0 = v0; p.part0 = parts;
         parts += launch_logits<T, EPI_LSE>(p, few, s);
     }

@@ -305,6 +305,20 @@ def test_logit_scales_below_one(det, scale, n, vocab, width):
     check_loss(run_loss(det, h, w, t, 0, scale, grad_mean=1.0), ref)
 
 
+@pytest.mark.parametrize("n,vocab,gap", [(9, 300, (5, 0)), (300, 5001, (5, 0)), (2100, 9001, (5, 0)), (9, 300, (0, 5)), (300, 5001, (0, 5))])
+def test_words_that_are_switched_off(det, n, vocab, gap):
+    """A word whose logit is minus infinity, by the last element of its weights, counts for nothing; hidden states or
+    weights alone are copied, and the copy's rows go on where the others end."""
+    d = 72
+    h, w, t = randn((n, d), 1, BF16), randn((vocab, d), 2, BF16, 0.3), refs.tokens(n, vocab - 1, 3)
+    h[:, -1] = 1.0
+    w[-1, -1] = float("-inf")
+    ref = refs.Loss(h, w[:-1], t)
+    out = det.alloc_vocab_loss(n)
+    det.vocab_loss(spaced(h, gap[0]), spaced(w, gap[1]), t.cuda(), out, poison(det.alloc_vocab_loss_work(n, vocab, d)))
+    check_loss(out, ref, grad=False)
+
+
 def test_strided_targets_and_gradients(det):
     n, V, d = 150, 700, 72
     h, w = randn((n, d), 1, BF16), randn((V, d), 2, BF16, 0.3)
