@@ -41,8 +41,9 @@ constexpr size_t HEAD = 64;
 
 __host__ __device__ inline size_t chunks_at(uint32_t n_tensors) { return HEAD + (size_t)n_tensors * sizeof(table_tensor); }
 
-// The table's pointers are to device memory; said to the compiler, which otherwise asks the LDS as well at every access.  With 8-bit states what is read and written is marked as passing through once (1 910 -> 1 874 us for
-// 540 M elements); with 32-bit ones it is not (1 109 against 1 185 us for 200 M).
+// The table's pointers are to device memory; said to the compiler, which otherwise asks the LDS as well at every access.
+// With 8-bit states what is read and written is marked as passing through once (1 910 -> 1 874 us for 540 M elements);
+// with 32-bit ones it is not (1 109 against 1 185 us for 200 M).
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 template <typename X>

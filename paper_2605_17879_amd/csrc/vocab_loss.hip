@@ -508,14 +508,16 @@ __device__ __forceinline__ void tile_g(const product_args& p, f32x4 (&acc)[FM][F
 #pragma unroll
         for (int r = 0; r < 4; ++r) acc[f][j][r] = __builtin_amdgcn_exp2f(fmaf(acc[f][j][r], p.scale2, -row.lse2)) * row.low;
     const int32_t span = (int32_t)(words[FM - 1] - words[0]) + 3, left = words_left(p, words[0]), met = row.target - (int32_t)words[0];
-    if (__ballot((met >= 0 && met <= span) || span >= left)) {       // (all lanes alike)
+    // (a row without a gradient is zeros, also against a word of infinities)
+    const bool none = row.coef == 0.0f;
+    if (__ballot((met >= 0 && met <= span) || span >= left || none)) {       // (all lanes alike)
 #pragma unroll
         for (int f = 0; f < FM; ++f)
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
                 const int32_t w = (int32_t)(words[f] - words[0]) + r;
                 acc[f][j][r] -= w == met ? row.coef : 0.0f;
-                if (w >= left) acc[f][j][r] = 0.0f;
+                if (w >= left || none) acc[f][j][r] = 0.0f;
             }
     }
 }

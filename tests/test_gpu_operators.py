@@ -319,6 +319,23 @@ def test_words_that_are_switched_off(det, n, vocab, gap):
     check_loss(out, ref, grad=False)
 
 
+@pytest.mark.parametrize("n,vocab", [(9, 300), (100, 3001), (300, 5001), (2100, 9001)])
+def test_weights_gradient_with_words_that_are_switched_off(det, n, vocab):
+    """A word whose logit is minus infinity has a gradient of zeros, whatever the number of rows (those that fill the last
+    tile are not there); the other words' is the one without it."""
+    d = 72
+    h, w, t = randn((n, d), 1, BF16), randn((vocab, d), 2, BF16, 0.3), refs.tokens(n, vocab - 1, 3, padding=0.1)
+    h[:, -1] = 1.0
+    w[-1, -1] = float("-inf")
+    ref = refs.Loss(h, w[:-1], t, grad_mean=1.0)
+    out, work = det.alloc_vocab_loss(n), poison(det.alloc_vocab_loss_work(n, vocab, d, grad=True))
+    g = {"weight": poison(torch.empty((vocab, d), dtype=BF16, device="cuda"))}
+    det.vocab_loss(h.cuda(), w.cuda(), t.cuda(), out, work)
+    det.vocab_loss_grad(h.cuda(), w.cuda(), t.cuda(), out, g, work, grad_mean=torch.ones(1, device="cuda"))
+    within(g["weight"][:-1], ref.weight_grad, ref.weight_grad_bound, "gradient of the weights")
+    assert bool((g["weight"][-1] == 0).all())
+
+
 def test_strided_targets_and_gradients(det):
     n, V, d = 150, 700, 72
     h, w = randn((n, d), 1, BF16), randn((V, d), 2, BF16, 0.3)
