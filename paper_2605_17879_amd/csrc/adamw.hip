@@ -394,7 +394,7 @@ size_t gd_adamw_table(const gd_adamw_tensor* t, uint32_t n, void* out) {
 
 hipError_t gd_launch_adamw(const gd_adamw_args& a, hipStream_t s) {
     const uint64_t most = (a.table_bytes - HEAD) / sizeof(table_chunk);
-    const uint32_t grid = (uint32_t)(most < 2048 ? most : 2048);
+    const uint32_t grid = (uint32_t)(most < (1u << 20) ? most : (1u << 20));
     hipLaunchKernelGGL(adamw_kernel, dim3(grid), dim3(NT), 0, s, a);
     return hipGetLastError();
 }

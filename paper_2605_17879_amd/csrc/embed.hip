@@ -10,6 +10,9 @@
 // partial sums (one at the front and one at the back of each stretch), which a second kernel adds up in
 // order: however often a token occurs, the work stays even.
 //
+// Short lists cost launches, not work: up to FEW rows each row's workgroup looks for its token in the whole list and,
+// if the row is the token's first, sums them all, in one launch.
+//
 // The gradient's zeros are written by workgroups of the sorting launches that have no keys: sorting is
 // a chain of short launches that leaves the memory idle.
 #include "gd_operators.h"
@@ -20,11 +23,48 @@ constexpr uint32_t NT = 256;
 constexpr uint32_t BITS = 9, DIGITS = 1u << BITS;   // of a sorting pass: two passes up to 262 143 rows
 constexpr uint32_t SORT_KEYS = 1024;      // keys of a workgroup in a sorting pass
 constexpr uint32_t ONE_SORT = 4096;       // most keys that one workgroup sorts by itself
-constexpr uint32_t SELF_SCAN = 64;        // most workgroups of a pass that add up the counts before them themselves
+// Workgroups of a sorting pass (us for two passes of n rows x 1 000, all launches): up to SELF_COUNT each counts all keys itself (5 000
+// rows 30.3 against 36.9, 16 384 47.2 against 44.9), up to SELF_SCAN each adds up the counts of a first launch, else a third one does.
+constexpr uint32_t SELF_COUNT = 8, SELF_SCAN = 64;
+// Most rows whose tokens are compared with each other instead of sorted, and most workgroups that this may take (us for rows
+// of 1 000 bf16 added, few / sorted: 1 100 rows 9.4 / 17.2, 2 000 13.4 / 18.0; of 4 096 fp32, 8 workgroups a row: 1 100 21.8 / 20.7,
+// 2 000 33.9 / 26.6).
+constexpr uint32_t FEW = 2048, FEW_GROUPS = 8192;
 constexpr uint32_t BATCH = 8;             // rows on their way at once in the sums
+constexpr uint32_t FILL_ROWS = 16384;     // most rows that one of its workgroups fills with zeros
 constexpr uint32_t NO_ROW = 0xFFFFFFFFu;
 
 // ---- lookup ------------------------------------------------------------------------------------
+
+// A lane's V columns from c on.  The last lane of a row that is no multiple of V long reads (and sums) the row's last V
+// columns, `skip` of which are its neighbour's, and writes the others.  Rows have V columns at least.
+struct columns {
+    uint32_t at, skip;
+};
+template <int V>
+__device__ __forceinline__ columns columns_of(uint32_t c, uint32_t width) {
+    const uint32_t at = min(c, width - V);
+    return columns{at, c - at};
+}
+template <typename T, int V>
+__device__ __forceinline__ void write_own(T* p, const gd_vec<T, V>& q, uint32_t skip) {
+    if (skip == 0) {
+        gd_write_through(p, q);
+    } else if constexpr (sizeof(q) == 16) {                   // (in pieces of 8, 4 and 2 bytes, from a copy moved down)
+        const auto w = __builtin_bit_cast(uint4, q);
+        const uint64_t lo = (uint64_t)w.y << 32 | w.x, hi = (uint64_t)w.w << 32 | w.z;
+        const uint32_t bits = skip * sizeof(T) * 8, left = 16 - skip * (uint32_t)sizeof(T);
+        uint64_t rest = bits < 64 ? lo >> bits | hi << (64 - bits) : hi >> (bits - 64);
+        uint8_t* to = reinterpret_cast<uint8_t*>(p + skip);
+        if (left & 8) { __builtin_memcpy(to, &rest, 8); to += 8; rest = hi >> (bits & 63); }
+        if (left & 4) { const uint32_t x = (uint32_t)rest; __builtin_memcpy(to, &x, 4); to += 4; rest >>= 32; }
+        if (left & 2) { const uint16_t x = (uint16_t)rest; __builtin_memcpy(to, &x, 2); }
+    } else {
+#pragma unroll
+        for (uint32_t j = 1; j < V; ++j)
+            if (j >= skip) p[j] = q.v[j];
+    }
+}
 
 // tx lanes side by side on a row, NT / tx rows a workgroup; V elements a lane at a time.
 template <typename T, int V>
@@ -37,12 +77,13 @@ __global__ __launch_bounds__(NT) void embed_kernel(const gd_embed_args a, uint32
     const bool row = t >= 0 && t < (int64_t)a.vocab;
     const T* w = static_cast<const T*>(a.weight) + (row ? (uint64_t)t : 0) * a.weight_stride;
     const float other = t < 0 ? 0.0f : __uint_as_float(0x7FC00000u);
-    for (uint32_t c = (blockIdx.y * tx + lane) * V; c < a.width; c += gridDim.y * tx * V) {
+    for (uint32_t c0 = (blockIdx.y * tx + lane) * V; c0 < a.width; c0 += gridDim.y * tx * V) {
+        const columns c = columns_of<V>(c0, a.width);
         gd_vec<T, V> q;
-        if (row) q = *reinterpret_cast<const gd_vec<T, V>*>(w + c);
+        if (row) q = gd_read<T, V>(w + c.at);
 #pragma unroll
         for (int j = 0; j < V; ++j) q.v[j] = gd_from_f32<T>(row ? gd_to_f32(q.v[j]) * a.scale : other);
-        gd_write_through(out + c, q);
+        write_own<T, V>(out + c.at, q, c.skip);
     }
 }
 
@@ -53,14 +94,6 @@ hipError_t launch_embed(const gd_embed_args& a, hipStream_t s) {
     const uint32_t rows = NT >> log_tx;
     hipLaunchKernelGGL((embed_kernel<T, V>), dim3((a.tokens.n + rows - 1) / rows), dim3(NT), 0, s, a, log_tx);
     return hipGetLastError();
-}
-
-// The most elements (a power of two, 16 bytes at most) that every row of both matrices can be read
-// and written by at once.
-uint32_t vector_of(const void* p, uint64_t ps, const void* q, uint64_t qs, uint64_t width, uint32_t size) {
-    uint32_t v = 16 / size;
-    while (v > 1 && ((uintptr_t)p % (v * size) || (uintptr_t)q % (v * size) || ps % v || qs % v || width % v)) v /= 2;
-    return v;
 }
 
 // ---- the stable sort by token ---------------------------------------------------------------
@@ -80,9 +113,20 @@ struct fill_args {
 };
 
 // Tokens to keys: those without a row get the largest one and sort behind all others.
-__device__ __forceinline__ uint32_t key_of(const gd_token_list& l, uint32_t i, uint32_t vocab) {
-    const int64_t t = gd_token(l, i);
-    return t >= 0 && t < (int64_t)vocab ? (uint32_t)t : vocab;
+__device__ __forceinline__ uint32_t key_of(int64_t t, uint32_t vocab) { return t >= 0 && t < (int64_t)vocab ? (uint32_t)t : vocab; }
+
+// The keys of positions from, from + step, ...; those behind the list's end are the last one's.
+template <int N>
+__device__ __forceinline__ void keys_of(const sort_args& a, uint32_t from, uint32_t step, uint32_t (&k)[N]) {
+    if (a.shift) {
+#pragma unroll
+        for (int b = 0; b < N; ++b) k[b] = a.key[a.from][min(from + b * step, a.n - 1)];
+    } else {
+        int64_t t[N];
+        gd_tokens<N>(a.tokens, from, step, t);
+#pragma unroll
+        for (int b = 0; b < N; ++b) k[b] = key_of(t[b], a.vocab);
+    }
 }
 
 // For each lane: which lanes of the wave hold the same digit (among those with a key).
@@ -96,23 +140,34 @@ __device__ __forceinline__ uint64_t same_digit(uint32_t d, bool there) {
     return same;
 }
 
-// Workgroup `block` of `blocks` fills its share.
+// Workgroup `block` of `blocks` fills its share: of rows next to each other 16 bytes a lane and no more (512 MB: 79 us; 16 bytes
+// again and again by 2 048 workgroups 112 us), of rows apart every blocks-th row.
 template <typename T, int V, int THREADS>
 __device__ __forceinline__ void fill_rows(const fill_args& f, uint32_t block, uint32_t blocks) {
-    gd_vec<T, V> zero;
+    if (f.stride == f.width) {
+        T* const begin = static_cast<T*>(f.p) + (uint64_t)f.from * f.width;
+        T* const end = static_cast<T*>(f.p) + (uint64_t)f.to * f.width;
+        typedef gd_vec<T, 16 / sizeof(T)> line;
+        T* const p = reinterpret_cast<T*>(((uintptr_t)begin & ~(uintptr_t)15) + ((uint64_t)block * THREADS + threadIdx.x) * 16);
+        if (p >= begin && p + 16 / sizeof(T) <= end) {
+            gd_write_through(p, line{});
+        } else {
 #pragma unroll
-    for (int j = 0; j < V; ++j) zero.v[j] = gd_from_f32<T>(0.0f);
-    if (f.stride == f.width) {                                // one stretch of memory
-        T* p = static_cast<T*>(f.p);
-        const uint64_t end = (uint64_t)f.to * f.width;
-        for (uint64_t i = (uint64_t)f.from * f.width + ((uint64_t)block * THREADS + threadIdx.x) * V; i < end;
-             i += (uint64_t)blocks * THREADS * V)
-            gd_write_through(p + i, zero);
+            for (uint32_t j = 0; j < 16 / sizeof(T); ++j)
+                if (p + j >= begin && p + j < end) p[j] = gd_from_f32<T>(0.0f);
+        }
     } else {
         for (uint32_t r = f.from + block; r < f.to; r += blocks)
             for (uint32_t c = threadIdx.x * V; c < f.width; c += THREADS * V)
-                gd_write_through(static_cast<T*>(f.p) + (uint64_t)r * f.stride + c, zero);
+                gd_write_through(static_cast<T*>(f.p) + (uint64_t)r * f.stride + columns_of<V>(c, f.width).at, gd_vec<T, V>{});
     }
+}
+template <typename T, int THREADS>
+uint32_t fillers(const fill_args& f) {
+    if (f.from == f.to) return 0;
+    if (f.stride != f.width) return f.to - f.from < 8192 ? f.to - f.from : 8192;
+    // (one more where the first line begins before the first row)
+    return (uint32_t)(((uint64_t)(f.to - f.from) * f.width * sizeof(T) + 14) / 16 / THREADS + 1);
 }
 
 // All passes by one workgroup of sixteen waves, the keys in its registers and, between passes, in the LDS.
@@ -130,11 +185,9 @@ __global__ __launch_bounds__(1024) void sort_alone(sort_args a, fill_args f) {
     uint32_t key[ROUNDS], pos[ROUNDS];
     // (rounds that there are not have no keys: every lane is behind the end)
     const auto there = [&](uint32_t r) { return r < rounds && base + r * 64 + lane < a.n; };
+    keys_of<ROUNDS>(a, base + lane, 64, key);
 #pragma unroll
-    for (uint32_t r = 0; r < ROUNDS; ++r) {
-        pos[r] = base + r * 64 + lane;
-        key[r] = there(r) ? key_of(a.tokens, pos[r], a.vocab) : 0;
-    }
+    for (uint32_t r = 0; r < ROUNDS; ++r) pos[r] = base + r * 64 + lane;
     for (uint32_t shift = 0; shift == 0 || (a.vocab >> shift) > 0; shift += BITS) {
         for (uint32_t i = threadIdx.x; i < WAVES * DIGITS; i += 1024) (&next[0][0])[i] = 0;
         __syncthreads();
@@ -198,20 +251,86 @@ __global__ __launch_bounds__(1024) void sort_alone(sort_args a, fill_args f) {
     }
 }
 
+// A whole pass in one launch where there are few blocks: each workgroup of sixteen waves counts all keys itself, those
+// before its own apart.
+template <typename T, int V>
+__global__ __launch_bounds__(1024) void sort_pass(sort_args a, fill_args f) {
+    if (blockIdx.x >= a.blocks) return fill_rows<T, V, 1024>(f, blockIdx.x - a.blocks, gridDim.x - a.blocks);
+    constexpr uint32_t WAVES = 16, ASK = 8;
+    __shared__ uint32_t count[2][DIGITS];                     // of the keys in blocks before this one; of the others
+    __shared__ uint32_t next[WAVES][DIGITS];
+    __shared__ uint32_t part[DIGITS / 64];
+    static_assert(SORT_KEYS == 1024, "a key a lane");
+    const uint32_t wave = threadIdx.x / 64, lane = threadIdx.x & 63, mine = blockIdx.x * SORT_KEYS + threadIdx.x;
+    const auto digit = [&](uint32_t k) { return (k >> a.shift) & (DIGITS - 1); };
+    (&count[0][0])[threadIdx.x] = 0;
+    for (uint32_t i = threadIdx.x; i < WAVES * DIGITS; i += 1024) (&next[0][0])[i] = 0;
+    const bool there = mine < a.n;
+    uint32_t own[1];
+    keys_of<1>(a, mine, 0, own);
+    const uint32_t key = own[0], pos = there && a.shift ? a.pos[a.from][mine] : mine;
+    __syncthreads();
+    for (uint32_t b0 = 0; b0 < a.blocks; b0 += ASK) {
+        uint32_t k[ASK];
+        keys_of<ASK>(a, b0 * SORT_KEYS + threadIdx.x, SORT_KEYS, k);
+#pragma unroll
+        for (uint32_t b = 0; b < ASK; ++b) {
+            const bool in = (b0 + b) * SORT_KEYS + threadIdx.x < a.n;
+            const uint32_t d = digit(k[b]);
+            const uint64_t who = __ballot(in);
+            if (who == 0) continue;
+            uint32_t* to = count[b0 + b < blockIdx.x ? 0 : 1];
+            // (a frequent token's keys come in runs from the second pass on: one addition for a wave of them)
+            if (__ballot(in && d == (uint32_t)__builtin_amdgcn_readfirstlane(d)) == who) {
+                if (lane == 0) atomicAdd(&to[d], (uint32_t)__popcll(who));
+            } else if (in) {
+                atomicAdd(&to[d], 1u);
+            }
+        }
+    }
+    const uint64_t same = same_digit(digit(key), there);
+    const uint32_t before = (uint32_t)__popcll(same & ((1ull << lane) - 1));
+    if (there && before == 0) next[wave][digit(key)] = (uint32_t)__popcll(same);
+    __syncthreads();
+    // places of each digit's keys, then of each wave's
+    uint32_t total = 0, sum = 0;
+    if (threadIdx.x < DIGITS) {
+        total = sum = count[0][threadIdx.x] + count[1][threadIdx.x];
+#pragma unroll
+        for (uint32_t d = 1; d < 64; d <<= 1) {
+            const uint32_t v = __shfl_up(sum, d);
+            if (lane >= d) sum += v;
+        }
+        if (lane == 63) part[wave] = sum;
+    }
+    __syncthreads();
+    if (threadIdx.x < DIGITS) {
+        uint32_t at = sum - total + count[0][threadIdx.x], c[WAVES];
+        for (uint32_t w = 0; w < wave; ++w) at += part[w];
+#pragma unroll
+        for (uint32_t w = 0; w < WAVES; ++w) c[w] = next[w][threadIdx.x];
+#pragma unroll
+        for (uint32_t w = 0; w < WAVES; ++w) { next[w][threadIdx.x] = at; at += c[w]; }
+    }
+    __syncthreads();
+    if (there) {
+        const uint32_t to = next[wave][digit(key)] + before;
+        a.key[a.from ^ 1][to] = key;
+        a.pos[a.from ^ 1][to] = pos;
+    }
+}
+
 template <typename T, int V>
 __global__ __launch_bounds__(NT) void sort_count(sort_args a, fill_args f) {
     if (blockIdx.x >= a.blocks) return fill_rows<T, V, NT>(f, blockIdx.x - a.blocks, gridDim.x - a.blocks);
     __shared__ uint32_t h[DIGITS];
     for (uint32_t d = threadIdx.x; d < DIGITS; d += NT) h[d] = 0;
     __syncthreads();
+    uint32_t key[SORT_KEYS / NT];
+    keys_of<SORT_KEYS / NT>(a, blockIdx.x * SORT_KEYS + threadIdx.x, NT, key);
 #pragma unroll
-    for (uint32_t r = 0; r < SORT_KEYS / NT; ++r) {
-        const uint32_t i = blockIdx.x * SORT_KEYS + r * NT + threadIdx.x;
-        if (i < a.n) {
-            const uint32_t key = a.shift ? a.key[a.from][i] : key_of(a.tokens, i, a.vocab);
-            atomicAdd(&h[(key >> a.shift) & (DIGITS - 1)], 1u);
-        }
-    }
+    for (uint32_t r = 0; r < SORT_KEYS / NT; ++r)
+        if (blockIdx.x * SORT_KEYS + r * NT + threadIdx.x < a.n) atomicAdd(&h[(key[r] >> a.shift) & (DIGITS - 1)], 1u);
     __syncthreads();
     for (uint32_t d = threadIdx.x; d < DIGITS; d += NT) a.hist[(uint64_t)blockIdx.x * DIGITS + d] = h[d];
 }
@@ -250,11 +369,11 @@ __global__ __launch_bounds__(NT) void sort_scatter(sort_args a, fill_args f) {
     for (uint32_t i = threadIdx.x; i < WAVES * DIGITS; i += NT) (&next[0][0])[i] = 0;
     __syncthreads();
     uint32_t key[ROUNDS], pos[ROUNDS], before[ROUNDS];
+    keys_of<ROUNDS>(a, base + lane, 64, key);
 #pragma unroll
     for (uint32_t r = 0; r < ROUNDS; ++r) {
         const uint32_t i = base + r * 64 + lane;
-        key[r] = i < a.n ? (a.shift ? a.key[a.from][i] : key_of(a.tokens, i, a.vocab)) : 0;
-        pos[r] = i < a.n && a.shift ? a.pos[a.from][i] : i;
+        pos[r] = a.shift ? a.pos[a.from][min(i, a.n - 1)] : i;
     }
 #pragma unroll
     for (uint32_t r = 0; r < ROUNDS; ++r) {
@@ -329,16 +448,16 @@ __global__ __launch_bounds__(NT) void fill_kernel(fill_args f) { fill_rows<T, V,
 
 // A token's row of the gradient from its sum and, where that is added to, its old values.
 template <typename T, int V>
-__device__ __forceinline__ void write_sum(const gd_embed_grad_args& a, uint32_t token, uint32_t c, const float sum[V], bool add,
+__device__ __forceinline__ void write_sum(const gd_embed_grad_args& a, uint32_t token, columns c, const float sum[V], bool add,
                                           const gd_vec<T, V>& old) {
     gd_vec<T, V> q;
 #pragma unroll
     for (int j = 0; j < V; ++j) q.v[j] = gd_from_f32<T>(add ? gd_to_f32(old.v[j]) + a.scale * sum[j] : a.scale * sum[j]);
-    gd_write_through(static_cast<T*>(a.weight_grad) + (uint64_t)token * a.weight_grad_stride + c, q);
+    write_own<T, V>(static_cast<T*>(a.weight_grad) + (uint64_t)token * a.weight_grad_stride + c.at, q, c.skip);
 }
 template <typename T, int V>
-__device__ __forceinline__ gd_vec<T, V> old_row(const gd_embed_grad_args& a, uint32_t token, uint32_t c) {
-    return *reinterpret_cast<const gd_vec<T, V>*>(static_cast<const T*>(a.weight_grad) + (uint64_t)token * a.weight_grad_stride + c);
+__device__ __forceinline__ gd_vec<T, V> old_row(const gd_embed_grad_args& a, uint32_t token, columns c) {
+    return gd_read<T, V>(static_cast<const T*>(a.weight_grad) + (uint64_t)token * a.weight_grad_stride + c.at);
 }
 
 // Stretch blockIdx.x of `span` entries, columns by blockIdx.y.  partial: [stretch][2][width], the sums of
@@ -348,12 +467,13 @@ __device__ __forceinline__ gd_vec<T, V> old_row(const gd_embed_grad_args& a, uin
 template <typename T, int V, bool ADD>
 __global__ __launch_bounds__(NT) void grad_sum(gd_embed_grad_args a, const uint32_t* __restrict__ key, const uint32_t* __restrict__ pos,
                                                float* partial, uint32_t n, uint32_t span) {
-    const uint32_t c = (blockIdx.y * NT + threadIdx.x) * V;
+    const uint32_t c0 = (blockIdx.y * NT + threadIdx.x) * V;
     const uint32_t from = blockIdx.x * span, to = min(from + span, n);
     const uint32_t begin = key[from];
-    if (begin == a.vocab || c >= a.width) return;             // tokens without a row stand at the end
+    if (begin == a.vocab || c0 >= a.width) return;            // tokens without a row stand at the end
+    const columns c = columns_of<V>(c0, a.width);
     const uint32_t before = from ? key[from - 1] : NO_ROW, behind = to < n ? key[to] : NO_ROW;
-    const T* rows = static_cast<const T*>(a.out_grad) + c;
+    const T* rows = static_cast<const T*>(a.out_grad) + c.at;
     float sum[V];
 #pragma unroll
     for (int j = 0; j < V; ++j) sum[j] = 0.0f;
@@ -366,17 +486,17 @@ __global__ __launch_bounds__(NT) void grad_sum(gd_embed_grad_args a, const uint3
             k[b] = i < to ? key[i] : a.vocab;
             // (one without a row: the stretch's first row once more)
             const bool row = k[b] != a.vocab;
-            q[b] = *reinterpret_cast<const gd_vec<T, V>*>(rows + (uint64_t)pos[row ? i : from] * a.out_grad_stride);
-            if constexpr (ADD)
-                if (row && k[b] != before && k[b] != behind) old[b] = old_row<T, V>(a, k[b], c);
+            q[b] = gd_read<T, V>(rows + (uint64_t)pos[row ? i : from] * a.out_grad_stride);
+            // (asked for without a condition, behind which it would be waited for)
+            if constexpr (ADD) old[b] = old_row<T, V>(a, row ? k[b] : begin, c);
         }
     };
     // The token's rows here are summed up.
     auto finish = [&]() {
         if (token == before || token == behind) {            // (the stretch's first one, or its last)
-            float* p = partial + ((uint64_t)blockIdx.x * 2 + (token == before ? 0 : 1)) * a.width + c;
-#pragma unroll
-            for (int j = 0; j < V; ++j) p[j] = sum[j];
+            // (the last two lanes of a row write the same sums where they overlap)
+            float* p = partial + ((uint64_t)blockIdx.x * 2 + (token == before ? 0 : 1)) * a.width + c.at;
+            __builtin_memcpy(p, sum, sizeof(sum));
         } else {
             write_sum<T, V>(a, token, c, sum, ADD, held);
         }
@@ -410,7 +530,7 @@ __global__ __launch_bounds__(NT) void grad_sum(gd_embed_grad_args a, const uint3
 template <typename T, int V>
 __global__ __launch_bounds__(NT) void grad_join(gd_embed_grad_args a, const uint32_t* __restrict__ key, const float* __restrict__ partial,
                                                 uint32_t n, uint32_t span) {
-    const uint32_t c = (blockIdx.y * NT + threadIdx.x) * V;
+    const uint32_t c0 = (blockIdx.y * NT + threadIdx.x) * V;
     const uint32_t from = blockIdx.x * span, to = min(from + span, n);
     if (to >= n) return;
     const uint32_t token = key[to - 1];
@@ -425,17 +545,18 @@ __global__ __launch_bounds__(NT) void grad_join(gd_embed_grad_args a, const uint
         if (other) { hi += (uint32_t)__builtin_ctzll(other); break; }
         hi += 64;
     }
-    if (c >= a.width) return;
-    const float* p = partial + ((uint64_t)blockIdx.x * 2 + 1) * a.width + c;
+    if (c0 >= a.width) return;
+    const columns c = columns_of<V>(c0, a.width);
+    const gd_vec<float, V> first = gd_read<float, V>(partial + ((uint64_t)blockIdx.x * 2 + 1) * a.width + c.at);
     constexpr uint32_t PARTS = 16;                            // on their way at once
     float sum[V];
 #pragma unroll
-    for (int j = 0; j < V; ++j) sum[j] = p[j];
+    for (int j = 0; j < V; ++j) sum[j] = first.v[j];
     for (uint32_t s0 = blockIdx.x + 1; s0 < hi; s0 += PARTS) {
         gd_vec<float, V> q[PARTS];
 #pragma unroll
         for (uint32_t b = 0; b < PARTS; ++b)
-            q[b] = *reinterpret_cast<const gd_vec<float, V>*>(partial + (uint64_t)min(s0 + b, hi - 1) * 2 * a.width + c);
+            q[b] = gd_read<float, V>(partial + (uint64_t)min(s0 + b, hi - 1) * 2 * a.width + c.at);
 #pragma unroll
         for (uint32_t b = 0; b < PARTS; ++b)
             if (s0 + b < hi)
@@ -443,6 +564,140 @@ __global__ __launch_bounds__(NT) void grad_join(gd_embed_grad_args a, const uint
                 for (int j = 0; j < V; ++j) sum[j] += q[b].v[j];
     }
     write_sum<T, V>(a, token, c, sum, a.accumulate, a.accumulate ? old_row<T, V>(a, token, c) : gd_vec<T, V>{});
+}
+
+// ---- few rows: no list ------------------------------------------------------------------------
+
+// Workgroup i * across + y: row i and the columns of y, 64 * V << log_sub of them; those behind write zeros into the rows
+// without a token.  A token's rows are summed in order of their positions, more than BATCH of them in four parts
+// of the list, a wave each.
+template <typename T, int V, bool ADD, uint32_t ROUNDS>
+__global__ __launch_bounds__(NT) void grad_few(gd_embed_grad_args a, uint32_t across, uint32_t log_sub, uint32_t log_tx) {
+    constexpr uint32_t WAVES = NT / 64, MARKS = FILL_ROWS / 32;
+    __shared__ uint32_t marks[MARKS];
+    __shared__ uint16_t list[ROUNDS * NT];
+    __shared__ uint32_t counts[ROUNDS * WAVES];
+    __shared__ float sums[WAVES - 1][V][64];
+    const uint32_t n = a.tokens.n, wave = threadIdx.x / 64, lane = threadIdx.x & 63;
+    int64_t t[ROUNDS];
+    gd_tokens<ROUNDS>(a.tokens, threadIdx.x, NT, t);
+#pragma unroll
+    for (uint32_t r = 0; r < ROUNDS; ++r)
+        if (r * NT + threadIdx.x >= n) t[r] = -1;
+    if (blockIdx.x >= n * across) {
+        const uint64_t block = blockIdx.x - n * across, blocks = gridDim.x - n * across;
+        const uint32_t from = (uint32_t)(a.vocab * block / blocks), to = (uint32_t)(a.vocab * (block + 1) / blocks);
+        for (uint32_t i = threadIdx.x; i < MARKS; i += NT) marks[i] = 0;
+        __syncthreads();
+#pragma unroll
+        for (uint32_t r = 0; r < ROUNDS; ++r)
+            if (t[r] >= (int64_t)from && t[r] < (int64_t)to) atomicOr(&marks[((uint32_t)t[r] - from) / 32], 1u << (((uint32_t)t[r] - from) & 31));
+        __syncthreads();
+        const uint32_t tx = 1u << log_tx;
+        for (uint32_t r = threadIdx.x >> log_tx; r < to - from; r += NT >> log_tx)
+            if (!(marks[r / 32] >> (r & 31) & 1))
+                for (uint32_t c = (threadIdx.x & (tx - 1)) * V; c < a.width; c += tx * V)
+                    gd_write_through(static_cast<T*>(a.weight_grad) + (uint64_t)(from + r) * a.weight_grad_stride + columns_of<V>(c, a.width).at, gd_vec<T, V>{});
+        return;
+    }
+    const uint32_t i = blockIdx.x / across;
+    const int64_t token = gd_token(a.tokens, i);
+    if (token < 0 || token >= (int64_t)a.vocab) return;
+    constexpr uint32_t EARLIER = 1u << 31;
+    uint64_t who[ROUNDS];
+#pragma unroll
+    for (uint32_t r = 0; r < ROUNDS; ++r) {
+        who[r] = __ballot(t[r] == token);
+        const uint32_t first = r * NT + wave * 64 + (who[r] ? (uint32_t)__builtin_ctzll(who[r]) : 0);
+        if (lane == 0) counts[r * WAVES + wave] = (uint32_t)__popcll(who[r]) | (who[r] && first < i ? EARLIER : 0);
+    }
+    __syncthreads();
+    uint32_t count = 0;
+#pragma unroll
+    for (uint32_t k = 0; k < ROUNDS * WAVES; ++k) count |= counts[k];
+    if (count & EARLIER) return;                              // the token's first row sums them all
+    count = 0;
+#pragma unroll
+    for (uint32_t k = 0; k < ROUNDS * WAVES; ++k) {
+        if (k % WAVES == wave && (who[k / WAVES] >> lane & 1))
+            list[count + (uint32_t)__popcll(who[k / WAVES] & ((1ull << lane) - 1))] = (uint16_t)(k / WAVES * NT + threadIdx.x);
+        count += counts[k];
+    }
+    __syncthreads();
+    const T* rows = static_cast<const T*>(a.out_grad);
+    const auto sum_of = [&](uint32_t from, uint32_t to, columns c, float (&sum)[V]) {
+#pragma unroll
+        for (int j = 0; j < V; ++j) sum[j] = 0.0f;
+        for (uint32_t k0 = from; k0 < to; k0 += BATCH) {
+            gd_vec<T, V> q[BATCH];
+#pragma unroll
+            for (uint32_t b = 0; b < BATCH; ++b)
+                if (k0 + b < to) q[b] = gd_read<T, V>(rows + (uint64_t)list[k0 + b] * a.out_grad_stride + c.at);
+#pragma unroll
+            for (uint32_t b = 0; b < BATCH; ++b)
+                if (k0 + b < to)
+#pragma unroll
+                    for (int j = 0; j < V; ++j) sum[j] += gd_to_f32(q[b].v[j]);
+        }
+    };
+    const uint32_t subs = 1u << log_sub, c0 = (blockIdx.x % across) * (64 * V) * subs + lane * V;
+    float sum[V];
+    if (count <= BATCH) {
+        for (uint32_t sub = wave; sub < subs; sub += WAVES) {
+            if (c0 + sub * (64 * V) >= a.width) return;
+            const columns c = columns_of<V>(c0 + sub * (64 * V), a.width);
+            gd_vec<T, V> old{};
+            if constexpr (ADD) old = old_row<T, V>(a, (uint32_t)token, c);
+            sum_of(0, count, c, sum);
+            write_sum<T, V>(a, (uint32_t)token, c, sum, ADD, old);
+        }
+        return;
+    }
+    const uint32_t per = (count + WAVES - 1) / WAVES, from = min(wave * per, count), to = min(from + per, count);
+    for (uint32_t sub = 0; sub < subs; ++sub) {
+        const bool in = c0 + sub * (64 * V) < a.width;
+        const columns c = columns_of<V>(c0 + sub * (64 * V), a.width);
+        if (in) {
+            sum_of(from, to, c, sum);
+            if (wave > 0)
+#pragma unroll
+                for (int j = 0; j < V; ++j) sums[wave - 1][j][lane] = sum[j];
+        }
+        __syncthreads();
+        if (wave == 0 && in) {
+#pragma unroll
+            for (uint32_t w = 0; w < WAVES - 1; ++w)
+#pragma unroll
+                for (int j = 0; j < V; ++j) sum[j] += sums[w][j][lane];
+            write_sum<T, V>(a, (uint32_t)token, c, sum, ADD, ADD ? old_row<T, V>(a, (uint32_t)token, c) : gd_vec<T, V>{});
+        }
+        __syncthreads();
+    }
+}
+
+// Two blocks of columns a workgroup where single ones are more workgroups than the chip holds at once.
+uint32_t few_across(uint32_t width, uint32_t v, uint32_t log_sub) { return (width + ((64 * v) << log_sub) - 1) / ((64 * v) << log_sub); }
+uint32_t few_log_sub(uint32_t n, uint32_t width, uint32_t v) { return (uint64_t)n * few_across(width, v, 0) > 2048 ? 1 : 0; }
+bool few_rows(uint32_t n, uint32_t width, uint32_t v) {
+    return n <= FEW && (uint64_t)n * few_across(width, v, few_log_sub(n, width, v)) <= FEW_GROUPS;
+}
+
+template <typename T, int V, uint32_t ROUNDS>
+hipError_t launch_few(const gd_embed_grad_args& a, hipStream_t s) {
+    const uint32_t log_sub = few_log_sub(a.tokens.n, a.width, V), across = few_across(a.width, V, log_sub), sums = a.tokens.n * across;
+    uint32_t log_tx = 0;
+    if (a.accumulate) {
+        hipLaunchKernelGGL((grad_few<T, V, true, ROUNDS>), dim3(sums), dim3(NT), 0, s, a, across, log_sub, log_tx);
+        return hipGetLastError();
+    }
+    while (log_tx < 8 && (1u << log_tx) * V < a.width) ++log_tx;
+    // workgroups that fill have 16 KB each to write, or a row
+    const uint64_t bytes = (uint64_t)a.vocab * a.width * sizeof(T), least = (a.vocab + FILL_ROWS - 1) / FILL_ROWS;
+    uint64_t fill = (bytes + 16383) / 16384;
+    if (fill > a.vocab) fill = a.vocab;
+    if (fill < least) fill = least;
+    hipLaunchKernelGGL((grad_few<T, V, false, ROUNDS>), dim3(sums + (uint32_t)fill), dim3(NT), 0, s, a, across, log_sub, log_tx);
+    return hipGetLastError();
 }
 
 struct grad_layout {
@@ -472,17 +727,13 @@ hipError_t launch_grad(const gd_embed_grad_args& a, hipStream_t s) {
     const grad_layout l = layout_of(n, a.width);
     fill_args f;
     f.p = a.weight_grad; f.stride = a.weight_grad_stride; f.width = a.width; f.from = 0; f.to = 0;
-    // workgroups that fill: enough for the memory, no more than have 4 KB each to write
-    const auto fillers = [&](const fill_args& g, uint32_t threads) {
-        const uint64_t w = ((uint64_t)(g.to - g.from) * g.width * sizeof(T) + 4095) / 4096, most = 2048 * 256 / threads;
-        return (uint32_t)(w < most ? w : most);
-    };
     if (n == 0) {
         if (a.accumulate) return hipSuccess;
         f.to = a.vocab;
-        hipLaunchKernelGGL((fill_kernel<T, V>), dim3(fillers(f, NT)), dim3(NT), 0, s, f);
+        hipLaunchKernelGGL((fill_kernel<T, V>), dim3(fillers<T, NT>(f)), dim3(NT), 0, s, f);
         return hipGetLastError();
     }
+    if (few_rows(n, a.width, V)) return n <= FEW / 2 ? launch_few<T, V, FEW / 2 / NT>(a, s) : launch_few<T, V, FEW / NT>(a, s);
     sort_args b;
     for (int i = 0; i < 2; ++i) {
         b.key[i] = reinterpret_cast<uint32_t*>(a.work + l.key[i]);
@@ -493,22 +744,28 @@ hipError_t launch_grad(const gd_embed_grad_args& a, hipStream_t s) {
     uint32_t sorted = 0;
     if (n <= ONE_SORT) {
         if (!a.accumulate) f.to = a.vocab;
-        hipLaunchKernelGGL((sort_alone<T, V>), dim3(1 + fillers(f, 1024)), dim3(1024), 0, s, b, f);
+        hipLaunchKernelGGL((sort_alone<T, V>), dim3(1 + fillers<T, 1024>(f)), dim3(1024), 0, s, b, f);
     } else {
         uint32_t passes = 1;
         while (((uint64_t)a.vocab >> (passes * BITS)) > 0) ++passes;
+        const bool self = l.blocks <= SELF_COUNT;
         b.scanned = l.blocks > SELF_SCAN;
-        for (uint32_t i = 0; i < passes; ++i) {
-            b.shift = i * BITS;
-            for (uint32_t half = 0; half < 2; ++half) {       // (each launch fills its share)
-                f.from = f.to;
-                if (!a.accumulate) f.to = (uint32_t)((uint64_t)a.vocab * (2 * i + half + 1) / (2 * passes));
-                const dim3 grid(l.blocks + fillers(f, NT));
-                if (half == 0) hipLaunchKernelGGL((sort_count<T, V>), grid, dim3(NT), 0, s, b, f);
-                else hipLaunchKernelGGL((sort_scatter<T, V>), grid, dim3(NT), 0, s, b, f);
-                if (half == 0 && b.scanned) hipLaunchKernelGGL(sort_scan, dim3(DIGITS), dim3(NT), 0, s, b.hist, l.blocks);
+        const uint32_t launches = self ? passes : 2 * passes;
+        for (uint32_t i = 0; i < launches; ++i) {             // (each fills its share)
+            f.from = f.to;
+            if (!a.accumulate) f.to = (uint32_t)((uint64_t)a.vocab * (i + 1) / launches);
+            if (self) {
+                b.shift = i * BITS;
+                hipLaunchKernelGGL((sort_pass<T, V>), dim3(l.blocks + fillers<T, 1024>(f)), dim3(1024), 0, s, b, f);
+                b.from ^= 1;
+            } else if (i % 2 == 0) {
+                b.shift = i / 2 * BITS;
+                hipLaunchKernelGGL((sort_count<T, V>), dim3(l.blocks + fillers<T, NT>(f)), dim3(NT), 0, s, b, f);
+                if (b.scanned) hipLaunchKernelGGL(sort_scan, dim3(DIGITS), dim3(NT), 0, s, b.hist, l.blocks);
+            } else {
+                hipLaunchKernelGGL((sort_scatter<T, V>), dim3(l.blocks + fillers<T, NT>(f)), dim3(NT), 0, s, b, f);
+                b.from ^= 1;
             }
-            b.from ^= 1;
         }
         sorted = b.from;
     }
@@ -532,18 +789,20 @@ size_t gd_embed_grad_work(uint64_t n, uint64_t width) { return layout_of(n, widt
 
 hipError_t gd_launch_embed(const gd_embed_args& a, hipStream_t s) {
     if (a.tokens.n == 0 || a.width == 0) return hipSuccess;
-    const uint32_t size = a.dtype == GD_F32 ? 4 : 2;
-    const uint32_t v = vector_of(a.weight, a.weight_stride, a.out, a.out_stride, a.width, size);
-    if (a.dtype == GD_F32) return v == 4 ? launch_embed<float, 4>(a, s) : launch_embed<float, 1>(a, s);
-    if (a.dtype == GD_BF16) return v == 8 ? launch_embed<gd_bf16, 8>(a, s) : v >= 2 ? launch_embed<gd_bf16, 2>(a, s) : launch_embed<gd_bf16, 1>(a, s);
-    return v == 8 ? launch_embed<gd_f16, 8>(a, s) : v >= 2 ? launch_embed<gd_f16, 2>(a, s) : launch_embed<gd_f16, 1>(a, s);
+    const auto launch = [&](auto zero) {                          // (rows shorter than 16 bytes: an element a lane)
+        typedef decltype(zero) T;
+        constexpr int V = 16 / sizeof(T);
+        return a.width >= V ? launch_embed<T, V>(a, s) : launch_embed<T, 1>(a, s);
+    };
+    return a.dtype == GD_F32 ? launch(0.0f) : a.dtype == GD_BF16 ? launch(gd_bf16(0.0f)) : launch(gd_f16(0.0f));
 }
 
 hipError_t gd_launch_embed_grad(const gd_embed_grad_args& a, hipStream_t s) {
     if (a.width == 0 || a.vocab == 0) return hipSuccess;
-    const uint32_t size = a.dtype == GD_F32 ? 4 : 2;
-    const uint32_t v = vector_of(a.out_grad, a.out_grad_stride, a.weight_grad, a.weight_grad_stride, a.width, size);
-    if (a.dtype == GD_F32) return v == 4 ? launch_grad<float, 4>(a, s) : launch_grad<float, 1>(a, s);
-    if (a.dtype == GD_BF16) return v == 8 ? launch_grad<gd_bf16, 8>(a, s) : v >= 2 ? launch_grad<gd_bf16, 2>(a, s) : launch_grad<gd_bf16, 1>(a, s);
-    return v == 8 ? launch_grad<gd_f16, 8>(a, s) : v >= 2 ? launch_grad<gd_f16, 2>(a, s) : launch_grad<gd_f16, 1>(a, s);
+    const auto launch = [&](auto zero) {
+        typedef decltype(zero) T;
+        constexpr int V = 16 / sizeof(T);
+        return a.width >= V ? launch_grad<T, V>(a, s) : launch_grad<T, 1>(a, s);
+    };
+    return a.dtype == GD_F32 ? launch(0.0f) : a.dtype == GD_BF16 ? launch(gd_bf16(0.0f)) : launch(gd_f16(0.0f));
 }

@@ -90,22 +90,49 @@ __device__ __forceinline__ int64_t gd_token(const gd_token_list& l, uint64_t i) 
                   : (int64_t)static_cast<const int32_t*>(l.p)[i * l.stride];
 }
 
+// Elements from, from + step, ... of a list (the last one where they lie behind its end), all on their way at once: one
+// after another behind their own branches, each would be waited for.  The list is not empty.
+template <int N>
+__device__ __forceinline__ void gd_tokens(const gd_token_list& l, uint32_t from, uint32_t step, int64_t (&t)[N]) {
+    if (l.wide) {
+#pragma unroll
+        for (int b = 0; b < N; ++b) t[b] = static_cast<const int64_t*>(l.p)[min(from + b * step, l.n - 1) * l.stride];
+    } else {
+        int32_t q[N];
+#pragma unroll
+        for (int b = 0; b < N; ++b) q[b] = static_cast<const int32_t*>(l.p)[min(from + b * step, l.n - 1) * l.stride];
+#pragma unroll
+        for (int b = 0; b < N; ++b) t[b] = q[b];
+    }
+}
+
 // Conversions: to fp32 exactly, from it to nearest even.
 template <typename T> __device__ __forceinline__ float gd_to_f32(T v) { return (float)v; }
 template <typename T> __device__ __forceinline__ T gd_from_f32(float v) { return (T)v; }
 
-// V elements at once (V * sizeof(T) = 4, 8 or 16 bytes, aligned to that).
+// V elements at once.  Memory is read and written 16 bytes at a time wherever a row begins: such an access needs no more
+// alignment than its element has (rows of 4 095 elements in pieces that divide their distance took 2 to 3 times as long).
 template <typename T, int V> struct alignas(sizeof(T) * V) gd_vec { T v[V]; };
+
+typedef uint32_t gd_u32x4 __attribute__((ext_vector_type(4)));
+typedef gd_u32x4 gd_u32x4_anywhere __attribute__((aligned(2)));
+
+template <typename T, int V>
+__device__ __forceinline__ gd_vec<T, V> gd_read(const T* p) {
+    if constexpr (sizeof(gd_vec<T, V>) == 16) {
+        return __builtin_bit_cast(gd_vec<T, V>, (gd_u32x4)*reinterpret_cast<const gd_u32x4_anywhere*>(p));
+    } else {
+        gd_vec<T, V> q;
+        __builtin_memcpy(&q, p, sizeof(q));
+        return q;
+    }
+}
 
 // A store of data that is not read again soon.
 template <typename T, int V>
 __device__ __forceinline__ void gd_write_through(T* p, const gd_vec<T, V>& q) {
-    if constexpr (sizeof(q) == 16) {
-        typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-        __builtin_nontemporal_store(*reinterpret_cast<const u32x4*>(&q), reinterpret_cast<u32x4*>(p));
-    } else {
-        *reinterpret_cast<gd_vec<T, V>*>(p) = q;
-    }
+    if constexpr (sizeof(q) == 16) __builtin_nontemporal_store(__builtin_bit_cast(gd_u32x4, q), reinterpret_cast<gd_u32x4_anywhere*>(p));
+    else __builtin_memcpy(p, &q, sizeof(q));
 }
 #endif
 

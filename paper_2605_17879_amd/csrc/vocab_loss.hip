@@ -581,16 +581,14 @@ __global__ __launch_bounds__(TILE::NT, 512 / TILE::NT) void product_kernel(const
         const uint32_t c = lane & 15, ch = f * 2 + (lane >> 5);
         *reinterpret_cast<gd_vec<T, 4>*>(spare + c * (CH * 16) + ((ch ^ (c & (CH - 1))) * 16) + ((lane >> 4) & 1) * 8) = q;
     };
-    auto take = [&](auto wide, auto write) {                     // `wide`: elements a lane, 8 or fewer
-        constexpr uint32_t V = decltype(wide)::value, LANES = FM * 16 / V;
+    auto take = [&](auto write) {
 #pragma unroll
-        for (uint32_t it = 0; it < 16 * LANES / 64; ++it) {
-            const uint32_t at = it * 64 + lane, c = at / LANES, e = at % LANES * V, ch = e / 8;
-            const uint8_t* from = spare + c * (CH * 16) + ((ch ^ (c & (CH - 1))) * 16) + e % 8 * 2;
-            write(c, m0 + TILE::row_of(wm, e / 16) + e % 16, *reinterpret_cast<const gd_vec<T, V>*>(from));
+        for (uint32_t it = 0; it < 16 * CH / 64; ++it) {
+            const uint32_t at = it * 64 + lane, c = at / CH, ch = at % CH;
+            const uint8_t* from = spare + c * (CH * 16) + ((ch ^ (c & (CH - 1))) * 16);
+            write(c, m0 + TILE::row_of(wm, ch / 2) + ch % 2 * 8, *reinterpret_cast<const gd_vec<T, 8>*>(from));
         }
     };
-    typedef std::integral_constant<uint32_t, 8> eight;
     if constexpr (EPI == EPI_LSE) {
         __shared__ float2 join[WM * BN];
 #pragma unroll
@@ -613,7 +611,7 @@ __global__ __launch_bounds__(TILE::NT, 512 / TILE::NT) void product_kernel(const
 #pragma unroll
             for (int f = 0; f < FM; ++f) put(f, four_of<T>(acc[f][j]));
             // (there is room for whole tiles of rows)
-            take(eight(), [&](uint32_t c, uint32_t m, const gd_vec<T, 8>& q) {
+            take([&](uint32_t c, uint32_t m, const gd_vec<T, 8>& q) {
                 *reinterpret_cast<gd_vec<T, 8>*>(g + (uint64_t)(n0 + TILE::col_of(wn, j) + c) * p.ldc + m) = q;
             });
         }
@@ -634,38 +632,58 @@ __global__ __launch_bounds__(TILE::NT, 512 / TILE::NT) void product_kernel(const
     } else {
         T* out = static_cast<T*>(p.c);
         const float back = p.head->back, more = p.head->more * p.scale;
-        auto rows_of = [&](auto wide) {
-            constexpr uint32_t V = decltype(wide)::value;
 #pragma unroll
-            for (int j = 0; j < FN; ++j) {
+        for (int j = 0; j < FN; ++j) {
 #pragma unroll
-                for (int f = 0; f < FM; ++f) put(f, four_of<T>(acc[f][j] * back * more));
-                take(wide, [&](uint32_t c, uint32_t m, const gd_vec<T, V>& q) {
-                    const uint32_t i = n0 + TILE::col_of(wn, j) + c;
-                    if (i >= p.n) return;
-                    T* to = out + (uint64_t)i * p.ldc + m;
-                    if (m + V <= p.m) {
-                        gd_write_through(to, q);
-                    } else {
+            for (int f = 0; f < FM; ++f) put(f, four_of<T>(acc[f][j] * back * more));
+            take([&](uint32_t c, uint32_t m, const gd_vec<T, 8>& q) {
+                const uint32_t i = n0 + TILE::col_of(wn, j) + c;
+                if (i >= p.n) return;
+                T* to = out + (uint64_t)i * p.ldc + m;
+                if (m + 8 <= p.m) {
+                    gd_write_through(to, q);
+                } else {
 #pragma unroll
-                        for (uint32_t r = 0; r < V; ++r)
-                            if (m + r < p.m) to[r] = q.v[r];
-                    }
-                });
-            }
-        };
-        // (what every row is aligned to; lanes side by side write what lies side by side)
-        if ((p.ldc & 7) == 0 && ((uintptr_t)out & 15) == 0) rows_of(eight());
-        else if ((p.ldc & 1) == 0 && ((uintptr_t)out & 3) == 0) rows_of(std::integral_constant<uint32_t, 2>());
-        else rows_of(std::integral_constant<uint32_t, 1>());
+                    for (uint32_t r = 0; r < 8; ++r)
+                        if (m + r < p.m) to[r] = q.v[r];
+                }
+            });
+        }
     }
 }
 
 // ---- few rows ----------------------------------------------------------------------------------
 
+// Eight elements of a row, wherever it begins.
+template <typename T>
+__device__ __forceinline__ typename of_type<T>::x8 eight_at(const T* p) {
+    return __builtin_bit_cast(typename of_type<T>::x8, gd_read<T, 8>(p));
+}
+// Those from `at` on, zeros behind the row's end; no branch where the row has eight elements (`whole`): what lies in front
+// of the end is read and moved down.
+template <typename T>
+__device__ __forceinline__ typename of_type<T>::x8 last_at(const T* row, int32_t at, int32_t end, bool whole) {
+    typename of_type<T>::x8 x(0);
+    if (whole) {
+        const int32_t down = max(at + 8 - end, 0);
+        struct { uint64_t lo, hi; } q = __builtin_bit_cast(decltype(q), eight_at(row + at - down));
+        const uint32_t bits = (uint32_t)(down & 3) * 16;
+        const uint64_t lo = down & 4 ? q.hi : q.lo, hi = down & 4 ? 0 : q.hi;
+        q.lo = down >= 8 ? 0 : lo >> bits | (hi << 1) << (63 - bits);
+        q.hi = down >= 8 ? 0 : hi >> bits;
+        return __builtin_bit_cast(typename of_type<T>::x8, q);
+    }
+#pragma unroll
+    for (int32_t j = 0; j < 8; ++j) {
+        const T e = row[min(at + j, end - 1)];
+        x[j] = at + j < end ? e : T(0.0f);
+    }
+    return x;
+}
+
 // Logits where rows and words make too few tiles for the chip: a workgroup takes 32 words and up to 64 rows, its
 // four waves a block of 64 k each in turn, straight into registers and DEPTH blocks ahead, with no LDS and no
-// barrier between the loads; their sums are added up through the LDS.
+// barrier between the loads; their sums are added up through the LDS.  Rows are read where they lie, aligned or not.
 template <typename T, int FN, int EPI>
 __global__ __launch_bounds__(256) void few_rows_kernel(const product_args p) {
     typedef typename of_type<T>::x8 X8;
@@ -695,9 +713,9 @@ __global__ __launch_bounds__(256) void few_rows_kernel(const product_args p) {
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
 #pragma unroll
-            for (int i = 0; i < FM; ++i) fa[d][i][h] = *reinterpret_cast<const X8*>(a[i] + at + h * 32);
+            for (int i = 0; i < FM; ++i) fa[d][i][h] = eight_at(a[i] + at + h * 32);
 #pragma unroll
-            for (int j = 0; j < FN; ++j) fb[d][j][h] = *reinterpret_cast<const X8*>(b[j] + at + h * 32);
+            for (int j = 0; j < FN; ++j) fb[d][j][h] = eight_at(b[j] + at + h * 32);
         }
     };
     auto use = [&](int d) {
@@ -720,14 +738,26 @@ __global__ __launch_bounds__(256) void few_rows_kernel(const product_args p) {
             }
     }
     if (k % BK && whole % WAVES == wave) {                       // the last block ends inside: zeros behind the end
-        const uint32_t at = whole * BK;
+        // (a lane's rows are counted from its own place, which may lie behind their end)
+        const int32_t at = (int32_t)(whole * BK), end = (int32_t)k - (int32_t)(lane >> 4) * 8;
+        if (k % 8 == 0) {
 #pragma unroll
-        for (uint32_t h = 0; h < 2; ++h) {
-            const bool in = at + h * 32 + (lane >> 4) * 8 < k;
+            for (int32_t h = 0; h < 2; ++h) {
+                const int32_t from = min(at + h * 32, end - 8);
+                const bool in = at + h * 32 < end;
 #pragma unroll
-            for (int i = 0; i < FM; ++i) fa[0][i][h] = in ? *reinterpret_cast<const X8*>(a[i] + at + h * 32) : X8(0);
+                for (int i = 0; i < FM; ++i) fa[0][i][h] = in ? eight_at(a[i] + from) : X8(0);
 #pragma unroll
-            for (int j = 0; j < FN; ++j) fb[0][j][h] = in ? *reinterpret_cast<const X8*>(b[j] + at + h * 32) : X8(0);
+                for (int j = 0; j < FN; ++j) fb[0][j][h] = in ? eight_at(b[j] + from) : X8(0);
+            }
+        } else {
+#pragma unroll
+            for (int32_t h = 0; h < 2; ++h) {
+#pragma unroll
+                for (int i = 0; i < FM; ++i) fa[0][i][h] = last_at(a[i], at + h * 32, end, k >= 8);
+#pragma unroll
+                for (int j = 0; j < FN; ++j) fb[0][j][h] = last_at(b[j], at + h * 32, end, k >= 8);
+            }
         }
         use(0);
     }
@@ -779,20 +809,13 @@ __global__ __launch_bounds__(256) void pack_kernel(const void* in, uint64_t stri
                                                    const uint32_t* rows, uint32_t n, T* out, uint32_t ldo) {
     if (head) n = head->count;
     const uint32_t last = head ? (n + 255) / 256 * 256 : n, chunks = ldo / 8;
-    const bool whole = ((uintptr_t)in & 15) == 0 && stride % 8 == 0 && width % 8 == 0;
     const uint64_t total = (uint64_t)last * chunks;
     for (uint64_t x = (uint64_t)blockIdx.x * 256 + threadIdx.x; x < total; x += (uint64_t)gridDim.x * 256) {
         const uint32_t r = (uint32_t)(x / chunks), c = (uint32_t)(x - (uint64_t)r * chunks) * 8;
         gd_vec<T, 8> q{};
         if (r < n) {
-            const T* from = static_cast<const T*>(in) + (rows ? (uint64_t)rows[r] : (uint64_t)r) * stride + c;
-            if (whole) {
-                q = *reinterpret_cast<const gd_vec<T, 8>*>(from);
-            } else {
-#pragma unroll
-                for (uint32_t j = 0; j < 8; ++j)
-                    if (c + j < width) q.v[j] = from[j];
-            }
+            const uint64_t row = rows ? rows[r] : r;
+            if (c < width) q = __builtin_bit_cast(gd_vec<T, 8>, last_at(static_cast<const T*>(in) + row * stride, (int32_t)c, (int32_t)width, width >= 8));
         }
         *reinterpret_cast<gd_vec<T, 8>*>(out + (uint64_t)r * ldo + c) = q;
     }
@@ -880,17 +903,26 @@ __global__ __launch_bounds__(1024) void join_alone(const join_args a, uint32_t s
     }
 }
 
-// Mean over the rows not left out, one workgroup, in a fixed order.
+// Mean over the rows not left out, one workgroup, in a fixed order, AT_ONCE rows a lane at once.
+template <int AT_ONCE>
 __global__ __launch_bounds__(1024) void mean_kernel(const float* loss, gd_token_list targets, float* mean) {
     __shared__ float s[16];
     __shared__ uint32_t c[16];
     const uint32_t wave = threadIdx.x / 64, lane = threadIdx.x & 63;
     float sum = 0.0f;
     uint32_t count = 0;
-#pragma unroll 4
-    for (uint32_t i = threadIdx.x; i < targets.n; i += 1024) {
-        sum += loss[i];
-        count += gd_token(targets, i) >= 0;
+    for (uint32_t i = threadIdx.x; i < targets.n; i += AT_ONCE * 1024) {
+        int64_t t[AT_ONCE];
+        float l[AT_ONCE];
+        gd_tokens<AT_ONCE>(targets, i, 1024, t);
+#pragma unroll
+        for (int b = 0; b < AT_ONCE; ++b) l[b] = loss[min(i + b * 1024, targets.n - 1)];
+#pragma unroll
+        for (int b = 0; b < AT_ONCE; ++b)
+            if (i + b * 1024 < targets.n) {
+                sum += l[b];
+                count += t[b] >= 0;
+            }
     }
 #pragma unroll
     for (int d = 32; d > 0; d >>= 1) {
@@ -923,14 +955,6 @@ struct rows_args {
     float* row_lse2;  float* row_coef;  int32_t* row_target;
 };
 
-__device__ __forceinline__ float coef_of(const rows_args& a, uint32_t i) {
-    const int64_t t = gd_token(a.targets, i);
-    if (t < 0 || t >= (int64_t)a.vocab) return 0.0f;
-    float c = a.grad_rows ? a.grad_rows[i] : 0.0f;
-    if (a.grad_mean) c += *a.grad_mean / fmaxf(a.mean[1], 1.0f);
-    return c;
-}
-
 // What the coefficients are scaled by.  Gradients of a mean over many rows, and of improbable words, would underflow
 // as G is rounded to 16 bits, and the -1 at the target would be rounded as well: coefficients are divided by the
 // largest one and multiplied by 2^15 in f16 (G is at most that then) and by 2^40 in bf16 (where every
@@ -955,42 +979,70 @@ __device__ __forceinline__ uint32_t wave_max(uint32_t v, uint32_t lane) {
     v = max(v, gd_lane_xor<16>(v, lane)); return max(v, gd_lane_xor<32>(v, lane));
 }
 
-// Row i, the at-th with a gradient.
-__device__ __forceinline__ void write_row(const rows_args& a, uint32_t i, uint32_t at, float coef) {
-    a.row_lse2[at] = a.lse[i] * LOG2E;
-    a.row_coef[at] = coef;
-    a.row_target[at] = (int32_t)gd_token(a.targets, i);
-}
-
-// Lists the rows with a gradient and works out what their tiles need.  One workgroup: the list is in order of the
-// rows.
+// Lists the rows with a gradient and works out what their tiles need.  One workgroup, EACH rows a lane at once: the list
+// is in order of the rows.
+template <int EACH>
 __global__ __launch_bounds__(1024) void prepare_rows(const rows_args a) {
-    __shared__ uint32_t s[16];
+    constexpr uint32_t ROUND = EACH * 1024, WAVES = 16;
+    __shared__ uint32_t s[EACH * WAVES];
     const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x / 64, n = a.targets.n;
+    const float each = a.grad_mean ? *a.grad_mean / fmaxf(a.mean[1], 1.0f) : 0.0f;
+    float c[EACH], lse[EACH];
+    int64_t t[EACH];
+    const auto load = [&](uint32_t base) {
+        const uint32_t from = base + threadIdx.x;
+        gd_tokens<EACH>(a.targets, from, 1024, t);
+#pragma unroll
+        for (int b = 0; b < EACH; ++b) {
+            lse[b] = a.lse[min(from + b * 1024, n - 1)];
+            c[b] = 0.0f;
+        }
+        if (a.grad_rows)
+#pragma unroll
+            for (int b = 0; b < EACH; ++b) c[b] = a.grad_rows[min(from + b * 1024, n - 1)];
+#pragma unroll
+        for (int b = 0; b < EACH; ++b) {
+            if (a.grad_mean) c[b] += each;
+            if (from + b * 1024 >= n || t[b] < 0 || t[b] >= (int64_t)a.vocab) c[b] = 0.0f;
+        }
+    };
     uint32_t top = 0;
-    for (uint32_t i = threadIdx.x; i < n; i += 1024) top = max(top, __float_as_uint(coef_of(a, i)) & 0x7FFFFFFFu);
+    for (uint32_t base = 0; base < n; base += ROUND) {
+        load(base);
+#pragma unroll
+        for (int b = 0; b < EACH; ++b) top = max(top, __float_as_uint(c[b]) & 0x7FFFFFFFu);
+    }
     top = wave_max(top, lane);
     if (lane == 0) s[wave] = top;
     __syncthreads();
-    for (int w = 0; w < 16; ++w) top = max(top, s[w]);
+    for (uint32_t w = 0; w < WAVES; ++w) top = max(top, s[w]);
     __syncthreads();
     const coef_scale scale(top, a.half);
     uint32_t count = 0;
-    for (uint32_t base = 0; base < n; base += 1024) {
-        const uint32_t i = base + threadIdx.x;
-        const float c = i < n ? coef_of(a, i) : 0.0f;
-        const bool in = c != 0.0f;
-        const uint64_t who = __ballot(in);
-        if (lane == 0) s[wave] = (uint32_t)__popcll(who);
-        __syncthreads();
-        uint32_t at = count;
-        for (uint32_t w = 0; w < 16; ++w) { if (w < wave) at += s[w]; count += s[w]; }
-        at += (uint32_t)__popcll(who & ((1ull << lane) - 1));
-        if (in) {
-            a.rows[at] = i;
-            write_row(a, i, at, scale.of(c));
+    for (uint32_t base = 0; base < n; base += ROUND) {
+        if (n > ROUND) load(base);                            // (else they are still here)
+        uint64_t who[EACH];
+#pragma unroll
+        for (int b = 0; b < EACH; ++b) {
+            who[b] = __ballot(c[b] != 0.0f);
+            if (lane == 0) s[b * WAVES + wave] = (uint32_t)__popcll(who[b]);
         }
-        if (i < n) a.slot[i] = in ? (int32_t)at : -1;
+        __syncthreads();
+#pragma unroll
+        for (int b = 0; b < EACH; ++b) {
+            uint32_t at = count;
+            for (uint32_t w = 0; w < WAVES; ++w) { if (w < wave) at += s[b * WAVES + w]; count += s[b * WAVES + w]; }
+            at += (uint32_t)__popcll(who[b] & ((1ull << lane) - 1));
+            const uint32_t i = base + b * 1024 + threadIdx.x;
+            const bool in = c[b] != 0.0f;
+            if (in) {
+                a.rows[at] = i;
+                a.row_lse2[at] = lse[b] * LOG2E;
+                a.row_coef[at] = scale.of(c[b]);
+                a.row_target[at] = (int32_t)t[b];
+            }
+            if (i < n) a.slot[i] = in ? (int32_t)at : -1;
+        }
         __syncthreads();
     }
     if (threadIdx.x == 0) scale.write(a.head, count);
@@ -1003,7 +1055,6 @@ __global__ __launch_bounds__(256) void finish_hidden(const float* slabs, uint32_
                                                      uint32_t width, T* out, uint64_t ldo) {
     const uint32_t quads = lds / 4;
     const float back = head->back, more = head->more * scale;
-    const bool whole = (ldo & 3) == 0 && ((uintptr_t)out & 7) == 0;
     const uint64_t total = (uint64_t)n * quads;
     for (uint64_t x = (uint64_t)blockIdx.x * 256 + threadIdx.x; x < total; x += (uint64_t)gridDim.x * 256) {
         const uint32_t i = (uint32_t)(x / quads), c = (uint32_t)(x - (uint64_t)i * quads) * 4;
@@ -1032,8 +1083,8 @@ __global__ __launch_bounds__(256) void finish_hidden(const float* slabs, uint32_
 #pragma unroll
         for (int r = 0; r < 4; ++r) q.v[r] = gd_from_f32<T>(sum[r] * back * more);
         T* to = out + (uint64_t)i * ldo + c;
-        if (whole && c + 4 <= width) {
-            *reinterpret_cast<gd_vec<T, 4>*>(to) = q;
+        if (c + 4 <= width) {
+            __builtin_memcpy(to, &q, sizeof(q));
         } else {
 #pragma unroll
             for (uint32_t r = 0; r < 4; ++r)
@@ -1234,14 +1285,15 @@ hipError_t forward(const gd_vocab_loss_args& a, hipStream_t s) {
     T* hidden = reinterpret_cast<T*>(a.work + l.hidden);
     T* weight = reinterpret_cast<T*>(a.work + l.weight);
     product_args p = {};
+    const bool few = few_tiles(n, a.vocab);
     p.b = operand{a.hidden, a.hidden_stride, n, a.width};
-    if (!direct(a.hidden, a.hidden_stride, a.width)) {
+    if (!few && !direct(a.hidden, a.hidden_stride, a.width)) {
         hipLaunchKernelGGL((pack_kernel<T>), dim3(blocks_for((uint64_t)n * ldh / 8)), dim3(256), 0, s, a.hidden, a.hidden_stride, a.width,
                            (const grad_head*)nullptr, (const uint32_t*)nullptr, n, hidden, ldh);
         p.b = operand{hidden, ldh, n, ldh};
     }
-    const bool plain = direct(a.weight, a.weight_stride, a.width);
-    p.k = (uint32_t)up_to(a.width, 8);                           // (rows of a copy go on with zeros)
+    const bool plain = few || direct(a.weight, a.weight_stride, a.width);
+    p.k = few ? a.width : (uint32_t)up_to(a.width, 8);           // (rows of a copy go on with zeros)
     p.n = n; p.scale = a.scale; p.scale2 = a.scale * LOG2E; p.vocab = a.vocab; p.targets = a.targets;
     p.target_logit = reinterpret_cast<float*>(a.work + l.target_logit);
     p.part = reinterpret_cast<float2*>(a.work + l.part);
@@ -1249,7 +1301,6 @@ hipError_t forward(const gd_vocab_loss_args& a, hipStream_t s) {
     // (a launch has no more than 2^28 tiles)
     const uint64_t most = ((1ull << 28) / (up_to(n, 128) / 128)) * 128, want = plain ? a.vocab : l.pack_piece;
     const uint32_t piece = (uint32_t)(want < most ? want : most);
-    const bool few = few_tiles(n, a.vocab);
     uint32_t parts = 0;
     for (uint32_t v0 = 0; v0 < a.vocab; v0 += piece) {
         const uint32_t here = a.vocab - v0 < piece ? a.vocab - v0 : piece;
@@ -1272,7 +1323,8 @@ hipError_t forward(const gd_vocab_loss_args& a, hipStream_t s) {
         return hipGetLastError();
     }
     hipLaunchKernelGGL(join_kernel, dim3((n + 3) / 4), dim3(256), 0, s, j);
-    hipLaunchKernelGGL(mean_kernel, dim3(1), dim3(1024), 0, s, a.loss, a.targets, a.mean);
+    if (n <= 1024) hipLaunchKernelGGL((mean_kernel<1>), dim3(1), dim3(1024), 0, s, a.loss, a.targets, a.mean);
+    else hipLaunchKernelGGL((mean_kernel<8>), dim3(1), dim3(1024), 0, s, a.loss, a.targets, a.mean);
     return hipGetLastError();
 }
 
@@ -1296,7 +1348,8 @@ hipError_t backward(const gd_vocab_grad_args& a, hipStream_t s) {
     r.row_coef = reinterpret_cast<float*>(a.work + l.coef);
     r.row_target = reinterpret_cast<int32_t*>(a.work + l.target);
     const uint32_t padded = (uint32_t)l.padded_rows;
-    hipLaunchKernelGGL(prepare_rows, dim3(1), dim3(1024), 0, s, r);
+    if (n <= 1024) hipLaunchKernelGGL((prepare_rows<1>), dim3(1), dim3(1024), 0, s, r);
+    else hipLaunchKernelGGL((prepare_rows<8>), dim3(1), dim3(1024), 0, s, r);
     hipLaunchKernelGGL((pack_kernel<T>), dim3(blocks_for((uint64_t)padded * ldh / 8)), dim3(256), 0, s, a.hidden, a.hidden_stride, a.width,
                        head, r.rows, n, hidden, ldh);
     const bool plain = direct(a.weight, a.weight_stride, a.width);
@@ -1307,7 +1360,7 @@ hipError_t backward(const gd_vocab_grad_args& a, hipStream_t s) {
         const uint32_t here = a.vocab - v0 < piece ? a.vocab - v0 : piece;
         const T* w = static_cast<const T*>(a.weight) + (uint64_t)v0 * a.weight_stride;
         operand wo{w, a.weight_stride, here, a.width};
-        if (!plain) {
+        if (!plain && (a.hidden_grad || !few)) {
             hipLaunchKernelGGL((pack_kernel<T>), dim3(blocks_for((uint64_t)here * ldh / 8)), dim3(256), 0, s, w, a.weight_stride, a.width,
                                (const grad_head*)nullptr, (const uint32_t*)nullptr, here, weight, ldh);
             wo = operand{weight, ldh, here, ldh};
@@ -1317,7 +1370,7 @@ hipError_t backward(const gd_vocab_grad_args& a, hipStream_t s) {
         p.head = head;
         p.a = wo;
         p.b = operand{hidden, ldh, padded, ldh};
-        p.m = here; p.n = n; p.k = (uint32_t)up_to(a.width, 8);
+        p.m = here; p.n = n; p.k = few ? a.width : (uint32_t)up_to(a.width, 8);
         p.scale2 = a.scale * LOG2E; p.v0 = v0; p.vocab = a.vocab;
         p.row_lse2 = r.row_lse2; p.row_coef = r.row_coef; p.row_target = r.row_target;
         p.c = g; p.ldc = piece;
@@ -1358,7 +1411,7 @@ size_t gd_vocab_loss_work(uint64_t n, uint64_t vocab, uint64_t width, bool with_
 
 hipError_t gd_launch_vocab_loss(const gd_vocab_loss_args& a, hipStream_t s) {
     if (a.targets.n == 0) {
-        hipLaunchKernelGGL(mean_kernel, dim3(1), dim3(1024), 0, s, a.loss, a.targets, a.mean);
+        hipLaunchKernelGGL((mean_kernel<1>), dim3(1), dim3(1024), 0, s, a.loss, a.targets, a.mean);
         return hipGetLastError();
     }
     return a.dtype == GD_BF16 ? forward<gd_bf16>(a, s) : forward<gd_f16>(a, s);

@@ -121,6 +121,30 @@ def test_lookup_grad(det, accumulate, dtype, n, vocab, width, gap):
     check_grad(det, randn((n, width), n, dtype), t, vocab, 1.7, accumulate, randn((vocab, width), n + 2, dtype), gap)
 
 
+@pytest.mark.parametrize("accumulate", [False, True])
+@pytest.mark.parametrize("n,vocab,width,dtype", [
+    # both sides of the lines between lists that are compared, sorted at once, by workgroups that count all, and by ones that do not
+    (1024, 3000, 520, BF16), (1024, 40, 33, F32), (1025, 3000, 136, BF16), (2048, 50, 72, F16), (2049, 3000, 24, F32), (3000, 70000, 24, F16), (4096, 500, 72, F32),
+    (65536, 600, 8, BF16), (65537, 600, 8, BF16), (30000, 1 << 19, 8, F32),
+    # few rows: wide ones, rows that are not aligned, more rows of the table than one workgroup marks
+    (700, 90, 4096, F32), (1000, 50, 2500, F16), (900, 12, 1001, BF16), (9, 16385, 1, BF16), (300, 300000, 2, F32), (2, 1 << 20, 4, F32),
+])
+def test_lookup_grad_of_lists_of_all_lengths(det, accumulate, n, vocab, width, dtype):
+    say(f"lookup_grad of lists {dtype} n={n} vocab={vocab} width={width} accumulate={accumulate}")
+    t = refs.tokens(n, vocab, n + 1, padding=0.05)
+    check_grad(det, randn((n, width), n, dtype), t, vocab, 0.7, accumulate, randn((vocab, width), n + 2, dtype))
+
+
+@pytest.mark.parametrize("n", [9, 63, 64, 65, 700, 1024, 1500, 2048])
+def test_lookup_grad_of_few_tokens_over_and_over(det, n):
+    """One to three tokens in a list of few rows, in runs and in turn."""
+    say(f"few tokens over and over, n={n}")
+    i = torch.arange(n)
+    for t in (torch.full((n,), 3), i % 2 * 4, torch.where(i < n // 2, 1, 2), torch.where(i % 3 == 0, -1, 5)):
+        check_grad(det, randn((n, 264), n, BF16), t, 9, 1.0, False)
+        check_grad(det, randn((n, 264), n, F32), t, 9, 1.5, True, randn((9, 264), 1, F32))
+
+
 @pytest.mark.parametrize("n", [5, 5000])
 @pytest.mark.parametrize("gap", [8, 3])
 def test_lookup_grad_into_rows_apart(det, n, gap):
