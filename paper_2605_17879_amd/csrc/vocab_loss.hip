@@ -532,14 +532,16 @@ __device__ __forceinline__ gd_vec<T, 4> four_of(const f32x4& x) {
 template <typename T, typename TILE, int EPI>
 __global__ __launch_bounds__(TILE::NT, 512 / TILE::NT) void product_kernel(const product_args p) {
     constexpr int BM = TILE::BM, BN = TILE::BN, WM = TILE::WM, WN = TILE::WN, FM = TILE::FM, FN = TILE::FN;
-    uint32_t tm, tn;
-    // (strips of four for the weights' gradient: 6 970 against 7 150 us, 8 192 rows x 131 072 x 4 096; of eight otherwise)
-    tile_of<EPI == EPI_OUT ? 4 : 8>(blockIdx.x, p.tiles_m, p.tiles_n, tm, tn);
-    uint32_t n = p.n, k = p.k;
-    if (EPI == EPI_G || EPI == EPI_SLAB) n = p.head->count;
+    uint32_t tm, tn, n = p.n, k = p.k, tiles_n = p.tiles_n;
+    if (EPI == EPI_G || EPI == EPI_SLAB) {                           // (the grid is made for every row)
+        n = p.head->count;
+        tiles_n = (n + BN - 1) / BN;
+        if (blockIdx.x >= p.tiles_m * tiles_n) return;
+    }
     if (EPI == EPI_OUT) k = p.head->count;
+    // (strips of four for the weights' gradient: 6 970 against 7 150 us, 8 192 rows x 131 072 x 4 096; of eight otherwise)
+    tile_of<EPI == EPI_OUT ? 4 : 8>(blockIdx.x, p.tiles_m, tiles_n, tm, tn);
     const uint32_t m0 = tm * BM, n0 = tn * BN;
-    if (EPI != EPI_LSE && EPI != EPI_OUT && n0 >= n) return;         // (the grid is made for every row)
     uint32_t blocks = (k + BK - 1) / BK, kfirst = 0;
     if (EPI == EPI_SLAB) {
         const uint32_t per = (blocks + p.splits - 1) / p.splits;
