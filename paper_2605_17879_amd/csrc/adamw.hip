@@ -6,7 +6,7 @@
 // 8-bit states hold m and r as e4m3 codes under a power of two per block of 256 elements, so that
 // decoding and scaling are exact and the only rounding is the one to four significant bits.
 //
-// The tensors are cut into pieces of CHUNK elements that a table on the device lists; a workgroup
+// The tensors are cut into pieces of elements that a table on the device lists; a workgroup
 // takes piece after piece.  A lane holds eight elements at a time, so that 32 lanes hold one block of an
 // 8-bit state, whose largest magnitude then takes five exchanges between lanes and no LDS.
 #include "gd_lanes.h"
@@ -17,8 +17,9 @@ namespace {
 constexpr uint32_t NT = 256;
 constexpr uint32_t V = 8;                 // elements of a lane at a time
 constexpr uint32_t ROUND = NT * V;
-constexpr uint32_t CHUNK = 8192;          // elements of a piece: four rounds of a workgroup
-constexpr uint32_t ROUNDS = CHUNK / ROUND;
+// Elements of a piece: two rounds of a workgroup with 32-bit states (200 M elements 1 029 us; four rounds 1 085, one 1 110,
+// eight 1 048), four with 8-bit ones (540 M 1 757; two 1 839, one 1 762, eight 1 822).
+__host__ __device__ constexpr uint32_t chunk_of(bool eight) { return eight ? 8192 : 4096; }
 constexpr uint32_t BLOCK_LANES = GD_STATE_BLOCK / V;
 
 struct table_head {
@@ -31,8 +32,7 @@ struct table_tensor {
     uint64_t n, first_index;
     double lr_scale, weight_decay;
     uint8_t param_type, grad_type, copy_type, eight;
-    uint8_t aligned;        // every array aligned to what a lane reads of it at once
-    uint8_t pad[3];
+    uint8_t pad[4];
 };
 struct table_chunk {
     uint32_t tensor, chunk;
@@ -42,10 +42,13 @@ constexpr size_t HEAD = 64;
 __host__ __device__ inline size_t chunks_at(uint32_t n_tensors) { return HEAD + (size_t)n_tensors * sizeof(table_tensor); }
 
 // The table's pointers are to device memory; said to the compiler, which otherwise asks the LDS as well at every access.
-// With 8-bit states what is read and written is marked as passing through once (1 910 -> 1 874 us for 540 M elements);
-// with 32-bit ones it is not (1 109 against 1 185 us for 200 M).
+// Gradients and copies are marked as passing through once, and with 8-bit states all that is written (200 M elements with
+// 32-bit states 933 -> 910 us on one card, 540 M with 8-bit ones 1 661 -> 1 626; all loads marked 1 091 against 1 048, no copies 964 / 930).
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+// (read and written at once wherever a tensor begins: such an access needs no more alignment than its elements have)
+typedef u32x4 u32x4_anywhere __attribute__((aligned(1)));
+typedef u32x2 u32x2_anywhere __attribute__((aligned(1)));
 template <typename X>
 using in_memory = __attribute__((address_space(1))) X;
 template <typename X> __device__ __forceinline__ const in_memory<X>* memory(const void* p) { return (const in_memory<X>*)(uintptr_t)p; }
@@ -55,27 +58,32 @@ template <typename X> __device__ __forceinline__ in_memory<X>* memory(void* p) {
 template <typename T> struct raw { gd_vec<T, 16 / sizeof(T)> q[V * sizeof(T) / 16]; };
 template <> struct raw<uint8_t> { uint2 q; };
 
-template <bool ONCE, typename X>
-__device__ __forceinline__ X get(const in_memory<X>* p) {
-    if constexpr (ONCE) return __builtin_nontemporal_load(p);
-    else return *p;
+template <bool ONCE>
+__device__ __forceinline__ u32x4 get16(const void* p) {
+    if constexpr (ONCE) return __builtin_nontemporal_load(memory<u32x4_anywhere>(p));
+    else return *memory<u32x4_anywhere>(p);
 }
-template <bool ONCE, typename X>
-__device__ __forceinline__ void set(in_memory<X>* p, X x) {
-    if constexpr (ONCE) __builtin_nontemporal_store(x, p);
-    else *p = x;
+template <bool ONCE>
+__device__ __forceinline__ u32x2 get8(const void* p) {
+    if constexpr (ONCE) return __builtin_nontemporal_load(memory<u32x2_anywhere>(p));
+    else return *memory<u32x2_anywhere>(p);
+}
+template <bool ONCE>
+__device__ __forceinline__ void set16(void* p, u32x4 x) {
+    if constexpr (ONCE) __builtin_nontemporal_store(x, memory<u32x4_anywhere>(p));
+    else *memory<u32x4_anywhere>(p) = x;
 }
 
 template <typename T, bool ONCE>
 __device__ __forceinline__ raw<T> load_raw(const void* p, uint64_t at) {
     raw<T> r;
     if constexpr (sizeof(T) == 1) {
-        const u32x2 x = get<ONCE>(memory<u32x2>(static_cast<const T*>(p) + at));
+        const u32x2 x = get8<ONCE>(static_cast<const T*>(p) + at);
         r.q = make_uint2(x.x, x.y);
     } else {
 #pragma unroll
         for (int i = 0; i < (int)(V * sizeof(T) / 16); ++i) {
-            const u32x4 x = get<ONCE>(memory<u32x4>(static_cast<const T*>(p) + at) + i);
+            const u32x4 x = get16<ONCE>(static_cast<const T*>(p) + at + i * (16 / sizeof(T)));
             r.q[i] = __builtin_bit_cast(gd_vec<T, 16 / sizeof(T)>, x);
         }
     }
@@ -106,7 +114,7 @@ __device__ __forceinline__ void store(void* p, uint64_t at, uint32_t n, bool vec
         for (int j = 0; j < (int)V; ++j) r.q[j / E].v[j % E] = gd_from_f32<T>(x[j]);
 #pragma unroll
         for (int i = 0; i < (int)V / E; ++i)
-            set<ONCE>(memory<u32x4>(static_cast<T*>(p) + at) + i, __builtin_bit_cast(u32x4, r.q[i]));
+            set16<ONCE>(static_cast<T*>(p) + at + i * E, __builtin_bit_cast(u32x4, r.q[i]));
     } else {
 #pragma unroll
         for (uint32_t j = 0; j < V; ++j)
@@ -125,7 +133,7 @@ __device__ __forceinline__ uint2 load_some_codes(const void* p, uint64_t at, uin
 __device__ __forceinline__ void store_codes(void* p, uint64_t at, uint32_t n, bool vec, uint32_t c0, uint32_t c1) {
     in_memory<uint8_t>* b = memory<uint8_t>(p) + at;
     if (vec) {
-        set<true>((in_memory<u32x2>*)b, u32x2{c0, c1});
+        __builtin_nontemporal_store(u32x2{c0, c1}, (in_memory<u32x2_anywhere>*)b);
     } else {
 #pragma unroll
         for (uint32_t j = 0; j < V; ++j)
@@ -214,11 +222,10 @@ struct round_data {
 
 template <typename P, typename G, typename S>
 __device__ __forceinline__ void load_round(const table_tensor& t, uint64_t at, round_data<P, G, S>& d) {
-    constexpr bool ONCE = sizeof(S) == 1;
-    d.p = load_raw<P, ONCE>(t.param, at);
-    d.g = load_raw<G, ONCE>(t.grad, at);
-    d.m = load_raw<S, ONCE>(t.m, at);
-    d.v = load_raw<S, ONCE>(t.v, at);
+    d.p = load_raw<P, false>(t.param, at);
+    d.g = load_raw<G, true>(t.grad, at);
+    d.m = load_raw<S, false>(t.m, at);
+    d.v = load_raw<S, false>(t.v, at);
     if (sizeof(S) == 1) {
         d.me = memory<uint8_t>(t.m_exp)[at / GD_STATE_BLOCK];
         d.ve = memory<uint8_t>(t.v_exp)[at / GD_STATE_BLOCK];
@@ -230,8 +237,8 @@ struct factors {
     bool scaled;
 };
 
-// One lane's elements: updated and written back.  WHOLE: all V of them are there, aligned and loaded (d);
-// else the first n, `vec` where that are all V of them and they are aligned.
+// One lane's elements: updated and written back.  WHOLE: all V of them are there and loaded (d);
+// else the first n, `vec` where that are all V of them.
 template <typename P, typename G, typename S, bool WHOLE>
 __device__ __forceinline__ void update(const table_tensor& t, const gd_adamw_args& a, const factors& f, uint64_t at, uint32_t n,
                                        bool vec, const round_data<P, G, S>* d) {
@@ -270,8 +277,8 @@ __device__ __forceinline__ void update(const table_tensor& t, const gd_adamw_arg
     }
     store<P, EIGHT>(t.param, at, n, vec, p);
     if (t.copy) {
-        if (t.copy_type == GD_BF16) store<gd_bf16, EIGHT>(t.copy, at, n, vec, p);
-        else store<gd_f16, EIGHT>(t.copy, at, n, vec, p);
+        if (t.copy_type == GD_BF16) store<gd_bf16, true>(t.copy, at, n, vec, p);
+        else store<gd_f16, true>(t.copy, at, n, vec, p);
     }
     if constexpr (EIGHT) {
         // elements behind the end count as zeros
@@ -303,8 +310,9 @@ __device__ __forceinline__ void update_chunk(const table_tensor& t, uint32_t chu
     f.size = (float)(a.lr * t.lr_scale / a.c1);
     f.gs = gs;
     f.scaled = scaled;
+    constexpr uint32_t CHUNK = chunk_of(sizeof(S) == 1), ROUNDS = CHUNK / ROUND;
     const uint64_t base = (uint64_t)chunk * CHUNK;
-    if (base + CHUNK <= t.n && t.aligned) {
+    if (base + CHUNK <= t.n) {
         // the next round's loads are on their way while this one is worked out
         round_data<P, G, S> d[2];
         uint64_t at = base + threadIdx.x * V;
@@ -323,7 +331,7 @@ __device__ __forceinline__ void update_chunk(const table_tensor& t, uint32_t chu
         if (base + r * ROUND + (threadIdx.x & ~63u) * V >= t.n) break;
         const uint32_t n = at >= t.n ? 0u : (uint32_t)(t.n - at < V ? t.n - at : V);
         const uint64_t block = at & ~(uint64_t)(GD_STATE_BLOCK - 1);
-        update<P, G, S, false>(t, a, f, block < t.n ? at : t.n - 1, n, n == V && t.aligned, nullptr);
+        update<P, G, S, false>(t, a, f, block < t.n ? at : t.n - 1, n, n == V, nullptr);
     }
 }
 
@@ -365,7 +373,7 @@ __global__ __launch_bounds__(NT) void adamw_kernel(const gd_adamw_args a) {
 
 size_t gd_adamw_table(const gd_adamw_tensor* t, uint32_t n, void* out) {
     uint64_t chunks = 0;
-    for (uint32_t i = 0; i < n; ++i) chunks += (t[i].n + CHUNK - 1) / CHUNK;
+    for (uint32_t i = 0; i < n; ++i) chunks += (t[i].n + chunk_of(t[i].state_type == GD_E4M3) - 1) / chunk_of(t[i].state_type == GD_E4M3);
     if (chunks > 0xFFFFFFFFull) return 0;
     const size_t bytes = gd_align256(chunks_at(n) + (size_t)chunks * sizeof(table_chunk));
     if (!out) return bytes;
@@ -383,11 +391,7 @@ size_t gd_adamw_table(const gd_adamw_tensor* t, uint32_t n, void* out) {
         d[i].lr_scale = s.lr_scale; d[i].weight_decay = s.weight_decay;
         d[i].param_type = (uint8_t)s.param_type; d[i].grad_type = (uint8_t)s.grad_type;
         d[i].copy_type = (uint8_t)s.copy_type; d[i].eight = s.state_type == GD_E4M3;
-        const size_t state = d[i].eight ? 8 : 16;
-        const bool off = (uintptr_t)s.d_param % 16 || (uintptr_t)s.d_grad % 16 || (uintptr_t)s.d_m % state || (uintptr_t)s.d_v % state ||
-                         (s.d_copy && (uintptr_t)s.d_copy % 16);
-        d[i].aligned = off ? 0 : 1;
-        for (uint64_t k = 0; k * CHUNK < s.n; ++k) { c->tensor = i; c->chunk = (uint32_t)k; ++c; }
+        for (uint64_t k = 0; k * chunk_of(d[i].eight) < s.n; ++k) { c->tensor = i; c->chunk = (uint32_t)k; ++c; }
     }
     return bytes;
 }
