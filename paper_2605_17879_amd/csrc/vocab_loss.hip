@@ -15,6 +15,9 @@
 // For the gradients the rows that have one are gathered first: rows left out cost nothing, and what
 // their hidden states hold (infinities, NaN) reaches no product.
 //
+// The matrix cores bound large products (8 192 x 131 072 x 4 096: logits 6.28 ms, 1 400 TFLOP/s), few rows the weights' stream (4 rows x
+// 131 072 x 4 096: 171 us, 6.3 TB/s), and what lies between them what a tile takes beside its sum.
+//
 // Tiles are staged with loads that go from memory straight to the LDS, into one of two buffers while
 // the other is multiplied.  Places in the LDS are exchanged by exclusive or within a row, so that reads
 // of eight or sixteen rows at one k fall on different banks.
