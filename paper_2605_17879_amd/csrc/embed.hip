@@ -32,6 +32,7 @@ constexpr uint32_t SELF_COUNT = 8, SELF_SCAN = 64;
 // of 1 000 bf16 added, few / sorted: 1 100 rows 9.4 / 17.2, 2 000 13.4 / 18.0; of 4 096 fp32, 8 workgroups a row: 1 100 21.8 / 20.7,
 // 2 000 33.9 / 26.6).
 constexpr uint32_t FEW = 2048, FEW_GROUPS = 8192;
+constexpr uint32_t MOST_GROUPS = 1u << 21;  // of a launch: HIP takes less than 2^32 threads in a dimension
 constexpr uint32_t BATCH = 8;             // rows on their way at once in the sums
 constexpr uint32_t FILL_ROWS = 16384;     // most rows that one of its workgroups fills with zeros
 constexpr uint32_t NO_ROW = 0xFFFFFFFFu;
@@ -72,20 +73,21 @@ __device__ __forceinline__ void write_own(T* p, const gd_vec<T, V>& q, uint32_t 
 template <typename T, int V>
 __global__ __launch_bounds__(NT) void embed_kernel(const gd_embed_args a, uint32_t log_tx) {
     const uint32_t tx = 1u << log_tx, lane = threadIdx.x & (tx - 1);
-    const uint64_t i = (uint64_t)blockIdx.x * (NT >> log_tx) + (threadIdx.x >> log_tx);
-    if (i >= a.tokens.n) return;
-    const int64_t t = gd_token(a.tokens, i);
-    T* out = static_cast<T*>(a.out) + i * a.out_stride;
-    const bool row = t >= 0 && t < (int64_t)a.vocab;
-    const T* w = static_cast<const T*>(a.weight) + (row ? (uint64_t)t : 0) * a.weight_stride;
-    const float other = t < 0 ? 0.0f : __uint_as_float(0x7FC00000u);
-    for (uint32_t c0 = (blockIdx.y * tx + lane) * V; c0 < a.width; c0 += gridDim.y * tx * V) {
-        const columns c = columns_of<V>(c0, a.width);
-        gd_vec<T, V> q;
-        if (row) q = gd_read<T, V>(w + c.at);
+    const uint32_t rows = NT >> log_tx;
+    for (uint32_t i = blockIdx.x * rows + (threadIdx.x >> log_tx); i < a.tokens.n; i += gridDim.x * rows) {
+        const int64_t t = gd_token(a.tokens, i);
+        T* out = static_cast<T*>(a.out) + i * a.out_stride;
+        const bool row = t >= 0 && t < (int64_t)a.vocab;
+        const T* w = static_cast<const T*>(a.weight) + (row ? (uint64_t)t : 0) * a.weight_stride;
+        const float other = t < 0 ? 0.0f : __uint_as_float(0x7FC00000u);
+        for (uint32_t c0 = lane * V; c0 < a.width; c0 += tx * V) {
+            const columns c = columns_of<V>(c0, a.width);
+            gd_vec<T, V> q;
+            if (row) q = gd_read<T, V>(w + c.at);
 #pragma unroll
-        for (int j = 0; j < V; ++j) q.v[j] = gd_from_f32<T>(row ? gd_to_f32(q.v[j]) * a.scale : other);
-        write_own<T, V>(out + c.at, q, c.skip);
+            for (int j = 0; j < V; ++j) q.v[j] = gd_from_f32<T>(row ? gd_to_f32(q.v[j]) * a.scale : other);
+            write_own<T, V>(out + c.at, q, c.skip);
+        }
     }
 }
 
@@ -93,8 +95,8 @@ template <typename T, int V>
 hipError_t launch_embed(const gd_embed_args& a, hipStream_t s) {
     uint32_t log_tx = 0;
     while (log_tx < 8 && (1u << log_tx) * V < a.width) ++log_tx;
-    const uint32_t rows = NT >> log_tx;
-    hipLaunchKernelGGL((embed_kernel<T, V>), dim3((a.tokens.n + rows - 1) / rows), dim3(NT), 0, s, a, log_tx);
+    const uint32_t rows = NT >> log_tx, groups = (a.tokens.n + rows - 1) / rows;
+    hipLaunchKernelGGL((embed_kernel<T, V>), dim3(groups < MOST_GROUPS ? groups : MOST_GROUPS), dim3(NT), 0, s, a, log_tx);
     return hipGetLastError();
 }
 
@@ -142,7 +144,7 @@ __device__ __forceinline__ uint64_t same_digit(uint32_t d, bool there) {
     return same;
 }
 
-// Workgroup `block` of `blocks` fills its share: of rows next to each other 16 bytes a lane and no more (512 MB: 79 us; 16 bytes
+// Workgroup `block` of `blocks` fills its share: of rows next to each other 16 bytes a lane and, below 8 GB, no more (512 MB: 79 us; 16 bytes
 // again and again by 2 048 workgroups 112 us), of rows apart every blocks-th row.
 template <typename T, int V, int THREADS>
 __device__ __forceinline__ void fill_rows(const fill_args& f, uint32_t block, uint32_t blocks) {
@@ -150,13 +152,15 @@ __device__ __forceinline__ void fill_rows(const fill_args& f, uint32_t block, ui
         T* const begin = static_cast<T*>(f.p) + (uint64_t)f.from * f.width;
         T* const end = static_cast<T*>(f.p) + (uint64_t)f.to * f.width;
         typedef gd_vec<T, 16 / sizeof(T)> line;
-        T* const p = reinterpret_cast<T*>(((uintptr_t)begin & ~(uintptr_t)15) + ((uint64_t)block * THREADS + threadIdx.x) * 16);
-        if (p >= begin && p + 16 / sizeof(T) <= end) {
-            gd_write_through(p, line{});
-        } else {
+        T* p = reinterpret_cast<T*>(((uintptr_t)begin & ~(uintptr_t)15) + ((uint64_t)block * THREADS + threadIdx.x) * 16);
+        for (; p < end; p += (uint64_t)blocks * THREADS * (16 / sizeof(T))) {
+            if (p >= begin && p + 16 / sizeof(T) <= end) {
+                gd_write_through(p, line{});
+            } else {
 #pragma unroll
-            for (uint32_t j = 0; j < 16 / sizeof(T); ++j)
-                if (p + j >= begin && p + j < end) p[j] = gd_from_f32<T>(0.0f);
+                for (uint32_t j = 0; j < 16 / sizeof(T); ++j)
+                    if (p + j >= begin && p + j < end) p[j] = gd_from_f32<T>(0.0f);
+            }
         }
     } else {
         for (uint32_t r = f.from + block; r < f.to; r += blocks)
@@ -169,7 +173,8 @@ uint32_t fillers(const fill_args& f) {
     if (f.from == f.to) return 0;
     if (f.stride != f.width) return f.to - f.from < 8192 ? f.to - f.from : 8192;
     // (one more where the first line begins before the first row)
-    return (uint32_t)(((uint64_t)(f.to - f.from) * f.width * sizeof(T) + 14) / 16 / THREADS + 1);
+    const uint64_t groups = ((uint64_t)(f.to - f.from) * f.width * sizeof(T) + 14) / 16 / THREADS + 1;
+    return (uint32_t)(groups < MOST_GROUPS ? groups : MOST_GROUPS);
 }
 
 // All passes by one workgroup of sixteen waves, the keys in its registers and, between passes, in the LDS.
@@ -697,6 +702,7 @@ hipError_t launch_few(const gd_embed_grad_args& a, hipStream_t s) {
     const uint64_t bytes = (uint64_t)a.vocab * a.width * sizeof(T), least = (a.vocab + FILL_ROWS - 1) / FILL_ROWS;
     uint64_t fill = (bytes + 16383) / 16384;
     if (fill > a.vocab) fill = a.vocab;
+    if (fill > MOST_GROUPS) fill = MOST_GROUPS;
     if (fill < least) fill = least;
     hipLaunchKernelGGL((grad_few<T, V, false, ROUNDS>), dim3(sums + (uint32_t)fill), dim3(NT), 0, s, a, across, log_sub, log_tx);
     return hipGetLastError();

@@ -1303,8 +1303,8 @@ hipError_t forward(const gd_vocab_loss_args& a, hipStream_t s) {
     p.target_logit = reinterpret_cast<float*>(a.work + l.target_logit);
     p.part = reinterpret_cast<float2*>(a.work + l.part);
     p.parts = l.parts;
-    // (a launch has no more than 2^28 tiles)
-    const uint64_t most = ((1ull << 28) / (up_to(n, 128) / 128)) * 128, want = plain ? a.vocab : l.pack_piece;
+    // (a launch has no more than 2^23 tiles: HIP takes less than 2^32 threads in a dimension)
+    const uint64_t most = ((1ull << 23) / (up_to(n, 128) / 128)) * 128, want = plain ? a.vocab : l.pack_piece;
     const uint32_t piece = (uint32_t)(want < most ? want : most);
     uint32_t parts = 0;
     for (uint32_t v0 = 0; v0 < a.vocab; v0 += piece) {
