@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 from dataclasses import dataclass, field
 from typing import Optional, Sequence
 
@@ -199,6 +200,11 @@ class Config:
         return c
 
 
+_PACK_MATRIX = struct.Struct("=QQQQII").pack            # gd_matrix
+_PACK_ADAMW = struct.Struct("=IIddddQ").pack            # gd_adamw_config
+_ADAMW_BYTES = ctypes.sizeof(_CAdamwConfig)
+
+
 def _p(t) -> Optional[int]:
     return None if t is None else t.data_ptr()
 
@@ -220,6 +226,14 @@ class Detector:
         self.device = torch.device(device)
         self._raw_stream = torch._C._cuda_getCurrentRawStream
         self._index = self.device.index
+        self._f32 = torch.float32
+        # the operators' entry points as their methods call them: structures come as packed bytes
+        vp, f32, sz = ctypes.c_void_p, ctypes.c_float, ctypes.c_size_t
+        self._embed = self._entry("gd_embed", vp, vp, vp, f32, vp, vp)
+        self._embed_grad = self._entry("gd_embed_grad", vp, vp, vp, f32, ctypes.c_int32, vp, vp, sz, vp)
+        self._vocab_loss = self._entry("gd_vocab_loss", vp, vp, vp, vp, f32, vp, vp, vp, vp, sz, vp)
+        self._vocab_loss_grad = self._entry("gd_vocab_loss_grad", vp, vp, vp, vp, f32, *[vp] * 7, sz, vp)
+        self._adamw = self._entry("gd_adamw", vp, vp, sz, vp, vp, vp)
         self._types = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16, torch.int32: I32, torch.int64: I64}
         self.R, self.M = cfg.n_ranks, cfg.n_metrics
         self.N = self.R // cfg.gpus_per_node
@@ -238,6 +252,11 @@ class Detector:
             self.close()
         except Exception:
             pass
+
+    def _entry(self, name: str, *types):
+        f = self.lib[name]                              # (a function object of its own)
+        f.argtypes, f.restype = types, ctypes.c_int
+        return f
 
     def _check(self, st: int):
         if st != GD_OK:
@@ -432,45 +451,43 @@ class Detector:
             raise GuardError(4, f"tensors of {t.dtype} are not built")
         return code
 
-    def _on_device(self, *tensors):
-        for t in tensors:
-            assert t is None or (t.is_cuda and (self._index is None or t.get_device() == self._index)), \
-                f"a tensor is on {t.device}, the detector on {self.device}"
+    def _at(self, t) -> int:
+        """The address of a tensor on the detector's device."""
+        at = t.get_device()
+        if at != self._index and (self._index is not None or at < 0):
+            raise AssertionError(f"a tensor is on {t.device}, the detector on {self.device}")
+        return t.data_ptr()
 
-    def _matrix(self, t) -> _CMatrix:
-        """t[rows][cols], rows any distance apart; a list t[n] is a matrix of one column."""
+    def _matrix(self, t) -> bytes:
+        """t[rows][cols], rows any distance apart, as a gd_matrix; a list t[n] is a matrix of one column."""
+        # (a short call's time is its marshalling: a packed gd_matrix takes a third of a ctypes structure's time)
         shape, strides = t.shape, t.stride()
-        rows = shape[0]
         if len(shape) == 2:
-            cols = shape[1]
+            rows, cols = shape
             assert cols <= 1 or strides[1] == 1, "the elements of a row must be next to each other"
         else:
             assert len(shape) == 1, "a matrix or a list"
-            cols = 1
-        # (a short call's time is its marshalling: no helper is called for what is looked at here)
-        assert t.is_cuda and (self._index is None or t.get_device() == self._index), \
-            f"a tensor is on {t.device}, the detector on {self.device}"
+            rows, cols = shape[0], 1
         code = self._types.get(t.dtype)
         if code is None:
             raise GuardError(4, f"tensors of {t.dtype} are not built")
         # the distance to a row that is not there says nothing
-        return _CMatrix(t.data_ptr(), rows, cols, strides[0] if rows > 1 else cols or 1, code, 0)
+        return _PACK_MATRIX(self._at(t), rows, cols, strides[0] if rows > 1 else cols or 1, code, 0)
 
     def _vector(self, t, n: int):
         """The address of n f32 values next to each other, or None."""
         if t is None:
             return None
-        self._on_device(t)
-        assert t.dtype == self._torch.float32 and t.is_contiguous() and t.numel() == n
-        return t.data_ptr()
+        assert t.dtype is self._f32 and t.numel() == n and t.is_contiguous()
+        return self._at(t)
 
     def _bytes(self, n: int):
         return self._torch.empty(n, dtype=self._torch.uint8, device=self.device)
 
     def embed(self, weight, tokens, out, scale: float = 1.0, stream=None):
         """out[i] = scale * weight[tokens[i]]; zeros for a negative token."""
-        w, t, o = self._matrix(weight), self._matrix(tokens), self._matrix(out)
-        self._check(self.lib.gd_embed(self.h, w, t, scale, o, self._stream(stream)))
+        m = self._matrix
+        self._check(self._embed(self.h, m(weight), m(tokens), scale, m(out), self._stream(stream)))
 
     def embed_grad_work_bytes(self, n: int, vocab: int, width: int) -> int:
         return int(self.lib.gd_embed_grad_work_bytes(n, vocab, width))
@@ -481,10 +498,9 @@ class Detector:
     def embed_grad(self, out_grad, tokens, weight_grad, work, scale: float = 1.0, accumulate: bool = False,
                    stream=None):
         """weight_grad[v] = (its old value, with accumulate) + scale * sum of out_grad[i] over tokens[i] == v."""
-        g, t, w = self._matrix(out_grad), self._matrix(tokens), self._matrix(weight_grad)
-        self._on_device(work)
-        self._check(self.lib.gd_embed_grad(self.h, g, t, scale, int(accumulate), w, work.data_ptr(),
-                                           work.numel() * work.element_size(), self._stream(stream)))
+        m = self._matrix
+        self._check(self._embed_grad(self.h, m(out_grad), m(tokens), scale, accumulate, m(weight_grad),
+                                     self._at(work), work.nbytes, self._stream(stream)))
 
     def alloc_vocab_loss(self, n: int) -> dict:
         """Outputs of vocab_loss: loss[n], lse[n] and mean[2] (the mean and the rows in it)."""
@@ -500,25 +516,20 @@ class Detector:
 
     def vocab_loss(self, hidden, weight, targets, out: dict, work, logit_scale: float = 1.0, stream=None):
         """Cross entropy of softmax(logit_scale * hidden weight^T) against targets (negative: left out)."""
-        h, w, t = self._matrix(hidden), self._matrix(weight), self._matrix(targets)
-        n = targets.shape[0]
-        self._on_device(work)
-        self._check(self.lib.gd_vocab_loss(
-            self.h, h, w, t, logit_scale, self._vector(out["loss"], n), self._vector(out["lse"], n),
-            self._vector(out["mean"], 2), work.data_ptr(), work.numel() * work.element_size(), self._stream(stream)))
+        m, v, n = self._matrix, self._vector, targets.shape[0]
+        self._check(self._vocab_loss(
+            self.h, m(hidden), m(weight), m(targets), logit_scale, v(out["loss"], n), v(out["lse"], n), v(out["mean"], 2),
+            self._at(work), work.nbytes, self._stream(stream)))
 
     def vocab_loss_grad(self, hidden, weight, targets, out: dict, grad: dict, work, grad_mean=None, grad_rows=None,
                         logit_scale: float = 1.0, stream=None):
         """Gradients grad["hidden"] and grad["weight"] (either may be missing) of
         sum(grad_rows * loss) + grad_mean * mean, behind vocab_loss on the same inputs."""
-        h, w, t = self._matrix(hidden), self._matrix(weight), self._matrix(targets)
-        n = targets.shape[0]
+        m, v, n = self._matrix, self._vector, targets.shape[0]
         gh, gw = grad.get("hidden"), grad.get("weight")
-        self._on_device(work)
-        self._check(self.lib.gd_vocab_loss_grad(
-            self.h, h, w, t, logit_scale, self._vector(out["lse"], n), self._vector(out["mean"], 2),
-            self._vector(grad_mean, 1), self._vector(grad_rows, n), None if gh is None else self._matrix(gh),
-            None if gw is None else self._matrix(gw), work.data_ptr(), work.numel() * work.element_size(),
+        self._check(self._vocab_loss_grad(
+            self.h, m(hidden), m(weight), m(targets), logit_scale, v(out["lse"], n), v(out["mean"], 2), v(grad_mean, 1),
+            v(grad_rows, n), None if gh is None else m(gh), None if gw is None else m(gw), self._at(work), work.nbytes,
             self._stream(stream)))
 
     def alloc_adamw_state(self, params, bits: int = 32) -> dict:
@@ -546,7 +557,9 @@ class Detector:
         rows = (_CAdamwTensor * max(n, 1))()
         for row, p, g, m, v, c, decay, rate, first, me, ve in zip(rows, *lists):
             k = p.numel()
-            self._on_device(p, g, m, v, c, me, ve)
+            for x in (p, g, m, v, c, me, ve):
+                if x is not None:
+                    self._at(x)
             assert all(t is None or (t.is_contiguous() and t.numel() == k) for t in (p, g, m, v, c))
             assert all(t is None or (t.is_contiguous() and t.dtype == torch.uint8 and
                                      t.numel() == -(-k // STATE_BLOCK)) for t in (me, ve))
@@ -569,8 +582,7 @@ class Detector:
         """One update (step counts from 1) of every tensor of the table, in place.  grad_scale: a
         device scalar that multiplies the gradients; where it is not finite nothing is written.
         seed: of the 8-bit states' rounding, the step unless it is given."""
-        c = _CAdamwConfig(ctypes.sizeof(_CAdamwConfig), (step if seed is None else seed) & 0xFFFFFFFF, lr, beta1,
-                          beta2, eps, step)
+        # (a step below 1 is refused as 0)
+        c = _PACK_ADAMW(_ADAMW_BYTES, (step if seed is None else seed) & 0xFFFFFFFF, lr, beta1, beta2, eps, max(step, 0))
         b = table["bytes"]
-        self._check(self.lib.gd_adamw(self.h, b.data_ptr(), b.numel(), c, self._vector(grad_scale, 1),
-                                      self._stream(stream)))
+        self._check(self._adamw(self.h, b.data_ptr(), b.nbytes, c, self._vector(grad_scale, 1), self._stream(stream)))
