@@ -12,6 +12,8 @@
 //   G         the same tile again, with lse known: one piece of G in the type of H
 //   dH        m = width, n = rows, k = the piece's vocabulary: fp32 sums, the pieces added up
 //   dW        m = width, n = the piece's vocabulary, k = rows: written as the piece's rows
+// Up to FOLD rows fill half a block of k of dW, which takes two halves all the same: the second one holds the rows once more, against
+// what the rounding of G has dropped, so that dW of few rows is not rounded twice.
 // For the gradients the rows that have one are gathered first: rows left out cost nothing, and what
 // their hidden states hold (infinities, NaN) reaches no product.
 //
@@ -30,6 +32,7 @@ namespace {
 
 constexpr uint32_t BK = 64;                       // elements of k staged at a time
 constexpr float LOG2E = 1.44269504088896340736f, LN2 = 0.69314718055994530942f;
+constexpr uint32_t FOLD = BK / 2;                 // most rows whose G is held in two numbers
 constexpr uint64_t PIECE = 1ull << 28;            // the most elements of a piece of G
 constexpr uint64_t PACK = 1ull << 27;             // the most elements of a packed piece of W
 
@@ -82,6 +85,7 @@ struct product_args {
     const float* row_lse2;          // G: per gathered row, in units of log 2
     const float* row_coef;
     const int32_t* row_target;
+    uint32_t fold;                  // G: row FOLD + i is what rounding drops of row i
     // outputs
     void* c;  uint64_t ldc;         // G, slabs, dW
     uint64_t slab;                  // elements between two slabs of dH
@@ -502,6 +506,9 @@ __device__ __forceinline__ g_row g_row_of(const product_args& p, uint32_t i, boo
     return g_row{p.row_lse2[i] - 64.0f, coef, coef * 5.421010862427522e-20f, p.row_target[i] - (int32_t)p.v0};
 }
 
+// The row whose place i is.
+__device__ __forceinline__ uint32_t folded(const product_args& p, uint32_t i) { return p.fold && i >= FOLD && i < 2 * FOLD ? i - FOLD : i; }
+
 // Column j of a wave's tile of logits to G.  The exponential's instruction drops subnormal results: it is taken 2^64
 // times as large, and the coefficient as much smaller.
 template <int FM, int FN>
@@ -530,6 +537,19 @@ template <typename T>
 __device__ __forceinline__ gd_vec<T, 4> four_of(const f32x4& x) {
     typedef T x4 __attribute__((ext_vector_type(4)));
     return __builtin_bit_cast(gd_vec<T, 4>, __builtin_convertvector(x, x4));
+}
+
+// What that drops; nothing where the result is no number.
+template <typename T>
+__device__ __forceinline__ f32x4 dropped_by(const f32x4& x) {
+    const gd_vec<T, 4> q = four_of<T>(x);
+    f32x4 d;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+        d[r] = x[r] - gd_to_f32(q.v[r]);
+        d[r] = d[r] == d[r] ? d[r] : 0.0f;
+    }
+    return d;
 }
 
 template <typename T, typename TILE, int EPI>
@@ -564,7 +584,7 @@ __global__ __launch_bounds__(TILE::NT, 512 / TILE::NT) void product_kernel(const
     row_data mine{};
     if ((EPI == EPI_LSE || EPI == EPI_G) && threadIdx.x < BN) {
         const uint32_t i = n0 + threadIdx.x;
-        if constexpr (EPI == EPI_G) mine = g_row_of(p, i, i < n);
+        if constexpr (EPI == EPI_G) mine = g_row_of(p, folded(p, i), folded(p, i) < n);
         else mine = target_from(p, i, n);
     }
     // operands that lie along k end where their rows do
@@ -613,6 +633,9 @@ __global__ __launch_bounds__(TILE::NT, 512 / TILE::NT) void product_kernel(const
 #pragma unroll
         for (int j = 0; j < FN; ++j) {
             tile_g<FM, FN>(p, acc, j, row, row_of[col[j] - n0]);
+            if (p.fold && n0 + TILE::col_of(wn, j) >= FOLD)
+#pragma unroll
+                for (int f = 0; f < FM; ++f) acc[f][j] = dropped_by<T>(acc[f][j]);
 #pragma unroll
             for (int f = 0; f < FM; ++f) put(f, four_of<T>(acc[f][j]));
             // (there is room for whole tiles of rows)
@@ -796,12 +819,16 @@ __global__ __launch_bounds__(256) void few_rows_kernel(const product_args p) {
             for (int f = 0; f < FM; ++f)
                 *reinterpret_cast<gd_vec<T, 4>*>(static_cast<T*>(p.c) + (uint64_t)i * p.ldc + rows[f]) = four_of<T>(acc[f][j]);
         }
-        // (the weights' gradient takes the rows in blocks of 64)
+        // (the weights' gradient takes the rows in blocks of 64: what rounding drops, and zeros between)
+        constexpr int HALF = FOLD / 16;
 #pragma unroll
-        for (int j = FN; j < (int)BK / 16; ++j)
+        for (int j = FN; j < 2 * HALF; ++j)
 #pragma unroll
-            for (int f = 0; f < FM; ++f)
-                *reinterpret_cast<gd_vec<T, 4>*>(static_cast<T*>(p.c) + (uint64_t)(j * 16 + (lane & 15)) * p.ldc + rows[f]) = gd_vec<T, 4>{};
+            for (int f = 0; f < FM; ++f) {
+                const bool rest = FN <= HALF && j >= HALF && j - HALF < FN;
+                const gd_vec<T, 4> q = rest ? four_of<T>(dropped_by<T>(acc[f][rest ? j - HALF : 0])) : gd_vec<T, 4>{};
+                *reinterpret_cast<gd_vec<T, 4>*>(static_cast<T*>(p.c) + (uint64_t)(j * 16 + (lane & 15)) * p.ldc + rows[f]) = q;
+            }
     }
 }
 
@@ -811,15 +838,16 @@ __global__ __launch_bounds__(256) void few_rows_kernel(const product_args p) {
 // and, behind a list, up to the next 256 rows.
 template <typename T>
 __global__ __launch_bounds__(256) void pack_kernel(const void* in, uint64_t stride, uint32_t width, const grad_head* head,
-                                                   const uint32_t* rows, uint32_t n, T* out, uint32_t ldo) {
+                                                   const uint32_t* rows, uint32_t n, T* out, uint32_t ldo, bool fold) {
     if (head) n = head->count;
     const uint32_t last = head ? (n + 255) / 256 * 256 : n, chunks = ldo / 8;
     const uint64_t total = (uint64_t)last * chunks;
     for (uint64_t x = (uint64_t)blockIdx.x * 256 + threadIdx.x; x < total; x += (uint64_t)gridDim.x * 256) {
         const uint32_t r = (uint32_t)(x / chunks), c = (uint32_t)(x - (uint64_t)r * chunks) * 8;
+        const uint32_t at = fold && r >= FOLD && r < 2 * FOLD ? r - FOLD : r;
         gd_vec<T, 8> q{};
-        if (r < n) {
-            const uint64_t row = rows ? rows[r] : r;
+        if (at < n) {
+            const uint64_t row = rows ? rows[at] : at;
             if (c < width) q = __builtin_bit_cast(gd_vec<T, 8>, last_at(static_cast<const T*>(in) + row * stride, (int32_t)c, (int32_t)width, width >= 8));
         }
         *reinterpret_cast<gd_vec<T, 8>*>(out + (uint64_t)r * ldo + c) = q;
@@ -1294,7 +1322,7 @@ hipError_t forward(const gd_vocab_loss_args& a, hipStream_t s) {
     p.b = operand{a.hidden, a.hidden_stride, n, a.width};
     if (!few && !direct(a.hidden, a.hidden_stride, a.width)) {
         hipLaunchKernelGGL((pack_kernel<T>), dim3(blocks_for((uint64_t)n * ldh / 8)), dim3(256), 0, s, a.hidden, a.hidden_stride, a.width,
-                           (const grad_head*)nullptr, (const uint32_t*)nullptr, n, hidden, ldh);
+                           (const grad_head*)nullptr, (const uint32_t*)nullptr, n, hidden, ldh, false);
         p.b = operand{hidden, ldh, n, ldh};
     }
     const bool plain = few || direct(a.weight, a.weight_stride, a.width);
@@ -1314,7 +1342,7 @@ hipError_t forward(const gd_vocab_loss_args& a, hipStream_t s) {
             p.a = operand{w, a.weight_stride, here, a.width};
         } else {
             hipLaunchKernelGGL((pack_kernel<T>), dim3(blocks_for((uint64_t)here * ldh / 8)), dim3(256), 0, s, w, a.weight_stride, a.width,
-                               (const grad_head*)nullptr, (const uint32_t*)nullptr, here, weight, ldh);
+                               (const grad_head*)nullptr, (const uint32_t*)nullptr, here, weight, ldh, false);
             p.a = operand{weight, ldh, here, ldh};
         }
         p.m = here; p.v0 = v0; p.part0 = parts;
@@ -1356,7 +1384,7 @@ hipError_t backward(const gd_vocab_grad_args& a, hipStream_t s) {
     if (n <= 1024) hipLaunchKernelGGL((prepare_rows<1>), dim3(1), dim3(1024), 0, s, r);
     else hipLaunchKernelGGL((prepare_rows<8>), dim3(1), dim3(1024), 0, s, r);
     hipLaunchKernelGGL((pack_kernel<T>), dim3(blocks_for((uint64_t)padded * ldh / 8)), dim3(256), 0, s, a.hidden, a.hidden_stride, a.width,
-                       head, r.rows, n, hidden, ldh);
+                       head, r.rows, n, hidden, ldh, n <= FOLD);
     const bool plain = direct(a.weight, a.weight_stride, a.width);
     uint32_t piece = (uint32_t)l.piece;
     if (!plain && piece > l.pack_piece) piece = (uint32_t)l.pack_piece;
@@ -1367,7 +1395,7 @@ hipError_t backward(const gd_vocab_grad_args& a, hipStream_t s) {
         operand wo{w, a.weight_stride, here, a.width};
         if (!plain && (a.hidden_grad || !few)) {
             hipLaunchKernelGGL((pack_kernel<T>), dim3(blocks_for((uint64_t)here * ldh / 8)), dim3(256), 0, s, w, a.weight_stride, a.width,
-                               (const grad_head*)nullptr, (const uint32_t*)nullptr, here, weight, ldh);
+                               (const grad_head*)nullptr, (const uint32_t*)nullptr, here, weight, ldh, false);
             wo = operand{weight, ldh, here, ldh};
         }
         const operand go{g, piece, padded, piece};
@@ -1378,7 +1406,7 @@ hipError_t backward(const gd_vocab_grad_args& a, hipStream_t s) {
         p.m = here; p.n = n; p.k = few ? a.width : (uint32_t)up_to(a.width, 8);
         p.scale2 = a.scale * LOG2E; p.v0 = v0; p.vocab = a.vocab;
         p.row_lse2 = r.row_lse2; p.row_coef = r.row_coef; p.row_target = r.row_target;
-        p.c = g; p.ldc = piece;
+        p.c = g; p.ldc = piece; p.fold = n <= FOLD;
         launch_logits<T, EPI_G>(p, few, s);
         const uint32_t padded_here = (uint32_t)up_to(here, BK);      // (the tiles of G have written so far at least)
         if (a.hidden_grad) {

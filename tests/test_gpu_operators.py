@@ -360,6 +360,31 @@ def test_weights_gradient_with_words_that_are_switched_off(det, n, vocab):
     assert bool((g["weight"][-1] == 0).all())
 
 
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("n,vocab,width,padding", [(1, 300, 72, 0.0), (2, 3001, 136, 0.0), (16, 1057, 200, 0.2), (17, 1025, 64, 0.0), (32, 66001, 40, 0.1),
+                                                   (9, 70003, 72, 0.0)])
+def test_weights_gradient_of_few_rows_is_rounded_once(det, dtype, n, vocab, width, padding):
+    """Up to 32 rows: G is held in two numbers, whose sum is off by the square of a rounding (and in f16 by half of the least
+    number, in units of 2^-14 of the largest coefficient's power of two), so that the gradient's own rounding is all that counts."""
+    h, w = randn((n, width), n + width, dtype), randn((vocab, width), n + vocab, dtype, 2 / width ** 0.5)
+    t = refs.tokens(n, vocab, n, padding)
+    ref = refs.Loss(h, w, t, grad_mean=1.0)
+    out = run_loss(det, h, w, t, grad_mean=1.0)
+    keep = t >= 0
+    logits = h.double() @ w.double().T
+    p = torch.exp(logits - ref.lse[:, None])
+    c = keep.double()[:, None] / max(1, ref.count)
+    expo = ref.logit_err + ref.lse_bound[:, None] + 4 * refs.U32 * (logits.abs() + ref.lse.abs()[:, None])
+    g = p.clone()
+    g[torch.arange(n)[keep], t[keep].long()] -= 1.0
+    g_err = c * (p * (torch.expm1(expo) + 4 * refs.U32) + (refs.u(dtype) ** 2 + 6 * refs.U32) * g.abs() * (1 + expo))
+    if dtype == F16:
+        g_err = g_err + c.max() * 2.0 ** -25 * 2.0 ** -13
+    e = g_err.T @ h.double().abs() + 66 * refs.U32 * ((c * g).abs() + g_err).T @ h.double().abs()
+    low = torch.finfo(dtype).smallest_normal * refs.u(dtype) * 2
+    within(out["weight_grad"], ref.weight_grad, e + refs.u(dtype) * (ref.weight_grad.abs() + e) + low, "gradient of the weights")
+
+
 def test_strided_targets_and_gradients(det):
     n, V, d = 150, 700, 72
     h, w = randn((n, d), 1, BF16), randn((V, d), 2, BF16, 0.3)
