@@ -27,14 +27,14 @@
 
 #include "gd_lanes.h"
 #include "gd_operators.h"
+#include "gd_vocab_plan.h"
 
 namespace {
 
-constexpr uint32_t BK = 64;                       // elements of k staged at a time
+using namespace vocab_plan;
+
 constexpr float LOG2E = 1.44269504088896340736f, LN2 = 0.69314718055994530942f;
 constexpr uint32_t FOLD = BK / 2;                 // most rows whose G is held in two numbers
-constexpr uint64_t PIECE = 1ull << 28;            // the most elements of a piece of G
-constexpr uint64_t PACK = 1ull << 27;             // the most elements of a packed piece of W
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef gd_bf16 bf16x8 __attribute__((ext_vector_type(8)));
@@ -71,13 +71,13 @@ struct grad_head {
 
 struct product_args {
     operand a, b;
-    uint32_t m, n, k;               // sizes; k is rounded up to BK by the staging
+    uint32_t m, n, k;               // sizes; k is rounded up to BK by the staging; m: the launch's words, for logits
     uint32_t tiles_m, tiles_n;
     const grad_head* head;          // or null: n (or k) is as given
     // forward and G
     float scale2;                   // s * log2(e)
     float scale;
-    uint32_t v0, vocab;             // the piece's first row of W; rows of W
+    uint32_t v0;                    // the launch's first row of W
     gd_token_list targets;          // forward
     float* target_logit;            // [n]
     float2* part;                   // [n][parts]
@@ -434,21 +434,22 @@ __device__ __forceinline__ float2 join_sums(float2 a, float2 b) {
 // Target i as it is seen from the launch's first word on; -1 where it has none there.
 __device__ __forceinline__ int32_t target_from(const product_args& p, uint32_t i, uint32_t n) {
     const int64_t t = i < n ? gd_token(p.targets, i) : -1;
-    return t >= (int64_t)p.v0 && t < (int64_t)p.vocab ? (int32_t)(t - p.v0) : -1;
+    return t >= (int64_t)p.v0 && t - (int64_t)p.v0 < (int64_t)p.m ? (int32_t)(t - p.v0) : -1;
 }
 
-// How many of the launch's words lie below the vocabulary's end from `first` on, the same number each time.  (Comparisons
+// How many of the launch's words there are from `first` on, the same number each time: tiles may reach behind them, where the
+// last one is staged again, and another launch's words may follow.  (Comparisons
 // with it stay in the branches that need them.  Worked out once for all columns they fill the scalar registers: a tile of
 // 256 x 256 spent 6.7 us behind its sum, with a wait for each column's targets, where it spends 3.5 now.)
 __device__ __forceinline__ int32_t words_left(const product_args& p, uint32_t first) {
-    int32_t left = (int32_t)(p.vocab - p.v0) - (int32_t)first;
+    int32_t left = (int32_t)p.m - (int32_t)first;
     asm volatile("" : "+v"(left));
     return left;
 }
 
 // Column j of a wave's tile, row i, over all of its words (words[f] + 0..3), the same in the four lanes that share the
 // column.  `target` as from target_from.  What few tiles need stands behind branches that all lanes take alike:
-// words behind the vocabulary's end, and the target's logit, which is written where it is met.
+// words behind the launch's last, and the target's logit, which is written where it is met.
 template <int FM, int FN>
 __device__ __forceinline__ float2 tile_sums(const product_args& p, f32x4 (&acc)[FM][FN], int j, const uint32_t (&words)[FM], uint32_t i,
                                             int32_t target, uint32_t lane) {
@@ -1134,60 +1135,6 @@ __global__ __launch_bounds__(256) void zero_rows(T* out, uint64_t ldo, uint32_t 
 
 // ---- host side ----------------------------------------------------------------------------
 
-uint64_t up_to(uint64_t v, uint64_t unit) { return (v + unit - 1) / unit * unit; }
-
-// Which tiles.  Large ones move half as much per product but come one to a CU, small ones two, and a launch ends with
-// its last round: what a choice costs is rounds x (blocks of k + what a tile takes before and behind them) x the
-// time of a block of all CUs at once (measured with long k: 1.5 us for 256 large tiles, 1.1 for 512 small ones).
-constexpr uint64_t CUS = 256;
-constexpr double LARGE_BLOCK = 1.5, SMALL_BLOCK = 1.1, AROUND = 7.0;
-double large_cost(uint64_t tiles, double blocks) { return (double)((tiles + CUS - 1) / CUS) * (blocks + AROUND) * LARGE_BLOCK; }
-double small_cost(uint64_t tiles, double blocks) { return (double)((tiles + 2 * CUS - 1) / (2 * CUS)) * (blocks + AROUND) * SMALL_BLOCK; }
-
-// How many of `cols` go to large tiles where `rows` stand against them (a multiple of 256, or all of them): full rounds of
-// large tiles, the rest in small ones, or one kind alone.
-uint64_t large_part(uint64_t cols, uint64_t rows, uint64_t k) {
-    const double blocks = (double)up_to(k, BK) / BK;
-    const uint64_t across = up_to(rows, 256) / 256, all = up_to(cols, 256) / 256, small = up_to(rows, 128) / 128;
-    uint64_t best = 0;
-    double least = small_cost(small * (up_to(cols, 128) / 128), blocks);
-    const double whole = large_cost(across * all, blocks);
-    if (whole < least) { least = whole; best = cols; }
-    const uint64_t full = across * all / CUS * CUS / across;     // tiles across `cols` in full rounds
-    if (full > 0 && full < all) {
-        const double both = large_cost(across * full, blocks) + small_cost(small * (up_to(cols - full * 256, 128) / 128), blocks) + 3.0;
-        if (both < least) best = full * 256;
-    }
-    return best;
-}
-
-// The product with a long k and few tiles: parts of k, a slab of sums each, that the CUs have work alike.
-struct split_plan {
-    bool large;
-    uint32_t splits;
-};
-split_plan split_for(uint64_t m, uint64_t n, uint64_t k) {
-    const uint64_t blocks = up_to(k, BK) / BK;
-    const uint64_t large = up_to(m, 256) / 256 * (up_to(n, 256) / 256), small = up_to(m, 128) / 128 * (up_to(n, 128) / 128);
-    split_plan best{false, 1};
-    double least = 1e30;
-    for (uint32_t s = 1; s <= 64; ++s) {
-        const double per = (double)((blocks + s - 1) / s);
-        if (s > 1 && per < 8) break;
-        const double sums = s * (double)m * (double)n * 8 / 4.9e6;       // a slab written and read
-        const double l = large_cost(large * s, per) + sums, t = small_cost(small * s, per) + sums;
-        if (l < least) { least = l; best = split_plan{true, s}; }
-        if (t < least) { least = t; best = split_plan{false, s}; }
-    }
-    return best;
-}
-
-// Where rows and words make too few tiles for the chip, the waves' blocks of k in turn win: while tiles of 64 rows and
-// 128 words are at most half as many as CUs (us, tiles of 128 x 128 / in turn, width 2 048: 128 rows x 8 000 words
-// 37.9 / 33.4, x 16 000 43.1 / 58.2, 256 x 4 000 31.8 / 32.8, 512 x 2 000 32.1 / 32.6; width 4 096: 64 x 16 384
-// 70.4 / 58.6, 4 x 32 768 77.1 / 76.1).
-bool few_tiles(uint64_t n, uint64_t vocab) { return up_to(n, 64) / 64 * (up_to(vocab, 128) / 128) <= CUS / 2; }
-
 struct loss_layout {
     // forward and both
     size_t target_logit, part, hidden, weight;
@@ -1269,26 +1216,24 @@ uint32_t launch_logits(const product_args& p, bool few, hipStream_t s) {
         if (p.n <= 16) launch_few<T, 1, EPI>(p, s);
         else if (p.n <= 32) launch_few<T, 2, EPI>(p, s);
         else launch_few<T, 4, EPI>(p, s);
-        return (p.m + 31) / 32;
+        return parts_of_words(p.m, p.n, p.k, true);
     }
     const uint32_t large = (uint32_t)large_part(p.m, p.n, p.k);
-    uint32_t parts = 0;
+    const uint32_t large_parts = (large + 255) / 256;
     if (large > 0) {
         product_args q = p;
         q.m = large;
         launch_tiles<T, large_tile<T, true, true>, EPI>(q, s);
-        parts = (large + 255) / 256;
     }
     if (large < p.m) {
         product_args q = p;
-        q.m -= large; q.v0 += large; q.part0 += parts;
+        q.m -= large; q.v0 += large; q.part0 += large_parts;
         q.a.p = static_cast<const T*>(p.a.p) + (uint64_t)large * p.a.stride;
         q.a.rows -= large;
         q.c = static_cast<T*>(p.c) + large;
         launch_tiles<T, small_tile<T, true, true>, EPI>(q, s);
-        parts += (q.m + 127) / 128;
     }
-    return parts;
+    return parts_of_words(p.m, p.n, p.k, false);
 }
 
 // The rows of the weights' gradient for a piece.
@@ -1327,13 +1272,11 @@ hipError_t forward(const gd_vocab_loss_args& a, hipStream_t s) {
     }
     const bool plain = few || direct(a.weight, a.weight_stride, a.width);
     p.k = few ? a.width : (uint32_t)up_to(a.width, 8);           // (rows of a copy go on with zeros)
-    p.n = n; p.scale = a.scale; p.scale2 = a.scale * LOG2E; p.vocab = a.vocab; p.targets = a.targets;
+    p.n = n; p.scale = a.scale; p.scale2 = a.scale * LOG2E; p.targets = a.targets;
     p.target_logit = reinterpret_cast<float*>(a.work + l.target_logit);
     p.part = reinterpret_cast<float2*>(a.work + l.part);
     p.parts = l.parts;
-    // (a launch has no more than 2^23 tiles: HIP takes less than 2^32 threads in a dimension)
-    const uint64_t most = ((1ull << 23) / (up_to(n, 128) / 128)) * 128, want = plain ? a.vocab : l.pack_piece;
-    const uint32_t piece = (uint32_t)(want < most ? want : most);
+    const uint32_t piece = words_at_once(n, a.vocab, plain ? a.vocab : l.pack_piece);
     uint32_t parts = 0;
     for (uint32_t v0 = 0; v0 < a.vocab; v0 += piece) {
         const uint32_t here = a.vocab - v0 < piece ? a.vocab - v0 : piece;
@@ -1404,7 +1347,7 @@ hipError_t backward(const gd_vocab_grad_args& a, hipStream_t s) {
         p.a = wo;
         p.b = operand{hidden, ldh, padded, ldh};
         p.m = here; p.n = n; p.k = few ? a.width : (uint32_t)up_to(a.width, 8);
-        p.scale2 = a.scale * LOG2E; p.v0 = v0; p.vocab = a.vocab;
+        p.scale2 = a.scale * LOG2E; p.v0 = v0;
         p.row_lse2 = r.row_lse2; p.row_coef = r.row_coef; p.row_target = r.row_target;
         p.c = g; p.ldc = piece; p.fold = n <= FOLD;
         launch_logits<T, EPI_G>(p, few, s);
