@@ -93,10 +93,11 @@ class SweepStep:
         for t in (self.master, self.weight, self.hidden, self.grad["hidden"], self.grad["weight"],
                   *self.out.values(), *(x for v in self.state.values() for x in v)):
             b = t.contiguous().view(torch.uint8).view(-1)
-            words = b[:b.numel() // 4 * 4].view(torch.int32).long() & 0xFFFFFFFF
-            place = torch.arange(1, words.numel() + 1, device=words.device) & 0xFFFF
-            tail = b[b.numel() // 4 * 4:].long().sum()
-            total = (total * 1000003 + int((words * place).sum()) + int(tail)) & 0xFFFFFFFFFFFFFFFF
+            b = torch.cat([b, b.new_zeros(-b.numel() % 4)])
+            words = b.view(torch.int32).long() & 0xFFFFFFFF
+            # (odd factors: no word that changes alone leaves the sum as it was)
+            place = torch.arange(words.numel(), device=words.device) * -0x61C8864680B583EB | 1
+            total = (total * 1000003 + int((words * place).sum())) & 0xFFFFFFFFFFFFFFFF
         return total
 
     def work(self) -> dict:
