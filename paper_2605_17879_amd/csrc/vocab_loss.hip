@@ -467,8 +467,8 @@ __device__ __forceinline__ float2 tile_sums(const product_args& p, f32x4 (&acc)[
 #pragma unroll
         for (int f = 0; f < FM; ++f) acc[f][j] = -acc[f][j];
     }
-    // (never 0: words that are not there are -inf, and their exponentials 0)
-    const float up = fmaxf(fabsf(p.scale2), 1.1754943508222875e-38f);
+    // (never 0: words that are not there are -inf, and their exponentials 0; a scale that is no number makes every sum none)
+    const float up = fabsf(p.scale2) < 1.1754943508222875e-38f ? 1.1754943508222875e-38f : fabsf(p.scale2);
     float top = -__builtin_inff();
     if (__ballot((int32_t)(words[FM - 1] - words[0]) + 3 >= words_left(p, words[0]))) {
         const int32_t left = words_left(p, words[0]);
@@ -1115,7 +1115,7 @@ __global__ __launch_bounds__(256) void finish_hidden(const float* slabs, uint32_
         }
         gd_vec<T, 4> q;
 #pragma unroll
-        for (int r = 0; r < 4; ++r) q.v[r] = gd_from_f32<T>(sum[r] * back * more);
+        for (int r = 0; r < 4; ++r) q.v[r] = gd_from_f32<T>(at >= 0 ? sum[r] * back * more : 0.0f);
         T* to = out + (uint64_t)i * ldo + c;
         if (c + 4 <= width) {
             __builtin_memcpy(to, &q, sizeof(q));

@@ -37,3 +37,15 @@ def test_loss_of_more_tiles_than_a_launch_holds(det, n, gap):
     within(out["loss"][rows.cuda()], ref.loss, ref.loss_bound, "loss")
     assert float(out["mean"][1]) == n
     assert abs(float(out["mean"][0]) - float(out["loss"].double().mean())) < 1e-5 * float(out["mean"][0])
+
+
+@pytest.mark.parametrize("n,vocab,width", [(9, 300, 64), (300, 5001, 72), (2100, 9001, 72)])
+def test_a_logit_scale_that_is_no_number(det, n, vocab, width):
+    """Every logit is none then, and so is all that comes of them: sums, losses, the gradients' rows that have one."""
+    h, w, t = randn((n, width), 1, BF16), randn((vocab, width), 2, BF16, 0.5), refs.tokens(n, vocab, 3, 0.2)
+    out = run_loss(det, h, w, t, 0, float("nan"), grad_mean=1.0)
+    keep = (t >= 0).cuda()
+    assert bool(torch.isnan(out["lse"]).all())
+    assert bool(torch.isnan(out["loss"][keep]).all()) and bool((out["loss"][~keep] == 0).all()) and bool(torch.isnan(out["mean"][0]))
+    assert bool(torch.isnan(out["hidden_grad"][keep]).all()) and bool((out["hidden_grad"][~keep] == 0).all())
+    assert bool(torch.isnan(out["weight_grad"]).all())
