@@ -5,7 +5,7 @@ import torch
 
 import operator_refs as refs
 from paper_2605_17879_amd import Config, Detector
-from test_gpu_operators import BF16, randn, run_loss, say, within
+from test_gpu_operators import BF16, F16, randn, run_loss, say, within
 
 pytestmark = pytest.mark.gpu
 
@@ -49,3 +49,53 @@ def test_a_logit_scale_that_is_no_number(det, n, vocab, width):
     assert bool(torch.isnan(out["loss"][keep]).all()) and bool((out["loss"][~keep] == 0).all()) and bool(torch.isnan(out["mean"][0]))
     assert bool(torch.isnan(out["hidden_grad"][keep]).all()) and bool((out["hidden_grad"][~keep] == 0).all())
     assert bool(torch.isnan(out["weight_grad"]).all())
+
+
+PROBABLE = [(9, 300, 64), (20, 70000, 72), (70, 1500, 72), (300, 5001, 64), (2100, 9001, 72)]
+
+
+def probable_targets(n, vocab, d, dtype):
+    """Hidden states, weights and targets that are probable: 24 words share most of each row's probability.  Column c of the
+    first 24 is 1.5 for the c-th of those words and 0 for all others, so that an element of the hidden states'
+    gradient there is one element of G times 1.5."""
+    some = torch.randperm(vocab, generator=torch.Generator().manual_seed(5))[:24]
+    h, w = randn((n, d), 1, dtype), randn((vocab, d), 2, dtype, 0.1)
+    w[some] = randn((24, d), 3, dtype, 2 / d ** 0.5)
+    w[:, :24] = 0
+    w[some, torch.arange(24)] = 1.5
+    # (5 to 9 above the other words' logits, whose number that makes up for)
+    h[:, -1] = 1.0
+    w[:, -1] = 0
+    w[some, -1] = 3.0 + float(torch.tensor(vocab).log2()) / 2
+    which = torch.multinomial(torch.softmax(h.double() @ w[some].double().T, 1), 1, generator=torch.Generator().manual_seed(6))[:, 0]
+    return h, w, some, which
+
+
+def target_element(ref, h, w, t, c, dtype):
+    """G at the rows' targets where what rounding drops there is kept, rounded to the type itself: its value, and how far off it
+    may be (the exponent's error, the exponential's, the subtraction's and products', the square of a rounding)."""
+    n = len(t)
+    logits = (h.double() @ w.double().T)[torch.arange(n), t]
+    p = torch.exp(logits - ref.lse)
+    expo = ref.logit_err[torch.arange(n), t] + ref.lse_bound + 4 * refs.U32 * (logits.abs() + ref.lse.abs())
+    g = c * (p - 1)
+    err = abs(c) * p * (torch.expm1(expo) + 4 * refs.U32) + (refs.u(dtype) ** 2 + 6 * refs.U32) * g.abs() * (1 + expo)
+    return p, g, err + (abs(c) * 2.0 ** -38 if dtype == F16 else 0.0)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("n,vocab,d", PROBABLE)
+def test_hidden_gradient_at_probable_targets_is_rounded_once(det, dtype, n, vocab, d):
+    """One product, its addition to zeros, what the rounding of G drops, two factors: eight roundings to fp32, one to the type."""
+    say(f"probable targets, hidden: {dtype} n={n} vocab={vocab} d={d}")
+    h, w, some, which = probable_targets(n, vocab, d, dtype)
+    t = some[which]
+    ref = refs.Loss(h, w, t, grad_mean=1.0)
+    p, g, err = target_element(ref, h, w, t, 1.0 / n, dtype)
+    assert float(((p > 0.05) & (p < 0.95)).double().mean()) > 0.3, "the targets are not what the test is about"
+    out = run_loss(det, h, w, t, grad_mean=1.0)
+    want = 1.5 * g
+    err = 1.5 * err + 8 * refs.U32 * want.abs()
+    low = torch.finfo(dtype).smallest_normal * refs.u(dtype) * 2
+    within(out["hidden_grad"].cpu()[torch.arange(n), which], want, err + refs.u(dtype) * (want.abs() + err) + low, "gradient at the target")
+    within(out["hidden_grad"], ref.hidden_grad, ref.hidden_grad_bound, "gradient of the hidden states")
