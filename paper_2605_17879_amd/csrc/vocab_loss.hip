@@ -186,6 +186,18 @@ __device__ __forceinline__ void tile_of(uint32_t b, uint32_t tiles_m, uint32_t t
     tm = in / width;
 }
 
+// s_waitcnt operands: all but `n` loads (n below 16); all LDS reads
+constexpr int loads_but(int n) { return 0x0F70 | n; }
+constexpr int LDS_READ = 0xC07F;
+
+// A barrier behind which what every wave has staged is there.  The wait for a wave's own loads to the LDS is written out: a
+// barrier by itself orders what a wave has written, and leaves loads that go past its registers to the compiler, which waits
+// where it sees this wave read them, in front of the barrier or not.
+__device__ __forceinline__ void staged_by_all() {
+    __builtin_amdgcn_s_waitcnt(loads_but(0));
+    __syncthreads();
+}
+
 constexpr uint32_t SPARE = 4096;   // bytes of the LDS that a wave has to itself behind the sum
 
 // The sum over k for tiles of 128 x 128 by four waves, two workgroups a CU.  Sixteen rows of A at a
@@ -243,7 +255,7 @@ struct small_tile {
             for (int s = 0; s < STEPS; ++s) {
                 if (s == 1) read_b(b, 1);
                 if (s + AHEAD == STEPS) {
-                    __syncthreads();                         // (the next block is there, this one read by all)
+                    staged_by_all();                         // (the next block is there, this one read by all)
                     if (ends != 0 && kt + 2 == blocks) end_rows(na, nb);
                     if (kt + 2 < blocks) stage(a, b, kt + 2);
                     read_b(nb, 0);
@@ -260,7 +272,7 @@ struct small_tile {
         auto start = [&](uint8_t* a, uint8_t* b, uint8_t* na, uint8_t* nb) {
             stage(a, b, 0);
             meanwhile();
-            __syncthreads();
+            staged_by_all();
             if (ends != 0 && blocks == 1) end_rows(a, b);
             if (blocks > 1) stage(na, nb, 1);
             read_b(b, 0);
@@ -308,10 +320,6 @@ struct large_tile {
         return APART ? wm * 128 + i * 16 : (i / 4) * 128 + wm * 64 + (i % 4) * 16;
     }
     static __device__ __forceinline__ uint32_t col_of(uint32_t wn, int j) { return wn * 64 + j * 16; }
-
-    // s_waitcnt operands: all but `n` loads (n below 16); all LDS reads
-    static constexpr int loads_but(int n) { return 0x0F70 | n; }
-    static constexpr int LDS_READ = 0xC07F;
 
     template <typename Meanwhile>
     static __device__ __forceinline__ void run(const operand& oa, const operand& ob, uint32_t m0, uint32_t n0, uint32_t kfirst,
