@@ -466,8 +466,9 @@ gd_status gd_vocab_loss(gd_handle h, const gd_matrix* hidden, const gd_matrix* w
  *   weight_grad = logit_scale * transposed G hidden  [vocab][width]
  * both of the type of hidden; either may be null.  G is rounded to that type for the matrix
  * cores (relative to the largest c in f16, so that no gradient underflows for being a mean's).  What that
- * drops at the targets is kept and added to hidden_grad; up to 32 rows weight_grad takes all
- * that it drops, so that its own rounding is the only one.
+ * drops at the targets (where it counts most: with probable targets both gradients were off by 1.25 times
+ * their own rounding, 1.04 with it) is kept and added to both, to weight_grad from a sixteenth of the most that it can be on;
+ * up to 32 rows weight_grad takes all that it drops, so that its own rounding is the only one.
  * Rows with c[i] == 0 have no part in weight_grad, whatever their hidden state holds.
  *   d_work: gd_vocab_loss_work_bytes(n, vocab, width, 1) bytes, 256-byte aligned
  */

@@ -14,9 +14,11 @@
 //   dW        m = width, n = the piece's vocabulary, k = rows: written as the piece's rows
 // Up to FOLD rows fill half a block of k of dW, which takes two halves all the same: the second one holds the rows once more, against
 // what the rounding of G has dropped, so that dW of few rows is not rounded twice.
-// Of the other rows' G what counts most is the element at the target, 1 less than a probability: what rounding drops of it is kept, and
-// added to dH as one row of W times it (with probable targets, logits of standard deviation 4, dH of 256 rows x 5 000 x 256 is
-// off by 0.00178 of itself, 0.00167 of which is its own rounding; 0.00215 without).
+// Of other rows' G what counts most is the element at the target, 1 less than a probability: what rounding drops of it is kept, and
+// added to dH as a row of W times it, and to dW as a block of k more in the tiles whose words are targets, where it is not
+// little.  With targets drawn from the softmax of logits of standard deviation 4, 2 000 rows x 20 000 x 512: dH and dW off by 0.00173
+// and 0.00172 of themselves (0.00206 and 0.00205 without; 0.00166 are their own rounding), 240 -> 246 us; 8 192 x 131 072 x 4 096
+// 26.56 -> 26.76 ms.  What remains is the other elements' rounding.
 // For the gradients the rows that have one are gathered first: rows left out cost nothing, and what
 // their hidden states hold (infinities, NaN) reaches no product.
 //
@@ -88,7 +90,10 @@ struct product_args {
     const float* row_lse2;          // G: per gathered row, in units of log 2
     const float* row_coef;
     const int32_t* row_target;
-    float* row_rest;                // what rounding drops of a row's G at its target: written with G
+    float* row_rest;                // what rounding drops of a row's G at its target (rest_of): written with G, read for dW
+    const uint2* list;              // dW: rows and their targets in order of the targets' groups, or null
+    const uint32_t* list_at;        // [groups + 1] where a group's begin
+    uint32_t groups;
     uint32_t fold;                  // G: row FOLD + i is what rounding drops of row i
     // outputs
     void* c;  uint64_t ldc;         // G, slabs, dW
@@ -198,7 +203,8 @@ __device__ __forceinline__ void staged_by_all() {
     __syncthreads();
 }
 
-constexpr uint32_t SPARE = 4096;   // bytes of the LDS that a wave has to itself behind the sum
+// Behind the sum the buffers of B are free, `room`; of the first one a wave has SPARE bytes to itself.
+constexpr uint32_t SPARE = 4096;
 
 // The sum over k for tiles of 128 x 128 by four waves, two workgroups a CU.  Sixteen rows of A at a
 // time (a step) are multiplied by all of the wave's columns, over the first half of the block's k, then the
@@ -216,14 +222,15 @@ struct small_tile {
 
     template <typename Meanwhile>
     static __device__ __forceinline__ void run(const operand& oa, const operand& ob, uint32_t m0, uint32_t n0, uint32_t kfirst,
-                                               uint32_t blocks, uint32_t ends, f32x4 (&acc)[FM][FN], uint8_t*& spare,
+                                               uint32_t blocks, uint32_t ends, f32x4 (&acc)[FM][FN], uint8_t* (&room)[2],
                                                Meanwhile meanwhile) {
         // (one array a buffer, so that the compiler knows which loads a read has to wait for)
         __shared__ __attribute__((aligned(16))) uint8_t sa0[BM * BK * 2], sb0[BN * BK * 2];
         __shared__ __attribute__((aligned(16))) uint8_t sa1[BM * BK * 2], sb1[BN * BK * 2];
         const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
         const uint32_t wm = wave / WN, wn = wave % WN;
-        spare = sb0 + wave * SPARE;
+        room[0] = sb0;
+        room[1] = sb1;
         if (blocks == 0) return;
         stager<BM, A_ALONG, NT> la;
         stager<BN, B_ALONG, NT> lb;
@@ -323,13 +330,14 @@ struct large_tile {
 
     template <typename Meanwhile>
     static __device__ __forceinline__ void run(const operand& oa, const operand& ob, uint32_t m0, uint32_t n0, uint32_t kfirst,
-                                               uint32_t blocks, uint32_t ends, f32x4 (&acc)[FM][FN], uint8_t*& spare,
+                                               uint32_t blocks, uint32_t ends, f32x4 (&acc)[FM][FN], uint8_t* (&room)[2],
                                                Meanwhile meanwhile) {
         __shared__ __attribute__((aligned(16))) uint8_t up0[128 * BK * 2], low0[128 * BK * 2], sb0[BN * BK * 2];
         __shared__ __attribute__((aligned(16))) uint8_t up1[128 * BK * 2], low1[128 * BK * 2], sb1[BN * BK * 2];
         const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
         const uint32_t wm = wave / WN, wn = wave % WN, group = wm;   // (waves w and w + 4 share a SIMD)
-        spare = sb0 + wave * SPARE;
+        room[0] = sb0;
+        room[1] = sb1;
         if (blocks == 0) return;
         stager<128, A_ALONG, NT, APART> lu, ll;
         stager<BN, B_ALONG, NT> lb;
@@ -522,6 +530,16 @@ __device__ __forceinline__ g_row g_row_of(const product_args& p, uint32_t i, boo
 // The row whose place i is.
 __device__ __forceinline__ uint32_t folded(const product_args& p, uint32_t i) { return p.fold && i >= FOLD && i < 2 * FOLD ? i - FOLD : i; }
 
+// What rounding to T drops of an element of G, with a last bit of 1 where that is little, less than a sixteenth of what it may drop;
+// 0 where it drops nothing or the result is no number.
+template <typename T>
+__device__ __forceinline__ float rest_of(float g) {
+    const float rest = g - gd_to_f32(gd_from_f32<T>(g));
+    const float little = fabsf(g) * (std::is_same<T, gd_f16>::value ? 0x1p-15f : 0x1p-12f);
+    if (rest == 0.0f || !(fabsf(rest) < __builtin_inff())) return 0.0f;
+    return __uint_as_float((__float_as_uint(rest) & ~1u) | (fabsf(rest) < little ? 1u : 0u));
+}
+
 // Column j of a wave's tile of logits, row i, to G.  The exponential's instruction drops subnormal results: it is taken 2^64
 // times as large, and the coefficient as much smaller.  What the rounding to T drops at the row's target is kept.
 template <typename T, int FM, int FN>
@@ -546,10 +564,7 @@ __device__ __forceinline__ void tile_g(const product_args& p, f32x4 (&acc)[FM][F
                 if (w >= left || none) acc[f][j][r] = 0.0f;
                 if (w == met) { g = acc[f][j][r]; here = true; }
             }
-        if (here) {
-            const float rest = g - gd_to_f32(gd_from_f32<T>(g));
-            p.row_rest[i] = fabsf(rest) < __builtin_inff() ? rest : 0.0f;
-        }
+        if (here) p.row_rest[i] = rest_of<T>(g);
     }
 }
 
@@ -571,6 +586,89 @@ __device__ __forceinline__ f32x4 dropped_by(const f32x4& x) {
         d[r] = d[r] == d[r] ? d[r] : 0.0f;
     }
     return d;
+}
+
+// ---- what the rounding of G drops at the targets, for dW ----------------------------------------------
+
+constexpr uint32_t GROUP = 128;    // words of a group of the list of rows by their targets
+
+// A row whose target is a word of the tile: which row, which word of the tile, what rounding has dropped there.
+struct alignas(16) rest_of_row {
+    uint32_t row, word;
+    float rest;
+};
+// (those of rows that are not there are 0, and left out)
+__device__ __forceinline__ rest_of_row rest_at(const product_args& p, uint32_t word0, uint32_t e, uint32_t to) {
+    if (e >= to) return rest_of_row{0, 0, 0.0f};
+    const uint2 x = p.list[e];
+    return rest_of_row{x.x, x.y - word0, p.row_rest[x.x]};
+}
+
+// Added to a tile of the weights' gradient whose sum is taken: the rows whose targets are words of the tile, entries from..to of the
+// list, where rounding has not dropped little, 64 at a time against a matrix with one number a row.  Most tiles
+// have a few such rows, or none.  listed: one entry for each thread, the first ones in it; while a block is multiplied, the
+// next one's rows are on their way.
+template <typename T, typename TILE>
+__device__ __forceinline__ void add_rests(const product_args& p, uint32_t m0, uint32_t n0, uint32_t from, uint32_t to, uint32_t wave, uint32_t lane,
+                                          uint8_t* const (&room)[2], rest_of_row* listed, f32x4 (&acc)[TILE::FM][TILE::FN]) {
+    typedef typename of_type<T>::x8 X8;
+    constexpr uint32_t BM = TILE::BM, BN = TILE::BN, NT = TILE::NT, LOADS = BM * 8 / NT;
+    static_assert(BM == BN, "a lane's chunks of the two operands are the same rows'");
+    __shared__ uint32_t counts[NT / 64];
+    uint8_t* const sa = room[1];                                 // as the sum's images: chunk c of row k at c ^ turn(k)
+    uint8_t* const sb = room[0];
+    const uint32_t wm = wave / TILE::WN, wn = wave % TILE::WN;
+    for (uint32_t base = from; base < to; base += NT) {
+        const rest_of_row mine = base == from ? listed[threadIdx.x] : rest_at(p, p.v0 + n0, base + threadIdx.x, to);
+        const bool keep = mine.rest != 0.0f && !(__float_as_uint(mine.rest) & 1);
+        const uint64_t who = __ballot(keep);
+        if (lane == 0) counts[wave] = (uint32_t)__popcll(who);
+        __syncthreads();
+        uint32_t at = (uint32_t)__popcll(who & ((1ull << lane) - 1)), count = 0;
+#pragma unroll
+        for (uint32_t w = 0; w < NT / 64; ++w) { if (w < wave) at += counts[w]; count += counts[w]; }
+        if (keep) listed[at] = mine;
+        __syncthreads();
+        X8 ahead[LOADS];
+        const auto ask = [&](uint32_t e0) {
+#pragma unroll
+            for (uint32_t j = 0; j < LOADS; ++j) {
+                const uint32_t i = j * NT + threadIdx.x, e = e0 + i / (BM / 8), c = min(m0 / 8 + i % (BM / 8), p.a.cols / 8 - 1);
+                ahead[j] = X8(0);
+                if (e < count) ahead[j] = *reinterpret_cast<const X8*>(static_cast<const T*>(p.a.p) + (uint64_t)listed[e].row * p.a.stride + c * 8);
+            }
+        };
+        if (count > 0) ask(0);
+        for (uint32_t e0 = 0; e0 < count; e0 += BK) {
+#pragma unroll
+            for (uint32_t j = 0; j < LOADS; ++j) {
+                const uint32_t i = j * NT + threadIdx.x, k = i / (BM / 8), c = i % (BM / 8), to_k = k * (BM * 2) + ((c ^ (turn(k) % (BM / 8))) * 16);
+                *reinterpret_cast<X8*>(sa + to_k) = ahead[j];
+                const rest_of_row r = listed[min(e0 + k, count - 1)];
+                const T value = gd_from_f32<T>(e0 + k < count ? r.rest : 0.0f);
+                X8 x(0);
+#pragma unroll
+                for (uint32_t w = 0; w < 8; ++w) x[w] = r.word == c * 8 + w ? value : T(0.0f);
+                *reinterpret_cast<X8*>(sb + to_k) = x;
+            }
+            __syncthreads();
+            if (e0 + BK < count) ask(e0 + BK);
+#pragma unroll
+            for (uint32_t half = 0; half < 2; ++half) {
+                if (e0 + half * 32 >= count) break;
+                X8 fb[TILE::FN];
+#pragma unroll
+                for (int j = 0; j < TILE::FN; ++j) fb[j] = fragment<BN, false, X8>(sb, TILE::col_of(wn, j), half, lane);
+#pragma unroll
+                for (int i = 0; i < TILE::FM; ++i) {
+                    const X8 fa = fragment<BM, false, X8>(sa, TILE::row_of(wm, i), half, lane);
+#pragma unroll
+                    for (int j = 0; j < TILE::FN; ++j) acc[i][j] = multiply(fa, fb[j], acc[i][j]);
+                }
+            }
+            __syncthreads();
+        }
+    }
 }
 
 template <typename T, typename TILE, int EPI>
@@ -608,11 +706,26 @@ __global__ __launch_bounds__(TILE::NT, 512 / TILE::NT) void product_kernel(const
         if constexpr (EPI == EPI_G) mine = g_row_of(p, folded(p, i), folded(p, i) < n);
         else mine = target_from(p, i, n);
     }
+    // So do the first rows whose targets are words of a tile of the weights' gradient.
+    __shared__ rest_of_row listed[EPI == EPI_OUT ? TILE::NT : 1];
+    uint2 entry = make_uint2(0, 0);
+    uint32_t from = 0, to = 0;
+    if (EPI == EPI_OUT && p.list) {
+        const uint32_t group = (p.v0 + n0) / GROUP;
+        from = p.list_at[group];
+        to = p.list_at[min(group + BN / GROUP, p.groups)];
+        if (from + threadIdx.x < to) entry = p.list[from + threadIdx.x];
+    }
     // operands that lie along k end where their rows do
-    uint8_t* spare;
-    TILE::run(p.a, p.b, m0, n0, kfirst, blocks, EPI == EPI_LSE || EPI == EPI_G ? k % BK : 0, acc, spare, [&] {
+    uint8_t* room[2];
+    TILE::run(p.a, p.b, m0, n0, kfirst, blocks, EPI == EPI_LSE || EPI == EPI_G ? k % BK : 0, acc, room, [&] {
         if ((EPI == EPI_LSE || EPI == EPI_G) && threadIdx.x < BN) row_of[threadIdx.x] = mine;
+        if (EPI == EPI_OUT && from < to)
+            listed[threadIdx.x] = rest_of_row{entry.x, entry.y - (p.v0 + n0), from + threadIdx.x < to ? p.row_rest[entry.x] : 0.0f};
     });
+    if constexpr (EPI == EPI_OUT)
+        if (from < to) add_rests<T, TILE>(p, m0, n0, from, to, wave, lane, room, listed, acc);
+    uint8_t* const spare = room[0] + wave * SPARE;
 
     // lane l holds rows 4 (l / 16) + 0..3 and column l % 16 of each 16 x 16 block
     uint32_t row[FM], col[FN];
@@ -620,6 +733,7 @@ __global__ __launch_bounds__(TILE::NT, 512 / TILE::NT) void product_kernel(const
     for (int i = 0; i < FM; ++i) row[i] = m0 + TILE::row_of(wm, i) + (lane >> 4) * 4;
 #pragma unroll
     for (int j = 0; j < FN; ++j) col[j] = n0 + TILE::col_of(wn, j) + (lane & 15);
+
     // Rows are what lies next to each other in memory: through the wave's part of the LDS, 16 columns at a time, lanes
     // that have four rows of a column each become lanes with eight, and whole lines are written.
     constexpr uint32_t CH = FM * 2;                              // 16-byte chunks of a column
@@ -858,12 +972,12 @@ __global__ __launch_bounds__(256) void few_rows_kernel(const product_args p) {
 // Rows of `in` (all, or those listed) into rows of a padded copy, eight elements a lane: zeros behind the row's end
 // and, behind a list, up to the next 256 rows.
 template <typename T>
-__global__ __launch_bounds__(256) void pack_kernel(const void* in, uint64_t stride, uint32_t width, const grad_head* head,
-                                                   const uint32_t* rows, uint32_t n, T* out, uint32_t ldo, bool fold) {
+__device__ __forceinline__ void pack_rows(const void* in, uint64_t stride, uint32_t width, const grad_head* head,
+                                          const uint32_t* rows, uint32_t n, T* out, uint32_t ldo, bool fold, uint32_t packers) {
     if (head) n = head->count;
     const uint32_t last = head ? (n + 255) / 256 * 256 : n, chunks = ldo / 8;
     const uint64_t total = (uint64_t)last * chunks;
-    for (uint64_t x = (uint64_t)blockIdx.x * 256 + threadIdx.x; x < total; x += (uint64_t)gridDim.x * 256) {
+    for (uint64_t x = (uint64_t)blockIdx.x * 256 + threadIdx.x; x < total; x += (uint64_t)packers * 256) {
         const uint32_t r = (uint32_t)(x / chunks), c = (uint32_t)(x - (uint64_t)r * chunks) * 8;
         const uint32_t at = fold && r >= FOLD && r < 2 * FOLD ? r - FOLD : r;
         gd_vec<T, 8> q{};
@@ -872,6 +986,61 @@ __global__ __launch_bounds__(256) void pack_kernel(const void* in, uint64_t stri
             if (c < width) q = __builtin_bit_cast(gd_vec<T, 8>, last_at(static_cast<const T*>(in) + row * stride, (int32_t)c, (int32_t)width, width >= 8));
         }
         *reinterpret_cast<gd_vec<T, 8>*>(out + (uint64_t)r * ldo + c) = q;
+    }
+}
+
+template <typename T>
+__global__ __launch_bounds__(256) void pack_kernel(const void* in, uint64_t stride, uint32_t width, uint32_t n, T* out, uint32_t ldo) {
+    pack_rows<T>(in, stride, width, nullptr, nullptr, n, out, ldo, false, gridDim.x);
+}
+
+// The rows with a gradient into a copy and, by the workgroups behind the `packers`, their list in order of the targets' groups: workgroup
+// g counts the rows whose targets lie in groups before g, then lists its own behind those, in order of the rows.  A wave looks
+// at a stretch of the rows, 512 at once.
+template <typename T>
+__global__ __launch_bounds__(256) void gather_kernel(const void* in, uint64_t stride, uint32_t width, const grad_head* head, const uint32_t* rows,
+                                                     T* out, uint32_t ldo, bool fold, uint32_t packers, const int32_t* target,
+                                                     uint32_t groups, uint2* list, uint32_t* list_at) {
+    if (blockIdx.x < packers) return pack_rows<T>(in, stride, width, head, rows, 0, out, ldo, fold, packers);
+    constexpr uint32_t WAVES = 4, EACH = 8;
+    __shared__ uint32_t before[WAVES], own[WAVES];
+    const uint32_t n = head->count, g = blockIdx.x - packers, wave = threadIdx.x / 64, lane = threadIdx.x & 63;
+    const uint32_t per = (n + WAVES - 1) / WAVES, from = min(wave * per, n), to = min(from + per, n);
+    uint32_t t[EACH];
+    const auto look = [&](uint32_t i0) {                         // (rows that are not there lie behind all words)
+#pragma unroll
+        for (uint32_t b = 0; b < EACH; ++b) t[b] = (uint32_t)target[min(i0 + b * 64 + lane, n - 1)];
+#pragma unroll
+        for (uint32_t b = 0; b < EACH; ++b)
+            if (i0 + b * 64 + lane >= to) t[b] = 0xFFFFFFFFu;
+    };
+    uint32_t less = 0, mine = 0;
+    for (uint32_t i0 = from; i0 < to; i0 += EACH * 64) {
+        look(i0);
+#pragma unroll
+        for (uint32_t b = 0; b < EACH; ++b) {
+            less += (uint32_t)__popcll(__ballot(t[b] / GROUP < g));
+            mine += (uint32_t)__popcll(__ballot(t[b] / GROUP == g));
+        }
+    }
+    if (lane == 0) { before[wave] = less; own[wave] = mine; }
+    __syncthreads();
+    uint32_t at = 0;
+    for (uint32_t w = 0; w < WAVES; ++w) at += before[w];
+    if (threadIdx.x == 0) {
+        list_at[g] = at;
+        if (g + 1 == groups) list_at[groups] = n;
+    }
+    for (uint32_t w = 0; w < wave; ++w) at += own[w];
+    if (mine == 0) return;
+    for (uint32_t i0 = from; i0 < to; i0 += EACH * 64) {
+        if (per > EACH * 64) look(i0);                           // (else they are still here)
+#pragma unroll
+        for (uint32_t b = 0; b < EACH; ++b) {
+            const uint64_t who = __ballot(t[b] / GROUP == g);
+            if (t[b] / GROUP == g) list[at + (uint32_t)__popcll(who & ((1ull << lane) - 1))] = make_uint2(i0 + b * 64 + lane, t[b]);
+            at += (uint32_t)__popcll(who);
+        }
     }
 }
 
@@ -1174,7 +1343,7 @@ struct loss_layout {
     // forward and both
     size_t target_logit, part, hidden, weight;
     // gradients
-    size_t head, rows, slot, lse2, coef, target, rest, g, slabs;
+    size_t head, rows, slot, lse2, coef, target, rest, list, list_at, g, slabs;
     size_t total;
     uint64_t padded_rows, ldh, piece, pack_piece, slab;
     split_plan split;
@@ -1199,7 +1368,7 @@ loss_layout layout_of(uint64_t n, uint64_t vocab, uint64_t width, bool with_grad
     l.hidden = f;  f = gd_align256(f + l.padded_rows * l.ldh * 2);
     l.weight = f;  f = gd_align256(f + l.pack_piece * l.ldh * 2);
     l.total = f;
-    l.head = l.rows = l.slot = l.lse2 = l.coef = l.target = l.rest = l.g = l.slabs = 0;
+    l.head = l.rows = l.slot = l.lse2 = l.coef = l.target = l.rest = l.list = l.list_at = l.g = l.slabs = 0;
     l.piece = l.slab = 0;
     if (!with_grad) return l;
     // pieces of G alike in size
@@ -1216,6 +1385,8 @@ loss_layout layout_of(uint64_t n, uint64_t vocab, uint64_t width, bool with_grad
     l.coef = f;   f = gd_align256(f + n * 4);
     l.target = f; f = gd_align256(f + n * 4);
     l.rest = f;   f = gd_align256(f + n * 4);
+    l.list = f;   f = gd_align256(f + n * 8);
+    l.list_at = f; f = gd_align256(f + (up_to(vocab, GROUP) / GROUP + 1) * 4);
     l.g = f;      f = gd_align256(f + l.padded_rows * l.piece * 2);
     l.slabs = f;  f = gd_align256(f + l.split.splits * l.slab * 4);
     l.total = f;
@@ -1283,7 +1454,7 @@ void launch_weight_grad(const product_args& p, hipStream_t s) {
     }
     if (large < p.n) {
         product_args q = p;
-        q.n -= large;
+        q.n -= large; q.v0 += large;
         q.b.p = static_cast<const T*>(p.b.p) + large;
         q.b.cols -= large;
         q.c = static_cast<T*>(p.c) + (uint64_t)large * p.ldc;
@@ -1302,8 +1473,8 @@ hipError_t forward(const gd_vocab_loss_args& a, hipStream_t s) {
     const bool few = few_tiles(n, a.vocab);
     p.b = operand{a.hidden, a.hidden_stride, n, a.width};
     if (!few && !direct(a.hidden, a.hidden_stride, a.width)) {
-        hipLaunchKernelGGL((pack_kernel<T>), dim3(blocks_for((uint64_t)n * ldh / 8)), dim3(256), 0, s, a.hidden, a.hidden_stride, a.width,
-                           (const grad_head*)nullptr, (const uint32_t*)nullptr, n, hidden, ldh, false);
+        hipLaunchKernelGGL((pack_kernel<T>), dim3(blocks_for((uint64_t)n * ldh / 8)), dim3(256), 0, s, a.hidden, a.hidden_stride, a.width, n,
+                           hidden, ldh);
         p.b = operand{hidden, ldh, n, ldh};
     }
     const bool plain = few || direct(a.weight, a.weight_stride, a.width);
@@ -1320,8 +1491,8 @@ hipError_t forward(const gd_vocab_loss_args& a, hipStream_t s) {
         if (plain) {
             p.a = operand{w, a.weight_stride, here, a.width};
         } else {
-            hipLaunchKernelGGL((pack_kernel<T>), dim3(blocks_for((uint64_t)here * ldh / 8)), dim3(256), 0, s, w, a.weight_stride, a.width,
-                               (const grad_head*)nullptr, (const uint32_t*)nullptr, here, weight, ldh, false);
+            hipLaunchKernelGGL((pack_kernel<T>), dim3(blocks_for((uint64_t)here * ldh / 8)), dim3(256), 0, s, w, a.weight_stride, a.width, here,
+                               weight, ldh);
             p.a = operand{weight, ldh, here, ldh};
         }
         p.m = here; p.v0 = v0; p.part0 = parts;
@@ -1363,8 +1534,12 @@ hipError_t backward(const gd_vocab_grad_args& a, hipStream_t s) {
     const uint32_t padded = (uint32_t)l.padded_rows;
     if (n <= 1024) hipLaunchKernelGGL((prepare_rows<1>), dim3(1), dim3(1024), 0, s, r);
     else hipLaunchKernelGGL((prepare_rows<8>), dim3(1), dim3(1024), 0, s, r);
-    hipLaunchKernelGGL((pack_kernel<T>), dim3(blocks_for((uint64_t)padded * ldh / 8)), dim3(256), 0, s, a.hidden, a.hidden_stride, a.width,
-                       head, r.rows, n, hidden, ldh, n <= FOLD);
+    uint2* list = reinterpret_cast<uint2*>(a.work + l.list);
+    uint32_t* list_at = reinterpret_cast<uint32_t*>(a.work + l.list_at);
+    const bool listed = a.weight_grad && n > FOLD;
+    const uint32_t packers = blocks_for((uint64_t)padded * ldh / 8), groups = (a.vocab + GROUP - 1) / GROUP;
+    hipLaunchKernelGGL((gather_kernel<T>), dim3(packers + (listed ? groups : 0)), dim3(256), 0, s, a.hidden, a.hidden_stride, a.width, head, r.rows,
+                       hidden, ldh, n <= FOLD, packers, r.row_target, groups, list, list_at);
     const bool plain = direct(a.weight, a.weight_stride, a.width);
     uint32_t piece = (uint32_t)l.piece;
     if (!plain && piece > l.pack_piece) piece = (uint32_t)l.pack_piece;
@@ -1374,8 +1549,8 @@ hipError_t backward(const gd_vocab_grad_args& a, hipStream_t s) {
         const T* w = static_cast<const T*>(a.weight) + (uint64_t)v0 * a.weight_stride;
         operand wo{w, a.weight_stride, here, a.width};
         if (!plain && (a.hidden_grad || !few)) {
-            hipLaunchKernelGGL((pack_kernel<T>), dim3(blocks_for((uint64_t)here * ldh / 8)), dim3(256), 0, s, w, a.weight_stride, a.width,
-                               (const grad_head*)nullptr, (const uint32_t*)nullptr, here, weight, ldh, false);
+            hipLaunchKernelGGL((pack_kernel<T>), dim3(blocks_for((uint64_t)here * ldh / 8)), dim3(256), 0, s, w, a.weight_stride, a.width, here,
+                               weight, ldh);
             wo = operand{weight, ldh, here, ldh};
         }
         const operand go{g, piece, padded, piece};
@@ -1405,7 +1580,9 @@ hipError_t backward(const gd_vocab_grad_args& a, hipStream_t s) {
             q.a = operand{hidden, ldh, padded, ldh};
             q.b = go;
             q.m = a.width; q.n = here; q.k = n;
-            q.scale = a.scale;
+            q.scale = a.scale; q.v0 = v0;
+            q.row_rest = rest;
+            q.list = listed ? list : nullptr; q.list_at = list_at; q.groups = groups;
             q.c = static_cast<T*>(a.weight_grad) + (uint64_t)v0 * a.weight_grad_stride; q.ldc = a.weight_grad_stride;
             launch_weight_grad<T>(q, s);
         }

@@ -54,11 +54,11 @@ def test_a_logit_scale_that_is_no_number(det, n, vocab, width):
 PROBABLE = [(9, 300, 64), (20, 70000, 72), (70, 1500, 72), (300, 5001, 64), (2100, 9001, 72)]
 
 
-def probable_targets(n, vocab, d, dtype):
+def probable_targets(n, vocab, d, dtype, near=False):
     """Hidden states, weights and targets that are probable: 24 words share most of each row's probability.  Column c of the
     first 24 is 1.5 for the c-th of those words and 0 for all others, so that an element of the hidden states'
-    gradient there is one element of G times 1.5."""
-    some = torch.randperm(vocab, generator=torch.Generator().manual_seed(5))[:24]
+    gradient there is one element of G times 1.5.  near: the 24 words are the first ones."""
+    some = torch.arange(24) if near else torch.randperm(vocab, generator=torch.Generator().manual_seed(5))[:24]
     h, w = randn((n, d), 1, dtype), randn((vocab, d), 2, dtype, 0.1)
     w[some] = randn((24, d), 3, dtype, 2 / d ** 0.5)
     w[:, :24] = 0
@@ -71,15 +71,16 @@ def probable_targets(n, vocab, d, dtype):
     return h, w, some, which
 
 
-def target_element(ref, h, w, t, c, dtype):
+def target_element(ref, h, w, t, c, dtype, left_out=0.0):
     """G at the rows' targets where what rounding drops there is kept, rounded to the type itself: its value, and how far off it
-    may be (the exponent's error, the exponential's, the subtraction's and products', the square of a rounding)."""
+    may be (the exponent's error, the exponential's, the subtraction's and products', the square of a rounding, and what is
+    left out for being little)."""
     n = len(t)
     logits = (h.double() @ w.double().T)[torch.arange(n), t]
     p = torch.exp(logits - ref.lse)
     expo = ref.logit_err[torch.arange(n), t] + ref.lse_bound + 4 * refs.U32 * (logits.abs() + ref.lse.abs())
     g = c * (p - 1)
-    err = abs(c) * p * (torch.expm1(expo) + 4 * refs.U32) + (refs.u(dtype) ** 2 + 6 * refs.U32) * g.abs() * (1 + expo)
+    err = abs(c) * p * (torch.expm1(expo) + 4 * refs.U32) + (refs.u(dtype) ** 2 + left_out + 6 * refs.U32) * g.abs() * (1 + expo)
     return p, g, err + (abs(c) * 2.0 ** -38 if dtype == F16 else 0.0)
 
 
@@ -99,3 +100,32 @@ def test_hidden_gradient_at_probable_targets_is_rounded_once(det, dtype, n, voca
     low = torch.finfo(dtype).smallest_normal * refs.u(dtype) * 2
     within(out["hidden_grad"].cpu()[torch.arange(n), which], want, err + refs.u(dtype) * (want.abs() + err) + low, "gradient at the target")
     within(out["hidden_grad"], ref.hidden_grad, ref.hidden_grad_bound, "gradient of the hidden states")
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("n,vocab,near", [(24, 300, False), (40, 300, False), (70, 1500, False), (200, 33001, False), (300, 5001, False), (2100, 9001, False),
+                                          (2100, 9001, True), (2100, 9100, True), (200, 200, True)])
+def test_weights_gradient_at_probable_targets_is_rounded_once(det, dtype, n, vocab, near):
+    """Columns in which one row's hidden state is 1.5 and all others are 0: the target's gradient there is one element of G times
+    1.5.  Up to 2 100 rows have their targets in one tile, in several or in none.  What rounding drops counts from a sixteenth of
+    the most that it may drop on."""
+    d = 264
+    say(f"probable targets, weights: {dtype} n={n} vocab={vocab} near={near}")
+    h, w, some, which = probable_targets(n, vocab, d, dtype, near)
+    rows = torch.arange(n)[::max(1, n // 200)][:200]
+    at = 24 + torch.arange(len(rows))
+    h[:, 24:224] = 0
+    h[rows, at] = 1.5
+    t = some[which]
+    t[3] = -1
+    ref = refs.Loss(h, w, t, grad_mean=1.0)
+    keep = t[rows] >= 0
+    rows, at = rows[keep], at[keep]
+    part = refs.Loss(h[rows], w, t[rows])
+    p, g, err = target_element(part, h[rows], w, t[rows], 1.0 / ref.count, dtype, refs.u(dtype) / 16)
+    out = run_loss(det, h, w, t, grad_mean=1.0)
+    want = 1.5 * g
+    err = 1.5 * err + 8 * refs.U32 * want.abs()
+    low = torch.finfo(dtype).smallest_normal * refs.u(dtype) * 2
+    within(out["weight_grad"].cpu()[t[rows], at], want, err + refs.u(dtype) * (want.abs() + err) + low, "gradient at the target")
+    within(out["weight_grad"], ref.weight_grad, ref.weight_grad_bound, "gradient of the weights")
