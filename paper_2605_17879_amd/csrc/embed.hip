@@ -9,11 +9,16 @@
 // stretches.  A workgroup sums the rows of one stretch, one column vector per lane, and writes a
 // token's sum when the next token begins.  A token that goes on over a stretch's end leaves fp32
 // partial sums (one at the front and one at the back of each stretch), which a second kernel adds up in
-// order: however often a token occurs, the work stays even.  The sums run at the memory's rate (16 384 x 4 096 bf16 added: 41 us,
+// order, in pairs, fours, ... of sixteen parts and these one behind another.  There are at most MOST_STRETCHES, so that the longest chain
+// of additions of n rows is that of n / 4 096 rows and 256 more (1 000 000 rows x 256 bf16 233 us; in stretches of 32 rows all of them
+// 340, and a token of 4 194 304 rows was off by 1e-3).  The sums run at the memory's rate (16 384 x 4 096 bf16 added: 41 us,
 // 6 TB/s); the rest of the time are short launches one behind another (85 us in all).
+// The parts of one token are one workgroup's for 1 024 columns: a list that one token dominates takes longer (32 768 x 2 048, no token /
+// one on half / on all of the rows: 127 / 157 / 186 us; 16 384 x 4 096 added: 84 / 116 / 127).
 //
 // Short lists cost launches, not work: up to FEW rows each row's workgroup looks for its token in the whole list and,
-// if the row is the token's first, sums them all, in one launch.
+// if the row is the token's first, sums them all, in one launch (1 000 x 1 000 fp32, no token / one on half / on all of the rows: 8.6 / 24 / 49
+// us; 2 048 x 512: 8.8 / 39 / 76).
 //
 // The gradient's zeros are written by workgroups of the sorting launches that have no keys: sorting is
 // a chain of short launches that leaves the memory idle.
@@ -34,6 +39,7 @@ constexpr uint32_t SELF_COUNT = 8, SELF_SCAN = 64;
 constexpr uint32_t FEW = 2048, FEW_GROUPS = 8192;
 constexpr uint32_t MOST_GROUPS = 1u << 21;  // of a launch: HIP takes less than 2^32 threads in a dimension
 constexpr uint32_t BATCH = 8;             // rows on their way at once in the sums
+constexpr uint32_t MOST_STRETCHES = 4096;
 constexpr uint32_t FILL_ROWS = 16384;     // most rows that one of its workgroups fills with zeros
 constexpr uint32_t NO_ROW = 0xFFFFFFFFu;
 
@@ -564,11 +570,18 @@ __global__ __launch_bounds__(NT) void grad_join(gd_embed_grad_args a, const uint
 #pragma unroll
         for (uint32_t b = 0; b < PARTS; ++b)
             q[b] = gd_read<float, V>(partial + (uint64_t)min(s0 + b, hi - 1) * 2 * a.width + c.at);
+        // (in pairs first: the sum of 4 096 parts is a chain of 256 additions then)
 #pragma unroll
         for (uint32_t b = 0; b < PARTS; ++b)
-            if (s0 + b < hi)
+            if (s0 + b >= hi) q[b] = gd_vec<float, V>{};
 #pragma unroll
-                for (int j = 0; j < V; ++j) sum[j] += q[b].v[j];
+        for (uint32_t d = 1; d < PARTS; d *= 2)
+#pragma unroll
+            for (uint32_t b = 0; b < PARTS; b += 2 * d)
+#pragma unroll
+                for (int j = 0; j < V; ++j) q[b].v[j] += q[b + d].v[j];
+#pragma unroll
+        for (int j = 0; j < V; ++j) sum[j] += q[0].v[j];
     }
     write_sum<T, V>(a, token, c, sum, a.accumulate, a.accumulate ? old_row<T, V>(a, token, c) : gd_vec<T, V>{});
 }
@@ -716,8 +729,10 @@ struct grad_layout {
 grad_layout layout_of(uint64_t n, uint64_t width) {
     grad_layout l;
     l.blocks = (uint32_t)((n + SORT_KEYS - 1) / SORT_KEYS);
-    // stretches: 1 024 of them, that all CUs have some, between one batch and four
+    // stretches: 1 024 of them, that all CUs have some, between one batch and four; no more than MOST_STRETCHES, since a
+    // token's parts are added up one behind another
     l.span = n <= 1024 * BATCH ? BATCH : n <= 2048 * BATCH ? 2 * BATCH : 4 * BATCH;
+    if (n > (uint64_t)MOST_STRETCHES * l.span) l.span = (uint32_t)((n + (uint64_t)MOST_STRETCHES * BATCH - 1) / ((uint64_t)MOST_STRETCHES * BATCH)) * BATCH;
     size_t o = 0;
     for (int i = 0; i < 2; ++i) {
         l.key[i] = o; o = gd_align256(o + n * 4);

@@ -5,7 +5,7 @@ import torch
 
 import operator_refs as refs
 from paper_2605_17879_amd import Config, Detector
-from test_gpu_operators import BF16, F16, randn, run_loss, say, within
+from test_gpu_operators import BF16, F16, F32, check_grad, poison, randn, run_loss, say, within
 
 pytestmark = pytest.mark.gpu
 
@@ -129,3 +129,28 @@ def test_weights_gradient_at_probable_targets_is_rounded_once(det, dtype, n, voc
     low = torch.finfo(dtype).smallest_normal * refs.u(dtype) * 2
     within(out["weight_grad"].cpu()[t[rows], at], want, err + refs.u(dtype) * (want.abs() + err) + low, "gradient at the target")
     within(out["weight_grad"], ref.weight_grad, ref.weight_grad_bound, "gradient of the weights")
+
+
+@pytest.mark.parametrize("n,width", [(1 << 22, 4), (3_000_001, 3), (131_073, 8), (131_072, 8)])
+def test_lookup_grad_of_a_token_over_millions_of_rows(det, n, width):
+    """All rows are one token's, and their values alike, so that every addition's error goes the same way: the sum is as far off
+    as its longest chain of additions allows, a stretch of at most 32 rows or a 4 096th of them, and a sixteenth of
+    4 096 parts' with four levels of pairs in front of them."""
+    say(f"one token, n={n}")
+    vocab, value = 9, 1.9
+    t = torch.full((n,), 3, device="cuda")
+    g = torch.full((n, width), value, device="cuda")
+    w = poison(torch.empty((vocab, width), device="cuda"))
+    det.embed_grad(g, t, w, det.alloc_embed_grad_work(n, vocab, width), scale=0.5)
+    chain = max(32, -(-n // (4096 * 8)) * 8) + 256 + 4 + 2
+    want = torch.full((width,), float(torch.tensor(value)) * n * 0.5, dtype=torch.float64)
+    within(w[3], want, chain * refs.U32 * want, "gradient")
+    assert bool((w[torch.arange(vocab) != 3] == 0).all())
+
+
+@pytest.mark.parametrize("accumulate", [False, True])
+@pytest.mark.parametrize("n,vocab,width", [(200_003, 2, 24), (150_000, 70_000, 8), (400_001, 40, 9)])
+def test_lookup_grad_of_long_lists(det, accumulate, n, vocab, width):
+    say(f"lookup_grad n={n} vocab={vocab} width={width} accumulate={accumulate}")
+    t = refs.tokens(n, vocab, n + 1, padding=0.1)
+    check_grad(det, randn((n, width), n, F32), t, vocab, 1.7, accumulate, randn((vocab, width), n + 2, F32))
