@@ -5,7 +5,7 @@ import torch
 
 import operator_refs as refs
 from paper_2605_17879_amd import Config, Detector
-from test_gpu_operators import BF16, F16, F32, check_grad, poison, randn, run_loss, say, within
+from test_gpu_operators import BF16, F16, F32, check_grad, check_loss, poison, randn, run_loss, say, within
 
 pytestmark = pytest.mark.gpu
 
@@ -154,3 +154,44 @@ def test_lookup_grad_of_long_lists(det, accumulate, n, vocab, width):
     say(f"lookup_grad n={n} vocab={vocab} width={width} accumulate={accumulate}")
     t = refs.tokens(n, vocab, n + 1, padding=0.1)
     check_grad(det, randn((n, width), n, F32), t, vocab, 1.7, accumulate, randn((vocab, width), n + 2, F32))
+
+
+@pytest.mark.parametrize("n,vocab,width,gap,padding", [
+    (2100, 9001, 72, 0, 0.1), (22000, 130, 520, 0, 0.3), (40, 33001, 264, 0, 0.0), (2305, 8000, 200, 8, 0.0), (2049, 8191, 33, 0, 0.5),
+])
+def test_loss_and_gradients_in_large_tiles_of_f16(det, n, vocab, width, gap, padding):
+    say(f"large tiles f16 n={n} vocab={vocab} width={width} gap={gap} padding={padding}")
+    h, w = randn((n, width), n + width, F16), randn((vocab, width), n + vocab, F16, 2 / width ** 0.5)
+    t = refs.tokens(n, vocab, n, padding)
+    check_loss(run_loss(det, h, w, t, gap, grad_mean=1.0), refs.Loss(h, w, t, grad_mean=1.0))
+
+
+@pytest.mark.parametrize("n,vocab,width,padding", [(1, 66001, 40, 0.0), (17, 70003, 136, 0.3), (33, 66001, 64, 0.1), (65, 66001, 72, 0.0), (9, 95, 2056, 0.0),
+                                                   (64, 1090, 1000, 0.2)])
+def test_loss_and_gradients_of_few_rows_of_f16(det, n, vocab, width, padding):
+    say(f"few rows f16 n={n} vocab={vocab} width={width} padding={padding}")
+    h, w = randn((n, width), n + width, F16), randn((vocab, width), n + vocab, F16, 2 / width ** 0.5)
+    t = refs.tokens(n, vocab, n, padding)
+    check_loss(run_loss(det, h, w, t, grad_mean=1.0), refs.Loss(h, w, t, grad_mean=1.0))
+
+
+@pytest.mark.parametrize("scale", [-0.75, 0.0])
+@pytest.mark.parametrize("n,vocab,width", [(9, 300, 64), (300, 5001, 72), (2100, 9001, 72)])
+def test_logit_scales_below_one_of_f16(det, scale, n, vocab, width):
+    h, w, t = randn((n, width), 1, F16), randn((vocab, width), 2, F16, 0.5), refs.tokens(n, vocab, 3, 0.1)
+    check_loss(run_loss(det, h, w, t, 0, scale, grad_mean=1.0), refs.Loss(h, w, t, scale, grad_mean=1.0))
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("grad_mean", [1.0, 2.0 ** 10])
+@pytest.mark.parametrize("n,vocab,width", [(2500, 3000, 40), (2100, 9001, 72)])
+def test_small_probabilities_have_their_part_in_the_gradients(det, dtype, grad_mean, n, vocab, width):
+    """A mean over thousands of rows: where G is not taken relative to the largest coefficient, the words without a target
+    have one of a few of f16's least numbers, and the bound on its rounding is passed."""
+    h, w = randn((n, width), 1, dtype), randn((vocab, width), 2, dtype, 0.1)
+    t = refs.tokens(n, vocab // 2, 3)                               # (the second half is no row's target)
+    ref = refs.Loss(h, w, t, grad_mean=grad_mean)
+    out = run_loss(det, h, w, t, grad_mean=grad_mean)
+    check_loss(out, ref)
+    others = out["weight_grad"][vocab // 2:].double().cpu()
+    assert float((others != 0).double().mean()) > 0.95
