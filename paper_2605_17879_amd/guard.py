@@ -545,8 +545,11 @@ class Detector:
 
     def adamw_table(self, params, grads, state: dict, copies=None, weight_decay=0.0, lr_scale=1.0, first_index=0):
         """What adamw needs to know about its tensors (lists of the same length; weight_decay,
-        lr_scale and first_index are lists too, or one value for all).  The tensors are kept
-        alive by it and must stay where they are."""
+        lr_scale and first_index are lists too, or one value for all).  It holds addresses, and keeps
+        the memory there alive.  A tensor that has moved (gradients that are freed and made anew each
+        step, storage that is exchanged) needs a new table: an update by the old one reads and writes
+        the old memory, and nothing says so.  Making one takes the host 3 us a tensor and copies it
+        to the device (160 tensors: 0.5 ms)."""
         torch, n = self._torch, len(params)
         each = lambda v: list(v) if isinstance(v, (list, tuple)) else [v] * n
         eight = "m_exp" in state
@@ -575,7 +578,9 @@ class Detector:
             raise GuardError(1, (self.lib.gd_last_error(self.h) or b"").decode())
         host = torch.empty(size, dtype=torch.uint8)
         self._check(self.lib.gd_adamw_fill_table(self.h, rows, n, host.data_ptr(), size))
-        return dict(bytes=host.to(self.device), tensors=lists)
+        # (a tensor whose storage is exchanged lets the old one go: the storages themselves are kept)
+        kept = [t.untyped_storage() for l in (*lists[:5], *lists[8:]) for t in l if t is not None]
+        return dict(bytes=host.to(self.device), tensors=lists, storages=kept)
 
     def adamw(self, table: dict, lr: float, step: int, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8,
               grad_scale=None, seed: Optional[int] = None, stream=None):

@@ -195,3 +195,33 @@ def test_small_probabilities_have_their_part_in_the_gradients(det, dtype, grad_m
     check_loss(out, ref)
     others = out["weight_grad"][vocab // 2:].double().cpu()
     assert float((others != 0).double().mean()) > 0.95
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_adamw_table_keeps_the_memory_that_it_updates(det, bits):
+    """Storages exchanged behind a table: the update by it goes to the old memory, which nobody else has got meanwhile."""
+    n = 3_000_001
+    make = lambda: torch.ones(n, device="cuda")                      # noqa: E731
+    p, g, c = make(), make(), torch.zeros(n, dtype=BF16, device="cuda")
+    state = det.alloc_adamw_state([p], bits)
+    table = det.adamw_table([p], [g], state, copies=[c])
+    tensors = [p, g, c] + [x[0] for x in state.values()]
+    old = {t.data_ptr() for t in tensors}
+    for t in tensors:
+        t.data = torch.zeros(8, dtype=t.dtype, device="cuda")
+    others = [torch.full((n,), 7, dtype=t.dtype, device="cuda") for t in tensors[:5] for _ in range(2)]
+    assert not old & {t.data_ptr() for t in others}
+    det.adamw(table, lr=1e-2, step=1)
+    torch.cuda.synchronize()
+    assert all(bool((t == 7).all()) for t in others)
+
+
+def test_adamw_with_another_table_size_writes_nothing(det):
+    p, g = [torch.ones(1000, device="cuda") for _ in range(40)], [torch.ones(1000, device="cuda") for _ in range(40)]
+    state = det.alloc_adamw_state(p)
+    table = det.adamw_table(p, g, state)
+    assert table["bytes"].numel() > 512
+    det.adamw({"bytes": table["bytes"][:512]}, lr=1e-2, step=1)
+    assert all(bool((t == 1).all()) for t in p) and all(bool((t == 0).all()) for v in state.values() for t in v)
+    det.adamw(table, lr=1e-2, step=1)
+    assert all(bool((t < 1).all()) for t in p)
