@@ -399,8 +399,9 @@ typedef enum {
 } gd_dtype;
 
 /* A matrix in device memory: row r begins at element r * stride, its cols elements are next to
- * each other.  stride >= cols; the pointer is aligned to its element.  A list (tokens, targets)
- * has cols = 1, with any stride.  A matrix without elements may have a null pointer. */
+ * each other.  cols <= stride <= 2^22; the pointer is aligned to its element.  A list (tokens, targets)
+ * has cols = 1, and as any matrix of one column a stride of 1 to 2^40.  A matrix without elements may have a
+ * null pointer. */
 typedef struct gd_matrix {
     void* d_data;
     uint64_t rows, cols, stride;
@@ -529,7 +530,9 @@ gd_status gd_adamw_fill_table(gd_handle h, const gd_adamw_tensor* tensors, uint3
                               void* host_table, size_t bytes);
 
 /* One update of all tensors of a table.  d_grad_scale: one f32 in device memory that every gradient is
- * multiplied by (clipping, loss scaling), or null; where it is infinite or NaN nothing is written. */
+ * multiplied by (clipping, loss scaling), or null; where it is infinite or NaN nothing is written.
+ * What is in device memory no status can tell: a d_table that does not say itself that it has table_bytes
+ * bytes writes nothing either, and one whose tensors have moved is followed to where they were. */
 gd_status gd_adamw(gd_handle h, const void* d_table, size_t table_bytes, const gd_adamw_config* cfg,
                    const float* d_grad_scale, void* stream);
 
