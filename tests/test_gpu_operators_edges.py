@@ -225,3 +225,40 @@ def test_adamw_with_another_table_size_writes_nothing(det):
     assert all(bool((t == 1).all()) for t in p) and all(bool((t == 0).all()) for v in state.values() for t in v)
     det.adamw(table, lr=1e-2, step=1)
     assert all(bool((t < 1).all()) for t in p)
+
+
+@pytest.mark.parametrize("n,vocab,d,gap,dtype", [
+    # rows apart and unaligned, copied in one piece and in two; G in two pieces
+    (70, 1500, 264, 3, F16), (300, 5001, 264, 8, BF16), (70, 70_000, 2056, 3, BF16), (9, 70_000, 2056, 3, BF16), (20, 300, 264, 3, F16),
+    (4200, 66_001, 264, 0, BF16), (4200, 66_001, 264, 0, F16), (2100, 9001, 265, 0, BF16),
+])
+def test_gradients_at_probable_targets_over_pieces(det, n, vocab, d, gap, dtype):
+    """The elements of the two tests before, with coefficients of each row's own, a logit scale, rows left out, and operands that lie and
+    are cut in other ways."""
+    say(f"probable targets over pieces: {dtype} n={n} vocab={vocab} d={d} gap={gap}")
+    h, w, some, which = probable_targets(n, vocab, d, dtype)
+    w = w * 2                                                        # (exact, and undone by the scale)
+    picked = torch.arange(n)[::max(1, n // 60)][:60]
+    at = 24 + torch.arange(len(picked))
+    h[:, 24:224] = 0
+    h[picked, at] = 1.5
+    t = some[which]
+    t[3::7] = -1
+    coef = randn((n,), 8, F32, 0.5) + 1.0
+    out = run_loss(det, h, w, t, gap, 0.5, grad_mean=0.75, grad_rows=coef)
+    keep = t[picked] >= 0
+    picked, at, which = picked[keep], at[keep], which[picked[keep]]
+    ref = refs.Loss(h[picked], w, t[picked], 0.5)
+    c = coef[picked].double() + 0.75 / int((t >= 0).sum())
+    most = float(coef.abs().max()) + 1.0
+    logits = 0.5 * (h[picked].double() @ w.double().T)[torch.arange(len(picked)), t[picked]]
+    p = torch.exp(logits - ref.lse)
+    expo = ref.logit_err[torch.arange(len(picked)), t[picked]] + ref.lse_bound + 4 * refs.U32 * (logits.abs() + ref.lse.abs())
+    g = c * (p - 1)
+    low = torch.finfo(dtype).smallest_normal * refs.u(dtype) * 2
+    for name, i, j, factor, left_out in (("hidden_grad", picked, which, 1.5, 0.0), ("weight_grad", t[picked], at, 0.75, refs.u(dtype) / 16)):
+        want = factor * g
+        err = c.abs() * p * (torch.expm1(expo) + 4 * refs.U32) + (refs.u(dtype) ** 2 + left_out + 6 * refs.U32) * g.abs() * (1 + expo)
+        err = factor * (err + (most * 2.0 ** -38 if dtype == F16 else 0.0)) + 8 * refs.U32 * want.abs()
+        within(out[name].cpu()[i, j], want, err + refs.u(dtype) * (want.abs() + err) + low, name)
+    assert bool((out["hidden_grad"][(t < 0).cuda()] == 0).all())
