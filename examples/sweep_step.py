@@ -103,10 +103,13 @@ class SweepStep:
     def work(self) -> dict:
         """What a step's parts move (bytes) or compute (operations)."""
         counted = int((self.targets >= 0).sum())
+        distinct = int(torch.unique(self.tokens).numel())
         row = self.width * 2
         state = 16 if self.bits == 32 else 4
-        return {"lookup": 2 * (self.rows * 8 + 3 * self.rows * row),
-                "loss": (4.0 * self.rows + 6.0 * counted) * self.vocab * self.width,
+        # there: rows of the table read, looked up ones written; back: their gradients read, the table's read and written
+        return {"lookup": 2 * self.rows * 8 + (2 * self.rows + 3 * distinct) * row,
+                # the logits of every row; again, and both gradients, of the rows with a target
+                "loss": (2.0 * self.rows + 6.0 * counted) * self.vocab * self.width,
                 "update": self.vocab * self.width * (4 + 2 + 4 + 2 + state)}
 
 
