@@ -22,7 +22,8 @@
  *
  * What a sweep has its GPUs run stands at the end: the operators on both sides of a
  * language model's vocabulary (gd_embed, gd_vocab_loss, gd_adamw and the gradients),
- * which make one training step of the job's own kind and repeat bit for bit.
+ * which make one training step of the job's own kind and repeat bit for bit, and those of the
+ * matrices between them (gd_pack, gd_packed_product, gd_muon).
  *
  * The paper states the decision in words only.  The estimators and constants
  * used here (median / MAD x 1.4826 / threshold 3.5 / k-of-W / scaled node sum)
@@ -395,7 +396,9 @@ typedef enum {
     GD_F16 = 2,
     GD_I32 = 3,
     GD_I64 = 4,
-    GD_E4M3 = 5 /* the 8-bit states of gd_adamw */
+    GD_E4M3 = 5, /* the 8-bit states of gd_adamw; codes of packed matrices */
+    GD_E5M2 = 6, /* codes of packed matrices */
+    GD_U8 = 7    /* their powers of two */
 } gd_dtype;
 
 /* A matrix in device memory: row r begins at element r * stride, its cols elements are next to
@@ -535,6 +538,98 @@ gd_status gd_adamw_fill_table(gd_handle h, const gd_adamw_tensor* tensors, uint3
  * bytes writes nothing either, and one whose tensors have moved is followed to where they were. */
 gd_status gd_adamw(gd_handle h, const void* d_table, size_t table_bytes, const gd_adamw_config* cfg,
                    const float* d_grad_scale, void* stream);
+
+/*
+ * Packed matrices: 8-bit floating point with a power of two for each block of 128 elements of a row.
+ *   codes [rows][cols]               GD_E4M3 or GD_E5M2, one byte each; 16-byte aligned, the stride a multiple of 16
+ *   exp   [ceil(cols / 128)][rows]   GD_U8; 4-byte aligned, the stride a multiple of 4
+ * Element (i, k) stands for codes[i][k] * 2^(exp[k / 128][i] - 127); a byte of 255 stands for a block of NaN.  In front
+ * of the last row what lies between its end and the next one's begin is neither read as a number nor written.
+ */
+typedef struct gd_packed {
+    gd_matrix codes, exp;
+} gd_packed;
+
+#define GD_PACK_BLOCK 128u
+
+/*
+ * Packing: codes = the nearest to x * 2^(127 - e), ties to even, with e the least of 1..254 for which the largest
+ * magnitude of the block is at most MOST * 2^(e - 127) (MOST = 448 for e4m3, 57344 for e5m2; for e > 1 it is more than half
+ * of that); e = 0 for a block of zeros, 255 and codes of NaN for a block that holds an infinity or a NaN.
+ *   x       [n][k]  in   f32, bf16 or f16
+ *   along   [n][k]  out  blocks of 128 along the rows of x, or null
+ *   across  [k][n]  out  x transposed, blocks of 128 along the columns of x, or null
+ *   square != 0: one e for each 128 x 128 of x (written for each of its rows), so that `across` holds the same
+ *   numbers as `along`, transposed
+ * One of the two is there; where both are, x is read once.  A linear layer's y = x w^T, dx = dy w and dw = dy^T x are products
+ * of x, w (square) and dy packed both ways.
+ */
+gd_status gd_pack(gd_handle h, const gd_matrix* x, int32_t square, const gd_packed* along, const gd_packed* across, void* stream);
+
+/*
+ * Product of packed matrices: out[i][j] = round((accumulate ? out[i][j] : 0) + sum over k of a[i][k] b[j][k]), summed in
+ * fp32 in an order that the sizes alone fix.  For an out of 16 bits the products of eight neighbouring k are added by the 8-bit
+ * matrix cores, which keep 13 binary digits behind the largest of them (1.5e-5 of the result for normal numbers, 7e-5
+ * for numbers of wide range); for an out of fp32 by the 16-bit ones, at half the rate, and numbers below 2^-126 may count as 0.
+ *   a    [n][k]  in       either's codes e4m3 or e5m2
+ *   b    [m][k]  in
+ *   out  [n][m]  in, out  f32, bf16 or f16
+ *   d_work: gd_packed_product_work_bytes(n, m, k) bytes, 256-byte aligned
+ * n, m up to 2^24, k up to 2^22.
+ */
+size_t gd_packed_product_work_bytes(uint64_t n, uint64_t m, uint64_t k);
+gd_status gd_packed_product(gd_handle h, const gd_packed* a, const gd_packed* b, const gd_matrix* out, int32_t accumulate,
+                            void* d_work, size_t work_bytes, void* stream);
+
+/*
+ * Update of matrices by their orthogonalised momentum, many at once.  For each, M and U in fp32 (g = grad * grad_scale):
+ *   M = M * [momentum] + g;  U = g + [momentum] * M with nesterov, else M
+ *   X = U / (|U| + eps), |U| the root of the sum of the squares, summed in fp64
+ *   for each step, with its coefficients a, b, c:  A = X X^T;  X = a X + (b A + c A A) X   (X^T X for tall matrices)
+ *   p = param * [1 - lr * lr_scale * weight_decay] - [lr * lr_scale] * X
+ * param = round(p) and, where d_copy is given, copy = round(p).  A matrix of zeros has X = 0.
+ * products: GD_F32 multiplies numbers of 22 binary digits, three products of f16 for one; GD_F16 numbers of 11, apart from
+ * X in its product with b A + c A A, which keeps 22 (X off by 1 to 2 thousandths of itself, for a 16-bit param or copy).
+ * Sums are fp32 in both.  coefficients: three a step, such that the polynomial a s + b s^3 + c s^5 of each step
+ * leaves singular values from 0 to 1 (then what the step before left) at magnitudes of at most 1.35; null:
+ * 3.4445, -4.7750, 2.0315 in every step.
+ */
+typedef struct gd_muon_tensor {
+    void* d_param;
+    const void* d_grad;
+    void* d_m;            /* f32 */
+    void* d_copy;         /* or null */
+    uint64_t rows, cols;  /* up to 65536; elements next to each other in every array, row by row */
+    double lr_scale, weight_decay;
+    uint32_t param_type, grad_type; /* f32, bf16 or f16 */
+    uint32_t copy_type;             /* bf16 or f16; read where d_copy is given */
+    uint32_t reserved;              /* 0 */
+} gd_muon_tensor;
+
+#define GD_MUON_MAX_STEPS 16u
+
+typedef struct gd_muon_config {
+    uint32_t struct_size;   /* = sizeof(gd_muon_config) */
+    uint32_t nesterov;
+    uint32_t products;      /* GD_F32 or GD_F16 */
+    uint32_t steps;         /* 0 to GD_MUON_MAX_STEPS */
+    double lr, momentum, eps;
+    const double* coefficients; /* host memory, [steps][3], or null */
+} gd_muon_config;
+
+/* What the launches read about the matrices: gd_muon_table_bytes bytes (0 where the list is refused), written to host
+ * memory by gd_muon_fill_table.  The caller copies them to the device once (256-byte aligned there) and keeps both as
+ * long as the tensors stay where they are.  No tensor may stand twice in a table. */
+size_t gd_muon_table_bytes(gd_handle h, const gd_muon_tensor* tensors, uint32_t n_tensors);
+gd_status gd_muon_fill_table(gd_handle h, const gd_muon_tensor* tensors, uint32_t n_tensors, void* host_table, size_t bytes);
+/* Of the work area of an update with these products (256-byte aligned, nothing is kept in it between calls); 0 where the
+ * bytes are no table. */
+size_t gd_muon_work_bytes(gd_handle h, const void* host_table, size_t table_bytes, uint32_t products);
+
+/* One update of all matrices of a table.  d_grad_scale: one f32 in device memory that every gradient is multiplied by, or
+ * null; where it is infinite or NaN nothing is written but the work area. */
+gd_status gd_muon(gd_handle h, const void* host_table, const void* d_table, size_t table_bytes, const gd_muon_config* cfg,
+                  const float* d_grad_scale, void* d_work, size_t work_bytes, void* stream);
 
 /*
  * NOT part of the detector's contract -- a diagnostic for benchmarks, exported so that

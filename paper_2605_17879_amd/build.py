@@ -13,7 +13,7 @@ SCORE_SOURCES = ["score.hip", "score_z.hip"]
 RAGGED_SOURCES = ["score_ragged_few.hip", "score_ragged_few_z.hip", "score_ragged_many.hip",
                   "score_ragged_many_z.hip", "score_ragged_columns.hip", "score_ragged_columns_z.hip"]
 SOURCES = [*RAGGED_SOURCES, *SCORE_SOURCES, "api.hip", "window.hip", "topk.hip", "severity.hip", "sweep.hip", "ledger.hip", "membership.hip",
-           "embed.hip", "vocab_loss.hip", "adamw.hip"]
+           "embed.hip", "vocab_loss.hip", "adamw.hip", "pack.hip", "packed_product.hip", "muon.hip"]
 
 # One rounding per written operation (no FMA contraction), IEEE divide,
 # denormals kept, and no packed-fp32 instructions.

@@ -85,7 +85,8 @@ gd_status hip_fail(gd_handle h, hipError_t e, const char* what) {
 // Rows are addressed by 32-bit byte offsets from a tile's first one.
 constexpr uint64_t MAX_STRIDE = 1u << 22;
 
-uint32_t bytes_of(uint32_t type) { return type == GD_F32 || type == GD_I32 ? 4 : type == GD_I64 ? 8 : type == GD_E4M3 ? 1 : 2; }
+bool is_byte(uint32_t type) { return type == GD_E4M3 || type == GD_E5M2 || type == GD_U8; }
+uint32_t bytes_of(uint32_t type) { return type == GD_F32 || type == GD_I32 ? 4 : type == GD_I64 ? 8 : is_byte(type) ? 1 : 2; }
 bool is_float(uint32_t type) { return type == GD_F32 || type == GD_BF16 || type == GD_F16; }
 
 // What is wrong with a matrix of rows x cols elements, or null.
@@ -160,6 +161,45 @@ const char* bad_tensors(const gd_adamw_tensor* t, uint32_t n) {
     if (n && !t) return "null list of tensors";
     for (uint32_t i = 0; i < n; ++i)
         if (const char* e = bad_tensor(t[i])) return e;
+    return nullptr;
+}
+
+// What is wrong with a packed matrix of rows x cols, or null.
+const char* bad_packed(const gd_packed* p, uint64_t rows, uint64_t cols) {
+    if (!p) return "null packed matrix";
+    if (p->codes.dtype != GD_E4M3 && p->codes.dtype != GD_E5M2) return "codes must be e4m3 or e5m2";
+    if (p->exp.dtype != GD_U8) return "powers of two must be u8";
+    if (const char* e = bad_matrix(&p->codes, rows, cols)) return e;
+    if (const char* e = bad_matrix(&p->exp, (cols + GD_PACK_BLOCK - 1) / GD_PACK_BLOCK, rows)) return e;
+    if (rows == 0 || cols == 0) return nullptr;
+    if (((uintptr_t)p->codes.d_data & 15) || (rows > 1 && (p->codes.stride & 15))) return "codes and their stride must be 16-byte aligned";
+    if (p->codes.stride > MAX_STRIDE) return "stride above 2^22 elements";
+    if (((uintptr_t)p->exp.d_data & 3) || (cols > GD_PACK_BLOCK && (p->exp.stride & 3))) return "powers of two and their stride must be 4-byte aligned";
+    return nullptr;
+}
+
+gd_packed_out packed_out(const gd_packed* p) {
+    return gd_packed_out{static_cast<uint8_t*>(p->codes.d_data), p->codes.stride, static_cast<uint8_t*>(p->exp.d_data), p->exp.stride};
+}
+
+constexpr uint64_t MAX_INNER = 1u << 22;    // of a packed product: rows of `across`, which a stride spans
+
+// What is wrong with the matrices of an update, or null.
+const char* bad_matrices(const gd_muon_tensor* list, uint32_t n) {
+    if (n && !list) return "null list of tensors";
+    for (uint32_t i = 0; i < n; ++i) {
+        const gd_muon_tensor& t = list[i];
+        if (t.reserved != 0) return "reserved field of a tensor is not 0";
+        if (!is_float(t.param_type) || !is_float(t.grad_type)) return "param and grad must be f32, bf16 or f16";
+        if (t.d_copy && t.copy_type != GD_BF16 && t.copy_type != GD_F16) return "a copy must be bf16 or f16";
+        if (!(isfinite(t.lr_scale) && isfinite(t.weight_decay))) return "lr_scale and weight_decay must be finite";
+        if (t.rows > GD_MAX_WIDTH || t.cols > GD_MAX_WIDTH) return "side of a matrix above 65536";
+        if (t.rows == 0 || t.cols == 0) continue;
+        if (!t.d_param || !t.d_grad || !t.d_m) return "null pointer of a tensor";
+        if ((uintptr_t)t.d_param % bytes_of(t.param_type) || (uintptr_t)t.d_grad % bytes_of(t.grad_type) || ((uintptr_t)t.d_m & 3) ||
+            ((uintptr_t)t.d_copy & 1))
+            return "pointer of a tensor not aligned to its element";
+    }
     return nullptr;
 }
 
@@ -733,6 +773,122 @@ gd_status gd_adamw(gd_handle h, const void* d_table, size_t table_bytes, const g
     a.eps = (float)c->eps; a.seed = c->seed;
     hipError_t e = gd_launch_adamw(a, static_cast<hipStream_t>(stream));
     if (e != hipSuccess) return hip_fail(h, e, "gd_adamw");
+    return GD_OK;
+}
+
+gd_status gd_pack(gd_handle h, const gd_matrix* x, int32_t square, const gd_packed* along, const gd_packed* across, void* stream) {
+    if (!h) return GD_ERR_INVALID_ARG;
+    if (!x) return invalid(h, "gd_pack", "null matrix");
+    if (!along && !across) return invalid(h, "gd_pack", "no output");
+    if (!is_float(x->dtype)) return fail(h, GD_ERR_UNSUPPORTED, "gd_pack: x must be f32, bf16 or f16");
+    if (x->rows > GD_MAX_TOKENS || x->cols > MAX_INNER) return invalid(h, "gd_pack", "more than 2^24 rows or 2^22 columns");
+    if (const char* e = bad_matrix(x, x->rows, x->cols)) return invalid(h, "gd_pack", e);
+    if (along)
+        if (const char* e = bad_packed(along, x->rows, x->cols)) return invalid(h, "gd_pack", e);
+    if (across)
+        if (const char* e = bad_packed(across, x->cols, x->rows)) return invalid(h, "gd_pack", e);
+    if (along && across && along->codes.dtype != across->codes.dtype) return invalid(h, "gd_pack", "the outputs differ in type");
+    if (((x->rows + 127) / 128) * ((x->cols + 127) / 128) >= 1u << 24)      // (a launch has fewer than 2^32 threads)
+        return fail(h, GD_ERR_UNSUPPORTED, "gd_pack: 2^38 elements or more in one call are not built");
+    gd_pack_args a = {};
+    a.x = x->d_data; a.stride = x->stride;
+    a.rows = (uint32_t)x->rows; a.cols = (uint32_t)x->cols; a.dtype = x->dtype; a.square = square != 0;
+    a.codes = along ? along->codes.dtype : across->codes.dtype;
+    if (along) a.along = packed_out(along);
+    if (across) a.across = packed_out(across);
+    hipError_t e = gd_launch_pack(a, static_cast<hipStream_t>(stream));
+    if (e != hipSuccess) return hip_fail(h, e, "gd_pack");
+    return GD_OK;
+}
+
+size_t gd_packed_product_work_bytes(uint64_t n, uint64_t m, uint64_t k) {
+    if (n > GD_MAX_TOKENS || m > GD_MAX_TOKENS || k > MAX_INNER) return 0;
+    return gd_packed_product_work(n, m, k);
+}
+
+gd_status gd_packed_product(gd_handle h, const gd_packed* a, const gd_packed* b, const gd_matrix* out, int32_t accumulate,
+                            void* d_work, size_t work_bytes, void* stream) {
+    if (!h) return GD_ERR_INVALID_ARG;
+    const char* call = "gd_packed_product";
+    if (!a || !b) return invalid(h, call, "null packed matrix");
+    if (!out) return invalid(h, call, "null matrix");
+    const uint64_t n = a->codes.rows, m = b->codes.rows, k = a->codes.cols;
+    if (n > GD_MAX_TOKENS || m > GD_MAX_TOKENS || k > MAX_INNER) return invalid(h, call, "more than 2^24 rows or 2^22 of k");
+    if (!is_float(out->dtype)) return fail(h, GD_ERR_UNSUPPORTED, "gd_packed_product: out must be f32, bf16 or f16");
+    if (const char* e = bad_packed(a, n, k)) return invalid(h, call, e);
+    if (const char* e = bad_packed(b, m, k)) return invalid(h, call, e);
+    if (const char* e = bad_matrix(out, n, m)) return invalid(h, call, e);
+    if (n == 0 || m == 0) return GD_OK;
+    if (((n + 127) / 128) * ((m + 127) / 128) >= 1u << 24)                  // (a launch has fewer than 2^32 threads)
+        return fail(h, GD_ERR_UNSUPPORTED, "gd_packed_product: 2^38 results or more in one call are not built");
+    if (gd_status st = bad_work(h, call, d_work, work_bytes, gd_packed_product_work(n, m, k))) return st;
+    gd_packed_product_args g = {};
+    g.a = a->codes.d_data; g.a_stride = a->codes.stride; g.a_exp = static_cast<const uint8_t*>(a->exp.d_data); g.a_exp_stride = a->exp.stride;
+    g.b = b->codes.d_data; g.b_stride = b->codes.stride; g.b_exp = static_cast<const uint8_t*>(b->exp.d_data); g.b_exp_stride = b->exp.stride;
+    g.n = (uint32_t)n; g.m = (uint32_t)m; g.k = (uint32_t)k; g.a_codes = a->codes.dtype; g.b_codes = b->codes.dtype;
+    g.out = out->d_data; g.out_stride = out->stride; g.out_type = out->dtype; g.accumulate = accumulate != 0;
+    g.work = static_cast<uint8_t*>(d_work);
+    hipError_t e = gd_launch_packed_product(g, static_cast<hipStream_t>(stream));
+    if (e != hipSuccess) return hip_fail(h, e, call);
+    return GD_OK;
+}
+
+size_t gd_muon_table_bytes(gd_handle h, const gd_muon_tensor* tensors, uint32_t n_tensors) {
+    if (!h) return 0;
+    if (const char* e = bad_matrices(tensors, n_tensors)) { invalid(h, "gd_muon_table_bytes", e); return 0; }
+    size_t bytes = 0;
+    try { bytes = gd_muon_table(tensors, n_tensors, nullptr); } catch (...) {}
+    if (!bytes) invalid(h, "gd_muon_table_bytes", "too many elements");
+    return bytes;
+}
+
+gd_status gd_muon_fill_table(gd_handle h, const gd_muon_tensor* tensors, uint32_t n_tensors, void* host_table, size_t bytes) {
+    if (!h) return GD_ERR_INVALID_ARG;
+    if (const char* e = bad_matrices(tensors, n_tensors)) return invalid(h, "gd_muon_fill_table", e);
+    if (!host_table) return invalid(h, "gd_muon_fill_table", "null table");
+    try {
+        const size_t need = gd_muon_table(tensors, n_tensors, nullptr);
+        if (!need) return invalid(h, "gd_muon_fill_table", "too many elements");
+        if (bytes != need) return fail(h, GD_ERR_BUFFER_TOO_SMALL, "gd_muon_fill_table: not gd_muon_table_bytes bytes");
+        gd_muon_table(tensors, n_tensors, host_table);
+    } catch (...) {
+        return invalid(h, "gd_muon_fill_table", "out of host memory");
+    }
+    return GD_OK;
+}
+
+size_t gd_muon_work_bytes(gd_handle h, const void* host_table, size_t table_bytes, uint32_t products) {
+    if (!h) return 0;
+    if (!host_table || !gd_muon_table_fits(host_table, table_bytes)) { invalid(h, "gd_muon_work_bytes", "the bytes are no table"); return 0; }
+    if (products != GD_F32 && products != GD_F16) { invalid(h, "gd_muon_work_bytes", "products must be f32 or f16"); return 0; }
+    return gd_muon_work(host_table, products == GD_F32);
+}
+
+gd_status gd_muon(gd_handle h, const void* host_table, const void* d_table, size_t table_bytes, const gd_muon_config* c,
+                  const float* d_grad_scale, void* d_work, size_t work_bytes, void* stream) {
+    if (!h) return GD_ERR_INVALID_ARG;
+    if (!host_table || !d_table || !c) return invalid(h, "gd_muon", "null argument");
+    if (c->struct_size != sizeof(gd_muon_config))
+        return fail(h, GD_ERR_BAD_CONFIG, "gd_muon: struct_size does not match this library's gd_muon_config");
+    if (((uintptr_t)d_table & 255) || ((uintptr_t)d_grad_scale & 3)) return invalid(h, "gd_muon", "misaligned pointer");
+    if (!gd_muon_table_fits(host_table, table_bytes)) return invalid(h, "gd_muon", "the bytes are no table");
+    if (c->products != GD_F32 && c->products != GD_F16) return fail(h, GD_ERR_BAD_CONFIG, "gd_muon: products must be f32 or f16");
+    if (c->steps > GD_MUON_MAX_STEPS) return fail(h, GD_ERR_BAD_CONFIG, "gd_muon: more than 16 steps");
+    if (!(c->momentum >= 0.0 && c->momentum < 1.0)) return fail(h, GD_ERR_BAD_CONFIG, "gd_muon: momentum must be in [0, 1)");
+    if (!(isfinite(c->lr) && c->eps >= 0.0 && isfinite(c->eps))) return fail(h, GD_ERR_BAD_CONFIG, "gd_muon: lr must be finite, eps finite and not negative");
+    double usual[3 * GD_MUON_MAX_STEPS];
+    for (uint32_t i = 0; i < GD_MUON_MAX_STEPS; ++i) { usual[3 * i] = 3.4445; usual[3 * i + 1] = -4.7750; usual[3 * i + 2] = 2.0315; }
+    const double* coefficients = c->coefficients ? c->coefficients : usual;
+    if (!gd_muon_coefficients_fit(coefficients, c->steps))
+        return fail(h, GD_ERR_BAD_CONFIG, "gd_muon: coefficients must be finite and leave singular values at 1.35 or below");
+    if (gd_status st = bad_work(h, "gd_muon", d_work, work_bytes, gd_muon_work(host_table, c->products == GD_F32))) return st;
+    gd_muon_args a;
+    a.host_table = host_table; a.table = static_cast<const uint8_t*>(d_table); a.work = static_cast<uint8_t*>(d_work);
+    a.grad_scale = d_grad_scale; a.coefficients = coefficients;
+    a.steps = c->steps; a.nesterov = c->nesterov != 0; a.both = c->products == GD_F32;
+    a.momentum = (float)c->momentum; a.lr = c->lr; a.eps = c->eps;
+    hipError_t e = gd_launch_muon(a, static_cast<hipStream_t>(stream));
+    if (e != hipSuccess) return hip_fail(h, e, "gd_muon");
     return GD_OK;
 }
 

@@ -67,16 +67,58 @@ struct gd_adamw_args {
     uint32_t seed;
 };
 
+// Codes [rows][cols], rows `stride` bytes apart, and the powers of two [blocks of cols][rows].
+struct gd_packed_out {
+    uint8_t* codes;  uint64_t stride;
+    uint8_t* exp;    uint64_t exp_stride;
+};
+
+struct gd_pack_args {
+    const void* x;  uint64_t stride;
+    uint32_t rows, cols, dtype, codes, square;
+    gd_packed_out along, across;   // of x, of x transposed; null codes: not asked for
+};
+
+struct gd_packed_product_args {
+    const void* a;  uint64_t a_stride;  const uint8_t* a_exp;  uint64_t a_exp_stride;
+    const void* b;  uint64_t b_stride;  const uint8_t* b_exp;  uint64_t b_exp_stride;
+    uint32_t n, m, k, a_codes, b_codes;
+    void* out;  uint64_t out_stride;
+    uint32_t out_type, accumulate;
+    uint8_t* work;
+};
+
+struct gd_muon_args {
+    const void* host_table;
+    const uint8_t* table;
+    uint8_t* work;
+    const float* grad_scale;
+    const double* coefficients;   // three a step
+    uint32_t steps, nesterov, both;
+    float momentum;
+    double lr, eps;
+};
+
 size_t gd_embed_grad_work(uint64_t n, uint64_t width);
 size_t gd_vocab_loss_work(uint64_t n, uint64_t vocab, uint64_t width, bool with_grad);
 // Host side of the table: its size, or its bytes where `out` is given.
 size_t gd_adamw_table(const gd_adamw_tensor* t, uint32_t n, void* out);
+
+size_t gd_packed_product_work(uint64_t n, uint64_t m, uint64_t k);
+// Host side of an update's table, as gd_adamw_table; whether bytes are one; the work area that its matrices need.
+size_t gd_muon_table(const gd_muon_tensor* t, uint32_t n, void* out);
+bool gd_muon_table_fits(const void* host_table, size_t bytes);
+size_t gd_muon_work(const void* host_table, bool both);
+bool gd_muon_coefficients_fit(const double* coefficients, uint32_t steps);
 
 hipError_t gd_launch_embed(const gd_embed_args& a, hipStream_t s);
 hipError_t gd_launch_embed_grad(const gd_embed_grad_args& a, hipStream_t s);
 hipError_t gd_launch_vocab_loss(const gd_vocab_loss_args& a, hipStream_t s);
 hipError_t gd_launch_vocab_grad(const gd_vocab_grad_args& a, hipStream_t s);
 hipError_t gd_launch_adamw(const gd_adamw_args& a, hipStream_t s);
+hipError_t gd_launch_muon(const gd_muon_args& a, hipStream_t s);
+hipError_t gd_launch_pack(const gd_pack_args& a, hipStream_t s);
+hipError_t gd_launch_packed_product(const gd_packed_product_args& a, hipStream_t s);
 
 #if defined(__HIPCC__)
 // ---- what the kernels share ----------------------------------------------------------------

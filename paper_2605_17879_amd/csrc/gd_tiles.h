@@ -1,0 +1,610 @@
+// Tiled products C[q][p] = sum_k P[p][k] Q[q][k] of matrices whose rows lie along k, 128 bytes of a row (a
+// block) at a time: 64 numbers of f16, or 128 codes of 8 bits with a power of two for each row's block.
+//
+// Sixteen rows of an operand make a fragment of the matrix cores.  Here they are every fourth row: fragment i of a
+// group of 64 rows holds rows 4 c + i, lane l row c = l % 16.  So what a lane needs of four fragments lies next to each
+// other: the rows' powers of two are the four bytes of a word that the scaled instruction picks from, and of a
+// product a lane holds columns 16 (l / 16) + 4 r + i, r, i = 0..3, of the rows 4 (l % 16) + j -- sixteen numbers
+// next to each other of a row of C, four next to each other of a row of its transpose, so that both are written in whole
+// lines without an exchange between lanes.
+//
+// Which k a lane's bytes stand for does not matter to a sum as long as both operands agree: the quarter l / 16 of a
+// wave takes the 16-byte chunks l / 16 and 4 + l / 16 of a block.
+#ifndef GD_TILES_H_
+#define GD_TILES_H_
+
+#include <type_traits>
+#include <utility>
+
+#include "gd_operators.h"
+
+namespace gd_tiles {
+
+constexpr uint32_t BYTES = 128;                  // of a row in a block
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef gd_f16 f16x8 __attribute__((ext_vector_type(8)));
+typedef gd_bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef gd_bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef int i32x8 __attribute__((ext_vector_type(8)));
+typedef __attribute__((address_space(3))) void lds_void;
+
+template <int N, typename F, int... I>
+__device__ __forceinline__ void each_of(F&& f, std::integer_sequence<int, I...>) { (f(std::integral_constant<int, I>{}), ...); }
+template <int N, typename F>
+__device__ __forceinline__ void each(F&& f) { each_of<N>(f, std::make_integer_sequence<int, N>{}); }
+
+// A lane's 32 bytes of a row's block.
+struct fragment {
+    gd_u32x4 h[2];
+};
+
+// ---- the two kinds of products ---------------------------------------------------------------
+
+// Numbers of 16 bits.
+__device__ __forceinline__ f32x4 multiply_16(f16x8 p, f16x8 q, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(p, q, c, 0, 0, 0); }
+__device__ __forceinline__ f32x4 multiply_16(bf16x8 p, bf16x8 q, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(p, q, c, 0, 0, 0); }
+
+template <typename X8>
+struct of_16 {
+    static constexpr bool SCALED = false;
+    template <int I, int J>
+    static __device__ __forceinline__ f32x4 multiply(const fragment& p, const fragment& q, f32x4 c, uint32_t, uint32_t) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) c = multiply_16(__builtin_bit_cast(X8, p.h[h]), __builtin_bit_cast(X8, q.h[h]), c);
+        return c;
+    }
+};
+typedef of_16<f16x8> of_f16;
+typedef of_16<bf16x8> of_bf16;
+
+// Codes of P and of Q: 0 for e4m3, 1 for e5m2.  Byte I of `pe` is the power of two of the lane's row of P, byte J of `qe`
+// that of Q.  The 8-bit matrix cores cut the products of eight neighbouring k at 2^-13 of the largest one's power of two
+// before they add them (beside 2^16, 2^3 counts and 2^2 does not; such sums are added in fp32): results are off by 1.5e-5 of
+// themselves for normal numbers, 7e-5 for numbers of wide range.
+template <int P_CODES, int Q_CODES>
+struct of_codes {
+    static constexpr bool SCALED = true;
+    template <int I, int J>
+    static __device__ __forceinline__ f32x4 multiply(const fragment& p, const fragment& q, f32x4 c, uint32_t pe, uint32_t qe) {
+        return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(__builtin_bit_cast(i32x8, p), __builtin_bit_cast(i32x8, q), c, P_CODES, Q_CODES,
+                                                                I, (int)pe, J, (int)qe);
+    }
+};
+
+// Eight codes, from byte `from` of a fragment's half on, times 2^(e - 127): exact in bf16 (but for what lies below 2^-126).
+template <int CODES>
+__device__ __forceinline__ bf16x8 numbers_of(uint32_t lo, uint32_t hi, float two) {
+    union {
+        bf16x2 two_of[4];
+        bf16x8 x;
+    } u;
+    if constexpr (CODES == 0) {
+        u.two_of[0] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, two, false);
+        u.two_of[1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, two, true);
+        u.two_of[2] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, two, false);
+        u.two_of[3] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, two, true);
+    } else {
+        u.two_of[0] = __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8(lo, two, false);
+        u.two_of[1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8(lo, two, true);
+        u.two_of[2] = __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8(hi, two, false);
+        u.two_of[3] = __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8(hi, two, true);
+    }
+    return u.x;
+}
+// 2^(e - 127); 0 for e = 0 (all codes are zeros), NaN for 255
+__device__ __forceinline__ float power_of(uint32_t e) { return __builtin_bit_cast(float, e == 255 ? 0x7FC00000u : e << 23); }
+
+// The same products by the 16-bit matrix cores, whose sums are of fp32.
+template <int P_CODES, int Q_CODES>
+struct of_codes_in_16 {
+    static constexpr bool SCALED = true;
+    template <int FP, int FQ>
+    static __device__ __forceinline__ void multiply_all(const fragment (&p)[FP], const fragment (&q)[FQ], f32x4 (&acc)[FP][FQ], uint32_t pe, uint32_t qe) {
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {                // eight codes of each row at a time
+            bf16x8 x[FP];
+#pragma unroll
+            for (int i = 0; i < FP; ++i) x[i] = numbers_of<P_CODES>(p[i].h[w / 2][w % 2 * 2], p[i].h[w / 2][w % 2 * 2 + 1], power_of(pe >> (8 * i) & 255));
+#pragma unroll
+            for (int j = 0; j < FQ; ++j) {
+                const bf16x8 y = numbers_of<Q_CODES>(q[j].h[w / 2][w % 2 * 2], q[j].h[w / 2][w % 2 * 2 + 1], power_of(qe >> (8 * j) & 255));
+#pragma unroll
+                for (int i = 0; i < FP; ++i) acc[i][j] = multiply_16(x[i], y, acc[i][j]);
+            }
+        }
+    }
+};
+
+template <typename MUL> struct requires_all : std::false_type {};
+template <int P, int Q> struct requires_all<of_codes_in_16<P, Q>> : std::true_type {};
+
+template <typename MUL, int FP, int FQ>
+__device__ __forceinline__ void multiply_all(const fragment (&p)[FP], const fragment (&q)[FQ], f32x4 (&acc)[FP][FQ], uint32_t pe, uint32_t qe) {
+    each<FP>([&](auto of_p) {
+        each<FQ>([&](auto of_q) {
+            constexpr int i = decltype(of_p)::value, j = decltype(of_q)::value;
+            acc[i][j] = MUL::template multiply<i, j>(p[i], q[j], acc[i][j], pe, qe);
+        });
+    });
+}
+
+// ---- operands ----------------------------------------------------------------------------------
+
+struct operand {
+    const uint8_t* p;
+    uint64_t pitch;        // bytes between rows, a multiple of 16
+    uint32_t rows;         // that are there, at least one
+    uint32_t row_bytes;    // that a row has along k with all its parts, up to whole chunks of 16, at least one chunk
+    const uint8_t* exp;    // powers of two, [block][row], 4-byte aligned, or unused
+    uint64_t exp_pitch;    // a multiple of 4
+};
+
+// Where a product's blocks are: block t of `parts` parts of `blocks` each is block t % blocks of what begins at
+// p_at(part) (q_at(part)) bytes in a row.  Behind the part `shrink` - 1 the sum so far is multiplied by 2^-11.
+struct passage {
+    uint32_t blocks, parts, shrink;
+    uint32_t p0, p1, q0, q1;   // of the first two parts; a third begins with the rows
+    uint32_t ends;             // bytes of the last block that are there; 0: all
+    __device__ __forceinline__ uint32_t part_of(uint32_t t) const { return parts == 1 ? 0 : (t >= blocks) + (t >= 2 * blocks); }
+    // (by masks: a choice between two members would be read at a computed address, which keeps the struct in scratch memory)
+    static __device__ __forceinline__ uint32_t choose(uint32_t part, uint32_t a, uint32_t b) {
+        return (-(uint32_t)(part == 0) & a) | (-(uint32_t)(part == 1) & b);
+    }
+    __device__ __forceinline__ uint32_t p_at(uint32_t part) const { return choose(part, p0, p1); }
+    __device__ __forceinline__ uint32_t q_at(uint32_t part) const { return choose(part, q0, q1); }
+};
+
+constexpr float SHRINK = 0x1p-11f;
+
+// What lies behind the end of k: zeros.
+__device__ __forceinline__ void cut(fragment& f, uint32_t ends, uint32_t lane) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const int left = (int)ends - (int)((h * 4 + (lane >> 4)) * 16);
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            const int bytes = left - 4 * w;
+            f.h[h][w] &= bytes >= 4 ? 0xFFFFFFFFu : bytes <= 0 ? 0u : (1u << (8 * bytes)) - 1;
+        }
+    }
+}
+
+// s_waitcnt operands: all but `n` loads (n below 16); all LDS reads
+constexpr int loads_but(int n) { return 0x0F70 | n; }
+constexpr int LDS_READ = 0xC07F;
+
+// Loads of a workgroup of NT lanes that stage ROWS rows of an operand, straight to the LDS: chunk c of row r lies at
+// c ^ (r / 4 % 8), so that the 16 rows of a fragment fall on different banks.  What lies behind the last row's last chunk
+// comes as zeros (the buffer ends there); behind the end of another row lies the next one, which is cut off where it
+// would count.  A lane has one offset, the rest is scalar.
+template <int ROWS, int NT>
+struct stager {
+    static constexpr int LOADS = ROWS * 8 / NT, EACH = NT / 8;   // 16 bytes a lane, so many rows a load
+    const uint8_t* base;
+    uint64_t pitch;
+    uint32_t at;                                  // this lane's chunk of the first block
+    uint32_t left[LOADS];                         // bytes from a load's first row to the end, at most 2^30
+
+    __device__ __forceinline__ void init(const operand& o, uint32_t first) {
+        static_assert(EACH % 32 == 0, "rows of one lane agree in r / 4 % 8");
+        base = o.p + first * o.pitch;
+        pitch = o.pitch;
+        at = threadIdx.x / 8 * (uint32_t)o.pitch + ((threadIdx.x & 7) ^ ((threadIdx.x / 32) & 7)) * 16;
+#pragma unroll
+        for (int j = 0; j < LOADS; ++j) {
+            const uint32_t row = first + j * EACH;
+            left[j] = row < o.rows ? (uint32_t)min((o.rows - 1 - row) * o.pitch + o.row_bytes, (uint64_t)1 << 30) : 0;
+        }
+    }
+    // Block t of what begins at `part` bytes in the rows.
+    __device__ __forceinline__ void stage(uint8_t* s, uint32_t part, uint32_t t) const {
+        const uint32_t skip = part + t * BYTES;
+#pragma unroll
+        for (int j = 0; j < LOADS; ++j) {
+            const uint8_t* from = base + skip + j * EACH * pitch;
+            __amdgpu_buffer_rsrc_t rsrc =
+                __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(from), 0, left[j] > skip ? left[j] - skip : 0, 0x00020000);
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lds_void*)(s + (j * NT + (threadIdx.x & ~63u)) * 16), 16, at, 0, 0, 0);
+        }
+    }
+};
+
+// The powers of two of a block: P_ROWS bytes, then Q_ROWS, sixteen words a wave.  (A word that begins in front of the
+// last row ends behind it: it is aligned, so that it lies in the same line as the row.)
+template <int P_ROWS, int Q_ROWS, int NT>
+struct exp_stager {
+    static_assert(P_ROWS + Q_ROWS == NT, "a byte a lane");
+    const uint8_t* base;
+    uint64_t pitch;
+    uint32_t at;
+    __device__ __forceinline__ void init(const operand& p, uint32_t p0, const operand& q, uint32_t q0, uint32_t lane, uint32_t wave) {
+        const bool of_q = wave * 64 >= P_ROWS;
+        base = of_q ? q.exp : p.exp;
+        pitch = of_q ? q.exp_pitch : p.exp_pitch;
+        const uint32_t row = (of_q ? q0 + wave * 64 - P_ROWS : p0 + wave * 64) + (lane & 15) * 4;
+        at = min(row, ((of_q ? q.rows : p.rows) - 1) & ~3u);
+    }
+    __device__ __forceinline__ void stage(uint8_t* s, uint32_t t, uint32_t lane, uint32_t wave) const {
+        __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(base + t * pitch), 0, 0xFFFFFFFF, 0x00020000);
+        if (lane < 16) __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lds_void*)(s + wave * 64), 4, at, 0, 0, 0);
+    }
+};
+
+// Fragment i of the 64 rows from `row` on.
+__device__ __forceinline__ fragment read_fragment(const uint8_t* s, uint32_t row, int i, uint32_t lane) {
+    const uint32_t r = row + 4 * (lane & 15) + i;
+    fragment f;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) f.h[h] = *reinterpret_cast<const gd_u32x4*>(s + r * BYTES + (((h * 4 + (lane >> 4)) ^ (lane & 7)) * 16));
+    return f;
+}
+
+template <int FP, int FQ>
+__device__ __forceinline__ void shrink(f32x4 (&acc)[FP][FQ]) {
+#pragma unroll
+    for (int i = 0; i < FP; ++i)
+#pragma unroll
+        for (int j = 0; j < FQ; ++j) acc[i][j] *= SHRINK;
+}
+
+// ---- tiles -------------------------------------------------------------------------------------
+
+// 256 x 256 by eight waves, one workgroup a CU, two waves a SIMD that take turns: while the waves of one
+// group multiply, those of the other read their operands from the LDS, and a barrier changes the roles.  A block takes
+// two turns of a wave: Q and the upper half of P's rows, then the lower half.  The buffers of Q and of P's upper
+// half are free again behind the first turn and are filled for the block after the next at once, those of the lower
+// half behind the second: every load has three turns of both groups, one and a half blocks, to arrive.
+//
+//   turn          g0 reads    g1 reads     loads issued (each group in its reading turn)
+//   4 t           Q, upper    (lower t-1)  g0: lower t+1
+//   4 t + 1                   Q, upper     g1: lower t+1
+//   4 t + 2       lower                    g0: Q, upper t+2
+//   4 t + 3                   lower        g1: Q, upper t+2
+//
+// What is read in turns 4 t and on was issued before the latest loads of one block; the wait stands before the barrier in
+// front of the even turns, which g0 reaches multiplying and g1 reading.
+template <typename MUL>
+struct large_tile {
+    static constexpr int BP = 256, BQ = 256, WP = 2, WQ = 4, NT = 512, FP = 8, FQ = 4;
+    // The first of the 64 rows of P that fragments 4 g .. 4 g + 3 of a wave hold, and of Q.
+    static __device__ __forceinline__ uint32_t p_of(uint32_t wave, int g) { return g * 128 + (wave / WQ) * 64; }
+    static __device__ __forceinline__ uint32_t q_of(uint32_t wave) { return (wave % WQ) * 64; }
+
+    static __device__ __forceinline__ void run(const operand& op, const operand& oq, uint32_t p0, uint32_t q0, const passage& way,
+                                               f32x4 (&acc)[FP][FQ]) {
+        __shared__ __attribute__((aligned(16))) uint8_t up0[128 * BYTES], low0[128 * BYTES], sq0[BQ * BYTES];
+        __shared__ __attribute__((aligned(16))) uint8_t up1[128 * BYTES], low1[128 * BYTES], sq1[BQ * BYTES];
+        __shared__ __attribute__((aligned(16))) uint8_t se0[BP + BQ], se1[BP + BQ];
+        const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+        const uint32_t wp = wave / WQ, group = wp;           // (waves w and w + 4 share a SIMD)
+        const uint32_t blocks = way.blocks * way.parts;
+        if (blocks == 0) return;
+        constexpr int ALL = MUL::SCALED ? 9 : 8;             // loads of a wave in a block, two of them the lower half's
+        stager<128, NT> lu, ll;
+        stager<BQ, NT> lq;
+        exp_stager<BP, BQ, NT> le;
+        lu.init(op, p0);
+        ll.init(op, p0 + 128);
+        lq.init(oq, q0);
+        if (MUL::SCALED) le.init(op, p0, oq, q0, lane, wave);
+        fragment fp[4], fq[FQ];
+        uint32_t eu = 0, el = 0, eq = 0;
+        auto stage_low = [&](uint8_t* low, uint32_t t) {
+            const uint32_t part = way.part_of(t);
+            ll.stage(low, way.p_at(part), t - part * way.blocks);
+        };
+        auto stage_up = [&](uint8_t* up, uint8_t* sq, uint8_t* se, uint32_t t) {
+            const uint32_t part = way.part_of(t);
+            lq.stage(sq, way.q_at(part), t - part * way.blocks);
+            lu.stage(up, way.p_at(part), t - part * way.blocks);
+            if (MUL::SCALED) le.stage(se, t, lane, wave);
+        };
+        auto read_p = [&](const uint8_t* s) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) fp[i] = read_fragment(s, wp * 64, i, lane);
+        };
+        // `newer`: how many of the wave's loads were issued behind those that the next turn reads
+        auto turn_over = [&](bool wait, uint32_t newer) {
+            asm volatile("" ::: "memory");
+            if (wait) {
+                if (newer == ALL) __builtin_amdgcn_s_waitcnt(loads_but(ALL));
+                else if (newer == 2) __builtin_amdgcn_s_waitcnt(loads_but(2));
+                else __builtin_amdgcn_s_waitcnt(loads_but(0));
+            }
+            __builtin_amdgcn_s_barrier();
+            asm volatile("" ::: "memory");
+            __builtin_amdgcn_sched_barrier(0);
+        };
+        auto multiply_half = [&](auto first, uint32_t e) {
+            __builtin_amdgcn_s_setprio(1);
+            each<4>([&](auto i) {
+                each<FQ>([&](auto j) {
+                    constexpr int I = decltype(i)::value, J = decltype(j)::value, AT = decltype(first)::value + I;
+                    acc[AT][J] = MUL::template multiply<I, J>(fp[I], fq[J], acc[AT][J], e, eq);
+                });
+            });
+            __builtin_amdgcn_s_setprio(0);
+            __builtin_amdgcn_sched_barrier(0);
+        };
+        auto block = [&](uint8_t* up, uint8_t* low, uint8_t* sq, uint8_t* se, uint8_t* nlow, uint32_t t) {
+            const bool tail = way.ends != 0 && t + 1 == blocks;
+            const uint32_t newer_up = t + 1 < blocks ? ALL : 0, newer_low = t + 2 < blocks ? ALL : t + 1 < blocks ? 2 : 0;
+            if (t != 0 && t == way.shrink * way.blocks) shrink(acc);
+#pragma unroll
+            for (int j = 0; j < FQ; ++j) fq[j] = read_fragment(sq, q_of(wave), j, lane);
+            read_p(up);
+            if (MUL::SCALED) {
+                eu = *reinterpret_cast<const uint32_t*>(se + wp * 64 + 4 * (lane & 15));
+                el = *reinterpret_cast<const uint32_t*>(se + 128 + wp * 64 + 4 * (lane & 15));
+                eq = *reinterpret_cast<const uint32_t*>(se + BP + q_of(wave) + 4 * (lane & 15));
+            }
+            if (t > 0 && t + 1 < blocks) stage_low(nlow, t + 1);
+            if (tail) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    cut(fp[i], way.ends, lane);
+                    cut(fq[i], way.ends, lane);
+                }
+            }
+            __builtin_amdgcn_s_waitcnt(LDS_READ);
+            turn_over(group == 1, newer_up);
+            multiply_half(std::integral_constant<int, 0>{}, eu);
+            turn_over(group == 0, newer_up);
+            read_p(low);
+            if (t + 2 < blocks) stage_up(up, sq, se, t + 2);
+            if (tail) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) cut(fp[i], way.ends, lane);
+            }
+            __builtin_amdgcn_s_waitcnt(LDS_READ);
+            turn_over(group == 1, newer_low);
+            multiply_half(std::integral_constant<int, 4>{}, el);
+            turn_over(group == 0, newer_low);
+        };
+        auto start = [&](uint8_t* up, uint8_t* low, uint8_t* sq, uint8_t* se, uint8_t* nup, uint8_t* nlow, uint8_t* nsq, uint8_t* nse) {
+            stage_up(up, sq, se, 0);
+            stage_low(low, 0);
+            if (blocks > 1) {
+                stage_up(nup, nsq, nse, 1);
+                stage_low(nlow, 1);
+                __builtin_amdgcn_s_waitcnt(loads_but(ALL));
+            } else {
+                __builtin_amdgcn_s_waitcnt(loads_but(0));
+            }
+            turn_over(false, 0);
+            if (group == 1) turn_over(false, 0);             // one turn behind
+        };
+        // blocks go through the buffers in turn and end with the second one
+        uint32_t t = blocks & 1;
+        if (t) {
+            start(up1, low1, sq1, se1, up0, low0, sq0, se0);
+            block(up1, low1, sq1, se1, low0, 0);
+        } else {
+            start(up0, low0, sq0, se0, up1, low1, sq1, se1);
+        }
+        for (; t < blocks; t += 2) {
+            block(up0, low0, sq0, se0, low1, t);
+            block(up1, low1, sq1, se1, low0, t + 1);
+        }
+        if (group == 0) turn_over(false, 0);
+    }
+};
+
+// 128 x 128 by four waves, two workgroups a CU.  A step multiplies one fragment of P by the wave's four of Q; P's are read
+// three steps ahead, Q's a block ahead, so that the matrix cores do not wait for the LDS behind the barrier.
+template <typename MUL>
+struct small_tile {
+    static constexpr int BP = 128, BQ = 128, WP = 2, WQ = 2, NT = 256, FP = 4, FQ = 4;
+    static __device__ __forceinline__ uint32_t p_of(uint32_t wave, int) { return (wave / WQ) * 64; }
+    static __device__ __forceinline__ uint32_t q_of(uint32_t wave) { return (wave % WQ) * 64; }
+
+    static __device__ __forceinline__ void run(const operand& op, const operand& oq, uint32_t p0, uint32_t q0, const passage& way,
+                                               f32x4 (&acc)[FP][FQ]) {
+        __shared__ __attribute__((aligned(16))) uint8_t sp0[BP * BYTES], sq0[BQ * BYTES], se0[BP + BQ];
+        __shared__ __attribute__((aligned(16))) uint8_t sp1[BP * BYTES], sq1[BQ * BYTES], se1[BP + BQ];
+        const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+        const uint32_t blocks = way.blocks * way.parts;
+        if (blocks == 0) return;
+        stager<BP, NT> lp;
+        stager<BQ, NT> lq;
+        exp_stager<BP, BQ, NT> le;
+        lp.init(op, p0);
+        lq.init(oq, q0);
+        if (MUL::SCALED) le.init(op, p0, oq, q0, lane, wave);
+        auto stage = [&](uint8_t* sp, uint8_t* sq, uint8_t* se, uint32_t t) {
+            const uint32_t part = way.part_of(t);
+            lp.stage(sp, way.p_at(part), t - part * way.blocks);
+            lq.stage(sq, way.q_at(part), t - part * way.blocks);
+            if (MUL::SCALED) le.stage(se, t, lane, wave);
+        };
+        fragment fp[4], fq[2][FQ];
+        uint32_t ep[2] = {0, 0}, eq[2] = {0, 0};
+        auto read_q = [&](const uint8_t* sq, const uint8_t* se, int b) {
+#pragma unroll
+            for (int j = 0; j < FQ; ++j) fq[b][j] = read_fragment(sq, q_of(wave), j, lane);
+            if (MUL::SCALED) {
+                ep[b] = *reinterpret_cast<const uint32_t*>(se + p_of(wave, 0) + 4 * (lane & 15));
+                eq[b] = *reinterpret_cast<const uint32_t*>(se + BP + q_of(wave) + 4 * (lane & 15));
+            }
+        };
+        // What every wave has staged is there behind this: the wait for a wave's own loads is written out, a barrier orders
+        // only what goes through registers.
+        auto staged_by_all = [&]() {
+            __builtin_amdgcn_s_waitcnt(loads_but(0));
+            __syncthreads();
+        };
+        // Block t from the buffers of b, then the first fragments of the one behind it from the others: where there is
+        // none they are read for nothing.
+        auto block = [&](auto b, uint8_t* sp, uint8_t* sq, uint8_t* se, uint8_t* np, uint8_t* nq, uint8_t* ne, uint32_t t) {
+            const bool tail = way.ends != 0 && t + 1 == blocks;
+            if (t != 0 && t == way.shrink * way.blocks) shrink(acc);
+            if (tail) {
+#pragma unroll
+                for (int j = 0; j < FQ; ++j) cut(fq[b][j], way.ends, lane);
+            }
+            each<4>([&](auto step) {
+                constexpr int i = decltype(step)::value, B = decltype(b)::value;
+                if (i == 0) fp[3] = read_fragment(sp, p_of(wave, 0), 3, lane);
+                if (i == 1) {
+                    staged_by_all();                         // (the next block is there, this one read by all)
+                    if (t + 2 < blocks) stage(sp, sq, se, t + 2);
+                    read_q(nq, ne, 1 - B);
+                }
+                if (tail) cut(fp[i], way.ends, lane);
+                each<FQ>([&](auto of_q) {
+                    constexpr int j = decltype(of_q)::value;
+                    acc[i][j] = MUL::template multiply<i, j>(fp[i], fq[B][j], acc[i][j], ep[B], eq[B]);
+                });
+                if (i > 0) fp[(i + 3) % 4] = read_fragment(np, p_of(wave, 0), (i + 3) % 4, lane);
+                __builtin_amdgcn_sched_barrier(0);
+            });
+        };
+        auto start = [&](int b, uint8_t* sp, uint8_t* sq, uint8_t* se, uint8_t* np, uint8_t* nq, uint8_t* ne) {
+            stage(sp, sq, se, 0);
+            staged_by_all();
+            if (blocks > 1) stage(np, nq, ne, 1);
+            read_q(sq, se, b);
+#pragma unroll
+            for (int i = 0; i < 3; ++i) fp[i] = read_fragment(sp, p_of(wave, 0), i, lane);
+        };
+        const std::integral_constant<int, 0> zero;
+        const std::integral_constant<int, 1> one;
+        uint32_t t = blocks & 1;
+        if (t) {
+            start(1, sp1, sq1, se1, sp0, sq0, se0);
+            block(one, sp1, sq1, se1, sp0, sq0, se0, 0);
+        } else {
+            start(0, sp0, sq0, se0, sp1, sq1, se1);
+        }
+        for (; t < blocks; t += 2) {
+            block(zero, sp0, sq0, se0, sp1, sq1, se1, t);
+            block(one, sp1, sq1, se1, sp0, sq0, se0, t + 1);
+        }
+        __syncthreads();                                     // (the last block read for the next by all)
+    }
+};
+
+// 64 x 16 FQ by eight waves that share k and read their operands from memory straight into registers; what the waves
+// have summed is joined in the LDS, in their order.  For products of few tiles, and of few rows of Q, where every byte of
+// P is read once.  Fragments of Q hold rows FQ c + j.
+template <typename MUL, int FQ_>
+struct direct_tile {
+    static constexpr int FP = 4, FQ = FQ_, BP = 64, BQ = 16 * FQ, WAVES = 8, NT = 64 * WAVES;
+
+    typedef f32x4 sums[FQ][FP][64];
+    // Blocks from `first` up to `end`.  Behind it waves 0 .. FQ - 1 have the sums of column j = wave in `sum`, the others nothing.
+    // Returned: room in the LDS that the waves have read (each its own column j of each wave's sums).
+    static __device__ __forceinline__ sums* run(const operand& op, const operand& oq, uint32_t p0, uint32_t q0, const passage& way,
+                                               uint32_t first, uint32_t end, f32x4 (&sum)[FP]) {
+        __shared__ __attribute__((aligned(16))) sums shared[WAVES];
+        const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+        const uint32_t blocks = way.blocks * way.parts, c = lane & 15;
+        f32x4 acc[FP][FQ] = {};
+        struct loaded {
+            fragment p[FP], q[FQ];
+            uint32_t pe, qe;
+        };
+        // A lane's rows are FP c + i of P, FQ c + j of Q: one offset, and for each i a buffer that begins a row further on.
+        const uint32_t p_row = min(p0 + FP * c, (op.rows - 1) & ~3u), q_row = min(q0 + FQ * c, oq.rows - 1);
+        const uint32_t p_off = FP * c * (uint32_t)op.pitch + (lane >> 4) * 16, q_off = FQ * c * (uint32_t)oq.pitch + (lane >> 4) * 16;
+        uint32_t p_left[FP], q_left[FQ];
+        auto left_of = [](const operand& o, uint32_t row) {
+            return row < o.rows ? (uint32_t)min((o.rows - 1 - row) * o.pitch + o.row_bytes, (uint64_t)1 << 30) : 0;
+        };
+#pragma unroll
+        for (int i = 0; i < FP; ++i) p_left[i] = left_of(op, p0 + i);
+#pragma unroll
+        for (int j = 0; j < FQ; ++j) q_left[j] = left_of(oq, q0 + j);
+        auto chunk_of = [](const operand& o, uint32_t row, uint32_t skip, uint32_t left, uint32_t off) {
+            const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(o.p + row * o.pitch + skip), 0,
+                                                                                  left > skip ? left - skip : 0, 0x00020000);
+            return __builtin_bit_cast(gd_u32x4, __builtin_amdgcn_raw_buffer_load_b128(rsrc, off, 0, 0));
+        };
+        auto load = [&](loaded& l, uint32_t t) {
+            const uint32_t part = way.part_of(t), in = (t - part * way.blocks) * BYTES;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+#pragma unroll
+                for (int i = 0; i < FP; ++i) l.p[i].h[h] = chunk_of(op, p0 + i, in + way.p_at(part), p_left[i], p_off + h * 64);
+#pragma unroll
+                for (int j = 0; j < FQ; ++j) l.q[j].h[h] = chunk_of(oq, q0 + j, in + way.q_at(part), q_left[j], q_off + h * 64);
+            }
+            if (MUL::SCALED) {
+                l.pe = *reinterpret_cast<const uint32_t*>(op.exp + t * op.exp_pitch + p_row);
+                const uint8_t* qe = oq.exp + t * oq.exp_pitch;
+                if (FQ == 4) {
+                    l.qe = *reinterpret_cast<const uint32_t*>(qe + (q_row & ~3u));
+                } else {
+                    l.qe = 0;
+#pragma unroll
+                    for (int j = 0; j < FQ; ++j) l.qe |= (uint32_t)qe[min(q0 + FQ * c + j, oq.rows - 1)] << (8 * j);
+                }
+            }
+        };
+        auto multiply = [&](loaded& l, uint32_t t) {
+            if (way.ends != 0 && t + 1 == blocks) {
+#pragma unroll
+                for (int i = 0; i < FP; ++i) cut(l.p[i], way.ends, lane);
+#pragma unroll
+                for (int j = 0; j < FQ; ++j) cut(l.q[j], way.ends, lane);
+            }
+            if constexpr (requires_all<MUL>::value) MUL::multiply_all(l.p, l.q, acc, l.pe, l.qe);
+            else multiply_all<MUL>(l.p, l.q, acc, l.pe, l.qe);
+        };
+        // (a wave that goes past the part that shrinks does so once; one that has no block there scales zeros, or at the end)
+        bool whole = way.shrink == 0;
+        auto pass = [&](uint32_t t) {
+            if (!whole && t >= way.shrink * way.blocks) {
+                shrink(acc);
+                whole = true;
+            }
+        };
+        loaded a, b;
+        uint32_t t = first + wave;
+        if (t < end) load(a, t);
+        while (t < end) {
+            if (t + WAVES < end) load(b, t + WAVES);
+            pass(t);
+            multiply(a, t);
+            t += WAVES;
+            if (t >= end) break;
+            if (t + WAVES < end) load(a, t + WAVES);
+            pass(t);
+            multiply(b, t);
+            t += WAVES;
+        }
+        if (!whole) shrink(acc);
+#pragma unroll
+        for (int i = 0; i < FP; ++i)
+#pragma unroll
+            for (int j = 0; j < FQ; ++j) shared[wave][j][i][lane] = acc[i][j];
+        __syncthreads();
+        if (wave < FQ) {
+#pragma unroll
+            for (int i = 0; i < FP; ++i) {
+                sum[i] = shared[0][wave][i][lane];
+#pragma unroll
+                for (int w = 1; w < WAVES; ++w) sum[i] += shared[w][wave][i][lane];
+            }
+        }
+        return shared;
+    }
+};
+
+// Tiles in an order in which those that run at the same time share operands: workgroups go to the
+// eight chiplets in turn, each takes a stretch of the tiles, walked in strips of STRIP tiles of q.
+__device__ __forceinline__ uint32_t stretch_of(uint32_t b, uint32_t tiles) {
+    const uint32_t chip = b & 7, each = tiles / 8, more = tiles % 8;
+    return chip * each + min(chip, more) + b / 8;
+}
+template <uint32_t STRIP>
+__device__ __forceinline__ void tile_of(uint32_t t, uint32_t tiles_p, uint32_t tiles_q, uint32_t& tp, uint32_t& tq) {
+    const uint32_t strip = t / (STRIP * tiles_p), in = t - strip * STRIP * tiles_p;
+    const uint32_t width = min(STRIP, tiles_q - strip * STRIP);
+    tq = strip * STRIP + in % width;
+    tp = in / width;
+}
+
+}  // namespace gd_tiles
+#endif  // GD_TILES_H_

@@ -1,0 +1,683 @@
+// Update of matrices by their orthogonalised momentum.  For a matrix W with gradient G and momentum M, all
+// of them of many matrices at once:
+//
+//   M = mu M + G;  U = G + mu M, or M;  X = U / (|U| + eps), |U| the root of the sum of squares
+//   steps times:  X = a X + (b A + c A^2) X,  A = X X^T        (of the shorter side: X^T X for tall matrices)
+//   W = W (1 - lr decay) - lr X
+//
+// An odd polynomial p(s) = a s + b s^3 + c s^5 is applied to the singular values of X: those of the first step lie in (0, 1],
+// the coefficients bring them towards 1.
+//
+// The matrix cores bound it: 2 a^2 b numbers are multiplied for A, half of them since A is symmetric, a^3 likewise for
+// A^2, and a^2 b for the product with X.  They take f16; X, A and B = b A + c A^2 are kept in numbers of f16 times a power of two
+// that their largest singular values allow, as hi + 2^-11 lo, and a product is one of
+//   GD_F32   lo hi + hi lo + hi hi: 22 digits of each operand
+//   GD_F16   hi hi of A and A^2, B hi (X lo + X hi).  X itself needs its lo: what rounding drops of it would lie in directions
+//            whose singular values are small, and grow with them, up to a^steps = 485 times (a matrix of 16 strong directions over a
+//            floor of noise: 1.1e-2 off with X in f16, 1.5e-4 with hi + lo; bf16 9e-2).
+//
+// Every product is C[q][p] = sum_k P[p][k] Q[q][k] of rows that lie along k, so X is kept both ways, R as the matrix lies and
+// C transposed; a lane's part of a tile is written both ways in whole lines (gd_tiles.h).  Symmetric products are computed on and
+// above the diagonal of tiles and written to both sides.  One launch does a step's product for all matrices.
+#include <algorithm>
+#include <cmath>
+#include <cstring>
+#include <vector>
+
+#include "gd_tiles.h"
+
+namespace {
+
+using namespace gd_tiles;
+
+constexpr float ONE_X = 0x1p15f;                   // X and A are kept times 2^15: below 65 504 for values below 1.99
+constexpr uint32_t CHUNKS = 1024;                  // most pieces of a matrix that its sum of squares is taken in
+constexpr uint32_t CHUNK = 4096;                   // elements of a piece: a multiple of it
+enum { LARGE, SMALL, DIRECT, KINDS };
+constexpr uint32_t EDGE[KINDS] = {256, 128, 64};
+
+// ---- the table ---------------------------------------------------------------------------------
+
+struct entry {
+    void* param;  const void* grad;  float* m;  void* copy;
+    double lr_scale, decay;
+    uint32_t rows, cols;
+    uint32_t param_type, grad_type, copy_type;
+    uint32_t chunks, chunk;       // pieces, and elements of one
+    uint32_t partial;             // the first of its sums
+    uint64_t at[2];               // where its matrices begin in the work area, with products of f32 and of f16
+};
+
+struct head {
+    uint64_t bytes;
+    uint32_t magic, n;
+    uint32_t first[KINDS + 1];    // entries of a kind of tiles
+    uint32_t half[KINDS], full[KINDS];   // tiles of a symmetric product, and of the others
+    uint32_t chunks, tiles;       // pieces of all matrices, and 64 x 64 of them
+    uint64_t work[2];
+};
+constexpr uint32_t MAGIC = 0x6D756F6E;
+enum { OF_CHUNKS, OF_TILES, OF_HALF, OF_FULL, LISTS };   // lists of what begins where, one number an entry
+
+constexpr uint64_t HEAD = 256;
+static_assert(sizeof(head) <= HEAD, "the table's head");
+
+__host__ __device__ inline uint64_t up_to(uint64_t v, uint64_t unit) { return (v + unit - 1) / unit * unit; }
+__host__ __device__ inline uint64_t list_at(uint32_t n, int list) { return HEAD + n * sizeof(entry) + (uint64_t)list * up_to(n * 4, 16); }
+
+// Where an entry's matrices lie from its place in the work area on; pitches in bytes.
+struct layout {
+    uint32_t a, b;                // the shorter and the longer side
+    uint64_t r_pitch, c_pitch, s_pitch, lo_r, lo_c, lo_s;
+    uint64_t of_r, of_c, sa, sb, total;
+    __host__ __device__ layout(uint32_t rows, uint32_t cols, bool both) {
+        a = rows < cols ? rows : cols;
+        b = rows < cols ? cols : rows;
+        lo_r = up_to(cols, 64) * 2; lo_c = up_to(rows, 64) * 2; lo_s = up_to(a, 64) * 2;
+        r_pitch = 2 * lo_r; c_pitch = 2 * lo_c; s_pitch = both ? 2 * lo_s : lo_s;
+        of_r = up_to(rows * r_pitch, 256);
+        of_c = up_to(cols * c_pitch, 256);
+        const uint64_t of_s = up_to(a * s_pitch, 256);
+        sa = 2 * (of_r + of_c);
+        sb = sa + of_s;
+        total = sb + of_s;
+    }
+    // The first and the second X, as the matrix lies and transposed.
+    __host__ __device__ uint64_t r(uint32_t i) const { return i * of_r; }
+    __host__ __device__ uint64_t c(uint32_t i) const { return 2 * of_r + i * of_c; }
+};
+
+struct muon_args {
+    const uint8_t* table;
+    uint32_t n, first, count;     // entries; of the launch's kind
+    uint8_t* work;
+    const float* grad_scale;
+    uint32_t both;                // products of f32
+    uint32_t from, to;            // which of the two X is read and written
+    float a, b, c, one_b;         // coefficients, and the power of two that B is kept times
+    float mu;
+    double eps;
+    uint32_t nesterov;
+    double lr;
+};
+
+// An entry, in scalar registers.
+__device__ __forceinline__ entry entry_at(const muon_args& g, uint32_t i) {
+    const uint32_t* from = reinterpret_cast<const uint32_t*>(g.table + HEAD + i * sizeof(entry));
+    struct words {
+        uint32_t w[sizeof(entry) / 4];
+    } x;
+#pragma unroll
+    for (uint32_t k = 0; k < sizeof(entry) / 4; ++k) x.w[k] = __builtin_amdgcn_readfirstlane(from[k]);
+    return __builtin_bit_cast(entry, x);
+}
+
+// Which of `count` entries from `first` on has number t of a list, t less where it begins: the last that does not begin behind it.
+__device__ __forceinline__ uint32_t find(const muon_args& g, int list, uint32_t first, uint32_t count, uint32_t& t) {
+    const uint32_t* at = reinterpret_cast<const uint32_t*>(g.table + list_at(g.n, list)) + first;
+    const uint32_t lane = threadIdx.x & 63;
+    uint32_t before = 0;
+    for (uint32_t i = 0; i < count; i += 64) {
+        const uint64_t begun = __ballot(i + lane < count && at[min(i + lane, count - 1)] <= t);
+        before += (uint32_t)__popcll(begun);
+        if (begun != ~0ull) break;
+    }
+    const uint32_t k = __builtin_amdgcn_readfirstlane(before - 1);
+    t -= __builtin_amdgcn_readfirstlane(at[k]);
+    return first + k;
+}
+
+// Whether gradients are to be used at all; their factor.
+__device__ __forceinline__ bool factor_of(const muon_args& g, float& f) {
+    f = g.grad_scale ? *g.grad_scale : 1.0f;
+    return (__builtin_bit_cast(uint32_t, f) & 0x7F800000u) != 0x7F800000u;
+}
+
+__device__ __forceinline__ float grad_at(const entry& e, uint64_t i) {
+    return e.grad_type == GD_F32 ? static_cast<const float*>(e.grad)[i]
+         : e.grad_type == GD_BF16 ? gd_to_f32(static_cast<const gd_bf16*>(e.grad)[i]) : gd_to_f32(static_cast<const gd_f16*>(e.grad)[i]);
+}
+
+// ---- momentum and norm ---------------------------------------------------------------------------
+
+// U from the new momentum.
+__device__ __forceinline__ float update_of(const muon_args& g, float grad, float m) { return g.nesterov ? grad + g.mu * m : m; }
+
+__device__ __forceinline__ double sum_of_all(double s) {
+    __shared__ double part[16];
+#pragma unroll
+    for (int d = 32; d; d /= 2) s += __shfl_xor(s, d);
+    if ((threadIdx.x & 63) == 0) part[threadIdx.x / 64] = s;
+    __syncthreads();
+    s = 0;
+    for (uint32_t w = 0; w < blockDim.x / 64; ++w) s += part[w];
+    return s;
+}
+
+template <typename T, int V>
+__device__ __forceinline__ double advance(const muon_args& g, const entry& e, uint64_t i, float f) {
+    const gd_vec<T, V> grad = gd_read<T, V>(static_cast<const T*>(e.grad) + i);
+    gd_vec<float, 4> m[V / 4];
+    double s = 0;
+#pragma unroll
+    for (int h = 0; h < V / 4; ++h) {
+        m[h] = gd_read<float, 4>(e.m + i + 4 * h);
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+            const float gr = g.grad_scale ? gd_to_f32(grad.v[4 * h + x]) * f : gd_to_f32(grad.v[4 * h + x]);
+            m[h].v[x] = m[h].v[x] * g.mu + gr;
+            const double u = update_of(g, gr, m[h].v[x]);
+            s += u * u;
+        }
+    }
+#pragma unroll
+    for (int h = 0; h < V / 4; ++h) *reinterpret_cast<gd_u32x4_anywhere*>(e.m + i + 4 * h) = __builtin_bit_cast(gd_u32x4, m[h]);
+    return s;
+}
+
+// M, and the sums of squares of U, a piece a workgroup.
+__global__ __launch_bounds__(512) void momentum_kernel(const muon_args g) {
+    float f;
+    if (!factor_of(g, f)) return;
+    uint32_t t = blockIdx.x;
+    const entry e = entry_at(g, find(g, OF_CHUNKS, 0, g.n, t));
+    const uint64_t size = (uint64_t)e.rows * e.cols, from = (uint64_t)t * e.chunk, end = min(from + e.chunk, size);
+    double s = 0;
+    uint64_t i = from + threadIdx.x * 8;
+    for (; i + 8 <= end; i += 4096)
+        s += e.grad_type == GD_F32 ? advance<float, 4>(g, e, i, f) + advance<float, 4>(g, e, i + 4, f)
+           : e.grad_type == GD_BF16 ? advance<gd_bf16, 8>(g, e, i, f) : advance<gd_f16, 8>(g, e, i, f);
+    for (uint64_t j = i; j < min(i + 8, end); ++j) {
+        const float gr = g.grad_scale ? grad_at(e, j) * f : grad_at(e, j), m = e.m[j] * g.mu + gr;
+        e.m[j] = m;
+        const double u = update_of(g, gr, m);
+        s += u * u;
+    }
+    s = sum_of_all(s);
+    if (threadIdx.x == 0) reinterpret_cast<double*>(g.work)[e.partial + t] = s;
+}
+
+struct halves {
+    gd_f16 hi, lo;
+};
+__device__ __forceinline__ halves split(float x) {
+    const gd_f16 hi = (gd_f16)x;
+    return {hi, (gd_f16)((x - (float)hi) * 0x1p11f)};
+}
+__device__ __forceinline__ float whole(gd_f16 hi, gd_f16 lo) { return (float)hi + (float)lo * SHRINK; }
+
+typedef gd_f16 f16x4 __attribute__((ext_vector_type(4)));
+
+// X of the first step, 64 x 64 a workgroup, both ways, with zeros up to the end of a block of k.
+__global__ __launch_bounds__(256) void start_kernel(const muon_args g) {
+    float f;
+    if (!factor_of(g, f)) return;
+    uint32_t t = blockIdx.x;
+    const entry e = entry_at(g, find(g, OF_TILES, 0, g.n, t));
+    const double* part = reinterpret_cast<const double*>(g.work) + e.partial;
+    double s = 0;
+    for (uint32_t i = threadIdx.x; i < e.chunks; i += 256) s += part[i];
+    const double size = sqrt(sum_of_all(s)) + g.eps, scale = size == 0 ? 0 : ONE_X / size;   // (in 64 bits: no gradient is too small)
+    const layout l(e.rows, e.cols, g.both);
+    uint8_t* base = g.work + e.at[!g.both];
+    const uint32_t tiles_c = (e.cols + 63) / 64, row = t / tiles_c * 64 + threadIdx.x / 16 * 4, col = t % tiles_c * 64 + threadIdx.x % 16 * 4;
+    halves x[4][4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            float u = 0;
+            if (row + i < e.rows && col + j < e.cols) {
+                const uint64_t at = (uint64_t)(row + i) * e.cols + col + j;
+                const float gr = grad_at(e, at);
+                u = (float)(update_of(g, g.grad_scale ? gr * f : gr, e.m[at]) * scale);
+            }
+            x[i][j] = split(u);
+        }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if (row + i < e.rows) {
+            uint8_t* to = base + l.r(0) + (row + i) * l.r_pitch + col * 2;
+            *reinterpret_cast<f16x4*>(to) = f16x4{x[i][0].hi, x[i][1].hi, x[i][2].hi, x[i][3].hi};
+            *reinterpret_cast<f16x4*>(to + l.lo_r) = f16x4{x[i][0].lo, x[i][1].lo, x[i][2].lo, x[i][3].lo};
+        }
+        if (col + i < e.cols) {
+            uint8_t* to = base + l.c(0) + (col + i) * l.c_pitch + row * 2;
+            *reinterpret_cast<f16x4*>(to) = f16x4{x[0][i].hi, x[1][i].hi, x[2][i].hi, x[3][i].hi};
+            *reinterpret_cast<f16x4*>(to + l.lo_c) = f16x4{x[0][i].lo, x[1][i].lo, x[2][i].lo, x[3][i].lo};
+        }
+    }
+}
+
+// ---- products ------------------------------------------------------------------------------------
+
+enum { OF_X, OF_A, STEP, LAST };                   // A = X X^T; B = b A + c A A; X = a X + B X; the same, and W
+
+// What becomes of a tile: element (q, p) of a matrix D [rows_d][.], and of its transpose.
+struct target {
+    uint8_t* d;  uint64_t d_pitch, d_lo;           // written as it lies
+    uint8_t* t;  uint64_t t_pitch, t_lo;           // written transposed, or null
+    const uint8_t* old;                            // A or X at the same places as d
+    uint32_t rows, cols;
+    bool lo;                                       // of what is written
+    bool old_lo;                                   // of what is read
+};
+
+struct problem {
+    operand p, q;
+    passage way;
+    target out;
+};
+
+template <int PHASE>
+__device__ __forceinline__ problem problem_of(const muon_args& g, const entry& e, bool off_diagonal) {
+    const layout l(e.rows, e.cols, g.both);
+    uint8_t* base = g.work + e.at[!g.both];
+    const bool tall = e.rows > e.cols;
+    uint8_t *r0 = base + l.r(g.from), *c0 = base + l.c(g.from), *r1 = base + l.r(g.to), *c1 = base + l.c(g.to);
+    uint8_t *sa = base + l.sa, *sb = base + l.sb;
+    problem x;
+    auto matrix = [](const uint8_t* p, uint64_t pitch, uint32_t rows) { return operand{p, pitch, rows, (uint32_t)pitch, nullptr, 0}; };
+    // the part with a lo comes first
+    auto parts = [&](uint32_t n, uint64_t p_lo, uint64_t q_lo) {
+        x.way.parts = n;
+        x.way.shrink = n - 1;
+        x.way.p0 = n > 1 ? (uint32_t)p_lo : 0;
+        x.way.q1 = n > 2 ? (uint32_t)q_lo : 0;
+        x.way.p1 = x.way.q0 = 0;
+        x.way.ends = 0;
+    };
+    if (PHASE == OF_X || PHASE == OF_A) {
+        if (PHASE == OF_X) x.p = tall ? matrix(c0, l.c_pitch, l.a) : matrix(r0, l.r_pitch, l.a);
+        else x.p = matrix(sa, l.s_pitch, l.a);
+        x.q = x.p;
+        const uint64_t lo = PHASE == OF_A ? l.lo_s : tall ? l.lo_c : l.lo_r;
+        x.way.blocks = (uint32_t)(lo / BYTES);
+        parts(g.both ? 3 : 1, lo, lo);
+        uint8_t* to = PHASE == OF_X ? sa : sb;
+        x.out = target{to, l.s_pitch, l.lo_s, off_diagonal ? to : nullptr, l.s_pitch, l.lo_s, sa, l.a, l.a, g.both != 0, g.both != 0};
+    } else {
+        const operand b = matrix(sb, l.s_pitch, l.a);
+        x.way.blocks = (uint32_t)(l.lo_s / BYTES);
+        // (X first where it has a lo and B has none)
+        if (tall) {
+            x.p = b;
+            x.q = matrix(r0, l.r_pitch, e.rows);
+            parts(g.both ? 3 : 2, g.both ? l.lo_s : 0, l.lo_r);
+            if (!g.both) x.way.q0 = (uint32_t)l.lo_r;
+        } else {
+            x.p = matrix(c0, l.c_pitch, e.cols);
+            x.q = b;
+            parts(g.both ? 3 : 2, l.lo_c, l.lo_s);
+        }
+        x.out = target{r1, l.r_pitch, l.lo_r, c1, l.c_pitch, l.lo_c, r0, e.rows, e.cols, true, true};
+    }
+    return x;
+}
+
+// Sixteen columns, from `col` on, of a row: v[i][r] is column 4 r + i.  Returned: what the row becomes, as it is kept.
+template <int PHASE>
+__device__ __forceinline__ void finish_row(const muon_args& g, const entry& e, const target& o, uint32_t row, uint32_t col, f32x4 (&v)[4]) {
+    if (PHASE == OF_X) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) v[i][r] = row < o.rows && col + 4 * r + i < o.cols ? v[i][r] * (1 / ONE_X) : 0.0f;
+        return;
+    }
+    gd_vec<gd_f16, 8> hi[2] = {}, lo[2] = {};
+    if (row < o.rows && col < o.d_lo / 2) {        // (zeros up to the end of a block)
+        const gd_f16* from = reinterpret_cast<const gd_f16*>(o.old + row * o.d_pitch) + col;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            hi[h] = gd_read<gd_f16, 8>(from + 8 * h);
+            if (o.old_lo) lo[h] = gd_read<gd_f16, 8>(from + o.d_lo / 2 + 8 * h);
+        }
+    }
+#pragma unroll
+    for (int x = 0; x < 16; ++x) {
+        const float old = whole(hi[x / 8].v[x % 8], lo[x / 8].v[x % 8]);
+        float w = v[x % 4][x / 4];
+        if (PHASE == OF_A) w = (g.c * (w * (1 / (ONE_X * ONE_X))) + g.b * (old * (1 / ONE_X))) * g.one_b;
+        else w = g.a * old + w * (1 / g.one_b);
+        v[x % 4][x / 4] = row < o.rows && col + x < o.cols ? w : 0.0f;
+    }
+}
+
+__device__ __forceinline__ void write_row(const target& o, uint32_t row, uint32_t col, const f32x4 (&v)[4]) {
+    if (row >= o.rows || col >= o.d_lo / 2) return;
+    uint8_t* to = o.d + row * o.d_pitch + col * 2;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        gd_vec<gd_f16, 8> hi, lo;
+#pragma unroll
+        for (int x = 0; x < 8; ++x) {
+            const halves s = split(v[x % 4][2 * h + x / 4]);
+            hi.v[x] = s.hi;
+            lo.v[x] = s.lo;
+        }
+        *reinterpret_cast<gd_u32x4*>(to + 16 * h) = __builtin_bit_cast(gd_u32x4, hi);
+        if (o.lo) *reinterpret_cast<gd_u32x4*>(to + o.d_lo + 16 * h) = __builtin_bit_cast(gd_u32x4, lo);
+    }
+}
+
+// Four rows from `row` on of a column, written next to each other.
+__device__ __forceinline__ void write_column(const target& o, uint32_t row, uint32_t col, float x0, float x1, float x2, float x3) {
+    if (!o.t || col >= o.cols || row >= o.t_lo / 2) return;
+    uint8_t* to = o.t + col * o.t_pitch + row * 2;
+    const halves s0 = split(x0), s1 = split(x1), s2 = split(x2), s3 = split(x3);
+    *reinterpret_cast<f16x4*>(to) = f16x4{s0.hi, s1.hi, s2.hi, s3.hi};
+    if (o.lo) *reinterpret_cast<f16x4*>(to + o.t_lo) = f16x4{s0.lo, s1.lo, s2.lo, s3.lo};
+}
+
+template <typename T>
+__device__ __forceinline__ void write_param(const entry& e, uint64_t at, uint32_t there, float keep, float rate, const f32x4 (&v)[4]) {
+    T* p = static_cast<T*>(e.param) + at;
+    gd_bf16* b = e.copy && e.copy_type == GD_BF16 ? static_cast<gd_bf16*>(e.copy) + at : nullptr;
+    gd_f16* h = e.copy && e.copy_type == GD_F16 ? static_cast<gd_f16*>(e.copy) + at : nullptr;
+    constexpr int V = 16 / sizeof(T);
+    if (there >= 16) {
+        float x[16];
+#pragma unroll
+        for (int q = 0; q < 16; q += V) {
+            gd_vec<T, V> old = gd_read<T, V>(p + q);
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                x[q + i] = gd_to_f32(old.v[i]) * keep - v[(q + i) % 4][(q + i) / 4] * rate;
+                old.v[i] = gd_from_f32<T>(x[q + i]);
+            }
+            gd_write_through<T, V>(p + q, old);
+        }
+#pragma unroll
+        for (int q = 0; q < 16; q += 8) {
+            gd_vec<gd_bf16, 8> to_b;
+            gd_vec<gd_f16, 8> to_h;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                to_b.v[i] = gd_from_f32<gd_bf16>(x[q + i]);
+                to_h.v[i] = gd_from_f32<gd_f16>(x[q + i]);
+            }
+            if (b) gd_write_through<gd_bf16, 8>(b + q, to_b);
+            if (h) gd_write_through<gd_f16, 8>(h + q, to_h);
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+            if (i < there) {
+                const float x = gd_to_f32(p[i]) * keep - v[i % 4][i / 4] * rate;
+                p[i] = gd_from_f32<T>(x);
+                if (b) b[i] = gd_from_f32<gd_bf16>(x);
+                if (h) h[i] = gd_from_f32<gd_f16>(x);
+            }
+    }
+}
+
+__device__ __forceinline__ void update_row(const muon_args& g, const entry& e, uint32_t row, uint32_t col, const f32x4 (&v)[4]) {
+    if (row >= e.rows || col >= e.cols) return;
+    const double rate = g.lr * e.lr_scale;
+    const float keep = (float)(1.0 - rate * e.decay), move = (float)(rate / ONE_X);
+    const uint64_t at = (uint64_t)row * e.cols + col;
+    if (e.param_type == GD_F32) write_param<float>(e, at, e.cols - col, keep, move, v);
+    else if (e.param_type == GD_BF16) write_param<gd_bf16>(e, at, e.cols - col, keep, move, v);
+    else write_param<gd_f16>(e, at, e.cols - col, keep, move, v);
+}
+
+// Tile t of a triangle of them: column tq, row tp <= tq.
+__device__ __forceinline__ void corner_of(uint32_t t, uint32_t& tp, uint32_t& tq) {
+    uint32_t q = (uint32_t)((sqrtf(8.0f * (float)t + 1.0f) - 1.0f) * 0.5f);
+    while (q * (q + 1) / 2 > t) --q;
+    while ((q + 1) * (q + 2) / 2 <= t) ++q;
+    tq = q;
+    tp = t - q * (q + 1) / 2;
+}
+
+template <int PHASE>
+__device__ __forceinline__ entry place_of(const muon_args& g, uint32_t edge, uint32_t& tp, uint32_t& tq) {
+    constexpr bool HALF = PHASE == OF_X || PHASE == OF_A;
+    uint32_t t = stretch_of(blockIdx.x, gridDim.x);
+    const entry e = entry_at(g, find(g, HALF ? OF_HALF : OF_FULL, g.first, g.count, t));
+    if (HALF) corner_of(t, tq, tp);                // (columns at or behind the rows)
+    else tile_of<4>(t, (e.cols + edge - 1) / edge, (e.rows + edge - 1) / edge, tp, tq);
+    return e;
+}
+
+template <int PHASE, template <typename> class TILE>
+__global__ __launch_bounds__(TILE<of_f16>::NT, 512 / TILE<of_f16>::NT) void tiled_kernel(const muon_args g) {
+    typedef TILE<of_f16> tile;
+    float f;
+    if (!factor_of(g, f)) return;
+    uint32_t tp, tq;
+    const entry e = place_of<PHASE>(g, tile::BP, tp, tq);
+    const problem x = problem_of<PHASE>(g, e, tp != tq);
+    f32x4 acc[tile::FP][tile::FQ] = {};
+    tile::run(x.p, x.q, tp * tile::BP, tq * tile::BQ, x.way, acc);
+    const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    const uint32_t row = tq * tile::BQ + tile::q_of(wave) + 4 * (lane & 15);
+#pragma unroll
+    for (int h = 0; h < tile::FP / 4; ++h) {
+        const uint32_t col = tp * tile::BP + tile::p_of(wave, h) + 16 * (lane >> 4);
+        f32x4 v[4][4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[j][i] = acc[4 * h + i][j];
+            finish_row<PHASE>(g, e, x.out, row + j, col, v[j]);
+            if (PHASE == LAST) update_row(g, e, row + j, col, v[j]);
+            else write_row(x.out, row + j, col, v[j]);
+        }
+        if (PHASE != LAST) {
+#pragma unroll
+            for (int c = 0; c < 16; ++c)
+                write_column(x.out, row, col + c, v[0][c % 4][c / 4], v[1][c % 4][c / 4], v[2][c % 4][c / 4], v[3][c % 4][c / 4]);
+        }
+    }
+}
+
+template <int PHASE>
+__global__ __launch_bounds__(512, 2) void direct_kernel(const muon_args g) {
+    typedef direct_tile<of_f16, 4> tile;
+    float f;
+    if (!factor_of(g, f)) return;
+    uint32_t tp, tq;
+    const entry e = place_of<PHASE>(g, 64, tp, tq);
+    const problem x = problem_of<PHASE>(g, e, tp != tq);
+    f32x4 v[4];
+    tile::sums* room = tile::run(x.p, x.q, tp * 64, tq * 64, x.way, 0, x.way.blocks * x.way.parts, v);
+    const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    const uint32_t row = tq * 64 + 4 * (lane & 15), col = tp * 64 + 16 * (lane >> 4);
+    if (wave < 4) {
+        finish_row<PHASE>(g, e, x.out, row + wave, col, v);
+        if (PHASE == LAST) update_row(g, e, row + wave, col, v);
+        else write_row(x.out, row + wave, col, v);
+    }
+    if (PHASE == LAST || !x.out.t) return;
+    // the four rows of a lane together, for the transpose: wave r has columns 4 r .. 4 r + 3
+    if (wave < 4) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) room[0][wave][i][lane] = v[i];
+    }
+    __syncthreads();
+    if (wave < 4) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            write_column(x.out, row, col + 4 * wave + i, room[0][0][i][lane][wave], room[0][1][i][lane][wave], room[0][2][i][lane][wave], room[0][3][i][lane][wave]);
+    }
+}
+
+// steps = 0: W from X of the start.
+__global__ __launch_bounds__(256) void apply_kernel(const muon_args g) {
+    float f;
+    if (!factor_of(g, f)) return;
+    uint32_t t = blockIdx.x;
+    const entry e = entry_at(g, find(g, OF_TILES, 0, g.n, t));
+    const layout l(e.rows, e.cols, g.both);
+    const uint8_t* base = g.work + e.at[!g.both] + l.r(0);
+    const uint32_t tiles_c = (e.cols + 63) / 64, row = t / tiles_c * 64 + threadIdx.x / 4, col = t % tiles_c * 64 + threadIdx.x % 4 * 16;
+    if (row >= e.rows || col >= e.cols) return;
+    const gd_f16* from = reinterpret_cast<const gd_f16*>(base + row * l.r_pitch) + col;
+    f32x4 v[4];
+#pragma unroll
+    for (int x = 0; x < 16; ++x) v[x % 4][x / 4] = whole(from[x], from[l.lo_r / 2 + x]);
+    update_row(g, e, row, col, v);
+}
+
+template <int PHASE>
+void launch_phase(muon_args g, const head& h, hipStream_t s) {
+    const uint32_t* tiles = PHASE == OF_X || PHASE == OF_A ? h.half : h.full;
+    for (int k = 0; k < KINDS; ++k) {
+        if (!tiles[k]) continue;
+        g.first = h.first[k];
+        g.count = h.first[k + 1] - h.first[k];
+        if (k == LARGE) tiled_kernel<PHASE, large_tile><<<tiles[k], 512, 0, s>>>(g);
+        else if (k == SMALL) tiled_kernel<PHASE, small_tile><<<tiles[k], 256, 0, s>>>(g);
+        else direct_kernel<PHASE><<<tiles[k], 512, 0, s>>>(g);
+    }
+}
+
+// Which tiles a matrix takes.
+int kind_of(uint32_t rows, uint32_t cols) {
+    const uint32_t a = std::min(rows, cols);
+    return a >= 2048 ? LARGE : a >= 512 ? SMALL : DIRECT;
+}
+
+// The largest magnitude of a polynomial c1 x + c3 x^3 + c5 x^5 (of b x^2 + c x^4 with `even`) over [0, s].
+double most_of(double c1, double c3, double c5, double s) {
+    double most = 0;
+    auto look = [&](double x2) {
+        if (x2 > 0 && x2 <= s * s) most = std::max(most, std::fabs(std::sqrt(x2) * (c1 + x2 * (c3 + x2 * c5))));
+    };
+    look(s * s);
+    const double d = 9 * c3 * c3 - 20 * c5 * c1;
+    if (c5 == 0) {
+        if (c3 != 0) look(-c1 / (3 * c3));
+    } else if (d >= 0) {
+        look((-3 * c3 + std::sqrt(d)) / (10 * c5));
+        look((-3 * c3 - std::sqrt(d)) / (10 * c5));
+    }
+    return most;
+}
+double most_of_even(double b, double c, double s) {
+    double most = std::fabs(s * s * (b + s * s * c));
+    if (c != 0) {
+        const double x2 = -b / (2 * c);
+        if (x2 > 0 && x2 < s * s) most = std::max(most, std::fabs(x2 * (b + x2 * c)));
+    }
+    return most;
+}
+
+}  // namespace
+
+size_t gd_muon_table(const gd_muon_tensor* t, uint32_t n, void* out) {
+    std::vector<uint32_t> order[KINDS];
+    uint32_t there = 0;
+    for (uint32_t i = 0; i < n; ++i)
+        if (t[i].rows && t[i].cols) {
+            order[kind_of((uint32_t)t[i].rows, (uint32_t)t[i].cols)].push_back(i);
+            ++there;
+        }
+    const size_t bytes = gd_align256(list_at(there, LISTS));
+    uint8_t* to = static_cast<uint8_t*>(out);
+    if (to) memset(to, 0, bytes);
+    head h = {};
+    h.bytes = bytes;
+    h.magic = MAGIC;
+    h.n = there;
+    uint64_t chunks = 0, tiles = 0, work[2];
+    uint32_t k = 0;
+    // the sums of squares first
+    for (uint32_t i = 0; i < n; ++i) chunks += (t[i].rows * t[i].cols + CHUNK - 1) / CHUNK;   // (an upper bound)
+    work[0] = work[1] = gd_align256(std::min<uint64_t>(chunks, (uint64_t)there * CHUNKS) * 8);
+    chunks = 0;
+    for (int kind = 0; kind < KINDS; ++kind) {
+        uint64_t half = 0, full = 0;
+        h.first[kind] = k;
+        for (uint32_t i : order[kind]) {
+            const gd_muon_tensor& x = t[i];
+            const uint64_t size = x.rows * x.cols, edge = EDGE[kind];
+            entry e = {};
+            e.param = x.d_param; e.grad = x.d_grad; e.m = static_cast<float*>(x.d_m); e.copy = x.d_copy;
+            e.lr_scale = x.lr_scale; e.decay = x.weight_decay;
+            e.rows = (uint32_t)x.rows; e.cols = (uint32_t)x.cols;
+            e.param_type = x.param_type; e.grad_type = x.grad_type; e.copy_type = x.copy_type;
+            e.chunk = (uint32_t)up_to((size + CHUNKS - 1) / CHUNKS, CHUNK);
+            e.chunks = (uint32_t)((size + e.chunk - 1) / e.chunk);
+            e.partial = (uint32_t)chunks;
+            const uint64_t tr = (x.rows + edge - 1) / edge, tc = (x.cols + edge - 1) / edge, ta = std::min(tr, tc);
+            if (to) {
+                const uint32_t begins[LISTS] = {(uint32_t)chunks, (uint32_t)tiles, (uint32_t)half, (uint32_t)full};
+                for (int b = 0; b < 2; ++b) e.at[b] = work[b];
+                memcpy(to + HEAD + k * sizeof(entry), &e, sizeof(e));
+                for (int b = 0; b < LISTS; ++b) memcpy(to + list_at(there, b) + 4ull * k, &begins[b], 4);
+            }
+            for (int b = 0; b < 2; ++b) work[b] += layout(e.rows, e.cols, b == 0).total;
+            chunks += e.chunks;
+            tiles += ((x.rows + 63) / 64) * ((x.cols + 63) / 64);
+            half += ta * (ta + 1) / 2;
+            full += tr * tc;
+            ++k;
+        }
+        // (launches of fewer than 2^32 threads)
+        if (half >= 1u << 23 || full >= 1u << 23) return 0;
+        h.half[kind] = (uint32_t)half;
+        h.full[kind] = (uint32_t)full;
+    }
+    if (chunks >= 1u << 23 || tiles >= 1u << 24) return 0;
+    h.first[KINDS] = k;
+    h.chunks = (uint32_t)chunks;
+    h.tiles = (uint32_t)tiles;
+    h.work[0] = work[0];
+    h.work[1] = work[1];
+    if (to) memcpy(to, &h, sizeof(h));
+    return bytes;
+}
+
+bool gd_muon_table_fits(const void* host_table, size_t bytes) {
+    head h;
+    if (bytes < HEAD) return false;
+    memcpy(&h, host_table, sizeof(h));
+    return h.magic == MAGIC && h.bytes == bytes && list_at(h.n, LISTS) <= bytes;
+}
+
+size_t gd_muon_work(const void* host_table, bool both) {
+    head h;
+    memcpy(&h, host_table, sizeof(h));
+    return h.work[both ? 0 : 1];
+}
+
+bool gd_muon_coefficients_fit(const double* c, uint32_t steps) {
+    double s = 1.001;
+    for (uint32_t i = 0; i < steps; ++i) {
+        if (!(std::isfinite(c[3 * i]) && std::isfinite(c[3 * i + 1]) && std::isfinite(c[3 * i + 2]))) return false;
+        s = most_of(c[3 * i], c[3 * i + 1], c[3 * i + 2], s) * 1.001;
+        if (!(s <= 1.35)) return false;
+    }
+    return true;
+}
+
+hipError_t gd_launch_muon(const gd_muon_args& m, hipStream_t s) {
+    head h;
+    memcpy(&h, m.host_table, sizeof(h));
+    if (h.n == 0) return hipSuccess;
+    muon_args g = {};
+    g.table = m.table; g.n = h.n; g.work = m.work; g.grad_scale = m.grad_scale;
+    g.both = m.both; g.mu = m.momentum; g.eps = m.eps; g.nesterov = m.nesterov; g.lr = m.lr;
+    momentum_kernel<<<h.chunks, 512, 0, s>>>(g);
+    start_kernel<<<h.tiles, 256, 0, s>>>(g);
+    if (m.steps == 0) apply_kernel<<<h.tiles, 256, 0, s>>>(g);
+    double most = 1.001;
+    for (uint32_t i = 0; i < m.steps; ++i) {
+        const double* c = m.coefficients + 3 * i;
+        g.a = (float)c[0]; g.b = (float)c[1]; g.c = (float)c[2];
+        // B's singular values are below `b_most`: times the largest power of two that leaves them half of f16's range
+        const double b_most = most_of_even(c[1], c[2], most);
+        g.one_b = (float)std::exp2(std::min(15.0, std::floor(std::log2(32768.0 / std::max(b_most, 1e-30)))));
+        most = most_of(c[0], c[1], c[2], most) * 1.001;
+        g.from = i & 1;
+        g.to = 1 - g.from;
+        launch_phase<OF_X>(g, h, s);
+        launch_phase<OF_A>(g, h, s);
+        if (i + 1 < m.steps) launch_phase<STEP>(g, h, s);
+        else launch_phase<LAST>(g, h, s);
+    }
+    return hipGetLastError();
+}

@@ -1,0 +1,259 @@
+// Products of packed matrices: C[n][m] = sum_k A[n][k] B[m][k], A and B codes of 8 bits with a power of two for each
+// 128 of a row, C in fp32 or rounded once, added to what is there or not.
+//
+//   C_ij = sum over blocks b of 2^(ea_bi - 127 + eb_bj - 127) sum over the block's k of a_ik b_jk
+//
+// A C of 16 bits comes from the scaled 8-bit instruction of the matrix cores, which takes 128 of k at a time with their powers
+// of two, so that a block costs what a plain 8-bit product costs.  That instruction's own sums are short (off by up
+// to 7e-5, gd_tiles.h: far below the rounding to 16 bits, 1.7e-3 for bf16 and 2.1e-4 for f16), so a C of fp32 is computed by the 16-bit matrix
+// cores, for which codes times powers of two are exact, at half the rate: the operands are written out in bf16 first, or
+// converted in registers where tiles are read straight into them.
+//
+// Rows of B are the operand P (columns of C, which a lane holds sixteen of next to each other), rows of A the operand Q.
+#include <algorithm>
+
+#include "gd_tiles.h"
+
+namespace {
+
+using namespace gd_tiles;
+
+struct product_args {
+    operand p, q;
+    passage way;
+    uint32_t n, m;                 // rows and columns of C
+    uint32_t tiles_p, tiles_q;
+    void* c;  uint64_t ldc;        // elements
+    uint32_t add;
+    float* slab;                   // splits: [split][n][m4]; null: one split
+    uint32_t m4, each;             // columns of a slab; blocks of k of a split
+};
+
+// Sixteen columns of a row of C: v[i][r] is column 4 r + i.
+__device__ __forceinline__ float column(const f32x4 (&v)[4], int e) { return v[e % 4][e / 4]; }
+
+template <typename T>
+__device__ __forceinline__ void write_row(const product_args& a, uint32_t row, uint32_t col, const f32x4 (&v)[4]) {
+    if (row >= a.n || col >= a.m) return;
+    T* to = static_cast<T*>(a.c) + row * a.ldc + col;
+    constexpr int V = 16 / sizeof(T);
+    if (col + 16 <= a.m) {
+#pragma unroll
+        for (int b = 0; b < 16; b += V) {
+            gd_vec<T, V> old, x;
+            if (a.add) old = gd_read<T, V>(to + b);
+#pragma unroll
+            for (int e = 0; e < V; ++e) x.v[e] = gd_from_f32<T>(a.add ? column(v, b + e) + gd_to_f32(old.v[e]) : column(v, b + e));
+            gd_write_through<T, V>(to + b, x);
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+            if (col + e < a.m) to[e] = gd_from_f32<T>(a.add ? column(v, e) + gd_to_f32(to[e]) : column(v, e));
+    }
+}
+
+template <typename MUL, typename T, template <typename> class TILE>
+__global__ __launch_bounds__(TILE<MUL>::NT, 512 / TILE<MUL>::NT) void tiled_kernel(const product_args a) {
+    typedef TILE<MUL> tile;
+    uint32_t tp, tq;
+    tile_of<4>(stretch_of(blockIdx.x, a.tiles_p * a.tiles_q), a.tiles_p, a.tiles_q, tp, tq);
+    f32x4 acc[tile::FP][tile::FQ] = {};
+    tile::run(a.p, a.q, tp * tile::BP, tq * tile::BQ, a.way, acc);
+    const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+#pragma unroll
+    for (int j = 0; j < tile::FQ; ++j)
+#pragma unroll
+        for (int g = 0; g < tile::FP / 4; ++g) {
+            const f32x4 v[4] = {acc[4 * g][j], acc[4 * g + 1][j], acc[4 * g + 2][j], acc[4 * g + 3][j]};
+            write_row<T>(a, tq * tile::BQ + tile::q_of(wave) + 4 * (lane & 15) + j, tp * tile::BP + tile::p_of(wave, g) + 16 * (lane >> 4), v);
+        }
+}
+
+template <typename MUL, typename T, int FQ>
+__global__ __launch_bounds__(512, 2) void direct_kernel(const product_args a) {
+    typedef direct_tile<MUL, FQ> tile;
+    const uint32_t b = blockIdx.x, tq = b % a.tiles_q, tp = b / a.tiles_q, split = blockIdx.y;
+    const uint32_t first = split * a.each, blocks = a.way.blocks;
+    f32x4 v[4];
+    tile::run(a.p, a.q, tp * tile::BP, tq * tile::BQ, a.way, first, min(first + a.each, blocks), v);
+    const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    if (wave >= FQ) return;
+    const uint32_t row = tq * tile::BQ + FQ * (lane & 15) + wave, col = tp * tile::BP + 16 * (lane >> 4);
+    if (!a.slab) {
+        write_row<T>(a, row, col, v);
+    } else if (row < a.n && col < a.m4) {
+        float* to = a.slab + (split * (uint64_t)a.n + row) * a.m4 + col;
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+            if (col + 4 * r < a.m4) *reinterpret_cast<f32x4*>(to + 4 * r) = f32x4{v[0][r], v[1][r], v[2][r], v[3][r]};
+    }
+}
+
+// The splits' sums in their order: four columns a lane.
+template <typename T>
+__global__ __launch_bounds__(256) void join_kernel(const product_args a, uint32_t splits) {
+    const uint64_t i = blockIdx.x * 256ull + threadIdx.x, each = a.m4 / 4;
+    if (i >= a.n * each) return;
+    const uint32_t row = (uint32_t)(i / each), col = (uint32_t)(i % each) * 4;
+    const float* from = a.slab + (uint64_t)row * a.m4 + col;
+    f32x4 s = *reinterpret_cast<const f32x4*>(from);
+    for (uint32_t p = 1; p < splits; ++p) s += *reinterpret_cast<const f32x4*>(from + p * (uint64_t)a.n * a.m4);
+    T* to = static_cast<T*>(a.c) + row * a.ldc + col;
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+        if (col + e < a.m) to[e] = gd_from_f32<T>(a.add ? s[e] + gd_to_f32(to[e]) : s[e]);
+}
+
+// k = 0: a sum of nothing.
+template <typename T>
+__global__ __launch_bounds__(256) void zero_kernel(const product_args a) {
+    for (uint32_t row = blockIdx.x; row < a.n; row += gridDim.x)
+        for (uint32_t col = threadIdx.x; col < a.m; col += 256) static_cast<T*>(a.c)[row * a.ldc + col] = T(0);
+}
+
+// Codes as bf16, with zeros up to the end of a block of 64: sixteen a lane.
+struct numbers_args {
+    const uint8_t* codes;  uint64_t stride;
+    const uint8_t* exp;  uint64_t exp_stride;
+    uint32_t rows, k, e5m2, pieces;    // of sixteen, of a row, to the end of a block
+    uint64_t count;                    // pieces of all rows
+    uint8_t* out;
+};
+
+__global__ __launch_bounds__(256) void numbers_kernel(const numbers_args a, const numbers_args b) {
+    uint64_t i = blockIdx.x * 256ull + threadIdx.x;
+    const bool second = i >= a.count;
+    const numbers_args& x = second ? b : a;
+    if (second) i -= a.count;
+    if (i >= x.count) return;
+    const uint32_t row = (uint32_t)(i / x.pieces), piece = (uint32_t)(i % x.pieces);
+    bf16x8 q[2] = {};
+    if (piece * 16 < x.k) {
+        gd_u32x4 w = *reinterpret_cast<const gd_u32x4*>(x.codes + row * x.stride + piece * 16);
+#pragma unroll
+        for (int h = 0; h < 4; ++h) {
+            const int bytes = (int)(x.k - piece * 16) - 4 * h;
+            w[h] &= bytes >= 4 ? 0xFFFFFFFFu : bytes <= 0 ? 0u : (1u << (8 * bytes)) - 1;
+        }
+        const float two = power_of(x.exp[piece / 8 * x.exp_stride + row]);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) q[h] = x.e5m2 ? numbers_of<1>(w[2 * h], w[2 * h + 1], two) : numbers_of<0>(w[2 * h], w[2 * h + 1], two);
+    }
+    gd_u32x4* to = reinterpret_cast<gd_u32x4*>(x.out + i * 32);
+    to[0] = __builtin_bit_cast(gd_u32x4, q[0]);
+    to[1] = __builtin_bit_cast(gd_u32x4, q[1]);
+}
+
+// ---- which tiles ------------------------------------------------------------------------------
+
+struct plan {
+    enum { LARGE, SMALL, DIRECT } kind;
+    uint32_t fq, splits, each;
+};
+
+uint32_t up(uint64_t a, uint64_t b) { return (uint32_t)((a + b - 1) / b); }
+
+plan plan_of(uint64_t n, uint64_t m, uint64_t k) {
+    const uint64_t blocks = up(k, BYTES);
+    const uint64_t large = (uint64_t)up(n, 256) * up(m, 256), small = (uint64_t)up(n, 128) * up(m, 128);
+    plan w{plan::LARGE, 4, 1, (uint32_t)blocks};
+    if (n > 64 && large >= 192) return w;
+    w.kind = plan::SMALL;
+    if (n > 64 && small >= 256) return w;
+    w.kind = plan::DIRECT;
+    w.fq = n <= 16 ? 1 : n <= 32 ? 2 : 4;
+    const uint64_t tiles = (uint64_t)up(n, 16 * w.fq) * up(m, 64);
+    // workgroups for every CU, as long as a wave keeps a few blocks
+    const uint64_t most = std::max<uint64_t>(1, blocks / 16);
+    w.splits = (uint32_t)std::min<uint64_t>(most, std::max<uint64_t>(1, 256 / tiles));
+    w.each = up(blocks, w.splits);
+    w.splits = std::max(1u, up(blocks, w.each));
+    return w;
+}
+
+// Of the splits' sums, or of the operands in bf16.
+uint64_t row_of_numbers(uint64_t k) { return (k + 63) / 64 * 128; }
+uint64_t work_bytes(const plan& w, uint64_t n, uint64_t m, uint64_t k) {
+    return w.kind != plan::DIRECT ? (n + m) * row_of_numbers(k) : w.splits > 1 ? w.splits * n * gd_align256(m * 4) : 0;
+}
+
+template <typename MUL, typename T>
+hipError_t launch_tiles(product_args& a, const plan& w, hipStream_t s) {
+    const uint32_t edge = w.kind == plan::LARGE ? 256 : 128;
+    a.tiles_p = up(a.m, edge);
+    a.tiles_q = up(a.n, edge);
+    const uint32_t tiles = a.tiles_p * a.tiles_q;
+    if (w.kind == plan::LARGE) tiled_kernel<MUL, T, large_tile><<<tiles, 512, 0, s>>>(a);
+    else tiled_kernel<MUL, T, small_tile><<<tiles, 256, 0, s>>>(a);
+    return hipGetLastError();
+}
+
+template <typename MUL, typename T>
+hipError_t launch_direct(product_args& a, const plan& w, hipStream_t s) {
+    a.tiles_p = up(a.m, 64);
+    a.tiles_q = up(a.n, 16 * w.fq);
+    a.each = w.each;
+    if (w.splits == 1) a.slab = nullptr;
+    const dim3 grid(a.tiles_p * a.tiles_q, w.splits);
+    if (w.fq == 1) direct_kernel<MUL, T, 1><<<grid, 512, 0, s>>>(a);
+    else if (w.fq == 2) direct_kernel<MUL, T, 2><<<grid, 512, 0, s>>>(a);
+    else direct_kernel<MUL, T, 4><<<grid, 512, 0, s>>>(a);
+    if (hipError_t e = hipGetLastError()) return e;
+    if (w.splits > 1) join_kernel<T><<<up((uint64_t)a.n * (a.m4 / 4), 256), 256, 0, s>>>(a, w.splits);
+    return hipGetLastError();
+}
+
+// P_CODES, Q_CODES: 1 for e5m2.
+template <int P_CODES, int Q_CODES>
+hipError_t launch(product_args& a, const plan& w, const gd_packed_product_args& g, hipStream_t s) {
+    if (w.kind == plan::DIRECT) {
+        if (g.out_type == GD_F32) return launch_direct<of_codes_in_16<P_CODES, Q_CODES>, float>(a, w, s);
+        if (g.out_type == GD_BF16) return launch_direct<of_codes<P_CODES, Q_CODES>, gd_bf16>(a, w, s);
+        return launch_direct<of_codes<P_CODES, Q_CODES>, gd_f16>(a, w, s);
+    }
+    if (g.out_type == GD_BF16) return launch_tiles<of_codes<P_CODES, Q_CODES>, gd_bf16>(a, w, s);
+    if (g.out_type == GD_F16) return launch_tiles<of_codes<P_CODES, Q_CODES>, gd_f16>(a, w, s);
+    const uint64_t pitch = row_of_numbers(g.k);
+    const uint32_t pieces = (uint32_t)(pitch / 32);
+    numbers_args x[2];
+    for (int i = 0; i < 2; ++i) {
+        operand& o = i ? a.q : a.p;
+        x[i] = numbers_args{o.p, o.pitch, o.exp, o.exp_pitch, o.rows, g.k, (uint32_t)(i ? Q_CODES : P_CODES), pieces, (uint64_t)o.rows * pieces,
+                            g.work + (i ? g.m * pitch : 0)};
+        o = operand{x[i].out, pitch, o.rows, (uint32_t)pitch, nullptr, 0};
+    }
+    numbers_kernel<<<up(x[0].count + x[1].count, 256), 256, 0, s>>>(x[0], x[1]);
+    if (hipError_t e = hipGetLastError()) return e;
+    a.way.blocks = (uint32_t)(pitch / BYTES);
+    a.way.ends = 0;
+    return launch_tiles<of_bf16, float>(a, w, s);
+}
+
+}  // namespace
+
+size_t gd_packed_product_work(uint64_t n, uint64_t m, uint64_t k) {
+    return n && m && k ? gd_align256(work_bytes(plan_of(n, m, k), n, m, k)) : 0;
+}
+
+hipError_t gd_launch_packed_product(const gd_packed_product_args& g, hipStream_t s) {
+    product_args a = {};
+    a.n = g.n; a.m = g.m;
+    a.c = g.out; a.ldc = g.out_stride; a.add = g.accumulate;
+    if (g.k == 0) {
+        if (g.accumulate) return hipSuccess;
+        const uint32_t grid = std::min<uint32_t>(g.n, 65536);
+        if (g.out_type == GD_F32) zero_kernel<float><<<grid, 256, 0, s>>>(a);
+        else zero_kernel<uint16_t><<<grid, 256, 0, s>>>(a);
+        return hipGetLastError();
+    }
+    const uint32_t row = up(g.k, 16) * 16;
+    a.p = operand{static_cast<const uint8_t*>(g.b), g.b_stride, g.m, row, g.b_exp, g.b_exp_stride};
+    a.q = operand{static_cast<const uint8_t*>(g.a), g.a_stride, g.n, row, g.a_exp, g.a_exp_stride};
+    a.way.blocks = up(g.k, BYTES); a.way.parts = 1; a.way.ends = g.k % BYTES;
+    a.slab = reinterpret_cast<float*>(g.work);
+    a.m4 = (uint32_t)(gd_align256(g.m * 4ull) / 4);
+    const plan w = plan_of(g.n, g.m, g.k);
+    if (g.a_codes == GD_E4M3) return g.b_codes == GD_E4M3 ? launch<0, 0>(a, w, g, s) : launch<1, 0>(a, w, g, s);
+    return g.b_codes == GD_E4M3 ? launch<0, 1>(a, w, g, s) : launch<1, 1>(a, w, g, s);
+}

@@ -29,10 +29,13 @@ EXPORTS = ("gd_default_config", "gd_create", "gd_destroy", "gd_state_bytes", "gd
            "gd_ledger_flags", "gd_topk_nodes_mean", "gd_set_streaming_hints", "gd_apply_membership",
            "gd_update_ledger_static", "gd_ledger_static_scratch_bytes",
            "gd_embed", "gd_embed_grad", "gd_embed_grad_work_bytes", "gd_vocab_loss", "gd_vocab_loss_grad",
-           "gd_vocab_loss_work_bytes", "gd_adamw", "gd_adamw_table_bytes", "gd_adamw_fill_table")
+           "gd_vocab_loss_work_bytes", "gd_adamw", "gd_adamw_table_bytes", "gd_adamw_fill_table",
+           "gd_pack", "gd_packed_product", "gd_packed_product_work_bytes",
+           "gd_muon", "gd_muon_table_bytes", "gd_muon_fill_table", "gd_muon_work_bytes")
 
-F32, BF16, F16, I32, I64, E4M3 = range(6)      # gd_dtype
+F32, BF16, F16, I32, I64, E4M3, E5M2, U8 = range(8)      # gd_dtype
 STATE_BLOCK = 256                              # GD_STATE_BLOCK
+PACK_BLOCK = 128                               # GD_PACK_BLOCK
 
 
 class GuardError(RuntimeError):
@@ -61,6 +64,23 @@ class _CLedgerConfig(ctypes.Structure):
 class _CMatrix(ctypes.Structure):
     _fields_ = [("d_data", ctypes.c_void_p), ("rows", ctypes.c_uint64), ("cols", ctypes.c_uint64),
                 ("stride", ctypes.c_uint64), ("dtype", ctypes.c_uint32), ("reserved", ctypes.c_uint32)]
+
+
+class _CPacked(ctypes.Structure):
+    _fields_ = [("codes", _CMatrix), ("exp", _CMatrix)]
+
+
+class _CMuonTensor(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("d_param", "d_grad", "d_m", "d_copy")] + [
+        ("rows", ctypes.c_uint64), ("cols", ctypes.c_uint64), ("lr_scale", ctypes.c_double), ("weight_decay", ctypes.c_double),
+        ("param_type", ctypes.c_uint32), ("grad_type", ctypes.c_uint32), ("copy_type", ctypes.c_uint32),
+        ("reserved", ctypes.c_uint32)]
+
+
+class _CMuonConfig(ctypes.Structure):
+    _fields_ = [("struct_size", ctypes.c_uint32), ("nesterov", ctypes.c_uint32), ("products", ctypes.c_uint32),
+                ("steps", ctypes.c_uint32), ("lr", ctypes.c_double), ("momentum", ctypes.c_double), ("eps", ctypes.c_double),
+                ("coefficients", ctypes.c_void_p)]
 
 
 class _CAdamwTensor(ctypes.Structure):
@@ -159,6 +179,21 @@ def load_library() -> ctypes.CDLL:
     lib.gd_adamw_fill_table.restype = ctypes.c_int
     lib.gd_adamw.argtypes = [vp, vp, sz, ctypes.POINTER(_CAdamwConfig), vp, vp]
     lib.gd_adamw.restype = ctypes.c_int
+    packed = ctypes.POINTER(_CPacked)
+    lib.gd_pack.argtypes = [vp, mat, i32, packed, packed, vp]
+    lib.gd_pack.restype = ctypes.c_int
+    lib.gd_packed_product_work_bytes.argtypes = [u64, u64, u64]
+    lib.gd_packed_product_work_bytes.restype = sz
+    lib.gd_packed_product.argtypes = [vp, packed, packed, mat, i32, vp, sz, vp]
+    lib.gd_packed_product.restype = ctypes.c_int
+    lib.gd_muon_table_bytes.argtypes = [vp, ctypes.POINTER(_CMuonTensor), u32]
+    lib.gd_muon_table_bytes.restype = sz
+    lib.gd_muon_fill_table.argtypes = [vp, ctypes.POINTER(_CMuonTensor), u32, vp, sz]
+    lib.gd_muon_fill_table.restype = ctypes.c_int
+    lib.gd_muon_work_bytes.argtypes = [vp, vp, sz, u32]
+    lib.gd_muon_work_bytes.restype = sz
+    lib.gd_muon.argtypes = [vp, vp, vp, sz, ctypes.POINTER(_CMuonConfig), vp, vp, sz, vp]
+    lib.gd_muon.restype = ctypes.c_int
     lib.gd_last_error.argtypes = [vp]
     lib.gd_last_error.restype = ctypes.c_char_p
     _lib = lib
@@ -203,6 +238,8 @@ class Config:
 _PACK_MATRIX = struct.Struct("=QQQQII").pack            # gd_matrix
 _PACK_ADAMW = struct.Struct("=IIddddQ").pack            # gd_adamw_config
 _ADAMW_BYTES = ctypes.sizeof(_CAdamwConfig)
+_PACK_MUON = struct.Struct("=IIIIdddQ").pack            # gd_muon_config
+_MUON_BYTES = ctypes.sizeof(_CMuonConfig)
 
 
 def _p(t) -> Optional[int]:
@@ -234,6 +271,10 @@ class Detector:
         self._vocab_loss = self._entry("gd_vocab_loss", vp, vp, vp, vp, f32, vp, vp, vp, vp, sz, vp)
         self._vocab_loss_grad = self._entry("gd_vocab_loss_grad", vp, vp, vp, vp, f32, *[vp] * 7, sz, vp)
         self._adamw = self._entry("gd_adamw", vp, vp, sz, vp, vp, vp)
+        self._pack = self._entry("gd_pack", vp, vp, ctypes.c_int32, vp, vp, vp)
+        self._packed_product = self._entry("gd_packed_product", vp, vp, vp, vp, ctypes.c_int32, vp, sz, vp)
+        self._muon = self._entry("gd_muon", vp, vp, vp, sz, vp, vp, vp, sz, vp)
+        self._codes = {torch.float8_e4m3fn: E4M3, torch.float8_e5m2: E5M2}
         self._types = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16, torch.int32: I32, torch.int64: I64}
         self.R, self.M = cfg.n_ranks, cfg.n_metrics
         self.N = self.R // cfg.gpus_per_node
@@ -591,3 +632,99 @@ class Detector:
         c = _PACK_ADAMW(_ADAMW_BYTES, (step if seed is None else seed) & 0xFFFFFFFF, lr, beta1, beta2, eps, max(step, 0))
         b = table["bytes"]
         self._check(self._adamw(self.h, b.data_ptr(), b.nbytes, c, self._vector(grad_scale, 1), self._stream(stream)))
+
+    # ---- packed matrices and their products ---------------------------------------------
+    def alloc_packed(self, rows: int, cols: int, codes: str = "e4m3") -> dict:
+        """Room for a packed matrix: codes[rows][cols] (torch's float8 type) and exp[ceil(cols / 128)][rows]."""
+        torch = self._torch
+        kind = {"e4m3": torch.float8_e4m3fn, "e5m2": torch.float8_e5m2}[codes]
+        wide = lambda n: -(-max(n, 1) // 16) * 16
+        return dict(codes=self._bytes(rows * wide(cols)).view(kind).view(rows, wide(cols))[:, :cols],
+                    exp=self._bytes(-(-cols // PACK_BLOCK) * wide(rows)).view(-1, wide(rows))[:, :rows])
+
+    def _packed(self, p: dict) -> bytes:
+        """codes[rows][cols] and exp[ceil(cols / 128)][rows] as a gd_packed."""
+        out = b""
+        for t, types in ((p["codes"], self._codes), (p["exp"], {self._torch.uint8: U8})):
+            code = types.get(t.dtype)
+            if code is None:
+                raise GuardError(4, f"packed matrices of {t.dtype} are not built")
+            (rows, cols), strides = t.shape, t.stride()
+            assert cols <= 1 or strides[1] == 1, "the elements of a row must be next to each other"
+            out += _PACK_MATRIX(self._at(t), rows, cols, strides[0] if rows > 1 else cols or 1, code, 0)
+        return out
+
+    def pack(self, x, along: Optional[dict] = None, across: Optional[dict] = None, square: bool = False, stream=None):
+        """x[n][k] into 8-bit codes with a power of two for each block of 128: along its rows, across (x transposed,
+        blocks along its columns), or both; square: one power of two for each 128 x 128."""
+        self._check(self._pack(self.h, self._matrix(x), square, None if along is None else self._packed(along),
+                               None if across is None else self._packed(across), self._stream(stream)))
+
+    def packed_product_work_bytes(self, n: int, m: int, k: int) -> int:
+        return int(self.lib.gd_packed_product_work_bytes(n, m, k))
+
+    def alloc_packed_product_work(self, n: int, m: int, k: int):
+        return self._bytes(self.packed_product_work_bytes(n, m, k))
+
+    def packed_product(self, a: dict, b: dict, out, work, accumulate: bool = False, stream=None):
+        """out[n][m] = (its old value, with accumulate) + a b^T of packed a[n][k] and b[m][k]."""
+        self._check(self._packed_product(self.h, self._packed(a), self._packed(b), self._matrix(out), accumulate,
+                                         self._at(work), work.nbytes, self._stream(stream)))
+
+    # ---- updates of matrices --------------------------------------------------------------
+    def alloc_muon_state(self, params) -> list:
+        """Fresh momenta for a list of matrices: fp32."""
+        return [self._torch.zeros(p.shape, dtype=self._f32, device=self.device) for p in params]
+
+    def muon_table(self, params, grads, momenta, copies=None, weight_decay=0.0, lr_scale=1.0) -> dict:
+        """What muon needs to know about its matrices (lists of the same length; weight_decay and lr_scale are
+        lists too, or one value for all).  It holds addresses, and keeps the memory there alive; as adamw_table, it
+        has to be made anew for tensors that have moved."""
+        torch, n = self._torch, len(params)
+        each = lambda v: list(v) if isinstance(v, (list, tuple)) else [v] * n
+        lists = [params, grads, momenta, copies if copies is not None else [None] * n, each(weight_decay), each(lr_scale)]
+        assert all(len(l) == n for l in lists)
+        rows = (_CMuonTensor * max(n, 1))()
+        for row, p, g, m, c, decay, rate in zip(rows, *lists):
+            assert p.dim() == 2, "a matrix"
+            for t in (p, g, m, c):
+                if t is not None:
+                    self._at(t)
+            assert all(t is None or (t.is_contiguous() and t.shape == p.shape) for t in (p, g, m, c))
+            assert m.dtype is self._f32
+            row.d_param, row.d_grad, row.d_m, row.d_copy = _p(p), _p(g), _p(m), _p(c)
+            row.rows, row.cols = p.shape
+            row.lr_scale, row.weight_decay = rate, decay
+            row.param_type, row.grad_type = self._type(p), self._type(g)
+            row.copy_type = BF16 if c is None else self._type(c)
+        size = int(self.lib.gd_muon_table_bytes(self.h, rows, n))
+        if size == 0:
+            raise GuardError(1, (self.lib.gd_last_error(self.h) or b"").decode())
+        host = torch.empty(size, dtype=torch.uint8)
+        self._check(self.lib.gd_muon_fill_table(self.h, rows, n, host.data_ptr(), size))
+        kept = [t.untyped_storage() for l in lists[:4] for t in l if t is not None]
+        return dict(bytes=host.to(self.device), host=host, tensors=lists, storages=kept)
+
+    def muon_work_bytes(self, table: dict, products: str = "f32") -> int:
+        host = table["host"]
+        n = int(self.lib.gd_muon_work_bytes(self.h, host.data_ptr(), host.nbytes, {"f32": F32, "f16": F16}[products]))
+        return n
+
+    def alloc_muon_work(self, table: dict, products: str = "f32"):
+        return self._bytes(self.muon_work_bytes(table, products))
+
+    def muon(self, table: dict, work, lr: float, momentum: float = 0.95, nesterov: bool = True, eps: float = 1e-7,
+             steps: int = 5, coefficients=None, products: str = "f32", grad_scale=None, stream=None):
+        """One update of every matrix of the table by its orthogonalised momentum, in place.  coefficients: (a, b, c) for
+        every step, or a list of them, one a step.  products: "f32", or "f16" for 16-bit parameters.  grad_scale: a device
+        scalar that multiplies the gradients; where it is not finite nothing is written."""
+        c, at = None, 0
+        if coefficients is not None:
+            flat = [float(v) for t in coefficients for v in t] if hasattr(coefficients[0], "__len__") else [float(v) for v in coefficients] * steps
+            assert len(flat) == 3 * steps, "three coefficients a step"
+            c = (ctypes.c_double * max(len(flat), 1))(*flat)
+            at = ctypes.addressof(c)
+        cfg = _PACK_MUON(_MUON_BYTES, bool(nesterov), {"f32": F32, "f16": F16}[products], steps, lr, momentum, eps, at)
+        b, host = table["bytes"], table["host"]
+        self._check(self._muon(self.h, host.data_ptr(), b.data_ptr(), b.nbytes, cfg, self._vector(grad_scale, 1),
+                               self._at(work), work.nbytes, self._stream(stream)))
