@@ -72,6 +72,40 @@ struct of_codes {
     }
 };
 
+// Sixteen scaled instructions, c[i][j] += p[i] q[j], in a piece of assembly: the compiler gives this instruction's sum a
+// register apart from the addend's, runs out of runs of eight registers with it, and keeps sums in scratch memory inside the loop
+// (a tile of 256 x 256: 365 registers).  The waits stand with it: 2 cycles from a vector instruction's result to its use, 20
+// from the last sum to a vector instruction that reads it, which is as long as the matrix cores take to finish.
+#define GD_SCALED(c, p, q, low, high) \
+    "v_mfma_scale_f32_16x16x128_f8f6f4 %" #c ", %" #p ", %" #q ", %" #c ", %24, %25 op_sel:[" low ",0] op_sel_hi:[" high ",0] cbsz:%26 blgp:%27\n"
+template <int P_CODES, int Q_CODES>
+__device__ __forceinline__ void multiply_sixteen(f32x4 (&c)[4][4], const fragment (&p)[4], const fragment (&q)[4], uint32_t pe, uint32_t qe) {
+    const i32x8 p0 = __builtin_bit_cast(i32x8, p[0]), p1 = __builtin_bit_cast(i32x8, p[1]), p2 = __builtin_bit_cast(i32x8, p[2]), p3 = __builtin_bit_cast(i32x8, p[3]);
+    const i32x8 q0 = __builtin_bit_cast(i32x8, q[0]), q1 = __builtin_bit_cast(i32x8, q[1]), q2 = __builtin_bit_cast(i32x8, q[2]), q3 = __builtin_bit_cast(i32x8, q[3]);
+    asm volatile("s_nop 1\n"
+            GD_SCALED(0, 16, 20, "0,0", "0,0")
+            GD_SCALED(1, 16, 21, "0,1", "0,0")
+            GD_SCALED(2, 16, 22, "0,0", "0,1")
+            GD_SCALED(3, 16, 23, "0,1", "0,1")
+            GD_SCALED(4, 17, 20, "1,0", "0,0")
+            GD_SCALED(5, 17, 21, "1,1", "0,0")
+            GD_SCALED(6, 17, 22, "1,0", "0,1")
+            GD_SCALED(7, 17, 23, "1,1", "0,1")
+            GD_SCALED(8, 18, 20, "0,0", "1,0")
+            GD_SCALED(9, 18, 21, "0,1", "1,0")
+            GD_SCALED(10, 18, 22, "0,0", "1,1")
+            GD_SCALED(11, 18, 23, "0,1", "1,1")
+            GD_SCALED(12, 19, 20, "1,0", "1,0")
+            GD_SCALED(13, 19, 21, "1,1", "1,0")
+            GD_SCALED(14, 19, 22, "1,0", "1,1")
+            GD_SCALED(15, 19, 23, "1,1", "1,1")
+                 "s_nop 15\ns_nop 3"
+                 : "+v"(c[0][0]), "+v"(c[0][1]), "+v"(c[0][2]), "+v"(c[0][3]), "+v"(c[1][0]), "+v"(c[1][1]), "+v"(c[1][2]), "+v"(c[1][3]),
+                   "+v"(c[2][0]), "+v"(c[2][1]), "+v"(c[2][2]), "+v"(c[2][3]), "+v"(c[3][0]), "+v"(c[3][1]), "+v"(c[3][2]), "+v"(c[3][3])
+                 : "v"(p0), "v"(p1), "v"(p2), "v"(p3), "v"(q0), "v"(q1), "v"(q2), "v"(q3), "v"(pe), "v"(qe), "n"(P_CODES), "n"(Q_CODES));
+}
+#undef GD_SCALED
+
 // Eight codes, from byte `from` of a fragment's half on, times 2^(e - 127): exact in bf16 (but for what lies below 2^-126).
 template <int CODES>
 __device__ __forceinline__ bf16x8 numbers_of(uint32_t lo, uint32_t hi, float two) {
@@ -116,6 +150,23 @@ struct of_codes_in_16 {
     }
 };
 
+// The same of sums a fragment of P apart.
+template <typename MUL> struct sixteen {
+    static __device__ __forceinline__ void multiply(f32x4 (&c)[4][4], const fragment (&p)[4], const fragment (&q)[4], uint32_t pe, uint32_t qe) {
+        each<4>([&](auto of_p) {
+            each<4>([&](auto of_q) {
+                constexpr int i = decltype(of_p)::value, j = decltype(of_q)::value;
+                c[i][j] = MUL::template multiply<i, j>(p[i], q[j], c[i][j], pe, qe);
+            });
+        });
+    }
+};
+template <int P, int Q> struct sixteen<of_codes<P, Q>> {
+    static __device__ __forceinline__ void multiply(f32x4 (&c)[4][4], const fragment (&p)[4], const fragment (&q)[4], uint32_t pe, uint32_t qe) {
+        multiply_sixteen<P, Q>(c, p, q, pe, qe);
+    }
+};
+
 template <typename MUL> struct requires_all : std::false_type {};
 template <int P, int Q> struct requires_all<of_codes_in_16<P, Q>> : std::true_type {};
 
@@ -157,17 +208,32 @@ struct passage {
 
 constexpr float SHRINK = 0x1p-11f;
 
-// What lies behind the end of k: zeros.
+// Of a row's chunk in the last block, of which `ends` bytes are there: zeros behind them.
+__device__ __forceinline__ void cut(gd_u32x4& x, uint32_t ends, uint32_t chunk) {
+    const int left = (int)ends - (int)(chunk * 16);
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+        const int bytes = left - 4 * w;
+        x[w] &= bytes >= 4 ? 0xFFFFFFFFu : bytes <= 0 ? 0u : (1u << (8 * bytes)) - 1;
+    }
+}
 __device__ __forceinline__ void cut(fragment& f, uint32_t ends, uint32_t lane) {
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-        const int left = (int)ends - (int)((h * 4 + (lane >> 4)) * 16);
-#pragma unroll
-        for (int w = 0; w < 4; ++w) {
-            const int bytes = left - 4 * w;
-            f.h[h][w] &= bytes >= 4 ? 0xFFFFFFFFu : bytes <= 0 ? 0u : (1u << (8 * bytes)) - 1;
-        }
-    }
+    for (int h = 0; h < 2; ++h) cut(f.h[h], ends, h * 4 + (lane >> 4));
+}
+
+// Bytes from a row on to the end of an operand, at most 2^30, and a pointer, in scalar registers: a buffer's description in
+// vector registers would be loaded with in a loop over the lanes.
+__device__ __forceinline__ uint32_t left_of(const operand& o, uint32_t row) {
+    const uint64_t left = (o.rows - 1 - row) * o.pitch + o.row_bytes;
+    return __builtin_amdgcn_readfirstlane(row >= o.rows ? 0u : left >> 30 ? 1u << 30 : (uint32_t)left);
+}
+// What is left behind `skip` bytes.  (Signed: the difference of unsigned numbers that ends at 0 is a vector instruction.)
+__device__ __forceinline__ int behind(uint32_t left, uint32_t skip) { return max((int)left - (int)skip, 0); }
+__device__ __forceinline__ const uint8_t* scalar(const uint8_t* p) {
+    const uint64_t a = reinterpret_cast<uint64_t>(p);
+    return reinterpret_cast<const uint8_t*>((uint64_t)__builtin_amdgcn_readfirstlane((uint32_t)(a >> 32)) << 32 |
+                                            (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)a));
 }
 
 // s_waitcnt operands: all but `n` loads (n below 16); all LDS reads
@@ -188,14 +254,11 @@ struct stager {
 
     __device__ __forceinline__ void init(const operand& o, uint32_t first) {
         static_assert(EACH % 32 == 0, "rows of one lane agree in r / 4 % 8");
-        base = o.p + first * o.pitch;
+        base = scalar(o.p + first * o.pitch);
         pitch = o.pitch;
         at = threadIdx.x / 8 * (uint32_t)o.pitch + ((threadIdx.x & 7) ^ ((threadIdx.x / 32) & 7)) * 16;
 #pragma unroll
-        for (int j = 0; j < LOADS; ++j) {
-            const uint32_t row = first + j * EACH;
-            left[j] = row < o.rows ? (uint32_t)min((o.rows - 1 - row) * o.pitch + o.row_bytes, (uint64_t)1 << 30) : 0;
-        }
+        for (int j = 0; j < LOADS; ++j) left[j] = left_of(o, first + j * EACH);
     }
     // Block t of what begins at `part` bytes in the rows.
     __device__ __forceinline__ void stage(uint8_t* s, uint32_t part, uint32_t t) const {
@@ -204,8 +267,21 @@ struct stager {
         for (int j = 0; j < LOADS; ++j) {
             const uint8_t* from = base + skip + j * EACH * pitch;
             __amdgpu_buffer_rsrc_t rsrc =
-                __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(from), 0, left[j] > skip ? left[j] - skip : 0, 0x00020000);
+                __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(from), 0, behind(left[j], skip), 0x00020000);
             __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lds_void*)(s + (j * NT + (threadIdx.x & ~63u)) * 16), 16, at, 0, 0, 0);
+        }
+    }
+    // The last block, of which `ends` bytes are there: through registers, with zeros behind them.  (Every load before these is
+    // there behind it too: they return in order.  What is written has to be waited for.)
+    __device__ __forceinline__ void stage_end(uint8_t* s, uint32_t t, uint32_t ends) const {
+        const uint32_t skip = t * BYTES, chunk = (threadIdx.x & 7) ^ ((threadIdx.x / 32) & 7);
+#pragma unroll
+        for (int j = 0; j < LOADS; ++j) {
+            const __amdgpu_buffer_rsrc_t rsrc =
+                __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(base + skip + j * EACH * pitch), 0, behind(left[j], skip), 0x00020000);
+            gd_u32x4 x = __builtin_bit_cast(gd_u32x4, __builtin_amdgcn_raw_buffer_load_b128(rsrc, at, 0, 0));
+            cut(x, ends, chunk);
+            *reinterpret_cast<gd_u32x4*>(s + (j * NT + threadIdx.x) * 16) = x;
         }
     }
 };
@@ -220,8 +296,8 @@ struct exp_stager {
     uint32_t at;
     __device__ __forceinline__ void init(const operand& p, uint32_t p0, const operand& q, uint32_t q0, uint32_t lane, uint32_t wave) {
         const bool of_q = wave * 64 >= P_ROWS;
-        base = of_q ? q.exp : p.exp;
-        pitch = of_q ? q.exp_pitch : p.exp_pitch;
+        base = scalar(of_q ? q.exp : p.exp);
+        pitch = (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)(of_q ? q.exp_pitch : p.exp_pitch));
         const uint32_t row = (of_q ? q0 + wave * 64 - P_ROWS : p0 + wave * 64) + (lane & 15) * 4;
         at = min(row, ((of_q ? q.rows : p.rows) - 1) & ~3u);
     }
@@ -290,15 +366,22 @@ struct large_tile {
         if (MUL::SCALED) le.init(op, p0, oq, q0, lane, wave);
         fragment fp[4], fq[FQ];
         uint32_t eu = 0, el = 0, eq = 0;
-        auto stage_low = [&](uint8_t* low, uint32_t t) {
+        // `inner`: this is not the last block
+        auto stage_low = [&](bool inner, uint8_t* low, uint32_t t) {
             const uint32_t part = way.part_of(t);
-            ll.stage(low, way.p_at(part), t - part * way.blocks);
+            if (MUL::SCALED && !inner && way.ends != 0 && t + 1 == blocks) ll.stage_end(low, t, way.ends);
+            else ll.stage(low, way.p_at(part), t - part * way.blocks);
         };
-        auto stage_up = [&](uint8_t* up, uint8_t* sq, uint8_t* se, uint32_t t) {
+        auto stage_up = [&](bool inner, uint8_t* up, uint8_t* sq, uint8_t* se, uint32_t t) {
             const uint32_t part = way.part_of(t);
-            lq.stage(sq, way.q_at(part), t - part * way.blocks);
-            lu.stage(up, way.p_at(part), t - part * way.blocks);
             if (MUL::SCALED) le.stage(se, t, lane, wave);
+            if (MUL::SCALED && !inner && way.ends != 0 && t + 1 == blocks) {
+                lq.stage_end(sq, t, way.ends);
+                lu.stage_end(up, t, way.ends);
+            } else {
+                lq.stage(sq, way.q_at(part), t - part * way.blocks);
+                lu.stage(up, way.p_at(part), t - part * way.blocks);
+            }
         };
         auto read_p = [&](const uint8_t* s) {
 #pragma unroll
@@ -316,21 +399,17 @@ struct large_tile {
             asm volatile("" ::: "memory");
             __builtin_amdgcn_sched_barrier(0);
         };
-        auto multiply_half = [&](auto first, uint32_t e) {
+        auto multiply_half = [&](f32x4 (&c)[4][FQ], uint32_t e) {
             __builtin_amdgcn_s_setprio(1);
-            each<4>([&](auto i) {
-                each<FQ>([&](auto j) {
-                    constexpr int I = decltype(i)::value, J = decltype(j)::value, AT = decltype(first)::value + I;
-                    acc[AT][J] = MUL::template multiply<I, J>(fp[I], fq[J], acc[AT][J], e, eq);
-                });
-            });
+            sixteen<MUL>::multiply(c, fp, fq, e, eq);
             __builtin_amdgcn_s_setprio(0);
             __builtin_amdgcn_sched_barrier(0);
         };
-        auto block = [&](uint8_t* up, uint8_t* low, uint8_t* sq, uint8_t* se, uint8_t* nlow, uint32_t t) {
-            const bool tail = way.ends != 0 && t + 1 == blocks;
-            const uint32_t newer_up = t + 1 < blocks ? ALL : 0, newer_low = t + 2 < blocks ? ALL : t + 1 < blocks ? 2 : 0;
-            if (t != 0 && t == way.shrink * way.blocks) shrink(acc);
+        // With `more` three blocks follow at least, and no question is asked.
+        auto block = [&](auto more, uint8_t* up, uint8_t* low, uint8_t* sq, uint8_t* se, uint8_t* nlow, uint32_t t) {
+            constexpr bool MORE = decltype(more)::value;
+            const uint32_t newer_up = MORE || t + 1 < blocks ? ALL : 0, newer_low = MORE || t + 2 < blocks ? ALL : t + 1 < blocks ? 2 : 0;
+            if (!MUL::SCALED && t != 0 && t == way.shrink * way.blocks) shrink(acc);
 #pragma unroll
             for (int j = 0; j < FQ; ++j) fq[j] = read_fragment(sq, q_of(wave), j, lane);
             read_p(up);
@@ -339,53 +418,48 @@ struct large_tile {
                 el = *reinterpret_cast<const uint32_t*>(se + 128 + wp * 64 + 4 * (lane & 15));
                 eq = *reinterpret_cast<const uint32_t*>(se + BP + q_of(wave) + 4 * (lane & 15));
             }
-            if (t > 0 && t + 1 < blocks) stage_low(nlow, t + 1);
-            if (tail) {
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    cut(fp[i], way.ends, lane);
-                    cut(fq[i], way.ends, lane);
-                }
-            }
+            if (MORE || t + 1 < blocks) stage_low(MORE, nlow, t + 1);
             __builtin_amdgcn_s_waitcnt(LDS_READ);
             turn_over(group == 1, newer_up);
-            multiply_half(std::integral_constant<int, 0>{}, eu);
+            multiply_half(*reinterpret_cast<f32x4 (*)[4][FQ]>(&acc[0]), eu);
             turn_over(group == 0, newer_up);
             read_p(low);
-            if (t + 2 < blocks) stage_up(up, sq, se, t + 2);
-            if (tail) {
-#pragma unroll
-                for (int i = 0; i < 4; ++i) cut(fp[i], way.ends, lane);
-            }
+            if (MORE || t + 2 < blocks) stage_up(MORE, up, sq, se, t + 2);
             __builtin_amdgcn_s_waitcnt(LDS_READ);
             turn_over(group == 1, newer_low);
-            multiply_half(std::integral_constant<int, 4>{}, el);
+            multiply_half(*reinterpret_cast<f32x4 (*)[4][FQ]>(&acc[4]), el);
             turn_over(group == 0, newer_low);
         };
-        auto start = [&](uint8_t* up, uint8_t* low, uint8_t* sq, uint8_t* se, uint8_t* nup, uint8_t* nlow, uint8_t* nsq, uint8_t* nse) {
-            stage_up(up, sq, se, 0);
-            stage_low(low, 0);
+        auto start = [&](uint8_t* up, uint8_t* low, uint8_t* sq, uint8_t* se, uint8_t* nup, uint8_t* nsq, uint8_t* nse) {
+            stage_up(false, up, sq, se, 0);
+            stage_low(false, low, 0);
             if (blocks > 1) {
-                stage_up(nup, nsq, nse, 1);
-                stage_low(nlow, 1);
-                __builtin_amdgcn_s_waitcnt(loads_but(ALL));
+                stage_up(false, nup, nsq, nse, 1);
+                __builtin_amdgcn_s_waitcnt(loads_but(ALL - 2));
             } else {
                 __builtin_amdgcn_s_waitcnt(loads_but(0));
             }
+            __builtin_amdgcn_s_waitcnt(LDS_READ);
             turn_over(false, 0);
             if (group == 1) turn_over(false, 0);             // one turn behind
         };
         // blocks go through the buffers in turn and end with the second one
+        const std::true_type more;
+        const std::false_type last;
         uint32_t t = blocks & 1;
         if (t) {
-            start(up1, low1, sq1, se1, up0, low0, sq0, se0);
-            block(up1, low1, sq1, se1, low0, 0);
+            start(up1, low1, sq1, se1, up0, sq0, se0);
+            block(last, up1, low1, sq1, se1, low0, 0);
         } else {
-            start(up0, low0, sq0, se0, up1, low1, sq1, se1);
+            start(up0, low0, sq0, se0, up1, sq1, se1);
+        }
+        for (; t + 4 < blocks; t += 2) {
+            block(more, up0, low0, sq0, se0, low1, t);
+            block(more, up1, low1, sq1, se1, low0, t + 1);
         }
         for (; t < blocks; t += 2) {
-            block(up0, low0, sq0, se0, low1, t);
-            block(up1, low1, sq1, se1, low0, t + 1);
+            block(last, up0, low0, sq0, se0, low1, t);
+            block(last, up1, low1, sq1, se1, low0, t + 1);
         }
         if (group == 0) turn_over(false, 0);
     }
@@ -412,11 +486,16 @@ struct small_tile {
         lp.init(op, p0);
         lq.init(oq, q0);
         if (MUL::SCALED) le.init(op, p0, oq, q0, lane, wave);
-        auto stage = [&](uint8_t* sp, uint8_t* sq, uint8_t* se, uint32_t t) {
+        auto stage = [&](bool inner, uint8_t* sp, uint8_t* sq, uint8_t* se, uint32_t t) {
             const uint32_t part = way.part_of(t);
-            lp.stage(sp, way.p_at(part), t - part * way.blocks);
-            lq.stage(sq, way.q_at(part), t - part * way.blocks);
             if (MUL::SCALED) le.stage(se, t, lane, wave);
+            if (MUL::SCALED && !inner && way.ends != 0 && t + 1 == blocks) {
+                lp.stage_end(sp, t, way.ends);
+                lq.stage_end(sq, t, way.ends);
+            } else {
+                lp.stage(sp, way.p_at(part), t - part * way.blocks);
+                lq.stage(sq, way.q_at(part), t - part * way.blocks);
+            }
         };
         fragment fp[4], fq[2][FQ];
         uint32_t ep[2] = {0, 0}, eq[2] = {0, 0};
@@ -436,22 +515,17 @@ struct small_tile {
         };
         // Block t from the buffers of b, then the first fragments of the one behind it from the others: where there is
         // none they are read for nothing.
-        auto block = [&](auto b, uint8_t* sp, uint8_t* sq, uint8_t* se, uint8_t* np, uint8_t* nq, uint8_t* ne, uint32_t t) {
-            const bool tail = way.ends != 0 && t + 1 == blocks;
-            if (t != 0 && t == way.shrink * way.blocks) shrink(acc);
-            if (tail) {
-#pragma unroll
-                for (int j = 0; j < FQ; ++j) cut(fq[b][j], way.ends, lane);
-            }
+        auto block = [&](auto b, auto more, uint8_t* sp, uint8_t* sq, uint8_t* se, uint8_t* np, uint8_t* nq, uint8_t* ne, uint32_t t) {
+            constexpr bool MORE = decltype(more)::value;
+            if (!MUL::SCALED && t != 0 && t == way.shrink * way.blocks) shrink(acc);
             each<4>([&](auto step) {
                 constexpr int i = decltype(step)::value, B = decltype(b)::value;
                 if (i == 0) fp[3] = read_fragment(sp, p_of(wave, 0), 3, lane);
                 if (i == 1) {
                     staged_by_all();                         // (the next block is there, this one read by all)
-                    if (t + 2 < blocks) stage(sp, sq, se, t + 2);
+                    if (MORE || t + 2 < blocks) stage(MORE, sp, sq, se, t + 2);
                     read_q(nq, ne, 1 - B);
                 }
-                if (tail) cut(fp[i], way.ends, lane);
                 each<FQ>([&](auto of_q) {
                     constexpr int j = decltype(of_q)::value;
                     acc[i][j] = MUL::template multiply<i, j>(fp[i], fq[B][j], acc[i][j], ep[B], eq[B]);
@@ -461,25 +535,31 @@ struct small_tile {
             });
         };
         auto start = [&](int b, uint8_t* sp, uint8_t* sq, uint8_t* se, uint8_t* np, uint8_t* nq, uint8_t* ne) {
-            stage(sp, sq, se, 0);
+            stage(false, sp, sq, se, 0);
             staged_by_all();
-            if (blocks > 1) stage(np, nq, ne, 1);
+            if (blocks > 1) stage(false, np, nq, ne, 1);
             read_q(sq, se, b);
 #pragma unroll
             for (int i = 0; i < 3; ++i) fp[i] = read_fragment(sp, p_of(wave, 0), i, lane);
         };
         const std::integral_constant<int, 0> zero;
         const std::integral_constant<int, 1> one;
+        const std::true_type more;
+        const std::false_type last;
         uint32_t t = blocks & 1;
         if (t) {
             start(1, sp1, sq1, se1, sp0, sq0, se0);
-            block(one, sp1, sq1, se1, sp0, sq0, se0, 0);
+            block(one, last, sp1, sq1, se1, sp0, sq0, se0, 0);
         } else {
             start(0, sp0, sq0, se0, sp1, sq1, se1);
         }
+        for (; t + 4 < blocks; t += 2) {
+            block(zero, more, sp0, sq0, se0, sp1, sq1, se1, t);
+            block(one, more, sp1, sq1, se1, sp0, sq0, se0, t + 1);
+        }
         for (; t < blocks; t += 2) {
-            block(zero, sp0, sq0, se0, sp1, sq1, se1, t);
-            block(one, sp1, sq1, se1, sp0, sq0, se0, t + 1);
+            block(zero, last, sp0, sq0, se0, sp1, sq1, se1, t);
+            block(one, last, sp1, sq1, se1, sp0, sq0, se0, t + 1);
         }
         __syncthreads();                                     // (the last block read for the next by all)
     }
@@ -509,16 +589,13 @@ struct direct_tile {
         const uint32_t p_row = min(p0 + FP * c, (op.rows - 1) & ~3u), q_row = min(q0 + FQ * c, oq.rows - 1);
         const uint32_t p_off = FP * c * (uint32_t)op.pitch + (lane >> 4) * 16, q_off = FQ * c * (uint32_t)oq.pitch + (lane >> 4) * 16;
         uint32_t p_left[FP], q_left[FQ];
-        auto left_of = [](const operand& o, uint32_t row) {
-            return row < o.rows ? (uint32_t)min((o.rows - 1 - row) * o.pitch + o.row_bytes, (uint64_t)1 << 30) : 0;
-        };
 #pragma unroll
         for (int i = 0; i < FP; ++i) p_left[i] = left_of(op, p0 + i);
 #pragma unroll
         for (int j = 0; j < FQ; ++j) q_left[j] = left_of(oq, q0 + j);
         auto chunk_of = [](const operand& o, uint32_t row, uint32_t skip, uint32_t left, uint32_t off) {
             const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(o.p + row * o.pitch + skip), 0,
-                                                                                  left > skip ? left - skip : 0, 0x00020000);
+                                                                                  behind(left, skip), 0x00020000);
             return __builtin_bit_cast(gd_u32x4, __builtin_amdgcn_raw_buffer_load_b128(rsrc, off, 0, 0));
         };
         auto load = [&](loaded& l, uint32_t t) {
