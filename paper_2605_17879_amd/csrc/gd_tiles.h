@@ -240,32 +240,35 @@ __device__ __forceinline__ const uint8_t* scalar(const uint8_t* p) {
 constexpr int loads_but(int n) { return 0x0F70 | n; }
 constexpr int LDS_READ = 0xC07F;
 
-// Loads of a workgroup of NT lanes that stage ROWS rows of an operand, straight to the LDS: chunk c of row r lies at
-// c ^ (r / 4 % 8), so that the 16 rows of a fragment fall on different banks.  What lies behind the last row's last chunk
+// Loads of a workgroup of NT lanes that stage ROWS rows of an operand, straight to the LDS.  The rows of a fragment lie
+// next to each other there, and chunk k of place r at k ^ (r % 8), so that a read of sixteen rows meets every bank once
+// (rows in their order, of which a read takes every fourth, met half of them twice: 8 192 x 8 192 x 8 192 469 us).  What lies behind the last row's last chunk
 // comes as zeros (the buffer ends there); behind the end of another row lies the next one, which is cut off where it
 // would count.  A lane has one offset, the rest is scalar.
 template <int ROWS, int NT>
 struct stager {
-    static constexpr int LOADS = ROWS * 8 / NT, EACH = NT / 8;   // 16 bytes a lane, so many rows a load
+    static constexpr int LOADS = ROWS * 8 / NT, EACH = NT / 8;   // 16 bytes a lane, so many rows a load: 32 or 64
     const uint8_t* base;
     uint64_t pitch;
-    uint32_t at;                                  // this lane's chunk of the first block
+    uint32_t at, chunk;                           // this lane's chunk of the first block: bytes from base, and which of its row
     uint32_t left[LOADS];                         // bytes from a load's first row to the end, at most 2^30
 
     __device__ __forceinline__ void init(const operand& o, uint32_t first) {
-        static_assert(EACH % 32 == 0, "rows of one lane agree in r / 4 % 8");
         base = scalar(o.p + first * o.pitch);
         pitch = o.pitch;
-        at = threadIdx.x / 8 * (uint32_t)o.pitch + ((threadIdx.x & 7) ^ ((threadIdx.x / 32) & 7)) * 16;
+        chunk = (threadIdx.x ^ (threadIdx.x / 8)) & 7;
+        at = (threadIdx.x / 8 % 16 * 4 + threadIdx.x / 128) * (uint32_t)o.pitch + chunk * 16;
 #pragma unroll
-        for (int j = 0; j < LOADS; ++j) left[j] = left_of(o, first + j * EACH);
+        for (int j = 0; j < LOADS; ++j) left[j] = left_of(o, first + row_of(j));
     }
+    // The first row of a load: 64 of them are two loads of 256 lanes, fragments 0 and 1, 2 and 3, or one of 512.
+    static __device__ __forceinline__ constexpr uint32_t row_of(int j) { return EACH == 64 ? 64 * j : j / 2 * 64 + j % 2 * 2; }
     // Block t of what begins at `part` bytes in the rows.
     __device__ __forceinline__ void stage(uint8_t* s, uint32_t part, uint32_t t) const {
         const uint32_t skip = part + t * BYTES;
 #pragma unroll
         for (int j = 0; j < LOADS; ++j) {
-            const uint8_t* from = base + skip + j * EACH * pitch;
+            const uint8_t* from = base + skip + row_of(j) * pitch;
             __amdgpu_buffer_rsrc_t rsrc =
                 __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(from), 0, behind(left[j], skip), 0x00020000);
             __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lds_void*)(s + (j * NT + (threadIdx.x & ~63u)) * 16), 16, at, 0, 0, 0);
@@ -274,11 +277,11 @@ struct stager {
     // The last block, of which `ends` bytes are there: through registers, with zeros behind them.  (Every load before these is
     // there behind it too: they return in order.  What is written has to be waited for.)
     __device__ __forceinline__ void stage_end(uint8_t* s, uint32_t t, uint32_t ends) const {
-        const uint32_t skip = t * BYTES, chunk = (threadIdx.x & 7) ^ ((threadIdx.x / 32) & 7);
+        const uint32_t skip = t * BYTES;
 #pragma unroll
         for (int j = 0; j < LOADS; ++j) {
             const __amdgpu_buffer_rsrc_t rsrc =
-                __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(base + skip + j * EACH * pitch), 0, behind(left[j], skip), 0x00020000);
+                __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(base + skip + row_of(j) * pitch), 0, behind(left[j], skip), 0x00020000);
             gd_u32x4 x = __builtin_bit_cast(gd_u32x4, __builtin_amdgcn_raw_buffer_load_b128(rsrc, at, 0, 0));
             cut(x, ends, chunk);
             *reinterpret_cast<gd_u32x4*>(s + (j * NT + threadIdx.x) * 16) = x;
@@ -309,7 +312,7 @@ struct exp_stager {
 
 // Fragment i of the 64 rows from `row` on.
 __device__ __forceinline__ fragment read_fragment(const uint8_t* s, uint32_t row, int i, uint32_t lane) {
-    const uint32_t r = row + 4 * (lane & 15) + i;
+    const uint32_t r = row + 16 * i + (lane & 15);
     fragment f;
 #pragma unroll
     for (int h = 0; h < 2; ++h) f.h[h] = *reinterpret_cast<const gd_u32x4*>(s + r * BYTES + (((h * 4 + (lane >> 4)) ^ (lane & 7)) * 16));
@@ -668,6 +671,35 @@ struct direct_tile {
         return shared;
     }
 };
+
+// A row's neighbours: the lanes whose number differs in the lowest bits hold the same columns of the rows 4 and 8 further on.
+// N pieces of 16 bytes of each lane's row become piece lane % N of the rows of the N lanes, so that what the lanes write
+// at once lies next to each other: 128 bytes of a row instead of four times 16 (a C of 8 192 x 8 192 in bf16: 21 us, 70 with stores
+// that go through and were split so).
+template <int BIT>
+__device__ __forceinline__ uint32_t from_neighbour(uint32_t x) {
+    return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, BIT == 1 ? 0xB1 : 0x4E, 0xF, 0xF, true);
+}
+template <int N>
+__device__ __forceinline__ void exchange(gd_u32x4 (&x)[N], uint32_t lane) {
+    static_assert(N == 2 || N == 4, "within four lanes");
+    each<2>([&](auto of_bit) {
+        constexpr int BIT = 1 << decltype(of_bit)::value;
+        if constexpr (BIT < N) {
+            const uint32_t set = lane & BIT ? ~0u : 0u;      // (choices by masks, as above)
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+                if (!(i & BIT)) {
+#pragma unroll
+                    for (int w = 0; w < 4; ++w) {
+                        const uint32_t a = x[i][w], b = x[i | BIT][w], got = from_neighbour<BIT>((a & set) | (b & ~set));
+                        x[i][w] = (got & set) | (a & ~set);
+                        x[i | BIT][w] = (b & set) | (got & ~set);
+                    }
+                }
+        }
+    });
+}
 
 // Tiles in an order in which those that run at the same time share operands: workgroups go to the
 // eight chiplets in turn, each takes a stretch of the tiles, walked in strips of STRIP tiles of q.

@@ -32,21 +32,29 @@ struct product_args {
 // Sixteen columns of a row of C: v[i][r] is column 4 r + i.
 __device__ __forceinline__ float column(const f32x4 (&v)[4], int e) { return v[e % 4][e / 4]; }
 
+// (Called by all lanes of a wave; the next lane's row is `apart` further on.)
 template <typename T>
-__device__ __forceinline__ void write_row(const product_args& a, uint32_t row, uint32_t col, const f32x4 (&v)[4]) {
-    if (row >= a.n || col >= a.m) return;
+__device__ __forceinline__ void write_row(const product_args& a, uint32_t row, uint32_t col, const f32x4 (&v)[4], uint32_t apart, uint32_t lane) {
+    constexpr int V = 16 / sizeof(T), N = 16 / V;
     T* to = static_cast<T*>(a.c) + row * a.ldc + col;
-    constexpr int V = 16 / sizeof(T);
     if (col + 16 <= a.m) {
+        gd_u32x4 x[N];
 #pragma unroll
-        for (int b = 0; b < 16; b += V) {
-            gd_vec<T, V> old, x;
-            if (a.add) old = gd_read<T, V>(to + b);
+        for (int b = 0; b < N; ++b) {
+            gd_vec<T, V> old = {}, q;
+            if (a.add && row < a.n) old = gd_read<T, V>(to + b * V);
 #pragma unroll
-            for (int e = 0; e < V; ++e) x.v[e] = gd_from_f32<T>(a.add ? column(v, b + e) + gd_to_f32(old.v[e]) : column(v, b + e));
-            gd_write_through<T, V>(to + b, x);
+            for (int e = 0; e < V; ++e) q.v[e] = gd_from_f32<T>(a.add ? column(v, b * V + e) + gd_to_f32(old.v[e]) : column(v, b * V + e));
+            x[b] = __builtin_bit_cast(gd_u32x4, q);
         }
-    } else {
+        exchange<N>(x, lane);
+        const uint32_t first = row - (lane % N) * apart;
+#pragma unroll
+        for (int b = 0; b < N; ++b) {
+            const uint32_t r = first + b * apart;
+            if (r < a.n) *reinterpret_cast<gd_u32x4_anywhere*>(static_cast<T*>(a.c) + r * a.ldc + col + lane % N * V) = x[b];
+        }
+    } else if (row < a.n) {
 #pragma unroll
         for (int e = 0; e < 16; ++e)
             if (col + e < a.m) to[e] = gd_from_f32<T>(a.add ? column(v, e) + gd_to_f32(to[e]) : column(v, e));
@@ -66,7 +74,7 @@ __global__ __launch_bounds__(TILE<MUL>::NT, 512 / TILE<MUL>::NT) void tiled_kern
 #pragma unroll
         for (int g = 0; g < tile::FP / 4; ++g) {
             const f32x4 v[4] = {acc[4 * g][j], acc[4 * g + 1][j], acc[4 * g + 2][j], acc[4 * g + 3][j]};
-            write_row<T>(a, tq * tile::BQ + tile::q_of(wave) + 4 * (lane & 15) + j, tp * tile::BP + tile::p_of(wave, g) + 16 * (lane >> 4), v);
+            write_row<T>(a, tq * tile::BQ + tile::q_of(wave) + 4 * (lane & 15) + j, tp * tile::BP + tile::p_of(wave, g) + 16 * (lane >> 4), v, 4, lane);
         }
 }
 
@@ -81,7 +89,7 @@ __global__ __launch_bounds__(512, 2) void direct_kernel(const product_args a) {
     if (wave >= FQ) return;
     const uint32_t row = tq * tile::BQ + FQ * (lane & 15) + wave, col = tp * tile::BP + 16 * (lane >> 4);
     if (!a.slab) {
-        write_row<T>(a, row, col, v);
+        write_row<T>(a, row, col, v, FQ, lane);
     } else if (row < a.n && col < a.m4) {
         float* to = a.slab + (split * (uint64_t)a.n + row) * a.m4 + col;
 #pragma unroll
