@@ -197,7 +197,7 @@ struct passage {
     uint32_t blocks, parts, shrink;
     uint32_t p0, p1, q0, q1;   // of the first two parts; a third begins with the rows
     uint32_t ends;             // bytes of the last block that are there; 0: all
-    __device__ __forceinline__ uint32_t part_of(uint32_t t) const { return parts == 1 ? 0 : (t >= blocks) + (t >= 2 * blocks); }
+    __device__ __forceinline__ uint32_t part_of(uint32_t t) const { return (t >= blocks) + (t >= 2 * blocks); }   // (one part ends with the blocks)
     // (by masks: a choice between two members would be read at a computed address, which keeps the struct in scratch memory)
     static __device__ __forceinline__ uint32_t choose(uint32_t part, uint32_t a, uint32_t b) {
         return (-(uint32_t)(part == 0) & a) | (-(uint32_t)(part == 1) & b);
@@ -244,35 +244,37 @@ constexpr int LDS_READ = 0xC07F;
 // next to each other there, and chunk k of place r at k ^ (r % 8), so that a read of sixteen rows meets every bank once
 // (rows in their order, of which a read takes every fourth, met half of them twice: 8 192 x 8 192 x 8 192 469 us).  What lies behind the last row's last chunk
 // comes as zeros (the buffer ends there); behind the end of another row lies the next one, which is cut off where it
-// would count.  A lane has one offset, the rest is scalar.
+// would count.  A lane has one offset, the rest is scalar and does not change from block to block.
 template <int ROWS, int NT>
 struct stager {
     static constexpr int LOADS = ROWS * 8 / NT, EACH = NT / 8;   // 16 bytes a lane, so many rows a load: 32 or 64
+    __amdgpu_buffer_rsrc_t from[LOADS];           // a load's rows to the end of the operand
     const uint8_t* base;
     uint64_t pitch;
     uint32_t at, chunk;                           // this lane's chunk of the first block: bytes from base, and which of its row
     uint32_t left[LOADS];                         // bytes from a load's first row to the end, at most 2^30
+    uint32_t to;                                  // where the wave's part begins in a buffer
 
-    __device__ __forceinline__ void init(const operand& o, uint32_t first) {
+    __device__ __forceinline__ void init(const operand& o, uint32_t first, uint32_t wave) {
         base = scalar(o.p + first * o.pitch);
         pitch = o.pitch;
         chunk = (threadIdx.x ^ (threadIdx.x / 8)) & 7;
         at = (threadIdx.x / 8 % 16 * 4 + threadIdx.x / 128) * (uint32_t)o.pitch + chunk * 16;
+        to = wave * 1024;
 #pragma unroll
-        for (int j = 0; j < LOADS; ++j) left[j] = left_of(o, first + row_of(j));
+        for (int j = 0; j < LOADS; ++j) {
+            left[j] = left_of(o, first + row_of(j));
+            from[j] = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(base + row_of(j) * pitch), 0, (int)left[j], 0x00020000);
+        }
     }
     // The first row of a load: 64 of them are two loads of 256 lanes, fragments 0 and 1, 2 and 3, or one of 512.
     static __device__ __forceinline__ constexpr uint32_t row_of(int j) { return EACH == 64 ? 64 * j : j / 2 * 64 + j % 2 * 2; }
-    // Block t of what begins at `part` bytes in the rows.
-    __device__ __forceinline__ void stage(uint8_t* s, uint32_t part, uint32_t t) const {
-        const uint32_t skip = part + t * BYTES;
+    // The whole block that begins `skip` bytes into the rows.  (An offset beside the lane's own is not held against the buffer's end:
+    // that is right for whole blocks, whose chunks are there where the row is.)
+    __device__ __forceinline__ void stage(uint8_t* s, uint32_t skip) const {
 #pragma unroll
-        for (int j = 0; j < LOADS; ++j) {
-            const uint8_t* from = base + skip + row_of(j) * pitch;
-            __amdgpu_buffer_rsrc_t rsrc =
-                __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(from), 0, behind(left[j], skip), 0x00020000);
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lds_void*)(s + (j * NT + (threadIdx.x & ~63u)) * 16), 16, at, 0, 0, 0);
-        }
+        for (int j = 0; j < LOADS; ++j)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(from[j], (lds_void*)(s + to + j * NT * 16), 16, at, skip, 0, 0);
     }
     // The last block, of which `ends` bytes are there: through registers, with zeros behind them.  (Every load before these is
     // there behind it too: they return in order.  What is written has to be waited for.)
@@ -363,27 +365,27 @@ struct large_tile {
         stager<128, NT> lu, ll;
         stager<BQ, NT> lq;
         exp_stager<BP, BQ, NT> le;
-        lu.init(op, p0);
-        ll.init(op, p0 + 128);
-        lq.init(oq, q0);
+        lu.init(op, p0, wave);
+        ll.init(op, p0 + 128, wave);
+        lq.init(oq, q0, wave);
         if (MUL::SCALED) le.init(op, p0, oq, q0, lane, wave);
         fragment fp[4], fq[FQ];
         uint32_t eu = 0, el = 0, eq = 0;
         // `inner`: this is not the last block
         auto stage_low = [&](bool inner, uint8_t* low, uint32_t t) {
-            const uint32_t part = way.part_of(t);
+            const uint32_t part = MUL::SCALED ? 0 : way.part_of(t);
             if (MUL::SCALED && !inner && way.ends != 0 && t + 1 == blocks) ll.stage_end(low, t, way.ends);
-            else ll.stage(low, way.p_at(part), t - part * way.blocks);
+            else ll.stage(low, way.p_at(part) + (t - part * way.blocks) * BYTES);
         };
         auto stage_up = [&](bool inner, uint8_t* up, uint8_t* sq, uint8_t* se, uint32_t t) {
-            const uint32_t part = way.part_of(t);
+            const uint32_t part = MUL::SCALED ? 0 : way.part_of(t);
             if (MUL::SCALED) le.stage(se, t, lane, wave);
             if (MUL::SCALED && !inner && way.ends != 0 && t + 1 == blocks) {
                 lq.stage_end(sq, t, way.ends);
                 lu.stage_end(up, t, way.ends);
             } else {
-                lq.stage(sq, way.q_at(part), t - part * way.blocks);
-                lu.stage(up, way.p_at(part), t - part * way.blocks);
+                lq.stage(sq, way.q_at(part) + (t - part * way.blocks) * BYTES);
+                lu.stage(up, way.p_at(part) + (t - part * way.blocks) * BYTES);
             }
         };
         auto read_p = [&](const uint8_t* s) {
@@ -486,18 +488,18 @@ struct small_tile {
         stager<BP, NT> lp;
         stager<BQ, NT> lq;
         exp_stager<BP, BQ, NT> le;
-        lp.init(op, p0);
-        lq.init(oq, q0);
+        lp.init(op, p0, wave);
+        lq.init(oq, q0, wave);
         if (MUL::SCALED) le.init(op, p0, oq, q0, lane, wave);
         auto stage = [&](bool inner, uint8_t* sp, uint8_t* sq, uint8_t* se, uint32_t t) {
-            const uint32_t part = way.part_of(t);
+            const uint32_t part = MUL::SCALED ? 0 : way.part_of(t);
             if (MUL::SCALED) le.stage(se, t, lane, wave);
             if (MUL::SCALED && !inner && way.ends != 0 && t + 1 == blocks) {
                 lp.stage_end(sp, t, way.ends);
                 lq.stage_end(sq, t, way.ends);
             } else {
-                lp.stage(sp, way.p_at(part), t - part * way.blocks);
-                lq.stage(sq, way.q_at(part), t - part * way.blocks);
+                lp.stage(sp, way.p_at(part) + (t - part * way.blocks) * BYTES);
+                lq.stage(sq, way.q_at(part) + (t - part * way.blocks) * BYTES);
             }
         };
         fragment fp[4], fq[2][FQ];
@@ -602,7 +604,7 @@ struct direct_tile {
             return __builtin_bit_cast(gd_u32x4, __builtin_amdgcn_raw_buffer_load_b128(rsrc, off, 0, 0));
         };
         auto load = [&](loaded& l, uint32_t t) {
-            const uint32_t part = way.part_of(t), in = (t - part * way.blocks) * BYTES;
+            const uint32_t part = MUL::SCALED ? 0 : way.part_of(t), in = (t - part * way.blocks) * BYTES;
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
 #pragma unroll
