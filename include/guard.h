@@ -588,8 +588,8 @@ gd_status gd_packed_product(gd_handle h, const gd_packed* a, const gd_packed* b,
  *   for each step, with its coefficients a, b, c:  A = X X^T;  X = a X + (b A + c A A) X   (X^T X for tall matrices)
  *   p = param * [1 - lr * lr_scale * weight_decay] - [lr * lr_scale] * X
  * param = round(p) and, where d_copy is given, copy = round(p).  A matrix of zeros has X = 0.
- * products: GD_F32 multiplies numbers of 22 binary digits, three products of f16 for one; GD_F16 numbers of 11, apart from
- * X in its product with b A + c A A, which keeps 22 (X off by 1 to 2 thousandths of itself, for a 16-bit param or copy).
+ * products: GD_F32 multiplies numbers of 22 binary digits, three products of f16 for one; GD_F16 numbers of 11, while
+ * X itself is kept with 22 from step to step (X off by 1 to 2 thousandths of itself, for a 16-bit param or copy).
  * Sums are fp32 in both.  coefficients: three a step, such that the polynomial a s + b s^3 + c s^5 of each step
  * leaves singular values from 0 to 1 (then what the step before left) at magnitudes of at most 1.35; null:
  * 3.4445, -4.7750, 2.0315 in every step.

@@ -12,9 +12,10 @@
 // A^2, and a^2 b for the product with X.  They take f16; X, A and B = b A + c A^2 are kept in numbers of f16 times a power of two
 // that their largest singular values allow, as hi + 2^-11 lo, and a product is one of
 //   GD_F32   lo hi + hi lo + hi hi: 22 digits of each operand
-//   GD_F16   hi hi of A and A^2, B hi (X lo + X hi).  X itself needs its lo: what rounding drops of it would lie in directions
-//            whose singular values are small, and grow with them, up to a^steps = 485 times (a matrix of 16 strong directions over a
-//            floor of noise: 1.1e-2 off with X in f16, 1.5e-4 with hi + lo; bf16 9e-2).
+//   GD_F16   hi hi.  The X that is a part of the next one keeps its lo: what rounding drops of it would lie in directions whose
+//            singular values are small, and grow with them, up to a^steps = 485 times (512 x 512, 16 strong directions over a floor of
+//            noise: 1.1e-2 off with X in f16, 1.7e-4 with hi + lo; bf16 9e-2).  In the product with B it matters little: X hi there
+//            instead of hi + lo changes 1.2e-3 to 1.6e-3 for a matrix of normal numbers, and saves half of the product.
 //
 // Every product is C[q][p] = sum_k P[p][k] Q[q][k] of rows that lie along k, so X is kept both ways, R as the matrix lies and
 // C transposed; a lane's part of a tile is written both ways in whole lines (gd_tiles.h).  Symmetric products are computed on and
@@ -74,7 +75,7 @@ struct layout {
         a = rows < cols ? rows : cols;
         b = rows < cols ? cols : rows;
         lo_r = up_to(cols, 64) * 2; lo_c = up_to(rows, 64) * 2; lo_s = up_to(a, 64) * 2;
-        r_pitch = 2 * lo_r; c_pitch = 2 * lo_c; s_pitch = both ? 2 * lo_s : lo_s;
+        r_pitch = 2 * lo_r; c_pitch = both ? 2 * lo_c : lo_c; s_pitch = both ? 2 * lo_s : lo_s;   // (R alone is a part of the next X)
         of_r = up_to(rows * r_pitch, 256);
         of_c = up_to(cols * c_pitch, 256);
         const uint64_t of_s = up_to(a * s_pitch, 256);
@@ -208,6 +209,37 @@ __device__ __forceinline__ float whole(gd_f16 hi, gd_f16 lo) { return (float)hi 
 
 typedef gd_f16 f16x4 __attribute__((ext_vector_type(4)));
 
+// U of four rows of four columns each, as far as they are there.
+template <typename T>
+__device__ __forceinline__ void updates_of(const muon_args& g, const entry& e, uint32_t row, uint32_t col, float f, float (&u)[4][4]) {
+    gd_vec<T, 4> grad[4] = {};
+    gd_vec<float, 4> m[4] = {};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if (row + i >= e.rows) break;
+        const uint64_t at = (uint64_t)(row + i) * e.cols + col;
+        const T* from = static_cast<const T*>(e.grad) + at;
+        if (col + 4 <= e.cols) {
+            __builtin_memcpy(&grad[i], from, sizeof(grad[i]));
+            m[i] = gd_read<float, 4>(e.m + at);
+        } else {
+#pragma unroll
+            for (int j = 0; j < 3; ++j)
+                if (col + j < e.cols) {
+                    grad[i].v[j] = from[j];
+                    m[i].v[j] = e.m[at + j];
+                }
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const float gr = gd_to_f32(grad[i].v[j]);
+            u[i][j] = update_of(g, g.grad_scale ? gr * f : gr, m[i].v[j]);
+        }
+}
+
 // X of the first step, 64 x 64 a workgroup, both ways, with zeros up to the end of a block of k.
 __global__ __launch_bounds__(256) void start_kernel(const muon_args g) {
     float f;
@@ -222,18 +254,16 @@ __global__ __launch_bounds__(256) void start_kernel(const muon_args g) {
     uint8_t* base = g.work + e.at[!g.both];
     const uint32_t tiles_c = (e.cols + 63) / 64, row = t / tiles_c * 64 + threadIdx.x / 16 * 4, col = t % tiles_c * 64 + threadIdx.x % 16 * 4;
     halves x[4][4];
+    float u[4][4] = {};
+    if (row < e.rows && col < e.cols) {
+        if (e.grad_type == GD_F32) updates_of<float>(g, e, row, col, f, u);
+        else if (e.grad_type == GD_BF16) updates_of<gd_bf16>(g, e, row, col, f, u);
+        else updates_of<gd_f16>(g, e, row, col, f, u);
+    }
 #pragma unroll
     for (int i = 0; i < 4; ++i)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            float u = 0;
-            if (row + i < e.rows && col + j < e.cols) {
-                const uint64_t at = (uint64_t)(row + i) * e.cols + col + j;
-                const float gr = grad_at(e, at);
-                u = (float)(update_of(g, g.grad_scale ? gr * f : gr, e.m[at]) * scale);
-            }
-            x[i][j] = split(u);
-        }
+        for (int j = 0; j < 4; ++j) x[i][j] = split((float)(u[i][j] * scale));
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         if (row + i < e.rows) {
@@ -244,7 +274,7 @@ __global__ __launch_bounds__(256) void start_kernel(const muon_args g) {
         if (col + i < e.cols) {
             uint8_t* to = base + l.c(0) + (col + i) * l.c_pitch + row * 2;
             *reinterpret_cast<f16x4*>(to) = f16x4{x[0][i].hi, x[1][i].hi, x[2][i].hi, x[3][i].hi};
-            *reinterpret_cast<f16x4*>(to + l.lo_c) = f16x4{x[0][i].lo, x[1][i].lo, x[2][i].lo, x[3][i].lo};
+            if (g.both) *reinterpret_cast<f16x4*>(to + l.lo_c) = f16x4{x[0][i].lo, x[1][i].lo, x[2][i].lo, x[3][i].lo};
         }
     }
 }
@@ -259,7 +289,7 @@ struct target {
     uint8_t* t;  uint64_t t_pitch, t_lo;           // written transposed, or null
     const uint8_t* old;                            // A or X at the same places as d
     uint32_t rows, cols;
-    bool lo;                                       // of what is written
+    bool lo, t_lo_too;                             // of what is written, as it lies and transposed
     bool old_lo;                                   // of what is read
 };
 
@@ -295,22 +325,20 @@ __device__ __forceinline__ problem problem_of(const muon_args& g, const entry& e
         x.way.blocks = (uint32_t)(lo / BYTES);
         parts(g.both ? 3 : 1, lo, lo);
         uint8_t* to = PHASE == OF_X ? sa : sb;
-        x.out = target{to, l.s_pitch, l.lo_s, off_diagonal ? to : nullptr, l.s_pitch, l.lo_s, sa, l.a, l.a, g.both != 0, g.both != 0};
+        x.out = target{to, l.s_pitch, l.lo_s, off_diagonal ? to : nullptr, l.s_pitch, l.lo_s, sa, l.a, l.a, g.both != 0, g.both != 0, g.both != 0};
     } else {
         const operand b = matrix(sb, l.s_pitch, l.a);
         x.way.blocks = (uint32_t)(l.lo_s / BYTES);
-        // (X first where it has a lo and B has none)
         if (tall) {
             x.p = b;
             x.q = matrix(r0, l.r_pitch, e.rows);
-            parts(g.both ? 3 : 2, g.both ? l.lo_s : 0, l.lo_r);
-            if (!g.both) x.way.q0 = (uint32_t)l.lo_r;
+            parts(g.both ? 3 : 1, l.lo_s, l.lo_r);
         } else {
             x.p = matrix(c0, l.c_pitch, e.cols);
             x.q = b;
-            parts(g.both ? 3 : 2, l.lo_c, l.lo_s);
+            parts(g.both ? 3 : 1, l.lo_c, l.lo_s);
         }
-        x.out = target{r1, l.r_pitch, l.lo_r, c1, l.c_pitch, l.lo_c, r0, e.rows, e.cols, true, true};
+        x.out = target{r1, l.r_pitch, l.lo_r, c1, l.c_pitch, l.lo_c, r0, e.rows, e.cols, true, g.both != 0, true};
     }
     return x;
 }
@@ -344,20 +372,32 @@ __device__ __forceinline__ void finish_row(const muon_args& g, const entry& e, c
     }
 }
 
-__device__ __forceinline__ void write_row(const target& o, uint32_t row, uint32_t col, const f32x4 (&v)[4]) {
-    if (row >= o.rows || col >= o.d_lo / 2) return;
-    uint8_t* to = o.d + row * o.d_pitch + col * 2;
+// (Called by all lanes of a wave; the next lane's row is four further on.)
+__device__ __forceinline__ void write_row(const target& o, uint32_t row, uint32_t col, const f32x4 (&v)[4], uint32_t lane) {
+    if (col >= o.d_lo / 2) return;                 // (the same for lanes that exchange)
+    gd_u32x4 hi[2], lo[2];
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-        gd_vec<gd_f16, 8> hi, lo;
+        gd_vec<gd_f16, 8> x, y;
 #pragma unroll
-        for (int x = 0; x < 8; ++x) {
-            const halves s = split(v[x % 4][2 * h + x / 4]);
-            hi.v[x] = s.hi;
-            lo.v[x] = s.lo;
+        for (int e = 0; e < 8; ++e) {
+            const halves s = split(v[e % 4][2 * h + e / 4]);
+            x.v[e] = s.hi;
+            y.v[e] = s.lo;
         }
-        *reinterpret_cast<gd_u32x4*>(to + 16 * h) = __builtin_bit_cast(gd_u32x4, hi);
-        if (o.lo) *reinterpret_cast<gd_u32x4*>(to + o.d_lo + 16 * h) = __builtin_bit_cast(gd_u32x4, lo);
+        hi[h] = __builtin_bit_cast(gd_u32x4, x);
+        lo[h] = __builtin_bit_cast(gd_u32x4, y);
+    }
+    exchange<2>(hi, lane);
+    if (o.lo) exchange<2>(lo, lane);
+    const uint32_t first = row - lane % 2 * 4;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const uint32_t r = first + 4 * h;
+        if (r >= o.rows) break;
+        uint8_t* to = o.d + r * o.d_pitch + col * 2 + lane % 2 * 16;
+        *reinterpret_cast<gd_u32x4*>(to) = hi[h];
+        if (o.lo) *reinterpret_cast<gd_u32x4*>(to + o.d_lo) = lo[h];
     }
 }
 
@@ -367,7 +407,7 @@ __device__ __forceinline__ void write_column(const target& o, uint32_t row, uint
     uint8_t* to = o.t + col * o.t_pitch + row * 2;
     const halves s0 = split(x0), s1 = split(x1), s2 = split(x2), s3 = split(x3);
     *reinterpret_cast<f16x4*>(to) = f16x4{s0.hi, s1.hi, s2.hi, s3.hi};
-    if (o.lo) *reinterpret_cast<f16x4*>(to + o.t_lo) = f16x4{s0.lo, s1.lo, s2.lo, s3.lo};
+    if (o.t_lo_too) *reinterpret_cast<f16x4*>(to + o.t_lo) = f16x4{s0.lo, s1.lo, s2.lo, s3.lo};
 }
 
 template <typename T>
@@ -463,7 +503,7 @@ __global__ __launch_bounds__(TILE<of_f16>::NT, 512 / TILE<of_f16>::NT) void tile
             for (int i = 0; i < 4; ++i) v[j][i] = acc[4 * h + i][j];
             finish_row<PHASE>(g, e, x.out, row + j, col, v[j]);
             if (PHASE == LAST) update_row(g, e, row + j, col, v[j]);
-            else write_row(x.out, row + j, col, v[j]);
+            else write_row(x.out, row + j, col, v[j], lane);
         }
         if (PHASE != LAST) {
 #pragma unroll
@@ -488,7 +528,7 @@ __global__ __launch_bounds__(512, 2) void direct_kernel(const muon_args g) {
     if (wave < 4) {
         finish_row<PHASE>(g, e, x.out, row + wave, col, v);
         if (PHASE == LAST) update_row(g, e, row + wave, col, v);
-        else write_row(x.out, row + wave, col, v);
+        else write_row(x.out, row + wave, col, v, lane);
     }
     if (PHASE == LAST || !x.out.t) return;
     // the four rows of a lane together, for the transpose: wave r has columns 4 r .. 4 r + 3
@@ -534,10 +574,24 @@ void launch_phase(muon_args g, const head& h, hipStream_t s) {
     }
 }
 
-// Which tiles a matrix takes.
-int kind_of(uint32_t rows, uint32_t cols) {
-    const uint32_t a = std::min(rows, cols);
-    return a >= 2048 ? LARGE : a >= 512 ? SMALL : DIRECT;
+uint64_t tiles_of(const gd_muon_tensor& t, uint64_t edge) { return ((t.rows + edge - 1) / edge) * ((t.cols + edge - 1) / edge); }
+
+// Which tiles the matrices take.  Tiles of 256 x 256 where they fill the chip (24 of 1 024 x 1 024, 384 of them: 2.16 ms, with tiles of
+// 128 x 128 2.29; 4 of 2 048 x 2 048, 256: 2.29 and 2.68; 8 of 1 024 x 1 024, 128: 1.22 and 0.87) and are not mostly empty; else
+// tiles of 128 x 128 where those of 64 x 64 would be more than two rounds of the chip's workgroups (16 of 512 x 512, 1 024: 0.41
+// and 0.81; 8 of 333 x 500, 384: 0.32 and 0.31; 8 of 128 x 128, 32: 0.18 and 0.14).
+void choose_kinds(const gd_muon_tensor* t, uint32_t n, std::vector<int>& kinds) {
+    kinds.assign(n, DIRECT);
+    auto side = [&](uint32_t i) { return std::min(t[i].rows, t[i].cols); };
+    auto fills = [&](uint32_t i) { return side(i) >= 512 && tiles_of(t[i], 256) * 4 * 10 <= tiles_of(t[i], 128) * 13; };
+    uint64_t large = 0, direct = 0;
+    for (uint32_t i = 0; i < n; ++i)
+        if (fills(i)) large += tiles_of(t[i], 256);
+    for (uint32_t i = 0; i < n; ++i)
+        if (large >= 240 && fills(i)) kinds[i] = LARGE;
+        else if (side(i) > 64) direct += tiles_of(t[i], 64);
+    for (uint32_t i = 0; i < n; ++i)
+        if (kinds[i] == DIRECT && side(i) > 64 && direct > 512) kinds[i] = SMALL;
 }
 
 // The largest magnitude of a polynomial c1 x + c3 x^3 + c5 x^5 (of b x^2 + c x^4 with `even`) over [0, s].
@@ -569,10 +623,12 @@ double most_of_even(double b, double c, double s) {
 
 size_t gd_muon_table(const gd_muon_tensor* t, uint32_t n, void* out) {
     std::vector<uint32_t> order[KINDS];
+    std::vector<int> kinds;
+    choose_kinds(t, n, kinds);
     uint32_t there = 0;
     for (uint32_t i = 0; i < n; ++i)
         if (t[i].rows && t[i].cols) {
-            order[kind_of((uint32_t)t[i].rows, (uint32_t)t[i].cols)].push_back(i);
+            order[kinds[i]].push_back(i);
             ++there;
         }
     const size_t bytes = gd_align256(list_at(there, LISTS));

@@ -162,17 +162,19 @@ struct plan {
 
 uint32_t up(uint64_t a, uint64_t b) { return (uint32_t)((a + b - 1) / b); }
 
-plan plan_of(uint64_t n, uint64_t m, uint64_t k) {
+// Tiles of 64 x 64 and smaller up to one round of the chip's workgroups (1 000 x 1 001 x 1 000, 256 of them: 8.5 us, tiles of 128 x 128 11.2,
+// of 256 x 256 22.5; 1 500 x 1 000 x 2 000, 384: 18.5, 15.3, 30.2), three where the others need their operands written out in bf16 first
+// (2 000 x 1 500 x 1 000, 768: 21.4, 26.3, 38.8; 2 048 x 2 048 x 2 048, 1 024: 48, 40, 58); tiles of 256 x 256 from where they fill more
+// than half of the chip (3 000 x 3 000 x 3 000, 144 of them: 44 us, 50 with 128 x 128; 2 048 x 4 096 x 4 096, 128: 51 and 36).
+plan plan_of(uint64_t n, uint64_t m, uint64_t k, bool f32) {
     const uint64_t blocks = up(k, BYTES);
-    const uint64_t large = (uint64_t)up(n, 256) * up(m, 256), small = (uint64_t)up(n, 128) * up(m, 128);
-    plan w{plan::LARGE, 4, 1, (uint32_t)blocks};
-    if (n > 64 && large >= 192) return w;
-    w.kind = plan::SMALL;
-    if (n > 64 && small >= 256) return w;
-    w.kind = plan::DIRECT;
-    w.fq = n <= 16 ? 1 : n <= 32 ? 2 : 4;
+    plan w{plan::DIRECT, n <= 16 ? 1u : n <= 32 ? 2u : 4u, 1, (uint32_t)blocks};
     const uint64_t tiles = (uint64_t)up(n, 16 * w.fq) * up(m, 64);
-    // workgroups for every CU, as long as a wave keeps a few blocks
+    if (n > 64 && tiles > (f32 ? 768 : 256)) {
+        w.kind = (uint64_t)up(n, 256) * up(m, 256) >= 140 ? plan::LARGE : plan::SMALL;
+        return w;
+    }
+    // workgroups for every CU, as long as a wave keeps two blocks
     const uint64_t most = std::max<uint64_t>(1, blocks / 16);
     w.splits = (uint32_t)std::min<uint64_t>(most, std::max<uint64_t>(1, 256 / tiles));
     w.each = up(blocks, w.splits);
@@ -182,8 +184,9 @@ plan plan_of(uint64_t n, uint64_t m, uint64_t k) {
 
 // Of the splits' sums, or of the operands in bf16.
 uint64_t row_of_numbers(uint64_t k) { return (k + 63) / 64 * 128; }
-uint64_t work_bytes(const plan& w, uint64_t n, uint64_t m, uint64_t k) {
-    return w.kind != plan::DIRECT ? (n + m) * row_of_numbers(k) : w.splits > 1 ? w.splits * n * gd_align256(m * 4) : 0;
+uint64_t work_bytes(uint64_t n, uint64_t m, uint64_t k, bool f32) {
+    const plan w = plan_of(n, m, k, f32);
+    return w.kind != plan::DIRECT ? (f32 ? (n + m) * row_of_numbers(k) : 0) : w.splits > 1 ? w.splits * n * gd_align256(m * 4) : 0;
 }
 
 template <typename MUL, typename T>
@@ -241,7 +244,7 @@ hipError_t launch(product_args& a, const plan& w, const gd_packed_product_args& 
 }  // namespace
 
 size_t gd_packed_product_work(uint64_t n, uint64_t m, uint64_t k) {
-    return n && m && k ? gd_align256(work_bytes(plan_of(n, m, k), n, m, k)) : 0;
+    return n && m && k ? gd_align256(std::max(work_bytes(n, m, k, false), work_bytes(n, m, k, true))) : 0;
 }
 
 hipError_t gd_launch_packed_product(const gd_packed_product_args& g, hipStream_t s) {
@@ -261,7 +264,7 @@ hipError_t gd_launch_packed_product(const gd_packed_product_args& g, hipStream_t
     a.way.blocks = up(g.k, BYTES); a.way.parts = 1; a.way.ends = g.k % BYTES;
     a.slab = reinterpret_cast<float*>(g.work);
     a.m4 = (uint32_t)(gd_align256(g.m * 4ull) / 4);
-    const plan w = plan_of(g.n, g.m, g.k);
+    const plan w = plan_of(g.n, g.m, g.k, g.out_type == GD_F32);
     if (g.a_codes == GD_E4M3) return g.b_codes == GD_E4M3 ? launch<0, 0>(a, w, g, s) : launch<1, 0>(a, w, g, s);
     return g.b_codes == GD_E4M3 ? launch<0, 1>(a, w, g, s) : launch<1, 1>(a, w, g, s);
 }

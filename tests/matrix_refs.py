@@ -105,7 +105,7 @@ def orthogonal(u_, steps=5, coefficients=None, products=None, eps=1e-7):
         bb = f32(b * aa + c * (aa @ aa))
         most = max(float(bb.abs().max()), 1e-30)
         bb = _digits(bb, both, 2.0 ** math.floor(math.log2(32768.0 / max(most, 4.0))))
-        x = a * x2 + bb @ x2
+        x = a * x2 + bb @ xs
     x = f32(x)
     return x.t().contiguous() if tall else x
 
