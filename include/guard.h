@@ -541,7 +541,8 @@ gd_status gd_adamw(gd_handle h, const void* d_table, size_t table_bytes, const g
 
 /*
  * Packed matrices: 8-bit floating point with a power of two for each block of 128 elements of a row.
- *   codes [rows][cols]               GD_E4M3 or GD_E5M2, one byte each; 16-byte aligned, the stride a multiple of 16
+ *   codes [rows][cols]               GD_E4M3 or GD_E5M2, one byte each; 16-byte aligned, the stride a multiple of 16 (rather not
+ *                                    of 256: such rows meet at the same channels of the memory)
  *   exp   [ceil(cols / 128)][rows]   GD_U8; 4-byte aligned, the stride a multiple of 4
  * Element (i, k) stands for codes[i][k] * 2^(exp[k / 128][i] - 127); a byte of 255 stands for a block of NaN.  In front
  * of the last row what lies between its end and the next one's begin is neither read as a number nor written.

@@ -236,8 +236,8 @@ __device__ __forceinline__ const uint8_t* scalar(const uint8_t* p) {
                                             (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)a));
 }
 
-// s_waitcnt operands: all but `n` loads (n below 16); all LDS reads
-constexpr int loads_but(int n) { return 0x0F70 | n; }
+// s_waitcnt operands: all but `n` loads (n below 64); all LDS reads
+constexpr int loads_but(int n) { return 0x0F70 | (n & 15) | (n >> 4) << 14; }
 constexpr int LDS_READ = 0xC07F;
 
 // Loads of a workgroup of NT lanes that stage ROWS rows of an operand, straight to the LDS.  The rows of a fragment lie
@@ -570,93 +570,96 @@ struct small_tile {
     }
 };
 
-// 64 x 16 FQ by eight waves that share k and read their operands from memory straight into registers; what the waves
-// have summed is joined in the LDS, in their order.  For products of few tiles, and of few rows of Q, where every byte of
-// P is read once.  Fragments of Q hold rows FQ c + j.
+// 64 x 16 FQ by eight waves that share k, for products of few tiles, and of few rows of Q, where every byte of P is read once.
+// Each wave stages blocks of its own in a part of the LDS that no other wave touches, so that it waits for nothing but its
+// own loads: the next block is on its way while this one, read into registers, is multiplied.  What the waves have
+// summed is joined in the LDS, in their order.  (Fragments read from memory straight into registers took half as long again:
+// neighbouring lanes hold rows apart, and the loads' addresses are taken four lanes at a time.)  Fragments of Q hold
+// rows FQ c + j.
 template <typename MUL, int FQ_>
 struct direct_tile {
     static constexpr int FP = 4, FQ = FQ_, BP = 64, BQ = 16 * FQ, WAVES = 8, NT = 64 * WAVES;
-
+    static constexpr int PART = (BP + BQ) * BYTES, EXPS = 128;
     typedef f32x4 sums[FQ][FP][64];
+    static_assert(sizeof(sums) <= PART, "the sums take the place of the blocks");
+
     // Blocks from `first` up to `end`.  Behind it waves 0 .. FQ - 1 have the sums of column j = wave in `sum`, the others nothing.
     // Returned: room in the LDS that the waves have read (each its own column j of each wave's sums).
     static __device__ __forceinline__ sums* run(const operand& op, const operand& oq, uint32_t p0, uint32_t q0, const passage& way,
-                                               uint32_t first, uint32_t end, f32x4 (&sum)[FP]) {
-        __shared__ __attribute__((aligned(16))) sums shared[WAVES];
+                                                uint32_t first, uint32_t end, f32x4 (&sum)[FP]) {
+        __shared__ __attribute__((aligned(16))) uint8_t rows[WAVES * PART], exps[WAVES * EXPS];
         const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
         const uint32_t blocks = way.blocks * way.parts, c = lane & 15;
         f32x4 acc[FP][FQ] = {};
-        struct loaded {
-            fragment p[FP], q[FQ];
-            uint32_t pe, qe;
-        };
-        // A lane's rows are FP c + i of P, FQ c + j of Q: one offset, and for each i a buffer that begins a row further on.
-        const uint32_t p_row = min(p0 + FP * c, (op.rows - 1) & ~3u), q_row = min(q0 + FQ * c, oq.rows - 1);
-        const uint32_t p_off = FP * c * (uint32_t)op.pitch + (lane >> 4) * 16, q_off = FQ * c * (uint32_t)oq.pitch + (lane >> 4) * 16;
-        uint32_t p_left[FP], q_left[FQ];
+        // Eight places of the LDS a load, a row's chunk a lane: place 16 i + c holds row FP c + i, chunk k at k ^ (c % 8).
+        constexpr int PL = BP / 8, QL = BQ / 8;
+        const uint32_t chunk = ((lane ^ (lane / 8)) & 7) * 16;
+        uint32_t p_at[PL], q_at[QL];
 #pragma unroll
-        for (int i = 0; i < FP; ++i) p_left[i] = left_of(op, p0 + i);
+        for (int j = 0; j < PL; ++j) p_at[j] = (min(p0 + FP * (j % 2 * 8 + lane / 8) + j / 2, op.rows - 1) - min(p0, op.rows - 1)) * (uint32_t)op.pitch;
 #pragma unroll
-        for (int j = 0; j < FQ; ++j) q_left[j] = left_of(oq, q0 + j);
-        auto chunk_of = [](const operand& o, uint32_t row, uint32_t skip, uint32_t left, uint32_t off) {
-            const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(o.p + row * o.pitch + skip), 0,
-                                                                                  behind(left, skip), 0x00020000);
-            return __builtin_bit_cast(gd_u32x4, __builtin_amdgcn_raw_buffer_load_b128(rsrc, off, 0, 0));
+        for (int j = 0; j < QL; ++j) q_at[j] = (min(q0 + FQ * (j % 2 * 8 + lane / 8) + j / 2, oq.rows - 1) - min(q0, oq.rows - 1)) * (uint32_t)oq.pitch;
+        const uint8_t *p_base = scalar(op.p + min(p0, op.rows - 1) * op.pitch), *q_base = scalar(oq.p + min(q0, oq.rows - 1) * oq.pitch);
+        const uint32_t pe_at = min(p0 + 4 * lane, (op.rows - 1) & ~3u), qe_at = min(q0 + 4 * lane, (oq.rows - 1) & ~3u);
+        auto whole_buffer = [](const uint8_t* p) { return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(p), 0, -1, 0x00020000); };
+        auto load = [](__amdgpu_buffer_rsrc_t from, uint8_t* to, uint32_t at) {
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (lds_void*)to, 16, at, 0, 0, 0);
         };
-        auto load = [&](loaded& l, uint32_t t) {
+        uint8_t *const to = rows + wave * PART, *const to_exp = exps + wave * EXPS;
+        auto stage = [&](uint32_t t) {
             const uint32_t part = MUL::SCALED ? 0 : way.part_of(t), in = (t - part * way.blocks) * BYTES;
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-#pragma unroll
-                for (int i = 0; i < FP; ++i) l.p[i].h[h] = chunk_of(op, p0 + i, in + way.p_at(part), p_left[i], p_off + h * 64);
-#pragma unroll
-                for (int j = 0; j < FQ; ++j) l.q[j].h[h] = chunk_of(oq, q0 + j, in + way.q_at(part), q_left[j], q_off + h * 64);
-            }
             if (MUL::SCALED) {
-                l.pe = *reinterpret_cast<const uint32_t*>(op.exp + t * op.exp_pitch + p_row);
-                const uint8_t* qe = oq.exp + t * oq.exp_pitch;
-                if (FQ == 4) {
-                    l.qe = *reinterpret_cast<const uint32_t*>(qe + (q_row & ~3u));
-                } else {
-                    l.qe = 0;
-#pragma unroll
-                    for (int j = 0; j < FQ; ++j) l.qe |= (uint32_t)qe[min(q0 + FQ * c + j, oq.rows - 1)] << (8 * j);
-                }
+                if (lane < BP / 4)
+                    __builtin_amdgcn_raw_ptr_buffer_load_lds(whole_buffer(scalar(op.exp + t * op.exp_pitch)), (lds_void*)to_exp, 4, pe_at, 0, 0, 0);
+                if (lane < BQ / 4)
+                    __builtin_amdgcn_raw_ptr_buffer_load_lds(whole_buffer(scalar(oq.exp + t * oq.exp_pitch)), (lds_void*)(to_exp + BP), 4, qe_at, 0, 0, 0);
             }
-        };
-        auto multiply = [&](loaded& l, uint32_t t) {
-            if (way.ends != 0 && t + 1 == blocks) {
+            // (chunks behind the row's end: its last one again, which is cut off)
+            const uint32_t here = min(chunk, op.row_bytes - 16 - way.p_at(part) - in), there = min(chunk, oq.row_bytes - 16 - way.q_at(part) - in);
+            const __amdgpu_buffer_rsrc_t from_p = whole_buffer(p_base + way.p_at(part) + in), from_q = whole_buffer(q_base + way.q_at(part) + in);
 #pragma unroll
-                for (int i = 0; i < FP; ++i) cut(l.p[i], way.ends, lane);
+            for (int j = 0; j < PL; ++j) load(from_p, to + j * 1024, p_at[j] + here);
 #pragma unroll
-                for (int j = 0; j < FQ; ++j) cut(l.q[j], way.ends, lane);
-            }
-            if constexpr (requires_all<MUL>::value) MUL::multiply_all(l.p, l.q, acc, l.pe, l.qe);
-            else multiply_all<MUL>(l.p, l.q, acc, l.pe, l.qe);
+            for (int j = 0; j < QL; ++j) load(from_q, to + BP * BYTES + j * 1024, q_at[j] + there);
         };
-        // (a wave that goes past the part that shrinks does so once; one that has no block there scales zeros, or at the end)
+        // (a wave that goes past the part that shrinks does so once; one that has no block there scales at the end)
         bool whole = way.shrink == 0;
-        auto pass = [&](uint32_t t) {
-            if (!whole && t >= way.shrink * way.blocks) {
+        uint32_t t = first + wave;
+        if (t < end) stage(t);
+        for (; t < end; t += WAVES) {
+            __builtin_amdgcn_s_waitcnt(loads_but(0));
+            asm volatile("" ::: "memory");
+            fragment p[FP], q[FQ];
+#pragma unroll
+            for (int i = 0; i < FP; ++i) p[i] = read_fragment(to, 0, i, lane);
+#pragma unroll
+            for (int j = 0; j < FQ; ++j) q[j] = read_fragment(to + BP * BYTES, 0, j, lane);
+            uint32_t pe = 0, qe = 0;
+            if (MUL::SCALED) {
+                pe = *reinterpret_cast<const uint32_t*>(to_exp + 4 * c);
+                if (FQ == 4) qe = *reinterpret_cast<const uint32_t*>(to_exp + BP + 4 * c);
+                else if (FQ == 2) qe = *reinterpret_cast<const uint16_t*>(to_exp + BP + 2 * c);
+                else qe = to_exp[BP + c];
+            }
+            __builtin_amdgcn_s_waitcnt(LDS_READ);            // (read: there is room for the next)
+            asm volatile("" ::: "memory");
+            if (t + WAVES < end) stage(t + WAVES);
+            if (MUL::SCALED && way.ends != 0 && t + 1 == blocks) {
+#pragma unroll
+                for (int i = 0; i < FP; ++i) cut(p[i], way.ends, lane);
+#pragma unroll
+                for (int j = 0; j < FQ; ++j) cut(q[j], way.ends, lane);
+            }
+            if (!MUL::SCALED && !whole && t >= way.shrink * way.blocks) {
                 shrink(acc);
                 whole = true;
             }
-        };
-        loaded a, b;
-        uint32_t t = first + wave;
-        if (t < end) load(a, t);
-        while (t < end) {
-            if (t + WAVES < end) load(b, t + WAVES);
-            pass(t);
-            multiply(a, t);
-            t += WAVES;
-            if (t >= end) break;
-            if (t + WAVES < end) load(a, t + WAVES);
-            pass(t);
-            multiply(b, t);
-            t += WAVES;
+            if constexpr (requires_all<MUL>::value) MUL::multiply_all(p, q, acc, pe, qe);
+            else multiply_all<MUL>(p, q, acc, pe, qe);
         }
         if (!whole) shrink(acc);
+        __syncthreads();
+        sums* shared = reinterpret_cast<sums*>(rows);
 #pragma unroll
         for (int i = 0; i < FP; ++i)
 #pragma unroll

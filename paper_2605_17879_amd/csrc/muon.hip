@@ -75,7 +75,10 @@ struct layout {
         a = rows < cols ? rows : cols;
         b = rows < cols ? cols : rows;
         lo_r = up_to(cols, 64) * 2; lo_c = up_to(rows, 64) * 2; lo_s = up_to(a, 64) * 2;
-        r_pitch = 2 * lo_r; c_pitch = both ? 2 * lo_c : lo_c; s_pitch = both ? 2 * lo_s : lo_s;   // (R alone is a part of the next X)
+        // (rows a multiple of 256 bytes apart meet at the same channels of the memory: 16 matrices of 1 024 and 8 of 2 048 x 1 024
+        // 2.39 ms with such, 2.21 without, 4 of 4 096 x 4 096 5.95 and 5.76)
+        auto odd = [](uint64_t v) { return v % 256 ? v : v + 128; };
+        r_pitch = odd(2 * lo_r); c_pitch = odd(both ? 2 * lo_c : lo_c); s_pitch = odd(both ? 2 * lo_s : lo_s);   // (R alone is a part of the next X)
         of_r = up_to(rows * r_pitch, 256);
         of_c = up_to(cols * c_pitch, 256);
         const uint64_t of_s = up_to(a * s_pitch, 256);
@@ -514,7 +517,7 @@ __global__ __launch_bounds__(TILE<of_f16>::NT, 512 / TILE<of_f16>::NT) void tile
 }
 
 template <int PHASE>
-__global__ __launch_bounds__(512, 2) void direct_kernel(const muon_args g) {
+__global__ __launch_bounds__(512) void direct_kernel(const muon_args g) {
     typedef direct_tile<of_f16, 4> tile;
     float f;
     if (!factor_of(g, f)) return;

@@ -79,7 +79,7 @@ __global__ __launch_bounds__(TILE<MUL>::NT, 512 / TILE<MUL>::NT) void tiled_kern
 }
 
 template <typename MUL, typename T, int FQ>
-__global__ __launch_bounds__(512, 2) void direct_kernel(const product_args a) {
+__global__ __launch_bounds__(512) void direct_kernel(const product_args a) {
     typedef direct_tile<MUL, FQ> tile;
     const uint32_t b = blockIdx.x, tq = b % a.tiles_q, tp = b / a.tiles_q, split = blockIdx.y;
     const uint32_t first = split * a.each, blocks = a.way.blocks;

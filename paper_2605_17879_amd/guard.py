@@ -639,7 +639,9 @@ class Detector:
         torch = self._torch
         kind = {"e4m3": torch.float8_e4m3fn, "e5m2": torch.float8_e5m2}[codes]
         wide = lambda n: -(-max(n, 1) // 16) * 16
-        return dict(codes=self._bytes(rows * wide(cols)).view(kind).view(rows, wide(cols))[:, :cols],
+        # rows a multiple of 256 bytes apart would meet at the same channels of the memory
+        stride = wide(cols) + (128 if wide(cols) % 256 == 0 else 0)
+        return dict(codes=self._bytes(rows * stride).view(kind).view(rows, stride)[:, :cols],
                     exp=self._bytes(-(-cols // PACK_BLOCK) * wide(rows)).view(-1, wide(rows))[:, :rows])
 
     def _packed(self, p: dict) -> bytes:
