@@ -34,8 +34,9 @@ using namespace gd_tiles;
 constexpr float ONE_X = 0x1p15f;                   // X and A are kept times 2^15: below 65 504 for values below 1.99
 constexpr uint32_t CHUNKS = 1024;                  // most pieces of a matrix that its sum of squares is taken in
 constexpr uint32_t CHUNK = 4096;                   // elements of a piece: a multiple of it
-enum { LARGE, SMALL, DIRECT, KINDS };
-constexpr uint32_t EDGE[KINDS] = {256, 128, 64};
+enum { LARGE, SMALL, DIRECT, KINDS, TINY = KINDS };   // tiles of the products; TINY: a matrix in one workgroup, in one launch
+constexpr uint32_t EDGE[KINDS + 1] = {256, 128, 64, 0};
+constexpr uint32_t TINY_A = 64, TINY_B = 192;      // the longest sides of a tiny matrix
 
 // ---- the table ---------------------------------------------------------------------------------
 
@@ -52,7 +53,7 @@ struct entry {
 struct head {
     uint64_t bytes;
     uint32_t magic, n;
-    uint32_t first[KINDS + 1];    // entries of a kind of tiles
+    uint32_t first[KINDS + 1];    // entries of a kind of tiles; behind the last one's lie the tiny ones
     uint32_t half[KINDS], full[KINDS];   // tiles of a symmetric product, and of the others
     uint32_t chunks, tiles;       // pieces of all matrices, and 64 x 64 of them
     uint64_t work[2];
@@ -75,7 +76,7 @@ struct layout {
         a = rows < cols ? rows : cols;
         b = rows < cols ? cols : rows;
         lo_r = up_to(cols, 64) * 2; lo_c = up_to(rows, 64) * 2; lo_s = up_to(a, 64) * 2;
-        // (rows a multiple of 256 bytes apart meet at the same channels of the memory: 16 matrices of 1 024 and 8 of 2 048 x 1 024
+        // (rows a multiple of 256 bytes apart meet at the same channels of the memory: 8 matrices of 1 024 x 1 024 and 8 of 2 048 x 1 024
         // 2.39 ms with such, 2.21 without, 4 of 4 096 x 4 096 5.95 and 5.76)
         auto odd = [](uint64_t v) { return v % 256 ? v : v + 128; };
         r_pitch = odd(2 * lo_r); c_pitch = odd(both ? 2 * lo_c : lo_c); s_pitch = odd(both ? 2 * lo_s : lo_s);   // (R alone is a part of the next X)
@@ -93,7 +94,8 @@ struct layout {
 
 struct muon_args {
     const uint8_t* table;
-    uint32_t n, first, count;     // entries; of the launch's kind
+    uint32_t n, tiled;            // entries, those that are not tiny
+    uint32_t first, count;        // entries of the launch's kind
     uint8_t* work;
     const float* grad_scale;
     uint32_t both;                // products of f32
@@ -184,7 +186,7 @@ __global__ __launch_bounds__(512) void momentum_kernel(const muon_args g) {
     float f;
     if (!factor_of(g, f)) return;
     uint32_t t = blockIdx.x;
-    const entry e = entry_at(g, find(g, OF_CHUNKS, 0, g.n, t));
+    const entry e = entry_at(g, find(g, OF_CHUNKS, 0, g.tiled, t));
     const uint64_t size = (uint64_t)e.rows * e.cols, from = (uint64_t)t * e.chunk, end = min(from + e.chunk, size);
     double s = 0;
     uint64_t i = from + threadIdx.x * 8;
@@ -248,7 +250,7 @@ __global__ __launch_bounds__(256) void start_kernel(const muon_args g) {
     float f;
     if (!factor_of(g, f)) return;
     uint32_t t = blockIdx.x;
-    const entry e = entry_at(g, find(g, OF_TILES, 0, g.n, t));
+    const entry e = entry_at(g, find(g, OF_TILES, 0, g.tiled, t));
     const double* part = reinterpret_cast<const double*>(g.work) + e.partial;
     double s = 0;
     for (uint32_t i = threadIdx.x; i < e.chunks; i += 256) s += part[i];
@@ -552,7 +554,7 @@ __global__ __launch_bounds__(256) void apply_kernel(const muon_args g) {
     float f;
     if (!factor_of(g, f)) return;
     uint32_t t = blockIdx.x;
-    const entry e = entry_at(g, find(g, OF_TILES, 0, g.n, t));
+    const entry e = entry_at(g, find(g, OF_TILES, 0, g.tiled, t));
     const layout l(e.rows, e.cols, g.both);
     const uint8_t* base = g.work + e.at[!g.both] + l.r(0);
     const uint32_t tiles_c = (e.cols + 63) / 64, row = t / tiles_c * 64 + threadIdx.x / 4, col = t % tiles_c * 64 + threadIdx.x % 4 * 16;
@@ -562,6 +564,166 @@ __global__ __launch_bounds__(256) void apply_kernel(const muon_args g) {
 #pragma unroll
     for (int x = 0; x < 16; ++x) v[x % 4][x / 4] = whole(from[x], from[l.lo_r / 2 + x]);
     update_row(g, e, row, col, v);
+}
+
+// ---- tiny matrices -------------------------------------------------------------------------------
+
+// A matrix of up to 64 x 192 (or 192 x 64), momentum to parameters: X as a lane holds it, in fp32, in registers, and as
+// operands in the LDS, hi and lo, both ways (R [i][j], C [j][i], i along the shorter side), A and B [i][i'].  A wave has pieces of 16 x 16 of a product: a
+// lane four neighbouring j of one i of X.  Five steps take 13 products one behind the other of some hundred cycles each; with the launches of
+// the larger matrices they took 6 to 8 us each (six of 64 x 96: 105 us).
+struct tiny_lds {
+    static constexpr uint32_t R = 2 * 2 * TINY_B, C = 2 * 2 * TINY_A, S = 2 * 2 * TINY_A;   // bytes of a row: hi, lo
+    uint8_t r[TINY_A * R], c[TINY_B * C], a[TINY_A * S], b[TINY_A * S];
+};
+
+// Where 16 bytes of a row lie: neighbouring rows' chunks on different banks.
+__device__ __forceinline__ uint32_t tiny_at(uint32_t row, uint32_t pitch, uint32_t byte) { return row * pitch + (byte ^ ((row & 7) << 4)); }
+
+// The product of 16 rows of P from p0 on and 16 of Q from q0 on, k_bytes of each along k, hi at 0 and lo behind `p_lo` (`q_lo`).
+__device__ __forceinline__ f32x4 tiny_product(const uint8_t* p, uint32_t p0, uint32_t p_pitch, const uint8_t* q, uint32_t q0, uint32_t q_pitch,
+                                              uint32_t k_bytes, bool both, uint32_t lane) {
+    const uint32_t pr = p0 + (lane & 15), qr = q0 + (lane & 15), at = (lane >> 4) * 16;
+    f32x4 low = {}, high = {};
+    for (uint32_t k = 0; k < k_bytes; k += 64) {
+        const f16x8 ph = *reinterpret_cast<const f16x8*>(p + tiny_at(pr, p_pitch, k + at)), qh = *reinterpret_cast<const f16x8*>(q + tiny_at(qr, q_pitch, k + at));
+        high = multiply_16(ph, qh, high);
+        if (both) {
+            const f16x8 pl = *reinterpret_cast<const f16x8*>(p + tiny_at(pr, p_pitch, p_pitch / 2 + k + at));
+            const f16x8 ql = *reinterpret_cast<const f16x8*>(q + tiny_at(qr, q_pitch, q_pitch / 2 + k + at));
+            low = multiply_16(pl, qh, low);
+            low = multiply_16(ph, ql, low);
+        }
+    }
+    return both ? high + low * SHRINK : high;
+}
+
+// Four neighbouring numbers of a row from `col` on.
+__device__ __forceinline__ void tiny_write(uint8_t* m, uint32_t pitch, uint32_t row, uint32_t col, const f32x4& x) {
+    const halves a = split(x[0]), b = split(x[1]), c = split(x[2]), d = split(x[3]);
+    *reinterpret_cast<f16x4*>(m + tiny_at(row, pitch, col * 2 & ~15u) + (col * 2 & 15)) = f16x4{a.hi, b.hi, c.hi, d.hi};
+    *reinterpret_cast<f16x4*>(m + tiny_at(row, pitch, (pitch / 2 + col * 2) & ~15u) + (col * 2 & 15)) = f16x4{a.lo, b.lo, c.lo, d.lo};
+}
+
+struct tiny_steps {
+    uint32_t steps;
+    float c[GD_MUON_MAX_STEPS][4];                 // a, b, c, and the power of two that B is kept times
+};
+
+__global__ __launch_bounds__(512) void tiny_kernel(const muon_args g, const tiny_steps way) {
+    __shared__ __attribute__((aligned(16))) tiny_lds lds;
+    constexpr int MINE = TINY_A / 16 * (TINY_B / 16) / 8, SQUARES = TINY_A / 16 * (TINY_A / 16) / 8;
+    float f;
+    if (!factor_of(g, f)) return;
+    const entry e = entry_at(g, g.first + blockIdx.x);
+    const bool tall = e.rows > e.cols, both = g.both;
+    const uint32_t a = tall ? e.cols : e.rows, b = tall ? e.rows : e.cols;
+    const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    const uint32_t ni = (a + 31) / 32 * 2, nj = (b + 31) / 32 * 2;      // pieces: whole steps of k of 32
+    // piece t: i from 16 (t % ni) on, j from 16 (t / ni) on
+    auto i_of = [&](uint32_t t) { return t % ni * 16 + (lane & 15); };
+    auto j_of = [&](uint32_t t) { return t / ni * 16 + 4 * (lane >> 4); };
+    auto place = [&](uint32_t i, uint32_t j) { return tall ? (uint64_t)j * e.cols + i : (uint64_t)i * e.cols + j; };
+    f32x4 x[MINE];
+    double sum = 0;
+#pragma unroll
+    for (int k = 0; k < MINE; ++k) {
+        const uint32_t t = wave + 8 * k;
+        x[k] = f32x4{0, 0, 0, 0};
+        if (t >= ni * nj) continue;
+        const uint32_t i = i_of(t), j = j_of(t);
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+            if (i < a && j + r < b) {
+                const uint64_t at = place(i, j + r);
+                const float gr = g.grad_scale ? grad_at(e, at) * f : grad_at(e, at), m = e.m[at] * g.mu + gr;
+                e.m[at] = m;
+                x[k][r] = update_of(g, gr, m);
+                sum += (double)x[k][r] * x[k][r];
+            }
+    }
+    const double size = sqrt(sum_of_all(sum)) + g.eps, scale = size == 0 ? 0 : ONE_X / size;
+    auto keep_x = [&]() {
+#pragma unroll
+        for (int k = 0; k < MINE; ++k) {
+            const uint32_t t = wave + 8 * k;
+            if (t >= ni * nj) continue;
+            const uint32_t i = i_of(t), j = j_of(t);
+            tiny_write(lds.r, tiny_lds::R, i, j, x[k]);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const halves h = split(x[k][r]);
+                *reinterpret_cast<gd_f16*>(lds.c + tiny_at(j + r, tiny_lds::C, i * 2 & ~15u) + (i * 2 & 15)) = h.hi;
+                *reinterpret_cast<gd_f16*>(lds.c + tiny_at(j + r, tiny_lds::C, (tiny_lds::C / 2 + i * 2) & ~15u) + (i * 2 & 15)) = h.lo;
+            }
+        }
+        __syncthreads();
+    };
+#pragma unroll
+    for (int k = 0; k < MINE; ++k)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) x[k][r] = (float)(x[k][r] * scale);
+    if (way.steps) keep_x();
+    for (uint32_t s = 0; s < way.steps; ++s) {
+        const float ca = way.c[s][0], cb = way.c[s][1], cc = way.c[s][2], one_b = way.c[s][3];
+        f32x4 mine[SQUARES];
+        // A, of which a piece's row i' is along P
+#pragma unroll
+        for (int k = 0; k < SQUARES; ++k) {
+            const uint32_t t = wave + 8 * k;
+            if (t >= ni * ni) continue;
+            const uint32_t to = t / ni * 16, from = t % ni * 16;
+            mine[k] = tiny_product(lds.r, to, tiny_lds::R, lds.r, from, tiny_lds::R, nj * 32, both, lane) * (1 / ONE_X);
+            tiny_write(lds.a, tiny_lds::S, from + (lane & 15), to + 4 * (lane >> 4), mine[k]);
+        }
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < SQUARES; ++k) {
+            const uint32_t t = wave + 8 * k;
+            if (t >= ni * ni) continue;
+            const uint32_t to = t / ni * 16, from = t % ni * 16;
+            const f32x4 square = tiny_product(lds.a, to, tiny_lds::S, lds.a, from, tiny_lds::S, ni * 32, both, lane);
+            const f32x4 w = (square * (cc / (ONE_X * ONE_X)) + mine[k] * (cb / ONE_X)) * one_b;
+            tiny_write(lds.b, tiny_lds::S, from + (lane & 15), to + 4 * (lane >> 4), w);
+        }
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < MINE; ++k) {
+            const uint32_t t = wave + 8 * k;
+            if (t >= ni * nj) continue;
+            x[k] = x[k] * ca + tiny_product(lds.c, t / ni * 16, tiny_lds::C, lds.b, t % ni * 16, tiny_lds::S, ni * 32, both, lane) * (1 / one_b);
+        }
+        if (s + 1 < way.steps) {
+            __syncthreads();                       // (X read by all)
+            keep_x();
+        }
+    }
+    const double rate = g.lr * e.lr_scale;
+    const float keep = (float)(1.0 - rate * e.decay), move = (float)(rate / ONE_X);
+#pragma unroll
+    for (int k = 0; k < MINE; ++k) {
+        const uint32_t t = wave + 8 * k;
+        if (t >= ni * nj) continue;
+        const uint32_t i = i_of(t), j = j_of(t);
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+            if (i < a && j + r < b) {
+                const uint64_t at = place(i, j + r);
+                float p;
+                if (e.param_type == GD_F32) {
+                    float* q = static_cast<float*>(e.param) + at;
+                    *q = p = *q * keep - x[k][r] * move;
+                } else if (e.param_type == GD_BF16) {
+                    gd_bf16* q = static_cast<gd_bf16*>(e.param) + at;
+                    *q = gd_from_f32<gd_bf16>(p = gd_to_f32(*q) * keep - x[k][r] * move);
+                } else {
+                    gd_f16* q = static_cast<gd_f16*>(e.param) + at;
+                    *q = gd_from_f32<gd_f16>(p = gd_to_f32(*q) * keep - x[k][r] * move);
+                }
+                if (e.copy && e.copy_type == GD_BF16) static_cast<gd_bf16*>(e.copy)[at] = gd_from_f32<gd_bf16>(p);
+                if (e.copy && e.copy_type == GD_F16) static_cast<gd_f16*>(e.copy)[at] = gd_from_f32<gd_f16>(p);
+            }
+    }
 }
 
 template <int PHASE>
@@ -588,6 +750,8 @@ void choose_kinds(const gd_muon_tensor* t, uint32_t n, std::vector<int>& kinds) 
     auto side = [&](uint32_t i) { return std::min(t[i].rows, t[i].cols); };
     auto fills = [&](uint32_t i) { return side(i) >= 512 && tiles_of(t[i], 256) * 4 * 10 <= tiles_of(t[i], 128) * 13; };
     uint64_t large = 0, direct = 0;
+    for (uint32_t i = 0; i < n; ++i)
+        if (side(i) <= TINY_A && std::max(t[i].rows, t[i].cols) <= TINY_B) kinds[i] = TINY;
     for (uint32_t i = 0; i < n; ++i)
         if (fills(i)) large += tiles_of(t[i], 256);
     for (uint32_t i = 0; i < n; ++i)
@@ -625,7 +789,7 @@ double most_of_even(double b, double c, double s) {
 }  // namespace
 
 size_t gd_muon_table(const gd_muon_tensor* t, uint32_t n, void* out) {
-    std::vector<uint32_t> order[KINDS];
+    std::vector<uint32_t> order[KINDS + 1];
     std::vector<int> kinds;
     choose_kinds(t, n, kinds);
     uint32_t there = 0;
@@ -647,12 +811,12 @@ size_t gd_muon_table(const gd_muon_tensor* t, uint32_t n, void* out) {
     for (uint32_t i = 0; i < n; ++i) chunks += (t[i].rows * t[i].cols + CHUNK - 1) / CHUNK;   // (an upper bound)
     work[0] = work[1] = gd_align256(std::min<uint64_t>(chunks, (uint64_t)there * CHUNKS) * 8);
     chunks = 0;
-    for (int kind = 0; kind < KINDS; ++kind) {
+    for (int kind = 0; kind <= KINDS; ++kind) {
         uint64_t half = 0, full = 0;
         h.first[kind] = k;
         for (uint32_t i : order[kind]) {
             const gd_muon_tensor& x = t[i];
-            const uint64_t size = x.rows * x.cols, edge = EDGE[kind];
+            const uint64_t size = x.rows * x.cols, edge = std::max(EDGE[kind], 1u);
             entry e = {};
             e.param = x.d_param; e.grad = x.d_grad; e.m = static_cast<float*>(x.d_m); e.copy = x.d_copy;
             e.lr_scale = x.lr_scale; e.decay = x.weight_decay;
@@ -668,20 +832,21 @@ size_t gd_muon_table(const gd_muon_tensor* t, uint32_t n, void* out) {
                 memcpy(to + HEAD + k * sizeof(entry), &e, sizeof(e));
                 for (int b = 0; b < LISTS; ++b) memcpy(to + list_at(there, b) + 4ull * k, &begins[b], 4);
             }
+            ++k;
+            if (kind == TINY) continue;
             for (int b = 0; b < 2; ++b) work[b] += layout(e.rows, e.cols, b == 0).total;
             chunks += e.chunks;
             tiles += ((x.rows + 63) / 64) * ((x.cols + 63) / 64);
             half += ta * (ta + 1) / 2;
             full += tr * tc;
-            ++k;
         }
         // (launches of fewer than 2^32 threads)
-        if (half >= 1u << 23 || full >= 1u << 23) return 0;
+        if (half >= 1u << 23 || full >= 1u << 23 || k >= 1u << 23) return 0;
+        if (kind == TINY) break;
         h.half[kind] = (uint32_t)half;
         h.full[kind] = (uint32_t)full;
     }
     if (chunks >= 1u << 23 || tiles >= 1u << 24) return 0;
-    h.first[KINDS] = k;
     h.chunks = (uint32_t)chunks;
     h.tiles = (uint32_t)tiles;
     h.work[0] = work[0];
@@ -720,9 +885,14 @@ hipError_t gd_launch_muon(const gd_muon_args& m, hipStream_t s) {
     muon_args g = {};
     g.table = m.table; g.n = h.n; g.work = m.work; g.grad_scale = m.grad_scale;
     g.both = m.both; g.mu = m.momentum; g.eps = m.eps; g.nesterov = m.nesterov; g.lr = m.lr;
-    momentum_kernel<<<h.chunks, 512, 0, s>>>(g);
-    start_kernel<<<h.tiles, 256, 0, s>>>(g);
-    if (m.steps == 0) apply_kernel<<<h.tiles, 256, 0, s>>>(g);
+    g.tiled = h.first[TINY];
+    if (g.tiled) {
+        momentum_kernel<<<h.chunks, 512, 0, s>>>(g);
+        start_kernel<<<h.tiles, 256, 0, s>>>(g);
+        if (m.steps == 0) apply_kernel<<<h.tiles, 256, 0, s>>>(g);
+    }
+    tiny_steps way;
+    way.steps = m.steps;
     double most = 1.001;
     for (uint32_t i = 0; i < m.steps; ++i) {
         const double* c = m.coefficients + 3 * i;
@@ -731,12 +901,19 @@ hipError_t gd_launch_muon(const gd_muon_args& m, hipStream_t s) {
         const double b_most = most_of_even(c[1], c[2], most);
         g.one_b = (float)std::exp2(std::min(15.0, std::floor(std::log2(32768.0 / std::max(b_most, 1e-30)))));
         most = most_of(c[0], c[1], c[2], most) * 1.001;
+        const float of_step[4] = {g.a, g.b, g.c, g.one_b};
+        memcpy(way.c[i], of_step, sizeof(of_step));
+        if (!g.tiled) continue;
         g.from = i & 1;
         g.to = 1 - g.from;
         launch_phase<OF_X>(g, h, s);
         launch_phase<OF_A>(g, h, s);
         if (i + 1 < m.steps) launch_phase<STEP>(g, h, s);
         else launch_phase<LAST>(g, h, s);
+    }
+    if (h.n > g.tiled) {
+        g.first = g.tiled;
+        tiny_kernel<<<h.n - g.tiled, 512, 0, s>>>(g, way);
     }
     return hipGetLastError();
 }
