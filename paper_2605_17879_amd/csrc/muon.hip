@@ -359,7 +359,7 @@ __device__ __forceinline__ void finish_row(const muon_args& g, const entry& e, c
         return;
     }
     gd_vec<gd_f16, 8> hi[2] = {}, lo[2] = {};
-    if (row < o.rows && col < o.d_lo / 2) {        // (zeros up to the end of a block)
+    if (row < o.rows && col < o.d_lo / 2) {
         const gd_f16* from = reinterpret_cast<const gd_f16*>(o.old + row * o.d_pitch) + col;
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
@@ -373,7 +373,7 @@ __device__ __forceinline__ void finish_row(const muon_args& g, const entry& e, c
         float w = v[x % 4][x / 4];
         if (PHASE == OF_A) w = (g.c * (w * (1 / (ONE_X * ONE_X))) + g.b * (old * (1 / ONE_X))) * g.one_b;
         else w = g.a * old + w * (1 / g.one_b);
-        v[x % 4][x / 4] = row < o.rows && col + x < o.cols ? w : 0.0f;
+        v[x % 4][x / 4] = row < o.rows && col + x < o.cols ? w : 0.0f;   // (zeros up to the end of a block)
     }
 }
 
@@ -574,28 +574,48 @@ __global__ __launch_bounds__(256) void apply_kernel(const muon_args g) {
 // the larger matrices they took 6 to 8 us each (six of 64 x 96: 105 us).
 struct tiny_lds {
     static constexpr uint32_t R = 2 * 2 * TINY_B, C = 2 * 2 * TINY_A, S = 2 * 2 * TINY_A;   // bytes of a row: hi, lo
-    uint8_t r[TINY_A * R], c[TINY_B * C], a[TINY_A * S], b[TINY_A * S];
+    uint8_t r[TINY_A * R], c[TINY_B * C];
+    union {
+        struct {
+            uint8_t a[TINY_A * S], b[TINY_A * S];
+        };
+        float u[TINY_A * TINY_B];                  // before the steps U, behind them X, as the matrix lies
+    };
 };
 
 // Where 16 bytes of a row lie: neighbouring rows' chunks on different banks.
 __device__ __forceinline__ uint32_t tiny_at(uint32_t row, uint32_t pitch, uint32_t byte) { return row * pitch + (byte ^ ((row & 7) << 4)); }
 
-// The product of 16 rows of P from p0 on and 16 of Q from q0 on, k_bytes of each along k, hi at 0 and lo behind `p_lo` (`q_lo`).
-__device__ __forceinline__ f32x4 tiny_product(const uint8_t* p, uint32_t p0, uint32_t p_pitch, const uint8_t* q, uint32_t q0, uint32_t q_pitch,
-                                              uint32_t k_bytes, bool both, uint32_t lane) {
-    const uint32_t pr = p0 + (lane & 15), qr = q0 + (lane & 15), at = (lane >> 4) * 16;
-    f32x4 low = {}, high = {};
+// N products of 16 rows of P from p0 on and 16 of Q from q0 on, k_bytes of each along k, hi at 0 and lo half a pitch behind it:
+// side by side, so that one's sums and reads are under way while another's are waited for.
+template <int N>
+__device__ __forceinline__ void tiny_products(f32x4 (&out)[N], const uint8_t* p, const uint32_t (&p0)[N], uint32_t p_pitch, const uint8_t* q,
+                                              const uint32_t (&q0)[N], uint32_t q_pitch, uint32_t k_bytes, bool both, uint32_t lane) {
+    const uint32_t row = lane & 15, at = (lane >> 4) * 16;
+    f32x4 low[N] = {}, high[N] = {};
     for (uint32_t k = 0; k < k_bytes; k += 64) {
-        const f16x8 ph = *reinterpret_cast<const f16x8*>(p + tiny_at(pr, p_pitch, k + at)), qh = *reinterpret_cast<const f16x8*>(q + tiny_at(qr, q_pitch, k + at));
-        high = multiply_16(ph, qh, high);
-        if (both) {
-            const f16x8 pl = *reinterpret_cast<const f16x8*>(p + tiny_at(pr, p_pitch, p_pitch / 2 + k + at));
-            const f16x8 ql = *reinterpret_cast<const f16x8*>(q + tiny_at(qr, q_pitch, q_pitch / 2 + k + at));
-            low = multiply_16(pl, qh, low);
-            low = multiply_16(ph, ql, low);
+        f16x8 ph[N], qh[N], pl[N], ql[N];
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            ph[n] = *reinterpret_cast<const f16x8*>(p + tiny_at(p0[n] + row, p_pitch, k + at));
+            qh[n] = *reinterpret_cast<const f16x8*>(q + tiny_at(q0[n] + row, q_pitch, k + at));
         }
+        if (both) {
+#pragma unroll
+            for (int n = 0; n < N; ++n) {
+                pl[n] = *reinterpret_cast<const f16x8*>(p + tiny_at(p0[n] + row, p_pitch, p_pitch / 2 + k + at));
+                ql[n] = *reinterpret_cast<const f16x8*>(q + tiny_at(q0[n] + row, q_pitch, q_pitch / 2 + k + at));
+            }
+#pragma unroll
+            for (int n = 0; n < N; ++n) low[n] = multiply_16(pl[n], qh[n], low[n]);
+#pragma unroll
+            for (int n = 0; n < N; ++n) low[n] = multiply_16(ph[n], ql[n], low[n]);
+        }
+#pragma unroll
+        for (int n = 0; n < N; ++n) high[n] = multiply_16(ph[n], qh[n], high[n]);
     }
-    return both ? high + low * SHRINK : high;
+#pragma unroll
+    for (int n = 0; n < N; ++n) out[n] = high[n] + low[n] * SHRINK;
 }
 
 // Four neighbouring numbers of a row from `col` on.
@@ -603,6 +623,41 @@ __device__ __forceinline__ void tiny_write(uint8_t* m, uint32_t pitch, uint32_t 
     const halves a = split(x[0]), b = split(x[1]), c = split(x[2]), d = split(x[3]);
     *reinterpret_cast<f16x4*>(m + tiny_at(row, pitch, col * 2 & ~15u) + (col * 2 & 15)) = f16x4{a.hi, b.hi, c.hi, d.hi};
     *reinterpret_cast<f16x4*>(m + tiny_at(row, pitch, (pitch / 2 + col * 2) & ~15u) + (col * 2 & 15)) = f16x4{a.lo, b.lo, c.lo, d.lo};
+}
+
+// Numbers from, from + 512, ... of a gradient of `all`.
+template <int N>
+__device__ __forceinline__ void grads_of(const entry& e, uint32_t from, uint32_t all, float (&x)[N]) {
+    if (e.grad_type == GD_F32) {
+#pragma unroll
+        for (int k = 0; k < N; ++k) x[k] = static_cast<const float*>(e.grad)[min(from + 512 * k, all - 1)];
+    } else {
+        uint16_t q[N];
+#pragma unroll
+        for (int k = 0; k < N; ++k) q[k] = static_cast<const uint16_t*>(e.grad)[min(from + 512 * k, all - 1)];
+#pragma unroll
+        for (int k = 0; k < N; ++k) x[k] = e.grad_type == GD_BF16 ? gd_to_f32(__builtin_bit_cast(gd_bf16, q[k])) : gd_to_f32(__builtin_bit_cast(gd_f16, q[k]));
+    }
+}
+
+template <typename T>
+__device__ __forceinline__ void tiny_update(const entry& e, const float* x, uint32_t all, float keep, float move) {
+    constexpr int N = 8;
+    T* p = static_cast<T*>(e.param);
+    for (uint32_t from = threadIdx.x; from < all; from += 512 * N) {
+        T q[N];
+#pragma unroll
+        for (int k = 0; k < N; ++k) q[k] = p[min(from + 512 * k, all - 1)];
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+            const uint32_t i = from + 512 * k;
+            if (i >= all) break;
+            const float w = gd_to_f32(q[k]) * keep - x[i] * move;
+            p[i] = gd_from_f32<T>(w);
+            if (e.copy && e.copy_type == GD_BF16) static_cast<gd_bf16*>(e.copy)[i] = gd_from_f32<gd_bf16>(w);
+            if (e.copy && e.copy_type == GD_F16) static_cast<gd_f16*>(e.copy)[i] = gd_from_f32<gd_f16>(w);
+        }
+    }
 }
 
 struct tiny_steps {
@@ -623,25 +678,29 @@ __global__ __launch_bounds__(512) void tiny_kernel(const muon_args g, const tiny
     // piece t: i from 16 (t % ni) on, j from 16 (t / ni) on
     auto i_of = [&](uint32_t t) { return t % ni * 16 + (lane & 15); };
     auto j_of = [&](uint32_t t) { return t / ni * 16 + 4 * (lane >> 4); };
-    auto place = [&](uint32_t i, uint32_t j) { return tall ? (uint64_t)j * e.cols + i : (uint64_t)i * e.cols + j; };
-    f32x4 x[MINE];
+    auto place = [&](uint32_t i, uint32_t j) { return tall ? j * e.cols + i : i * e.cols + j; };
+    // Eight numbers of a lane are asked for before one is written.  (All code is read from memory once a workgroup: loops that are
+    // unrolled to 52 KB took as long as what they did.)
+    constexpr int AT_ONCE = 8;
+    const uint32_t all = a * b;
     double sum = 0;
+    for (uint32_t from = threadIdx.x; from < all; from += 512 * AT_ONCE) {
+        float gr[AT_ONCE], m[AT_ONCE];
 #pragma unroll
-    for (int k = 0; k < MINE; ++k) {
-        const uint32_t t = wave + 8 * k;
-        x[k] = f32x4{0, 0, 0, 0};
-        if (t >= ni * nj) continue;
-        const uint32_t i = i_of(t), j = j_of(t);
+        for (int k = 0; k < AT_ONCE; ++k) m[k] = e.m[min(from + 512 * k, all - 1)];
+        grads_of<AT_ONCE>(e, from, all, gr);
 #pragma unroll
-        for (int r = 0; r < 4; ++r)
-            if (i < a && j + r < b) {
-                const uint64_t at = place(i, j + r);
-                const float gr = g.grad_scale ? grad_at(e, at) * f : grad_at(e, at), m = e.m[at] * g.mu + gr;
-                e.m[at] = m;
-                x[k][r] = update_of(g, gr, m);
-                sum += (double)x[k][r] * x[k][r];
-            }
+        for (int k = 0; k < AT_ONCE; ++k) {
+            if (g.grad_scale) gr[k] *= f;
+            m[k] = m[k] * g.mu + gr[k];
+            if (from + 512 * k >= all) break;
+            e.m[from + 512 * k] = m[k];
+            const float u = update_of(g, gr[k], m[k]);
+            lds.u[from + 512 * k] = u;
+            sum += (double)u * u;
+        }
     }
+    f32x4 x[MINE];
     const double size = sqrt(sum_of_all(sum)) + g.eps, scale = size == 0 ? 0 : ONE_X / size;
     auto keep_x = [&]() {
 #pragma unroll
@@ -660,70 +719,72 @@ __global__ __launch_bounds__(512) void tiny_kernel(const muon_args g, const tiny
         __syncthreads();
     };
 #pragma unroll
-    for (int k = 0; k < MINE; ++k)
+    for (int k = 0; k < MINE; ++k) {
+        const uint32_t t = wave + 8 * k, i = i_of(t), j = j_of(t);
 #pragma unroll
-        for (int r = 0; r < 4; ++r) x[k][r] = (float)(x[k][r] * scale);
+        for (int r = 0; r < 4; ++r) x[k][r] = t < ni * nj && i < a && j + r < b ? (float)(lds.u[place(i, j + r)] * scale) : 0.0f;
+    }
+    __syncthreads();
     if (way.steps) keep_x();
     for (uint32_t s = 0; s < way.steps; ++s) {
         const float ca = way.c[s][0], cb = way.c[s][1], cc = way.c[s][2], one_b = way.c[s][3];
-        f32x4 mine[SQUARES];
-        // A, of which a piece's row i' is along P
+        // (a piece that is not there: the last one again, written by the wave that has it)
+        uint32_t to[SQUARES], from[SQUARES];
 #pragma unroll
         for (int k = 0; k < SQUARES; ++k) {
-            const uint32_t t = wave + 8 * k;
-            if (t >= ni * ni) continue;
-            const uint32_t to = t / ni * 16, from = t % ni * 16;
-            mine[k] = tiny_product(lds.r, to, tiny_lds::R, lds.r, from, tiny_lds::R, nj * 32, both, lane) * (1 / ONE_X);
-            tiny_write(lds.a, tiny_lds::S, from + (lane & 15), to + 4 * (lane >> 4), mine[k]);
+            const uint32_t t = min(wave + 8 * k, ni * ni - 1);
+            to[k] = t / ni * 16;
+            from[k] = t % ni * 16;
         }
-        __syncthreads();
+        f32x4 mine[SQUARES], square[SQUARES];
+        // A, of which a piece's row is along Q
+        tiny_products(mine, lds.r, to, tiny_lds::R, lds.r, from, tiny_lds::R, nj * 32, both, lane);
 #pragma unroll
         for (int k = 0; k < SQUARES; ++k) {
-            const uint32_t t = wave + 8 * k;
-            if (t >= ni * ni) continue;
-            const uint32_t to = t / ni * 16, from = t % ni * 16;
-            const f32x4 square = tiny_product(lds.a, to, tiny_lds::S, lds.a, from, tiny_lds::S, ni * 32, both, lane);
-            const f32x4 w = (square * (cc / (ONE_X * ONE_X)) + mine[k] * (cb / ONE_X)) * one_b;
-            tiny_write(lds.b, tiny_lds::S, from + (lane & 15), to + 4 * (lane >> 4), w);
+            mine[k] *= 1 / ONE_X;
+            if (wave + 8 * k < ni * ni) tiny_write(lds.a, tiny_lds::S, from[k] + (lane & 15), to[k] + 4 * (lane >> 4), mine[k]);
         }
         __syncthreads();
+        tiny_products(square, lds.a, to, tiny_lds::S, lds.a, from, tiny_lds::S, ni * 32, both, lane);
 #pragma unroll
-        for (int k = 0; k < MINE; ++k) {
-            const uint32_t t = wave + 8 * k;
-            if (t >= ni * nj) continue;
-            x[k] = x[k] * ca + tiny_product(lds.c, t / ni * 16, tiny_lds::C, lds.b, t % ni * 16, tiny_lds::S, ni * 32, both, lane) * (1 / one_b);
+        for (int k = 0; k < SQUARES; ++k)
+            if (wave + 8 * k < ni * ni)
+                tiny_write(lds.b, tiny_lds::S, from[k] + (lane & 15), to[k] + 4 * (lane >> 4), (square[k] * (cc / (ONE_X * ONE_X)) + mine[k] * (cb / ONE_X)) * one_b);
+        __syncthreads();
+#pragma unroll
+        for (int first = 0; first < MINE; first += 3) {
+            if (wave + 8 * first >= ni * nj) break;
+            uint32_t j0[3], i0[3];
+#pragma unroll
+            for (int k = 0; k < 3; ++k) {
+                const uint32_t t = min(wave + 8 * (first + k), ni * nj - 1);
+                j0[k] = t / ni * 16;
+                i0[k] = t % ni * 16;
+            }
+            f32x4 bx[3];
+            tiny_products(bx, lds.c, j0, tiny_lds::C, lds.b, i0, tiny_lds::S, ni * 32, both, lane);
+#pragma unroll
+            for (int k = 0; k < 3; ++k) x[first + k] = x[first + k] * ca + bx[k] * (1 / one_b);
         }
         if (s + 1 < way.steps) {
             __syncthreads();                       // (X read by all)
             keep_x();
         }
     }
-    const double rate = g.lr * e.lr_scale;
-    const float keep = (float)(1.0 - rate * e.decay), move = (float)(rate / ONE_X);
+    __syncthreads();                               // (A and B read by all)
 #pragma unroll
     for (int k = 0; k < MINE; ++k) {
-        const uint32_t t = wave + 8 * k;
-        if (t >= ni * nj) continue;
-        const uint32_t i = i_of(t), j = j_of(t);
+        const uint32_t t = wave + 8 * k, i = i_of(t), j = j_of(t);
 #pragma unroll
         for (int r = 0; r < 4; ++r)
-            if (i < a && j + r < b) {
-                const uint64_t at = place(i, j + r);
-                float p;
-                if (e.param_type == GD_F32) {
-                    float* q = static_cast<float*>(e.param) + at;
-                    *q = p = *q * keep - x[k][r] * move;
-                } else if (e.param_type == GD_BF16) {
-                    gd_bf16* q = static_cast<gd_bf16*>(e.param) + at;
-                    *q = gd_from_f32<gd_bf16>(p = gd_to_f32(*q) * keep - x[k][r] * move);
-                } else {
-                    gd_f16* q = static_cast<gd_f16*>(e.param) + at;
-                    *q = gd_from_f32<gd_f16>(p = gd_to_f32(*q) * keep - x[k][r] * move);
-                }
-                if (e.copy && e.copy_type == GD_BF16) static_cast<gd_bf16*>(e.copy)[at] = gd_from_f32<gd_bf16>(p);
-                if (e.copy && e.copy_type == GD_F16) static_cast<gd_f16*>(e.copy)[at] = gd_from_f32<gd_f16>(p);
-            }
+            if (t < ni * nj && i < a && j + r < b) lds.u[place(i, j + r)] = x[k][r];
     }
+    __syncthreads();
+    const double rate = g.lr * e.lr_scale;
+    const float keep = (float)(1.0 - rate * e.decay), move = (float)(rate / ONE_X);
+    if (e.param_type == GD_F32) tiny_update<float>(e, lds.u, all, keep, move);
+    else if (e.param_type == GD_BF16) tiny_update<gd_bf16>(e, lds.u, all, keep, move);
+    else tiny_update<gd_f16>(e, lds.u, all, keep, move);
 }
 
 template <int PHASE>
@@ -761,7 +822,7 @@ void choose_kinds(const gd_muon_tensor* t, uint32_t n, std::vector<int>& kinds) 
         if (kinds[i] == DIRECT && side(i) > 64 && direct > 512) kinds[i] = SMALL;
 }
 
-// The largest magnitude of a polynomial c1 x + c3 x^3 + c5 x^5 (of b x^2 + c x^4 with `even`) over [0, s].
+// The largest magnitude of a polynomial c1 x + c3 x^3 + c5 x^5, and of b x^2 + c x^4, over [0, s].
 double most_of(double c1, double c3, double c5, double s) {
     double most = 0;
     auto look = [&](double x2) {
