@@ -36,7 +36,7 @@ constexpr uint32_t CHUNKS = 1024;                  // most pieces of a matrix th
 constexpr uint32_t CHUNK = 4096;                   // elements of a piece: a multiple of it
 enum { LARGE, SMALL, DIRECT, KINDS, TINY = KINDS };   // tiles of the products; TINY: a matrix in one workgroup, in one launch
 constexpr uint32_t EDGE[KINDS + 1] = {256, 128, 64, 0};
-constexpr uint32_t TINY_A = 64, TINY_B = 192;      // the longest sides of a tiny matrix
+constexpr uint32_t TINY_NT = 512, TINY_A = 64, TINY_B = 192;      // the longest sides of a tiny matrix
 
 // ---- the table ---------------------------------------------------------------------------------
 
@@ -573,7 +573,7 @@ __global__ __launch_bounds__(256) void apply_kernel(const muon_args g) {
 // lane four neighbouring j of one i of X.  Five steps take 13 products one behind the other of some hundred cycles each; with the launches of
 // the larger matrices they took 6 to 8 us each (six of 64 x 96: 105 us).
 struct tiny_lds {
-    static constexpr uint32_t R = 2 * 2 * TINY_B, C = 2 * 2 * TINY_A, S = 2 * 2 * TINY_A;   // bytes of a row: hi, lo
+    static constexpr uint32_t R = 2 * 2 * TINY_B, C = 2 * 2 * TINY_A, S = C;   // bytes of a row: hi, lo
     uint8_t r[TINY_A * R], c[TINY_B * C];
     union {
         struct {
@@ -583,58 +583,67 @@ struct tiny_lds {
     };
 };
 
-// Where 16 bytes of a row lie: neighbouring rows' chunks on different banks.
-__device__ __forceinline__ uint32_t tiny_at(uint32_t row, uint32_t pitch, uint32_t byte) { return row * pitch + (byte ^ ((row & 7) << 4)); }
+// Rows of 256 bytes for each 64 numbers: 128 of hi, 128 of lo.  In rows 8 to 15 of each 16 they change places, and of
+// each 128 bytes chunk c lies at c ^ (row % 8), so that a read of sixteen rows meets every bank once (they bound the products: rows that met
+// half of the banks 28.3 us for six of 96 x 64).  `at` is where a row's first 64 bytes of hi are; this is `shared` bytes of hi (a multiple of 32, the
+// same for all lanes) further on; lo is at ^ 128.
+__device__ __forceinline__ uint32_t tiny_further(uint32_t at, uint32_t shared) { return (at ^ (shared & 96)) + (shared & ~127u) * 2; }
+__device__ __forceinline__ constexpr uint32_t tiny_turn(uint32_t row) { return (row & 15) * 16; }
 
-// N products of 16 rows of P from p0 on and 16 of Q from q0 on, k_bytes of each along k, hi at 0 and lo half a pitch behind it:
-// side by side, so that one's sums and reads are under way while another's are waited for.
-template <int N>
-__device__ __forceinline__ void tiny_products(f32x4 (&out)[N], const uint8_t* p, const uint32_t (&p0)[N], uint32_t p_pitch, const uint8_t* q,
-                                              const uint32_t (&q0)[N], uint32_t q_pitch, uint32_t k_bytes, bool both, uint32_t lane) {
-    const uint32_t row = lane & 15, at = (lane >> 4) * 16;
+// N products of 16 rows of P and the same 16 of Q, k_bytes (a multiple of 64) of each along k: side by side, so that one's sums and reads
+// are under way while another's are waited for.
+template <uint32_t P_PITCH, uint32_t Q_PITCH, int N>
+__device__ __forceinline__ void tiny_products(f32x4 (&out)[N], const uint8_t* p, const uint32_t (&p0)[N], uint32_t p_row, const uint8_t* q,
+                                              uint32_t q0, uint32_t q_row, uint32_t k_bytes, bool both) {
     f32x4 low[N] = {}, high[N] = {};
+    q_row += q0 * Q_PITCH;
     for (uint32_t k = 0; k < k_bytes; k += 64) {
-        f16x8 ph[N], qh[N], pl[N], ql[N];
+        const uint32_t pk = tiny_further(p_row, k), qk = tiny_further(q_row, k);
+        f16x8 ph[N], pl[N];
+        const f16x8 qh = *reinterpret_cast<const f16x8*>(q + qk);
 #pragma unroll
-        for (int n = 0; n < N; ++n) {
-            ph[n] = *reinterpret_cast<const f16x8*>(p + tiny_at(p0[n] + row, p_pitch, k + at));
-            qh[n] = *reinterpret_cast<const f16x8*>(q + tiny_at(q0[n] + row, q_pitch, k + at));
-        }
+        for (int n = 0; n < N; ++n) ph[n] = *reinterpret_cast<const f16x8*>(p + pk + p0[n] * P_PITCH);
         if (both) {
+            const f16x8 ql = *reinterpret_cast<const f16x8*>(q + (qk ^ 128));
 #pragma unroll
-            for (int n = 0; n < N; ++n) {
-                pl[n] = *reinterpret_cast<const f16x8*>(p + tiny_at(p0[n] + row, p_pitch, p_pitch / 2 + k + at));
-                ql[n] = *reinterpret_cast<const f16x8*>(q + tiny_at(q0[n] + row, q_pitch, q_pitch / 2 + k + at));
-            }
+            for (int n = 0; n < N; ++n) pl[n] = *reinterpret_cast<const f16x8*>(p + (pk ^ 128) + p0[n] * P_PITCH);
 #pragma unroll
-            for (int n = 0; n < N; ++n) low[n] = multiply_16(pl[n], qh[n], low[n]);
+            for (int n = 0; n < N; ++n) low[n] = multiply_16(pl[n], qh, low[n]);
 #pragma unroll
-            for (int n = 0; n < N; ++n) low[n] = multiply_16(ph[n], ql[n], low[n]);
+            for (int n = 0; n < N; ++n) low[n] = multiply_16(ph[n], ql, low[n]);
         }
 #pragma unroll
-        for (int n = 0; n < N; ++n) high[n] = multiply_16(ph[n], qh[n], high[n]);
+        for (int n = 0; n < N; ++n) high[n] = multiply_16(ph[n], qh, high[n]);
     }
 #pragma unroll
     for (int n = 0; n < N; ++n) out[n] = high[n] + low[n] * SHRINK;
 }
 
-// Four neighbouring numbers of a row from `col` on.
-__device__ __forceinline__ void tiny_write(uint8_t* m, uint32_t pitch, uint32_t row, uint32_t col, const f32x4& x) {
+// Four neighbouring numbers of a row, as four hi and four lo.
+struct four_halves {
+    f16x4 hi, lo;
+};
+__device__ __forceinline__ four_halves split_four(const f32x4& x) {
     const halves a = split(x[0]), b = split(x[1]), c = split(x[2]), d = split(x[3]);
-    *reinterpret_cast<f16x4*>(m + tiny_at(row, pitch, col * 2 & ~15u) + (col * 2 & 15)) = f16x4{a.hi, b.hi, c.hi, d.hi};
-    *reinterpret_cast<f16x4*>(m + tiny_at(row, pitch, (pitch / 2 + col * 2) & ~15u) + (col * 2 & 15)) = f16x4{a.lo, b.lo, c.lo, d.lo};
+    return {f16x4{a.hi, b.hi, c.hi, d.hi}, f16x4{a.lo, b.lo, c.lo, d.lo}};
+}
+template <uint32_t PITCH>
+__device__ __forceinline__ void tiny_write(uint8_t* m, uint32_t row0, uint32_t at, uint32_t col0, const four_halves& x) {
+    const uint32_t to = row0 * PITCH + tiny_further(at, col0 * 2);
+    *reinterpret_cast<f16x4*>(m + to) = x.hi;
+    *reinterpret_cast<f16x4*>(m + (to ^ 128)) = x.lo;
 }
 
-// Numbers from, from + 512, ... of a gradient of `all`.
+// Numbers from, from + TINY_NT, ... of a gradient of `all`.
 template <int N>
 __device__ __forceinline__ void grads_of(const entry& e, uint32_t from, uint32_t all, float (&x)[N]) {
     if (e.grad_type == GD_F32) {
 #pragma unroll
-        for (int k = 0; k < N; ++k) x[k] = static_cast<const float*>(e.grad)[min(from + 512 * k, all - 1)];
+        for (int k = 0; k < N; ++k) x[k] = static_cast<const float*>(e.grad)[min(from + TINY_NT * k, all - 1)];
     } else {
         uint16_t q[N];
 #pragma unroll
-        for (int k = 0; k < N; ++k) q[k] = static_cast<const uint16_t*>(e.grad)[min(from + 512 * k, all - 1)];
+        for (int k = 0; k < N; ++k) q[k] = static_cast<const uint16_t*>(e.grad)[min(from + TINY_NT * k, all - 1)];
 #pragma unroll
         for (int k = 0; k < N; ++k) x[k] = e.grad_type == GD_BF16 ? gd_to_f32(__builtin_bit_cast(gd_bf16, q[k])) : gd_to_f32(__builtin_bit_cast(gd_f16, q[k]));
     }
@@ -644,13 +653,13 @@ template <typename T>
 __device__ __forceinline__ void tiny_update(const entry& e, const float* x, uint32_t all, float keep, float move) {
     constexpr int N = 8;
     T* p = static_cast<T*>(e.param);
-    for (uint32_t from = threadIdx.x; from < all; from += 512 * N) {
+    for (uint32_t from = threadIdx.x; from < all; from += TINY_NT * N) {
         T q[N];
 #pragma unroll
-        for (int k = 0; k < N; ++k) q[k] = p[min(from + 512 * k, all - 1)];
+        for (int k = 0; k < N; ++k) q[k] = p[min(from + TINY_NT * k, all - 1)];
 #pragma unroll
         for (int k = 0; k < N; ++k) {
-            const uint32_t i = from + 512 * k;
+            const uint32_t i = from + TINY_NT * k;
             if (i >= all) break;
             const float w = gd_to_f32(q[k]) * keep - x[i] * move;
             p[i] = gd_from_f32<T>(w);
@@ -665,9 +674,10 @@ struct tiny_steps {
     float c[GD_MUON_MAX_STEPS][4];                 // a, b, c, and the power of two that B is kept times
 };
 
-__global__ __launch_bounds__(512) void tiny_kernel(const muon_args g, const tiny_steps way) {
+__global__ __launch_bounds__(TINY_NT) void tiny_kernel(const muon_args g, const tiny_steps way) {
     __shared__ __attribute__((aligned(16))) tiny_lds lds;
-    constexpr int MINE = TINY_A / 16 * (TINY_B / 16) / 8, SQUARES = TINY_A / 16 * (TINY_A / 16) / 8;
+    constexpr uint32_t WAVES = TINY_NT / 64;
+    constexpr int MINE = TINY_A / 16 * (TINY_B / 16) / WAVES, SQUARES = TINY_A / 16 * (TINY_A / 16) / WAVES;
     float f;
     if (!factor_of(g, f)) return;
     const entry e = entry_at(g, g.first + blockIdx.x);
@@ -684,43 +694,51 @@ __global__ __launch_bounds__(512) void tiny_kernel(const muon_args g, const tiny
     constexpr int AT_ONCE = 8;
     const uint32_t all = a * b;
     double sum = 0;
-    for (uint32_t from = threadIdx.x; from < all; from += 512 * AT_ONCE) {
+    for (uint32_t from = threadIdx.x; from < all; from += TINY_NT * AT_ONCE) {
         float gr[AT_ONCE], m[AT_ONCE];
 #pragma unroll
-        for (int k = 0; k < AT_ONCE; ++k) m[k] = e.m[min(from + 512 * k, all - 1)];
+        for (int k = 0; k < AT_ONCE; ++k) m[k] = e.m[min(from + TINY_NT * k, all - 1)];
         grads_of<AT_ONCE>(e, from, all, gr);
 #pragma unroll
         for (int k = 0; k < AT_ONCE; ++k) {
             if (g.grad_scale) gr[k] *= f;
             m[k] = m[k] * g.mu + gr[k];
-            if (from + 512 * k >= all) break;
-            e.m[from + 512 * k] = m[k];
+            if (from + TINY_NT * k >= all) break;
+            e.m[from + TINY_NT * k] = m[k];
             const float u = update_of(g, gr[k], m[k]);
-            lds.u[from + 512 * k] = u;
+            lds.u[from + TINY_NT * k] = u;
             sum += (double)u * u;
         }
     }
     f32x4 x[MINE];
     const double size = sqrt(sum_of_all(sum)) + g.eps, scale = size == 0 ? 0 : ONE_X / size;
+    // Where a lane reads of an operand (row lane % 16, 16 bytes of 64) and writes of a result (row lane % 16, 8 bytes of 32; two
+    // bytes of 32 of each of four rows, transposed)
+    const uint32_t row = lane & 15, quarter = lane >> 4, chunk = quarter * 16 ^ tiny_turn(row);
+    const uint32_t r_read = row * tiny_lds::R + chunk, c_read = row * tiny_lds::C + chunk;
+    const uint32_t piece = (quarter / 2 * 16 ^ tiny_turn(row)) + quarter % 2 * 8;
+    const uint32_t r_write = row * tiny_lds::R + piece, s_write = row * tiny_lds::S + piece;
     auto keep_x = [&]() {
 #pragma unroll
         for (int k = 0; k < MINE; ++k) {
-            const uint32_t t = wave + 8 * k;
-            if (t >= ni * nj) continue;
-            const uint32_t i = i_of(t), j = j_of(t);
-            tiny_write(lds.r, tiny_lds::R, i, j, x[k]);
+            const uint32_t t = wave + WAVES * k;
+            if (t >= ni * nj) break;
+            const uint32_t i0 = t % ni * 16, j0 = t / ni * 16;
+            const four_halves h = split_four(x[k]);
+            tiny_write<tiny_lds::R>(lds.r, i0, r_write, j0, h);
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const halves h = split(x[k][r]);
-                *reinterpret_cast<gd_f16*>(lds.c + tiny_at(j + r, tiny_lds::C, i * 2 & ~15u) + (i * 2 & 15)) = h.hi;
-                *reinterpret_cast<gd_f16*>(lds.c + tiny_at(j + r, tiny_lds::C, (tiny_lds::C / 2 + i * 2) & ~15u) + (i * 2 & 15)) = h.lo;
+            for (uint32_t r = 0; r < 4; ++r) {
+                const uint32_t at = (4 * quarter + r) * tiny_lds::C + (row / 8 * 16 ^ tiny_turn(4 * quarter + r)) + row % 8 * 2;
+                const uint32_t to = j0 * tiny_lds::C + tiny_further(at, i0 * 2);
+                *reinterpret_cast<gd_f16*>(lds.c + to) = h.hi[r];
+                *reinterpret_cast<gd_f16*>(lds.c + (to ^ 128)) = h.lo[r];
             }
         }
         __syncthreads();
     };
 #pragma unroll
     for (int k = 0; k < MINE; ++k) {
-        const uint32_t t = wave + 8 * k, i = i_of(t), j = j_of(t);
+        const uint32_t t = wave + WAVES * k, i = i_of(t), j = j_of(t);
 #pragma unroll
         for (int r = 0; r < 4; ++r) x[k][r] = t < ni * nj && i < a && j + r < b ? (float)(lds.u[place(i, j + r)] * scale) : 0.0f;
     }
@@ -728,41 +746,34 @@ __global__ __launch_bounds__(512) void tiny_kernel(const muon_args g, const tiny
     if (way.steps) keep_x();
     for (uint32_t s = 0; s < way.steps; ++s) {
         const float ca = way.c[s][0], cb = way.c[s][1], cc = way.c[s][2], one_b = way.c[s][3];
-        // (a piece that is not there: the last one again, written by the wave that has it)
-        uint32_t to[SQUARES], from[SQUARES];
+        // (a wave's pieces have the same rows of Q: 8 is a multiple of ni; one that is not there has the last one's of P)
+        const uint32_t from = wave % ni * 16;
+        uint32_t to[SQUARES];
 #pragma unroll
-        for (int k = 0; k < SQUARES; ++k) {
-            const uint32_t t = min(wave + 8 * k, ni * ni - 1);
-            to[k] = t / ni * 16;
-            from[k] = t % ni * 16;
-        }
+        for (int k = 0; k < SQUARES; ++k) to[k] = min(wave + WAVES * k, ni * ni - 1) / ni * 16;
         f32x4 mine[SQUARES], square[SQUARES];
         // A, of which a piece's row is along Q
-        tiny_products(mine, lds.r, to, tiny_lds::R, lds.r, from, tiny_lds::R, nj * 32, both, lane);
+        tiny_products<tiny_lds::R, tiny_lds::R>(mine, lds.r, to, r_read, lds.r, from, r_read, nj * 32, both);
 #pragma unroll
         for (int k = 0; k < SQUARES; ++k) {
             mine[k] *= 1 / ONE_X;
-            if (wave + 8 * k < ni * ni) tiny_write(lds.a, tiny_lds::S, from[k] + (lane & 15), to[k] + 4 * (lane >> 4), mine[k]);
+            if (wave + WAVES * k < ni * ni) tiny_write<tiny_lds::S>(lds.a, from, s_write, to[k], split_four(mine[k]));
         }
         __syncthreads();
-        tiny_products(square, lds.a, to, tiny_lds::S, lds.a, from, tiny_lds::S, ni * 32, both, lane);
+        tiny_products<tiny_lds::S, tiny_lds::S>(square, lds.a, to, c_read, lds.a, from, c_read, ni * 32, both);
 #pragma unroll
         for (int k = 0; k < SQUARES; ++k)
-            if (wave + 8 * k < ni * ni)
-                tiny_write(lds.b, tiny_lds::S, from[k] + (lane & 15), to[k] + 4 * (lane >> 4), (square[k] * (cc / (ONE_X * ONE_X)) + mine[k] * (cb / ONE_X)) * one_b);
+            if (wave + WAVES * k < ni * ni)
+                tiny_write<tiny_lds::S>(lds.b, from, s_write, to[k], split_four((square[k] * (cc / (ONE_X * ONE_X)) + mine[k] * (cb / ONE_X)) * one_b));
         __syncthreads();
 #pragma unroll
         for (int first = 0; first < MINE; first += 3) {
-            if (wave + 8 * first >= ni * nj) break;
-            uint32_t j0[3], i0[3];
+            if (wave + WAVES * first >= ni * nj) break;
+            uint32_t j0[3];
 #pragma unroll
-            for (int k = 0; k < 3; ++k) {
-                const uint32_t t = min(wave + 8 * (first + k), ni * nj - 1);
-                j0[k] = t / ni * 16;
-                i0[k] = t % ni * 16;
-            }
+            for (int k = 0; k < 3; ++k) j0[k] = min(wave + WAVES * (first + k), ni * nj - 1) / ni * 16;
             f32x4 bx[3];
-            tiny_products(bx, lds.c, j0, tiny_lds::C, lds.b, i0, tiny_lds::S, ni * 32, both, lane);
+            tiny_products<tiny_lds::C, tiny_lds::S>(bx, lds.c, j0, c_read, lds.b, from, c_read, ni * 32, both);
 #pragma unroll
             for (int k = 0; k < 3; ++k) x[first + k] = x[first + k] * ca + bx[k] * (1 / one_b);
         }
@@ -774,7 +785,7 @@ __global__ __launch_bounds__(512) void tiny_kernel(const muon_args g, const tiny
     __syncthreads();                               // (A and B read by all)
 #pragma unroll
     for (int k = 0; k < MINE; ++k) {
-        const uint32_t t = wave + 8 * k, i = i_of(t), j = j_of(t);
+        const uint32_t t = wave + WAVES * k, i = i_of(t), j = j_of(t);
 #pragma unroll
         for (int r = 0; r < 4; ++r)
             if (t < ni * nj && i < a && j + r < b) lds.u[place(i, j + r)] = x[k][r];
@@ -902,7 +913,7 @@ size_t gd_muon_table(const gd_muon_tensor* t, uint32_t n, void* out) {
             full += tr * tc;
         }
         // (launches of fewer than 2^32 threads)
-        if (half >= 1u << 23 || full >= 1u << 23 || k >= 1u << 23) return 0;
+        if (half >= 1u << 23 || full >= 1u << 23 || k >= 1u << 22) return 0;
         if (kind == TINY) break;
         h.half[kind] = (uint32_t)half;
         h.full[kind] = (uint32_t)full;
@@ -974,7 +985,7 @@ hipError_t gd_launch_muon(const gd_muon_args& m, hipStream_t s) {
     }
     if (h.n > g.tiled) {
         g.first = g.tiled;
-        tiny_kernel<<<h.n - g.tiled, 512, 0, s>>>(g, way);
+        tiny_kernel<<<h.n - g.tiled, TINY_NT, 0, s>>>(g, way);
     }
     return hipGetLastError();
 }
