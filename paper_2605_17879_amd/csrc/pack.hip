@@ -10,45 +10,130 @@
 // The memory's streams bound it.  A workgroup takes 128 x 128: a lane 8 rows of 8 columns, which lie next to each other along
 // both, in registers from the one read to the codes; the row's largest comes from 16 lanes by exchange, the column's
 // through the LDS, as do the transposed codes, which are written 16 bytes a lane.
+#include <type_traits>
+
 #include "gd_operators.h"
 
 namespace {
 
 constexpr uint32_t EDGE = 128, NT = 256;
 
-template <bool E5M2> struct format {
-    static constexpr uint32_t TOP = E5M2 ? 15 : 8;               // MOST = 1.75 * 2^TOP
-    static __device__ __forceinline__ uint32_t four(float a, float b, float c, float d) {
-        int w = 0;
-        if constexpr (E5M2) {
-            w = __builtin_amdgcn_cvt_pk_bf8_f32(a, b, w, false);
-            w = __builtin_amdgcn_cvt_pk_bf8_f32(c, d, w, true);
-        } else {
-            w = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, w, false);
-            w = __builtin_amdgcn_cvt_pk_fp8_f32(c, d, w, true);
-        }
-        return (uint32_t)w;
-    }
-};
+typedef short s16x2 __attribute__((ext_vector_type(2)));
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+typedef gd_bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef gd_f16 f16x2 __attribute__((ext_vector_type(2)));
 constexpr uint32_t NONE = 255, NAN_CODES = 0x7F7F7F7Fu;          // a block that an infinity or a NaN came into
 
-// The exponent byte of a block whose largest magnitude has the bits `most`.
+// Two numbers over a power of two as codes, in half HIGH of a word.
+template <bool E5M2, bool HIGH>
+__device__ __forceinline__ s16x2 two_codes(s16x2 old, bf16x2 x, float two) {
+    if constexpr (E5M2) return __builtin_amdgcn_cvt_scalef32_pk_bf8_bf16(old, x, two, HIGH);
+    else return __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(old, x, two, HIGH);
+}
+template <bool E5M2, bool HIGH>
+__device__ __forceinline__ s16x2 two_codes(s16x2 old, f16x2 x, float two) {
+    if constexpr (E5M2) return __builtin_amdgcn_cvt_scalef32_pk_bf8_f16(old, x, two, HIGH);
+    else return __builtin_amdgcn_cvt_scalef32_pk_fp8_f16(old, x, two, HIGH);
+}
+template <bool E5M2, bool HIGH>
+__device__ __forceinline__ s16x2 two_codes(s16x2 old, float2 x, float two) {
+    if constexpr (E5M2) return __builtin_amdgcn_cvt_scalef32_pk_bf8_f32(old, x.x, x.y, two, HIGH);
+    else return __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(old, x.x, x.y, two, HIGH);
+}
+template <bool E5M2, typename P>
+__device__ __forceinline__ uint2 eight_codes(P a, P b, P c, P d, uint32_t e) {
+    if (e == NONE) return make_uint2(NAN_CODES, NAN_CODES);
+    const float two = __builtin_bit_cast(float, e == 0 ? 0x3F800000u : e << 23);      // (zeros over anything)
+    const s16x2 none = {};
+    const s16x2 lo = two_codes<E5M2, true>(two_codes<E5M2, false>(none, a, two), b, two);
+    const s16x2 hi = two_codes<E5M2, true>(two_codes<E5M2, false>(none, c, two), d, two);
+    return make_uint2(__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, hi));
+}
+
+// The exponent byte of a block whose largest magnitude has the bits `most`, of fp32.
 template <bool E5M2>
 __device__ __forceinline__ uint32_t exponent(uint32_t most) {
-    if (most == 0) return 0;
-    if (most >= 0x7F800000u) return NONE;
-    const int e = (int)(most >> 23) - (int)format<E5M2>::TOP + ((most & 0x7FFFFFu) > 0x600000u);
-    return e < 1 ? 1u : (uint32_t)e;
+    constexpr int TOP = E5M2 ? 15 : 8;                           // MOST = 1.75 * 2^TOP
+    const int e = (int)(most >> 23) - TOP + ((most & 0x7FFFFFu) > 0x600000u);
+    return most == 0 ? 0u : most >= 0x7F800000u ? NONE : (uint32_t)max(e, 1);
 }
-__device__ __forceinline__ float factor(uint32_t e) { return __builtin_bit_cast(float, (254 - min(e, 254u)) << 23); }
 
-__device__ __forceinline__ uint32_t magnitude(float x) { return __builtin_bit_cast(uint32_t, x) & 0x7FFFFFFFu; }
-
-template <bool E5M2>
-__device__ __forceinline__ uint2 eight(const float (&x)[8], float f, uint32_t e) {
-    if (e == NONE) return make_uint2(NAN_CODES, NAN_CODES);
-    return make_uint2(format<E5M2>::four(x[0] * f, x[1] * f, x[2] * f, x[3] * f), format<E5M2>::four(x[4] * f, x[5] * f, x[6] * f, x[7] * f));
+// The largest of sixteen neighbouring lanes.
+template <int CTRL>
+__device__ __forceinline__ uint32_t larger_of(uint32_t x) {
+    return max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, 0xF, 0xF, true));
 }
+__device__ __forceinline__ uint32_t most_of_sixteen(uint32_t x) {
+    return larger_of<0x121>(larger_of<0x122>(larger_of<0x124>(larger_of<0x128>(x))));     // (rotations by 8, 4, 2 and 1)
+}
+
+// Eight neighbouring numbers as they lie in memory, two a pair; magnitudes as numbers that are ordered like them.
+template <typename T> struct eight {
+    typedef std::conditional_t<std::is_same<T, gd_bf16>::value, bf16x2, f16x2> pair;
+    uint32_t w[4];
+    __device__ __forceinline__ void load(const T* p) {
+        const gd_u32x4 q = *reinterpret_cast<const gd_u32x4_anywhere*>(p);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = q[i];
+    }
+    __device__ __forceinline__ void load_some(const T* p, uint32_t there) {
+#pragma unroll
+        for (uint32_t i = 0; i < 8; ++i)
+            if (i < there) w[i / 2] |= (uint32_t)__builtin_bit_cast(uint16_t, p[i]) << (16 * (i % 2));
+    }
+    __device__ __forceinline__ pair at(int i) const { return __builtin_bit_cast(pair, w[i]); }
+    // number c of this and of the next row
+    static __device__ __forceinline__ pair below(const eight& a, const eight& b, int c) {
+        return __builtin_bit_cast(pair, c % 2 ? __builtin_amdgcn_perm(b.w[c / 2], a.w[c / 2], 0x07060302) : __builtin_amdgcn_perm(b.w[c / 2], a.w[c / 2], 0x05040100));
+    }
+    struct sizes {
+        u16x2 w[4];
+        __device__ __forceinline__ void take(const eight& x) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) w[i] = __builtin_elementwise_max(w[i], __builtin_bit_cast(u16x2, x.w[i] & 0x7FFF7FFFu));
+        }
+        // of number c, of all, as the bits of fp32
+        __device__ __forceinline__ uint32_t of(int c) const { return bits(w[c / 2][c % 2]); }
+        __device__ __forceinline__ uint32_t most() const {
+            const u16x2 m = __builtin_elementwise_max(__builtin_elementwise_max(w[0], w[1]), __builtin_elementwise_max(w[2], w[3]));
+            return bits(max(m[0], m[1]));
+        }
+        static __device__ __forceinline__ uint32_t bits(uint16_t m) { return __builtin_bit_cast(uint32_t, gd_to_f32(__builtin_bit_cast(T, m))); }
+    };
+};
+template <> struct eight<float> {
+    typedef float2 pair;
+    float x[8];
+    __device__ __forceinline__ void load(const float* p) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const gd_vec<float, 4> q = gd_read<float, 4>(p + 4 * h);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x[4 * h + i] = q.v[i];
+        }
+    }
+    __device__ __forceinline__ void load_some(const float* p, uint32_t there) {
+#pragma unroll
+        for (uint32_t i = 0; i < 8; ++i)
+            if (i < there) x[i] = p[i];
+    }
+    __device__ __forceinline__ pair at(int i) const { return make_float2(x[2 * i], x[2 * i + 1]); }
+    static __device__ __forceinline__ pair below(const eight& a, const eight& b, int c) { return make_float2(a.x[c], b.x[c]); }
+    struct sizes {
+        uint32_t w[8];
+        __device__ __forceinline__ void take(const eight& x) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) w[i] = max(w[i], __builtin_bit_cast(uint32_t, x.x[i]) & 0x7FFFFFFFu);
+        }
+        __device__ __forceinline__ uint32_t of(int c) const { return w[c]; }
+        __device__ __forceinline__ uint32_t most() const {
+            uint32_t m = 0;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) m = max(m, w[i]);
+            return m;
+        }
+    };
+};
 
 // The bytes from `at` on of a row that has `there` more.
 template <int N>
@@ -59,71 +144,48 @@ __device__ __forceinline__ void write_some(const uint32_t (&w)[N], uint8_t* at, 
 }
 
 template <typename T, bool E5M2>
-__global__ __launch_bounds__(NT) void pack_kernel(const gd_pack_args a) {
+__global__ __launch_bounds__(NT, 4) void pack_kernel(const gd_pack_args a) {
     __shared__ uint32_t most_of[EDGE][5];                        // a column's largest, by wave
     __shared__ uint32_t exp_of[EDGE];
     __shared__ __attribute__((aligned(16))) uint2 turned[EDGE][EDGE / 8 + 2];   // codes, transposed
     const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x / 64, tx = threadIdx.x % 16, ty = threadIdx.x / 16;
     const uint32_t tiles_c = (a.cols + EDGE - 1) / EDGE, tile_r = blockIdx.x / tiles_c, tile_c = blockIdx.x % tiles_c;
     const uint32_t row0 = tile_r * EDGE + ty * 8, col0 = tile_c * EDGE + tx * 8;
-    const T* x = static_cast<const T*>(a.x) + col0;
-    float v[8][8];
+    const T* x = static_cast<const T*>(a.x) + row0 * a.stride + col0;
     const bool whole = col0 + 8 <= a.cols;
-    constexpr int V = 16 / sizeof(T);
-    gd_vec<T, V> raw[8][8 / V];
+    eight<T> v[8] = {};
 #pragma unroll
     for (int j = 0; j < 8; ++j)
-#pragma unroll
-        for (int h = 0; h < 8 / V; ++h) {
-            raw[j][h] = gd_vec<T, V>{};
-            if (row0 + j < a.rows) {
-                const T* p = x + (row0 + j) * a.stride + h * V;
-                if (whole) {
-                    raw[j][h] = gd_read<T, V>(p);
-                } else {
-#pragma unroll
-                    for (int e = 0; e < V; ++e)
-                        if (col0 + h * V + e < a.cols) raw[j][h].v[e] = p[e];
-                }
-            }
+        if (row0 + j < a.rows) {
+            if (whole) v[j].load(x + j * a.stride);
+            else if (col0 < a.cols) v[j].load_some(x + j * a.stride, a.cols - col0);
         }
-#pragma unroll
-    for (int j = 0; j < 8; ++j)
-#pragma unroll
-        for (int c = 0; c < 8; ++c) v[j][c] = gd_to_f32(raw[j][c / V].v[c % V]);
-
-    uint32_t row_most[8], col_most[8] = {};
+    uint32_t row_most[8];
+    typename eight<T>::sizes columns = {};
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-        row_most[j] = 0;
-#pragma unroll
-        for (int c = 0; c < 8; ++c) {
-            const uint32_t b = magnitude(v[j][c]);
-            row_most[j] = max(row_most[j], b);
-            col_most[c] = max(col_most[c], b);
-        }
+        typename eight<T>::sizes row = {};
+        row.take(v[j]);
+        row_most[j] = row.most();
+        columns.take(v[j]);
     }
+    uint32_t square_most = 0;
     if (a.square) {
         uint32_t m = 0;
 #pragma unroll
         for (int j = 0; j < 8; ++j) m = max(m, row_most[j]);
-#pragma unroll
-        for (int d = 1; d < 64; d *= 2) m = max(m, (uint32_t)__shfl_xor((int)m, d));
+        m = most_of_sixteen(m);
+        m = max(m, (uint32_t)__shfl_xor((int)m, 16));
+        m = max(m, (uint32_t)__shfl_xor((int)m, 32));
         if (lane == 0) most_of[0][wave] = m;
         __syncthreads();
-        m = max(max(most_of[0][0], most_of[0][1]), max(most_of[0][2], most_of[0][3]));
-#pragma unroll
-        for (int j = 0; j < 8; ++j) row_most[j] = col_most[j] = m;
+        square_most = max(max(most_of[0][0], most_of[0][1]), max(most_of[0][2], most_of[0][3]));
     }
     if (a.along.codes) {
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            if (!a.square) {
-#pragma unroll
-                for (int d = 1; d < 16; d *= 2) row_most[j] = max(row_most[j], (uint32_t)__shfl_xor((int)row_most[j], d));
-            }
-            const uint32_t e = exponent<E5M2>(row_most[j]), row = row0 + j;
-            const uint2 w = eight<E5M2>(v[j], factor(e), e);
+            const uint32_t e = exponent<E5M2>(a.square ? square_most : most_of_sixteen(row_most[j])), row = row0 + j;
+            const uint2 w = eight_codes<E5M2>(v[j].at(0), v[j].at(1), v[j].at(2), v[j].at(3), e);
             if (row < a.rows) {
                 uint8_t* to = a.along.codes + row * a.along.stride + col0;
                 if (whole) *reinterpret_cast<uint2*>(to) = w;
@@ -136,28 +198,28 @@ __global__ __launch_bounds__(NT) void pack_kernel(const gd_pack_args a) {
     if (!a.square) {
 #pragma unroll
         for (int c = 0; c < 8; ++c) {
-            uint32_t m = col_most[c];
+            uint32_t m = columns.of(c);
             m = max(m, (uint32_t)__shfl_xor((int)m, 16));
             m = max(m, (uint32_t)__shfl_xor((int)m, 32));
             if (lane < 16) most_of[tx * 8 + c][wave] = m;
         }
         __syncthreads();
-#pragma unroll
-        for (int c = 0; c < 8; ++c) {
-            const uint32_t* m = most_of[tx * 8 + c];
-            col_most[c] = max(max(m[0], m[1]), max(m[2], m[3]));
+        // (each column's exponent once, by one lane)
+        if (threadIdx.x < EDGE) {
+            const uint32_t* m = most_of[threadIdx.x];
+            exp_of[threadIdx.x] = exponent<E5M2>(max(max(m[0], m[1]), max(m[2], m[3])));
         }
+        __syncthreads();
     }
 #pragma unroll
     for (int c = 0; c < 8; ++c) {
-        const uint32_t e = exponent<E5M2>(col_most[c]);
-        const float column[8] = {v[0][c], v[1][c], v[2][c], v[3][c], v[4][c], v[5][c], v[6][c], v[7][c]};
-        turned[tx * 8 + c][ty] = eight<E5M2>(column, factor(e), e);
-        if (ty == 0) exp_of[tx * 8 + c] = e;
+        const uint32_t e = a.square ? exponent<E5M2>(square_most) : exp_of[tx * 8 + c];
+        turned[tx * 8 + c][ty] = eight_codes<E5M2>(eight<T>::below(v[0], v[1], c), eight<T>::below(v[2], v[3], c), eight<T>::below(v[4], v[5], c),
+                                                   eight<T>::below(v[6], v[7], c), e);
     }
     __syncthreads();
     if (threadIdx.x < EDGE && tile_c * EDGE + threadIdx.x < a.cols)
-        a.across.exp[tile_r * a.across.exp_stride + tile_c * EDGE + threadIdx.x] = (uint8_t)exp_of[threadIdx.x];
+        a.across.exp[tile_r * a.across.exp_stride + tile_c * EDGE + threadIdx.x] = (uint8_t)(a.square ? exponent<E5M2>(square_most) : exp_of[threadIdx.x]);
     const uint32_t from = tile_r * EDGE + (threadIdx.x % 8) * 16;
     for (uint32_t c = threadIdx.x / 8; c < EDGE && tile_c * EDGE + c < a.cols; c += NT / 8) {
         if (from >= a.rows) break;
