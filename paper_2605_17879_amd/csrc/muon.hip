@@ -32,6 +32,7 @@ namespace {
 using namespace gd_tiles;
 
 constexpr float ONE_X = 0x1p15f;                   // X and A are kept times 2^15: below 65 504 for values below 1.99
+constexpr uint32_t CUS = 256;
 constexpr uint32_t CHUNKS = 1024;                  // most pieces of a matrix that its sum of squares is taken in
 constexpr uint32_t CHUNK = 4096;                   // elements of a piece: a multiple of it
 enum { LARGE, SMALL, DIRECT, KINDS, TINY = KINDS };   // tiles of the products; TINY: a matrix in one workgroup, in one launch
@@ -96,6 +97,7 @@ struct muon_args {
     const uint8_t* table;
     uint32_t n, tiled;            // entries, those that are not tiny
     uint32_t first, count;        // entries of the launch's kind
+    uint32_t quarters;            // of tiles of 256 x 256: the launch takes quarters of these, from this one on, plus 1; 0: no quarters
     uint8_t* work;
     const float* grad_scale;
     uint32_t both;                // products of f32
@@ -348,30 +350,38 @@ __device__ __forceinline__ problem problem_of(const muon_args& g, const entry& e
     return x;
 }
 
-// Sixteen columns, from `col` on, of a row: v[i][r] is column 4 r + i.  Returned: what the row becomes, as it is kept.
-template <int PHASE>
-__device__ __forceinline__ void finish_row(const muon_args& g, const entry& e, const target& o, uint32_t row, uint32_t col, f32x4 (&v)[4]) {
-    if (PHASE == OF_X) {
+// What was at sixteen columns of a row, from `col` on.
+struct old_row {
+    gd_u32x4 hi[2], lo[2];
+};
+__device__ __forceinline__ void read_old(const target& o, uint32_t row, uint32_t col, old_row& old) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) v[i][r] = row < o.rows && col + 4 * r + i < o.cols ? v[i][r] * (1 / ONE_X) : 0.0f;
-        return;
-    }
-    gd_vec<gd_f16, 8> hi[2] = {}, lo[2] = {};
+    for (int h = 0; h < 2; ++h) old.hi[h] = old.lo[h] = gd_u32x4{};
     if (row < o.rows && col < o.d_lo / 2) {
-        const gd_f16* from = reinterpret_cast<const gd_f16*>(o.old + row * o.d_pitch) + col;
+        const gd_u32x4* from = reinterpret_cast<const gd_u32x4*>(o.old + row * o.d_pitch + col * 2);
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            hi[h] = gd_read<gd_f16, 8>(from + 8 * h);
-            if (o.old_lo) lo[h] = gd_read<gd_f16, 8>(from + o.d_lo / 2 + 8 * h);
+            old.hi[h] = from[h];
+            if (o.old_lo) old.lo[h] = from[o.d_lo / 16 + h];
         }
+    }
+}
+
+// Sixteen columns, from `col` on, of a row: v[i][r] is column 4 r + i, and becomes what the row does.
+template <int PHASE>
+__device__ __forceinline__ void finish_row(const muon_args& g, const target& o, uint32_t row, uint32_t col, f32x4 (&v)[4], const old_row& was) {
+    gd_vec<gd_f16, 8> hi[2], lo[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        hi[h] = __builtin_bit_cast(gd_vec<gd_f16, 8>, was.hi[h]);
+        lo[h] = __builtin_bit_cast(gd_vec<gd_f16, 8>, was.lo[h]);
     }
 #pragma unroll
     for (int x = 0; x < 16; ++x) {
-        const float old = whole(hi[x / 8].v[x % 8], lo[x / 8].v[x % 8]);
         float w = v[x % 4][x / 4];
-        if (PHASE == OF_A) w = (g.c * (w * (1 / (ONE_X * ONE_X))) + g.b * (old * (1 / ONE_X))) * g.one_b;
+        const float old = whole(hi[x / 8].v[x % 8], lo[x / 8].v[x % 8]);
+        if (PHASE == OF_X) w *= 1 / ONE_X;
+        else if (PHASE == OF_A) w = (g.c * (w * (1 / (ONE_X * ONE_X))) + g.b * (old * (1 / ONE_X))) * g.one_b;
         else w = g.a * old + w * (1 / g.one_b);
         v[x % 4][x / 4] = row < o.rows && col + x < o.cols ? w : 0.0f;   // (zeros up to the end of a block)
     }
@@ -476,14 +486,24 @@ __device__ __forceinline__ void corner_of(uint32_t t, uint32_t& tp, uint32_t& tq
     tp = t - q * (q + 1) / 2;
 }
 
+// The workgroup's tile; false if there is none.
 template <int PHASE>
-__device__ __forceinline__ entry place_of(const muon_args& g, uint32_t edge, uint32_t& tp, uint32_t& tq) {
+__device__ __forceinline__ bool place_of(const muon_args& g, uint32_t edge, uint32_t& tp, uint32_t& tq, entry& e) {
     constexpr bool HALF = PHASE == OF_X || PHASE == OF_A;
     uint32_t t = stretch_of(blockIdx.x, gridDim.x);
-    const entry e = entry_at(g, find(g, HALF ? OF_HALF : OF_FULL, g.first, g.count, t));
+    const uint32_t quarter = t % 4;
+    if (g.quarters) {
+        t = g.quarters - 1 + t / 4;
+        edge = 256;
+    }
+    e = entry_at(g, find(g, HALF ? OF_HALF : OF_FULL, g.first, g.count, t));
     if (HALF) corner_of(t, tq, tp);                // (columns at or behind the rows)
     else tile_of<4>(t, (e.cols + edge - 1) / edge, (e.rows + edge - 1) / edge, tp, tq);
-    return e;
+    if (!g.quarters) return true;
+    tp = 2 * tp + quarter % 2;
+    tq = 2 * tq + quarter / 2;
+    const uint32_t a = min(e.rows, e.cols);
+    return (HALF ? tp >= tq : true) && tq * 128 < (HALF ? a : e.rows) && tp * 128 < (HALF ? a : e.cols);
 }
 
 template <int PHASE, template <typename> class TILE>
@@ -492,7 +512,8 @@ __global__ __launch_bounds__(TILE<of_f16>::NT, 512 / TILE<of_f16>::NT) void tile
     float f;
     if (!factor_of(g, f)) return;
     uint32_t tp, tq;
-    const entry e = place_of<PHASE>(g, tile::BP, tp, tq);
+    entry e;
+    if (!place_of<PHASE>(g, tile::BP, tp, tq, e)) return;
     const problem x = problem_of<PHASE>(g, e, tp != tq);
     f32x4 acc[tile::FP][tile::FQ] = {};
     tile::run(x.p, x.q, tp * tile::BP, tq * tile::BQ, x.way, acc);
@@ -502,11 +523,17 @@ __global__ __launch_bounds__(TILE<of_f16>::NT, 512 / TILE<of_f16>::NT) void tile
     for (int h = 0; h < tile::FP / 4; ++h) {
         const uint32_t col = tp * tile::BP + tile::p_of(wave, h) + 16 * (lane >> 4);
         f32x4 v[4][4];
+        // (four rows are asked for before one is waited for)
+        old_row old[4] = {};
+        if (PHASE != OF_X) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) read_old(x.out, row + j, col, old[j]);
+        }
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) v[j][i] = acc[4 * h + i][j];
-            finish_row<PHASE>(g, e, x.out, row + j, col, v[j]);
+            finish_row<PHASE>(g, x.out, row + j, col, v[j], old[j]);
             if (PHASE == LAST) update_row(g, e, row + j, col, v[j]);
             else write_row(x.out, row + j, col, v[j], lane);
         }
@@ -524,14 +551,17 @@ __global__ __launch_bounds__(512) void direct_kernel(const muon_args g) {
     float f;
     if (!factor_of(g, f)) return;
     uint32_t tp, tq;
-    const entry e = place_of<PHASE>(g, 64, tp, tq);
+    entry e;
+    place_of<PHASE>(g, 64, tp, tq, e);
     const problem x = problem_of<PHASE>(g, e, tp != tq);
     f32x4 v[4];
-    tile::sums* room = tile::run(x.p, x.q, tp * 64, tq * 64, x.way, 0, x.way.blocks * x.way.parts, v);
     const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const uint32_t row = tq * 64 + 4 * (lane & 15), col = tp * 64 + 16 * (lane >> 4);
+    old_row old = {};
+    if (PHASE != OF_X && wave < 4) read_old(x.out, row + wave, col, old);   // (on its way beside the sum)
+    tile::sums* room = tile::run(x.p, x.q, tp * 64, tq * 64, x.way, 0, x.way.blocks * x.way.parts, v);
     if (wave < 4) {
-        finish_row<PHASE>(g, e, x.out, row + wave, col, v);
+        finish_row<PHASE>(g, x.out, row + wave, col, v, old);
         if (PHASE == LAST) update_row(g, e, row + wave, col, v);
         else write_row(x.out, row + wave, col, v, lane);
     }
@@ -805,7 +835,17 @@ void launch_phase(muon_args g, const head& h, hipStream_t s) {
         if (!tiles[k]) continue;
         g.first = h.first[k];
         g.count = h.first[k + 1] - h.first[k];
-        if (k == LARGE) tiled_kernel<PHASE, large_tile><<<tiles[k], 512, 0, s>>>(g);
+        if (k == LARGE) {
+            // Whole rounds of the chip's 256 workgroups; what is left, if it is little, as quarters, which are less than a round of
+            // tiles of 128 x 128 (4 of 4 096 x 4 096, X X^T 544 tiles: 315 us as three rounds, 262 as two and 128 quarters).
+            const uint32_t left = tiles[k] > CUS && tiles[k] % CUS <= 3 * CUS / 8 ? tiles[k] % CUS : 0;
+            tiled_kernel<PHASE, large_tile><<<tiles[k] - left, 512, 0, s>>>(g);
+            if (left) {
+                muon_args q = g;
+                q.quarters = tiles[k] - left + 1;
+                tiled_kernel<PHASE, small_tile><<<4 * left, 256, 0, s>>>(q);
+            }
+        }
         else if (k == SMALL) tiled_kernel<PHASE, small_tile><<<tiles[k], 256, 0, s>>>(g);
         else direct_kernel<PHASE><<<tiles[k], 512, 0, s>>>(g);
     }
