@@ -570,15 +570,15 @@ struct small_tile {
     }
 };
 
-// 64 x 16 FQ by eight waves that share k, for products of few tiles, and of few rows of Q, where every byte of P is read once.
+// 64 x 16 FQ by eight waves (or four, two workgroups a CU) that share k, for products of few tiles, and of few rows of Q, where every byte of P is read once.
 // Each wave stages blocks of its own in a part of the LDS that no other wave touches, so that it waits for nothing but its
 // own loads: the next block is on its way while this one, read into registers, is multiplied.  What the waves have
 // summed is joined in the LDS, in their order.  (Fragments read from memory straight into registers took half as long again:
 // neighbouring lanes hold rows apart, and the loads' addresses are taken four lanes at a time.)  Fragments of Q hold
 // rows FQ c + j.
-template <typename MUL, int FQ_>
+template <typename MUL, int FQ_, int WAVES_>
 struct direct_tile {
-    static constexpr int FP = 4, FQ = FQ_, BP = 64, BQ = 16 * FQ, WAVES = 8, NT = 64 * WAVES;
+    static constexpr int FP = 4, FQ = FQ_, BP = 64, BQ = 16 * FQ, WAVES = WAVES_, NT = 64 * WAVES;
     static constexpr int PART = (BP + BQ) * BYTES, EXPS = 128;
     typedef f32x4 sums[FQ][FP][64];
     static_assert(sizeof(sums) <= PART, "the sums take the place of the blocks");

@@ -545,9 +545,9 @@ __global__ __launch_bounds__(TILE<of_f16>::NT, 512 / TILE<of_f16>::NT) void tile
     }
 }
 
-template <int PHASE>
-__global__ __launch_bounds__(512) void direct_kernel(const muon_args g) {
-    typedef direct_tile<of_f16, 4> tile;
+template <int PHASE, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, 8 / WAVES) void direct_kernel(const muon_args g) {
+    typedef direct_tile<of_f16, 4, WAVES> tile;
     float f;
     if (!factor_of(g, f)) return;
     uint32_t tp, tq;
@@ -559,7 +559,7 @@ __global__ __launch_bounds__(512) void direct_kernel(const muon_args g) {
     const uint32_t row = tq * 64 + 4 * (lane & 15), col = tp * 64 + 16 * (lane >> 4);
     old_row old = {};
     if (PHASE != OF_X && wave < 4) read_old(x.out, row + wave, col, old);   // (on its way beside the sum)
-    tile::sums* room = tile::run(x.p, x.q, tp * 64, tq * 64, x.way, 0, x.way.blocks * x.way.parts, v);
+    typename tile::sums* room = tile::run(x.p, x.q, tp * 64, tq * 64, x.way, 0, x.way.blocks * x.way.parts, v);
     if (wave < 4) {
         finish_row<PHASE>(g, x.out, row + wave, col, v, old);
         if (PHASE == LAST) update_row(g, e, row + wave, col, v);
@@ -847,16 +847,18 @@ void launch_phase(muon_args g, const head& h, hipStream_t s) {
             }
         }
         else if (k == SMALL) tiled_kernel<PHASE, small_tile><<<tiles[k], 256, 0, s>>>(g);
-        else direct_kernel<PHASE><<<tiles[k], 512, 0, s>>>(g);
+        else if (tiles[k] <= CUS) direct_kernel<PHASE, 8><<<tiles[k], 512, 0, s>>>(g);
+        else direct_kernel<PHASE, 4><<<tiles[k], 256, 0, s>>>(g);
     }
 }
 
 uint64_t tiles_of(const gd_muon_tensor& t, uint64_t edge) { return ((t.rows + edge - 1) / edge) * ((t.cols + edge - 1) / edge); }
 
-// Which tiles the matrices take.  Tiles of 256 x 256 where they fill the chip (24 of 1 024 x 1 024, 384 of them: 2.16 ms, with tiles of
-// 128 x 128 2.29; 4 of 2 048 x 2 048, 256: 2.29 and 2.68; 8 of 1 024 x 1 024, 128: 1.22 and 0.87) and are not mostly empty; else
-// tiles of 128 x 128 where those of 64 x 64 would be more than two rounds of the chip's workgroups (16 of 512 x 512, 1 024: 0.41
-// and 0.81; 8 of 333 x 500, 384: 0.32 and 0.31; 8 of 128 x 128, 32: 0.18 and 0.14).
+// Which tiles the matrices take.  Tiles of 256 x 256 where they fill the chip (24 of 1 024 x 1 024, 384: 2.20 ms, with
+// tiles of 128 x 128 2.36; 4 of 2 048 x 2 048, 256: 2.46 and 2.84; 8 of 1 024 x 1 024, 128: 1.17 and 0.89) and are not mostly empty; else
+// tiles of 128 x 128 where those of 64 x 64 would be two rounds of the chip and more (64 of 256 x 256, 1 024: 0.32 and 0.35; 8 of 1 024 x
+// 1 024, 2 048: 0.89 and 1.06; 8 of 333 x 500, 384: 0.32 and 0.19) of matrices that are not long, whose products over the long side are few
+// tiles of many blocks (4 of 512 x 2 048, 1 024: 0.57 and 0.35; 2 of 1 024 x 4 096, 2 048: 1.15 and 0.98).
 void choose_kinds(const gd_muon_tensor* t, uint32_t n, std::vector<int>& kinds) {
     kinds.assign(n, DIRECT);
     auto side = [&](uint32_t i) { return std::min(t[i].rows, t[i].cols); };
@@ -870,7 +872,7 @@ void choose_kinds(const gd_muon_tensor* t, uint32_t n, std::vector<int>& kinds) 
         if (large >= 240 && fills(i)) kinds[i] = LARGE;
         else if (side(i) > 64) direct += tiles_of(t[i], 64);
     for (uint32_t i = 0; i < n; ++i)
-        if (kinds[i] == DIRECT && side(i) > 64 && direct > 512) kinds[i] = SMALL;
+        if (kinds[i] == DIRECT && side(i) > 64 && direct >= 1024 && std::max(t[i].rows, t[i].cols) < 3 * side(i)) kinds[i] = SMALL;
 }
 
 // The largest magnitude of a polynomial c1 x + c3 x^3 + c5 x^5, and of b x^2 + c x^4, over [0, s].

@@ -78,9 +78,9 @@ __global__ __launch_bounds__(TILE<MUL>::NT, 512 / TILE<MUL>::NT) void tiled_kern
         }
 }
 
-template <typename MUL, typename T, int FQ>
-__global__ __launch_bounds__(512) void direct_kernel(const product_args a) {
-    typedef direct_tile<MUL, FQ> tile;
+template <typename MUL, typename T, int FQ, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, 8 / WAVES) void direct_kernel(const product_args a) {
+    typedef direct_tile<MUL, FQ, WAVES> tile;
     const uint32_t b = blockIdx.x, tq = b % a.tiles_q, tp = b / a.tiles_q, split = blockIdx.y;
     const uint32_t first = split * a.each, blocks = a.way.blocks;
     f32x4 v[4];
@@ -162,16 +162,18 @@ struct plan {
 
 uint32_t up(uint64_t a, uint64_t b) { return (uint32_t)((a + b - 1) / b); }
 
-// Tiles of 64 x 64 and smaller up to one round of the chip's workgroups (1 000 x 1 001 x 1 000, 256 of them: 8.5 us, tiles of 128 x 128 11.2,
-// of 256 x 256 22.5; 1 500 x 1 000 x 2 000, 384: 18.5, 15.3, 30.2), three where the others need their operands written out in bf16 first
-// (2 000 x 1 500 x 1 000, 768: 21.4, 26.3, 38.8; 2 048 x 2 048 x 2 048, 1 024: 48, 40, 58); tiles of 256 x 256 from where they fill more
-// than half of the chip (3 000 x 3 000 x 3 000, 144 of them: 44 us, 50 with 128 x 128; 2 048 x 4 096 x 4 096, 128: 51 and 36).
+// For 16 bits tiles of 64 x 64 and smaller up to 768 of them (2 000 x 1 500 x 1 000, 768: 12.1 us, tiles of 128 x 128 12.7, of 256 x 256 22.2;
+// 2 048 x 2 048 x 2 048, 1 024: 20.3, 16.0, 27.7), then of 256 x 256 from where they fill more than half of the chip (3 000 x 3 000 x 3 000, 144 of
+// them: 44 us, 50 with 128 x 128; 2 048 x 4 096 x 4 096, 128: 52 and 40).  For fp32, where larger tiles need their operands written out in
+// bf16 first, of 64 x 64 up to there (1 024 x 4 096 x 4 096, 1 024: 42 us, 65, 98; 2 500 x 2 500 x 1 000, 1 600: 27, 34, 42; 3 000 x 3 000 x 3 000: 84,
+// 90, 80).
 plan plan_of(uint64_t n, uint64_t m, uint64_t k, bool f32) {
     const uint64_t blocks = up(k, BYTES);
     plan w{plan::DIRECT, n <= 16 ? 1u : n <= 32 ? 2u : 4u, 1, (uint32_t)blocks};
     const uint64_t tiles = (uint64_t)up(n, 16 * w.fq) * up(m, 64);
-    if (n > 64 && tiles > (f32 ? 768 : 256)) {
-        w.kind = (uint64_t)up(n, 256) * up(m, 256) >= 140 ? plan::LARGE : plan::SMALL;
+    const bool large = (uint64_t)up(n, 256) * up(m, 256) >= 140;
+    if (n > 64 && tiles > 768 && (large || !f32)) {
+        w.kind = large ? plan::LARGE : plan::SMALL;
         return w;
     }
     // workgroups for every CU, as long as a wave keeps two blocks
@@ -195,8 +197,13 @@ hipError_t launch_tiles(product_args& a, const plan& w, hipStream_t s) {
     a.tiles_p = up(a.m, edge);
     a.tiles_q = up(a.n, edge);
     const uint32_t tiles = a.tiles_p * a.tiles_q;
-    if (w.kind == plan::LARGE) tiled_kernel<MUL, T, large_tile><<<tiles, 512, 0, s>>>(a);
-    else tiled_kernel<MUL, T, small_tile><<<tiles, 256, 0, s>>>(a);
+    if constexpr (MUL::SCALED) {                     // (fp32 has no tiles of 128 x 128)
+        if (w.kind == plan::SMALL) {
+            tiled_kernel<MUL, T, small_tile><<<tiles, 256, 0, s>>>(a);
+            return hipGetLastError();
+        }
+    }
+    tiled_kernel<MUL, T, large_tile><<<tiles, 512, 0, s>>>(a);
     return hipGetLastError();
 }
 
@@ -207,9 +214,10 @@ hipError_t launch_direct(product_args& a, const plan& w, hipStream_t s) {
     a.each = w.each;
     if (w.splits == 1) a.slab = nullptr;
     const dim3 grid(a.tiles_p * a.tiles_q, w.splits);
-    if (w.fq == 1) direct_kernel<MUL, T, 1><<<grid, 512, 0, s>>>(a);
-    else if (w.fq == 2) direct_kernel<MUL, T, 2><<<grid, 512, 0, s>>>(a);
-    else direct_kernel<MUL, T, 4><<<grid, 512, 0, s>>>(a);
+    if (w.fq == 1) direct_kernel<MUL, T, 1, 8><<<grid, 512, 0, s>>>(a);
+    else if (w.fq == 2) direct_kernel<MUL, T, 2, 8><<<grid, 512, 0, s>>>(a);
+    else if (a.tiles_p * a.tiles_q <= 256) direct_kernel<MUL, T, 4, 8><<<grid, 512, 0, s>>>(a);
+    else direct_kernel<MUL, T, 4, 4><<<grid, 256, 0, s>>>(a);
     if (hipError_t e = hipGetLastError()) return e;
     if (w.splits > 1) join_kernel<T><<<up((uint64_t)a.n * (a.m4 / 4), 256), 256, 0, s>>>(a, w.splits);
     return hipGetLastError();
