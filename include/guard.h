@@ -543,9 +543,11 @@ gd_status gd_adamw(gd_handle h, const void* d_table, size_t table_bytes, const g
  * Packed matrices: 8-bit floating point with a power of two for each block of 128 elements of a row.
  *   codes [rows][cols]               GD_E4M3 or GD_E5M2, one byte each; 16-byte aligned, the stride a multiple of 16 (rather not
  *                                    of 256: such rows meet at the same channels of the memory)
- *   exp   [ceil(cols / 128)][rows]   GD_U8; 4-byte aligned, the stride a multiple of 4
+ *   exp   [ceil(cols / 128)][rows]   GD_U8; 4-byte aligned, the stride a multiple of 4, up to 2^24
  * Element (i, k) stands for codes[i][k] * 2^(exp[k / 128][i] - 127); a byte of 255 stands for a block of NaN.  In front
- * of the last row what lies between its end and the next one's begin is neither read as a number nor written.
+ * of the last row what lies between its end and the next one's begin is neither read as a number nor written.  What a call
+ * writes (outputs, its work area) overlaps nothing else that it is given; calls that may run at the same time (on two streams,
+ * in two graphs) have work areas of their own.
  */
 typedef struct gd_packed {
     gd_matrix codes, exp;
@@ -620,7 +622,7 @@ typedef struct gd_muon_config {
 
 /* What the launches read about the matrices: gd_muon_table_bytes bytes (0 where the list is refused), written to host
  * memory by gd_muon_fill_table.  The caller copies them to the device once (256-byte aligned there) and keeps both as
- * long as the tensors stay where they are.  No tensor may stand twice in a table. */
+ * long as the tensors stay where they are.  A list whose written arrays (params, momenta, copies) overlap is refused. */
 size_t gd_muon_table_bytes(gd_handle h, const gd_muon_tensor* tensors, uint32_t n_tensors);
 gd_status gd_muon_fill_table(gd_handle h, const gd_muon_tensor* tensors, uint32_t n_tensors, void* host_table, size_t bytes);
 /* Of the work area of an update with these products (256-byte aligned, nothing is kept in it between calls); 0 where the

@@ -5,8 +5,11 @@
 #include <stdio.h>
 #include <string.h>
 
+#include <algorithm>
 #include <new>
 #include <string>
+#include <utility>
+#include <vector>
 
 #include "../../include/guard.h"
 #include "gd_internal.h"
@@ -90,14 +93,14 @@ uint32_t bytes_of(uint32_t type) { return type == GD_F32 || type == GD_I32 ? 4 :
 bool is_float(uint32_t type) { return type == GD_F32 || type == GD_BF16 || type == GD_F16; }
 
 // What is wrong with a matrix of rows x cols elements, or null.
-const char* bad_matrix(const gd_matrix* m, uint64_t rows, uint64_t cols) {
+const char* bad_matrix(const gd_matrix* m, uint64_t rows, uint64_t cols, uint64_t max_stride = MAX_STRIDE) {
     if (!m) return "null matrix";
     if (m->reserved != 0) return "reserved field of a matrix is not 0";
     if (m->rows != rows || m->cols != cols) return "sizes of the matrices do not fit each other";
     if (rows == 0 || cols == 0) return nullptr;
     if (!m->d_data) return "null pointer of a matrix";
     if (m->stride < cols) return "stride below the row's length";
-    if (m->stride > MAX_STRIDE && cols > 1) return "stride above 2^22 elements";
+    if (m->stride > max_stride && cols > 1) return max_stride == MAX_STRIDE ? "stride above 2^22 elements" : "stride above 2^24 elements";
     if (m->stride > (1ull << 40)) return "stride above 2^40 elements";
     if ((uintptr_t)m->d_data % bytes_of(m->dtype)) return "pointer of a matrix not aligned to its element";
     return nullptr;
@@ -170,7 +173,8 @@ const char* bad_packed(const gd_packed* p, uint64_t rows, uint64_t cols) {
     if (p->codes.dtype != GD_E4M3 && p->codes.dtype != GD_E5M2) return "codes must be e4m3 or e5m2";
     if (p->exp.dtype != GD_U8) return "powers of two must be u8";
     if (const char* e = bad_matrix(&p->codes, rows, cols)) return e;
-    if (const char* e = bad_matrix(&p->exp, (cols + GD_PACK_BLOCK - 1) / GD_PACK_BLOCK, rows)) return e;
+    // (rows of `exp` are not reached by offsets of 32 bits)
+    if (const char* e = bad_matrix(&p->exp, (cols + GD_PACK_BLOCK - 1) / GD_PACK_BLOCK, rows, GD_MAX_TOKENS)) return e;
     if (rows == 0 || cols == 0) return nullptr;
     if (((uintptr_t)p->codes.d_data & 15) || (rows > 1 && (p->codes.stride & 15))) return "codes and their stride must be 16-byte aligned";
     if (p->codes.stride > MAX_STRIDE) return "stride above 2^22 elements";
@@ -187,6 +191,7 @@ constexpr uint64_t MAX_INNER = 1u << 22;    // of a packed product: rows of `acr
 // What is wrong with the matrices of an update, or null.
 const char* bad_matrices(const gd_muon_tensor* list, uint32_t n) {
     if (n && !list) return "null list of tensors";
+    std::vector<std::pair<uintptr_t, uintptr_t>> written;
     for (uint32_t i = 0; i < n; ++i) {
         const gd_muon_tensor& t = list[i];
         if (t.reserved != 0) return "reserved field of a tensor is not 0";
@@ -199,7 +204,17 @@ const char* bad_matrices(const gd_muon_tensor* list, uint32_t n) {
         if ((uintptr_t)t.d_param % bytes_of(t.param_type) || (uintptr_t)t.d_grad % bytes_of(t.grad_type) || ((uintptr_t)t.d_m & 3) ||
             ((uintptr_t)t.d_copy & 1))
             return "pointer of a tensor not aligned to its element";
+        const uint64_t size = t.rows * t.cols;
+        auto writes = [&](const void* p, uint32_t type) {
+            if (p) written.emplace_back((uintptr_t)p, (uintptr_t)p + size * bytes_of(type));
+        };
+        writes(t.d_param, t.param_type);
+        writes(t.d_m, GD_F32);
+        writes(t.d_copy, t.copy_type);
     }
+    std::sort(written.begin(), written.end());
+    for (size_t i = 1; i < written.size(); ++i)
+        if (written[i].first < written[i - 1].second) return "tensors that are written overlap";
     return nullptr;
 }
 
@@ -835,18 +850,22 @@ gd_status gd_packed_product(gd_handle h, const gd_packed* a, const gd_packed* b,
 
 size_t gd_muon_table_bytes(gd_handle h, const gd_muon_tensor* tensors, uint32_t n_tensors) {
     if (!h) return 0;
-    if (const char* e = bad_matrices(tensors, n_tensors)) { invalid(h, "gd_muon_table_bytes", e); return 0; }
-    size_t bytes = 0;
-    try { bytes = gd_muon_table(tensors, n_tensors, nullptr); } catch (...) {}
-    if (!bytes) invalid(h, "gd_muon_table_bytes", "too many elements");
-    return bytes;
+    try {
+        if (const char* e = bad_matrices(tensors, n_tensors)) { invalid(h, "gd_muon_table_bytes", e); return 0; }
+        const size_t bytes = gd_muon_table(tensors, n_tensors, nullptr);
+        if (!bytes) invalid(h, "gd_muon_table_bytes", "too many elements");
+        return bytes;
+    } catch (...) {
+        invalid(h, "gd_muon_table_bytes", "out of host memory");
+        return 0;
+    }
 }
 
 gd_status gd_muon_fill_table(gd_handle h, const gd_muon_tensor* tensors, uint32_t n_tensors, void* host_table, size_t bytes) {
     if (!h) return GD_ERR_INVALID_ARG;
-    if (const char* e = bad_matrices(tensors, n_tensors)) return invalid(h, "gd_muon_fill_table", e);
     if (!host_table) return invalid(h, "gd_muon_fill_table", "null table");
     try {
+        if (const char* e = bad_matrices(tensors, n_tensors)) return invalid(h, "gd_muon_fill_table", e);
         const size_t need = gd_muon_table(tensors, n_tensors, nullptr);
         if (!need) return invalid(h, "gd_muon_fill_table", "too many elements");
         if (bytes != need) return fail(h, GD_ERR_BUFFER_TOO_SMALL, "gd_muon_fill_table: not gd_muon_table_bytes bytes");
