@@ -571,7 +571,7 @@ gd_status gd_pack(gd_handle h, const gd_matrix* x, int32_t square, const gd_pack
 
 /*
  * Product of packed matrices: out[i][j] = round((accumulate ? out[i][j] : 0) + sum over k of a[i][k] b[j][k]), summed in
- * fp32 in an order that the sizes alone fix.  For an out of 16 bits the products of eight neighbouring k are added by the 8-bit
+ * fp32 in an order that the sizes and the type of out alone fix.  For an out of 16 bits the products of eight neighbouring k are added by the 8-bit
  * matrix cores, which keep 13 binary digits behind the largest of them (1.5e-5 of the result for normal numbers, 7e-5
  * for numbers of wide range); for an out of fp32 by the 16-bit ones, at half the rate, and numbers below 2^-126 may count as 0.
  *   a    [n][k]  in       either's codes e4m3 or e5m2
@@ -630,7 +630,8 @@ gd_status gd_muon_fill_table(gd_handle h, const gd_muon_tensor* tensors, uint32_
 size_t gd_muon_work_bytes(gd_handle h, const void* host_table, size_t table_bytes, uint32_t products);
 
 /* One update of all matrices of a table.  d_grad_scale: one f32 in device memory that every gradient is multiplied by, or
- * null; where it is infinite or NaN nothing is written but the work area. */
+ * null; where it is infinite or NaN nothing is written.  What is in device memory no status can tell: a d_table
+ * that does not begin as host_table does writes nothing either, and one whose tensors have moved is followed to where they were. */
 gd_status gd_muon(gd_handle h, const void* host_table, const void* d_table, size_t table_bytes, const gd_muon_config* cfg,
                   const float* d_grad_scale, void* d_work, size_t work_bytes, void* stream);
 

@@ -52,6 +52,7 @@ struct entry {
 };
 
 struct head {
+    uint64_t mark;                // of all that follows: a launch reads a table that has the mark of the host's, or none
     uint64_t bytes;
     uint32_t magic, n;
     uint32_t first[KINDS + 1];    // entries of a kind of tiles; behind the last one's lie the tiny ones
@@ -95,6 +96,7 @@ struct layout {
 
 struct muon_args {
     const uint8_t* table;
+    uint64_t mark;
     uint32_t n, tiled;            // entries, those that are not tiny
     uint32_t first, count;        // entries of the launch's kind
     uint32_t quarters;            // of tiles of 256 x 256: the launch takes quarters of these, from this one on, plus 1; 0: no quarters
@@ -135,10 +137,10 @@ __device__ __forceinline__ uint32_t find(const muon_args& g, int list, uint32_t 
     return first + k;
 }
 
-// Whether gradients are to be used at all; their factor.
-__device__ __forceinline__ bool factor_of(const muon_args& g, float& f) {
+// Whether there is something to do: the table is the one that the launch was made for, the gradients' factor (in f) is finite.
+__device__ __forceinline__ bool begins(const muon_args& g, float& f) {
     f = g.grad_scale ? *g.grad_scale : 1.0f;
-    return (__builtin_bit_cast(uint32_t, f) & 0x7F800000u) != 0x7F800000u;
+    return reinterpret_cast<const head*>(g.table)->mark == g.mark && (__builtin_bit_cast(uint32_t, f) & 0x7F800000u) != 0x7F800000u;
 }
 
 __device__ __forceinline__ float grad_at(const entry& e, uint64_t i) {
@@ -186,7 +188,7 @@ __device__ __forceinline__ double advance(const muon_args& g, const entry& e, ui
 // M, and the sums of squares of U, a piece a workgroup.
 __global__ __launch_bounds__(512) void momentum_kernel(const muon_args g) {
     float f;
-    if (!factor_of(g, f)) return;
+    if (!begins(g, f)) return;
     uint32_t t = blockIdx.x;
     const entry e = entry_at(g, find(g, OF_CHUNKS, 0, g.tiled, t));
     const uint64_t size = (uint64_t)e.rows * e.cols, from = (uint64_t)t * e.chunk, end = min(from + e.chunk, size);
@@ -250,7 +252,7 @@ __device__ __forceinline__ void updates_of(const muon_args& g, const entry& e, u
 // X of the first step, 64 x 64 a workgroup, both ways, with zeros up to the end of a block of k.
 __global__ __launch_bounds__(256) void start_kernel(const muon_args g) {
     float f;
-    if (!factor_of(g, f)) return;
+    if (!begins(g, f)) return;
     uint32_t t = blockIdx.x;
     const entry e = entry_at(g, find(g, OF_TILES, 0, g.tiled, t));
     const double* part = reinterpret_cast<const double*>(g.work) + e.partial;
@@ -510,7 +512,7 @@ template <int PHASE, template <typename> class TILE>
 __global__ __launch_bounds__(TILE<of_f16>::NT, 512 / TILE<of_f16>::NT) void tiled_kernel(const muon_args g) {
     typedef TILE<of_f16> tile;
     float f;
-    if (!factor_of(g, f)) return;
+    if (!begins(g, f)) return;
     uint32_t tp, tq;
     entry e;
     if (!place_of<PHASE>(g, tile::BP, tp, tq, e)) return;
@@ -549,7 +551,7 @@ template <int PHASE, int WAVES>
 __global__ __launch_bounds__(64 * WAVES, 8 / WAVES) void direct_kernel(const muon_args g) {
     typedef direct_tile<of_f16, 4, WAVES> tile;
     float f;
-    if (!factor_of(g, f)) return;
+    if (!begins(g, f)) return;
     uint32_t tp, tq;
     entry e;
     place_of<PHASE>(g, 64, tp, tq, e);
@@ -582,7 +584,7 @@ __global__ __launch_bounds__(64 * WAVES, 8 / WAVES) void direct_kernel(const muo
 // steps = 0: W from X of the start.
 __global__ __launch_bounds__(256) void apply_kernel(const muon_args g) {
     float f;
-    if (!factor_of(g, f)) return;
+    if (!begins(g, f)) return;
     uint32_t t = blockIdx.x;
     const entry e = entry_at(g, find(g, OF_TILES, 0, g.tiled, t));
     const layout l(e.rows, e.cols, g.both);
@@ -709,7 +711,7 @@ __global__ __launch_bounds__(TINY_NT) void tiny_kernel(const muon_args g, const 
     constexpr uint32_t WAVES = TINY_NT / 64;
     constexpr int MINE = TINY_A / 16 * (TINY_B / 16) / WAVES, SQUARES = TINY_A / 16 * (TINY_A / 16) / WAVES;
     float f;
-    if (!factor_of(g, f)) return;
+    if (!begins(g, f)) return;
     const entry e = entry_at(g, g.first + blockIdx.x);
     const bool tall = e.rows > e.cols, both = g.both;
     const uint32_t a = tall ? e.cols : e.rows, b = tall ? e.rows : e.cols;
@@ -900,6 +902,13 @@ double most_of_even(double b, double c, double s) {
     return most;
 }
 
+// FNV-1a, 64 bits.
+uint64_t mark_of(const uint8_t* p, size_t n) {
+    uint64_t x = 0xCBF29CE484222325ull;
+    for (size_t i = 0; i < n; ++i) x = (x ^ p[i]) * 0x100000001B3ull;
+    return x;
+}
+
 }  // namespace
 
 size_t gd_muon_table(const gd_muon_tensor* t, uint32_t n, void* out) {
@@ -965,7 +974,11 @@ size_t gd_muon_table(const gd_muon_tensor* t, uint32_t n, void* out) {
     h.tiles = (uint32_t)tiles;
     h.work[0] = work[0];
     h.work[1] = work[1];
-    if (to) memcpy(to, &h, sizeof(h));
+    if (to) {
+        memcpy(to, &h, sizeof(h));
+        h.mark = mark_of(to + sizeof(h.mark), bytes - sizeof(h.mark));
+        memcpy(to, &h.mark, sizeof(h.mark));
+    }
     return bytes;
 }
 
@@ -997,7 +1010,7 @@ hipError_t gd_launch_muon(const gd_muon_args& m, hipStream_t s) {
     memcpy(&h, m.host_table, sizeof(h));
     if (h.n == 0) return hipSuccess;
     muon_args g = {};
-    g.table = m.table; g.n = h.n; g.work = m.work; g.grad_scale = m.grad_scale;
+    g.table = m.table; g.mark = h.mark; g.n = h.n; g.work = m.work; g.grad_scale = m.grad_scale;
     g.both = m.both; g.mu = m.momentum; g.eps = m.eps; g.nesterov = m.nesterov; g.lr = m.lr;
     g.tiled = h.first[TINY];
     if (g.tiled) {

@@ -721,7 +721,7 @@ class Detector:
         every step, or a list of them, one a step.  products: "f32", or "f16" for 16-bit parameters.  grad_scale: a device
         scalar that multiplies the gradients; where it is not finite nothing is written."""
         c, at = None, 0
-        if coefficients is not None:
+        if coefficients is not None and steps > 0:
             flat = [float(v) for t in coefficients for v in t] if hasattr(coefficients[0], "__len__") else [float(v) for v in coefficients] * steps
             assert len(flat) == 3 * steps, "three coefficients a step"
             c = (ctypes.c_double * max(len(flat), 1))(*flat)

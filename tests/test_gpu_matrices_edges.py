@@ -197,3 +197,34 @@ def test_an_update_behind_a_table_whose_lists_the_caller_drops(det):
     junk = [torch.full((70, 90), float("nan"), device="cuda") for _ in range(8)]
     det.muon(table, work, lr=1.0)
     assert torch.equal(p, want) and len(junk) == 8 and at.nbytes()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_one_row_against_many(det, dtype):
+    """One row of a matrix whose distance to the next says nothing, in tiles of every kind."""
+    for n, k in ((5, 101), (700, 77), (50_000, 101), (50_000, 300)):
+        a, b = packed(det, randn((n, k), 1)), packed(det, randn((1, k), 2))
+        ref, bound = refs.product(refs.values(a["codes"], a["exp"].cpu()), refs.values(b["codes"], b["exp"].cpu()), dtype)
+        for x, y, t in ((a, b, False), (b, a, True)):
+            shape = (1, n) if t else (n, 1)
+            out = torch.empty(shape, dtype=dtype, device="cuda")
+            det.packed_product(x, y, out, det.alloc_packed_product_work(*shape, k))
+            assert bool(((out.double().cpu() - (ref.t() if t else ref)).abs() <= (bound.t() if t else bound)).all()), (n, k, t)
+
+
+@pytest.mark.parametrize("shape", [(300, 200), (40, 64)])
+def test_a_table_that_is_not_the_host_s_writes_nothing(det, shape):
+    p, g, m = torch.zeros(shape, device="cuda"), low_rank(*shape, 1).cuda(), low_rank(*shape, 2).cuda()
+    table = det.muon_table([p], [g], [m])
+    work, before = det.alloc_muon_work(table), m.clone()
+    whole = table["bytes"].clone()
+    for spoil in (lambda b: b.zero_(), lambda b: b[300:301].add_(1), lambda b: b[-1:].add_(1)):
+        b = whole.clone()
+        spoil(b)
+        same_mark = bool((b[:8] == whole[:8]).all())
+        if same_mark:
+            b[:8] = 0                                        # (a copy that was not made whole: not the host's mark)
+        det.muon(dict(table, bytes=b), work, lr=1.0)
+        assert bool((p == 0).all()) and torch.equal(m, before)
+    det.muon(table, work, lr=1.0)
+    assert bool((p != 0).any())
