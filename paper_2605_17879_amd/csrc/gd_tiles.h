@@ -45,18 +45,30 @@ struct fragment {
 __device__ __forceinline__ f32x4 multiply_16(f16x8 p, f16x8 q, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(p, q, c, 0, 0, 0); }
 __device__ __forceinline__ f32x4 multiply_16(bf16x8 p, bf16x8 q, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(p, q, c, 0, 0, 0); }
 
+// A kind of product is STEPS instructions on a pair of fragments: one after the other on one sum they would wait for each other,
+// so that a tile takes a step for all of its sums before the next.
 template <typename X8>
 struct of_16 {
     static constexpr bool SCALED = false;
-    template <int I, int J>
+    static constexpr int STEPS = 2;
+    template <int STEP, int I, int J>
     static __device__ __forceinline__ f32x4 multiply(const fragment& p, const fragment& q, f32x4 c, uint32_t, uint32_t) {
-#pragma unroll
-        for (int h = 0; h < 2; ++h) c = multiply_16(__builtin_bit_cast(X8, p.h[h]), __builtin_bit_cast(X8, q.h[h]), c);
-        return c;
+        return multiply_16(__builtin_bit_cast(X8, p.h[STEP]), __builtin_bit_cast(X8, q.h[STEP]), c);
     }
 };
 typedef of_16<f16x8> of_f16;
 typedef of_16<bf16x8> of_bf16;
+
+// Numbers hi + lo of two f16 each, 32 hi and then their 32 lo in a block: lo hi + hi lo + hi hi.  A lane's first chunk of a block is hi, its
+// second the lo of the same numbers.
+struct of_pairs {
+    static constexpr bool SCALED = false;
+    static constexpr int STEPS = 3;
+    template <int STEP, int I, int J>
+    static __device__ __forceinline__ f32x4 multiply(const fragment& p, const fragment& q, f32x4 c, uint32_t, uint32_t) {
+        return multiply_16(__builtin_bit_cast(f16x8, p.h[STEP == 0]), __builtin_bit_cast(f16x8, q.h[STEP == 1]), c);
+    }
+};
 
 // Codes of P and of Q: 0 for e4m3, 1 for e5m2.  Byte I of `pe` is the power of two of the lane's row of P, byte J of `qe`
 // that of Q.  The 8-bit matrix cores cut the products of eight neighbouring k at 2^-13 of the largest one's power of two
@@ -65,7 +77,8 @@ typedef of_16<bf16x8> of_bf16;
 template <int P_CODES, int Q_CODES>
 struct of_codes {
     static constexpr bool SCALED = true;
-    template <int I, int J>
+    static constexpr int STEPS = 1;
+    template <int STEP, int I, int J>
     static __device__ __forceinline__ f32x4 multiply(const fragment& p, const fragment& q, f32x4 c, uint32_t pe, uint32_t qe) {
         return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(__builtin_bit_cast(i32x8, p), __builtin_bit_cast(i32x8, q), c, P_CODES, Q_CODES,
                                                                 I, (int)pe, J, (int)qe);
@@ -150,15 +163,21 @@ struct of_codes_in_16 {
     }
 };
 
-// The same of sums a fragment of P apart.
-template <typename MUL> struct sixteen {
-    static __device__ __forceinline__ void multiply(f32x4 (&c)[4][4], const fragment (&p)[4], const fragment (&q)[4], uint32_t pe, uint32_t qe) {
-        each<4>([&](auto of_p) {
-            each<4>([&](auto of_q) {
-                constexpr int i = decltype(of_p)::value, j = decltype(of_q)::value;
-                c[i][j] = MUL::template multiply<i, j>(p[i], q[j], c[i][j], pe, qe);
+template <typename MUL, int FP, int FQ>
+__device__ __forceinline__ void multiply_all(const fragment (&p)[FP], const fragment (&q)[FQ], f32x4 (&acc)[FP][FQ], uint32_t pe, uint32_t qe) {
+    each<MUL::STEPS>([&](auto of_step) {
+        each<FP>([&](auto of_p) {
+            each<FQ>([&](auto of_q) {
+                constexpr int s = decltype(of_step)::value, i = decltype(of_p)::value, j = decltype(of_q)::value;
+                acc[i][j] = MUL::template multiply<s, i, j>(p[i], q[j], acc[i][j], pe, qe);
             });
         });
+    });
+}
+
+template <typename MUL> struct sixteen {
+    static __device__ __forceinline__ void multiply(f32x4 (&c)[4][4], const fragment (&p)[4], const fragment (&q)[4], uint32_t pe, uint32_t qe) {
+        multiply_all<MUL>(p, q, c, pe, qe);
     }
 };
 template <int P, int Q> struct sixteen<of_codes<P, Q>> {
@@ -170,43 +189,21 @@ template <int P, int Q> struct sixteen<of_codes<P, Q>> {
 template <typename MUL> struct requires_all : std::false_type {};
 template <int P, int Q> struct requires_all<of_codes_in_16<P, Q>> : std::true_type {};
 
-template <typename MUL, int FP, int FQ>
-__device__ __forceinline__ void multiply_all(const fragment (&p)[FP], const fragment (&q)[FQ], f32x4 (&acc)[FP][FQ], uint32_t pe, uint32_t qe) {
-    each<FP>([&](auto of_p) {
-        each<FQ>([&](auto of_q) {
-            constexpr int i = decltype(of_p)::value, j = decltype(of_q)::value;
-            acc[i][j] = MUL::template multiply<i, j>(p[i], q[j], acc[i][j], pe, qe);
-        });
-    });
-}
-
 // ---- operands ----------------------------------------------------------------------------------
 
 struct operand {
     const uint8_t* p;
     uint64_t pitch;        // bytes between rows, a multiple of 16
     uint32_t rows;         // that are there, at least one
-    uint32_t row_bytes;    // that a row has along k with all its parts, up to whole chunks of 16, at least one chunk
+    uint32_t row_bytes;    // that a row has along k, up to whole chunks of 16, at least one chunk
     const uint8_t* exp;    // powers of two, [block][row], 4-byte aligned, or unused
     uint64_t exp_pitch;    // a multiple of 4
 };
 
-// Where a product's blocks are: block t of `parts` parts of `blocks` each is block t % blocks of what begins at
-// p_at(part) (q_at(part)) bytes in a row.  Behind the part `shrink` - 1 the sum so far is multiplied by 2^-11.
 struct passage {
-    uint32_t blocks, parts, shrink;
-    uint32_t p0, p1, q0, q1;   // of the first two parts; a third begins with the rows
-    uint32_t ends;             // bytes of the last block that are there; 0: all
-    __device__ __forceinline__ uint32_t part_of(uint32_t t) const { return (t >= blocks) + (t >= 2 * blocks); }   // (one part ends with the blocks)
-    // (by masks: a choice between two members would be read at a computed address, which keeps the struct in scratch memory)
-    static __device__ __forceinline__ uint32_t choose(uint32_t part, uint32_t a, uint32_t b) {
-        return (-(uint32_t)(part == 0) & a) | (-(uint32_t)(part == 1) & b);
-    }
-    __device__ __forceinline__ uint32_t p_at(uint32_t part) const { return choose(part, p0, p1); }
-    __device__ __forceinline__ uint32_t q_at(uint32_t part) const { return choose(part, q0, q1); }
+    uint32_t blocks;       // of k
+    uint32_t ends;         // bytes of the last block that are there; 0: all
 };
-
-constexpr float SHRINK = 0x1p-11f;
 
 // Of a row's chunk in the last block, of which `ends` bytes are there: zeros behind them.
 __device__ __forceinline__ void cut(gd_u32x4& x, uint32_t ends, uint32_t chunk) {
@@ -321,14 +318,6 @@ __device__ __forceinline__ fragment read_fragment(const uint8_t* s, uint32_t row
     return f;
 }
 
-template <int FP, int FQ>
-__device__ __forceinline__ void shrink(f32x4 (&acc)[FP][FQ]) {
-#pragma unroll
-    for (int i = 0; i < FP; ++i)
-#pragma unroll
-        for (int j = 0; j < FQ; ++j) acc[i][j] *= SHRINK;
-}
-
 // ---- tiles -------------------------------------------------------------------------------------
 
 // 256 x 256 by eight waves, one workgroup a CU, two waves a SIMD that take turns: while the waves of one
@@ -359,7 +348,7 @@ struct large_tile {
         __shared__ __attribute__((aligned(16))) uint8_t se0[BP + BQ], se1[BP + BQ];
         const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
         const uint32_t wp = wave / WQ, group = wp;           // (waves w and w + 4 share a SIMD)
-        const uint32_t blocks = way.blocks * way.parts;
+        const uint32_t blocks = way.blocks;
         if (blocks == 0) return;
         constexpr int ALL = MUL::SCALED ? 9 : 8;             // loads of a wave in a block, two of them the lower half's
         stager<128, NT> lu, ll;
@@ -373,19 +362,17 @@ struct large_tile {
         uint32_t eu = 0, el = 0, eq = 0;
         // `inner`: this is not the last block
         auto stage_low = [&](bool inner, uint8_t* low, uint32_t t) {
-            const uint32_t part = MUL::SCALED ? 0 : way.part_of(t);
             if (MUL::SCALED && !inner && way.ends != 0 && t + 1 == blocks) ll.stage_end(low, t, way.ends);
-            else ll.stage(low, way.p_at(part) + (t - part * way.blocks) * BYTES);
+            else ll.stage(low, t * BYTES);
         };
         auto stage_up = [&](bool inner, uint8_t* up, uint8_t* sq, uint8_t* se, uint32_t t) {
-            const uint32_t part = MUL::SCALED ? 0 : way.part_of(t);
             if (MUL::SCALED) le.stage(se, t, lane, wave);
             if (MUL::SCALED && !inner && way.ends != 0 && t + 1 == blocks) {
                 lq.stage_end(sq, t, way.ends);
                 lu.stage_end(up, t, way.ends);
             } else {
-                lq.stage(sq, way.q_at(part) + (t - part * way.blocks) * BYTES);
-                lu.stage(up, way.p_at(part) + (t - part * way.blocks) * BYTES);
+                lq.stage(sq, t * BYTES);
+                lu.stage(up, t * BYTES);
             }
         };
         auto read_p = [&](const uint8_t* s) {
@@ -414,7 +401,6 @@ struct large_tile {
         auto block = [&](auto more, uint8_t* up, uint8_t* low, uint8_t* sq, uint8_t* se, uint8_t* nlow, uint32_t t) {
             constexpr bool MORE = decltype(more)::value;
             const uint32_t newer_up = MORE || t + 1 < blocks ? ALL : 0, newer_low = MORE || t + 2 < blocks ? ALL : t + 1 < blocks ? 2 : 0;
-            if (!MUL::SCALED && t != 0 && t == way.shrink * way.blocks) shrink(acc);
 #pragma unroll
             for (int j = 0; j < FQ; ++j) fq[j] = read_fragment(sq, q_of(wave), j, lane);
             read_p(up);
@@ -483,7 +469,7 @@ struct small_tile {
         __shared__ __attribute__((aligned(16))) uint8_t sp0[BP * BYTES], sq0[BQ * BYTES], se0[BP + BQ];
         __shared__ __attribute__((aligned(16))) uint8_t sp1[BP * BYTES], sq1[BQ * BYTES], se1[BP + BQ];
         const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
-        const uint32_t blocks = way.blocks * way.parts;
+        const uint32_t blocks = way.blocks;
         if (blocks == 0) return;
         stager<BP, NT> lp;
         stager<BQ, NT> lq;
@@ -492,14 +478,13 @@ struct small_tile {
         lq.init(oq, q0, wave);
         if (MUL::SCALED) le.init(op, p0, oq, q0, lane, wave);
         auto stage = [&](bool inner, uint8_t* sp, uint8_t* sq, uint8_t* se, uint32_t t) {
-            const uint32_t part = MUL::SCALED ? 0 : way.part_of(t);
             if (MUL::SCALED) le.stage(se, t, lane, wave);
             if (MUL::SCALED && !inner && way.ends != 0 && t + 1 == blocks) {
                 lp.stage_end(sp, t, way.ends);
                 lq.stage_end(sq, t, way.ends);
             } else {
-                lp.stage(sp, way.p_at(part) + (t - part * way.blocks) * BYTES);
-                lq.stage(sq, way.q_at(part) + (t - part * way.blocks) * BYTES);
+                lp.stage(sp, t * BYTES);
+                lq.stage(sq, t * BYTES);
             }
         };
         fragment fp[4], fq[2][FQ];
@@ -522,7 +507,6 @@ struct small_tile {
         // none they are read for nothing.
         auto block = [&](auto b, auto more, uint8_t* sp, uint8_t* sq, uint8_t* se, uint8_t* np, uint8_t* nq, uint8_t* ne, uint32_t t) {
             constexpr bool MORE = decltype(more)::value;
-            if (!MUL::SCALED && t != 0 && t == way.shrink * way.blocks) shrink(acc);
             each<4>([&](auto step) {
                 constexpr int i = decltype(step)::value, B = decltype(b)::value;
                 if (i == 0) fp[3] = read_fragment(sp, p_of(wave, 0), 3, lane);
@@ -531,9 +515,11 @@ struct small_tile {
                     if (MORE || t + 2 < blocks) stage(MORE, sp, sq, se, t + 2);
                     read_q(nq, ne, 1 - B);
                 }
-                each<FQ>([&](auto of_q) {
-                    constexpr int j = decltype(of_q)::value;
-                    acc[i][j] = MUL::template multiply<i, j>(fp[i], fq[B][j], acc[i][j], ep[B], eq[B]);
+                each<MUL::STEPS>([&](auto of_step) {
+                    each<FQ>([&](auto of_q) {
+                        constexpr int s = decltype(of_step)::value, j = decltype(of_q)::value;
+                        acc[i][j] = MUL::template multiply<s, i, j>(fp[i], fq[B][j], acc[i][j], ep[B], eq[B]);
+                    });
                 });
                 if (i > 0) fp[(i + 3) % 4] = read_fragment(np, p_of(wave, 0), (i + 3) % 4, lane);
                 __builtin_amdgcn_sched_barrier(0);
@@ -589,7 +575,7 @@ struct direct_tile {
                                                 uint32_t first, uint32_t end, f32x4 (&sum)[FP]) {
         __shared__ __attribute__((aligned(16))) uint8_t rows[WAVES * PART], exps[WAVES * EXPS];
         const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
-        const uint32_t blocks = way.blocks * way.parts, c = lane & 15;
+        const uint32_t blocks = way.blocks, c = lane & 15;
         f32x4 acc[FP][FQ] = {};
         // Eight places of the LDS a load, a row's chunk a lane: place 16 i + c holds row FP c + i, chunk k at k ^ (c % 8).
         constexpr int PL = BP / 8, QL = BQ / 8;
@@ -607,7 +593,7 @@ struct direct_tile {
         };
         uint8_t *const to = rows + wave * PART, *const to_exp = exps + wave * EXPS;
         auto stage = [&](uint32_t t) {
-            const uint32_t part = MUL::SCALED ? 0 : way.part_of(t), in = (t - part * way.blocks) * BYTES;
+            const uint32_t in = t * BYTES;
             if (MUL::SCALED) {
                 if (lane < BP / 4)
                     __builtin_amdgcn_raw_ptr_buffer_load_lds(whole_buffer(scalar(op.exp + t * op.exp_pitch)), (lds_void*)to_exp, 4, pe_at, 0, 0, 0);
@@ -615,15 +601,13 @@ struct direct_tile {
                     __builtin_amdgcn_raw_ptr_buffer_load_lds(whole_buffer(scalar(oq.exp + t * oq.exp_pitch)), (lds_void*)(to_exp + BP), 4, qe_at, 0, 0, 0);
             }
             // (chunks behind the row's end: its last one again, which is cut off)
-            const uint32_t here = min(chunk, op.row_bytes - 16 - way.p_at(part) - in), there = min(chunk, oq.row_bytes - 16 - way.q_at(part) - in);
-            const __amdgpu_buffer_rsrc_t from_p = whole_buffer(p_base + way.p_at(part) + in), from_q = whole_buffer(q_base + way.q_at(part) + in);
+            const uint32_t here = min(chunk, op.row_bytes - 16 - in), there = min(chunk, oq.row_bytes - 16 - in);
+            const __amdgpu_buffer_rsrc_t from_p = whole_buffer(p_base + in), from_q = whole_buffer(q_base + in);
 #pragma unroll
             for (int j = 0; j < PL; ++j) load(from_p, to + j * 1024, p_at[j] + here);
 #pragma unroll
             for (int j = 0; j < QL; ++j) load(from_q, to + BP * BYTES + j * 1024, q_at[j] + there);
         };
-        // (a wave that goes past the part that shrinks does so once; one that has no block there scales at the end)
-        bool whole = way.shrink == 0;
         uint32_t t = first + wave;
         if (t < end) stage(t);
         for (; t < end; t += WAVES) {
@@ -650,14 +634,9 @@ struct direct_tile {
 #pragma unroll
                 for (int j = 0; j < FQ; ++j) cut(q[j], way.ends, lane);
             }
-            if (!MUL::SCALED && !whole && t >= way.shrink * way.blocks) {
-                shrink(acc);
-                whole = true;
-            }
             if constexpr (requires_all<MUL>::value) MUL::multiply_all(p, q, acc, pe, qe);
             else multiply_all<MUL>(p, q, acc, pe, qe);
         }
-        if (!whole) shrink(acc);
         __syncthreads();
         sums* shared = reinterpret_cast<sums*>(rows);
 #pragma unroll

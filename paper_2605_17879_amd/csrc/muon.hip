@@ -10,8 +10,9 @@
 //
 // The matrix cores bound it: 2 a^2 b numbers are multiplied for A, half of them since A is symmetric, a^3 likewise for
 // A^2, and a^2 b for the product with X.  They take f16; X, A and B = b A + c A^2 are kept in numbers of f16 times a power of two
-// that their largest singular values allow, as hi + 2^-11 lo, and a product is one of
-//   GD_F32   lo hi + hi lo + hi hi: 22 digits of each operand
+// that their largest singular values allow, as hi + lo, and a product is one of
+//   GD_F32   lo hi + hi lo + hi hi: 22 digits of each operand (hi and lo of 32 numbers side by side, so that each is loaded once for the
+//            three: lo hi, hi lo and hi hi one behind the other took 1.06 to 1.12 times as long)
 //   GD_F16   hi hi.  The X that is a part of the next one keeps its lo: what rounding drops of it would lie in directions whose
 //            singular values are small, and grow with them, up to a^steps = 485 times (512 x 512, 16 strong directions over a floor of
 //            noise: 1.1e-2 off with X in f16, 1.7e-4 with hi + lo; bf16 9e-2).  In the product with B it matters little: X hi there
@@ -69,29 +70,50 @@ static_assert(sizeof(head) <= HEAD, "the table's head");
 __host__ __device__ inline uint64_t up_to(uint64_t v, uint64_t unit) { return (v + unit - 1) / unit * unit; }
 __host__ __device__ inline uint64_t list_at(uint32_t n, int list) { return HEAD + n * sizeof(entry) + (uint64_t)list * up_to(n * 4, 16); }
 
-// Where an entry's matrices lie from its place in the work area on; pitches in bytes.
+// How a matrix of numbers of hi and lo lies: with `pairs` 32 hi and their 32 lo in turn, else the hi of a row and, `lo` bytes behind
+// them, its lo, if it has them.
+struct plane {
+    uint64_t pitch;               // bytes between rows
+    uint32_t cols;                // numbers of a row with the zeros behind its end
+    uint32_t lo;                  // bytes from a hi to its lo; 0: there are none
+    uint32_t pairs;
+    // The first of sixteen numbers that begin at a multiple of sixteen, or of fewer inside of them.
+    __host__ __device__ uint32_t at(uint32_t col) const { return pairs ? col / 32 * 128 + col % 32 * 2 : col * 2; }
+    __host__ __device__ uint32_t blocks() const { return pairs ? cols / 32 : cols / 64; }
+};
+
+// Where an entry's matrices lie from its place in the work area on.
 struct layout {
     uint32_t a, b;                // the shorter and the longer side
-    uint64_t r_pitch, c_pitch, s_pitch, lo_r, lo_c, lo_s;
+    plane r, c, s;                // X as the matrix lies and transposed; A and B
     uint64_t of_r, of_c, sa, sb, total;
     __host__ __device__ layout(uint32_t rows, uint32_t cols, bool both) {
         a = rows < cols ? rows : cols;
         b = rows < cols ? cols : rows;
-        lo_r = up_to(cols, 64) * 2; lo_c = up_to(rows, 64) * 2; lo_s = up_to(a, 64) * 2;
-        // (rows a multiple of 256 bytes apart meet at the same channels of the memory: 8 matrices of 1 024 x 1 024 and 8 of 2 048 x 1 024
-        // 2.39 ms with such, 2.21 without, 4 of 4 096 x 4 096 5.95 and 5.76)
-        auto odd = [](uint64_t v) { return v % 256 ? v : v + 128; };
-        r_pitch = odd(2 * lo_r); c_pitch = odd(both ? 2 * lo_c : lo_c); s_pitch = odd(both ? 2 * lo_s : lo_s);   // (R alone is a part of the next X)
-        of_r = up_to(rows * r_pitch, 256);
-        of_c = up_to(cols * c_pitch, 256);
-        const uint64_t of_s = up_to(a * s_pitch, 256);
+        r = plane_of(cols, both, true);
+        c = plane_of(rows, both, both);          // (without pairs R alone is a part of the next X)
+        s = plane_of(a, both, both);
+        of_r = up_to(rows * r.pitch, 256);
+        of_c = up_to(cols * c.pitch, 256);
+        const uint64_t of_s = up_to(a * s.pitch, 256);
         sa = 2 * (of_r + of_c);
         sb = sa + of_s;
         total = sb + of_s;
     }
+    static __host__ __device__ plane plane_of(uint32_t cols, bool pairs, bool lo) {
+        plane p;
+        p.pairs = pairs;
+        p.cols = (uint32_t)up_to(cols, pairs ? 32 : 64);
+        p.lo = !lo ? 0 : pairs ? 64 : p.cols * 2;
+        p.pitch = (uint64_t)p.cols * (lo ? 4 : 2);
+        // (rows a multiple of 256 bytes apart meet at the same channels of the memory: 8 matrices of 1 024 x 1 024 and 8 of 2 048 x 1 024
+        // 2.39 ms with such, 2.21 without, 4 of 4 096 x 4 096 5.95 and 5.76)
+        if (p.pitch % 256 == 0) p.pitch += 128;
+        return p;
+    }
     // The first and the second X, as the matrix lies and transposed.
-    __host__ __device__ uint64_t r(uint32_t i) const { return i * of_r; }
-    __host__ __device__ uint64_t c(uint32_t i) const { return 2 * of_r + i * of_c; }
+    __host__ __device__ uint64_t r_at(uint32_t i) const { return i * of_r; }
+    __host__ __device__ uint64_t c_at(uint32_t i) const { return 2 * of_r + i * of_c; }
 };
 
 struct muon_args {
@@ -212,9 +234,9 @@ struct halves {
 };
 __device__ __forceinline__ halves split(float x) {
     const gd_f16 hi = (gd_f16)x;
-    return {hi, (gd_f16)((x - (float)hi) * 0x1p11f)};
+    return {hi, (gd_f16)(x - (float)hi)};
 }
-__device__ __forceinline__ float whole(gd_f16 hi, gd_f16 lo) { return (float)hi + (float)lo * SHRINK; }
+__device__ __forceinline__ float whole(gd_f16 hi, gd_f16 lo) { return (float)hi + (float)lo; }
 
 typedef gd_f16 f16x4 __attribute__((ext_vector_type(4)));
 
@@ -275,15 +297,15 @@ __global__ __launch_bounds__(256) void start_kernel(const muon_args g) {
         for (int j = 0; j < 4; ++j) x[i][j] = split((float)(u[i][j] * scale));
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        if (row + i < e.rows) {
-            uint8_t* to = base + l.r(0) + (row + i) * l.r_pitch + col * 2;
+        if (row + i < e.rows && col < l.r.cols) {
+            uint8_t* to = base + l.r_at(0) + (row + i) * l.r.pitch + l.r.at(col);
             *reinterpret_cast<f16x4*>(to) = f16x4{x[i][0].hi, x[i][1].hi, x[i][2].hi, x[i][3].hi};
-            *reinterpret_cast<f16x4*>(to + l.lo_r) = f16x4{x[i][0].lo, x[i][1].lo, x[i][2].lo, x[i][3].lo};
+            *reinterpret_cast<f16x4*>(to + l.r.lo) = f16x4{x[i][0].lo, x[i][1].lo, x[i][2].lo, x[i][3].lo};
         }
-        if (col + i < e.cols) {
-            uint8_t* to = base + l.c(0) + (col + i) * l.c_pitch + row * 2;
+        if (col + i < e.cols && row < l.c.cols) {
+            uint8_t* to = base + l.c_at(0) + (col + i) * l.c.pitch + l.c.at(row);
             *reinterpret_cast<f16x4*>(to) = f16x4{x[0][i].hi, x[1][i].hi, x[2][i].hi, x[3][i].hi};
-            if (g.both) *reinterpret_cast<f16x4*>(to + l.lo_c) = f16x4{x[0][i].lo, x[1][i].lo, x[2][i].lo, x[3][i].lo};
+            if (l.c.lo) *reinterpret_cast<f16x4*>(to + l.c.lo) = f16x4{x[0][i].lo, x[1][i].lo, x[2][i].lo, x[3][i].lo};
         }
     }
 }
@@ -292,14 +314,12 @@ __global__ __launch_bounds__(256) void start_kernel(const muon_args g) {
 
 enum { OF_X, OF_A, STEP, LAST };                   // A = X X^T; B = b A + c A A; X = a X + B X; the same, and W
 
-// What becomes of a tile: element (q, p) of a matrix D [rows_d][.], and of its transpose.
+// What becomes of a tile: element (q, p) of a matrix D [rows][cols], and of its transpose.
 struct target {
-    uint8_t* d;  uint64_t d_pitch, d_lo;           // written as it lies
-    uint8_t* t;  uint64_t t_pitch, t_lo;           // written transposed, or null
-    const uint8_t* old;                            // A or X at the same places as d
+    uint8_t* d;  plane of_d;       // written as it lies
+    uint8_t* t;  plane of_t;       // written transposed, or null
+    const uint8_t* old;            // A or X, as d lies
     uint32_t rows, cols;
-    bool lo, t_lo_too;                             // of what is written, as it lies and transposed
-    bool old_lo;                                   // of what is read
 };
 
 struct problem {
@@ -313,41 +333,24 @@ __device__ __forceinline__ problem problem_of(const muon_args& g, const entry& e
     const layout l(e.rows, e.cols, g.both);
     uint8_t* base = g.work + e.at[!g.both];
     const bool tall = e.rows > e.cols;
-    uint8_t *r0 = base + l.r(g.from), *c0 = base + l.c(g.from), *r1 = base + l.r(g.to), *c1 = base + l.c(g.to);
+    uint8_t *r0 = base + l.r_at(g.from), *c0 = base + l.c_at(g.from), *r1 = base + l.r_at(g.to), *c1 = base + l.c_at(g.to);
     uint8_t *sa = base + l.sa, *sb = base + l.sb;
     problem x;
-    auto matrix = [](const uint8_t* p, uint64_t pitch, uint32_t rows) { return operand{p, pitch, rows, (uint32_t)pitch, nullptr, 0}; };
-    // the part with a lo comes first
-    auto parts = [&](uint32_t n, uint64_t p_lo, uint64_t q_lo) {
-        x.way.parts = n;
-        x.way.shrink = n - 1;
-        x.way.p0 = n > 1 ? (uint32_t)p_lo : 0;
-        x.way.q1 = n > 2 ? (uint32_t)q_lo : 0;
-        x.way.p1 = x.way.q0 = 0;
-        x.way.ends = 0;
-    };
+    auto matrix = [](const uint8_t* p, const plane& l, uint32_t rows) { return operand{p, l.pitch, rows, (uint32_t)l.pitch, nullptr, 0}; };
+    x.way.ends = 0;
     if (PHASE == OF_X || PHASE == OF_A) {
-        if (PHASE == OF_X) x.p = tall ? matrix(c0, l.c_pitch, l.a) : matrix(r0, l.r_pitch, l.a);
-        else x.p = matrix(sa, l.s_pitch, l.a);
+        if (PHASE == OF_X) x.p = tall ? matrix(c0, l.c, l.a) : matrix(r0, l.r, l.a);
+        else x.p = matrix(sa, l.s, l.a);
         x.q = x.p;
-        const uint64_t lo = PHASE == OF_A ? l.lo_s : tall ? l.lo_c : l.lo_r;
-        x.way.blocks = (uint32_t)(lo / BYTES);
-        parts(g.both ? 3 : 1, lo, lo);
+        x.way.blocks = PHASE == OF_A ? l.s.blocks() : tall ? l.c.blocks() : l.r.blocks();
         uint8_t* to = PHASE == OF_X ? sa : sb;
-        x.out = target{to, l.s_pitch, l.lo_s, off_diagonal ? to : nullptr, l.s_pitch, l.lo_s, sa, l.a, l.a, g.both != 0, g.both != 0, g.both != 0};
+        x.out = target{to, l.s, off_diagonal ? to : nullptr, l.s, sa, l.a, l.a};
     } else {
-        const operand b = matrix(sb, l.s_pitch, l.a);
-        x.way.blocks = (uint32_t)(l.lo_s / BYTES);
-        if (tall) {
-            x.p = b;
-            x.q = matrix(r0, l.r_pitch, e.rows);
-            parts(g.both ? 3 : 1, l.lo_s, l.lo_r);
-        } else {
-            x.p = matrix(c0, l.c_pitch, e.cols);
-            x.q = b;
-            parts(g.both ? 3 : 1, l.lo_c, l.lo_s);
-        }
-        x.out = target{r1, l.r_pitch, l.lo_r, c1, l.c_pitch, l.lo_c, r0, e.rows, e.cols, true, g.both != 0, true};
+        const operand b = matrix(sb, l.s, l.a);
+        x.p = tall ? b : matrix(c0, l.c, e.cols);
+        x.q = tall ? matrix(r0, l.r, e.rows) : b;
+        x.way.blocks = l.s.blocks();
+        x.out = target{r1, l.r, c1, l.c, r0, e.rows, e.cols};
     }
     return x;
 }
@@ -359,12 +362,12 @@ struct old_row {
 __device__ __forceinline__ void read_old(const target& o, uint32_t row, uint32_t col, old_row& old) {
 #pragma unroll
     for (int h = 0; h < 2; ++h) old.hi[h] = old.lo[h] = gd_u32x4{};
-    if (row < o.rows && col < o.d_lo / 2) {
-        const gd_u32x4* from = reinterpret_cast<const gd_u32x4*>(o.old + row * o.d_pitch + col * 2);
+    if (row < o.rows && col < o.of_d.cols) {
+        const gd_u32x4* from = reinterpret_cast<const gd_u32x4*>(o.old + row * o.of_d.pitch + o.of_d.at(col));
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             old.hi[h] = from[h];
-            if (o.old_lo) old.lo[h] = from[o.d_lo / 16 + h];
+            if (o.of_d.lo) old.lo[h] = from[o.of_d.lo / 16 + h];
         }
     }
 }
@@ -391,7 +394,7 @@ __device__ __forceinline__ void finish_row(const muon_args& g, const target& o, 
 
 // (Called by all lanes of a wave; the next lane's row is four further on.)
 __device__ __forceinline__ void write_row(const target& o, uint32_t row, uint32_t col, const f32x4 (&v)[4], uint32_t lane) {
-    if (col >= o.d_lo / 2) return;                 // (the same for lanes that exchange)
+    if (col >= o.of_d.cols) return;                // (the same for lanes that exchange)
     gd_u32x4 hi[2], lo[2];
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
@@ -406,25 +409,25 @@ __device__ __forceinline__ void write_row(const target& o, uint32_t row, uint32_
         lo[h] = __builtin_bit_cast(gd_u32x4, y);
     }
     exchange<2>(hi, lane);
-    if (o.lo) exchange<2>(lo, lane);
+    if (o.of_d.lo) exchange<2>(lo, lane);
     const uint32_t first = row - lane % 2 * 4;
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
         const uint32_t r = first + 4 * h;
         if (r >= o.rows) break;
-        uint8_t* to = o.d + r * o.d_pitch + col * 2 + lane % 2 * 16;
+        uint8_t* to = o.d + r * o.of_d.pitch + o.of_d.at(col) + lane % 2 * 16;
         *reinterpret_cast<gd_u32x4*>(to) = hi[h];
-        if (o.lo) *reinterpret_cast<gd_u32x4*>(to + o.d_lo) = lo[h];
+        if (o.of_d.lo) *reinterpret_cast<gd_u32x4*>(to + o.of_d.lo) = lo[h];
     }
 }
 
 // Four rows from `row` on of a column, written next to each other.
 __device__ __forceinline__ void write_column(const target& o, uint32_t row, uint32_t col, float x0, float x1, float x2, float x3) {
-    if (!o.t || col >= o.cols || row >= o.t_lo / 2) return;
-    uint8_t* to = o.t + col * o.t_pitch + row * 2;
+    if (!o.t || col >= o.cols || row >= o.of_t.cols) return;
+    uint8_t* to = o.t + col * o.of_t.pitch + o.of_t.at(row);
     const halves s0 = split(x0), s1 = split(x1), s2 = split(x2), s3 = split(x3);
     *reinterpret_cast<f16x4*>(to) = f16x4{s0.hi, s1.hi, s2.hi, s3.hi};
-    if (o.t_lo_too) *reinterpret_cast<f16x4*>(to + o.t_lo) = f16x4{s0.lo, s1.lo, s2.lo, s3.lo};
+    if (o.of_t.lo) *reinterpret_cast<f16x4*>(to + o.of_t.lo) = f16x4{s0.lo, s1.lo, s2.lo, s3.lo};
 }
 
 template <typename T>
@@ -508,9 +511,9 @@ __device__ __forceinline__ bool place_of(const muon_args& g, uint32_t edge, uint
     return (HALF ? tp >= tq : true) && tq * 128 < (HALF ? a : e.rows) && tp * 128 < (HALF ? a : e.cols);
 }
 
-template <int PHASE, template <typename> class TILE>
-__global__ __launch_bounds__(TILE<of_f16>::NT, 512 / TILE<of_f16>::NT) void tiled_kernel(const muon_args g) {
-    typedef TILE<of_f16> tile;
+template <int PHASE, typename TILE>
+__global__ __launch_bounds__(TILE::NT, 512 / TILE::NT) void tiled_kernel(const muon_args g) {
+    typedef TILE tile;
     float f;
     if (!begins(g, f)) return;
     uint32_t tp, tq;
@@ -547,9 +550,9 @@ __global__ __launch_bounds__(TILE<of_f16>::NT, 512 / TILE<of_f16>::NT) void tile
     }
 }
 
-template <int PHASE, int WAVES>
+template <int PHASE, typename MUL, int WAVES>
 __global__ __launch_bounds__(64 * WAVES, 8 / WAVES) void direct_kernel(const muon_args g) {
-    typedef direct_tile<of_f16, 4, WAVES> tile;
+    typedef direct_tile<MUL, 4, WAVES> tile;
     float f;
     if (!begins(g, f)) return;
     uint32_t tp, tq;
@@ -561,7 +564,7 @@ __global__ __launch_bounds__(64 * WAVES, 8 / WAVES) void direct_kernel(const muo
     const uint32_t row = tq * 64 + 4 * (lane & 15), col = tp * 64 + 16 * (lane >> 4);
     old_row old = {};
     if (PHASE != OF_X && wave < 4) read_old(x.out, row + wave, col, old);   // (on its way beside the sum)
-    typename tile::sums* room = tile::run(x.p, x.q, tp * 64, tq * 64, x.way, 0, x.way.blocks * x.way.parts, v);
+    typename tile::sums* room = tile::run(x.p, x.q, tp * 64, tq * 64, x.way, 0, x.way.blocks, v);
     if (wave < 4) {
         finish_row<PHASE>(g, x.out, row + wave, col, v, old);
         if (PHASE == LAST) update_row(g, e, row + wave, col, v);
@@ -588,13 +591,13 @@ __global__ __launch_bounds__(256) void apply_kernel(const muon_args g) {
     uint32_t t = blockIdx.x;
     const entry e = entry_at(g, find(g, OF_TILES, 0, g.tiled, t));
     const layout l(e.rows, e.cols, g.both);
-    const uint8_t* base = g.work + e.at[!g.both] + l.r(0);
+    const uint8_t* base = g.work + e.at[!g.both] + l.r_at(0);
     const uint32_t tiles_c = (e.cols + 63) / 64, row = t / tiles_c * 64 + threadIdx.x / 4, col = t % tiles_c * 64 + threadIdx.x % 4 * 16;
     if (row >= e.rows || col >= e.cols) return;
-    const gd_f16* from = reinterpret_cast<const gd_f16*>(base + row * l.r_pitch) + col;
+    const gd_f16* from = reinterpret_cast<const gd_f16*>(base + row * l.r.pitch + l.r.at(col));
     f32x4 v[4];
 #pragma unroll
-    for (int x = 0; x < 16; ++x) v[x % 4][x / 4] = whole(from[x], from[l.lo_r / 2 + x]);
+    for (int x = 0; x < 16; ++x) v[x % 4][x / 4] = whole(from[x], from[l.r.lo / 2 + x]);
     update_row(g, e, row, col, v);
 }
 
@@ -648,7 +651,7 @@ __device__ __forceinline__ void tiny_products(f32x4 (&out)[N], const uint8_t* p,
         for (int n = 0; n < N; ++n) high[n] = multiply_16(ph[n], qh, high[n]);
     }
 #pragma unroll
-    for (int n = 0; n < N; ++n) out[n] = high[n] + low[n] * SHRINK;
+    for (int n = 0; n < N; ++n) out[n] = high[n] + low[n];
 }
 
 // Four neighbouring numbers of a row, as four hi and four lo.
@@ -830,8 +833,8 @@ __global__ __launch_bounds__(TINY_NT) void tiny_kernel(const muon_args g, const 
     else tiny_update<gd_f16>(e, lds.u, all, keep, move);
 }
 
-template <int PHASE>
-void launch_phase(muon_args g, const head& h, hipStream_t s) {
+template <int PHASE, typename MUL>
+void launch_phase_of(muon_args g, const head& h, hipStream_t s) {
     const uint32_t* tiles = PHASE == OF_X || PHASE == OF_A ? h.half : h.full;
     for (int k = 0; k < KINDS; ++k) {
         if (!tiles[k]) continue;
@@ -839,28 +842,34 @@ void launch_phase(muon_args g, const head& h, hipStream_t s) {
         g.count = h.first[k + 1] - h.first[k];
         if (k == LARGE) {
             // Whole rounds of the chip's 256 workgroups; what is left, if it is little, as quarters, which are less than a round of
-            // tiles of 128 x 128 (4 of 4 096 x 4 096, X X^T 544 tiles: 315 us as three rounds, 262 as two and 128 quarters).
+            // tiles of 128 x 128 (4 of 4 096 x 4 096, X X^T 544 tiles: 315 us as three rounds, 292 as two and 128 quarters).
             const uint32_t left = tiles[k] > CUS && tiles[k] % CUS <= 3 * CUS / 8 ? tiles[k] % CUS : 0;
-            tiled_kernel<PHASE, large_tile><<<tiles[k] - left, 512, 0, s>>>(g);
+            tiled_kernel<PHASE, large_tile<MUL>><<<tiles[k] - left, 512, 0, s>>>(g);
             if (left) {
                 muon_args q = g;
                 q.quarters = tiles[k] - left + 1;
-                tiled_kernel<PHASE, small_tile><<<4 * left, 256, 0, s>>>(q);
+                tiled_kernel<PHASE, small_tile<MUL>><<<4 * left, 256, 0, s>>>(q);
             }
         }
-        else if (k == SMALL) tiled_kernel<PHASE, small_tile><<<tiles[k], 256, 0, s>>>(g);
-        else if (tiles[k] <= CUS) direct_kernel<PHASE, 8><<<tiles[k], 512, 0, s>>>(g);
-        else direct_kernel<PHASE, 4><<<tiles[k], 256, 0, s>>>(g);
+        else if (k == SMALL) tiled_kernel<PHASE, small_tile<MUL>><<<tiles[k], 256, 0, s>>>(g);
+        else if (tiles[k] <= CUS) direct_kernel<PHASE, MUL, 8><<<tiles[k], 512, 0, s>>>(g);
+        else direct_kernel<PHASE, MUL, 4><<<tiles[k], 256, 0, s>>>(g);
     }
+}
+
+template <int PHASE>
+void launch_phase(const muon_args& g, const head& h, hipStream_t s) {
+    if (g.both) launch_phase_of<PHASE, of_pairs>(g, h, s);
+    else launch_phase_of<PHASE, of_f16>(g, h, s);
 }
 
 uint64_t tiles_of(const gd_muon_tensor& t, uint64_t edge) { return ((t.rows + edge - 1) / edge) * ((t.cols + edge - 1) / edge); }
 
-// Which tiles the matrices take.  Tiles of 256 x 256 where they fill the chip (24 of 1 024 x 1 024, 384: 2.20 ms, with
-// tiles of 128 x 128 2.36; 4 of 2 048 x 2 048, 256: 2.46 and 2.84; 8 of 1 024 x 1 024, 128: 1.17 and 0.89) and are not mostly empty; else
-// tiles of 128 x 128 where those of 64 x 64 would be two rounds of the chip and more (64 of 256 x 256, 1 024: 0.32 and 0.35; 8 of 1 024 x
-// 1 024, 2 048: 0.89 and 1.06; 8 of 333 x 500, 384: 0.32 and 0.19) of matrices that are not long, whose products over the long side are few
-// tiles of many blocks (4 of 512 x 2 048, 1 024: 0.57 and 0.35; 2 of 1 024 x 4 096, 2 048: 1.15 and 0.98).
+// Which tiles the matrices take.  Tiles of 256 x 256 where they fill the chip (1 of 4 096 x 4 096, 256: 3.96 ms, with tiles of 128 x 128
+// 4.29; 4 of 2 048 x 2 048, 256: 2.27 and 2.33; 8 of 1 024 x 1 024, 128: 1.10 and 0.80) and are not mostly empty; else tiles of 128 x 128
+// where those of 64 x 64 would be two rounds of the chip and more (64 of 256 x 256, 1 024: 0.30 and 0.33; 8 of 1 024 x 1 024, 2 048: 0.80 and
+// 0.87; 8 of 333 x 500, 384: 0.26 and 0.17) of matrices that are not long, whose products over the long side are few tiles of many blocks (4 of
+// 512 x 2 048, 1 024: 0.45 and 0.32; 2 of 1 024 x 4 096, 2 048: 0.86 and 0.79).
 void choose_kinds(const gd_muon_tensor* t, uint32_t n, std::vector<int>& kinds) {
     kinds.assign(n, DIRECT);
     auto side = [&](uint32_t i) { return std::min(t[i].rows, t[i].cols); };

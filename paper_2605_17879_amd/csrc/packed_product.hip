@@ -270,7 +270,7 @@ hipError_t gd_launch_packed_product(const gd_packed_product_args& g, hipStream_t
     const uint32_t row = up(g.k, 16) * 16;
     a.p = operand{static_cast<const uint8_t*>(g.b), g.m > 1 ? g.b_stride : row, g.m, row, g.b_exp, g.b_exp_stride};
     a.q = operand{static_cast<const uint8_t*>(g.a), g.n > 1 ? g.a_stride : row, g.n, row, g.a_exp, g.a_exp_stride};
-    a.way.blocks = up(g.k, BYTES); a.way.parts = 1; a.way.ends = g.k % BYTES;
+    a.way.blocks = up(g.k, BYTES); a.way.ends = g.k % BYTES;
     a.slab = reinterpret_cast<float*>(g.work);
     a.m4 = (uint32_t)(gd_align256(g.m * 4ull) / 4);
     const plan w = plan_of(g.n, g.m, g.k, g.out_type == GD_F32);

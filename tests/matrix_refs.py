@@ -74,11 +74,11 @@ def product(a, b, dtype, old=None):
 
 
 def _digits(x, kept, one):
-    """x rounded as numbers of f16 times 1 / one: hi alone, or hi + 2^-11 lo."""
+    """x rounded as numbers of f16 times 1 / one: hi alone, or hi + lo."""
     x = x * one
     hi = x.to(torch.float16).double()
     if kept == 2:
-        hi = hi + ((x - hi) * 2.0 ** 11).to(torch.float16).double() * 2.0 ** -11
+        hi = hi + (x - hi).to(torch.float16).double()
     return hi / one
 
 
