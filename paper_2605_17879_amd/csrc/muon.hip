@@ -57,14 +57,18 @@ struct head {
     uint64_t bytes;
     uint32_t magic, n;
     uint32_t first[KINDS + 1];    // entries of a kind of tiles; behind the last one's lie the tiny ones
-    uint32_t half[KINDS], full[KINDS];   // tiles of a symmetric product, and of the others
+    uint32_t share[KINDS][2][8];  // tiles of a symmetric product, and of the others, that each XCD takes
+    uint32_t most[KINDS][2];      // that an XCD takes
+    uint32_t whole[3];            // of the large ones, what an XCD takes as such of X X^T, A A^T and the others; the rest is taken as quarters
     uint32_t chunks, tiles;       // pieces of all matrices, and 64 x 64 of them
     uint64_t work[2];
 };
 constexpr uint32_t MAGIC = 0x6D756F6E;
-enum { OF_CHUNKS, OF_TILES, OF_HALF, OF_FULL, LISTS };   // lists of what begins where, one number an entry
+// Lists of one number an entry: what begins where, and for each XCD, of the tiles of symmetric products and then of the others, where an
+// entry's begin, and what added to a place makes the tile of the entry's own.
+enum { OF_CHUNKS, OF_TILES, OF_SHARES, LISTS = OF_SHARES + 2 * 8 * 2 };
 
-constexpr uint64_t HEAD = 256;
+constexpr uint64_t HEAD = 512;
 static_assert(sizeof(head) <= HEAD, "the table's head");
 
 __host__ __device__ inline uint64_t up_to(uint64_t v, uint64_t unit) { return (v + unit - 1) / unit * unit; }
@@ -121,7 +125,8 @@ struct muon_args {
     uint64_t mark;
     uint32_t n, tiled;            // entries, those that are not tiny
     uint32_t first, count;        // entries of the launch's kind
-    uint32_t quarters;            // of tiles of 256 x 256: the launch takes quarters of these, from this one on, plus 1; 0: no quarters
+    uint32_t kind;                // of tiles
+    uint32_t quarters;            // of tiles of 256 x 256: the launch takes quarters of an XCD's, from this one on, plus 1; 0: no quarters
     uint8_t* work;
     const float* grad_scale;
     uint32_t both;                // products of f32
@@ -144,8 +149,8 @@ __device__ __forceinline__ entry entry_at(const muon_args& g, uint32_t i) {
     return __builtin_bit_cast(entry, x);
 }
 
-// Which of `count` entries from `first` on has number t of a list, t less where it begins: the last that does not begin behind it.
-__device__ __forceinline__ uint32_t find(const muon_args& g, int list, uint32_t first, uint32_t count, uint32_t& t) {
+// Which of `count` entries from `first` on has place t of a list: the last that does not begin behind it.
+__device__ __forceinline__ uint32_t entry_of(const muon_args& g, int list, uint32_t first, uint32_t count, uint32_t t) {
     const uint32_t* at = reinterpret_cast<const uint32_t*>(g.table + list_at(g.n, list)) + first;
     const uint32_t lane = threadIdx.x & 63;
     uint32_t before = 0;
@@ -154,9 +159,16 @@ __device__ __forceinline__ uint32_t find(const muon_args& g, int list, uint32_t 
         before += (uint32_t)__popcll(begun);
         if (begun != ~0ull) break;
     }
-    const uint32_t k = __builtin_amdgcn_readfirstlane(before - 1);
-    t -= __builtin_amdgcn_readfirstlane(at[k]);
-    return first + k;
+    return first + __builtin_amdgcn_readfirstlane(before - 1);
+}
+__device__ __forceinline__ uint32_t number_at(const muon_args& g, int list, uint32_t k) {
+    return __builtin_amdgcn_readfirstlane(reinterpret_cast<const uint32_t*>(g.table + list_at(g.n, list))[k]);
+}
+// t becomes the number of the entry's own.
+__device__ __forceinline__ uint32_t find(const muon_args& g, int list, uint32_t& t) {
+    const uint32_t k = entry_of(g, list, 0, g.tiled, t);
+    t -= number_at(g, list, k);
+    return k;
 }
 
 // Whether there is something to do: the table is the one that the launch was made for, the gradients' factor (in f) is finite.
@@ -212,7 +224,7 @@ __global__ __launch_bounds__(512) void momentum_kernel(const muon_args g) {
     float f;
     if (!begins(g, f)) return;
     uint32_t t = blockIdx.x;
-    const entry e = entry_at(g, find(g, OF_CHUNKS, 0, g.tiled, t));
+    const entry e = entry_at(g, find(g, OF_CHUNKS, t));
     const uint64_t size = (uint64_t)e.rows * e.cols, from = (uint64_t)t * e.chunk, end = min(from + e.chunk, size);
     double s = 0;
     uint64_t i = from + threadIdx.x * 8;
@@ -276,7 +288,7 @@ __global__ __launch_bounds__(256) void start_kernel(const muon_args g) {
     float f;
     if (!begins(g, f)) return;
     uint32_t t = blockIdx.x;
-    const entry e = entry_at(g, find(g, OF_TILES, 0, g.tiled, t));
+    const entry e = entry_at(g, find(g, OF_TILES, t));
     const double* part = reinterpret_cast<const double*>(g.work) + e.partial;
     double s = 0;
     for (uint32_t i = threadIdx.x; i < e.chunks; i += 256) s += part[i];
@@ -495,13 +507,19 @@ __device__ __forceinline__ void corner_of(uint32_t t, uint32_t& tp, uint32_t& tq
 template <int PHASE>
 __device__ __forceinline__ bool place_of(const muon_args& g, uint32_t edge, uint32_t& tp, uint32_t& tq, entry& e) {
     constexpr bool HALF = PHASE == OF_X || PHASE == OF_A;
-    uint32_t t = stretch_of(blockIdx.x, gridDim.x);
+    // (workgroup b is on XCD b % 8)
+    const uint32_t chip = blockIdx.x % 8;
+    const int list = OF_SHARES + ((HALF ? 0 : 8) + (int)chip) * 2;
+    uint32_t t = blockIdx.x / 8;
     const uint32_t quarter = t % 4;
     if (g.quarters) {
         t = g.quarters - 1 + t / 4;
         edge = 256;
     }
-    e = entry_at(g, find(g, HALF ? OF_HALF : OF_FULL, g.first, g.count, t));
+    if (t >= reinterpret_cast<const head*>(g.table)->share[g.kind][!HALF][chip]) return false;
+    const uint32_t k = entry_of(g, list, g.first, g.count, t);
+    t += number_at(g, list + 1, k);
+    e = entry_at(g, k);
     if (HALF) corner_of(t, tq, tp);                // (columns at or behind the rows)
     else tile_of<4>(t, (e.cols + edge - 1) / edge, (e.rows + edge - 1) / edge, tp, tq);
     if (!g.quarters) return true;
@@ -557,7 +575,7 @@ __global__ __launch_bounds__(64 * WAVES, 8 / WAVES) void direct_kernel(const muo
     if (!begins(g, f)) return;
     uint32_t tp, tq;
     entry e;
-    place_of<PHASE>(g, 64, tp, tq, e);
+    if (!place_of<PHASE>(g, 64, tp, tq, e)) return;
     const problem x = problem_of<PHASE>(g, e, tp != tq);
     f32x4 v[4];
     const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
@@ -589,7 +607,7 @@ __global__ __launch_bounds__(256) void apply_kernel(const muon_args g) {
     float f;
     if (!begins(g, f)) return;
     uint32_t t = blockIdx.x;
-    const entry e = entry_at(g, find(g, OF_TILES, 0, g.tiled, t));
+    const entry e = entry_at(g, find(g, OF_TILES, t));
     const layout l(e.rows, e.cols, g.both);
     const uint8_t* base = g.work + e.at[!g.both] + l.r_at(0);
     const uint32_t tiles_c = (e.cols + 63) / 64, row = t / tiles_c * 64 + threadIdx.x / 4, col = t % tiles_c * 64 + threadIdx.x % 4 * 16;
@@ -835,25 +853,24 @@ __global__ __launch_bounds__(TINY_NT) void tiny_kernel(const muon_args g, const 
 
 template <int PHASE, typename MUL>
 void launch_phase_of(muon_args g, const head& h, hipStream_t s) {
-    const uint32_t* tiles = PHASE == OF_X || PHASE == OF_A ? h.half : h.full;
     for (int k = 0; k < KINDS; ++k) {
-        if (!tiles[k]) continue;
+        const uint32_t most = h.most[k][PHASE == OF_X || PHASE == OF_A ? 0 : 1];
+        if (!most) continue;
         g.first = h.first[k];
         g.count = h.first[k + 1] - h.first[k];
+        g.kind = (uint32_t)k;
         if (k == LARGE) {
-            // Whole rounds of the chip's 256 workgroups; what is left, if it is little, as quarters, which are less than a round of
-            // tiles of 128 x 128 (4 of 4 096 x 4 096, X X^T 544 tiles: 315 us as three rounds, 292 as two and 128 quarters).
-            const uint32_t left = tiles[k] > CUS && tiles[k] % CUS <= 3 * CUS / 8 ? tiles[k] % CUS : 0;
-            tiled_kernel<PHASE, large_tile<MUL>><<<tiles[k] - left, 512, 0, s>>>(g);
-            if (left) {
-                muon_args q = g;
-                q.quarters = tiles[k] - left + 1;
-                tiled_kernel<PHASE, small_tile<MUL>><<<4 * left, 256, 0, s>>>(q);
+            const uint32_t whole = h.whole[PHASE == OF_X ? 0 : PHASE == OF_A ? 1 : 2];
+            if (whole) tiled_kernel<PHASE, large_tile<MUL>><<<8 * whole, 512, 0, s>>>(g);
+            if (whole < most) {
+                g.quarters = whole + 1;
+                tiled_kernel<PHASE, small_tile<MUL>><<<8 * 4 * (most - whole), 256, 0, s>>>(g);
+                g.quarters = 0;
             }
         }
-        else if (k == SMALL) tiled_kernel<PHASE, small_tile<MUL>><<<tiles[k], 256, 0, s>>>(g);
-        else if (tiles[k] <= CUS) direct_kernel<PHASE, MUL, 8><<<tiles[k], 512, 0, s>>>(g);
-        else direct_kernel<PHASE, MUL, 4><<<tiles[k], 256, 0, s>>>(g);
+        else if (k == SMALL) tiled_kernel<PHASE, small_tile<MUL>><<<8 * most, 256, 0, s>>>(g);
+        else if (8 * most <= CUS) direct_kernel<PHASE, MUL, 8><<<8 * most, 512, 0, s>>>(g);
+        else direct_kernel<PHASE, MUL, 4><<<8 * most, 256, 0, s>>>(g);
     }
 }
 
@@ -884,6 +901,91 @@ void choose_kinds(const gd_muon_tensor* t, uint32_t n, std::vector<int>& kinds) 
         else if (side(i) > 64) direct += tiles_of(t[i], 64);
     for (uint32_t i = 0; i < n; ++i)
         if (kinds[i] == DIRECT && side(i) > 64 && direct >= 1024 && std::max(t[i].rows, t[i].cols) < 3 * side(i)) kinds[i] = SMALL;
+}
+
+int bits_of(uint64_t v) { return v ? 64 - __builtin_clzll(v) : 0; }
+
+// A kind's matrices, and for the tiles of symmetric products and for the others what each XCD takes of them.
+struct dealt {
+    std::vector<uint32_t> order;
+    std::vector<uint32_t> begins[2][8], shift[2][8];
+    uint32_t share[2][8] = {};
+};
+
+// Each XCD takes a stretch of the tiles of all matrices alike in the bits of their sides, those with the longer ones first: as much work
+// as the others, and rows that it has in its L2 (2 of 4 096 x 4 096, 4 of 4 096 x 1 024 and 4 of 1 024 x
+// 1 024: 8.3 ms; eighths of the list as the caller has it, with all the long ones on one half of the chip: 9.4).
+void deal_out(const gd_muon_tensor* t, uint64_t edge, dealt& d) {
+    auto a = [&](uint32_t i) { return std::min(t[i].rows, t[i].cols); };
+    auto b = [&](uint32_t i) { return std::max(t[i].rows, t[i].cols); };
+    auto like = [&](uint32_t i) { return bits_of(a(i)) * 64 + bits_of(b(i)); };
+    std::stable_sort(d.order.begin(), d.order.end(), [&](uint32_t x, uint32_t y) { return like(x) > like(y); });
+    for (int full = 0; full < 2; ++full) {
+        double load[8] = {};
+        auto tiles = [&](uint32_t i) {
+            const uint64_t ta = (a(i) + edge - 1) / edge, tb = (b(i) + edge - 1) / edge;
+            return full ? ta * tb : ta * (ta + 1) / 2;
+        };
+        size_t end;
+        for (size_t begin = 0; begin < d.order.size(); begin = end) {
+            uint64_t all = 0;
+            for (end = begin; end < d.order.size() && like(d.order[end]) == like(d.order[begin]); ++end) all += tiles(d.order[end]);
+            // (what an eighth leaves goes where there is the least so far)
+            int chips[8] = {0, 1, 2, 3, 4, 5, 6, 7};
+            std::stable_sort(chips, chips + 8, [&](int x, int y) { return load[x] < load[y]; });
+            uint64_t from[9] = {}, behind = 0;
+            for (uint64_t r = 0; r < 8; ++r) from[chips[r] + 1] = all / 8 + (r < all % 8);
+            for (int x = 0; x < 8; ++x) {
+                load[x] += (double)from[x + 1] * (double)(full ? a(d.order[begin]) : a(d.order[begin]) + b(d.order[begin]));
+                from[x + 1] += from[x];
+            }
+            for (size_t k = begin; k < end; ++k) {
+                const uint64_t here = tiles(d.order[k]);
+                for (int x = 0; x < 8; ++x) {
+                    const uint64_t first = std::max(behind, from[x]), last = std::min(behind + here, from[x + 1]);
+                    d.begins[full][x].push_back(d.share[full][x]);
+                    d.shift[full][x].push_back((uint32_t)(first - behind) - d.share[full][x]);
+                    if (last > first) d.share[full][x] += (uint32_t)(last - first);
+                }
+                behind += here;
+            }
+        }
+    }
+}
+
+// Tiles of 256 x 256 that have a k of `cost`, with what their ends take; quarters of them that are there.
+struct large_tiles {
+    double cost;
+    uint64_t tiles, quarters;
+};
+
+// How many of a launch's large tiles are taken as such, a multiple of 256; UINT64_MAX: all.  One a CU, or two quarters: a round of those takes 0.6 of the time, 0.35 if there
+// is but one for a CU.  All tiles, whole rounds and the rest as quarters, or quarters alone: what is a tenth faster by that count (12 of 2 048 x
+// 1 024, X X^T and A A^T of 120 tiles as 432 quarters, the others of 384 as 256 and 512 quarters: 2.07 ms -> 1.72; 4 of 4 096 x 4 096, X X^T, 544: 315 us as three rounds, 292 as two and 128 quarters).
+uint64_t whole_of(std::vector<large_tiles> list) {
+    std::stable_sort(list.begin(), list.end(), [](const large_tiles& x, const large_tiles& y) { return x.cost > y.cost; });
+    uint64_t all = 0;
+    for (const auto& l : list) all += l.tiles;
+    auto time = [&](uint64_t whole) {
+        double sum = 0, last = 0;
+        uint64_t at = 0, quarters = 0;
+        for (const auto& l : list) {
+            const uint64_t w = std::min(l.tiles, whole - std::min(whole, at));
+            sum += l.cost * (double)((at + w + CUS - 1) / CUS - (at + CUS - 1) / CUS);
+            at += w;
+            if (w == l.tiles) continue;
+            const uint64_t q = l.quarters - l.quarters * w / l.tiles;
+            sum += 0.6 * l.cost * (double)((quarters + q + 2 * CUS - 1) / (2 * CUS) - (quarters + 2 * CUS - 1) / (2 * CUS));
+            if (quarters / (2 * CUS) != (quarters + q) / (2 * CUS) || quarters % (2 * CUS) == 0) last = l.cost;
+            quarters += q;
+        }
+        if (quarters % (2 * CUS) != 0 && quarters % (2 * CUS) <= CUS) sum -= 0.25 * last;
+        return sum;
+    };
+    uint64_t best = all;
+    for (uint64_t whole : {all / CUS * CUS, (uint64_t)0})
+        if (time(whole) < (best == all ? 0.9 : 1.0) * time(best)) best = whole;
+    return best == all ? UINT64_MAX : best;
 }
 
 // The largest magnitude of a polynomial c1 x + c3 x^3 + c5 x^5, and of b x^2 + c x^4, over [0, s].
@@ -921,13 +1023,13 @@ uint64_t mark_of(const uint8_t* p, size_t n) {
 }  // namespace
 
 size_t gd_muon_table(const gd_muon_tensor* t, uint32_t n, void* out) {
-    std::vector<uint32_t> order[KINDS + 1];
+    dealt of[KINDS + 1];
     std::vector<int> kinds;
     choose_kinds(t, n, kinds);
     uint32_t there = 0;
     for (uint32_t i = 0; i < n; ++i)
         if (t[i].rows && t[i].cols) {
-            order[kinds[i]].push_back(i);
+            of[kinds[i]].order.push_back(i);
             ++there;
         }
     const size_t bytes = gd_align256(list_at(there, LISTS));
@@ -943,12 +1045,21 @@ size_t gd_muon_table(const gd_muon_tensor* t, uint32_t n, void* out) {
     for (uint32_t i = 0; i < n; ++i) chunks += (t[i].rows * t[i].cols + CHUNK - 1) / CHUNK;   // (an upper bound)
     work[0] = work[1] = gd_align256(std::min<uint64_t>(chunks, (uint64_t)there * CHUNKS) * 8);
     chunks = 0;
+    std::vector<large_tiles> large[3];
     for (int kind = 0; kind <= KINDS; ++kind) {
         uint64_t half = 0, full = 0;
         h.first[kind] = k;
-        for (uint32_t i : order[kind]) {
+        for (uint32_t i : of[kind].order) {
+            const uint64_t edge = std::max(EDGE[kind], 1u), tr = (t[i].rows + edge - 1) / edge, tc = (t[i].cols + edge - 1) / edge, ta = std::min(tr, tc);
+            half += ta * (ta + 1) / 2;
+            full += tr * tc;
+        }
+        // (launches of fewer than 2^32 threads)
+        if (kind != TINY && (half >= 1u << 23 || full >= 1u << 23)) return 0;
+        if (kind != TINY) deal_out(t, EDGE[kind], of[kind]);
+        for (uint32_t i : of[kind].order) {
             const gd_muon_tensor& x = t[i];
-            const uint64_t size = x.rows * x.cols, edge = std::max(EDGE[kind], 1u);
+            const uint64_t size = x.rows * x.cols;
             entry e = {};
             e.param = x.d_param; e.grad = x.d_grad; e.m = static_cast<float*>(x.d_m); e.copy = x.d_copy;
             e.lr_scale = x.lr_scale; e.decay = x.weight_decay;
@@ -957,28 +1068,45 @@ size_t gd_muon_table(const gd_muon_tensor* t, uint32_t n, void* out) {
             e.chunk = (uint32_t)up_to((size + CHUNKS - 1) / CHUNKS, CHUNK);
             e.chunks = (uint32_t)((size + e.chunk - 1) / e.chunk);
             e.partial = (uint32_t)chunks;
-            const uint64_t tr = (x.rows + edge - 1) / edge, tc = (x.cols + edge - 1) / edge, ta = std::min(tr, tc);
             if (to) {
-                const uint32_t begins[LISTS] = {(uint32_t)chunks, (uint32_t)tiles, (uint32_t)half, (uint32_t)full};
                 for (int b = 0; b < 2; ++b) e.at[b] = work[b];
                 memcpy(to + HEAD + k * sizeof(entry), &e, sizeof(e));
-                for (int b = 0; b < LISTS; ++b) memcpy(to + list_at(there, b) + 4ull * k, &begins[b], 4);
+                auto note = [&](int list, uint64_t v) {
+                    const uint32_t number = (uint32_t)v;
+                    memcpy(to + list_at(there, list) + 4ull * k, &number, 4);
+                };
+                note(OF_CHUNKS, chunks);
+                note(OF_TILES, tiles);
+                for (int l = 0; l < 16 && kind != TINY; ++l) {
+                    note(OF_SHARES + 2 * l, of[kind].begins[l / 8][l % 8][k - h.first[kind]]);
+                    note(OF_SHARES + 2 * l + 1, of[kind].shift[l / 8][l % 8][k - h.first[kind]]);
+                }
             }
             ++k;
             if (kind == TINY) continue;
             for (int b = 0; b < 2; ++b) work[b] += layout(e.rows, e.cols, b == 0).total;
             chunks += e.chunks;
             tiles += ((x.rows + 63) / 64) * ((x.cols + 63) / 64);
-            half += ta * (ta + 1) / 2;
-            full += tr * tc;
+            if (kind == LARGE) {
+                // (a tile's ends take as long as 800 of k)
+                const uint64_t tr = (x.rows + 255) / 256, tc = (x.cols + 255) / 256, ta = std::min(tr, tc);
+                const uint64_t qr = (x.rows + 127) / 128, qc = (x.cols + 127) / 128, qa = std::min(qr, qc);
+                const double k_x = 800.0 + (double)std::max(x.rows, x.cols), k_a = 800.0 + (double)std::min(x.rows, x.cols);
+                large[0].push_back({k_x, ta * (ta + 1) / 2, qa * (qa + 1) / 2});
+                large[1].push_back({k_a, ta * (ta + 1) / 2, qa * (qa + 1) / 2});
+                large[2].push_back({k_a, tr * tc, qr * qc});
+            }
         }
-        // (launches of fewer than 2^32 threads)
-        if (half >= 1u << 23 || full >= 1u << 23 || k >= 1u << 22) return 0;
+        if (k >= 1u << 22) return 0;
         if (kind == TINY) break;
-        h.half[kind] = (uint32_t)half;
-        h.full[kind] = (uint32_t)full;
+        memcpy(h.share[kind], of[kind].share, sizeof(h.share[kind]));
+        for (int l = 0; l < 2; ++l) h.most[kind][l] = *std::max_element(h.share[kind][l], h.share[kind][l] + 8);
     }
     if (chunks >= 1u << 23 || tiles >= 1u << 24) return 0;
+    for (int phase = 0; phase < 3; ++phase) {
+        const uint32_t most = h.most[LARGE][phase == 2];
+        h.whole[phase] = (uint32_t)std::min<uint64_t>(most, whole_of(large[phase]) / 8);
+    }
     h.chunks = (uint32_t)chunks;
     h.tiles = (uint32_t)tiles;
     h.work[0] = work[0];
