@@ -185,6 +185,20 @@ def test_tiles_that_are_left_over(det, count, rows, cols):
             assert float(torch.linalg.matrix_norm(-p.double() - exact)) <= bound
 
 
+@pytest.mark.parametrize("products", ["f32", "f16"])
+def test_matrices_of_many_sizes_in_one_update(det, products):
+    """Sizes that share a launch are dealt out to the parts of the chip each by itself: large ones whose symmetric products are taken in
+    quarters, some of whose tiles lie outside, and numbers of tiles that no eighth divides."""
+    shapes = [(1030, 1100), (2300, 1100), (300, 260), (600, 4200), (130, 70), (2300, 1100), (1030, 1100), (600, 4200), (2300, 1100), (300, 260),
+              (2300, 1100), (1100, 2300), (600, 4200), (1025, 1025), (4200, 600), (2300, 1100)]
+    pairs = {s: (low_rank(*s, 1) * 1e-3, low_rank(*s, 4) * 1e-2) for s in set(shapes)}
+    params, _, _ = run_muon(det, [pairs[s] for s in shapes], products, eps=0.0)
+    bounds = {s: refs.orthogonal_bound(update_of(*pairs[s])[1].cuda(), products, eps=0.0) for s in pairs}
+    for s, p in zip(shapes, params):
+        exact, bound = bounds[s]
+        assert float(torch.linalg.matrix_norm(-p.double() - exact)) <= bound, s
+
+
 def test_an_update_behind_a_table_whose_lists_the_caller_drops(det):
     """The table keeps the memory of its tensors."""
     mats = [(low_rank(70, 90, 1), low_rank(70, 90, 2))]
