@@ -59,7 +59,7 @@ struct head {
     uint32_t first[KINDS + 1];    // entries of a kind of tiles; behind the last one's lie the tiny ones
     uint32_t share[KINDS][2][8];  // tiles of a symmetric product, and of the others, that each XCD takes
     uint32_t most[KINDS][2];      // that an XCD takes
-    uint32_t whole[3];            // of the large ones, what an XCD takes as such of X X^T, A A^T and the others; the rest is taken as quarters
+    uint32_t whole[3];            // of the large ones, what an XCD takes as such of X X^T, A A^T and the others; the rest is taken in parts
     uint32_t chunks, tiles;       // pieces of all matrices, and 64 x 64 of them
     uint64_t work[2];
 };
@@ -126,7 +126,7 @@ struct muon_args {
     uint32_t n, tiled;            // entries, those that are not tiny
     uint32_t first, count;        // entries of the launch's kind
     uint32_t kind;                // of tiles
-    uint32_t quarters;            // of tiles of 256 x 256: the launch takes quarters of an XCD's, from this one on, plus 1; 0: no quarters
+    uint32_t parts;               // of tiles of 256 x 256: the launch takes its own tiles of an XCD's, from this one on, plus 1; 0: of its kind
     uint8_t* work;
     const float* grad_scale;
     uint32_t both;                // products of f32
@@ -511,9 +511,9 @@ __device__ __forceinline__ bool place_of(const muon_args& g, uint32_t edge, uint
     const uint32_t chip = blockIdx.x % 8;
     const int list = OF_SHARES + ((HALF ? 0 : 8) + (int)chip) * 2;
     uint32_t t = blockIdx.x / 8;
-    const uint32_t quarter = t % 4;
-    if (g.quarters) {
-        t = g.quarters - 1 + t / 4;
+    const uint32_t cut = g.parts ? 256 / edge : 1, part = t % (cut * cut), own = edge;
+    if (g.parts) {
+        t = g.parts - 1 + t / (cut * cut);
         edge = 256;
     }
     if (t >= reinterpret_cast<const head*>(g.table)->share[g.kind][!HALF][chip]) return false;
@@ -522,11 +522,11 @@ __device__ __forceinline__ bool place_of(const muon_args& g, uint32_t edge, uint
     e = entry_at(g, k);
     if (HALF) corner_of(t, tq, tp);                // (columns at or behind the rows)
     else tile_of<4>(t, (e.cols + edge - 1) / edge, (e.rows + edge - 1) / edge, tp, tq);
-    if (!g.quarters) return true;
-    tp = 2 * tp + quarter % 2;
-    tq = 2 * tq + quarter / 2;
+    if (!g.parts) return true;
+    tp = cut * tp + part % cut;
+    tq = cut * tq + part / cut;
     const uint32_t a = min(e.rows, e.cols);
-    return (HALF ? tp >= tq : true) && tq * 128 < (HALF ? a : e.rows) && tp * 128 < (HALF ? a : e.cols);
+    return (HALF ? tp >= tq : true) && tq * own < (HALF ? a : e.rows) && tp * own < (HALF ? a : e.cols);
 }
 
 template <int PHASE, typename TILE>
@@ -863,9 +863,12 @@ void launch_phase_of(muon_args g, const head& h, hipStream_t s) {
             const uint32_t whole = h.whole[PHASE == OF_X ? 0 : PHASE == OF_A ? 1 : 2];
             if (whole) tiled_kernel<PHASE, large_tile<MUL>><<<8 * whole, 512, 0, s>>>(g);
             if (whole < most) {
-                g.quarters = whole + 1;
-                tiled_kernel<PHASE, small_tile<MUL>><<<8 * 4 * (most - whole), 256, 0, s>>>(g);
-                g.quarters = 0;
+                g.parts = whole + 1;
+                // (so few that two workgroups a CU take them as tiles of 64 x 64: of 4 096 x 4 352, 272 tiles, the last 16 as quarters 1.95 ms
+                // for all, so 1.79)
+                if (16 * 8 * (most - whole) <= 2 * CUS) direct_kernel<PHASE, MUL, 4><<<8 * 16 * (most - whole), 256, 0, s>>>(g);
+                else tiled_kernel<PHASE, small_tile<MUL>><<<8 * 4 * (most - whole), 256, 0, s>>>(g);
+                g.parts = 0;
             }
         }
         else if (k == SMALL) tiled_kernel<PHASE, small_tile<MUL>><<<8 * most, 256, 0, s>>>(g);
@@ -959,9 +962,10 @@ struct large_tiles {
     uint64_t tiles, quarters;
 };
 
-// How many of a launch's large tiles are taken as such, a multiple of 256; UINT64_MAX: all.  One a CU, or two quarters: a round of those takes 0.6 of the time, 0.35 if there
-// is but one for a CU.  All tiles, whole rounds and the rest as quarters, or quarters alone: what is a tenth faster by that count (12 of 2 048 x
-// 1 024, X X^T and A A^T of 120 tiles as 432 quarters, the others of 384 as 256 and 512 quarters: 2.07 ms -> 1.72; 4 of 4 096 x 4 096, X X^T, 544: 315 us as three rounds, 292 as two and 128 quarters).
+// How many of a launch's large tiles are taken as such, a multiple of 256; UINT64_MAX: all.  One a CU, or two quarters: a round of those
+// takes 0.6 of the time, 0.35 if there is but one for a CU.  All tiles, whole rounds and the rest in parts, or parts alone: what is a tenth
+// faster by that count (12 of 2 048 x 1 024, X X^T and A A^T of 120 tiles as 432 quarters, the others of 384 as 256 and 512 quarters: 2.07
+// ms -> 1.72; 4 of 4 096 x 4 096, X X^T, 544: 315 us as three rounds, 292 as two and 128 quarters).
 uint64_t whole_of(std::vector<large_tiles> list) {
     std::stable_sort(list.begin(), list.end(), [](const large_tiles& x, const large_tiles& y) { return x.cost > y.cost; });
     uint64_t all = 0;

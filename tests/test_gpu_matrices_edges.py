@@ -172,10 +172,10 @@ def test_long_lists_of_matrices_of_all_kinds(det, products):
         assert off <= bound, (tuple(gr.shape), off, bound)
 
 
-@pytest.mark.parametrize("count,rows,cols", [(4, 2100, 2100), (6, 2100, 2180), (3, 2177, 4400)])
+@pytest.mark.parametrize("count,rows,cols", [(4, 2100, 2100), (6, 2100, 2180), (3, 2177, 4400), (2, 2900, 3000)])
 def test_tiles_that_are_left_over(det, count, rows, cols):
-    """More large tiles than one round of the chip, the last ones taken in quarters: of the products (4: 324 tiles) and of the
-    symmetric ones (6: 270), wide and tall."""
+    """More large tiles than one round of the chip, the last ones taken in parts: of the products (4: 324 tiles in quarters, 2: 288 in
+    sixteenths) and of the symmetric ones (6: 270), wide and tall."""
     for shape in ((rows, cols), (cols, rows)):
         say(f"{count} of {shape}")
         g, m = low_rank(*shape, 1) * 1e-3, low_rank(*shape, 4) * 1e-2
