@@ -166,7 +166,7 @@ def test_products_of_middling_tiles(det, n, m, k, dtype):
 
 
 @pytest.mark.parametrize("dtype", [F32, F16])
-@pytest.mark.parametrize("n,m,k", [(4097, 3500, 17), (3600, 3700, 128), (3650, 3850, 264), (3585, 3585, 400)])
+@pytest.mark.parametrize("n,m,k", [(4097, 3500, 17), (3600, 3700, 128), (3650, 3850, 264), (3585, 3585, 400), (4300, 4250, 136)])
 def test_products_of_large_tiles(det, n, m, k, dtype):
     check_product(det, n, m, k, dtype, gap=1)
 
@@ -178,7 +178,7 @@ def test_products_of_other_codes(det, n, m, k, ca, cb):
         check_product(det, n, m, k, dtype, ca, cb)
 
 
-@pytest.mark.parametrize("n,m", [(3, 200), (200, 100), (2100, 2100), (3600, 3600)])
+@pytest.mark.parametrize("n,m", [(3, 200), (200, 100), (2100, 2100), (3600, 3600), (4300, 4250)])
 @pytest.mark.parametrize("dtype", [F32, BF16])
 def test_products_leave_out_what_is_not_theirs(det, n, m, dtype):
     """Bytes behind the rows' ends are codes of NaN, powers of two behind the rows are those of NaN; a NaN in a row stays in it."""
