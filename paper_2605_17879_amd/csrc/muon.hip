@@ -219,7 +219,8 @@ __device__ __forceinline__ double advance(const muon_args& g, const entry& e, ui
     return s;
 }
 
-// M, and the sums of squares of U, a piece a workgroup.
+// M, and the sums of squares of U, a piece a workgroup.  Memory bounds it: 4 of 4 096 x 4 096 with gradients in bf16, 671 MB, 112 us, 6.0 TB/s
+// (a part comes from the last level's cache).
 __global__ __launch_bounds__(512) void momentum_kernel(const muon_args g) {
     float f;
     if (!begins(g, f)) return;
@@ -283,7 +284,8 @@ __device__ __forceinline__ void updates_of(const muon_args& g, const entry& e, u
         }
 }
 
-// X of the first step, 64 x 64 a workgroup, both ways, with zeros up to the end of a block of k.
+// X of the first step, 64 x 64 a workgroup, both ways, with zeros up to the end of a block of k.  Memory bounds it: 4 of 4 096 x 4 096, 805
+// MB, 176 us, 4.6 TB/s.
 __global__ __launch_bounds__(256) void start_kernel(const muon_args g) {
     float f;
     if (!begins(g, f)) return;
@@ -624,7 +626,7 @@ __global__ __launch_bounds__(256) void apply_kernel(const muon_args g) {
 // A matrix of up to 64 x 192 (or 192 x 64), momentum to parameters: X as a lane holds it, in fp32, in registers, and as
 // operands in the LDS, hi and lo, both ways (R [i][j], C [j][i], i along the shorter side), A and B [i][i'].  A wave has pieces of 16 x 16 of a product: a
 // lane four neighbouring j of one i of X.  Five steps take 13 products one behind the other of some hundred cycles each; with the launches of
-// the larger matrices they took 6 to 8 us each (six of 64 x 96: 105 us).
+// the larger matrices they took 6 to 8 us each (six of 96 x 64: 105 us, so 24).
 struct tiny_lds {
     static constexpr uint32_t R = 2 * 2 * TINY_B, C = 2 * 2 * TINY_A, S = C;   // bytes of a row: hi, lo
     uint8_t r[TINY_A * R], c[TINY_B * C];
