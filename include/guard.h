@@ -622,7 +622,7 @@ typedef struct gd_muon_config {
 
 /* What the launches read about the matrices: gd_muon_table_bytes bytes (0 where the list is refused), written to host
  * memory by gd_muon_fill_table.  The caller copies them to the device once (256-byte aligned there) and keeps both as
- * long as the tensors stay where they are.  A list whose written arrays (params, momenta, copies) overlap is refused. */
+ * long as the tensors stay where they are.  A list whose written arrays (params, momenta, copies) overlap each other or a gradient is refused. */
 size_t gd_muon_table_bytes(gd_handle h, const gd_muon_tensor* tensors, uint32_t n_tensors);
 gd_status gd_muon_fill_table(gd_handle h, const gd_muon_tensor* tensors, uint32_t n_tensors, void* host_table, size_t bytes);
 /* Of the work area of an update with these products (256-byte aligned, nothing is kept in it between calls); 0 where the

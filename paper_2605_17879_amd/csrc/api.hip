@@ -191,7 +191,7 @@ constexpr uint64_t MAX_INNER = 1u << 22;    // of a packed product: rows of `acr
 // What is wrong with the matrices of an update, or null.
 const char* bad_matrices(const gd_muon_tensor* list, uint32_t n) {
     if (n && !list) return "null list of tensors";
-    std::vector<std::pair<uintptr_t, uintptr_t>> written;
+    std::vector<std::pair<uintptr_t, uintptr_t>> written, read;
     for (uint32_t i = 0; i < n; ++i) {
         const gd_muon_tensor& t = list[i];
         if (t.reserved != 0) return "reserved field of a tensor is not 0";
@@ -211,10 +211,15 @@ const char* bad_matrices(const gd_muon_tensor* list, uint32_t n) {
         writes(t.d_param, t.param_type);
         writes(t.d_m, GD_F32);
         writes(t.d_copy, t.copy_type);
+        read.emplace_back((uintptr_t)t.d_grad, (uintptr_t)t.d_grad + size * bytes_of(t.grad_type));
     }
     std::sort(written.begin(), written.end());
     for (size_t i = 1; i < written.size(); ++i)
         if (written[i].first < written[i - 1].second) return "tensors that are written overlap";
+    for (const auto& r : read) {
+        const auto next = std::lower_bound(written.begin(), written.end(), std::make_pair(r.second, (uintptr_t)0));   // the first that begins behind it
+        if (next != written.begin() && std::prev(next)->second > r.first) return "a gradient overlaps tensors that are written";
+    }
     return nullptr;
 }
 

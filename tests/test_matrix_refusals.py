@@ -99,6 +99,8 @@ def tensor(rows=10, cols=20, param=AT, grad=2 * AT, m=3 * AT, copy=None, rate=1.
     tensor(types=(I32, F32, BF16)), tensor(types=(F32, E4M3, BF16)), tensor(copy=4 * AT, types=(F32, F32, F32)), tensor(rows=65_537),
     tensor(cols=65_537), tensor(rate=float("nan")), tensor(decay=float("inf")), tensor(reserved=1),
     tensor(m=AT), tensor(m=AT + 4 * 199), tensor(copy=3 * AT + 8),                # (what is written overlaps)
+    tensor(grad=AT), tensor(grad=3 * AT), tensor(grad=3 * AT + 4 * 199), tensor(grad=3 * AT - 4 * 199), tensor(grad=7 * AT),   # (... a gradient)
+    tensor(copy=2 * AT + 16), tensor(copy=8 * AT),
 ])
 def test_matrices(lib, h, t):
     lst = (_CMuonTensor * 2)(tensor(param=7 * AT, grad=8 * AT, m=9 * AT), t)
