@@ -808,8 +808,8 @@ gd_status gd_pack(gd_handle h, const gd_matrix* x, int32_t square, const gd_pack
     if (across)
         if (const char* e = bad_packed(across, x->cols, x->rows)) return invalid(h, "gd_pack", e);
     if (along && across && along->codes.dtype != across->codes.dtype) return invalid(h, "gd_pack", "the outputs differ in type");
-    if (((x->rows + 127) / 128) * ((x->cols + 127) / 128) >= 1u << 24)      // (a launch has fewer than 2^32 threads)
-        return fail(h, GD_ERR_UNSUPPORTED, "gd_pack: 2^38 elements or more in one call are not built");
+    if (((x->rows + 127) / 128) * ((x->cols + 127) / 128) >= 1u << 23)      // (a launch has fewer than 2^32 threads)
+        return fail(h, GD_ERR_UNSUPPORTED, "gd_pack: 2^37 elements or more in one call are not built");
     gd_pack_args a = {};
     a.x = x->d_data; a.stride = x->stride;
     a.rows = (uint32_t)x->rows; a.cols = (uint32_t)x->cols; a.dtype = x->dtype; a.square = square != 0;

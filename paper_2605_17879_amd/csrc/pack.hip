@@ -7,17 +7,19 @@
 // so that the largest magnitude of a block lies in the upper half of the codes' range (MOST / 2, MOST], unless e is 1.  The
 // multiplication by a power of two is exact, so the code's rounding is the only one.
 //
-// The memory's streams bound it.  A workgroup takes 128 x 128: a lane 8 rows of 8 columns, which lie next to each other along
+// The memory's streams bound it.  A workgroup takes 128 x 128: a lane 4 rows of 8 columns, which lie next to each other along
 // both, in registers from the one read to the codes; the row's largest comes from 16 lanes by exchange, the column's
 // through the LDS, as do the transposed codes, which are written 16 bytes a lane.  16 384 x 4 096 of bf16 both ways, 271 MB: 50 us, 5.4 TB/s;
-// 5 003 x 3 001 of fp32, whose rows begin anywhere, squares: 17 to 19 us, 4.0 to 4.4 TB/s.
+// 5 003 x 3 001 of fp32, whose rows begin anywhere, squares: 16 to 18 us, 4.2 to 4.7 TB/s.  Where there are few of them it is how long one workgroup takes,
+// most of that its code's way from memory: 128 x 128 both ways 4.4 us, 6.0 with twice the rows a lane; 1 000 x 1 500 6.2, 8.0, and 10.2 where
+// the last numbers of a row were read and written one by one.
 #include <type_traits>
 
 #include "gd_operators.h"
 
 namespace {
 
-constexpr uint32_t EDGE = 128, NT = 256;
+constexpr uint32_t EDGE = 128, NT = 512, ROWS = 4, WAVES = NT / 64;     // (rows of a lane)
 
 typedef short s16x2 __attribute__((ext_vector_type(2)));
 typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
@@ -41,14 +43,10 @@ __device__ __forceinline__ s16x2 two_codes(s16x2 old, float2 x, float two) {
     if constexpr (E5M2) return __builtin_amdgcn_cvt_scalef32_pk_bf8_f32(old, x.x, x.y, two, HIGH);
     else return __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(old, x.x, x.y, two, HIGH);
 }
-template <bool E5M2, typename P>
-__device__ __forceinline__ uint2 eight_codes(P a, P b, P c, P d, uint32_t e) {
-    if (e == NONE) return make_uint2(NAN_CODES, NAN_CODES);
+template <bool E5M2, typename PAIR>
+__device__ __forceinline__ uint32_t four_codes(PAIR a, PAIR b, uint32_t e) {
     const float two = __builtin_bit_cast(float, e == 0 ? 0x3F800000u : e << 23);      // (zeros over anything)
-    const s16x2 none = {};
-    const s16x2 lo = two_codes<E5M2, true>(two_codes<E5M2, false>(none, a, two), b, two);
-    const s16x2 hi = two_codes<E5M2, true>(two_codes<E5M2, false>(none, c, two), d, two);
-    return make_uint2(__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, hi));
+    return e == NONE ? NAN_CODES : __builtin_bit_cast(uint32_t, two_codes<E5M2, true>(two_codes<E5M2, false>(s16x2{}, a, two), b, two));
 }
 
 // The exponent byte of a block whose largest magnitude has the bits `most`, of fp32.
@@ -81,6 +79,15 @@ template <typename T> struct eight {
 #pragma unroll
         for (uint32_t i = 0; i < 8; ++i)
             if (i < there) w[i / 2] |= (uint32_t)__builtin_bit_cast(uint16_t, p[i]) << (16 * (i % 2));
+    }
+    // Number i + gone becomes number i, zeros come from behind.
+    __device__ __forceinline__ void move_down(uint32_t gone) {
+#pragma unroll
+        for (int d = 2; d; d /= 2)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) w[i] = gone & (2 * d) ? (i + d < 4 ? w[i + d] : 0) : w[i];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = gone & 1 ? w[i] >> 16 | (i < 3 ? w[i + 1] << 16 : 0) : w[i];
     }
     __device__ __forceinline__ pair at(int i) const { return __builtin_bit_cast(pair, w[i]); }
     // number c of this and of the next row
@@ -118,6 +125,12 @@ template <> struct eight<float> {
         for (uint32_t i = 0; i < 8; ++i)
             if (i < there) x[i] = p[i];
     }
+    __device__ __forceinline__ void move_down(uint32_t gone) {
+#pragma unroll
+        for (int d = 4; d; d /= 2)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[i] = gone & d ? (i + d < 8 ? x[i + d] : 0.0f) : x[i];
+    }
     __device__ __forceinline__ pair at(int i) const { return make_float2(x[2 * i], x[2 * i + 1]); }
     static __device__ __forceinline__ pair below(const eight& a, const eight& b, int c) { return make_float2(a.x[c], b.x[c]); }
     struct sizes {
@@ -136,35 +149,60 @@ template <> struct eight<float> {
     };
 };
 
-// The bytes from `at` on of a row that has `there` more.
+// The first `there` bytes, fewer than all, eight, four, two and one at a time.
 template <int N>
-__device__ __forceinline__ void write_some(const uint32_t (&w)[N], uint8_t* at, uint32_t there) {
-#pragma unroll
-    for (int b = 0; b < 4 * N; ++b)
-        if ((uint32_t)b < there) at[b] = (uint8_t)(w[b / 4] >> (8 * (b % 4)));
+__device__ __forceinline__ void write_some(uint32_t (&&w)[N], uint8_t* at, uint32_t there) {
+    if (N == 4 && (there & 8)) {
+        __builtin_memcpy(at, &w[0], 8);
+        at += 8;
+        w[0] = w[N - 2];
+        w[1] = w[N - 1];
+    }
+    if (there & 4) {
+        __builtin_memcpy(at, &w[0], 4);
+        at += 4;
+        w[0] = w[1];
+    }
+    if (there & 2) {
+        __builtin_memcpy(at, &w[0], 2);
+        at += 2;
+        w[0] >>= 16;
+    }
+    if (there & 1) *at = (uint8_t)w[0];
 }
 
 template <typename T, bool E5M2>
 __global__ __launch_bounds__(NT, 4) void pack_kernel(const gd_pack_args a) {
-    __shared__ uint32_t most_of[EDGE][5];                        // a column's largest, by wave
+    __shared__ uint32_t most_of[EDGE][WAVES + 1];                // a column's largest, by wave
     __shared__ uint32_t exp_of[EDGE];
-    __shared__ __attribute__((aligned(16))) uint2 turned[EDGE][EDGE / 8 + 2];   // codes, transposed
+    __shared__ __attribute__((aligned(16))) uint32_t turned[EDGE][EDGE / 4 + 4];   // codes, transposed: column 8 t + c in row 16 c + t
     const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x / 64, tx = threadIdx.x % 16, ty = threadIdx.x / 16;
     const uint32_t tiles_c = (a.cols + EDGE - 1) / EDGE, tile_r = blockIdx.x / tiles_c, tile_c = blockIdx.x % tiles_c;
-    const uint32_t row0 = tile_r * EDGE + ty * 8, col0 = tile_c * EDGE + tx * 8;
+    const uint32_t row0 = tile_r * EDGE + ty * ROWS, col0 = tile_c * EDGE + tx * 8;
     const T* x = static_cast<const T*>(a.x) + row0 * a.stride + col0;
     const bool whole = col0 + 8 <= a.cols;
-    eight<T> v[8] = {};
+    eight<T> v[ROWS] = {};
+    // (of a row's last numbers, where they are not eight, the eight that end with them)
+    const uint32_t gone = whole ? 0 : col0 + 8 - a.cols;
+    if (a.cols >= 8) {
+        if (gone < 8) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j)
-        if (row0 + j < a.rows) {
-            if (whole) v[j].load(x + j * a.stride);
-            else if (col0 < a.cols) v[j].load_some(x + j * a.stride, a.cols - col0);
+            for (int j = 0; j < ROWS; ++j)
+                if (row0 + j < a.rows) v[j].load(x + j * a.stride - gone);
         }
-    uint32_t row_most[8];
+        if (gone) {
+#pragma unroll
+            for (int j = 0; j < ROWS; ++j) v[j].move_down(gone);
+        }
+    } else if (col0 == 0) {
+#pragma unroll
+        for (int j = 0; j < ROWS; ++j)
+            if (row0 + j < a.rows) v[j].load_some(x + j * a.stride, a.cols);
+    }
+    uint32_t row_most[ROWS];
     typename eight<T>::sizes columns = {};
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
+    for (int j = 0; j < ROWS; ++j) {
         typename eight<T>::sizes row = {};
         row.take(v[j]);
         row_most[j] = row.most();
@@ -174,19 +212,20 @@ __global__ __launch_bounds__(NT, 4) void pack_kernel(const gd_pack_args a) {
     if (a.square) {
         uint32_t m = 0;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) m = max(m, row_most[j]);
+        for (int j = 0; j < ROWS; ++j) m = max(m, row_most[j]);
         m = most_of_sixteen(m);
         m = max(m, (uint32_t)__shfl_xor((int)m, 16));
         m = max(m, (uint32_t)__shfl_xor((int)m, 32));
         if (lane == 0) most_of[0][wave] = m;
         __syncthreads();
-        square_most = max(max(most_of[0][0], most_of[0][1]), max(most_of[0][2], most_of[0][3]));
+#pragma unroll
+        for (uint32_t w = 0; w < WAVES; ++w) square_most = max(square_most, most_of[0][w]);
     }
     if (a.along.codes) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
+        for (int j = 0; j < ROWS; ++j) {
             const uint32_t e = exponent<E5M2>(a.square ? square_most : most_of_sixteen(row_most[j])), row = row0 + j;
-            const uint2 w = eight_codes<E5M2>(v[j].at(0), v[j].at(1), v[j].at(2), v[j].at(3), e);
+            const uint2 w = make_uint2(four_codes<E5M2>(v[j].at(0), v[j].at(1), e), four_codes<E5M2>(v[j].at(2), v[j].at(3), e));
             if (row < a.rows) {
                 uint8_t* to = a.along.codes + row * a.along.stride + col0;
                 if (whole) *reinterpret_cast<uint2*>(to) = w;
@@ -207,16 +246,17 @@ __global__ __launch_bounds__(NT, 4) void pack_kernel(const gd_pack_args a) {
         __syncthreads();
         // (each column's exponent once, by one lane)
         if (threadIdx.x < EDGE) {
-            const uint32_t* m = most_of[threadIdx.x];
-            exp_of[threadIdx.x] = exponent<E5M2>(max(max(m[0], m[1]), max(m[2], m[3])));
+            uint32_t m = 0;
+#pragma unroll
+            for (uint32_t w = 0; w < WAVES; ++w) m = max(m, most_of[threadIdx.x][w]);
+            exp_of[threadIdx.x] = exponent<E5M2>(m);
         }
         __syncthreads();
     }
 #pragma unroll
     for (int c = 0; c < 8; ++c) {
         const uint32_t e = a.square ? exponent<E5M2>(square_most) : exp_of[tx * 8 + c];
-        turned[tx * 8 + c][ty] = eight_codes<E5M2>(eight<T>::below(v[0], v[1], c), eight<T>::below(v[2], v[3], c), eight<T>::below(v[4], v[5], c),
-                                                   eight<T>::below(v[6], v[7], c), e);
+        turned[16 * c + tx][ty] = four_codes<E5M2>(eight<T>::below(v[0], v[1], c), eight<T>::below(v[2], v[3], c), e);
     }
     __syncthreads();
     if (threadIdx.x < EDGE && tile_c * EDGE + threadIdx.x < a.cols)
@@ -224,7 +264,7 @@ __global__ __launch_bounds__(NT, 4) void pack_kernel(const gd_pack_args a) {
     const uint32_t from = tile_r * EDGE + (threadIdx.x % 8) * 16;
     for (uint32_t c = threadIdx.x / 8; c < EDGE && tile_c * EDGE + c < a.cols; c += NT / 8) {
         if (from >= a.rows) break;
-        const uint4 w = *reinterpret_cast<const uint4*>(&turned[c][(threadIdx.x % 8) * 2]);
+        const uint4 w = *reinterpret_cast<const uint4*>(&turned[c % 8 * 16 + c / 8][(threadIdx.x % 8) * 4]);
         uint8_t* to = a.across.codes + (tile_c * EDGE + c) * a.across.stride + from;
         if (from + 16 <= a.rows) *reinterpret_cast<uint4*>(to) = w;
         else write_some({w.x, w.y, w.z, w.w}, to, a.rows - from);

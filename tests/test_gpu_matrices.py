@@ -92,6 +92,20 @@ def test_packing(det, n, k, gap, at, dtype, codes):
         assert untouched(alone) and untouched(turned)
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+def test_packing_of_rows_that_end_anywhere(det, dtype):
+    """Every number of rest behind eights, along and across; what lies behind the rows' ends counts for nothing."""
+    for k in (*range(1, 18), *range(127, 138)):
+        n = 5 * k % 23 + 1
+        x = randn((n, k), 77 + k, dtype, 3.0)
+        xd = torch.full((n, k + 9), float("nan"), dtype=dtype, device="cuda")[:, :k]
+        xd.copy_(x)
+        along, across = room(n, k, "e4m3", gap=1), room(k, n, "e4m3", gap=1)
+        det.pack(xd, along, across)
+        same_packed(along, x, False, "e4m3", f"along {n} x {k}")
+        same_packed(across, x.t().contiguous(), False, "e4m3", f"across {n} x {k}")
+
+
 @pytest.mark.parametrize("codes", ["e4m3", "e5m2"])
 @pytest.mark.parametrize("square", [False, True])
 def test_packing_of_values_at_the_borders(det, codes, square):

@@ -53,7 +53,7 @@ def test_structs_have_the_header_s_sizes():
     (mat(10, 64, stride=63), pk(10, 64), None, INVALID), (mat(10, 64, at=AT + 1), pk(10, 64), None, INVALID),
     (mat(2 ** 24 + 1, 64), pk(2 ** 24 + 1, 64), None, INVALID), (mat(10, 2 ** 22 + 1), pk(10, 2 ** 22 + 1), None, INVALID),
     (mat(10, 64), pk(10, 64, stride=2 ** 22 + 16), None, INVALID),
-    (mat(2 ** 23, 65_536), pk(2 ** 23, 65_536), None, UNSUPPORTED),
+    (mat(2 ** 23, 65_536), pk(2 ** 23, 65_536), None, UNSUPPORTED), (mat(2 ** 24, 8192), pk(2 ** 24, 8192), None, UNSUPPORTED),
 ])
 def test_packing(lib, h, x, along, across, status):
     assert lib.gd_pack(h, x, 0, along, across, None) == status
