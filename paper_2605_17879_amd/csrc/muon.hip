@@ -406,8 +406,8 @@ __device__ __forceinline__ void finish_row(const muon_args& g, const target& o, 
     }
 }
 
-// (Called by all lanes of a wave; the next lane's row is four further on.)
-__device__ __forceinline__ void write_row(const target& o, uint32_t row, uint32_t col, const f32x4 (&v)[4], uint32_t lane) {
+// (Called by all lanes of a wave; the next lane's row is `apart` further on.)
+__device__ __forceinline__ void write_row(const target& o, uint32_t row, uint32_t col, const f32x4 (&v)[4], uint32_t apart, uint32_t lane) {
     if (col >= o.of_d.cols) return;                // (the same for lanes that exchange)
     gd_u32x4 hi[2], lo[2];
 #pragma unroll
@@ -424,10 +424,10 @@ __device__ __forceinline__ void write_row(const target& o, uint32_t row, uint32_
     }
     exchange<2>(hi, lane);
     if (o.of_d.lo) exchange<2>(lo, lane);
-    const uint32_t first = row - lane % 2 * 4;
+    const uint32_t first = row - lane % 2 * apart;
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-        const uint32_t r = first + 4 * h;
+        const uint32_t r = first + apart * h;
         if (r >= o.rows) break;
         uint8_t* to = o.d + r * o.of_d.pitch + o.of_d.at(col) + lane % 2 * 16;
         *reinterpret_cast<gd_u32x4*>(to) = hi[h];
@@ -435,13 +435,21 @@ __device__ __forceinline__ void write_row(const target& o, uint32_t row, uint32_
     }
 }
 
-// Four rows from `row` on of a column, written next to each other.
-__device__ __forceinline__ void write_column(const target& o, uint32_t row, uint32_t col, float x0, float x1, float x2, float x3) {
+// N rows from `row` on of a column, written next to each other.
+template <int N>
+__device__ __forceinline__ void write_column(const target& o, uint32_t row, uint32_t col, const float (&x)[N]) {
     if (!o.t || col >= o.cols || row >= o.of_t.cols) return;
+    typedef gd_f16 some __attribute__((ext_vector_type(N)));
     uint8_t* to = o.t + col * o.of_t.pitch + o.of_t.at(row);
-    const halves s0 = split(x0), s1 = split(x1), s2 = split(x2), s3 = split(x3);
-    *reinterpret_cast<f16x4*>(to) = f16x4{s0.hi, s1.hi, s2.hi, s3.hi};
-    if (o.of_t.lo) *reinterpret_cast<f16x4*>(to + o.of_t.lo) = f16x4{s0.lo, s1.lo, s2.lo, s3.lo};
+    some hi, lo;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const halves h = split(x[i]);
+        hi[i] = h.hi;
+        lo[i] = h.lo;
+    }
+    *reinterpret_cast<some*>(to) = hi;
+    if (o.of_t.lo) *reinterpret_cast<some*>(to + o.of_t.lo) = lo;
 }
 
 template <typename T>
@@ -505,14 +513,16 @@ __device__ __forceinline__ void corner_of(uint32_t t, uint32_t& tp, uint32_t& tq
     tp = t - q * (q + 1) / 2;
 }
 
-// The workgroup's tile; false if there is none.
+// The workgroup's tile, and which of the `bands` of its rows; false if there is none.
 template <int PHASE>
-__device__ __forceinline__ bool place_of(const muon_args& g, uint32_t edge, uint32_t& tp, uint32_t& tq, entry& e) {
+__device__ __forceinline__ bool place_of(const muon_args& g, uint32_t edge, uint32_t bands, uint32_t& tp, uint32_t& tq, uint32_t& band, entry& e) {
     constexpr bool HALF = PHASE == OF_X || PHASE == OF_A;
     // (workgroup b is on XCD b % 8)
     const uint32_t chip = blockIdx.x % 8;
     const int list = OF_SHARES + ((HALF ? 0 : 8) + (int)chip) * 2;
     uint32_t t = blockIdx.x / 8;
+    band = t % bands;
+    t /= bands;
     const uint32_t cut = g.parts ? 256 / edge : 1, part = t % (cut * cut), own = edge;
     if (g.parts) {
         t = g.parts - 1 + t / (cut * cut);
@@ -536,9 +546,9 @@ __global__ __launch_bounds__(TILE::NT, 512 / TILE::NT) void tiled_kernel(const m
     typedef TILE tile;
     float f;
     if (!begins(g, f)) return;
-    uint32_t tp, tq;
+    uint32_t tp, tq, band;
     entry e;
-    if (!place_of<PHASE>(g, tile::BP, tp, tq, e)) return;
+    if (!place_of<PHASE>(g, tile::BP, 1, tp, tq, band, e)) return;
     const problem x = problem_of<PHASE>(g, e, tp != tq);
     f32x4 acc[tile::FP][tile::FQ] = {};
     tile::run(x.p, x.q, tp * tile::BP, tq * tile::BQ, x.way, acc);
@@ -560,47 +570,52 @@ __global__ __launch_bounds__(TILE::NT, 512 / TILE::NT) void tiled_kernel(const m
             for (int i = 0; i < 4; ++i) v[j][i] = acc[4 * h + i][j];
             finish_row<PHASE>(g, x.out, row + j, col, v[j], old[j]);
             if (PHASE == LAST) update_row(g, e, row + j, col, v[j]);
-            else write_row(x.out, row + j, col, v[j], lane);
+            else write_row(x.out, row + j, col, v[j], 4, lane);
         }
         if (PHASE != LAST) {
 #pragma unroll
             for (int c = 0; c < 16; ++c)
-                write_column(x.out, row, col + c, v[0][c % 4][c / 4], v[1][c % 4][c / 4], v[2][c % 4][c / 4], v[3][c % 4][c / 4]);
+                write_column<4>(x.out, row, col + c, {v[0][c % 4][c / 4], v[1][c % 4][c / 4], v[2][c % 4][c / 4], v[3][c % 4][c / 4]});
         }
     }
 }
 
-template <int PHASE, typename MUL, int WAVES>
+// Tiles of 64 columns and 16 FQ rows.
+template <int PHASE, typename MUL, int FQ, int WAVES>
 __global__ __launch_bounds__(64 * WAVES, 8 / WAVES) void direct_kernel(const muon_args g) {
-    typedef direct_tile<MUL, 4, WAVES> tile;
+    typedef direct_tile<MUL, FQ, WAVES> tile;
     float f;
     if (!begins(g, f)) return;
-    uint32_t tp, tq;
+    uint32_t tp, tq, part;
     entry e;
-    if (!place_of<PHASE>(g, 64, tp, tq, e)) return;
+    if (!place_of<PHASE>(g, 64, 4 / FQ, tp, tq, part, e)) return;
     const problem x = problem_of<PHASE>(g, e, tp != tq);
     f32x4 v[4];
-    const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
-    const uint32_t row = tq * 64 + 4 * (lane & 15), col = tp * 64 + 16 * (lane >> 4);
+    const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), first = tq * 64 + part * tile::BQ;
+    const uint32_t row = first + FQ * (lane & 15), col = tp * 64 + 16 * (lane >> 4);
     old_row old = {};
-    if (PHASE != OF_X && wave < 4) read_old(x.out, row + wave, col, old);   // (on its way beside the sum)
-    typename tile::sums* room = tile::run(x.p, x.q, tp * 64, tq * 64, x.way, 0, x.way.blocks, v);
-    if (wave < 4) {
+    if (PHASE != OF_X && wave < FQ) read_old(x.out, row + wave, col, old);  // (on its way beside the sum)
+    typename tile::sums* room = tile::run(x.p, x.q, tp * 64, first, x.way, 0, x.way.blocks, v);
+    if (wave < FQ) {
         finish_row<PHASE>(g, x.out, row + wave, col, v, old);
         if (PHASE == LAST) update_row(g, e, row + wave, col, v);
-        else write_row(x.out, row + wave, col, v, lane);
+        else write_row(x.out, row + wave, col, v, FQ, lane);
     }
     if (PHASE == LAST || !x.out.t) return;
-    // the four rows of a lane together, for the transpose: wave r has columns 4 r .. 4 r + 3
-    if (wave < 4) {
+    // the rows of a lane together, for the transpose: wave r has columns 4 r .. 4 r + 3
+    if (wave < FQ) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) room[0][wave][i][lane] = v[i];
     }
     __syncthreads();
     if (wave < 4) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            write_column(x.out, row, col + 4 * wave + i, room[0][0][i][lane][wave], room[0][1][i][lane][wave], room[0][2][i][lane][wave], room[0][3][i][lane][wave]);
+        for (int i = 0; i < 4; ++i) {
+            float some[FQ];
+#pragma unroll
+            for (int j = 0; j < FQ; ++j) some[j] = room[0][j][i][lane][wave];
+            write_column<FQ>(x.out, row, col + 4 * wave + i, some);
+        }
     }
 }
 
@@ -868,14 +883,18 @@ void launch_phase_of(muon_args g, const head& h, hipStream_t s) {
                 g.parts = whole + 1;
                 // (so few that two workgroups a CU take them as tiles of 64 x 64: of 4 096 x 4 352, 272 tiles, the last 16 as quarters 1.95 ms
                 // for all, so 1.79)
-                if (16 * 8 * (most - whole) <= 2 * CUS) direct_kernel<PHASE, MUL, 4><<<8 * 16 * (most - whole), 256, 0, s>>>(g);
+                if (16 * 8 * (most - whole) <= 2 * CUS) direct_kernel<PHASE, MUL, 4, 4><<<8 * 16 * (most - whole), 256, 0, s>>>(g);
                 else tiled_kernel<PHASE, small_tile<MUL>><<<8 * 4 * (most - whole), 256, 0, s>>>(g);
                 g.parts = 0;
             }
         }
         else if (k == SMALL) tiled_kernel<PHASE, small_tile<MUL>><<<8 * most, 256, 0, s>>>(g);
-        else if (8 * most <= CUS) direct_kernel<PHASE, MUL, 8><<<8 * most, 512, 0, s>>>(g);
-        else direct_kernel<PHASE, MUL, 4><<<8 * most, 256, 0, s>>>(g);
+        // (bands of 16 or 32 rows of a tile where there are CUs for them: 4 of 1 000 x 333 193 us, so 170; 1 of 512 x 512 162, 126; 8 of
+        // 128 x 128 117, 93)
+        else if (4 * 8 * most <= CUS) direct_kernel<PHASE, MUL, 1, 8><<<4 * 8 * most, 512, 0, s>>>(g);
+        else if (2 * 8 * most <= CUS) direct_kernel<PHASE, MUL, 2, 8><<<2 * 8 * most, 512, 0, s>>>(g);
+        else if (8 * most <= CUS) direct_kernel<PHASE, MUL, 4, 8><<<8 * most, 512, 0, s>>>(g);
+        else direct_kernel<PHASE, MUL, 4, 4><<<8 * most, 256, 0, s>>>(g);
     }
 }
 
