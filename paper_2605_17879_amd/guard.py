@@ -236,6 +236,7 @@ class Config:
 
 
 _PACK_MATRIX = struct.Struct("=QQQQII").pack            # gd_matrix
+_PACK_PACKED = struct.Struct("=QQQQIIQQQQII").pack      # gd_packed
 _PACK_ADAMW = struct.Struct("=IIddddQ").pack            # gd_adamw_config
 _ADAMW_BYTES = ctypes.sizeof(_CAdamwConfig)
 _PACK_MUON = struct.Struct("=IIIIdddQ").pack            # gd_muon_config
@@ -264,6 +265,7 @@ class Detector:
         self._raw_stream = torch._C._cuda_getCurrentRawStream
         self._index = self.device.index
         self._f32 = torch.float32
+        self._u8 = torch.uint8
         # the operators' entry points as their methods call them: structures come as packed bytes
         vp, f32, sz = ctypes.c_void_p, ctypes.c_float, ctypes.c_size_t
         self._embed = self._entry("gd_embed", vp, vp, vp, f32, vp, vp)
@@ -646,15 +648,15 @@ class Detector:
 
     def _packed(self, p: dict) -> bytes:
         """codes[rows][cols] and exp[ceil(cols / 128)][rows] as a gd_packed."""
-        out = b""
-        for t, types in ((p["codes"], self._codes), (p["exp"], {self._torch.uint8: U8})):
-            code = types.get(t.dtype)
-            if code is None:
-                raise GuardError(4, f"packed matrices of {t.dtype} are not built")
-            (rows, cols), strides = t.shape, t.stride()
-            assert cols <= 1 or strides[1] == 1, "the elements of a row must be next to each other"
-            out += _PACK_MATRIX(self._at(t), rows, cols, strides[0] if rows > 1 else cols or 1, code, 0)
-        return out
+        codes, exp = p["codes"], p["exp"]
+        code = self._codes.get(codes.dtype)
+        if code is None or exp.dtype is not self._u8:
+            raise GuardError(4, f"packed matrices of {codes.dtype} and {exp.dtype} are not built")
+        (rows, cols), (apart, one) = codes.shape, codes.stride()
+        (blocks, n), (exp_apart, exp_one) = exp.shape, exp.stride()
+        assert (cols <= 1 or one == 1) and (n <= 1 or exp_one == 1), "the elements of a row must be next to each other"
+        return _PACK_PACKED(self._at(codes), rows, cols, apart if rows > 1 else cols or 1, code, 0,
+                            self._at(exp), blocks, n, exp_apart if blocks > 1 else n or 1, U8, 0)
 
     def pack(self, x, along: Optional[dict] = None, across: Optional[dict] = None, square: bool = False, stream=None):
         """x[n][k] into 8-bit codes with a power of two for each block of 128: along its rows, across (x transposed,
