@@ -291,20 +291,20 @@ __global__ __launch_bounds__(256) void start_kernel(const muon_args g) {
     if (!begins(g, f)) return;
     uint32_t t = blockIdx.x;
     const entry e = entry_at(g, find(g, OF_TILES, t));
+    const uint32_t tiles_c = (e.cols + 63) / 64, row = t / tiles_c * 64 + threadIdx.x / 16 * 4, col = t % tiles_c * 64 + threadIdx.x % 16 * 4;
     const double* part = reinterpret_cast<const double*>(g.work) + e.partial;
     double s = 0;
     for (uint32_t i = threadIdx.x; i < e.chunks; i += 256) s += part[i];
-    const double size = sqrt(sum_of_all(s)) + g.eps, scale = size == 0 ? 0 : ONE_X / size;   // (in 64 bits: no gradient is too small)
-    const layout l(e.rows, e.cols, g.both);
-    uint8_t* base = g.work + e.at[!g.both];
-    const uint32_t tiles_c = (e.cols + 63) / 64, row = t / tiles_c * 64 + threadIdx.x / 16 * 4, col = t % tiles_c * 64 + threadIdx.x % 16 * 4;
-    halves x[4][4];
-    float u[4][4] = {};
+    float u[4][4] = {};                            // (on its way beside the sum)
     if (row < e.rows && col < e.cols) {
         if (e.grad_type == GD_F32) updates_of<float>(g, e, row, col, f, u);
         else if (e.grad_type == GD_BF16) updates_of<gd_bf16>(g, e, row, col, f, u);
         else updates_of<gd_f16>(g, e, row, col, f, u);
     }
+    const double size = sqrt(sum_of_all(s)) + g.eps, scale = size == 0 ? 0 : ONE_X / size;   // (in 64 bits: no gradient is too small)
+    const layout l(e.rows, e.cols, g.both);
+    uint8_t* base = g.work + e.at[!g.both];
+    halves x[4][4];
 #pragma unroll
     for (int i = 0; i < 4; ++i)
 #pragma unroll
