@@ -149,17 +149,19 @@ __device__ __forceinline__ entry entry_at(const muon_args& g, uint32_t i) {
     return __builtin_bit_cast(entry, x);
 }
 
-// Which of `count` entries from `first` on has place t of a list: the last that does not begin behind it.
+// Which of `count` entries from `first` on has place t of a list: the last that does not begin behind it.  A wave looks at 64 of them at
+// once, of more at 64 an equal way apart first (1 500 matrices of 130 x 70 0.99 ms, with all of them looked at in turn 1.25).
 __device__ __forceinline__ uint32_t entry_of(const muon_args& g, int list, uint32_t first, uint32_t count, uint32_t t) {
-    const uint32_t* at = reinterpret_cast<const uint32_t*>(g.table + list_at(g.n, list)) + first;
+    const uint32_t* at = reinterpret_cast<const uint32_t*>(g.table + list_at(g.n, list));
     const uint32_t lane = threadIdx.x & 63;
-    uint32_t before = 0;
-    for (uint32_t i = 0; i < count; i += 64) {
-        const uint64_t begun = __ballot(i + lane < count && at[min(i + lane, count - 1)] <= t);
-        before += (uint32_t)__popcll(begun);
-        if (begun != ~0ull) break;
+    for (uint32_t left = count;;) {
+        const uint32_t apart = (left + 63) / 64, i = lane * apart;
+        const uint64_t begun = __ballot(i < left && at[first + min(i, left - 1)] <= t);
+        const uint32_t behind = ((uint32_t)__popcll(begun) - 1) * apart;
+        first = __builtin_amdgcn_readfirstlane(first + behind);
+        if (apart == 1) return first;
+        left = min(apart, left - behind);
     }
-    return first + __builtin_amdgcn_readfirstlane(before - 1);
 }
 __device__ __forceinline__ uint32_t number_at(const muon_args& g, int list, uint32_t k) {
     return __builtin_amdgcn_readfirstlane(reinterpret_cast<const uint32_t*>(g.table + list_at(g.n, list))[k]);

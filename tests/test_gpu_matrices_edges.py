@@ -172,6 +172,20 @@ def test_long_lists_of_matrices_of_all_kinds(det, products):
         assert off <= bound, (tuple(gr.shape), off, bound)
 
 
+@pytest.mark.parametrize("count", [64, 65, 4097, 4500])
+def test_lists_that_are_looked_through_in_steps(det, count):
+    """64 matrices are looked at at once, 64 stretches of more, and stretches of those."""
+    shapes = [(66, 70), (70, 9), (5, 200)]
+    pairs = [(low_rank(*s, 7), low_rank(*s, 8)) for s in shapes]
+    bounds = [refs.orthogonal_bound(update_of(*p)[1].cuda(), "f32") for p in pairs]
+    which = [i % 7 % 3 for i in range(count)]
+    params, _, _ = run_muon(det, [pairs[w] for w in which])
+    for s in range(3):
+        all_of = torch.stack([p for p, w in zip(params, which) if w == s]).double()
+        off = torch.linalg.matrix_norm(-all_of - bounds[s][0])
+        assert float(off.max()) <= bounds[s][1], (shapes[s], int(off.argmax()))
+
+
 @pytest.mark.parametrize("count,rows,cols", [(4, 2100, 2100), (6, 2100, 2180), (3, 2177, 4400), (2, 2900, 3000)])
 def test_tiles_that_are_left_over(det, count, rows, cols):
     """More large tiles than one round of the chip, the last ones taken in parts: of the products (4: 324 tiles in quarters, 2: 288 in
