@@ -544,8 +544,9 @@ gd_status gd_adamw(gd_handle h, const void* d_table, size_t table_bytes, const g
  *   codes [rows][cols]               GD_E4M3 or GD_E5M2, one byte each; 16-byte aligned, the stride a multiple of 16 (rather not
  *                                    of 256: such rows meet at the same channels of the memory)
  *   exp   [ceil(cols / 128)][rows]   GD_U8; 4-byte aligned, the stride a multiple of 4, up to 2^24
- * Element (i, k) stands for codes[i][k] * 2^(exp[k / 128][i] - 127); a byte of 255 stands for a block of NaN.  In front
- * of the last row what lies between its end and the next one's begin is neither read as a number nor written.  What a call
+ * Element (i, k) stands for codes[i][k] * 2^(exp[k / 128][i] - 127), for a byte of 0 as for the others; one of 255 stands for a
+ * block of NaN, whatever its codes are.  An element of 2^128 and more, which gd_pack does not make, is infinite in a product
+ * with an fp32 out.  In front of the last row what lies between its end and the next one's begin is neither read as a number nor written.  What a call
  * writes (outputs, its work area) overlaps nothing else that it is given; calls that may run at the same time (on two streams,
  * in two graphs) have work areas of their own.
  */

@@ -139,7 +139,8 @@ __device__ __forceinline__ bf16x8 numbers_of(uint32_t lo, uint32_t hi, float two
     }
     return u.x;
 }
-// 2^(e - 127); 0 for e = 0 (all codes are zeros), NaN for 255
+// 2^(e - 127) as a conversion takes it, which reads the exponent's bits alone: those of 0 are 2^-127 there, as in the scaled instruction.
+// NaN for 255, of any code.
 __device__ __forceinline__ float power_of(uint32_t e) { return __builtin_bit_cast(float, e == 255 ? 0x7FC00000u : e << 23); }
 
 // The same products by the 16-bit matrix cores, whose sums are of fp32.
