@@ -178,6 +178,8 @@ const char* bad_packed(const gd_packed* p, uint64_t rows, uint64_t cols) {
     if (rows == 0 || cols == 0) return nullptr;
     if (((uintptr_t)p->codes.d_data & 15) || (rows > 1 && (p->codes.stride & 15))) return "codes and their stride must be 16-byte aligned";
     if (p->codes.stride > MAX_STRIDE) return "stride above 2^22 elements";
+    // (of one row too, which bad_matrix lets lie anywhere: tiles take the stride in 32 bits)
+    if (cols > GD_PACK_BLOCK && p->exp.stride > GD_MAX_TOKENS) return "stride above 2^24 elements";
     if (((uintptr_t)p->exp.d_data & 3) || (cols > GD_PACK_BLOCK && (p->exp.stride & 3))) return "powers of two and their stride must be 4-byte aligned";
     return nullptr;
 }

@@ -1,0 +1,26 @@
+"""The limits of packed matrices and their products, as the header has them: what lies at one is taken, what lies behind it
+refused by a message of its own, before any launch.  No GPU is needed, and no address given here is ever read."""
+import ctypes
+
+import pytest
+
+from paper_2605_17879_amd.guard import BF16, F32
+from test_matrix_refusals import AT, INVALID, OK, h, lib, mat, pk  # noqa: F401  (two of them fixtures)
+
+
+@pytest.mark.parametrize("rows", [1, 3])
+def test_powers_of_two_lie_at_most_2_24_apart(lib, h, rows):  # noqa: F811
+    """Of one row too: its blocks' bytes are as far apart as any's."""
+    far, next_ = pk(rows, 300, exp_stride=2 ** 24 + 4), pk(rows, 300, exp_stride=2 ** 24)
+    for stride in (2 ** 24 + 4, 2 ** 32 + 4, 2 ** 40):
+        assert lib.gd_pack(h, mat(rows, 300), 0, pk(rows, 300, exp_stride=stride), None, None) == INVALID
+        assert lib.gd_last_error(h) == b"gd_pack: stride above 2^24 elements"
+    out, work = mat(rows, rows), ctypes.c_size_t(1 << 40)
+    for a, b in ((far, next_), (next_, far)):
+        assert lib.gd_packed_product(h, a, b, out, 0, AT, work, None) == INVALID
+        assert lib.gd_last_error(h) == b"gd_packed_product: stride above 2^24 elements"
+
+
+def test_one_block_s_distance_to_the_next_says_nothing(lib, h):  # noqa: F811
+    """(of a matrix without a row: nothing is launched)"""
+    assert lib.gd_packed_product(h, pk(0, 100, at=None, exp_at=None), pk(1, 100, exp_stride=2 ** 32), mat(0, 1, F32, at=None), 0, None, 0, None) == OK
