@@ -641,8 +641,8 @@ class Detector:
         torch = self._torch
         kind = {"e4m3": torch.float8_e4m3fn, "e5m2": torch.float8_e5m2}[codes]
         wide = lambda n: -(-max(n, 1) // 16) * 16
-        # rows a multiple of 256 bytes apart would meet at the same channels of the memory
-        stride = wide(cols) + (128 if wide(cols) % 256 == 0 else 0)
+        # rows a multiple of 256 bytes apart would meet at the same channels of the memory (but a stride ends at 2^22)
+        stride = wide(cols) + (128 if wide(cols) % 256 == 0 and wide(cols) + 128 <= 1 << 22 else 0)
         return dict(codes=self._bytes(rows * stride).view(kind).view(rows, stride)[:, :cols],
                     exp=self._bytes(-(-cols // PACK_BLOCK) * wide(rows)).view(-1, wide(rows))[:, :rows])
 

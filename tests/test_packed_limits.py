@@ -4,7 +4,7 @@ import ctypes
 
 import pytest
 
-from paper_2605_17879_amd.guard import BF16, F32
+from paper_2605_17879_amd.guard import F32, Detector
 from test_matrix_refusals import AT, INVALID, OK, h, lib, mat, pk  # noqa: F401  (two of them fixtures)
 
 
@@ -24,3 +24,24 @@ def test_powers_of_two_lie_at_most_2_24_apart(lib, h, rows):  # noqa: F811
 def test_one_block_s_distance_to_the_next_says_nothing(lib, h):  # noqa: F811
     """(of a matrix without a row: nothing is launched)"""
     assert lib.gd_packed_product(h, pk(0, 100, at=None, exp_at=None), pk(1, 100, exp_stride=2 ** 32), mat(0, 1, F32, at=None), 0, None, 0, None) == OK
+
+
+class Room:
+    """What Detector.alloc_packed takes of a detector, on the CPU."""
+    import torch as _torch
+
+    @staticmethod
+    def _bytes(n):
+        return Room._torch.empty(n, dtype=Room._torch.uint8)
+
+
+@pytest.mark.parametrize("cols", [2 ** 22, 2 ** 22 - 5, 2 ** 22 - 128, 2 ** 22 - 300, 256, 128, 1])
+def test_rooms_keep_to_the_limits(lib, h, cols):  # noqa: F811
+    """Up to the longest row there is: of a product of what alloc_packed lays out only the result's size is refused."""
+    p = Detector.alloc_packed(Room, 2, cols)
+    codes, exp = p["codes"], p["exp"]
+    assert codes.shape == (2, cols) and codes.stride(0) % 16 == 0 and cols <= codes.stride(0) <= 2 ** 22
+    assert (codes.stride(0) % 256 != 0) or cols > 2 ** 22 - 128
+    a = pk(2, cols, stride=codes.stride(0), exp_stride=exp.stride(0))
+    assert lib.gd_packed_product(h, a, a, mat(2, 3, F32), 0, AT, ctypes.c_size_t(1 << 40), None) == INVALID
+    assert lib.gd_last_error(h) == b"gd_packed_product: sizes of the matrices do not fit each other"
