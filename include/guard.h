@@ -565,6 +565,7 @@ typedef struct gd_packed {
  *   across  [k][n]  out  x transposed, blocks of 128 along the columns of x, or null
  *   square != 0: one e for each 128 x 128 of x (written for each of its rows), so that `across` holds the same
  *   numbers as `along`, transposed
+ * n up to 2^24 (to 2^22 with `across`, whose rows they are), k up to 2^22, fewer than 2^37 elements.
  * One of the two is there; where both are, x is read once.  A linear layer's y = x w^T, dx = dy w and dw = dy^T x are products
  * of x, w (square) and dy packed both ways.
  */
@@ -579,7 +580,7 @@ gd_status gd_pack(gd_handle h, const gd_matrix* x, int32_t square, const gd_pack
  *   b    [m][k]  in
  *   out  [n][m]  in, out  f32, bf16 or f16
  *   d_work: gd_packed_product_work_bytes(n, m, k) bytes, 256-byte aligned
- * n, m up to 2^24, k up to 2^22.
+ * n up to 2^24, m and k up to 2^22, fewer than 2^38 results.
  */
 size_t gd_packed_product_work_bytes(uint64_t n, uint64_t m, uint64_t k);
 gd_status gd_packed_product(gd_handle h, const gd_packed* a, const gd_packed* b, const gd_matrix* out, int32_t accumulate,

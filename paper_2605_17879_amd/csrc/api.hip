@@ -824,7 +824,7 @@ gd_status gd_pack(gd_handle h, const gd_matrix* x, int32_t square, const gd_pack
 }
 
 size_t gd_packed_product_work_bytes(uint64_t n, uint64_t m, uint64_t k) {
-    if (n > GD_MAX_TOKENS || m > GD_MAX_TOKENS || k > MAX_INNER) return 0;
+    if (n > GD_MAX_TOKENS || m > MAX_STRIDE || k > MAX_INNER) return 0;
     return gd_packed_product_work(n, m, k);
 }
 
@@ -835,7 +835,7 @@ gd_status gd_packed_product(gd_handle h, const gd_packed* a, const gd_packed* b,
     if (!a || !b) return invalid(h, call, "null packed matrix");
     if (!out) return invalid(h, call, "null matrix");
     const uint64_t n = a->codes.rows, m = b->codes.rows, k = a->codes.cols;
-    if (n > GD_MAX_TOKENS || m > GD_MAX_TOKENS || k > MAX_INNER) return invalid(h, call, "more than 2^24 rows or 2^22 of k");
+    if (n > GD_MAX_TOKENS || m > MAX_STRIDE || k > MAX_INNER) return invalid(h, call, "more than 2^24 rows, 2^22 columns or 2^22 of k");
     if (!is_float(out->dtype)) return fail(h, GD_ERR_UNSUPPORTED, "gd_packed_product: out must be f32, bf16 or f16");
     if (const char* e = bad_packed(a, n, k)) return invalid(h, call, e);
     if (const char* e = bad_packed(b, m, k)) return invalid(h, call, e);

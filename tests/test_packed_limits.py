@@ -45,3 +45,14 @@ def test_rooms_keep_to_the_limits(lib, h, cols):  # noqa: F811
     a = pk(2, cols, stride=codes.stride(0), exp_stride=exp.stride(0))
     assert lib.gd_packed_product(h, a, a, mat(2, 3, F32), 0, AT, ctypes.c_size_t(1 << 40), None) == INVALID
     assert lib.gd_last_error(h) == b"gd_packed_product: sizes of the matrices do not fit each other"
+
+
+def test_columns_of_a_result(lib, h):  # noqa: F811
+    """2^22 of them, and 2^24 rows."""
+    wide = 2 ** 22 + 1
+    assert lib.gd_packed_product(h, pk(1, 64), pk(wide, 64), mat(1, wide), 0, AT, ctypes.c_size_t(1 << 40), None) == INVALID
+    assert lib.gd_last_error(h) == b"gd_packed_product: more than 2^24 rows, 2^22 columns or 2^22 of k"
+    assert lib.gd_packed_product_work_bytes(1, wide, 64) == 0
+    for n, m in ((1, 2 ** 22), (2 ** 24, 8)):                  # (refused for the result's address alone)
+        assert lib.gd_packed_product(h, pk(n, 64), pk(m, 64), mat(n, m, F32, at=AT + 1), 0, AT, ctypes.c_size_t(1 << 40), None) == INVALID
+        assert lib.gd_last_error(h) == b"gd_packed_product: pointer of a matrix not aligned to its element"
