@@ -4,8 +4,11 @@
 //   C_ij = sum over blocks b of 2^(ea_bi - 127 + eb_bj - 127) sum over the block's k of a_ik b_jk
 //
 // A C of 16 bits comes from the scaled 8-bit instruction of the matrix cores, which takes 128 of k at a time with their powers
-// of two, so that a block costs what a plain 8-bit product costs.  That instruction's own sums are short (off by up
-// to 7e-5, gd_tiles.h: far below the rounding to 16 bits, 1.7e-3 for bf16 and 2.1e-4 for f16), so a C of fp32 is computed by the 16-bit matrix
+// of two, so that a block costs what a plain 8-bit product costs.  That instruction's own sums are short: the products of eight k are cut at 2^-13 of
+// the largest (gd_tiles.h has the rule).  They are taken all the same where C has 16 bits, for twice the rate (8 192 x 8 192 x 8 192 400 us,
+// 800 by the 16-bit cores): in the norm the cut costs 1.5e-5 to 9e-5, C's own rounding 1.7e-3 in bf16 and 2.1e-4 in f16.  At its worst, seven small products
+// beside a large one, it is 8.0e-4 of that product, below half a step of bf16 (3.9e-3) but not of f16 (4.9e-4), and where large products cancel
+// nothing of a small result may be left: the header says so, and that a C of fp32 has sums of fp32.  Such a C is computed by the 16-bit matrix
 // cores, for which codes times powers of two are exact, at half the rate: the operands are written out in bf16 first, or
 // converted in registers where tiles are read straight into them.
 //

@@ -671,7 +671,8 @@ class Detector:
         return self._bytes(self.packed_product_work_bytes(n, m, k))
 
     def packed_product(self, a: dict, b: dict, out, work, accumulate: bool = False, stream=None):
-        """out[n][m] = (its old value, with accumulate) + a b^T of packed a[n][k] and b[m][k]."""
+        """out[n][m] = (its old value, with accumulate) + a b^T of packed a[n][k] and b[m][k].  An out of fp32 has sums of fp32; of 16
+        bits those of the 8-bit matrix cores, which cut products 2^-13 below the largest of eight neighbours (include/guard.h)."""
         self._check(self._packed_product(self.h, self._packed(a), self._packed(b), self._matrix(out), accumulate,
                                          self._at(work), work.nbytes, self._stream(stream)))
 
