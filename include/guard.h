@@ -601,6 +601,8 @@ gd_status gd_packed_product(gd_handle h, const gd_packed* a, const gd_packed* b,
  *   for each step, with its coefficients a, b, c:  A = X X^T;  X = a X + (b A + c A A) X   (X^T X for tall matrices)
  *   p = param * [1 - lr * lr_scale * weight_decay] - [lr * lr_scale] * X
  * param = round(p) and, where d_copy is given, copy = round(p).  A matrix of zeros has X = 0.
+ * lr_scale is of the whole rate, as gd_adamw's: the decay has it too.  Where a factor of the shape, max(1, rows / cols)^(1/2) or
+ * another, is to be of the step alone, with a decay of lr * d for every shape, weight_decay is d / lr_scale.
  * products: GD_F32 multiplies numbers of 22 binary digits, three products of f16 for one; GD_F16 numbers of 11, while
  * X itself is kept with 22 from step to step (X off by 1 to 2 thousandths of itself, for a 16-bit param or copy).
  * Sums are fp32 in both.  coefficients: three a step, such that the polynomial a s + b s^3 + c s^5 of each step

@@ -683,8 +683,9 @@ class Detector:
 
     def muon_table(self, params, grads, momenta, copies=None, weight_decay=0.0, lr_scale=1.0) -> dict:
         """What muon needs to know about its matrices (lists of the same length; weight_decay and lr_scale are
-        lists too, or one value for all).  It holds addresses, and keeps the memory there alive; as adamw_table, it
-        has to be made anew for tensors that have moved."""
+        lists too, or one value for all).  lr_scale scales the decay as well: weight_decay = d / lr_scale decays every
+        matrix by lr * d.  It holds addresses, and keeps the memory there alive; as adamw_table, it has to be made anew
+        for tensors that have moved."""
         torch, n = self._torch, len(params)
         each = lambda v: list(v) if isinstance(v, (list, tuple)) else [v] * n
         lists = [params, grads, momenta, copies if copies is not None else [None] * n, each(weight_decay), each(lr_scale)]
