@@ -587,7 +587,9 @@ gd_status gd_pack(gd_handle h, const gd_matrix* x, int32_t square, const gd_pack
  *   a    [n][k]  in       either's codes e4m3 or e5m2
  *   b    [m][k]  in
  *   out  [n][m]  in, out  f32, bf16 or f16
- *   d_work: gd_packed_product_work_bytes(n, m, k) bytes, 256-byte aligned
+ *   d_work: gd_packed_product_work_bytes(n, m, k) bytes, 256-byte aligned, for whichever type out has: where tiles are large, what an
+ *           out of fp32 needs, whose operands are written there as bf16 (2 (n + m) k), and of which an out of 16 bits touches
+ *           nothing; where few rows or columns share a long k, the parts' sums.  Products one behind the other can have one area.
  * n up to 2^24, m and k up to 2^22, fewer than 2^38 results.
  */
 size_t gd_packed_product_work_bytes(uint64_t n, uint64_t m, uint64_t k);
@@ -638,7 +640,9 @@ typedef struct gd_muon_config {
 size_t gd_muon_table_bytes(gd_handle h, const gd_muon_tensor* tensors, uint32_t n_tensors);
 gd_status gd_muon_fill_table(gd_handle h, const gd_muon_tensor* tensors, uint32_t n_tensors, void* host_table, size_t bytes);
 /* Of the work area of an update with these products (256-byte aligned, nothing is kept in it between calls); 0 where the
- * bytes are no table. */
+ * bytes are no table.  All matrices but those up to 64 x 192 have theirs in it at once: X twice both ways, A and B, which are 16 + 8 a / b bytes an element of
+ * a matrix of sides a <= b with products of fp32 (24 where it is square), 12 + 4 a / b with f16.  Updates of several tables, one behind the
+ * other, can have one area, of the largest's size. */
 size_t gd_muon_work_bytes(gd_handle h, const void* host_table, size_t table_bytes, uint32_t products);
 
 /* One update of all matrices of a table.  d_grad_scale: one f32 in device memory that every gradient is multiplied by, or
