@@ -119,7 +119,8 @@ class SweepStep:
 
 
 class LayerStep(SweepStep):
-    """The same with residual layers h = h + h W^T, products of packed numbers, between the table and the loss."""
+    """The same with residual layers h = h + h W^T, products of packed numbers, between the table and the loss.  Those with
+    results of 16 bits are the 8-bit matrix cores' load, and take their sums for it; the weights' gradients have sums of fp32."""
 
     parts, computed = PARTS + ("layers", "muon"), ("loss", "layers", "muon")
 
@@ -162,7 +163,7 @@ class LayerStep(SweepStep):
             d.pack(self.weights[i], *self.packed_weight[i], square=True)
             d.pack(h, *self.packed_hidden[i])
             self.hiddens[i].copy_(h)
-            d.packed_product(self.packed_hidden[i][0], self.packed_weight[i][0], self.hiddens[i], self.works[0], accumulate=True)
+            d.packed_product(self.packed_hidden[i][0], self.packed_weight[i][0], self.hiddens[i], self.works[0], accumulate=True, sums="short")
             h = self.hiddens[i]
 
     def backward(self):
@@ -171,7 +172,7 @@ class LayerStep(SweepStep):
         for i in reversed(range(self.layers)):
             d.pack(dh, *self.packed_grad)
             d.packed_product(self.packed_grad[1], self.packed_hidden[i][1], self.weight_grads[i], self.works[1])
-            d.packed_product(self.packed_grad[0], self.packed_weight[i][1], dh, self.works[0], accumulate=True)
+            d.packed_product(self.packed_grad[0], self.packed_weight[i][1], dh, self.works[0], accumulate=True, sums="short")
 
     def step(self, step: int, lr: float = 1e-3, mark=lambda part: None):
         self.lookup()

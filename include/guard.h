@@ -23,7 +23,7 @@
  * What a sweep has its GPUs run stands at the end: the operators on both sides of a
  * language model's vocabulary (gd_embed, gd_vocab_loss, gd_adamw and the gradients),
  * which make one training step of the job's own kind and repeat bit for bit, and those of the
- * matrices between them (gd_pack, gd_packed_product, gd_muon).
+ * matrices between them (gd_pack, gd_packed_product, gd_packed_product_short, gd_muon).
  *
  * The paper states the decision in words only.  The estimators and constants
  * used here (median / MAD x 1.4826 / threshold 3.5 / k-of-W / scaled node sum)
@@ -545,8 +545,8 @@ gd_status gd_adamw(gd_handle h, const void* d_table, size_t table_bytes, const g
  *                                    of 256: such rows meet at the same channels of the memory)
  *   exp   [ceil(cols / 128)][rows]   GD_U8; 4-byte aligned, the stride a multiple of 4, up to 2^24
  * Element (i, k) stands for codes[i][k] * 2^(exp[k / 128][i] - 127), for a byte of 0 as for the others; one of 255 stands for a
- * block of NaN, whatever its codes are.  An element of 2^128 and more, which gd_pack does not make, is infinite in a product
- * with an fp32 out.  In front of the last row what lies between its end and the next one's begin is neither read as a number nor written.  What a call
+ * block of NaN, whatever its codes are.  An element of 2^128 and more, which gd_pack does not make, is infinite
+ * in gd_packed_product.  In front of the last row what lies between its end and the next one's begin is neither read as a number nor written.  What a call
  * writes (outputs, its work area) overlaps nothing else that it is given; calls that may run at the same time (on two streams,
  * in two graphs) have work areas of their own.
  */
@@ -572,29 +572,33 @@ typedef struct gd_packed {
 gd_status gd_pack(gd_handle h, const gd_matrix* x, int32_t square, const gd_packed* along, const gd_packed* across, void* stream);
 
 /*
- * Product of packed matrices: out[i][j] = round((accumulate ? out[i][j] : 0) + sum over k of a[i][k] b[j][k]), summed in an order
- * that the sizes and the type of out alone fix.  What the sums keep is the type of out's choice:
- *   f32         products exact, sums in fp32, by the 16-bit matrix cores.  Elements below 2^-126 may count as 0.
- *   bf16, f16   by the 8-bit matrix cores, at twice the rate.  They cut the products of eight neighbouring k (8 g to 8 g + 7) toward zero, to
- *               multiples of 2^(E - 13) times the powers of two, before they add them; E is the largest sum of the exponents of a
- *               code of a and a code of b, neither of them 0, and a subnormal code's is its type's least, -6 or -14.  The sums of the eights are added in
- *               fp32.  So the sum is off by up to 7 * 2^(E - 13) for each eight, however small the result: products 2^13 below one beside
- *               them are lost (8.0e-4 of it for seven, where half a step of f16 is 4.9e-4 and of bf16 3.9e-3), and so may be
- *               all that is left of products that cancel.  In the norm, at k = 1 024 and before the rounding to out, which is off by 1.7e-3 in bf16 and
- *               2.1e-4 in f16: 1.5e-5 for normal numbers, 2e-5 to 5e-5 where one column in 500 is 20 times as large, 6e-5 to 9e-5
- *               for normal numbers times e^(1.5 of others) in both matrices.
- * Who needs sums of fp32 takes an out of fp32 and rounds that.
+ * Product of packed matrices: out[i][j] = round((accumulate ? out[i][j] : 0) + sum over k of a[i][k] b[j][k]), products exact, summed in
+ * fp32 in an order that the sizes alone fix, by the 16-bit matrix cores; elements below 2^-126 may count as 0.
  *   a    [n][k]  in       either's codes e4m3 or e5m2
  *   b    [m][k]  in
  *   out  [n][m]  in, out  f32, bf16 or f16
- *   d_work: gd_packed_product_work_bytes(n, m, k) bytes, 256-byte aligned, for whichever type out has: where tiles are large, what an
- *           out of fp32 needs, whose operands are written there as bf16 (2 (n + m) k), and of which an out of 16 bits touches
- *           nothing; where few rows or columns share a long k, the parts' sums.  Products one behind the other can have one area.
+ *   d_work: gd_packed_product_work_bytes(n, m, k) bytes, 256-byte aligned: where tiles are large the operands are written there as
+ *           bf16 (2 (n + m) k bytes), where few rows or columns share a long k the parts' sums.  Products one behind the other
+ *           can have one area.
  * n up to 2^24, m and k up to 2^22, fewer than 2^38 results.
  */
 size_t gd_packed_product_work_bytes(uint64_t n, uint64_t m, uint64_t k);
 gd_status gd_packed_product(gd_handle h, const gd_packed* a, const gd_packed* b, const gd_matrix* out, int32_t accumulate,
                             void* d_work, size_t work_bytes, void* stream);
+
+/*
+ * The same for an out of bf16 or f16 by the 8-bit matrix cores, at twice the rate where tiles are large, with sums that are shorter than fp32: for a
+ * load of those cores, or where a result's accuracy is not that of its products.  They cut the products of eight neighbouring k (8 g to 8 g + 7)
+ * toward zero, to multiples of 2^(E - 13) times the powers of two, before they add them; E is the largest sum of the exponents of a code of
+ * a and a code of b, neither of them 0, and a subnormal code's is its type's least, -6 or -14.  The sums of the eights are added in fp32.  So the
+ * sum is off by up to 7 * 2^(E - 13) for each eight, however small the result: products 2^13 below one beside them are lost
+ * (8.0e-4 of it for seven, where half a step of f16 is 4.9e-4 and of bf16 3.9e-3), and so may be all that is left of products
+ * that cancel.  In the norm, at k = 1 024 and before the rounding to out, which is off by 1.7e-3 in bf16 and 2.1e-4 in f16: 1.5e-5 for normal
+ * numbers, 2e-5 to 5e-5 where one column in 500 is 20 times as large, 6e-5 to 9e-5 for normal numbers times e^(1.5 of others)
+ * in both matrices.  The work area is gd_packed_product's (large tiles touch none of it).
+ */
+gd_status gd_packed_product_short(gd_handle h, const gd_packed* a, const gd_packed* b, const gd_matrix* out, int32_t accumulate,
+                                  void* d_work, size_t work_bytes, void* stream);
 
 /*
  * Update of matrices by their orthogonalised momentum, many at once.  For each, M and U in fp32 (g = grad * grad_scale):

@@ -190,6 +190,33 @@ gd_packed_out packed_out(const gd_packed* p) {
 
 constexpr uint64_t MAX_INNER = 1u << 22;    // of a packed product: rows of `across`, which a stride spans
 
+gd_status packed_product(gd_handle h, const char* call, const gd_packed* a, const gd_packed* b, const gd_matrix* out, int32_t accumulate,
+                         bool short_sums, void* d_work, size_t work_bytes, void* stream) {
+    if (!h) return GD_ERR_INVALID_ARG;
+    if (!a || !b) return invalid(h, call, "null packed matrix");
+    if (!out) return invalid(h, call, "null matrix");
+    const uint64_t n = a->codes.rows, m = b->codes.rows, k = a->codes.cols;
+    if (n > GD_MAX_TOKENS || m > MAX_STRIDE || k > MAX_INNER) return invalid(h, call, "more than 2^24 rows, 2^22 columns or 2^22 of k");
+    if (!is_float(out->dtype)) return fail(h, GD_ERR_UNSUPPORTED, std::string(call) + ": out must be f32, bf16 or f16");
+    if (short_sums && out->dtype == GD_F32) return fail(h, GD_ERR_UNSUPPORTED, std::string(call) + ": out must be bf16 or f16");
+    if (const char* e = bad_packed(a, n, k)) return invalid(h, call, e);
+    if (const char* e = bad_packed(b, m, k)) return invalid(h, call, e);
+    if (const char* e = bad_matrix(out, n, m)) return invalid(h, call, e);
+    if (n == 0 || m == 0) return GD_OK;
+    if (((n + 127) / 128) * ((m + 127) / 128) >= 1u << 24)                  // (a launch has fewer than 2^32 threads)
+        return fail(h, GD_ERR_UNSUPPORTED, std::string(call) + ": 2^38 results or more in one call are not built");
+    if (gd_status st = bad_work(h, call, d_work, work_bytes, gd_packed_product_work(n, m, k))) return st;
+    gd_packed_product_args g = {};
+    g.a = a->codes.d_data; g.a_stride = a->codes.stride; g.a_exp = static_cast<const uint8_t*>(a->exp.d_data); g.a_exp_stride = a->exp.stride;
+    g.b = b->codes.d_data; g.b_stride = b->codes.stride; g.b_exp = static_cast<const uint8_t*>(b->exp.d_data); g.b_exp_stride = b->exp.stride;
+    g.n = (uint32_t)n; g.m = (uint32_t)m; g.k = (uint32_t)k; g.a_codes = a->codes.dtype; g.b_codes = b->codes.dtype;
+    g.out = out->d_data; g.out_stride = out->stride; g.out_type = out->dtype; g.accumulate = accumulate != 0;
+    g.short_sums = short_sums; g.work = static_cast<uint8_t*>(d_work);
+    hipError_t e = gd_launch_packed_product(g, static_cast<hipStream_t>(stream));
+    if (e != hipSuccess) return hip_fail(h, e, call);
+    return GD_OK;
+}
+
 // What is wrong with the matrices of an update, or null.
 const char* bad_matrices(const gd_muon_tensor* list, uint32_t n) {
     if (n && !list) return "null list of tensors";
@@ -830,29 +857,12 @@ size_t gd_packed_product_work_bytes(uint64_t n, uint64_t m, uint64_t k) {
 
 gd_status gd_packed_product(gd_handle h, const gd_packed* a, const gd_packed* b, const gd_matrix* out, int32_t accumulate,
                             void* d_work, size_t work_bytes, void* stream) {
-    if (!h) return GD_ERR_INVALID_ARG;
-    const char* call = "gd_packed_product";
-    if (!a || !b) return invalid(h, call, "null packed matrix");
-    if (!out) return invalid(h, call, "null matrix");
-    const uint64_t n = a->codes.rows, m = b->codes.rows, k = a->codes.cols;
-    if (n > GD_MAX_TOKENS || m > MAX_STRIDE || k > MAX_INNER) return invalid(h, call, "more than 2^24 rows, 2^22 columns or 2^22 of k");
-    if (!is_float(out->dtype)) return fail(h, GD_ERR_UNSUPPORTED, "gd_packed_product: out must be f32, bf16 or f16");
-    if (const char* e = bad_packed(a, n, k)) return invalid(h, call, e);
-    if (const char* e = bad_packed(b, m, k)) return invalid(h, call, e);
-    if (const char* e = bad_matrix(out, n, m)) return invalid(h, call, e);
-    if (n == 0 || m == 0) return GD_OK;
-    if (((n + 127) / 128) * ((m + 127) / 128) >= 1u << 24)                  // (a launch has fewer than 2^32 threads)
-        return fail(h, GD_ERR_UNSUPPORTED, "gd_packed_product: 2^38 results or more in one call are not built");
-    if (gd_status st = bad_work(h, call, d_work, work_bytes, gd_packed_product_work(n, m, k))) return st;
-    gd_packed_product_args g = {};
-    g.a = a->codes.d_data; g.a_stride = a->codes.stride; g.a_exp = static_cast<const uint8_t*>(a->exp.d_data); g.a_exp_stride = a->exp.stride;
-    g.b = b->codes.d_data; g.b_stride = b->codes.stride; g.b_exp = static_cast<const uint8_t*>(b->exp.d_data); g.b_exp_stride = b->exp.stride;
-    g.n = (uint32_t)n; g.m = (uint32_t)m; g.k = (uint32_t)k; g.a_codes = a->codes.dtype; g.b_codes = b->codes.dtype;
-    g.out = out->d_data; g.out_stride = out->stride; g.out_type = out->dtype; g.accumulate = accumulate != 0;
-    g.work = static_cast<uint8_t*>(d_work);
-    hipError_t e = gd_launch_packed_product(g, static_cast<hipStream_t>(stream));
-    if (e != hipSuccess) return hip_fail(h, e, call);
-    return GD_OK;
+    return packed_product(h, "gd_packed_product", a, b, out, accumulate, false, d_work, work_bytes, stream);
+}
+
+gd_status gd_packed_product_short(gd_handle h, const gd_packed* a, const gd_packed* b, const gd_matrix* out, int32_t accumulate,
+                                  void* d_work, size_t work_bytes, void* stream) {
+    return packed_product(h, "gd_packed_product_short", a, b, out, accumulate, true, d_work, work_bytes, stream);
 }
 
 size_t gd_muon_table_bytes(gd_handle h, const gd_muon_tensor* tensors, uint32_t n_tensors) {

@@ -85,6 +85,7 @@ struct gd_packed_product_args {
     uint32_t n, m, k, a_codes, b_codes;
     void* out;  uint64_t out_stride;
     uint32_t out_type, accumulate;
+    uint32_t short_sums;           // by the 8-bit matrix cores; an out of 16 bits
     uint8_t* work;
 };
 

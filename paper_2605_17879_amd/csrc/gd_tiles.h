@@ -143,7 +143,7 @@ __device__ __forceinline__ bf16x8 numbers_of(uint32_t lo, uint32_t hi, float two
 // NaN for 255, of any code.
 __device__ __forceinline__ float power_of(uint32_t e) { return __builtin_bit_cast(float, e == 255 ? 0x7FC00000u : e << 23); }
 
-// The same products by the 16-bit matrix cores, whose sums are of fp32.
+// The same products by the 16-bit matrix cores, with sums of fp32.
 template <int P_CODES, int Q_CODES>
 struct of_codes_in_16 {
     static constexpr bool SCALED = true;

@@ -3,14 +3,14 @@
 //
 //   C_ij = sum over blocks b of 2^(ea_bi - 127 + eb_bj - 127) sum over the block's k of a_ik b_jk
 //
-// A C of 16 bits comes from the scaled 8-bit instruction of the matrix cores, which takes 128 of k at a time with their powers
-// of two, so that a block costs what a plain 8-bit product costs.  That instruction's own sums are short: the products of eight k are cut at 2^-13 of
-// the largest (gd_tiles.h has the rule).  They are taken all the same where C has 16 bits, for twice the rate (8 192 x 8 192 x 8 192 400 us,
-// 800 by the 16-bit cores): in the norm the cut costs 1.5e-5 to 9e-5, C's own rounding 1.7e-3 in bf16 and 2.1e-4 in f16.  At its worst, seven small products
-// beside a large one, it is 8.0e-4 of that product, below half a step of bf16 (3.9e-3) but not of f16 (4.9e-4), and where large products cancel
-// nothing of a small result may be left: the header says so, and that a C of fp32 has sums of fp32.  Such a C is computed by the 16-bit matrix
-// cores, for which codes times powers of two are exact, at half the rate: the operands are written out in bf16 first, or
-// converted in registers where tiles are read straight into them.
+// Sums are of fp32: by the 16-bit matrix cores, for which codes times powers of two are exact numbers of bf16.  The operands are written out as
+// such first, or converted in registers where tiles are read straight into them.
+//
+// For a C of 16 bits the caller can ask for the scaled 8-bit instruction instead, which takes 128 of k at a time with their powers
+// of two, so that a block costs what a plain 8-bit product costs, at twice the rate (8 192 x 8 192 x 8 192 400 us, 800 by the 16-bit cores).  Its own sums are short: the
+// products of eight k are cut at 2^-13 of the largest (gd_tiles.h has the rule).  In the norm that costs 1.5e-5 to 9e-5, C's own rounding 1.7e-3 in
+// bf16 and 2.1e-4 in f16; at its worst, seven small products beside a large one, 8.0e-4 of that product (half a step of bf16 is 3.9e-3, of
+// f16 4.9e-4), and where large products cancel nothing of a small result may be left.
 //
 // Rows of B are the operand P (columns of C, which a lane holds sixteen of next to each other), rows of A the operand Q.
 #include <algorithm>
@@ -28,7 +28,7 @@ struct product_args {
     uint32_t tiles_p, tiles_q;
     uint32_t parts;                // of tiles of 256 x 256: the launch takes quarters of these, from this one on, plus 1; 0: its own tiles
     void* c;  uint64_t ldc;        // elements
-    uint32_t add;
+    uint32_t add, type;            // type: of C, where the kernel is of any_type
     float* slab;                   // splits: [split][n][m4]; null: one split
     uint32_t m4, each;             // columns of a slab; blocks of k of a split
 };
@@ -65,6 +65,19 @@ __device__ __forceinline__ void write_row(const product_args& a, uint32_t row, u
     }
 }
 
+// A kernel of any_type asks what C is when its sums are ready (sixteen kernels of direct tiles instead of 48).
+struct any_type {};
+template <typename T> struct type_is {
+    typedef T type;
+};
+template <typename T, typename F>
+__device__ __forceinline__ void with_type(const product_args& a, F&& f) {
+    if constexpr (!std::is_same<T, any_type>::value) f(type_is<T>{});
+    else if (a.type == GD_F32) f(type_is<float>{});
+    else if (a.type == GD_BF16) f(type_is<gd_bf16>{});
+    else f(type_is<gd_f16>{});
+}
+
 template <typename MUL, typename T, template <typename> class TILE>
 __global__ __launch_bounds__(TILE<MUL>::NT, 512 / TILE<MUL>::NT) void tiled_kernel(const product_args a) {
     typedef TILE<MUL> tile;
@@ -80,13 +93,16 @@ __global__ __launch_bounds__(TILE<MUL>::NT, 512 / TILE<MUL>::NT) void tiled_kern
     f32x4 acc[tile::FP][tile::FQ] = {};
     tile::run(a.p, a.q, tp * tile::BP, tq * tile::BQ, a.way, acc);
     const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    with_type<T>(a, [&](auto of) {
 #pragma unroll
-    for (int j = 0; j < tile::FQ; ++j)
+        for (int j = 0; j < tile::FQ; ++j)
 #pragma unroll
-        for (int g = 0; g < tile::FP / 4; ++g) {
-            const f32x4 v[4] = {acc[4 * g][j], acc[4 * g + 1][j], acc[4 * g + 2][j], acc[4 * g + 3][j]};
-            write_row<T>(a, tq * tile::BQ + tile::q_of(wave) + 4 * (lane & 15) + j, tp * tile::BP + tile::p_of(wave, g) + 16 * (lane >> 4), v, 4, lane);
-        }
+            for (int g = 0; g < tile::FP / 4; ++g) {
+                const f32x4 v[4] = {acc[4 * g][j], acc[4 * g + 1][j], acc[4 * g + 2][j], acc[4 * g + 3][j]};
+                write_row<typename decltype(of)::type>(a, tq * tile::BQ + tile::q_of(wave) + 4 * (lane & 15) + j,
+                                                       tp * tile::BP + tile::p_of(wave, g) + 16 * (lane >> 4), v, 4, lane);
+            }
+    });
 }
 
 template <typename MUL, typename T, int FQ, int WAVES>
@@ -100,7 +116,7 @@ __global__ __launch_bounds__(64 * WAVES, 8 / WAVES) void direct_kernel(const pro
     if (wave >= FQ) return;
     const uint32_t row = tq * tile::BQ + FQ * (lane & 15) + wave, col = tp * tile::BP + 16 * (lane >> 4);
     if (!a.slab) {
-        write_row<T>(a, row, col, v, FQ, lane);
+        with_type<T>(a, [&](auto of) { write_row<typename decltype(of)::type>(a, row, col, v, FQ, lane); });
     } else if (row < a.n && col < a.m4) {
         float* to = a.slab + (split * (uint64_t)a.n + row) * a.m4 + col;
 #pragma unroll
@@ -176,12 +192,12 @@ struct plan {
 
 uint32_t up(uint64_t a, uint64_t b) { return (uint32_t)((a + b - 1) / b); }
 
-// For 16 bits tiles of 64 x 64 and smaller up to 768 of them (2 000 x 1 500 x 1 000, 768: 12.1 us, tiles of 128 x 128 12.7, of 256 x 256 22.2;
+// For the 8-bit cores tiles of 64 x 64 and smaller up to 768 of them (2 000 x 1 500 x 1 000, 768: 12.1 us, tiles of 128 x 128 12.7, of 256 x 256 22.2;
 // 2 048 x 2 048 x 2 048, 1 024: 20.3, 16.0, 27.7), then of 256 x 256 from where they fill more than half of the chip (3 000 x 3 000 x 3 000, 144 of
-// them: 44 us, 50 with 128 x 128; 2 048 x 4 096 x 4 096, 128: 52 and 40).  For fp32, where larger tiles need their operands written out in
+// them: 44 us, 50 with 128 x 128; 2 048 x 4 096 x 4 096, 128: 52 and 40).  For the 16-bit ones, where larger tiles need their operands written out in
 // bf16 first, of 64 x 64 up to there (1 024 x 4 096 x 4 096, 1 024: 42 us, 65, 98; 2 500 x 2 500 x 1 000, 1 600: 27, 34, 42; 3 000 x 3 000 x 3 000: 84,
 // 90, 80).
-plan plan_of(uint64_t n, uint64_t m, uint64_t k, bool f32) {
+plan plan_of(uint64_t n, uint64_t m, uint64_t k, bool in_16) {
     const uint64_t blocks = up(k, BYTES);
     plan w{plan::DIRECT, n <= 16 ? 1u : n <= 32 ? 2u : 4u, 1, (uint32_t)blocks};
     // (narrower where there is room for them, but of more than 64 rows, as every band of rows reads B: 700 x 700 x 4 000 in two splits 14.8 us,
@@ -189,7 +205,7 @@ plan plan_of(uint64_t n, uint64_t m, uint64_t k, bool f32) {
     while (n > 64 && w.fq > 1 && (uint64_t)up(n, 16 * w.fq / 2) * up(m, 64) <= 256) w.fq /= 2;
     const uint64_t tiles = (uint64_t)up(n, 16 * w.fq) * up(m, 64);
     const bool large = (uint64_t)up(n, 256) * up(m, 256) >= 140;
-    if (n > 64 && tiles > 768 && (large || !f32)) {
+    if (n > 64 && tiles > 768 && (large || !in_16)) {
         w.kind = large ? plan::LARGE : plan::SMALL;
         return w;
     }
@@ -203,9 +219,9 @@ plan plan_of(uint64_t n, uint64_t m, uint64_t k, bool f32) {
 
 // Of the splits' sums, or of the operands in bf16.
 uint64_t row_of_numbers(uint64_t k) { return (k + 63) / 64 * 128; }
-uint64_t work_bytes(uint64_t n, uint64_t m, uint64_t k, bool f32) {
-    const plan w = plan_of(n, m, k, f32);
-    return w.kind != plan::DIRECT ? (f32 ? (n + m) * row_of_numbers(k) : 0) : w.splits > 1 ? w.splits * n * gd_align256(m * 4) : 0;
+uint64_t work_bytes(uint64_t n, uint64_t m, uint64_t k, bool in_16) {
+    const plan w = plan_of(n, m, k, in_16);
+    return w.kind != plan::DIRECT ? (in_16 ? (n + m) * row_of_numbers(k) : 0) : w.splits > 1 ? w.splits * n * gd_align256(m * 4) : 0;
 }
 
 template <typename MUL, typename T>
@@ -242,20 +258,27 @@ hipError_t launch_direct(product_args& a, const plan& w, hipStream_t s) {
     else if (a.tiles_p * a.tiles_q <= 256) direct_kernel<MUL, T, 4, 8><<<grid, 512, 0, s>>>(a);
     else direct_kernel<MUL, T, 4, 4><<<grid, 256, 0, s>>>(a);
     if (hipError_t e = hipGetLastError()) return e;
-    if (w.splits > 1) join_kernel<T><<<up((uint64_t)a.n * (a.m4 / 4), 256), 256, 0, s>>>(a, w.splits);
+    if (w.splits > 1) {
+        const uint32_t groups = up((uint64_t)a.n * (a.m4 / 4), 256);
+        if (a.type == GD_F32) join_kernel<float><<<groups, 256, 0, s>>>(a, w.splits);
+        else if (a.type == GD_BF16) join_kernel<gd_bf16><<<groups, 256, 0, s>>>(a, w.splits);
+        else join_kernel<gd_f16><<<groups, 256, 0, s>>>(a, w.splits);
+    }
     return hipGetLastError();
 }
 
 // P_CODES, Q_CODES: 1 for e5m2.
 template <int P_CODES, int Q_CODES>
 hipError_t launch(product_args& a, const plan& w, const gd_packed_product_args& g, hipStream_t s) {
-    if (w.kind == plan::DIRECT) {
-        if (g.out_type == GD_F32) return launch_direct<of_codes_in_16<P_CODES, Q_CODES>, float>(a, w, s);
-        if (g.out_type == GD_BF16) return launch_direct<of_codes<P_CODES, Q_CODES>, gd_bf16>(a, w, s);
-        return launch_direct<of_codes<P_CODES, Q_CODES>, gd_f16>(a, w, s);
+    if (g.short_sums) {
+        if (w.kind == plan::DIRECT) {
+            if (g.out_type == GD_BF16) return launch_direct<of_codes<P_CODES, Q_CODES>, gd_bf16>(a, w, s);
+            return launch_direct<of_codes<P_CODES, Q_CODES>, gd_f16>(a, w, s);
+        }
+        if (g.out_type == GD_BF16) return launch_tiles<of_codes<P_CODES, Q_CODES>, gd_bf16>(a, w, s);
+        return launch_tiles<of_codes<P_CODES, Q_CODES>, gd_f16>(a, w, s);
     }
-    if (g.out_type == GD_BF16) return launch_tiles<of_codes<P_CODES, Q_CODES>, gd_bf16>(a, w, s);
-    if (g.out_type == GD_F16) return launch_tiles<of_codes<P_CODES, Q_CODES>, gd_f16>(a, w, s);
+    if (w.kind == plan::DIRECT) return launch_direct<of_codes_in_16<P_CODES, Q_CODES>, any_type>(a, w, s);
     const uint64_t pitch = row_of_numbers(g.k);
     const uint32_t pieces = (uint32_t)(pitch / 32);
     numbers_args x[2];
@@ -269,7 +292,7 @@ hipError_t launch(product_args& a, const plan& w, const gd_packed_product_args& 
     if (hipError_t e = hipGetLastError()) return e;
     a.way.blocks = (uint32_t)(pitch / BYTES);
     a.way.ends = 0;
-    return launch_tiles<of_bf16, float>(a, w, s);
+    return launch_tiles<of_bf16, any_type>(a, w, s);
 }
 
 }  // namespace
@@ -281,7 +304,7 @@ size_t gd_packed_product_work(uint64_t n, uint64_t m, uint64_t k) {
 hipError_t gd_launch_packed_product(const gd_packed_product_args& g, hipStream_t s) {
     product_args a = {};
     a.n = g.n; a.m = g.m;
-    a.c = g.out; a.ldc = g.out_stride; a.add = g.accumulate;
+    a.c = g.out; a.ldc = g.out_stride; a.add = g.accumulate; a.type = g.out_type;
     if (g.k == 0) {
         if (g.accumulate) return hipSuccess;
         const uint32_t grid = std::min<uint32_t>(g.n, 65536);
@@ -296,7 +319,7 @@ hipError_t gd_launch_packed_product(const gd_packed_product_args& g, hipStream_t
     a.way.blocks = up(g.k, BYTES); a.way.ends = g.k % BYTES;
     a.slab = reinterpret_cast<float*>(g.work);
     a.m4 = (uint32_t)(gd_align256(g.m * 4ull) / 4);
-    const plan w = plan_of(g.n, g.m, g.k, g.out_type == GD_F32);
+    const plan w = plan_of(g.n, g.m, g.k, !g.short_sums);
     if (g.a_codes == GD_E4M3) return g.b_codes == GD_E4M3 ? launch<0, 0>(a, w, g, s) : launch<1, 0>(a, w, g, s);
     return g.b_codes == GD_E4M3 ? launch<0, 1>(a, w, g, s) : launch<1, 1>(a, w, g, s);
 }

@@ -30,7 +30,7 @@ EXPORTS = ("gd_default_config", "gd_create", "gd_destroy", "gd_state_bytes", "gd
            "gd_update_ledger_static", "gd_ledger_static_scratch_bytes",
            "gd_embed", "gd_embed_grad", "gd_embed_grad_work_bytes", "gd_vocab_loss", "gd_vocab_loss_grad",
            "gd_vocab_loss_work_bytes", "gd_adamw", "gd_adamw_table_bytes", "gd_adamw_fill_table",
-           "gd_pack", "gd_packed_product", "gd_packed_product_work_bytes",
+           "gd_pack", "gd_packed_product", "gd_packed_product_short", "gd_packed_product_work_bytes",
            "gd_muon", "gd_muon_table_bytes", "gd_muon_fill_table", "gd_muon_work_bytes")
 
 F32, BF16, F16, I32, I64, E4M3, E5M2, U8 = range(8)      # gd_dtype
@@ -184,8 +184,9 @@ def load_library() -> ctypes.CDLL:
     lib.gd_pack.restype = ctypes.c_int
     lib.gd_packed_product_work_bytes.argtypes = [u64, u64, u64]
     lib.gd_packed_product_work_bytes.restype = sz
-    lib.gd_packed_product.argtypes = [vp, packed, packed, mat, i32, vp, sz, vp]
-    lib.gd_packed_product.restype = ctypes.c_int
+    for product in (lib.gd_packed_product, lib.gd_packed_product_short):
+        product.argtypes = [vp, packed, packed, mat, i32, vp, sz, vp]
+        product.restype = ctypes.c_int
     lib.gd_muon_table_bytes.argtypes = [vp, ctypes.POINTER(_CMuonTensor), u32]
     lib.gd_muon_table_bytes.restype = sz
     lib.gd_muon_fill_table.argtypes = [vp, ctypes.POINTER(_CMuonTensor), u32, vp, sz]
@@ -274,7 +275,8 @@ class Detector:
         self._vocab_loss_grad = self._entry("gd_vocab_loss_grad", vp, vp, vp, vp, f32, *[vp] * 7, sz, vp)
         self._adamw = self._entry("gd_adamw", vp, vp, sz, vp, vp, vp)
         self._pack = self._entry("gd_pack", vp, vp, ctypes.c_int32, vp, vp, vp)
-        self._packed_product = self._entry("gd_packed_product", vp, vp, vp, vp, ctypes.c_int32, vp, sz, vp)
+        self._packed_products = {sums: self._entry(name, vp, vp, vp, vp, ctypes.c_int32, vp, sz, vp)
+                                 for sums, name in (("f32", "gd_packed_product"), ("short", "gd_packed_product_short"))}
         self._muon = self._entry("gd_muon", vp, vp, vp, sz, vp, vp, vp, sz, vp)
         self._codes = {torch.float8_e4m3fn: E4M3, torch.float8_e5m2: E5M2}
         self._types = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16, torch.int32: I32, torch.int64: I64}
@@ -670,11 +672,11 @@ class Detector:
     def alloc_packed_product_work(self, n: int, m: int, k: int):
         return self._bytes(self.packed_product_work_bytes(n, m, k))
 
-    def packed_product(self, a: dict, b: dict, out, work, accumulate: bool = False, stream=None):
-        """out[n][m] = (its old value, with accumulate) + a b^T of packed a[n][k] and b[m][k].  An out of fp32 has sums of fp32; of 16
-        bits those of the 8-bit matrix cores, which cut products 2^-13 below the largest of eight neighbours (include/guard.h)."""
-        self._check(self._packed_product(self.h, self._packed(a), self._packed(b), self._matrix(out), accumulate,
-                                         self._at(work), work.nbytes, self._stream(stream)))
+    def packed_product(self, a: dict, b: dict, out, work, accumulate: bool = False, stream=None, sums: str = "f32"):
+        """out[n][m] = (its old value, with accumulate) + a b^T of packed a[n][k] and b[m][k].  sums: "f32", or "short" for an
+        out of 16 bits by the 8-bit matrix cores, which cut products 2^-13 below the largest of eight neighbours."""
+        self._check(self._packed_products[sums](self.h, self._packed(a), self._packed(b), self._matrix(out), accumulate,
+                                                self._at(work), work.nbytes, self._stream(stream)))
 
     # ---- updates of matrices --------------------------------------------------------------
     def alloc_muon_state(self, params) -> list:

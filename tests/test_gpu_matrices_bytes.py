@@ -1,5 +1,5 @@
 """Packed matrices that were not made by gd_pack: a power of two of byte 0 is 2^-127 whatever its codes are, one of 255 makes
-NaN of codes that are none, and what lies beyond fp32 is infinite where the result is fp32."""
+NaN of codes that are none, and what lies beyond fp32 is infinite."""
 import pytest
 import torch
 
@@ -68,11 +68,11 @@ def test_a_power_of_two_that_is_none(det, n, m, k, dtype):
 
 @pytest.mark.parametrize("n,m,k", SIZES)
 def test_elements_beyond_fp32(det, n, m, k):
-    """448 * 2^127 times 2^-20: infinite where the operands are numbers of fp32's range, 448 * 2^107 where codes and powers of two are multiplied."""
+    """448 * 2^127 times 2^-20."""
     a, b = coded(torch.zeros(n, k), "e4m3", 254), coded(torch.zeros(m, k), "e4m3", 127 - 20)
     a["codes"].view(torch.uint8)[1, 5] = torch.tensor(448.0).to(refs.CODES["e4m3"]).view(torch.uint8)
     b["codes"].view(torch.uint8)[:, 5] = torch.tensor(1.0).to(refs.CODES["e4m3"]).view(torch.uint8)
-    for dtype, want in ((F32, float("inf")), (BF16, 448 * 2.0 ** 107)):
+    for dtype in (F32, BF16, F16):
         out = torch.empty((n, m), dtype=dtype, device="cuda")
         det.packed_product(a, b, out, det.alloc_packed_product_work(n, m, k))
-        assert bool((out[1] == want).all()) and bool((out[0] == 0).all()), dtype
+        assert bool((out[1] == float("inf")).all()) and bool((out[0] == 0).all()), dtype

@@ -56,3 +56,13 @@ def test_columns_of_a_result(lib, h):  # noqa: F811
     for n, m in ((1, 2 ** 22), (2 ** 24, 8)):                  # (refused for the result's address alone)
         assert lib.gd_packed_product(h, pk(n, 64), pk(m, 64), mat(n, m, F32, at=AT + 1), 0, AT, ctypes.c_size_t(1 << 40), None) == INVALID
         assert lib.gd_last_error(h) == b"gd_packed_product: pointer of a matrix not aligned to its element"
+
+
+def test_short_sums_refuse_what_products_do_and_results_of_fp32(lib, h):  # noqa: F811
+    work = ctypes.c_size_t(1 << 40)
+    for args, status in (((None, pk(20, 64), mat(10, 20), 0, AT, work), INVALID), ((pk(10, 64), pk(20, 65), mat(10, 20), 0, AT, work), INVALID),
+                         ((pk(10, 64), pk(20, 64), mat(10, 20, F32), 0, AT, work), 4), ((pk(10, 64), pk(20, 64), mat(10, 21), 0, AT, work), INVALID),
+                         ((pk(2, 20_000), pk(64, 20_000), mat(2, 64), 0, AT, ctypes.c_size_t(16)), 3)):
+        assert lib.gd_packed_product_short(h, *args, None) == status
+        assert lib.gd_last_error(h).startswith(b"gd_packed_product_short: ")
+    assert lib.gd_packed_product_short(None, pk(10, 64), pk(20, 64), mat(10, 20), 0, AT, work, None) == INVALID
