@@ -336,9 +336,9 @@ __device__ __forceinline__ fragment read_fragment(const uint8_t* s, uint32_t row
 // What is read in turns 4 t and on was issued before the latest loads of one block; the wait stands before the barrier in
 // front of the even turns, which g0 reaches multiplying and g1 reading.
 //
-// The matrix cores bound it, and their clock, which falls under this load: 8 192 x 8 192 x 8 192 of codes 400 us, 2 750 TFLOP/s (the
-// library's plain 8-bit product 2 840 to 3 040, the instruction alone 3 200), of bf16 with its operands' writing 810.  A tile's ends, first loads
-// and C, are some 8 us, during which the matrix cores rest: 8 192 x 8 192 x 1 024 of codes 77 us, 1 780 TFLOP/s.
+// The matrix cores bound it, and their clock, which falls under this load: 8 192 x 8 192 x 8 192 of codes 404 to 435 us, 2 530 to 2 720 TFLOP/s (the
+// library's plain 8-bit product 2 840 to 3 040, the instruction alone 3 200), of bf16 700 to 855, 1 290 to 1 570 (library 1 580).  A tile's ends, first
+// loads and C, are some 8 us, during which the matrix cores rest: 8 192 x 8 192 x 1 024 of codes 77 to 84 us, 1 640 to 1 780 TFLOP/s.
 template <typename MUL>
 struct large_tile {
     static constexpr int BP = 256, BQ = 256, WP = 2, WQ = 4, NT = 512, FP = 8, FQ = 4;

@@ -642,8 +642,9 @@ __global__ __launch_bounds__(256) void apply_kernel(const muon_args g) {
 
 // A matrix of up to 64 x 192 (or 192 x 64), momentum to parameters: X as a lane holds it, in fp32, in registers, and as
 // operands in the LDS, hi and lo, both ways (R [i][j], C [j][i], i along the shorter side), A and B [i][i'].  A wave has pieces of 16 x 16 of a product: a
-// lane four neighbouring j of one i of X.  Five steps take 13 products one behind the other of some hundred cycles each; with the launches of
-// the larger matrices they took 6 to 8 us each (six of 96 x 64: 105 us, so 24).
+// lane four neighbouring j of one i of X.  Five steps are 15 products one behind the other, which with the launches of
+// the larger matrices took 6 to 8 us each (six of 96 x 64: 105 us, so 24).  By their count the matrix instructions are some 3 us of that; how the
+// rest falls on the reads, the writes and the four barriers of a step has not been measured.
 struct tiny_lds {
     static constexpr uint32_t R = 2 * 2 * TINY_B, C = 2 * 2 * TINY_A, S = C;   // bytes of a row: hi, lo
     uint8_t r[TINY_A * R], c[TINY_B * C];

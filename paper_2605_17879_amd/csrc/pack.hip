@@ -10,7 +10,7 @@
 // The memory's streams bound it.  A workgroup takes 128 x 128: a lane 4 rows of 8 columns, which lie next to each other along
 // both, in registers from the one read to the codes; the row's largest comes from 16 lanes by exchange, the column's
 // through the LDS, as do the transposed codes, which are written 16 bytes a lane.  16 384 x 4 096 of bf16 both ways, 271 MB: 50 us, 5.4 TB/s;
-// 5 003 x 3 001 of fp32, whose rows begin anywhere, squares: 17 to 19 us, 3.9 to 4.4 TB/s.  Where there are few of them it is how long one workgroup takes,
+// 5 003 x 3 001 of fp32, whose rows begin anywhere, in squares both ways, 90 MB: 17 to 20 us, 4.5 to 5.3 TB/s.  Where there are few of them it is how long one workgroup takes,
 // most of that its code's way from memory: 128 x 128 both ways 4.4 us, 6.0 with twice the rows a lane; 1 000 x 1 500 6.2, 8.0, and 10.2 where
 // the last numbers of a row were read and written one by one.
 #include <type_traits>
