@@ -264,6 +264,7 @@ class Detector:
         self.h = h
         self.device = torch.device(device)
         self._raw_stream = torch._C._cuda_getCurrentRawStream
+        self._current = torch._C._cuda_getDevice
         self._index = self.device.index
         self._f32 = torch.float32
         self._u8 = torch.uint8
@@ -308,12 +309,17 @@ class Detector:
             raise GuardError(st, (self.lib.gd_last_error(self.h) or b"").decode())
 
     def _stream(self, stream) -> int:
-        if stream is not None:
-            return stream.cuda_stream
         # The current stream's handle alone: building the Stream object around it took longer
         # than the rest of a call's marshalling, and a small job's calls are bound by that.
-        index = self.device.index
-        return self._raw_stream(self._torch.cuda.current_device() if index is None else index)
+        index = self._index
+        if stream is not None:
+            handle = stream.cuda_stream
+        else:
+            handle = self._raw_stream(self._torch.cuda.current_device() if index is None else index)
+        # (the default stream's handle, 0, is that of whichever device is current)
+        if handle == 0 and index is not None and self._current() != index:
+            raise GuardError(1, f"the default stream of cuda:{index} cannot be used while cuda:{self._current()} is the current device")
+        return handle
 
     # ---- the C ABI, one method per entry point --------------------------------
     def state_bytes(self) -> int:
